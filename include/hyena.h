@@ -382,6 +382,55 @@ hy_status hyena_mr_bwd_shard(const void *dy, const void *q, const void *k, const
 int64_t hyena_bwd_shard_workspace_bytes(int64_t B, int64_t L, int64_t D, int32_t lh, int32_t group, int32_t dtype);
 
 /*
+ * Gated linear recurrence, forward: the gates of Eq. 1 (u = k (.) v in front, q behind) around a memory whose decay is data
+ * instead of a filter,
+ *     s[b,t,c] = a[b,t,c] * s[b,t-1,c] + k[b,t,c] * v[b,t,c],   a[b,t,c] = exp(g[b,t,c / group]),
+ *     y[b,t,c] = q[b,t,c] * s[b,t,c],
+ * with s[b,-1,c] = state_in[b,c] (NULL: zero).  g is the logarithm of the decay: decays close to 1 keep their precision in
+ * bfloat16 that way, and g = -infinity forgets everything before its step (the first step of a document in a packed
+ * sequence; every gradient through it is zero).  g > 0 grows and overflows as the definition does.
+ * q, k, v, y: [B,L,D], g: [B,L,D/group], of `dtype`; state_in, state_out: fp32 [B,D], the state after the last step
+ * (NULL: not wanted; an empty sequence hands state_in on).  The state, the decays and every sum are fp32, y is rounded
+ * once.
+ * marks (NULL: not wanted): fp32 [B, ceil(L / HYENA_GLR_MARK_ROWS), D], the states before steps 0, 64, 128, ..., which spare
+ * hyena_glr_bwd a pass over k, v and g.
+ * strides: NULL where q, k, v, g are dense, else host memory with the distances, in elements, between batch items and between
+ * steps of each: {q_batch, q_step, k_batch, k_step, v_batch, v_step, g_batch, g_step} (channels are contiguous; 0 repeats
+ * a row; negative: HY_ERR_SHAPE).  Outputs are dense.  q, k, v, g may begin at any element, every other
+ * pointer is 16-byte aligned; where a size is zero the pointers to what is empty may be NULL.
+ * workspace: hyena_glr_fwd_workspace_bytes(...) bytes, disjoint from every argument, contents undefined afterwards.
+ */
+#define HYENA_GLR_MARK_ROWS 64
+hy_status hyena_glr_fwd(const void *q, const void *k, const void *v, const void *g, const float *state_in, void *y,
+                        float *state_out, float *marks, const int64_t *strides, void *workspace,
+                        int64_t workspace_bytes, int64_t B, int64_t L, int64_t D, int32_t group, int32_t dtype,
+                        void *hip_stream);
+int64_t hyena_glr_fwd_workspace_bytes(int64_t B, int64_t L, int64_t D, int32_t group, int32_t dtype);
+
+/*
+ * Backward of hyena_glr_fwd.  With dy = dLoss/dy, dstate_out = dLoss/d state_out (NULL: zero) and
+ *     m[b,t,c] = q[b,t,c] * dy[b,t,c] + a[b,t+1,c] * m[b,t+1,c]       (+ dstate_out[b,c] at the last step):
+ *     dq = dy (.) s,   dk = m (.) v,   dv = m (.) k,   dg[b,t,n] = sum over c in group n of m[b,t,c] * a[b,t,c] * s[b,t-1,c],
+ *     dstate_in[b,c] = a[b,0,c] * m[b,0,c]                            (NULL: not wanted)
+ * dq, dk, dv: dense [B,L,D], dg: dense [B,L,D/group], of `dtype`; fp32 inside, one rounding per stored element, sums in a
+ * fixed order.  marks: what the forward call wrote, or NULL: the states are computed again, from state_in (which is not
+ * looked at otherwise).  strides: as there, with dy in front: {dy_batch, dy_step, q_batch, ...}.
+ * workspace: hyena_glr_bwd_workspace_bytes(..., marks given or not) bytes.
+ */
+hy_status hyena_glr_bwd(const void *dy, const void *q, const void *k, const void *v, const void *g, const float *marks,
+                        const float *state_in, const float *dstate_out, void *dq, void *dk, void *dv, void *dg,
+                        float *dstate_in, const int64_t *strides, void *workspace, int64_t workspace_bytes, int64_t B,
+                        int64_t L, int64_t D, int32_t group, int32_t dtype, void *hip_stream);
+int64_t hyena_glr_bwd_workspace_bytes(int64_t B, int64_t L, int64_t D, int32_t group, int32_t dtype, int32_t with_marks);
+
+/*
+ * One step of hyena_glr_fwd for B sequences, in place on their states: state = exp(g) * state + k (.) v, y = q (.) state.
+ * q, k, v, y: dense [B,D], g: dense [B,D/group], of `dtype`; state: fp32 [B,D].
+ */
+hy_status hyena_glr_step(const void *q, const void *k, const void *v, const void *g, float *state, void *y, int64_t B,
+                         int64_t D, int32_t group, int32_t dtype, void *hip_stream);
+
+/*
  * Plain device-to-device streaming copy of `bytes` bytes (a multiple of 16) with the same launch
  * shape as the streaming kernels.  Used to measure the practical HBM ceiling and to calibrate
  * hardware byte counters; not part of the operator.

@@ -90,6 +90,9 @@ def lib() -> ctypes.CDLL:
         L.hyena_status_string.restype = ctypes.c_char_p
         L.hyena_version.argtypes = []
         L.hyena_version.restype = i32
+        from . import model_ops
+
+        model_ops.declare(L)
         _lib = L
         _load_fast()
     return _lib

@@ -268,6 +268,30 @@ hy_status launch_bwd_zero_dh(float* dh, int64_t D, int32_t lh, int32_t group, hi
 hy_status launch_stream_gate(const void* q, const void* k, const void* v, void* y, int64_t B, int64_t L, int64_t D,
                              int32_t strip, int64_t rows, int32_t depth, int32_t waves, hipStream_t st);
 
+// Gated linear recurrence.  Strides in elements, per input tensor in the order of the kGlr constants; outputs are dense.
+constexpr int kGlrRows = HYENA_GLR_MARK_ROWS;  // steps per tile
+constexpr int kGlrQ = 0, kGlrK = 1, kGlrV = 2, kGlrG = 3, kGlrDy = 4;
+struct GlrPtrs {
+    const void *q = nullptr, *k = nullptr, *v = nullptr, *g = nullptr, *dy = nullptr;
+    const float *state_in = nullptr, *dstate_out = nullptr;
+    const float* marks = nullptr;  // backward: the states before the tiles, if the caller has them
+    void *y = nullptr, *dq = nullptr, *dk = nullptr, *dv = nullptr, *dg = nullptr;
+    float *state_out = nullptr, *marks_out = nullptr, *dstate_in = nullptr;
+};
+struct GlrShape {
+    int64_t B, L, D;
+    int32_t group;
+    hy_dtype dtype;
+    int64_t bstride[5], rstride[5];
+    bool odd_start = false;  // an input begins where no two elements may be loaded together
+};
+int64_t glr_fwd_workspace_bytes(const GlrShape& s);
+int64_t glr_bwd_workspace_bytes(const GlrShape& s, bool marks);
+hy_status launch_glr_fwd(const GlrPtrs& p, const GlrShape& s, void* ws, hipStream_t st);
+hy_status launch_glr_bwd(const GlrPtrs& p, const GlrShape& s, void* ws, hipStream_t st);
+// One step of B sequences, the states (p.state_out) updated in place; D dense, L not looked at.
+hy_status launch_glr_step(const GlrPtrs& p, const GlrShape& s, hipStream_t st);
+
 // Launches `kernel` and returns the status of THIS launch as hipLaunchKernel reports it.  The thread's sticky
 // "last error" is neither read nor cleared: an error left behind by an earlier, unrelated HIP call of the caller
 // cannot make a healthy launch look failed, and stays there for the caller to find.

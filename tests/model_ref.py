@@ -1,0 +1,30 @@
+"""The operators around the mixers in 64 bits, written out step by step (numpy)."""
+import numpy as np
+
+
+def glr(q, k, v, g, group=1, state=None):
+    """(y, state after the last step, states after every step)."""
+    B, L, D = q.shape
+    a = np.exp(np.repeat(g, group, axis=2))
+    s = np.zeros((B, D)) if state is None else state.astype(np.float64).copy()
+    every = np.empty((B, L, D))
+    for t in range(L):
+        s = a[:, t] * s + k[:, t] * v[:, t]
+        every[:, t] = s
+    return q * every, s, every
+
+
+def glr_grads(dy, q, k, v, g, group=1, state=None, dstate=None):
+    """(dq, dk, dv, dg, dstate_in)."""
+    B, L, D = q.shape
+    a = np.exp(np.repeat(g, group, axis=2))
+    _, _, every = glr(q, k, v, g, group, state)
+    c = np.zeros((B, D)) if dstate is None else dstate.astype(np.float64).copy()
+    dq, dk, dv, da = (np.zeros((B, L, D)) for _ in range(4))
+    for t in range(L - 1, -1, -1):
+        before = every[:, t - 1] if t > 0 else (np.zeros((B, D)) if state is None else state)
+        m = q[:, t] * dy[:, t] + c
+        dq[:, t], dk[:, t], dv[:, t] = dy[:, t] * every[:, t], m * v[:, t], m * k[:, t]
+        c = a[:, t] * m
+        da[:, t] = c * before
+    return dq, dk, dv, da.reshape(B, L, D // group, group).sum(3), c

@@ -1,0 +1,67 @@
+"""Host-only checks of the entry points around the mixers: bad arguments are rejected before the GPU is touched."""
+import ctypes
+
+import pytest
+
+from paper_2503_01868_amd import binding
+
+P = [ctypes.c_void_p(1 << 20 | i << 36) for i in range(1, 20)]  # far apart, aligned, never looked at
+
+
+def fwd(q=P[0], k=P[1], v=P[2], g=P[3], s_in=None, y=P[4], s_out=None, marks=None, strides=None, ws=P[5], nbytes=1 << 30, B=1,
+        L=100, D=64, group=1, dtype=1):
+    return binding.lib().hyena_glr_fwd(q, k, v, g, s_in, y, s_out, marks, strides, ws, nbytes, B, L, D, group, dtype, None)
+
+
+def bwd(dy=P[0], q=P[1], k=P[2], v=P[3], g=P[4], marks=P[5], s_in=None, ds=None, dq=P[6], dk=P[7], dv=P[8], dg=P[9], ds_in=None,
+        strides=None, ws=P[10], nbytes=1 << 30, B=1, L=100, D=64, group=1, dtype=1):
+    return binding.lib().hyena_glr_bwd(dy, q, k, v, g, marks, s_in, ds, dq, dk, dv, dg, ds_in, strides, ws, nbytes, B, L, D, group,
+                                       dtype, None)
+
+
+def step(q=P[0], k=P[1], v=P[2], g=P[3], state=P[4], y=P[5], B=1, D=64, group=1, dtype=1):
+    return binding.lib().hyena_glr_step(q, k, v, g, state, y, B, D, group, dtype, None)
+
+
+@pytest.mark.parametrize("call,names", [(fwd, "q k v g y"), (bwd, "dy q k v g dq dk dv dg"), (step, "q k v g state y")])
+def test_recurrence_rejects_bad_arguments(call, names):
+    for n in names.split():
+        assert call(**{n: None}) == 1, n
+        assert call(**{n: ctypes.c_void_p((1 << 40) + 1)}) == 4, n
+    sizes = ("B", "D") if call is step else ("B", "L", "D")
+    for n in sizes:
+        assert call(**{n: -1}) == 2, n
+    assert call(group=0) == 2 and call(group=3) == 2
+    assert call(dtype=2) == 3 and call(dtype=-1) == 3
+    assert call(B=1 << 40, D=1 << 40) == 2
+    outputs = {"y", "dq", "dk", "dv", "dg", "state"}
+    for n in names.split():  # inputs may begin at any element
+        if n in outputs:
+            assert call(**{n: ctypes.c_void_p((1 << 40) + 8)}) == 4, n
+
+
+def test_recurrence_rejects_overlaps_strides_and_workspaces():
+    assert fwd(y=P[0]) == 4 and fwd(s_out=P[4]) == 4 and fwd(marks=P[1]) == 4 and fwd(ws=P[4]) == 4
+    assert bwd(dq=P[0]) == 4 and bwd(dq=P[7]) == 4 and bwd(ds_in=P[5]) == 4 and bwd(ws=P[9]) == 4
+    assert step(state=P[0]) == 4 and step(y=P[4]) == 4
+    assert fwd(ws=None) == 1 and fwd(nbytes=-1) == 2 and fwd(nbytes=16) == 2
+    assert bwd(ws=None) == 1 and bwd(nbytes=-1) == 2 and bwd(nbytes=16) == 2
+    assert fwd(strides=(ctypes.c_int64 * 8)(0, -1, 0, 0, 0, 0, 0, 0)) == 2
+    assert fwd(strides=(ctypes.c_int64 * 8)(0, 1 << 60, 0, 0, 0, 0, 0, 0)) == 2
+    # rows of q reach as far as y
+    far = ((P[4].value - P[0].value) // 2 // 99) + 1
+    assert fwd(strides=(ctypes.c_int64 * 8)(0, far, 0, 64, 0, 64, 0, 64)) == 4
+
+
+def test_recurrence_takes_empty_problems():
+    assert fwd(B=0) == 0 and fwd(L=0) == 0 and fwd(D=0, q=None, y=None) == 0
+    assert bwd(B=0, dy=None) == 0 and bwd(L=0) == 0
+    assert step(B=0) == 0 and step(D=0) == 0
+
+
+def test_recurrence_sizes_its_workspace():
+    f, b = binding.lib().hyena_glr_fwd_workspace_bytes, binding.lib().hyena_glr_bwd_workspace_bytes
+    assert f(1, 0, 64, 1, 1) == 0 and f(-1, 1, 64, 1, 1) == -1 and f(1, 1, 64, 5, 1) == -1 and f(1, 1, 64, 1, 7) == -1
+    assert b(1, 100, 64, 1, 1, 0) >= b(1, 100, 64, 1, 1, 1) > 0
+    assert b(1, 100, 63, 3, 1, 1) - b(1, 100, 63, 1, 1, 1) == 100 * 63 * 4   # the channels' shares of dg
+    assert b(1, 100, 192, 96, 1, 1) - b(1, 100, 192, 1, 1, 1) == 100 * 6 * 4  # in sums of 32

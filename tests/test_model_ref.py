@@ -1,0 +1,55 @@
+"""The 64-bit forms that the GPU tests compare with: gradients against differences, and closed forms."""
+import numpy as np
+import pytest
+
+import model_ref
+
+
+def difference(f, x, h=1e-5):
+    """Central differences of the scalar f in every element of x."""
+    d = np.zeros_like(x)
+    for i in np.ndindex(x.shape):
+        keep = x[i]
+        x[i] = keep + h
+        up = f()
+        x[i] = keep - h
+        d[i] = (up - f()) / (2 * h)
+        x[i] = keep
+    return d
+
+
+@pytest.mark.parametrize("B,L,D,group", [(1, 1, 1, 1), (2, 5, 4, 2), (1, 7, 6, 3)])
+def test_recurrence_gradients_match_differences(B, L, D, group):
+    rng = np.random.default_rng(10 + L)
+    q, k, v, dy = (rng.normal(size=(B, L, D)) for _ in range(4))
+    g = -rng.uniform(0.01, 2, size=(B, L, D // group))
+    state, dstate = rng.normal(size=(B, D)), rng.normal(size=(B, D))
+
+    def loss():
+        y, s, _ = model_ref.glr(q, k, v, g, group, state)
+        return (y * dy).sum() + (s * dstate).sum()
+
+    grads = model_ref.glr_grads(dy, q, k, v, g, group, state, dstate)
+    for got, x in zip(grads, (q, k, v, g, state)):
+        # central differences: h^2 / 6 times the third derivative, and 1e-16 / h from cancellation
+        np.testing.assert_allclose(got, difference(loss, x), rtol=1e-6, atol=1e-7)
+
+
+def test_recurrence_of_a_constant_decay_is_a_geometric_sum():
+    L, decay = 40, 0.9
+    one = np.ones((1, L, 1))
+    y, s, _ = model_ref.glr(one, one, one, np.log(decay) * one)
+    np.testing.assert_allclose(y[0, :, 0], (1 - decay ** np.arange(1, L + 1)) / (1 - decay), rtol=1e-12)
+    assert s[0, 0] == y[0, -1, 0]
+
+
+def test_recurrence_forgets_at_minus_infinity():
+    rng = np.random.default_rng(3)
+    q, k, v, dy = (rng.normal(size=(1, 9, 2)) for _ in range(4))
+    g = -rng.uniform(0, 1, size=(1, 9, 2))
+    g[:, 4] = -np.inf
+    y, s, _ = model_ref.glr(q, k, v, g)
+    y2, s2, _ = model_ref.glr(q[:, 4:], k[:, 4:], v[:, 4:], g[:, 4:])
+    np.testing.assert_array_equal(y[:, 4:], y2)
+    grads = model_ref.glr_grads(dy, q, k, v, g)
+    assert all(np.isfinite(d).all() for d in grads) and (grads[3][:, 4] == 0).all()
