@@ -431,6 +431,43 @@ hy_status hyena_glr_step(const void *q, const void *k, const void *v, const void
                          int64_t D, int32_t group, int32_t dtype, void *hip_stream);
 
 /*
+ * One AdamW step (decoupled weight decay, bias correction) over any number of tensors in one launch:
+ *     g' = grad_scale g,  m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2,
+ *     p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * in fp32.  Parameters and gradients are HY_F32 or HY_BF16 each.  A bf16 parameter may have an fp32 master: the step is taken
+ * on the master and the parameter is its rounded copy.
+ * bits = 32: exp_avg and exp_avg_sq hold m and v in fp32.  bits = 8: they hold m and sqrt(v) as OCP e4m3 numbers, one byte
+ * each, with an fp32 scale per HYENA_ADAMW_BLOCK elements (the last block of a tensor may be shorter) in avg_scale and
+ * sq_scale: value = number * scale, the block's largest magnitude at 448, rounded to nearest even; a root that is not zero is
+ * held as at least 2^-9 * scale; a block whose largest magnitude is below 2^-100 is held as zeros.  All zero bytes and scales
+ * are the states before the first step.  An element that is not finite is held as NaN and leaves its block's scale alone.
+ *
+ * hyena_adamw_table writes, into host memory, the table that the step reads: table_bytes >= hyena_adamw_table_bytes(...) of
+ * the same arguments (-1: not a valid problem).  The caller copies it to the device, once for as long as the tensors stay where
+ * they are, and hands the copy to hyena_adamw_step with the same n_tensors, param, grad, bits and with_master, and with the
+ * number of chunks that it returned.  The arguments are checked when the table is made: pointers NULL (HY_ERR_NULL; an empty
+ * tensor's may be), a written array that overlaps another array or pointers off their element's alignment (HY_ERR_ALIGN).
+ * hyena_adamw_step(step >= 1, 0 <= beta < 1, eps >= 0; else HY_ERR_SHAPE) reads grad_scale, one fp32 number in device
+ * memory, if it is not NULL.
+ */
+#define HYENA_ADAMW_BLOCK 256
+typedef struct hy_adamw_tensor {
+    void *param;
+    const void *grad;
+    void *exp_avg, *exp_avg_sq;
+    float *avg_scale, *sq_scale; /* bits = 8 */
+    float *master;               /* with_master */
+    int64_t count;
+    float weight_decay;
+} hy_adamw_tensor;
+int64_t hyena_adamw_table_bytes(const hy_adamw_tensor *tensors, int64_t n_tensors);
+hy_status hyena_adamw_table(const hy_adamw_tensor *tensors, int64_t n_tensors, int32_t param, int32_t grad, int32_t bits,
+                            int32_t with_master, void *table, int64_t table_bytes, int64_t *chunks);
+hy_status hyena_adamw_step(const void *table, int64_t n_tensors, int64_t chunks, int32_t param, int32_t grad, int32_t bits,
+                           int32_t with_master, double lr, double beta1, double beta2, double eps, int64_t step,
+                           const float *grad_scale, void *hip_stream);
+
+/*
  * Plain device-to-device streaming copy of `bytes` bytes (a multiple of 16) with the same launch
  * shape as the streaming kernels.  Used to measure the practical HBM ceiling and to calibrate
  * hardware byte counters; not part of the operator.

@@ -292,6 +292,29 @@ hy_status launch_glr_bwd(const GlrPtrs& p, const GlrShape& s, void* ws, hipStrea
 // One step of B sequences, the states (p.state_out) updated in place; D dense, L not looked at.
 hy_status launch_glr_step(const GlrPtrs& p, const GlrShape& s, hipStream_t st);
 
+// AdamW over many tensors: a table in device memory, an entry per tensor and the owner of each chunk of kAdamwChunk elements.
+constexpr int kAdamwBlock = HYENA_ADAMW_BLOCK;  // elements that share a scale where the states have 8 bits
+constexpr int kAdamwChunk = 4096;
+struct AdamwEntry {
+    void* param;
+    const void* grad;
+    void *exp_avg, *exp_avg_sq;
+    float *avg_scale, *sq_scale, *master;
+    int64_t count, first_chunk;
+    float weight_decay;
+    int32_t aligned;  // its elements can be moved four at a time
+};
+struct AdamwHyper {
+    double lr, beta1, beta2, eps, bias1, bias2_root;  // 1 - beta1^t, sqrt(1 - beta2^t)
+};
+struct AdamwShape {
+    int64_t chunks;
+    int32_t param, grad, bits;
+    bool master;
+};
+hy_status launch_adamw(const AdamwEntry* entries, const int32_t* owner, const float* grad_scale, const AdamwHyper& h,
+                       const AdamwShape& s, hipStream_t st);
+
 // Launches `kernel` and returns the status of THIS launch as hipLaunchKernel reports it.  The thread's sticky
 // "last error" is neither read nor cleared: an error left behind by an earlier, unrelated HIP call of the caller
 // cannot make a healthy launch look failed, and stays there for the caller to find.

@@ -1,4 +1,10 @@
 // C ABI of the operators around the mixers: argument validation (before any HIP call) and kernel selection.
+#include <math.h>
+#include <string.h>
+
+#include <algorithm>
+#include <vector>
+
 #include "hy_checks.hpp"
 #include "hy_common.hpp"
 #include "hy_launch.hpp"
@@ -69,9 +75,127 @@ hy_status take_starts(GlrShape& s, const Range* r, int n, int gate) {
 
 int64_t marks_bytes(const GlrShape& s) { return s.B * ((s.L + kGlrRows - 1) / kGlrRows) * s.D * 4; }
 
+// ---- AdamW
+
+int64_t chunks_of(int64_t count) { return (count + kAdamwChunk - 1) / kAdamwChunk; }
+
+// The chunks of all tensors; -1: not a valid problem.
+int64_t adamw_chunks(const hy_adamw_tensor* t, int64_t n) {
+    if (n < 0 || (n > 0 && !t)) return -1;
+    int64_t all = 0;
+    for (int64_t i = 0; i < n; ++i) {
+        if (t[i].count < 0 || t[i].count > kMostElements) return -1;
+        all += chunks_of(t[i].count);
+        if (all > INT32_MAX) return -1;  // one workgroup each
+    }
+    return n > INT32_MAX ? -1 : all;
+}
+
+struct Span {
+    uintptr_t from, to;
+    bool written;
+};
+
+// No written span meets another one.
+bool apart(std::vector<Span>& s) {
+    std::sort(s.begin(), s.end(), [](const Span& a, const Span& b) { return a.from < b.from; });
+    uintptr_t any = 0, written = 0;
+    for (const Span& x : s) {
+        if (x.from < written || (x.written && x.from < any)) return false;
+        any = std::max(any, x.to);
+        if (x.written) written = std::max(written, x.to);
+    }
+    return true;
+}
+
+hy_status adamw_entries(const hy_adamw_tensor* t, int64_t n, int32_t param, int32_t grad, int32_t bits, bool with_master,
+                        std::vector<AdamwEntry>& entries) {
+    std::vector<Span> spans;
+    int64_t chunk = 0;
+    for (int64_t i = 0; i < n; ++i) {
+        const int64_t c = t[i].count, e = bits == 8 ? 1 : 4, blocks = (c + kAdamwBlock - 1) / kAdamwBlock * 4;
+        const struct {
+            const void* p;
+            int64_t bytes, element;
+            bool written;
+        } arrays[7] = {{t[i].param, c * size_of(param), size_of(param), true}, {t[i].grad, c * size_of(grad), size_of(grad), false},
+                       {t[i].exp_avg, c * e, e, true}, {t[i].exp_avg_sq, c * e, e, true},
+                       {t[i].avg_scale, bits == 8 ? blocks : 0, 4, true}, {t[i].sq_scale, bits == 8 ? blocks : 0, 4, true},
+                       {t[i].master, with_master ? c * 4 : 0, 4, true}};
+        bool fours = true;
+        for (const auto& x : arrays) {
+            if (x.bytes == 0) continue;
+            const uintptr_t at = reinterpret_cast<uintptr_t>(x.p);
+            if (!x.p) return HY_ERR_NULL;
+            if (at % (uintptr_t)x.element != 0) return HY_ERR_ALIGN;
+            spans.push_back(Span{at, at + (uintptr_t)x.bytes, x.written});
+        }
+        for (const auto& x : {arrays[0], arrays[1], arrays[2], arrays[3], arrays[6]})
+            if (x.bytes > 0 && reinterpret_cast<uintptr_t>(x.p) % (uintptr_t)(4 * x.element) != 0) fours = false;
+        entries.push_back(AdamwEntry{t[i].param, t[i].grad, t[i].exp_avg, t[i].exp_avg_sq, t[i].avg_scale, t[i].sq_scale,
+                                     t[i].master, c, chunk, t[i].weight_decay, fours});
+        chunk += chunks_of(c);
+    }
+    return apart(spans) ? HY_OK : HY_ERR_ALIGN;
+}
+
+hy_status check_adamw_kinds(int32_t param, int32_t grad, int32_t bits, int32_t with_master) {
+    if (!known(param) || !known(grad)) return HY_ERR_DTYPE;
+    if (bits != 8 && bits != 32) return HY_ERR_UNSUPPORTED;
+    return with_master && param == HY_F32 ? HY_ERR_UNSUPPORTED : HY_OK;  // an fp32 parameter is its own master
+}
+
 }  // namespace
 
 extern "C" {
+
+int64_t hyena_adamw_table_bytes(const hy_adamw_tensor* tensors, int64_t n_tensors) {
+    const int64_t chunks = adamw_chunks(tensors, n_tensors);
+    return chunks < 0 ? -1 : n_tensors * (int64_t)sizeof(AdamwEntry) + chunks * (int64_t)sizeof(int32_t);
+}
+
+hy_status hyena_adamw_table(const hy_adamw_tensor* tensors, int64_t n_tensors, int32_t param, int32_t grad, int32_t bits,
+                            int32_t with_master, void* table, int64_t table_bytes, int64_t* chunks) {
+    if (!chunks || (n_tensors > 0 && (!tensors || !table))) return HY_ERR_NULL;
+    hy_status rc = check_adamw_kinds(param, grad, bits, with_master);
+    if (rc != HY_OK) return rc;
+    const int64_t all = adamw_chunks(tensors, n_tensors);
+    if (all < 0 || table_bytes < hyena_adamw_table_bytes(tensors, n_tensors)) return HY_ERR_SHAPE;
+    try {
+        std::vector<AdamwEntry> entries;
+        rc = adamw_entries(tensors, n_tensors, param, grad, bits, with_master != 0, entries);
+        if (rc != HY_OK) return rc;
+        *chunks = all;
+        if (n_tensors == 0) return HY_OK;
+        const size_t head = entries.size() * sizeof(AdamwEntry);
+        memcpy(table, entries.data(), head);
+        char* owner = static_cast<char*>(table) + head;
+        for (int64_t i = 0; i < n_tensors; ++i)
+            for (int64_t c = chunks_of(tensors[i].count); c > 0; --c, owner += sizeof(int32_t)) {
+                const int32_t me = (int32_t)i;
+                memcpy(owner, &me, sizeof me);
+            }
+    } catch (...) {  // no host memory
+        return HY_ERR_SCRATCH;
+    }
+    return HY_OK;
+}
+
+hy_status hyena_adamw_step(const void* table, int64_t n_tensors, int64_t chunks, int32_t param, int32_t grad, int32_t bits,
+                           int32_t with_master, double lr, double beta1, double beta2, double eps, int64_t step,
+                           const float* grad_scale, void* hip_stream) {
+    hy_status rc = check_adamw_kinds(param, grad, bits, with_master);
+    if (rc != HY_OK) return rc;
+    if (n_tensors < 0 || chunks < 0 || chunks > INT32_MAX || (n_tensors == 0 && chunks > 0)) return HY_ERR_SHAPE;
+    if (step < 1 || !(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1) || !(eps >= 0)) return HY_ERR_SHAPE;
+    if (chunks == 0) return HY_OK;
+    if (!table) return HY_ERR_NULL;
+    if (!aligned16(table) || reinterpret_cast<uintptr_t>(grad_scale) % 4 != 0) return HY_ERR_ALIGN;
+    const AdamwEntry* entries = static_cast<const AdamwEntry*>(table);
+    const AdamwHyper h{lr, beta1, beta2, eps, 1.0 - pow(beta1, (double)step), sqrt(1.0 - pow(beta2, (double)step))};
+    return launch_adamw(entries, reinterpret_cast<const int32_t*>(entries + n_tensors), grad_scale, h,
+                        AdamwShape{chunks, param, grad, bits, with_master != 0}, static_cast<hipStream_t>(hip_stream));
+}
 
 int64_t hyena_glr_fwd_workspace_bytes(int64_t B, int64_t L, int64_t D, int32_t group, int32_t dtype) {
     if (check_glr(B, L, D, group, dtype) != HY_OK) return -1;

@@ -1,4 +1,4 @@
-"""Binding of the operators around the mixers: gated linear recurrence.
+"""Binding of the operators around the mixers: gated linear recurrence, AdamW.
 
 As in ``binding``: arguments are checked and marshalled here, every step of the operators runs inside ``libhyena.so``, device
 memory and streams are PyTorch's, and a failed call raises ``HyenaError``.
@@ -9,7 +9,7 @@ import ctypes
 
 import torch
 
-from .binding import HY_OK, HyenaError, _dtype_code, _on, _stream, lib
+from .binding import _HERE, HY_OK, HyenaError, _dtype_code, _on, _stream, lib
 
 GLR_MARK_ROWS = 64  # HYENA_GLR_MARK_ROWS
 
@@ -20,12 +20,24 @@ def declare(L: ctypes.CDLL) -> None:
     L.hyena_glr_fwd.argtypes = [vp] * 10 + [i64, i64, i64, i64, i32, ci, vp]
     L.hyena_glr_bwd.argtypes = [vp] * 15 + [i64, i64, i64, i64, i32, ci, vp]
     L.hyena_glr_step.argtypes = [vp] * 6 + [i64, i64, i32, ci, vp]
-    for name in ("hyena_glr_fwd", "hyena_glr_bwd", "hyena_glr_step"):
+    L.hyena_adamw_table.argtypes = [vp, i64, ci, ci, ci, ci, vp, i64, vp]
+    L.hyena_adamw_step.argtypes = [vp, i64, i64, ci, ci, ci, ci] + [ctypes.c_double] * 4 + [i64, vp, vp]
+    for name in ("hyena_glr_fwd", "hyena_glr_bwd", "hyena_glr_step", "hyena_adamw_table", "hyena_adamw_step"):
         getattr(L, name).restype = ci
     L.hyena_glr_fwd_workspace_bytes.argtypes = [i64, i64, i64, i32, ci]
     L.hyena_glr_bwd_workspace_bytes.argtypes = [i64, i64, i64, i32, ci, i32]
-    for name in ("hyena_glr_fwd_workspace_bytes", "hyena_glr_bwd_workspace_bytes"):
+    L.hyena_adamw_table_bytes.argtypes = [vp, i64]
+    for name in ("hyena_glr_fwd_workspace_bytes", "hyena_glr_bwd_workspace_bytes", "hyena_adamw_table_bytes"):
         getattr(L, name).restype = i64
+
+
+def _under(x: torch.Tensor, stream):
+    """Context in which memory comes from the pool of the stream that the call runs on."""
+    if stream is None:
+        return _HERE
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(_stream(x, stream), device=x.device)
+    return torch.cuda.stream(stream)
 
 
 # ---- gated linear recurrence
@@ -101,13 +113,13 @@ def _glr_fwd(q, k, v, g, group, state_in, want_state, want_marks, out, workspace
     for name, t, s in (("q", q, shape), ("k", k, shape), ("v", v, shape), ("g", g, gates)):
         _glr_input(name, t, s, q)
     B, L, D = shape
-    y = _output(out, shape, q, "out")
-    state = torch.empty((B, D), dtype=torch.float32, device=q.device) if want_state else None
-    marks = torch.empty((B, -(-L // GLR_MARK_ROWS), D), dtype=torch.float32, device=q.device) if want_marks else None
     before = _glr_state("state_in", state_in, B, D, q)
     lb = lib()
-    ws, nbytes, keep = _workspace(int(lb.hyena_glr_fwd_workspace_bytes(B, L, D, group, code)), workspace, q)
-    with _on(q):
+    with _on(q), _under(q, stream):
+        y = _output(out, shape, q, "out")
+        state = torch.empty((B, D), dtype=torch.float32, device=q.device) if want_state else None
+        marks = torch.empty((B, -(-L // GLR_MARK_ROWS), D), dtype=torch.float32, device=q.device) if want_marks else None
+        ws, nbytes, keep = _workspace(int(lb.hyena_glr_fwd_workspace_bytes(B, L, D, group, code)), workspace, q)
         rc = lb.hyena_glr_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), before, y.data_ptr(), _ptr(state),
                               _ptr(marks), _strides((q, k, v, g)), ws, nbytes, B, L, D, group, code, _stream(q, stream))
     if rc != HY_OK:
@@ -142,12 +154,13 @@ def hyena_glr_bwd(dy, q, k, v, g, group: int = 1, marks=None, state_in=None, dst
                               or not marks.is_contiguous() or marks.get_device() != dy.get_device()):
         raise ValueError("marks must be the tensor that the forward call returned")
     before, behind = _glr_state("state_in", state_in, B, D, dy), _glr_state("dstate_out", dstate_out, B, D, dy)
-    dq, dk, dv = (torch.empty(shape, dtype=dy.dtype, device=dy.device) for _ in range(3))
-    dg = torch.empty(gates, dtype=dy.dtype, device=dy.device)
-    dstate = torch.empty((B, D), dtype=torch.float32, device=dy.device) if want_dstate else None
     lb = lib()
-    ws, nbytes, keep = _workspace(int(lb.hyena_glr_bwd_workspace_bytes(B, L, D, group, code, marks is not None)), workspace, dy)
-    with _on(dy):
+    with _on(dy), _under(dy, stream):
+        dq, dk, dv = (torch.empty(shape, dtype=dy.dtype, device=dy.device) for _ in range(3))
+        dg = torch.empty(gates, dtype=dy.dtype, device=dy.device)
+        dstate = torch.empty((B, D), dtype=torch.float32, device=dy.device) if want_dstate else None
+        need = int(lb.hyena_glr_bwd_workspace_bytes(B, L, D, group, code, marks is not None))
+        ws, nbytes, keep = _workspace(need, workspace, dy)
         rc = lb.hyena_glr_bwd(dy.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), _ptr(marks), before, behind,
                               dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), dg.data_ptr(), _ptr(dstate),
                               _strides((dy, q, k, v, g)), ws, nbytes, B, L, D, group, code, _stream(dy, stream))
@@ -170,10 +183,125 @@ def hyena_glr_step(q, k, v, g, state, group: int = 1, out=None, stream=None) -> 
     if state is None:
         raise ValueError("state must be a contiguous float32 [B, D] tensor on the same GPU")
     st = _glr_state("state", state, B, D, q)
-    y = _output(out, shape, q, "out")
-    with _on(q):
+    with _on(q), _under(q, stream):
+        y = _output(out, shape, q, "out")
         rc = lib().hyena_glr_step(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), st, y.data_ptr(), B, D, group, code,
                                   _stream(q, stream))
     if rc != HY_OK:
         raise HyenaError(rc, "hyena_glr_step")
     return y
+
+
+# ---- AdamW
+
+ADAMW_BLOCK = 256  # HYENA_ADAMW_BLOCK
+
+
+class _AdamwTensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "exp_avg", "exp_avg_sq", "avg_scale", "sq_scale", "master")] + [
+        ("count", ctypes.c_int64), ("weight_decay", ctypes.c_float)]
+
+
+def adamw_state(params, bits: int = 32, masters: bool = False) -> dict:
+    """The states before the first step, as keyword arguments of ``plan_adamw``: float32 moments, or with ``bits`` 8 the first
+    moment and the root of the second as float8_e4m3fn tensors with a float32 scale per 256 elements; with ``masters``, float32
+    copies of the parameters."""
+    if bits not in (8, 32):
+        raise ValueError("bits must be 8 or 32")
+    kind = torch.float32 if bits == 32 else torch.float8_e4m3fn
+
+    def zeros(dtype, per=1):
+        return [torch.zeros(-(-p.numel() // per) if per > 1 else p.shape, dtype=torch.uint8 if dtype.itemsize == 1 else dtype,
+                            device=p.device).view(dtype) for p in params]
+
+    state = dict(exp_avg=zeros(kind), exp_avg_sq=zeros(kind))
+    if bits == 8:
+        state.update(avg_scales=zeros(torch.float32, ADAMW_BLOCK), sq_scales=zeros(torch.float32, ADAMW_BLOCK))
+    if masters:
+        state["masters"] = [p.detach().float() for p in params]
+    return state
+
+
+def _adamw_list(name, ts, params, dtypes, per=1):
+    """The tensors of one kind: one dtype, contiguous, on the parameters' GPU, an element for every ``per`` of a parameter."""
+    ts = list(ts)
+    if len(ts) != len(params):
+        raise ValueError("%s must be one tensor for each parameter" % name)
+    for t, p in zip(ts, params):
+        if (not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in dtypes or t.dtype != ts[0].dtype
+                or not t.is_contiguous() or t.get_device() != params[0].get_device() or t.numel() != -(-p.numel() // per)):
+            raise ValueError("%s must be contiguous tensors of one dtype (%s) with %s on the parameters' GPU" % (
+                name, " or ".join(str(d) for d in dtypes), "a parameter's elements" if per == 1 else "an element per block"))
+    return ts
+
+
+class AdamwPlan:
+    """The tensors of ``hyena_adamw_step``, laid out once in a table on the GPU: calling it takes a step.  The tensors are kept
+    alive, and must stay where they are (gradients too: zero them in place)."""
+
+    def __init__(self, params, grads, exp_avg, exp_avg_sq, masters=None, avg_scales=None, sq_scales=None, weight_decay=0.0):
+        params = list(params)
+        plain = (torch.float32, torch.bfloat16)
+        params = _adamw_list("params", params, params, plain)
+        grads = _adamw_list("grads", grads, params, plain)
+        exp_avg = _adamw_list("exp_avg", exp_avg, params, (torch.float32, torch.float8_e4m3fn))
+        exp_avg_sq = _adamw_list("exp_avg_sq", exp_avg_sq, params, (exp_avg[0].dtype,) if params else plain)
+        narrow = bool(params) and exp_avg[0].dtype == torch.float8_e4m3fn
+        if narrow != (avg_scales is not None) or narrow != (sq_scales is not None):
+            raise ValueError("8-bit states come with avg_scales and sq_scales, others without")
+        n = len(params)
+        none = [None] * n
+        avg_scales = _adamw_list("avg_scales", avg_scales, params, (torch.float32,), ADAMW_BLOCK) if narrow else none
+        sq_scales = _adamw_list("sq_scales", sq_scales, params, (torch.float32,), ADAMW_BLOCK) if narrow else none
+        own = none if masters is None else _adamw_list("masters", masters, params, (torch.float32,))
+        decay = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else [float(x) for x in weight_decay]
+        if len(decay) != n:
+            raise ValueError("weight_decay must be a number or one for each parameter")
+        self._keep = (params, grads, exp_avg, exp_avg_sq, avg_scales, sq_scales, own)
+        self._kinds = (_dtype_code(params[0]), _dtype_code(grads[0]), 8 if narrow else 32, int(masters is not None)) if n else (
+            0, 0, 32, 0)
+        rows = (_AdamwTensor * n)(*(_AdamwTensor(*(_ptr(t) for t in ts), ts[0].numel(), wd)
+                                    for ts, wd in zip(zip(*self._keep), decay)))
+        lb = lib()
+        need = int(lb.hyena_adamw_table_bytes(rows, n))
+        if need < 0:
+            raise ValueError("not a valid problem")
+        table, chunks = torch.empty(need, dtype=torch.uint8), ctypes.c_int64()
+        rc = lb.hyena_adamw_table(rows, n, *self._kinds, table.data_ptr() if need else None, need, ctypes.byref(chunks))
+        if rc != HY_OK:
+            raise HyenaError(rc, "hyena_adamw_table")
+        self._n, self._chunks = n, chunks.value
+        self._table = table.to(params[0].device) if n else table
+        self._fn = lb.hyena_adamw_step
+
+    def __call__(self, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.95, eps: float = 1e-8, grad_scale=None,
+                 stream=None) -> None:
+        """The ``step``-th step, counted from 1.  ``grad_scale``: a float32 number on the GPU that multiplies the gradients (what
+        clipping found, or the inverse of a loss scale)."""
+        if not self._n:
+            return
+        first = self._keep[0][0]
+        if grad_scale is not None and (not isinstance(grad_scale, torch.Tensor) or grad_scale.dtype != torch.float32
+                                       or grad_scale.numel() != 1 or grad_scale.get_device() != first.get_device()):
+            raise ValueError("grad_scale must be one float32 number on the parameters' GPU")
+        with _on(first):
+            rc = self._fn(self._table.data_ptr(), self._n, self._chunks, *self._kinds, lr, beta1, beta2, eps, step,
+                          _ptr(grad_scale), _stream(first, stream))
+        if rc != HY_OK:
+            raise HyenaError(rc, "hyena_adamw_step")
+
+
+def plan_adamw(params, grads, exp_avg, exp_avg_sq, masters=None, avg_scales=None, sq_scales=None, weight_decay=0.0) -> AdamwPlan:
+    """Lay out the tensors of an AdamW step for repeated issue: parameters and gradients in float32 or bfloat16, states and
+    masters as ``adamw_state`` makes them, ``weight_decay`` one number or one per tensor; see ``hyena_adamw_step`` in hyena.h."""
+    return AdamwPlan(params, grads, exp_avg, exp_avg_sq, masters, avg_scales, sq_scales, weight_decay)
+
+
+def hyena_adamw_step(params, grads, exp_avg, exp_avg_sq, lr: float, step: int, masters=None, avg_scales=None, sq_scales=None,
+                     weight_decay=0.0, beta1: float = 0.9, beta2: float = 0.95, eps: float = 1e-8, grad_scale=None,
+                     stream=None) -> None:
+    """One AdamW step, the table laid out for this call alone (gradients that are new tensors every time)."""
+    params = list(params)
+    with _under(params[0], stream) if params else _HERE:
+        plan_adamw(params, grads, exp_avg, exp_avg_sq, masters, avg_scales, sq_scales, weight_decay)(
+            lr, step, beta1, beta2, eps, grad_scale, stream)

@@ -28,3 +28,11 @@ def glr_grads(dy, q, k, v, g, group=1, state=None, dstate=None):
         c = a[:, t] * m
         da[:, t] = c * before
     return dq, dk, dv, da.reshape(B, L, D // group, group).sum(3), c
+
+
+def adamw(p, g, m, v, lr, step, decay=0.0, beta1=0.9, beta2=0.95, eps=1e-8, scale=1.0):
+    """(p, m, v) after the step."""
+    g = g * scale
+    m = beta1 * m + (1 - beta1) * g
+    v = beta2 * v + (1 - beta2) * g * g
+    return p - lr * decay * p - lr * (m / (1 - beta1 ** step)) / (np.sqrt(v / (1 - beta2 ** step)) + eps), m, v

@@ -1,0 +1,180 @@
+"""AdamW over many tensors against its 64-bit form: every type, tensors around the sizes of blocks and chunks, views that begin
+anywhere, states in 32 and in 8 bits."""
+import numpy as np
+import pytest
+import torch
+
+import model_ref
+import paper_2503_01868_amd as hy
+
+from gpu_util import say
+
+pytestmark = pytest.mark.gpu
+
+SIZES = [1, 0, 3, 255, 256, 257, 4095, 4096, 4097, 10000, 70001]
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def wide(t):
+    return t.double().cpu().numpy()
+
+
+def tensors(rng, scale, dtype, shift=0):
+    out = []
+    for n in SIZES:
+        x = torch.zeros(n + shift, device="cuda", dtype=dtype)[shift:]
+        x.copy_(torch.from_numpy((rng.normal(size=n) * scale).astype(np.float32)))
+        out.append(x)
+    return out
+
+
+def values(state, name, scale):
+    """What a state holds, in 64 bits."""
+    got = []
+    for i, t in enumerate(state[name]):
+        x = wide(t.float())
+        if scale in state:
+            x = x * np.repeat(wide(state[scale][i]), hy.ADAMW_BLOCK)[:x.size]
+        got.append(x)
+    return got
+
+
+def held(x, got):
+    """|x - got| of a value held in 8 bits: half a step of four significant bits, or of the smallest numbers, at the block's scale;
+    the scale itself and x are fp32 (1e-6 of x)."""
+    for i in range(0, x.size, hy.ADAMW_BLOCK):
+        b, h = x[i:i + hy.ADAMW_BLOCK], got[i:i + hy.ADAMW_BLOCK]
+        unit = np.abs(b).max() / 448
+        yield np.abs(b - h) - (np.abs(b) * (2.0 ** -4 + 1e-6) + unit * 2.0 ** -10 * (1 + 1e-6)), unit
+
+
+@pytest.mark.parametrize("shift", [0, 1])
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("param,grad,masters", [("f32", "f32", False), ("bf16", "bf16", False), ("bf16", "f32", True),
+                                                ("bf16", "bf16", True), ("f32", "bf16", False)])
+def test_steps(param, grad, masters, bits, shift):
+    say("adamw %s %s masters=%s bits=%d shift=%d" % (param, grad, masters, bits, shift))
+    rng = np.random.default_rng(3)
+    params, grads = tensors(rng, 0.02, DTYPES[param], shift), tensors(rng, 1e-3, DTYPES[grad], shift)
+    decay = [0.1 * (i % 2) for i in range(len(SIZES))]
+    state = hy.adamw_state(params, bits, masters)
+    plan = hy.plan_adamw(params, grads, weight_decay=decay, **state)
+    clip = torch.full((1,), 0.5, device="cuda")
+    for step in (1, 2, 3):
+        for g in grads:
+            g.copy_(torch.from_numpy((rng.normal(size=g.shape) * 1e-3).astype(np.float32)))
+        before = [wide(p) for p in (state["masters"] if masters else params)]
+        m0, r0 = values(state, "exp_avg", "avg_scales"), values(state, "exp_avg_sq", "sq_scales")
+        plan(lr=1e-3, step=step, grad_scale=clip)
+        m1, r1 = values(state, "exp_avg", "avg_scales"), values(state, "exp_avg_sq", "sq_scales")
+        for i, p in enumerate(params):
+            if p.numel() == 0:
+                continue
+            v0 = r0[i] ** 2 if bits == 8 else r0[i]
+            rp, rm, rv = model_ref.adamw(before[i], wide(grads[i]), m0[i], v0, 1e-3, step, decay[i], scale=0.5)
+            # the step's some ten roundings of 6e-8 on its two parts, each of about lr at the most
+            now = wide(state["masters"][i] if masters else p)
+            eps = 2.0 ** -8 if param == "bf16" and not masters else 0.0
+            assert (np.abs(now - rp) <= 1e-6 * (np.abs(before[i]) + 0.02) + eps * np.abs(rp)).all()
+            if masters:
+                assert torch.equal(p, state["masters"][i].to(torch.bfloat16))
+            if bits == 32:
+                assert (np.abs(m1[i] - rm) <= 1e-6 * (np.abs(m0[i]) + 1e-3)).all()
+                assert (np.abs(r1[i] - rv) <= 1e-6 * rv + 1e-20).all()
+            else:
+                for over, _ in held(rm, m1[i]):
+                    assert (over <= 0).all()
+                root = np.sqrt(rv)
+                for (over, unit), b in zip(held(root, r1[i]), range(0, root.size, hy.ADAMW_BLOCK)):
+                    least = r1[i][b:b + hy.ADAMW_BLOCK] <= unit * 2.0 ** -9 * (1 + 1e-6)
+                    assert (over[~least] <= 0).all()
+                    assert (r1[i][b:b + hy.ADAMW_BLOCK][root[b:b + hy.ADAMW_BLOCK] > 0] > 0).all()
+
+
+def test_8_bit_states_are_the_formulas_bit_for_bit():
+    """Products and sums rounded one by one, as elementwise tensor operations round them: the same bytes."""
+    rng = np.random.default_rng(4)
+    n = 256 * 300
+    p, g = (torch.from_numpy((rng.normal(size=n) * s).astype(np.float32)).cuda() for s in (0.02, 1e-3))
+    state = hy.adamw_state([p], 8)
+    plan = hy.plan_adamw([p], [g], **state)
+    m = torch.zeros(n // 256, 256, device="cuda")
+    r = torch.zeros_like(m)
+    for step in (1, 2, 3, 4):
+        plan(lr=1e-3, step=step)
+        x = g.view(-1, 256)
+        m = m * 0.9 + x * (1 - 0.9)
+        r = torch.sqrt((r * r) * 0.95 + (x * x) * (1 - 0.95))
+        for y, codes, scales, root in ((m, "exp_avg", "avg_scales", False), (r, "exp_avg_sq", "sq_scales", True)):
+            top = y.abs().amax(1, keepdim=True)
+            z = y * (torch.full_like(top, 448.0) / top)
+            if root:
+                z = torch.where(y > 0, z.clamp(min=2.0 ** -9), z)
+            q = z.to(torch.float8_e4m3fn)
+            assert torch.equal(state[codes][0].view(torch.uint8), q.view(torch.uint8).view(-1))
+            assert torch.equal(state[scales][0], (top * (1 / 448)).view(-1))
+            y.copy_(q.float() * (top * (1 / 448)))
+
+
+def test_small_gradients_beside_large_ones_stay_bounded():
+    """An element whose root would round to zero in 8 bits must not be divided by nothing: no step is longer than a few lr."""
+    n = 256
+    p, g = torch.zeros(n, device="cuda"), torch.full((n,), 1e-9, device="cuda")
+    g[0] = 1.0
+    state = hy.adamw_state([p], 8)
+    plan = hy.plan_adamw([p], [g], **state)
+    for step in range(1, 30):
+        before = p.clone()
+        plan(lr=1e-3, step=step, eps=0.0)
+        assert (p - before).abs().max() <= 5e-3
+        if step == 10:
+            g[1:] = 0
+
+
+def test_what_is_not_finite_stays_in_its_element():
+    n = 1000
+    for bits in (32, 8):
+        p, g = torch.ones(n, device="cuda"), torch.full((n,), 1e-3, device="cuda")
+        g[300], g[301] = float("inf"), float("nan")
+        state = hy.adamw_state([p], bits)
+        hy.hyena_adamw_step([p], [g], lr=1e-3, step=1, **state)
+        bad = torch.zeros(n, dtype=torch.bool, device="cuda")
+        bad[300] = bad[301] = True
+        assert torch.isfinite(p[~bad]).all() and not torch.isfinite(p[bad]).any()
+        assert torch.isfinite(state["exp_avg"][0].float()[~bad]).all()
+
+
+def test_zero_gradients_leave_zero_states():
+    p, g = torch.ones(600, device="cuda"), torch.zeros(600, device="cuda")
+    state = hy.adamw_state([p], 8)
+    hy.hyena_adamw_step([p], [g], lr=1e-3, step=1, **state)
+    assert (p == 1).all() and all((t.view(torch.uint8) == 0).all() for t in state["exp_avg"] + state["exp_avg_sq"])
+    assert all((t == 0).all() for t in state["avg_scales"] + state["sq_scales"])
+
+
+def test_refusals():
+    p, g = torch.ones(8, device="cuda"), torch.zeros(8, device="cuda")
+    state = hy.adamw_state([p])
+    with pytest.raises(ValueError):
+        hy.plan_adamw([p], [g[:4]], **state)
+    with pytest.raises(ValueError):
+        hy.plan_adamw([p], [g.cpu()], **state)
+    with pytest.raises(ValueError):
+        hy.plan_adamw([p], [g.half()], **state)
+    with pytest.raises(ValueError):
+        hy.plan_adamw([p], [g], avg_scales=[g], **state)
+    with pytest.raises(ValueError):
+        hy.plan_adamw([p, p.bfloat16()], [g, g], **hy.adamw_state([p, p]))
+    with pytest.raises(ValueError):
+        hy.plan_adamw([p], [g], weight_decay=[0.1, 0.1], **state)
+    with pytest.raises(hy.HyenaError):
+        hy.plan_adamw([p], [p], **state)
+    with pytest.raises(hy.HyenaError):
+        hy.plan_adamw([p], [g], masters=[p.clone()], **state)
+    with pytest.raises(hy.HyenaError):
+        hy.plan_adamw([p], [g], **state)(lr=1e-3, step=0)
+    with pytest.raises(ValueError):
+        hy.plan_adamw([p], [g], **state)(lr=1e-3, step=1, grad_scale=0.5)
+    with pytest.raises(ValueError):
+        hy.adamw_state([p], bits=4)
+    hy.plan_adamw([], [], [], [])(lr=1e-3, step=1)

@@ -65,3 +65,57 @@ def test_recurrence_sizes_its_workspace():
     assert b(1, 100, 64, 1, 1, 0) >= b(1, 100, 64, 1, 1, 1) > 0
     assert b(1, 100, 63, 3, 1, 1) - b(1, 100, 63, 1, 1, 1) == 100 * 63 * 4   # the channels' shares of dg
     assert b(1, 100, 192, 96, 1, 1) - b(1, 100, 192, 1, 1, 1) == 100 * 6 * 4  # in sums of 32
+
+
+class Tensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "exp_avg", "exp_avg_sq", "avg_scale", "sq_scale", "master")] + [
+        ("count", ctypes.c_int64), ("weight_decay", ctypes.c_float)]
+
+
+def table(rows, param=0, grad=0, bits=32, masters=0, short=0):
+    rows = (Tensor * len(rows))(*rows)
+    need = binding.lib().hyena_adamw_table_bytes(rows, len(rows))
+    buf, chunks = ctypes.create_string_buffer(max(need, 0) + 1), ctypes.c_int64(-7)
+    rc = binding.lib().hyena_adamw_table(rows, len(rows), param, grad, bits, masters, buf, need - short, ctypes.byref(chunks))
+    return rc, need, chunks.value
+
+
+def at(*places, count=100):
+    return Tensor(*(None if x is None else (1 << 40) + x for x in places), count, 0.0)
+
+
+def test_adamw_table_checks_its_tensors():
+    good = at(0, 4096, 8192, 12288, None, None, None)
+    rc, need, chunks = table([good, at(1 << 20, 2 << 20, 3 << 20, 4 << 20, None, None, None, count=4097)])
+    assert rc == 0 and chunks == 3 and need > 0
+    assert table([])[0] == 0
+    assert table([at(None, None, None, None, None, None, None, count=0)])[::2] == (0, 0)
+    for i in range(4):
+        row = [0, 4096, 8192, 12288, None, None, None]
+        row[i] = None
+        assert table([at(*row)])[0] == 1
+        row[i] = 100002
+        assert table([at(*row)])[0] == 4
+    assert table([at(0, 0, 8192, 12288, None, None, None)])[0] == 4          # the gradient is the parameter
+    assert table([at(0, 4096, 8192, 8500, None, None, None)])[0] == 4        # states 308 bytes apart
+    assert table([good, at(1 << 20, 4096, 2 << 20, 3 << 20, None, None, None)])[0] == 0   # a gradient may be shared
+    assert table([good, at(1 << 20, 8192, 2 << 20, 3 << 20, None, None, None)])[0] == 4   # but not with a state
+    assert table([at(0, 4096, 8192, 12288, None, None, None, count=-1)])[:2] == (2, -1)
+    assert table([good], short=1)[0] == 2
+    assert table([good], param=2)[0] == 3 and table([good], grad=-1)[0] == 3
+    assert table([good], bits=16)[0] == 5 and table([good], masters=1)[0] == 5
+    assert table([good], bits=8)[0] == 1 and table([good], param=1, masters=1)[0] == 1
+    assert table([at(0, 4096, 8192, 12288, 16384, 20480, None)], bits=8)[0] == 0
+    assert table([at(1, 4097, 8193, 12289, 16384, 20480, None)], param=1, grad=1, bits=8)[0] == 4
+
+
+def test_adamw_step_rejects_bad_arguments():
+    def step(t=P[0], n=1, chunks=1, param=0, grad=0, bits=32, masters=0, lr=1e-3, b1=0.9, b2=0.95, eps=1e-8, count=1, scale=None):
+        return binding.lib().hyena_adamw_step(t, n, chunks, param, grad, bits, masters, lr, b1, b2, eps, count, scale, None)
+
+    assert step(t=None) == 1 and step(t=ctypes.c_void_p(8)) == 4 and step(scale=ctypes.c_void_p(2)) == 4
+    assert step(n=-1) == 2 and step(chunks=-1) == 2 and step(chunks=1 << 31) == 2 and step(n=0) == 2
+    assert step(count=0) == 2 and step(b1=1.0) == 2 and step(b2=-0.1) == 2 and step(eps=-1.0) == 2
+    assert step(b1=float("nan")) == 2
+    assert step(param=3) == 3 and step(bits=4) == 5 and step(masters=1) == 5
+    assert step(n=0, chunks=0, t=None) == 0

@@ -53,3 +53,12 @@ def test_recurrence_forgets_at_minus_infinity():
     np.testing.assert_array_equal(y[:, 4:], y2)
     grads = model_ref.glr_grads(dy, q, k, v, g)
     assert all(np.isfinite(d).all() for d in grads) and (grads[3][:, 4] == 0).all()
+
+
+def test_adamw_of_a_constant_gradient_moves_by_the_learning_rate():
+    """m / (1 - b1^t) = g and v / (1 - b2^t) = g^2 at every step."""
+    p, m, v = np.ones(3), np.zeros(3), np.zeros(3)
+    g = np.array([1.0, -2.0, 1e-3])
+    for step in range(1, 6):
+        p, m, v = model_ref.adamw(p, g, m, v, 0.01, step, eps=0.0)
+    np.testing.assert_allclose(p, 1 - 0.05 * np.sign(g), rtol=1e-12)
