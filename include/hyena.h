@@ -431,6 +431,30 @@ hy_status hyena_glr_step(const void *q, const void *k, const void *v, const void
                          int64_t D, int32_t group, int32_t dtype, void *hip_stream);
 
 /*
+ * Softmax cross entropy of a linear classifier over a vocabulary, without keeping the logits z = x W^T:
+ *     lse[n] = log sum_v exp(z[n,v]),   loss[n] = lse[n] - z[n,target[n]],   z[n,v] = sum_d x[n,d] w[v,d]
+ * x: [N,D], w: [V,D], dense, of `dtype`; target: int64 [N]; loss, lse: fp32 [N].  A row whose target is outside 0 .. V - 1 takes no
+ * part: its loss is 0 (its lse is written all the same).  The products run on the bf16 matrix cores with fp32 sums: bf16
+ * operands as they are, fp32 operands as three bf16 parts each, to fp32's precision.
+ * V, D >= 1 (HY_ERR_SHAPE); N = 0 is an empty problem.  workspace: hyena_xent_fwd_workspace_bytes(...) bytes.
+ */
+hy_status hyena_xent_fwd(const void *x, const void *w, const int64_t *target, float *loss, float *lse, void *workspace,
+                         int64_t workspace_bytes, int64_t N, int64_t V, int64_t D, int32_t dtype, void *hip_stream);
+int64_t hyena_xent_fwd_workspace_bytes(int64_t N, int64_t V, int64_t D, int32_t dtype);
+
+/*
+ * Backward of hyena_xent_fwd.  With dloss[n] = dLoss/dloss[n] (fp32 [N]; 1/N for a mean) and lse as the forward call wrote it,
+ *     P[n,v] = dloss[n] * (exp(z[n,v] - lse[n]) - [v = target[n]]),   dx = P W,   dw = P^T x
+ * dx: [N,D], dw: [V,D], of `dtype`, overwritten; zeros in dx for rows that take no part, and nothing in dw from them, whatever
+ * they hold.  P is rounded to bf16 for its two products in bf16 calls; sums are fp32, in a fixed order, one rounding per stored
+ * element.  The vocabulary is taken in pieces: workspace (hyena_xent_bwd_workspace_bytes(...) bytes) holds P of one piece.
+ */
+hy_status hyena_xent_bwd(const float *dloss, const void *x, const void *w, const int64_t *target, const float *lse, void *dx,
+                         void *dw, void *workspace, int64_t workspace_bytes, int64_t N, int64_t V, int64_t D,
+                         int32_t dtype, void *hip_stream);
+int64_t hyena_xent_bwd_workspace_bytes(int64_t N, int64_t V, int64_t D, int32_t dtype);
+
+/*
  * One AdamW step (decoupled weight decay, bias correction) over any number of tensors in one launch:
  *     g' = grad_scale g,  m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2,
  *     p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)

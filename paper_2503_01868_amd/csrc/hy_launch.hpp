@@ -315,6 +315,23 @@ struct AdamwShape {
 hy_status launch_adamw(const AdamwEntry* entries, const int32_t* owner, const float* grad_scale, const AdamwHyper& h,
                        const AdamwShape& s, hipStream_t st);
 
+// Softmax cross entropy of x W^T.
+struct XentPtrs {
+    const void *x = nullptr, *w = nullptr;
+    const int64_t* target = nullptr;
+    float *loss = nullptr, *lse = nullptr;                  // forward
+    const float *lse_in = nullptr, *dloss = nullptr;        // backward
+    void *dx = nullptr, *dw = nullptr;
+};
+struct XentShape {
+    int64_t N, V, D;
+    hy_dtype dtype;
+};
+int64_t xent_fwd_workspace_bytes(const XentShape& s);
+int64_t xent_bwd_workspace_bytes(const XentShape& s);
+hy_status launch_xent_fwd(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t st);
+hy_status launch_xent_bwd(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t st);
+
 // Launches `kernel` and returns the status of THIS launch as hipLaunchKernel reports it.  The thread's sticky
 // "last error" is neither read nor cleared: an error left behind by an earlier, unrelated HIP call of the caller
 // cannot make a healthy launch look failed, and stays there for the caller to find.

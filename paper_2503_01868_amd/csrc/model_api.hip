@@ -75,6 +75,13 @@ hy_status take_starts(GlrShape& s, const Range* r, int n, int gate) {
 
 int64_t marks_bytes(const GlrShape& s) { return s.B * ((s.L + kGlrRows - 1) / kGlrRows) * s.D * 4; }
 
+// ---- cross entropy
+
+hy_status check_xent(int64_t N, int64_t V, int64_t D, int32_t dtype) {
+    if (N < 0 || V < 1 || D < 1 || !fits(N, D, 1) || !fits(V, D, 1) || !fits(N, V, 1)) return HY_ERR_SHAPE;
+    return known(dtype) ? HY_OK : HY_ERR_DTYPE;
+}
+
 // ---- AdamW
 
 int64_t chunks_of(int64_t count) { return (count + kAdamwChunk - 1) / kAdamwChunk; }
@@ -148,6 +155,54 @@ hy_status check_adamw_kinds(int32_t param, int32_t grad, int32_t bits, int32_t w
 }  // namespace
 
 extern "C" {
+
+int64_t hyena_xent_fwd_workspace_bytes(int64_t N, int64_t V, int64_t D, int32_t dtype) {
+    if (check_xent(N, V, D, dtype) != HY_OK) return -1;
+    return N == 0 ? 0 : xent_fwd_workspace_bytes(XentShape{N, V, D, static_cast<hy_dtype>(dtype)});
+}
+
+int64_t hyena_xent_bwd_workspace_bytes(int64_t N, int64_t V, int64_t D, int32_t dtype) {
+    if (check_xent(N, V, D, dtype) != HY_OK) return -1;
+    return N == 0 ? 0 : xent_bwd_workspace_bytes(XentShape{N, V, D, static_cast<hy_dtype>(dtype)});
+}
+
+hy_status hyena_xent_fwd(const void* x, const void* w, const int64_t* target, float* loss, float* lse, void* workspace,
+                         int64_t workspace_bytes, int64_t N, int64_t V, int64_t D, int32_t dtype, void* hip_stream) {
+    hy_status rc = check_xent(N, V, D, dtype);
+    if (rc != HY_OK) return rc;
+    if (workspace_bytes < 0) return HY_ERR_SHAPE;
+    if (N == 0) return HY_OK;
+    if (!x || !w || !target || !loss || !lse) return HY_ERR_NULL;
+    const XentShape s{N, V, D, static_cast<hy_dtype>(dtype)};
+    const int64_t e = size_of(dtype);
+    const Range all[5] = {{x, N * D * e}, {w, V * D * e}, {target, N * 8}, {loss, N * 4}, {lse, N * 4}};
+    rc = all_aligned(all, 5);
+    if (rc == HY_OK) rc = check_disjoint(all, 3, all + 3, 2);
+    if (rc == HY_OK) rc = check_workspace(workspace, workspace_bytes, xent_fwd_workspace_bytes(s), all, 5);
+    if (rc != HY_OK) return rc;
+    XentPtrs p;
+    p.x = x, p.w = w, p.target = target, p.loss = loss, p.lse = lse;
+    return launch_xent_fwd(p, s, workspace, static_cast<hipStream_t>(hip_stream));
+}
+
+hy_status hyena_xent_bwd(const float* dloss, const void* x, const void* w, const int64_t* target, const float* lse, void* dx,
+                         void* dw, void* workspace, int64_t workspace_bytes, int64_t N, int64_t V, int64_t D, int32_t dtype,
+                         void* hip_stream) {
+    hy_status rc = check_xent(N, V, D, dtype);
+    if (rc != HY_OK) return rc;
+    if (workspace_bytes < 0) return HY_ERR_SHAPE;
+    if (!w || !dw || (N > 0 && (!dloss || !x || !target || !lse || !dx))) return HY_ERR_NULL;
+    const XentShape s{N, V, D, static_cast<hy_dtype>(dtype)};
+    const int64_t e = size_of(dtype);
+    const Range all[7] = {{x, N * D * e}, {w, V * D * e}, {target, N * 8}, {dloss, N * 4}, {lse, N * 4}, {dx, N * D * e}, {dw, V * D * e}};
+    rc = all_aligned(all, 7);
+    if (rc == HY_OK) rc = check_disjoint(all, 5, all + 5, 2);
+    if (rc == HY_OK) rc = check_workspace(workspace, workspace_bytes, N > 0 ? xent_bwd_workspace_bytes(s) : 0, all, 7);
+    if (rc != HY_OK) return rc;
+    XentPtrs p;
+    p.dloss = dloss, p.x = x, p.w = w, p.target = target, p.lse_in = lse, p.dx = dx, p.dw = dw;
+    return launch_xent_bwd(p, s, workspace, static_cast<hipStream_t>(hip_stream));
+}
 
 int64_t hyena_adamw_table_bytes(const hy_adamw_tensor* tensors, int64_t n_tensors) {
     const int64_t chunks = adamw_chunks(tensors, n_tensors);

@@ -1,0 +1,517 @@
+// Softmax cross entropy of z = x W^T over a vocabulary, and its gradients, without keeping z.
+//
+//     lse[n] = log sum_v exp z[n, v],  loss[n] = lse[n] - z[n, target[n]]
+//     P[n, v] = dloss[n] (exp(z[n, v] - lse[n]) - [v = target[n]]),  dx = P W,  dW = P^T x
+//
+// Forward: a tile of z stays in registers; each of its rows leaves the largest value and the sum of exponentials below it, and
+// a second kernel joins the tiles of a row.  Backward, for a piece of the vocabulary at a time: z again, P from it, and the two
+// products.  All four products are of the one form that hy_gemm.hpp has (k contiguous in both operands), so P is written in
+// both orders, and x and the piece of W are transposed once.  The matrix products are what bounds it: 8 N V D operations.
+//
+// bf16 operands enter the products as they are; P is rounded to bf16 for its two.  fp32 operands, and P of fp32 calls, are three
+// bf16 numbers (8 bits each, the head, the middle and the tail of the 24), and a product is the sum of the six products of
+// parts that reach its 24 bits.
+#include <algorithm>
+
+#include "hy_gemm.hpp"
+#include "hy_launch.hpp"
+
+namespace hy {
+
+namespace {
+
+// The parts of an fp32 number: cut, not rounded, so that no part overflows; all of a number that is not finite is in the first.
+__device__ __forceinline__ void parts_of(float x, uint16_t (&part)[3]) {
+    const uint32_t b = __float_as_uint(x);
+    part[0] = (uint16_t)(b >> 16);
+    part[1] = part[2] = 0;
+    if ((b & 0x7f800000u) == 0x7f800000u) {
+        if (b & 0x007fffffu) part[0] |= 0x40;  // a NaN stays one without its lower bits
+        return;
+    }
+    const float rest = x - __uint_as_float(b & 0xffff0000u);
+    const uint32_t m = __float_as_uint(rest);
+    part[1] = (uint16_t)(m >> 16);
+    part[2] = (uint16_t)(__float_as_uint(rest - __uint_as_float(m & 0xffff0000u)) >> 16);
+}
+
+template <typename T>
+__device__ __forceinline__ void bits_of(const char* p, uint16_t (&part)[3]) {
+    if constexpr (T::kBytes == 4) parts_of(*reinterpret_cast<const float*>(p), part);
+    else part[0] = *reinterpret_cast<const uint16_t*>(p);
+}
+
+// Rows of D values -> planes of rows of `ld` bf16 numbers, zeros behind the values.
+template <typename T>
+__global__ __launch_bounds__(256) void pack_kernel(const char* src, uint16_t* dst, int64_t rows, int64_t D, int64_t ld) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= rows * ld) return;
+    const int64_t r = i / ld, c = i % ld;
+    uint16_t part[3] = {};
+    if (c < D) bits_of<T>(src + (r * D + c) * T::kBytes, part);
+    for (int x = 0; x < (T::kBytes == 4 ? 3 : 1); ++x) dst[x * rows * ld + i] = part[x];
+}
+
+// Rows of D values -> planes of D rows of `ld` bf16 numbers; zeros behind the last row, and for the rows whose target is none.
+template <typename T>
+__global__ __launch_bounds__(256) void turn_kernel(const char* src, uint16_t* dst, int64_t rows, int64_t D, int64_t ld,
+                                                   const int64_t* target, int64_t V) {
+    constexpr int N = T::kBytes == 4 ? 3 : 1;
+    __shared__ uint16_t s[N][64][65];
+    const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;
+    const int x = threadIdx.x % 64;
+    for (int y = threadIdx.x / 64; y < 64; y += 4) {
+        uint16_t part[3] = {};
+        const int64_t r = r0 + y;
+        if (r < rows && c0 + x < D && (!target || (target[r] >= 0 && target[r] < V))) bits_of<T>(src + (r * D + c0 + x) * T::kBytes, part);
+        for (int i = 0; i < N; ++i) s[i][y][x] = part[i];
+    }
+    __syncthreads();
+    for (int y = threadIdx.x / 64; y < 64; y += 4)
+        if (c0 + y < D && r0 + x < ld)
+            for (int i = 0; i < N; ++i) dst[(i * D + c0 + y) * ld + r0 + x] = s[i][x][y];
+}
+
+struct XentArgs {
+    GemmArgs g;
+    const int64_t* target;
+    int64_t V, v0;            // the vocabulary, and the first column of this piece
+    // losses
+    float2* part;             // [rows][tiles]: the largest value and the sum below it
+    int64_t tiles, tile0;
+    float* zt;                // [rows] the targets' values
+    // gradients
+    const float *lse, *dloss;
+    uint16_t *p, *pt;
+    int64_t p_ld, p_plane, pt_ld, pt_plane;
+    // products
+    char* out;
+    float* sum;               // the sum so far (not of the first piece)
+    int64_t out_ld;
+    bool first, last;
+};
+
+// Tiles in runs of a few rows of tiles, a run of neighbours for each XCD: what its workgroups share stays in its L2.
+template <int BM, int BN>
+__device__ __forceinline__ void tile_of(const GemmArgs& g, int64_t* m0, int64_t* n0, uint32_t* tn) {
+    constexpr uint32_t kRun = 8;
+    const uint32_t i = xcd_contiguous(blockIdx.x, (uint32_t)g.mt * (uint32_t)g.nt);
+    const uint32_t per = kRun * (uint32_t)g.nt, first = i / per * kRun;
+    const uint32_t h = (uint32_t)g.mt - first < kRun ? (uint32_t)g.mt - first : kRun;
+    *tn = i % per / h;
+    *m0 = (int64_t)(first + i % per % h) * BM;
+    *n0 = (int64_t)*tn * BN;
+}
+
+template <int BM, int BN, int MW, int NW>
+__global__ __launch_bounds__(MW * NW * kWave) void loss_kernel(XentArgs a) {
+    using G = Gemm<BM, BN, MW, NW>;
+    __shared__ __attribute__((aligned(16))) char lds[2 * G::kBytes];
+    G t;
+    int64_t m0, n0;
+    uint32_t tn;
+    tile_of<BM, BN>(a.g, &m0, &n0, &tn);
+    t.run(lds, a.g, m0, n0);
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    const int wm = w % MW, wn = w / MW, li = lane % 16, lq = lane / 16;
+    float2(*share)[NW] = reinterpret_cast<float2(*)[NW]>(lds);
+    __syncthreads();  // the tiles have been read
+#pragma unroll
+    for (int i = 0; i < G::MI; ++i) {
+        const int row = wm * G::WM + i * 16 + li;
+        const int64_t m = m0 + row;
+        const int64_t want = m < a.g.a.rows ? a.target[m] - a.v0 : -1;  // of this piece's columns
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < G::NI; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int64_t n = n0 + wn * G::WN + j * 16 + 4 * lq + r;
+                if (n >= a.g.b.rows) t.acc[i][j][r] = -INFINITY;
+                else if (n == want) a.zt[m] = t.acc[i][j][r];
+                top = fmaxf(top, t.acc[i][j][r]);
+            }
+        top = fmaxf(top, __shfl_xor(top, 16, kWave));
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        const float ref = top == -INFINITY ? 0.0f : top;
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < G::NI; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum += expf(t.acc[i][j][r] - ref);
+        sum += __shfl_xor(sum, 16, kWave);
+        sum += __shfl_xor(sum, 32, kWave);
+        if (lq == 0) share[row][wn] = make_float2(top, sum);
+    }
+    __syncthreads();
+    for (int row = threadIdx.x; row < BM; row += G::kThreads) {
+        if (m0 + row >= a.g.a.rows) continue;
+        float top = -INFINITY, sum = 0.0f;
+        for (int x = 0; x < NW; ++x) top = fmaxf(top, share[row][x].x);
+        const float ref = top == -INFINITY ? 0.0f : top;
+        for (int x = 0; x < NW; ++x) sum += share[row][x].y * expf(share[row][x].x - ref);
+        a.part[(m0 + row) * a.tiles + a.tile0 + tn] = make_float2(top, sum);
+    }
+}
+
+// A wave joins the tiles of a row.
+__global__ __launch_bounds__(256) void join_kernel(const float2* part, const float* zt, const int64_t* target, float* loss,
+                                                   float* lse, int64_t rows, int64_t tiles, int64_t V) {
+    const int64_t m = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+    const int lane = threadIdx.x % kWave;
+    if (m >= rows) return;
+    float top = -INFINITY, sum = 0.0f;
+    for (int64_t i = lane; i < tiles; i += kWave) top = fmaxf(top, part[m * tiles + i].x);
+    for (int d = 32; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d, kWave));
+    const float ref = top == -INFINITY ? 0.0f : top;
+    for (int64_t i = lane; i < tiles; i += kWave) {
+        const float2 x = part[m * tiles + i];
+        sum += x.y * expf(x.x - ref);
+    }
+    for (int d = 32; d > 0; d /= 2) sum += __shfl_xor(sum, d, kWave);
+    if (lane == 0) {
+        const float all = ref + logf(sum);
+        lse[m] = all;
+        loss[m] = target[m] >= 0 && target[m] < V ? all - zt[m] : 0.0f;
+    }
+}
+
+template <typename T, int BM, int BN, int MW, int NW>
+__global__ __launch_bounds__(MW * NW * kWave) void grad_kernel(XentArgs a) {
+    using G = Gemm<BM, BN, MW, NW>;
+    constexpr int N = T::kBytes == 4 ? 3 : 1;
+    __shared__ __attribute__((aligned(16))) char lds[2 * G::kBytes];
+    G t;
+    int64_t m0, n0;
+    uint32_t tn;
+    tile_of<BM, BN>(a.g, &m0, &n0, &tn);
+    t.run(lds, a.g, m0, n0);
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    const int wm = w % MW, wn = w / MW, li = lane % 16, lq = lane / 16;
+    const int64_t rows = a.g.a.rows, cols = a.g.b.rows;
+#pragma unroll
+    for (int i = 0; i < G::MI; ++i) {
+        const int64_t m = m0 + wm * G::WM + i * 16 + li;
+        int64_t want = -1;
+        float lse = 0.0f, d = 0.0f;
+        bool counts = false;
+        if (m < rows) {
+            want = a.target[m];
+            counts = want >= 0 && want < a.V;
+            want -= a.v0;
+            lse = a.lse[m];
+            d = a.dloss[m];
+        }
+#pragma unroll
+        for (int j = 0; j < G::NI; ++j) {
+            const int64_t n = n0 + wn * G::WN + j * 16 + 4 * lq;
+            uint16_t part[4][3];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float p = expf(t.acc[i][j][r] - lse);
+                if (n + r == want) p -= 1.0f;
+                p = counts && n + r < cols ? d * p : 0.0f;  // zeros, whatever is in the row
+                if constexpr (N == 3) parts_of(p, part[r]);
+                else part[r][0] = (uint16_t)pack_bf16x2(p, 0.0f);
+            }
+#pragma unroll
+            for (int x = 0; x < N; ++x) {
+                if (m < rows && n < a.p_ld)  // p_ld: a multiple of 64
+                    *reinterpret_cast<uint2*>(a.p + x * a.p_plane + m * a.p_ld + n) =
+                        make_uint2(part[0][x] | (uint32_t)part[1][x] << 16, part[2][x] | (uint32_t)part[3][x] << 16);
+                if (m < a.pt_ld)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (n + r < cols) a.pt[x * a.pt_plane + (n + r) * a.pt_ld + m] = part[r][x];
+            }
+        }
+    }
+}
+
+// out = A B^T, or its sum over pieces.
+template <typename T, int BM, int BN, int MW, int NW>
+__global__ __launch_bounds__(MW * NW * kWave) void product_kernel(XentArgs a) {
+    using G = Gemm<BM, BN, MW, NW>;
+    __shared__ __attribute__((aligned(16))) char lds[2 * G::kBytes];
+    G t;
+    int64_t m0, n0;
+    uint32_t tn;
+    tile_of<BM, BN>(a.g, &m0, &n0, &tn);
+    t.run(lds, a.g, m0, n0);
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    const int wm = w % MW, wn = w / MW, li = lane % 16, lq = lane / 16;
+#pragma unroll
+    for (int i = 0; i < G::MI; ++i) {
+        const int64_t m = m0 + wm * G::WM + i * 16 + li;
+        if (m >= a.g.a.rows) continue;
+        const bool none = a.target && (a.target[m] < 0 || a.target[m] >= a.V);
+#pragma unroll
+        for (int j = 0; j < G::NI; ++j) {
+            const int64_t n = n0 + wn * G::WN + j * 16 + 4 * lq, at = m * a.out_ld + n;
+            const int have = a.g.b.rows - n < 4 ? (int)(a.g.b.rows - n) : 4;
+            float f[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                f[r] = none ? 0.0f : t.acc[i][j][r];
+                if (!a.first && r < have) f[r] += a.sum[at + r];
+            }
+            if (have == 4 && a.out_ld % 4 == 0) {
+                if (!a.last) Pack<F32, 4>::store(a.sum + at, Pack<F32, 4>::pack(f));
+                else Pack<T, 4>::store(a.out + at * T::kBytes, Pack<T, 4>::pack(f));
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (r < have) {
+                        const float one[1] = {f[r]};
+                        if (!a.last) a.sum[at + r] = f[r];
+                        else Pack<T, 1>::store(a.out + (at + r) * T::kBytes, Pack<T, 1>::pack(one));
+                    }
+            }
+        }
+    }
+}
+
+__global__ __launch_bounds__(256) void zero_kernel(char* p, int64_t bytes) {
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 2;
+    if (i < bytes) *reinterpret_cast<uint16_t*>(p + i) = 0;
+}
+
+int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+int64_t cut(int64_t n, int64_t by) { return (n + by - 1) / by; }
+
+// How a problem is laid out.
+struct Layout {
+    int planes;
+    bool packed;              // x and W are copied for the products (fp32, or rows that are no multiple of 128 bytes)
+    int64_t ld;               // of x and W in the products
+    int64_t nt;               // N rounded up: the k of dW
+    int64_t piece, pieces;    // columns of the vocabulary at a time
+};
+
+constexpr int64_t kPieceBytes = INT64_C(512) << 20;  // of P and its transpose
+
+Layout layout_of(const XentShape& s) {
+    Layout l;
+    l.planes = s.dtype == HY_F32 ? 3 : 1;
+    l.packed = s.dtype == HY_F32 || s.D % kGemmK != 0;
+    l.ld = up(s.D, kGemmK);
+    l.nt = up(s.N, kGemmK);
+    const int64_t most = std::max<int64_t>(1024, kPieceBytes / (4 * l.planes * l.nt) / 256 * 256);
+    l.pieces = cut(s.V, most);
+    l.piece = std::min(up(cut(s.V, l.pieces), 256), up(s.V, kGemmK));
+    l.pieces = cut(s.V, l.piece);
+    return l;
+}
+
+// Pieces of the workspace, in order.
+struct Carver {
+    char* at;
+    template <typename T>
+    T* take(int64_t n) {
+        char* p = at;
+        at += up(n * (int64_t)sizeof(T), 256);
+        return reinterpret_cast<T*>(p);
+    }
+};
+
+struct FwdSpace {
+    uint16_t *x, *w;
+    float2* part;
+    float* zt;
+    int64_t tiles;
+    FwdSpace(const XentShape& s, const Layout& l, Carver& c) {
+        tiles = 0;
+        for (int64_t i = 0; i < l.pieces; ++i) tiles += cut(std::min(l.piece, s.V - i * l.piece), 128);
+        x = l.packed ? c.take<uint16_t>(l.planes * s.N * l.ld) : nullptr;
+        w = l.packed ? c.take<uint16_t>(l.planes * std::min(l.piece, s.V) * l.ld) : nullptr;
+        part = c.take<float2>(s.N * tiles);
+        zt = c.take<float>(s.N);
+    }
+};
+
+struct BwdSpace {
+    uint16_t *x, *w, *xt, *wt, *p, *pt;
+    float* sum;
+    BwdSpace(const XentShape& s, const Layout& l, Carver& c) {
+        const int64_t piece = std::min(l.piece, s.V), ld = up(piece, kGemmK);
+        x = l.packed ? c.take<uint16_t>(l.planes * s.N * l.ld) : nullptr;
+        w = l.packed ? c.take<uint16_t>(l.planes * piece * l.ld) : nullptr;
+        xt = c.take<uint16_t>(l.planes * s.D * l.nt);
+        wt = c.take<uint16_t>(l.planes * s.D * ld);
+        p = c.take<uint16_t>(l.planes * s.N * ld);
+        pt = c.take<uint16_t>(l.planes * piece * l.nt);
+        sum = l.pieces > 1 ? c.take<float>(s.N * s.D) : nullptr;
+    }
+};
+
+GemmArgs product_of(const GemmOperand& a, const GemmOperand& b, int64_t K, int planes) {
+    GemmArgs g{};
+    g.a = a, g.b = b, g.K = (int32_t)K;
+    g.segments = planes == 3 ? 6 : 1;
+    // the smallest products first
+    g.aplanes = planes == 3 ? 0x001102u : 0u;
+    g.bplanes = planes == 3 ? 0x010120u : 0u;
+    return g;
+}
+
+// Tiles of 256 x 256 where they fill most of the chip, else of 128 x 128.
+bool large_tiles(const GemmArgs& g) { return cut(g.a.rows, 256) * cut(g.b.rows, 256) >= 192; }
+
+template <typename F>
+hy_status by_tile(XentArgs& a, F f) {
+    const bool large = large_tiles(a.g);
+    const int64_t mt = cut(a.g.a.rows, large ? 256 : 128), nt = cut(a.g.b.rows, large ? 256 : 128);
+    if (mt > INT32_MAX / nt) return HY_ERR_UNSUPPORTED;
+    a.g.mt = (int32_t)mt, a.g.nt = (int32_t)nt;
+    return f(large, dim3((uint32_t)(mt * nt)));
+}
+
+hy_status losses(XentArgs& a, hipStream_t st) {
+    return by_tile(a, [&](bool large, dim3 grid) {
+        return large ? launch_kernel(loss_kernel<256, 256, 2, 4>, grid, dim3(512), st, a)
+                     : launch_kernel(loss_kernel<128, 128, 2, 2>, grid, dim3(256), st, a);
+    });
+}
+
+template <typename T>
+hy_status gradients(XentArgs& a, hipStream_t st) {
+    return by_tile(a, [&](bool large, dim3 grid) {
+        return large ? launch_kernel(grad_kernel<T, 256, 256, 2, 4>, grid, dim3(512), st, a)
+                     : launch_kernel(grad_kernel<T, 128, 128, 2, 2>, grid, dim3(256), st, a);
+    });
+}
+
+template <typename T>
+hy_status product(XentArgs& a, hipStream_t st) {
+    return by_tile(a, [&](bool large, dim3 grid) {
+        return large ? launch_kernel(product_kernel<T, 256, 256, 2, 4>, grid, dim3(512), st, a)
+                     : launch_kernel(product_kernel<T, 128, 128, 2, 2>, grid, dim3(256), st, a);
+    });
+}
+
+template <typename T>
+hy_status pack(const void* src, uint16_t* dst, int64_t rows, int64_t D, int64_t ld, hipStream_t st) {
+    return launch_kernel(pack_kernel<T>, dim3((uint32_t)cut(rows * ld, 256)), dim3(256), st, (const char*)src, dst, rows, D, ld);
+}
+
+template <typename T>
+hy_status turn(const void* src, uint16_t* dst, int64_t rows, int64_t D, int64_t ld, const int64_t* target, int64_t V,
+               hipStream_t st) {
+    return launch_kernel(turn_kernel<T>, dim3((uint32_t)cut(ld, 64), (uint32_t)cut(D, 64)), dim3(256), st, (const char*)src, dst,
+                         rows, D, ld, target, V);
+}
+
+// x, and the piece of W that begins at row v, as operands.
+template <typename T>
+hy_status operands(const XentPtrs& p, const XentShape& s, const Layout& l, uint16_t* x, uint16_t* w, int64_t v, GemmOperand* ox,
+                   GemmOperand* ow, hipStream_t st) {
+    const int64_t rows = std::min(l.piece, s.V - v);
+    *ox = GemmOperand{l.packed ? x : (const uint16_t*)p.x, l.ld, s.N * l.ld, s.N};
+    *ow = GemmOperand{l.packed ? w : (const uint16_t*)p.w + v * s.D, l.ld, rows * l.ld, rows};
+    if (!l.packed) return HY_OK;
+    hy_status rc = v == 0 ? pack<T>(p.x, x, s.N, s.D, l.ld, st) : HY_OK;
+    if (rc == HY_OK) rc = pack<T>((const char*)p.w + v * s.D * T::kBytes, w, rows, s.D, l.ld, st);
+    return rc;
+}
+
+template <typename T>
+hy_status forward(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t st) {
+    const Layout l = layout_of(s);
+    Carver c{static_cast<char*>(ws)};
+    FwdSpace f(s, l, c);
+    XentArgs a{};
+    a.target = p.target, a.V = s.V;
+    a.part = f.part, a.zt = f.zt, a.tiles = f.tiles;
+    int64_t tile = 0;
+    for (int64_t v = 0; v < s.V; v += l.piece) {
+        GemmOperand x, w;
+        hy_status rc = operands<T>(p, s, l, f.x, f.w, v, &x, &w, st);
+        if (rc != HY_OK) return rc;
+        a.g = product_of(x, w, l.ld, l.planes);
+        a.v0 = v, a.tile0 = tile;
+        if (v == 0) {  // pieces have the same tiles, the last one fewer
+            a.tiles = 0;
+            for (int64_t u = 0; u < s.V; u += l.piece) {
+                GemmArgs g = a.g;
+                g.b.rows = std::min(l.piece, s.V - u);
+                a.tiles += cut(g.b.rows, large_tiles(g) ? 256 : 128);
+            }
+        }
+        rc = losses(a, st);
+        if (rc != HY_OK) return rc;
+        tile += a.g.nt;
+    }
+    return launch_kernel(join_kernel, dim3((uint32_t)cut(s.N, 4)), dim3(256), st, (const float2*)f.part, (const float*)f.zt, p.target,
+                         p.loss, p.lse, s.N, a.tiles, s.V);
+}
+
+template <typename T>
+hy_status backward(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t st) {
+    const Layout l = layout_of(s);
+    Carver c{static_cast<char*>(ws)};
+    BwdSpace b(s, l, c);
+    hy_status rc = turn<T>(p.x, b.xt, s.N, s.D, l.nt, p.target, s.V, st);
+    for (int64_t v = 0; rc == HY_OK && v < s.V; v += l.piece) {
+        const int64_t cols = std::min(l.piece, s.V - v), ld = up(cols, kGemmK);
+        GemmOperand x, w;
+        rc = operands<T>(p, s, l, b.x, b.w, v, &x, &w, st);
+        if (rc == HY_OK) rc = turn<T>((const char*)p.w + v * s.D * T::kBytes, b.wt, cols, s.D, ld, nullptr, 0, st);
+        XentArgs a{};
+        a.g = product_of(x, w, l.ld, l.planes);
+        a.target = p.target, a.V = s.V, a.v0 = v;
+        a.lse = p.lse_in, a.dloss = p.dloss;
+        a.p = b.p, a.p_ld = ld, a.p_plane = s.N * ld;
+        a.pt = b.pt, a.pt_ld = l.nt, a.pt_plane = cols * l.nt;
+        if (rc == HY_OK) rc = gradients<T>(a, st);
+        XentArgs dw{};
+        dw.g = product_of(GemmOperand{b.pt, l.nt, a.pt_plane, cols}, GemmOperand{b.xt, l.nt, s.D * l.nt, s.D}, l.nt, l.planes);
+        dw.out = (char*)p.dw + v * s.D * T::kBytes, dw.out_ld = s.D, dw.first = dw.last = true;
+        if (rc == HY_OK) rc = product<T>(dw, st);
+        XentArgs dx{};
+        dx.g = product_of(GemmOperand{b.p, ld, a.p_plane, s.N}, GemmOperand{b.wt, ld, s.D * ld, s.D}, ld, l.planes);
+        dx.out = (char*)p.dx, dx.out_ld = s.D, dx.sum = b.sum, dx.first = v == 0, dx.last = v + l.piece >= s.V;
+        dx.target = p.target, dx.V = s.V;
+        if (rc == HY_OK) rc = product<T>(dx, st);
+    }
+    return rc;
+}
+
+// Row distances that a lane's 32-bit offsets within a tile reach, and grids of 2^31 workgroups.
+bool served(const XentShape& s) {
+    const Layout l = layout_of(s);
+    return l.ld <= (1 << 22) && l.nt <= (1 << 22) && l.piece <= (1 << 22) && cut(s.N, 128) * cut(l.piece, 128) <= INT32_MAX &&
+           cut(s.N * l.ld, 256) <= INT32_MAX && cut(l.piece * l.ld, 256) <= INT32_MAX && l.ld <= 64 * 65535;
+}
+
+}  // namespace
+
+int64_t xent_fwd_workspace_bytes(const XentShape& s) {
+    const Layout l = layout_of(s);
+    Carver c{nullptr};
+    FwdSpace f(s, l, c);
+    return c.at - (char*)nullptr;
+}
+
+int64_t xent_bwd_workspace_bytes(const XentShape& s) {
+    const Layout l = layout_of(s);
+    Carver c{nullptr};
+    BwdSpace b(s, l, c);
+    return c.at - (char*)nullptr;
+}
+
+hy_status launch_xent_fwd(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t st) {
+    if (!served(s)) return HY_ERR_UNSUPPORTED;
+    return s.dtype == HY_F32 ? forward<F32>(p, s, ws, st) : forward<BF16>(p, s, ws, st);
+}
+
+hy_status launch_xent_bwd(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t st) {
+    if (s.N == 0) {  // no rows: nothing but zeros for the weights
+        const int64_t bytes = s.V * s.D * (s.dtype == HY_F32 ? 4 : 2);
+        if (cut(bytes, 512) > INT32_MAX) return HY_ERR_UNSUPPORTED;
+        return launch_kernel(zero_kernel, dim3((uint32_t)cut(bytes, 512)), dim3(256), st, (char*)p.dw, bytes);
+    }
+    if (!served(s)) return HY_ERR_UNSUPPORTED;
+    return s.dtype == HY_F32 ? backward<F32>(p, s, ws, st) : backward<BF16>(p, s, ws, st);
+}
+
+}  // namespace hy

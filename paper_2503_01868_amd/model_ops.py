@@ -1,4 +1,5 @@
-"""Binding of the operators around the mixers: gated linear recurrence, AdamW.
+"""Binding of the operators around the mixers: gated linear recurrence, cross entropy over a vocabulary,
+AdamW.
 
 As in ``binding``: arguments are checked and marshalled here, every step of the operators runs inside ``libhyena.so``, device
 memory and streams are PyTorch's, and a failed call raises ``HyenaError``.
@@ -20,14 +21,19 @@ def declare(L: ctypes.CDLL) -> None:
     L.hyena_glr_fwd.argtypes = [vp] * 10 + [i64, i64, i64, i64, i32, ci, vp]
     L.hyena_glr_bwd.argtypes = [vp] * 15 + [i64, i64, i64, i64, i32, ci, vp]
     L.hyena_glr_step.argtypes = [vp] * 6 + [i64, i64, i32, ci, vp]
+    L.hyena_xent_fwd.argtypes = [vp] * 6 + [i64, i64, i64, i64, ci, vp]
+    L.hyena_xent_bwd.argtypes = [vp] * 8 + [i64, i64, i64, i64, ci, vp]
     L.hyena_adamw_table.argtypes = [vp, i64, ci, ci, ci, ci, vp, i64, vp]
     L.hyena_adamw_step.argtypes = [vp, i64, i64, ci, ci, ci, ci] + [ctypes.c_double] * 4 + [i64, vp, vp]
-    for name in ("hyena_glr_fwd", "hyena_glr_bwd", "hyena_glr_step", "hyena_adamw_table", "hyena_adamw_step"):
+    for name in ("hyena_glr_fwd", "hyena_glr_bwd", "hyena_glr_step", "hyena_xent_fwd", "hyena_xent_bwd", "hyena_adamw_table",
+                 "hyena_adamw_step"):
         getattr(L, name).restype = ci
     L.hyena_glr_fwd_workspace_bytes.argtypes = [i64, i64, i64, i32, ci]
     L.hyena_glr_bwd_workspace_bytes.argtypes = [i64, i64, i64, i32, ci, i32]
+    L.hyena_xent_fwd_workspace_bytes.argtypes = L.hyena_xent_bwd_workspace_bytes.argtypes = [i64, i64, i64, ci]
     L.hyena_adamw_table_bytes.argtypes = [vp, i64]
-    for name in ("hyena_glr_fwd_workspace_bytes", "hyena_glr_bwd_workspace_bytes", "hyena_adamw_table_bytes"):
+    for name in ("hyena_glr_fwd_workspace_bytes", "hyena_glr_bwd_workspace_bytes", "hyena_xent_fwd_workspace_bytes",
+                 "hyena_xent_bwd_workspace_bytes", "hyena_adamw_table_bytes"):
         getattr(L, name).restype = i64
 
 
@@ -190,6 +196,59 @@ def hyena_glr_step(q, k, v, g, state, group: int = 1, out=None, stream=None) -> 
     if rc != HY_OK:
         raise HyenaError(rc, "hyena_glr_step")
     return y
+
+
+# ---- cross entropy over a vocabulary
+
+
+def _xent_inputs(x, w, target):
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dim() != 2 or not x.is_contiguous():
+        raise ValueError("x must be a contiguous [N, D] tensor on the GPU")
+    if (not isinstance(w, torch.Tensor) or w.dim() != 2 or not w.is_contiguous() or w.shape[1] != x.shape[1]
+            or w.dtype != x.dtype or w.get_device() != x.get_device()):
+        raise ValueError("w must be a contiguous [V, D] tensor of x's dtype on its GPU")
+    if (not isinstance(target, torch.Tensor) or target.dtype != torch.int64 or target.shape != x.shape[:1]
+            or not target.is_contiguous() or target.get_device() != x.get_device()):
+        raise ValueError("target must be a contiguous int64 [N] tensor on x's GPU")
+    return x.shape[0], w.shape[0], x.shape[1], _dtype_code(x)
+
+
+def _xent_column(name, t, N, x):
+    if (not isinstance(t, torch.Tensor) or t.dtype != torch.float32 or t.shape != (N,) or not t.is_contiguous()
+            or t.get_device() != x.get_device()):
+        raise ValueError("%s must be a contiguous float32 [N] tensor on x's GPU" % name)
+    return t.data_ptr()
+
+
+def hyena_xent_fwd(x, w, target, workspace=None, stream=None):
+    """(loss, lse), float32 [N]: softmax cross entropy of the rows of x w^T with ``target`` (int64; a row whose target is no row
+    of w has loss 0).  The logits are not kept; see ``hyena_xent_fwd`` in hyena.h."""
+    N, V, D, code = _xent_inputs(x, w, target)
+    lb = lib()
+    with _on(x), _under(x, stream):
+        loss, lse = (torch.empty(N, dtype=torch.float32, device=x.device) for _ in range(2))
+        ws, nbytes, keep = _workspace(int(lb.hyena_xent_fwd_workspace_bytes(N, V, D, code)), workspace, x)
+        rc = lb.hyena_xent_fwd(x.data_ptr(), w.data_ptr(), target.data_ptr(), loss.data_ptr(), lse.data_ptr(), ws, nbytes, N, V, D,
+                               code, _stream(x, stream))
+    if rc != HY_OK:
+        raise HyenaError(rc, "hyena_xent_fwd")
+    return loss, lse
+
+
+def hyena_xent_bwd(dloss, x, w, target, lse, workspace=None, stream=None):
+    """(dx, dw) of ``hyena_xent_fwd``, given the gradient of every row's loss (1 / N for a mean) and the ``lse`` it returned; see
+    ``hyena_xent_bwd`` in hyena.h."""
+    N, V, D, code = _xent_inputs(x, w, target)
+    dl, ls = _xent_column("dloss", dloss, N, x), _xent_column("lse", lse, N, x)
+    lb = lib()
+    with _on(x), _under(x, stream):
+        dx, dw = torch.empty_like(x), torch.empty_like(w)
+        ws, nbytes, keep = _workspace(int(lb.hyena_xent_bwd_workspace_bytes(N, V, D, code)), workspace, x)
+        rc = lb.hyena_xent_bwd(dl, x.data_ptr(), w.data_ptr(), target.data_ptr(), ls, dx.data_ptr(), dw.data_ptr(), ws, nbytes, N, V,
+                               D, code, _stream(x, stream))
+    if rc != HY_OK:
+        raise HyenaError(rc, "hyena_xent_bwd")
+    return dx, dw
 
 
 # ---- AdamW

@@ -36,3 +36,23 @@ def adamw(p, g, m, v, lr, step, decay=0.0, beta1=0.9, beta2=0.95, eps=1e-8, scal
     m = beta1 * m + (1 - beta1) * g
     v = beta2 * v + (1 - beta2) * g * g
     return p - lr * decay * p - lr * (m / (1 - beta1 ** step)) / (np.sqrt(v / (1 - beta2 ** step)) + eps), m, v
+
+
+def xent(x, w, target):
+    """(loss, lse, z); rows whose target is no row of w have loss 0."""
+    z = x @ w.T
+    top = z.max(1, keepdims=True)
+    lse = (top + np.log(np.exp(z - top).sum(1, keepdims=True)))[:, 0]
+    counts = (target >= 0) & (target < len(w))
+    loss = np.where(counts, lse - z[np.arange(len(x)), np.where(counts, target, 0)], 0.0)
+    return loss, lse, z
+
+
+def xent_grads(dloss, x, w, target):
+    """(dx, dw)."""
+    _, lse, z = xent(x, w, target)
+    counts = (target >= 0) & (target < len(w))
+    p = np.exp(z - lse[:, None])
+    p[np.flatnonzero(counts), target[counts]] -= 1
+    p *= np.where(counts, dloss, 0.0)[:, None]
+    return p @ w, p.T @ x

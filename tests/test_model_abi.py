@@ -119,3 +119,33 @@ def test_adamw_step_rejects_bad_arguments():
     assert step(b1=float("nan")) == 2
     assert step(param=3) == 3 and step(bits=4) == 5 and step(masters=1) == 5
     assert step(n=0, chunks=0, t=None) == 0
+
+
+def xent_fwd(x=P[0], w=P[1], t=P[2], loss=P[3], lse=P[4], ws=P[5], nbytes=1 << 34, N=10, V=20, D=64, dtype=1):
+    return binding.lib().hyena_xent_fwd(x, w, t, loss, lse, ws, nbytes, N, V, D, dtype, None)
+
+
+def xent_bwd(dl=P[0], x=P[1], w=P[2], t=P[3], lse=P[4], dx=P[5], dw=P[6], ws=P[7], nbytes=1 << 34, N=10, V=20, D=64, dtype=1):
+    return binding.lib().hyena_xent_bwd(dl, x, w, t, lse, dx, dw, ws, nbytes, N, V, D, dtype, None)
+
+
+@pytest.mark.parametrize("call,names", [(xent_fwd, "x w t loss lse ws"), (xent_bwd, "dl x w t lse dx dw ws")])
+def test_cross_entropy_rejects_bad_arguments(call, names):
+    for n in names.split():
+        assert call(**{n: None}) == 1, n
+        assert call(**{n: ctypes.c_void_p((1 << 40) + 8)}) == 4, n
+    assert call(N=-1) == 2 and call(V=0) == 2 and call(D=0) == 2 and call(V=1 << 40, D=1 << 40) == 2
+    assert call(dtype=2) == 3
+    assert call(nbytes=-1) == 2 and call(nbytes=16) == 2
+    assert call(ws=P[0]) == 4
+    if call is xent_fwd:
+        assert call(N=0, x=None, ws=None) == 0 and call(loss=P[0]) == 4 and call(lse=P[3]) == 4
+    else:
+        assert call(dx=P[1]) == 4 and call(dw=P[2]) == 4 and call(dw=P[5]) == 4
+
+
+def test_cross_entropy_sizes_its_workspace():
+    f, b = binding.lib().hyena_xent_fwd_workspace_bytes, binding.lib().hyena_xent_bwd_workspace_bytes
+    assert f(0, 10, 64, 1) == 0 == b(0, 10, 64, 1) and f(1, 0, 64, 1) == -1 and b(1, 10, 64, 9) == -1
+    assert 0 < f(8192, 65536, 4096, 1) < 1 << 30    # nothing like the logits
+    assert 0 < b(8192, 65536, 4096, 1) < 3 << 30

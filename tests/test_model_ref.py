@@ -62,3 +62,22 @@ def test_adamw_of_a_constant_gradient_moves_by_the_learning_rate():
     for step in range(1, 6):
         p, m, v = model_ref.adamw(p, g, m, v, 0.01, step, eps=0.0)
     np.testing.assert_allclose(p, 1 - 0.05 * np.sign(g), rtol=1e-12)
+
+
+def test_cross_entropy_gradients_match_differences():
+    rng = np.random.default_rng(7)
+    x, w = rng.normal(size=(5, 4)), rng.normal(size=(6, 4))
+    target, dloss = np.array([0, 5, -100, 2, 6]), rng.normal(size=5)
+
+    def loss():
+        return (model_ref.xent(x, w, target)[0] * dloss).sum()
+
+    for got, at in zip(model_ref.xent_grads(dloss, x, w, target), (x, w)):
+        np.testing.assert_allclose(got, difference(loss, at), rtol=1e-6, atol=1e-7)
+    assert model_ref.xent(x, w, target)[0][2] == 0 == model_ref.xent(x, w, target)[0][4]
+
+
+def test_cross_entropy_of_equal_logits():
+    x, w = np.zeros((2, 3)), np.ones((10, 3))
+    loss, lse, _ = model_ref.xent(x, w, np.array([3, 4]))
+    np.testing.assert_allclose(loss, np.log(10))
