@@ -528,6 +528,8 @@ hy_status hyena_stream_gate(const void *q, const void *k, const void *v, void *y
  *              1 = always the long-sequence kernel (where D is a multiple of 128), 2 = always the stencil
  *   "li_wait"  how Hyena-LI's tiles come by the states of the tiles before them, where it can do them in one pass:
  *              0 = wait for them (for a bounded time), 1 = compute them again, 2 = two passes everywhere
+ *   "glr_wait" how the tiles of the gated linear recurrence come by the states of the tiles before them: 0 = wait for them
+ *              (for a bounded time), 1 = compute them again (the same bits)
  * Unknown names return HY_ERR_UNSUPPORTED.  Results depend on these only through rounding, within the
  * documented precision of each entry point.
  */

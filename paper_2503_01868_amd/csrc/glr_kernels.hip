@@ -1,10 +1,21 @@
 // Gated linear recurrence: s[t] = a[t] s[t-1] + u[t], y[t] = q[t] s[t], a = exp(g), u = k v, and its gradients.
 //
 // The recurrence is linear, so a stretch of steps acts on the state before it as s -> A s + H with two numbers per channel,
-// A the product of its a and H its result from zero.  Tiles of kGlrRows steps are summed up this way in parallel, a scan over
-// the tiles' pairs gives each tile its incoming state (the "marks"), and the tile is walked from there.  The gradient runs
-// the other way with the same A: with m[t] = dLoss/ds[t] and c[t] = a[t] m[t] (what a step hands to the one before it),
-// m[t] = q[t] dy[t] + c[t+1], so a stretch takes c -> A c + C.
+// A the product of its a and H its result from zero.  The gradient runs the other way with the same A: with m[t] = dLoss/ds[t]
+// and c[t] = a[t] m[t] (what a step hands to the one before it), m[t] = q[t] dy[t] + c[t+1], so a stretch takes c -> A c + C.
+//
+// One pass: a workgroup loads a tile of kGlrRows steps by 64 or 128 channels into registers, each wave kRowsPerWave rows, sums
+// it up, publishes (A, H), takes the state at its edge from the tiles before it (behind it, backward), publishes its own and
+// writes the tile's results from the registers.  Every tensor is read and written once: that traffic is what bounds it.
+//
+// The edge: tile i needs s = A[i-1] (A[i-2] (...) + H[i-2]) + H[i-1].  A workgroup looks at kWindow tiles before it until one of
+// them has published its state and all tiles between have published their sums, and applies those one by one.  That is the
+// order a walk from the first tile has, wherever the look finds a state: results do not depend on timing.  A state travels up to
+// kWindow tiles per exchange between compute units, so the exchanges are few against the tiles that are in flight.
+// Without flags or fences: glr_unset_kernel fills the records with kUnset, a NaN that no value ever is (a producer that holds
+// it stores the plain NaN); words are stored and loaded as atomics at device scope, and a record is there when none of its words
+// is kUnset.  Tiles wait for tiles of lower launch index only, and for a bounded time: after kPolls looks the workgroup walks
+// the sequence itself, by the same sums.
 #include "hy_common.hpp"
 #include "hy_launch.hpp"
 
@@ -14,6 +25,9 @@ namespace {
 
 constexpr int kWaves = 8;                      // waves of a workgroup, one after the other in time
 constexpr int kRowsPerWave = kGlrRows / kWaves;
+constexpr int kWindow = 2 * kWaves;
+constexpr uint32_t kUnset = 0xffffdeadu;
+constexpr int kPolls = 4096;
 
 struct Src {
     const char* p;
@@ -24,11 +38,15 @@ struct GlrArgs {
     Src q, k, v, g, dy;
     char *y, *dq, *dk, *dv, *dg;
     float* dg_parts;           // [B, L, D / part] fp32, where a group is summed up in parts
-    const float* marks;        // [B, tiles, D] states before the tiles
-    const float* rmarks;       // [B, tiles, D] c of the step after the tile
-    float *A, *H;              // [B, tiles, D]
-    int64_t L, D;
+    const float* edge_in;      // [B, D]: the state before the first tile (the gradient behind the last), or null: zero
+    float* edge_out;           // [B, D]: what comes out at the other end, or null
+    const float* marks;        // [B, tiles, D] states before the tiles (backward)
+    float* marks_out;          // forward, or null
+    uint64_t* sums;            // [tiles, B, D]: (A, H) or (A, C) of the tiles, in the order of the walk
+    uint32_t* states;          // [tiles, B, D]: the state behind (the c before) them
+    int64_t B, L, D;
     int32_t tiles, ncb, group, part;  // part: channels of a group that a wave sums up (a power of two)
+    int32_t polls;
 };
 
 // VEC channels per lane; SHARED: both channels of a lane (or its only one) take the gate of their group.
@@ -45,13 +63,14 @@ struct Io {
 };
 
 struct Place {
-    int w, lane, tile;
-    int64_t b, c, row0;   // row0: the wave's first step
-    int rows;             // steps of the sequence that the wave has
+    int w, lane;
+    int order, tile;      // the tile's place in the walk and in the sequence
+    int64_t b, c;
     bool there;           // its channels exist
 };
 
-template <int VEC>
+// Launch order: tile by tile of the walk, in it all sequences and channels.
+template <int VEC, bool REV>
 __device__ __forceinline__ Place place(const GlrArgs& a) {
     Place p;
     p.w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -59,155 +78,268 @@ __device__ __forceinline__ Place place(const GlrArgs& a) {
     uint32_t i = blockIdx.x;
     const uint32_t cb = i % (uint32_t)a.ncb;
     i /= (uint32_t)a.ncb;
-    p.tile = i % (uint32_t)a.tiles;
-    p.b = i / (uint32_t)a.tiles;
+    p.b = i % (uint32_t)a.B;
+    p.order = i / (uint32_t)a.B;
+    p.tile = REV ? a.tiles - 1 - p.order : p.order;
     p.c = (int64_t)cb * (kWave * VEC) + p.lane * VEC;
     p.there = p.c < a.D;
     if (!p.there) p.c = 0;
-    p.row0 = (int64_t)p.tile * kGlrRows + p.w * kRowsPerWave;
-    const int64_t left = a.L - p.row0;
-    p.rows = left < 0 ? 0 : left < kRowsPerWave ? (int)left : kRowsPerWave;
     return p;
+}
+
+struct Rows {
+    int64_t first;
+    int n;  // steps of the sequence that the wave has
+};
+__device__ __forceinline__ Rows rows_of(const GlrArgs& a, int tile, int w) {
+    Rows r;
+    r.first = (int64_t)tile * kGlrRows + w * kRowsPerWave;
+    const int64_t left = a.L - r.first;
+    r.n = left < 0 ? 0 : left < kRowsPerWave ? (int)left : kRowsPerWave;
+    return r;
 }
 
 // The wave's rows of a tensor; steps behind the last are the last one again (their values are not used).
 template <typename PK>
 __device__ __forceinline__ void load_rows(typename PK::Raw (&r)[kRowsPerWave], const Src& s, const GlrArgs& a, const Place& p,
-                                          int64_t lane_bytes) {
+                                          const Rows& at, int64_t lane_bytes) {
     const char* base = s.p + p.b * s.bstride + lane_bytes;
 #pragma unroll
     for (int i = 0; i < kRowsPerWave; ++i) {
-        const int64_t t = p.row0 + i < a.L ? p.row0 + i : a.L - 1;
+        const int64_t t = at.first + i < a.L ? at.first + i : a.L - 1;
         r[i] = PK::load_nt(base + t * s.rstride);
     }
 }
 
-// What the waves before (or, REV, behind) wave w of a workgroup make of the state at the workgroup's edge.
+template <int VEC>
+struct Shared {
+    float A[kWaves][kWave * VEC], H[kWaves][kWave * VEC];            // of the waves
+    float wA[kWindow][kWave * VEC], wH[kWindow][kWave * VEC];        // of the tiles in the window, nearest first; or, in wH,
+    int32_t found[2][kWindow];                                       // their state.  0: nothing yet, 1: sums, 2: state
+};
+
+// What waves [0, w) (REV: (w, last]) of the workgroup make of the state at its edge; all of them with w = kWaves (REV: -1).
 template <int VEC, bool REV>
-__device__ __forceinline__ void join(const float (&lA)[kWaves][kWave * VEC], const float (&lH)[kWaves][kWave * VEC], int w,
-                                     int lane, float (&A)[VEC], float (&H)[VEC]) {
+__device__ __forceinline__ void join(const Shared<VEC>& s, int w, int lane, float (&A)[VEC], float (&H)[VEC]) {
 #pragma unroll
     for (int i = 0; i < VEC; ++i) A[i] = 1.0f, H[i] = 0.0f;
     for (int x = REV ? kWaves - 1 : 0; REV ? x > w : x < w; x += REV ? -1 : 1)
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            const float xa = lA[x][lane * VEC + i];
-            H[i] = fmaf(xa, H[i], lH[x][lane * VEC + i]);
+            const float xa = s.A[x][lane * VEC + i];
+            H[i] = fmaf(xa, H[i], s.H[x][lane * VEC + i]);
             A[i] *= xa;
         }
 }
 
-// A and H (REV: C) of every tile.
+__device__ __forceinline__ uint32_t word_of(float x) {
+    const uint32_t b = __float_as_uint(x);
+    return b == kUnset ? 0x7fc00000u : b;
+}
+
+// x and y of the steps (k and v forward, q and dy backward) -> A and H (C) of the wave's rows, into LDS.
 template <typename T, int VEC, bool SHARED, bool REV>
-__global__ __launch_bounds__(kWaves * kWave) void glr_sum_kernel(GlrArgs a) {
+__device__ __forceinline__ void sum_rows(Shared<VEC>& s, const typename Pack<T, VEC>::Raw (&x)[kRowsPerWave],
+                                         const typename Pack<T, VEC>::Raw (&y)[kRowsPerWave], const float (&ga)[kRowsPerWave][VEC],
+                                         const Place& p, int n) {
     using P = Pack<T, VEC>;
-    using IO = Io<T, VEC, SHARED>;
-    __shared__ float lA[kWaves][kWave * VEC], lH[kWaves][kWave * VEC];
-    const Place p = place<VEC>(a);
-    const int64_t at = p.c * T::kBytes, gat = p.c / a.group * T::kBytes;
-    typename P::Raw x[kRowsPerWave], y[kRowsPerWave];
-    typename IO::G::Raw g[kRowsPerWave];
-    load_rows<P>(x, REV ? a.q : a.k, a, p, at);
-    load_rows<P>(y, REV ? a.dy : a.v, a, p, at);
-    load_rows<typename IO::G>(g, a.g, a, p, gat);
     float A[VEC], H[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) A[i] = 1.0f, H[i] = 0.0f;
 #pragma unroll
     for (int j = 0; j < kRowsPerWave; ++j) {
         const int r = REV ? kRowsPerWave - 1 - j : j;
-        if (r < p.rows) {
-            float fx[VEC], fy[VEC], ga[VEC];
-            P::unpack(x[r], fx);
-            P::unpack(y[r], fy);
-            IO::gates(g[r], ga);
+        float fx[VEC], fy[VEC];
+        P::unpack(x[r], fx);
+        P::unpack(y[r], fy);
+        if (r < n)
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                H[i] = REV ? ga[i] * fmaf(fx[i], fy[i], H[i]) : fmaf(ga[i], H[i], fx[i] * fy[i]);
-                A[i] *= ga[i];
+                H[i] = REV ? ga[r][i] * fmaf(fx[i], fy[i], H[i]) : fmaf(ga[r][i], H[i], fx[i] * fy[i]);
+                A[i] *= ga[r][i];
             }
-        }
     }
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) lA[p.w][p.lane * VEC + i] = A[i], lH[p.w][p.lane * VEC + i] = H[i];
-    __syncthreads();
-    if (p.w == (REV ? 0 : kWaves - 1) && p.there) {
-        float eA[VEC], eH[VEC];
-        join<VEC, REV>(lA, lH, p.w, p.lane, eA, eH);
+    for (int i = 0; i < VEC; ++i) s.A[p.w][p.lane * VEC + i] = A[i], s.H[p.w][p.lane * VEC + i] = H[i];
+}
+
+// The wave's sums of any tile, row by row from memory: sum_rows' operations in few registers.
+template <typename T, int VEC, bool SHARED, bool REV>
+__device__ __forceinline__ void sum_tile(Shared<VEC>& s, const GlrArgs& a, const Place& p, int tile) {
+    using P = Pack<T, VEC>;
+    using IO = Io<T, VEC, SHARED>;
+    const Rows at = rows_of(a, tile, p.w);
+    const Src &sx = REV ? a.q : a.k, &sy = REV ? a.dy : a.v;
+    float A[VEC], H[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) A[i] = 1.0f, H[i] = 0.0f;
+#pragma unroll 1
+    for (int j = 0; j < at.n; ++j) {
+        const int64_t t = at.first + (REV ? at.n - 1 - j : j);
+        float fx[VEC], fy[VEC], ga[VEC];
+        P::unpack(P::load(sx.p + p.b * sx.bstride + t * sx.rstride + p.c * T::kBytes), fx);
+        P::unpack(P::load(sy.p + p.b * sy.bstride + t * sy.rstride + p.c * T::kBytes), fy);
+        IO::gates(IO::G::load(a.g.p + p.b * a.g.bstride + t * a.g.rstride + p.c / a.group * T::kBytes), ga);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            const int64_t o = (p.b * a.tiles + p.tile) * a.D + p.c + i;
-            a.A[o] = A[i] * eA[i];
-            a.H[o] = fmaf(A[i], eH[i], H[i]);
+            H[i] = REV ? ga[i] * fmaf(fx[i], fy[i], H[i]) : fmaf(ga[i], H[i], fx[i] * fy[i]);
+            A[i] *= ga[i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) s.A[p.w][p.lane * VEC + i] = A[i], s.H[p.w][p.lane * VEC + i] = H[i];
+}
+
+// The state at the tile's edge, with the waves' sums of the tile in LDS (and a barrier behind them); publishes the tile's own.
+template <typename T, int VEC, bool SHARED, bool REV>
+__device__ __forceinline__ void edge_of(Shared<VEC>& s, const GlrArgs& a, const Place& p, float (&S)[VEC]) {
+    const int64_t per = a.B * a.D, here = p.b * a.D + p.c;
+    float tA[VEC], tH[VEC];
+    const bool last = p.order == a.tiles - 1;
+    if (p.w == 0) {
+        join<VEC, REV>(s, REV ? -1 : kWaves, p.lane, tA, tH);
+        if (p.order > 0 && !last && p.there)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                __hip_atomic_store(a.sums + p.order * per + here + i, word_of(tA[i]) | (uint64_t)word_of(tH[i]) << 32,
+                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) S[i] = a.edge_in ? a.edge_in[here + i] : 0.0f;
+    if (p.order > 0) {
+        int have[2] = {0, 0};
+        int base = -1;  // the nearest tile whose state is there
+        for (int look = 0; look < a.polls; ++look) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int slot = p.w + x * kWaves, of = p.order - 1 - slot;
+                if (of >= 0 && have[x] < 2) {
+                    uint32_t st[VEC];
+                    uint64_t su[VEC];
+                    bool state = true, sums = true;
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) {
+                        st[i] = __hip_atomic_load(a.states + of * per + here + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                        su[i] = have[x] || of == 0 ? 0 : __hip_atomic_load(a.sums + of * per + here + i, __ATOMIC_RELAXED,
+                                                                           __HIP_MEMORY_SCOPE_AGENT);
+                        state = state && st[i] != kUnset;
+                        sums = sums && (uint32_t)su[i] != kUnset && (uint32_t)(su[i] >> 32) != kUnset;
+                    }
+                    if (__all(state || !p.there)) {
+                        have[x] = 2;
+#pragma unroll
+                        for (int i = 0; i < VEC; ++i) s.wH[slot][p.lane * VEC + i] = __uint_as_float(st[i]);
+                    } else if (have[x] == 0 && of > 0 && __all(sums || !p.there)) {
+                        have[x] = 1;
+#pragma unroll
+                        for (int i = 0; i < VEC; ++i) {
+                            s.wA[slot][p.lane * VEC + i] = __uint_as_float((uint32_t)su[i]);
+                            s.wH[slot][p.lane * VEC + i] = __uint_as_float((uint32_t)(su[i] >> 32));
+                        }
+                    }
+                }
+                if (p.lane == 0) s.found[look & 1][slot] = have[x];
+            }
+            __syncthreads();
+            // every wave sees the same and decides the same
+            base = -1;
+            for (int x = 0; x < kWindow; ++x) {
+                const int f = s.found[look & 1][x];
+                if (f != 1) {
+                    base = f == 2 ? x : -1;
+                    break;
+                }
+            }
+            if (base >= 0) break;
+            __builtin_amdgcn_s_sleep(2);
+        }
+        if (base >= 0) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) S[i] = s.wH[base][p.lane * VEC + i];
+            for (int x = base - 1; x >= 0; --x)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) S[i] = fmaf(s.wA[x][p.lane * VEC + i], S[i], s.wH[x][p.lane * VEC + i]);
+        } else {
+            float wA[VEC], wH[VEC];
+            for (int x = 0; x < p.order; ++x) {
+                __syncthreads();
+                sum_tile<T, VEC, SHARED, REV>(s, a, p, REV ? a.tiles - 1 - x : x);
+                __syncthreads();
+                join<VEC, REV>(s, REV ? -1 : kWaves, p.lane, wA, wH);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) S[i] = fmaf(wA[i], S[i], wH[i]);
+            }
+            __syncthreads();
+            sum_tile<T, VEC, SHARED, REV>(s, a, p, p.tile);  // the waves' sums again
+            __syncthreads();
+        }
+    }
+    if (p.w == 0 && p.there) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const float e = fmaf(tA[i], S[i], tH[i]);
+            if (!last) __hip_atomic_store(a.states + p.order * per + here + i, word_of(e), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            else if (a.edge_out) a.edge_out[here + i] = e;
         }
     }
 }
 
-// marks[b][tile][c]: the state before (REV: c behind) each tile; `out`: what comes out at the end.  A lane per channel.
-template <bool REV>
-__global__ __launch_bounds__(256) void glr_scan_kernel(const float* A, const float* H, const float* in, float* marks, float* out,
-                                                       int64_t B, int64_t tiles, int64_t D) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= B * D) return;
-    const int64_t b = i / D, c = i % D;
-    float s = in ? in[i] : 0.0f;
-    for (int64_t j = 0; j < tiles; ++j) {
-        const int64_t o = (b * tiles + (REV ? tiles - 1 - j : j)) * D + c;
-        marks[o] = s;
-        s = fmaf(A[o], s, H[o]);
-    }
-    if (out) out[i] = s;
+constexpr int kMarks = 4;  // 16-byte pieces per lane
+__global__ __launch_bounds__(256) void glr_unset_kernel(uint4* rec, int64_t n) {
+    const int64_t i0 = (int64_t)blockIdx.x * 256 * kMarks + threadIdx.x;
+#pragma unroll
+    for (int x = 0; x < kMarks; ++x)
+        if (i0 + 256 * x < n) store_words<4>(rec + i0 + 256 * x, Words<4>{{kUnset, kUnset, kUnset, kUnset}});
 }
 
-// y of every tile from the state before it.
-template <typename T, int VEC, bool SHARED>
+// The state of sequences without steps goes on as it is.
+__global__ __launch_bounds__(256) void glr_hand_on_kernel(const float* in, float* out, int64_t n) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < n) out[i] = in ? in[i] : 0.0f;
+}
+
+// Y: q comes in and y goes out; else the states alone.
+template <typename T, int VEC, bool SHARED, bool Y>
 __global__ __launch_bounds__(kWaves * kWave) void glr_fwd_kernel(GlrArgs a) {
     using P = Pack<T, VEC>;
     using IO = Io<T, VEC, SHARED>;
-    __shared__ float lA[kWaves][kWave * VEC], lH[kWaves][kWave * VEC];
-    const Place p = place<VEC>(a);
-    const int64_t at = p.c * T::kBytes, gat = p.c / a.group * T::kBytes;
+    __shared__ Shared<VEC> s;
+    const Place p = place<VEC, false>(a);
+    const Rows at = rows_of(a, p.tile, p.w);
+    const int64_t lane_bytes = p.c * T::kBytes;
     typename P::Raw q[kRowsPerWave], k[kRowsPerWave], v[kRowsPerWave];
     typename IO::G::Raw g[kRowsPerWave];
-    load_rows<P>(k, a.k, a, p, at);
-    load_rows<P>(v, a.v, a, p, at);
-    load_rows<typename IO::G>(g, a.g, a, p, gat);
-    load_rows<P>(q, a.q, a, p, at);
-    float A[VEC], H[VEC], pa[kRowsPerWave][VEC], ph[kRowsPerWave][VEC];
+    load_rows<P>(k, a.k, a, p, at, lane_bytes);
+    load_rows<P>(v, a.v, a, p, at, lane_bytes);
+    load_rows<typename IO::G>(g, a.g, a, p, at, p.c / a.group * T::kBytes);
+    if constexpr (Y) load_rows<P>(q, a.q, a, p, at, lane_bytes);
+    float ga[kRowsPerWave][VEC];
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) A[i] = 1.0f, H[i] = 0.0f;
-#pragma unroll
-    for (int r = 0; r < kRowsPerWave; ++r) {
-        float fk[VEC], fv[VEC], ga[VEC];
-        P::unpack(k[r], fk);
-        P::unpack(v[r], fv);
-        IO::gates(g[r], ga);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            if (r < p.rows) {
-                H[i] = fmaf(ga[i], H[i], fk[i] * fv[i]);
-                A[i] *= ga[i];
-            }
-            pa[r][i] = A[i];
-            ph[r][i] = H[i];
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) lA[p.w][p.lane * VEC + i] = A[i], lH[p.w][p.lane * VEC + i] = H[i];
+    for (int r = 0; r < kRowsPerWave; ++r) IO::gates(g[r], ga[r]);
+    sum_rows<T, VEC, SHARED, false>(s, k, v, ga, p, at.n);
     __syncthreads();
     float S[VEC], eA[VEC], eH[VEC];
-    join<VEC, false>(lA, lH, p.w, p.lane, eA, eH);
+    edge_of<T, VEC, SHARED, false>(s, a, p, S);
+    if (a.marks_out && p.w == 0 && p.there)
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) S[i] = fmaf(eA[i], a.marks[(p.b * a.tiles + p.tile) * a.D + p.c + i], eH[i]);
-    if (!p.there) return;
-    char* yp = a.y + ((p.b * a.L + p.row0) * a.D + p.c) * T::kBytes;
+        for (int i = 0; i < VEC; ++i) a.marks_out[(p.b * a.tiles + p.tile) * a.D + p.c + i] = S[i];
+    if (!Y || !p.there) return;
+    join<VEC, false>(s, p.w, p.lane, eA, eH);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) S[i] = fmaf(eA[i], S[i], eH[i]);
+    char* yp = a.y + ((p.b * a.L + at.first) * a.D + p.c) * T::kBytes;
 #pragma unroll
     for (int r = 0; r < kRowsPerWave; ++r) {
-        float fq[VEC];
+        float fq[VEC], fk[VEC], fv[VEC];
         P::unpack(q[r], fq);
+        P::unpack(k[r], fk);
+        P::unpack(v[r], fv);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) fq[i] *= fmaf(pa[r][i], S[i], ph[r][i]);
-        if (r < p.rows) P::store_nt(yp + (int64_t)r * a.D * T::kBytes, P::pack(fq));
+        for (int i = 0; i < VEC; ++i) {
+            S[i] = fmaf(ga[r][i], S[i], fk[i] * fv[i]);
+            fq[i] *= S[i];
+        }
+        if (r < at.n) P::store_nt(yp + (int64_t)r * a.D * T::kBytes, P::pack(fq));
     }
 }
 
@@ -216,57 +348,35 @@ template <typename T, int VEC, bool SHARED>
 __global__ __launch_bounds__(kWaves * kWave) void glr_bwd_kernel(GlrArgs a) {
     using P = Pack<T, VEC>;
     using IO = Io<T, VEC, SHARED>;
-    __shared__ float lA[kWaves][kWave * VEC], lH[kWaves][kWave * VEC], lC[kWaves][kWave * VEC];
-    const Place p = place<VEC>(a);
-    const int64_t at = p.c * T::kBytes, gat = p.c / a.group * T::kBytes;
+    __shared__ Shared<VEC> s;
+    const Place p = place<VEC, true>(a);
+    const Rows at = rows_of(a, p.tile, p.w);
+    const int64_t lane_bytes = p.c * T::kBytes;
     typename P::Raw q[kRowsPerWave], k[kRowsPerWave], v[kRowsPerWave], dy[kRowsPerWave];
     typename IO::G::Raw g[kRowsPerWave];
-    load_rows<P>(k, a.k, a, p, at);
-    load_rows<P>(v, a.v, a, p, at);
-    load_rows<typename IO::G>(g, a.g, a, p, gat);
-    load_rows<P>(q, a.q, a, p, at);
-    load_rows<P>(dy, a.dy, a, p, at);
-    float A[VEC], H[VEC], C[VEC], ga[kRowsPerWave][VEC];
+    load_rows<P>(q, a.q, a, p, at, lane_bytes);
+    load_rows<P>(dy, a.dy, a, p, at, lane_bytes);
+    load_rows<typename IO::G>(g, a.g, a, p, at, p.c / a.group * T::kBytes);
+    load_rows<P>(k, a.k, a, p, at, lane_bytes);
+    load_rows<P>(v, a.v, a, p, at, lane_bytes);
+    float ga[kRowsPerWave][VEC];
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) A[i] = 1.0f, H[i] = 0.0f, C[i] = 0.0f;
-#pragma unroll
-    for (int r = 0; r < kRowsPerWave; ++r) {
-        float fk[VEC], fv[VEC];
-        P::unpack(k[r], fk);
-        P::unpack(v[r], fv);
-        IO::gates(g[r], ga[r]);
-        if (r < p.rows)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                H[i] = fmaf(ga[r][i], H[i], fk[i] * fv[i]);
-                A[i] *= ga[r][i];
-            }
-    }
-#pragma unroll
-    for (int r = kRowsPerWave - 1; r >= 0; --r) {
-        float fq[VEC], fy[VEC];
-        P::unpack(q[r], fq);
-        P::unpack(dy[r], fy);
-        if (r < p.rows)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) C[i] = ga[r][i] * fmaf(fq[i], fy[i], C[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-        const int o = p.lane * VEC + i;
-        lA[p.w][o] = A[i], lH[p.w][o] = H[i], lC[p.w][o] = C[i];
-    }
-    __syncthreads();
+    for (int r = 0; r < kRowsPerWave; ++r) IO::gates(g[r], ga[r]);
     float S[VEC], R[VEC], eA[VEC], eH[VEC];
-    const int64_t m0 = (p.b * a.tiles + p.tile) * a.D + p.c;
-    join<VEC, false>(lA, lH, p.w, p.lane, eA, eH);
+    sum_rows<T, VEC, SHARED, true>(s, q, dy, ga, p, at.n);
+    __syncthreads();
+    edge_of<T, VEC, SHARED, true>(s, a, p, R);
+    join<VEC, true>(s, p.w, p.lane, eA, eH);
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) S[i] = fmaf(eA[i], a.marks[m0 + i], eH[i]);
-    join<VEC, true>(lA, lC, p.w, p.lane, eA, eH);
+    for (int i = 0; i < VEC; ++i) R[i] = fmaf(eA[i], R[i], eH[i]);
+    __syncthreads();
+    sum_rows<T, VEC, SHARED, false>(s, k, v, ga, p, at.n);
+    __syncthreads();
+    join<VEC, false>(s, p.w, p.lane, eA, eH);
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) R[i] = fmaf(eA[i], a.rmarks[m0 + i], eH[i]);
+    for (int i = 0; i < VEC; ++i) S[i] = fmaf(eA[i], a.marks[(p.b * a.tiles + p.tile) * a.D + p.c + i], eH[i]);
 
-    const int64_t row = p.b * a.L + p.row0;
+    const int64_t row = p.b * a.L + at.first;
     const int64_t o0 = (row * a.D + p.c) * T::kBytes;
     float kept[kRowsPerWave][VEC];  // a[t] s[t-1]
 #pragma unroll
@@ -281,11 +391,11 @@ __global__ __launch_bounds__(kWaves * kWave) void glr_bwd_kernel(GlrArgs a) {
             S[i] = fmaf(fk[i], fv[i], kept[r][i]);
             fy[i] *= S[i];
         }
-        if (r < p.rows && p.there) P::store_nt(a.dq + o0 + (int64_t)r * a.D * T::kBytes, P::pack(fy));
+        if (r < at.n && p.there) P::store_nt(a.dq + o0 + (int64_t)r * a.D * T::kBytes, P::pack(fy));
     }
 #pragma unroll
     for (int r = kRowsPerWave - 1; r >= 0; --r) {
-        if (r >= p.rows) continue;  // the same for all lanes
+        if (r >= at.n) continue;  // the same for all lanes
         float fk[VEC], fv[VEC], fq[VEC], fy[VEC], dg[VEC];
         P::unpack(k[r], fk);
         P::unpack(v[r], fv);
@@ -309,16 +419,16 @@ __global__ __launch_bounds__(kWaves * kWave) void glr_bwd_kernel(GlrArgs a) {
             if (p.there) P::store_nt(a.dg + o, P::pack(dg));
         } else {
             // the part's lanes are neighbours: halving distances, the same order in every call
-            float s = dg[0];
+            float sum = dg[0];
 #pragma unroll
-            for (int i = 1; i < VEC; ++i) s += dg[i];
+            for (int i = 1; i < VEC; ++i) sum += dg[i];
             const int lanes = a.part / VEC;
-            for (int d = lanes / 2; d > 0; d /= 2) s += __shfl_xor(s, d, kWave);
+            for (int d = lanes / 2; d > 0; d /= 2) sum += __shfl_xor(sum, d, kWave);
             if (p.there && p.lane % lanes == 0) {
-                const float one[1] = {s};
+                const float one[1] = {sum};
                 const int64_t n = (row + r) * (a.D / a.part) + p.c / a.part;
                 if (a.part == a.group) Pack<T, 1>::store_nt(a.dg + n * T::kBytes, Pack<T, 1>::pack(one));
-                else a.dg_parts[n] = s;
+                else a.dg_parts[n] = sum;
             }
         }
     }
@@ -362,23 +472,12 @@ __global__ __launch_bounds__(256) void glr_step_kernel(const char* q, const char
 
 template <typename T, int VEC, bool SHARED>
 struct Kernels {
-    static hy_status forward(GlrArgs& a, const GlrPtrs& p, uint32_t grid, float* marks, int64_t B, hipStream_t st) {
-        const dim3 g(grid), b(kWaves * kWave);
-        hy_status rc = launch_kernel(glr_sum_kernel<T, VEC, SHARED, false>, g, b, st, a);
-        if (rc == HY_OK)
-            rc = launch_kernel(glr_scan_kernel<false>, dim3((uint32_t)((B * a.D + 255) / 256)), dim3(256), st, (const float*)a.A,
-                               (const float*)a.H, p.state_in, marks, p.state_out, B, (int64_t)a.tiles, a.D);
-        if (rc == HY_OK && p.y) rc = launch_kernel(glr_fwd_kernel<T, VEC, SHARED>, g, b, st, a);
-        return rc;
+    static hy_status forward(const GlrArgs& a, uint32_t grid, hipStream_t st) {
+        return a.y ? launch_kernel(glr_fwd_kernel<T, VEC, SHARED, true>, dim3(grid), dim3(kWaves * kWave), st, a)
+                   : launch_kernel(glr_fwd_kernel<T, VEC, SHARED, false>, dim3(grid), dim3(kWaves * kWave), st, a);
     }
-    static hy_status backward(GlrArgs& a, const GlrPtrs& p, uint32_t grid, float* rmarks, int64_t B, hipStream_t st) {
-        const dim3 g(grid), b(kWaves * kWave);
-        hy_status rc = launch_kernel(glr_sum_kernel<T, VEC, SHARED, true>, g, b, st, a);
-        if (rc == HY_OK)
-            rc = launch_kernel(glr_scan_kernel<true>, dim3((uint32_t)((B * a.D + 255) / 256)), dim3(256), st, (const float*)a.A,
-                               (const float*)a.H, p.dstate_out, rmarks, p.dstate_in, B, (int64_t)a.tiles, a.D);
-        if (rc == HY_OK) rc = launch_kernel(glr_bwd_kernel<T, VEC, SHARED>, g, b, st, a);
-        return rc;
+    static hy_status backward(const GlrArgs& a, uint32_t grid, hipStream_t st) {
+        return launch_kernel(glr_bwd_kernel<T, VEC, SHARED>, dim3(grid), dim3(kWaves * kWave), st, a);
     }
     static hy_status step(const GlrPtrs& p, int64_t n, int32_t group, hipStream_t st) {
         const int64_t per = 256 * VEC;
@@ -426,7 +525,7 @@ GlrArgs args_of(const GlrPtrs& p, const GlrShape& s, int64_t* grid) {
     GlrArgs a{};
     a.q = src(p.q, kGlrQ), a.k = src(p.k, kGlrK), a.v = src(p.v, kGlrV), a.g = src(p.g, kGlrG), a.dy = src(p.dy, kGlrDy);
     a.y = (char*)p.y, a.dq = (char*)p.dq, a.dk = (char*)p.dk, a.dv = (char*)p.dv, a.dg = (char*)p.dg;
-    a.L = s.L, a.D = s.D, a.group = s.group;
+    a.B = s.B, a.L = s.L, a.D = s.D, a.group = s.group;
     const int64_t width = in_pairs(s) ? 2 * kWave : kWave, tiles = tiles_of(s), ncb = (s.D + width - 1) / width;
     *grid = tiles <= INT32_MAX && ncb <= INT32_MAX && s.B <= INT32_MAX / tiles / ncb ? s.B * tiles * ncb : -1;
     a.tiles = (int32_t)tiles, a.ncb = (int32_t)ncb;
@@ -434,22 +533,33 @@ GlrArgs args_of(const GlrPtrs& p, const GlrShape& s, int64_t* grid) {
     return a;
 }
 
-// No steps: the state goes on as it is.
 hy_status hand_on(const float* in, float* out, const GlrShape& s, hipStream_t st) {
-    return launch_kernel(glr_scan_kernel<false>, dim3((uint32_t)((s.B * s.D + 255) / 256)), dim3(256), st, (const float*)nullptr,
-                         (const float*)nullptr, in, (float*)nullptr, out, s.B, (int64_t)0, s.D);
+    return launch_kernel(glr_hand_on_kernel, dim3((uint32_t)((s.B * s.D + 255) / 256)), dim3(256), st, in, out, s.B * s.D);
+}
+
+// Records of the tiles: none where a sequence is one tile.
+int64_t record_bytes(const GlrShape& s) { return tiles_of(s) > 1 ? round16(s.B * tiles_of(s) * s.D * 12) : 0; }
+
+hy_status take_records(GlrArgs& a, const GlrShape& s, void* ws, hipStream_t st) {
+    const int64_t bytes = record_bytes(s), n = s.B * tiles_of(s) * s.D;
+    a.sums = static_cast<uint64_t*>(ws);
+    a.states = reinterpret_cast<uint32_t*>(a.sums + n);
+    a.polls = tuning().glr_wait == 1 ? 0 : kPolls;
+    if (bytes == 0) return HY_OK;
+    const int64_t per = 256 * kMarks * 16;
+    if ((bytes + per - 1) / per > INT32_MAX) return HY_ERR_UNSUPPORTED;
+    return launch_kernel(glr_unset_kernel, dim3((uint32_t)((bytes + per - 1) / per)), dim3(256), st, static_cast<uint4*>(ws), bytes / 16);
 }
 
 }  // namespace
 
-// A, H and the marks (where the caller does not take them).
-int64_t glr_fwd_workspace_bytes(const GlrShape& s) { return 3 * round16(s.B * tiles_of(s) * s.D * 4); }
+int64_t glr_fwd_workspace_bytes(const GlrShape& s) { return record_bytes(s); }
 
-// The same (a fourth array for the states where no marks come in), and the parts of dg, as many as lanes of one channel have.
+// Records, the states where no marks come in, and the parts of dg, as many as lanes of one channel have.
 int64_t glr_bwd_workspace_bytes(const GlrShape& s, bool marks) {
-    const int64_t n = round16(s.B * tiles_of(s) * s.D * 4);
     const int32_t part = part_of(s.group, kWave);
-    return (marks ? 3 : 4) * n + (part == s.group ? 0 : s.B * s.L * (s.D / part) * 4);
+    return record_bytes(s) + (marks ? 0 : round16(s.B * tiles_of(s) * s.D * 4)) +
+           (part == s.group ? 0 : s.B * s.L * (s.D / part) * 4);
 }
 
 hy_status launch_glr_fwd(const GlrPtrs& p, const GlrShape& s, void* ws, hipStream_t st) {
@@ -457,13 +567,10 @@ hy_status launch_glr_fwd(const GlrPtrs& p, const GlrShape& s, void* ws, hipStrea
     int64_t grid;
     GlrArgs a = args_of(p, s, &grid);
     if (grid < 0) return HY_ERR_UNSUPPORTED;
-    const int64_t n = round16(s.B * tiles_of(s) * s.D * 4);
-    char* w = static_cast<char*>(ws);
-    a.A = (float*)w, a.H = (float*)(w + n);
-    float* marks = p.marks_out ? p.marks_out : (float*)(w + 2 * n);
-    a.marks = marks;
-    return by_kind(s.dtype, in_pairs(s), s.group > 1,
-                   [&](auto kernels) { return kernels.forward(a, p, (uint32_t)grid, marks, s.B, st); });
+    a.edge_in = p.state_in, a.edge_out = p.state_out, a.marks_out = p.marks_out;
+    hy_status rc = take_records(a, s, ws, st);
+    if (rc != HY_OK) return rc;
+    return by_kind(s.dtype, in_pairs(s), s.group > 1, [&](auto kernels) { return kernels.forward(a, (uint32_t)grid, st); });
 }
 
 hy_status launch_glr_bwd(const GlrPtrs& p, const GlrShape& s, void* ws, hipStream_t st) {
@@ -471,28 +578,22 @@ hy_status launch_glr_bwd(const GlrPtrs& p, const GlrShape& s, void* ws, hipStrea
     int64_t grid;
     GlrArgs a = args_of(p, s, &grid);
     if (grid < 0) return HY_ERR_UNSUPPORTED;
-    const int64_t n = round16(s.B * tiles_of(s) * s.D * 4);
-    char* w = static_cast<char*>(ws);
-    a.A = (float*)w, a.H = (float*)(w + n);
-    float* rmarks = (float*)(w + 2 * n);
-    a.rmarks = rmarks;
-    w += 3 * n;
-    hy_status rc = HY_OK;
-    if (p.marks) {
-        a.marks = p.marks;
-    } else {
-        float* marks = (float*)w;
-        w += n;
-        a.marks = marks;
+    char* rest = static_cast<char*>(ws) + record_bytes(s);
+    a.marks = p.marks;
+    if (!p.marks) {
+        float* marks = reinterpret_cast<float*>(rest);
+        rest += round16(s.B * tiles_of(s) * s.D * 4);
         GlrPtrs f = p;  // the states alone
-        f.y = nullptr, f.state_out = nullptr;
-        rc = by_kind(s.dtype, in_pairs(s), s.group > 1,
-                     [&](auto kernels) { return kernels.forward(a, f, (uint32_t)grid, marks, s.B, st); });
+        f.y = nullptr, f.state_out = nullptr, f.marks_out = marks;
+        hy_status rc = launch_glr_fwd(f, s, ws, st);
+        if (rc != HY_OK) return rc;
+        a.marks = marks;
     }
-    a.dg_parts = (float*)w;
+    a.dg_parts = reinterpret_cast<float*>(rest);
+    a.edge_in = p.dstate_out, a.edge_out = p.dstate_in;
+    hy_status rc = take_records(a, s, ws, st);
     if (rc == HY_OK)
-        rc = by_kind(s.dtype, in_pairs(s), s.group > 1,
-                     [&](auto kernels) { return kernels.backward(a, p, (uint32_t)grid, rmarks, s.B, st); });
+        rc = by_kind(s.dtype, in_pairs(s), s.group > 1, [&](auto kernels) { return kernels.backward(a, (uint32_t)grid, st); });
     if (rc == HY_OK && a.part != s.group) {
         const int64_t out = s.B * s.L * (s.D / s.group);
         if ((out + 255) / 256 > INT32_MAX) return HY_ERR_UNSUPPORTED;

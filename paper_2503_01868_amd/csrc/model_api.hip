@@ -265,6 +265,7 @@ int64_t hyena_glr_bwd_workspace_bytes(int64_t B, int64_t L, int64_t D, int32_t g
 hy_status hyena_glr_fwd(const void* q, const void* k, const void* v, const void* g, const float* state_in, void* y,
                         float* state_out, float* marks, const int64_t* strides, void* workspace, int64_t workspace_bytes,
                         int64_t B, int64_t L, int64_t D, int32_t group, int32_t dtype, void* hip_stream) {
+    TuningSnapshot snap;
     hy_status rc = check_glr(B, L, D, group, dtype);
     if (rc != HY_OK) return rc;
     if (!empty(B, L, D) && (!q || !k || !v || !g || !y)) return HY_ERR_NULL;
@@ -296,6 +297,7 @@ hy_status hyena_glr_bwd(const void* dy, const void* q, const void* k, const void
                         const float* state_in, const float* dstate_out, void* dq, void* dk, void* dv, void* dg,
                         float* dstate_in, const int64_t* strides, void* workspace, int64_t workspace_bytes, int64_t B, int64_t L,
                         int64_t D, int32_t group, int32_t dtype, void* hip_stream) {
+    TuningSnapshot snap;
     hy_status rc = check_glr(B, L, D, group, dtype);
     if (rc != HY_OK) return rc;
     if (!empty(B, L, D) && (!dy || !q || !k || !v || !g || !dq || !dk || !dv || !dg)) return HY_ERR_NULL;

@@ -83,11 +83,32 @@ def test_many_tiles_are_deterministic(dtype):
     for _ in range(3):
         y, s, marks = hy.hyena_glr_fwd_carry(q, k, v, g, 1, state_in=state, want_marks=True)
         outs.append((y, s) + hy.hyena_glr_bwd(dy, q, k, v, g, 1, marks=marks, dstate_out=dstate, want_dstate=True))
+    for other in outs[1:]:
+        for a, b in zip(outs[0], other):
+            assert torch.equal(a, b)
     close(outs[0][0], ry, dtype, "y")
     close(outs[0][1], rs, "f32", "state")
     ref = model_ref.glr_grads(wide(dy), *(wide(x) for x in (q, k, v, g)), 1, wide(state), wide(dstate))
     for a, r, n in zip(outs[0][2:], ref, ("dq", "dk", "dv", "dg", "dstate")):
         close(a, r, "f32" if n == "dstate" else dtype, n)
+
+
+@pytest.mark.parametrize("dtype,group", [("f32", 1), ("bf16", 16), ("bf16", 3)])
+def test_tiles_that_do_not_wait_give_the_same_bits(dtype, group):
+    q, k, v, g, dy, state, dstate = make(6, 2, 900, 192, group, dtype)
+
+    def step():
+        y, s, marks = hy.hyena_glr_fwd_carry(q, k, v, g, group, state_in=state, want_marks=True)
+        return (y, s, marks) + hy.hyena_glr_bwd(dy, q, k, v, g, group, marks=marks, dstate_out=dstate, want_dstate=True)
+
+    waited = step()
+    binding.set_option("glr_wait", 1)
+    try:
+        alone = step()
+    finally:
+        binding.set_option("glr_wait", 0)
+    for a, b in zip(waited, alone):
+        assert torch.equal(a, b)
 
 
 @pytest.mark.parametrize("dtype,D,group", [("bf16", 256, 1), ("bf16", 250, 5), ("f32", 128, 16)])
