@@ -284,7 +284,7 @@ struct GlrShape {
     int32_t group;
     hy_dtype dtype;
     int64_t bstride[5], rstride[5];
-    bool odd_start = false;  // an input begins where no two elements may be loaded together
+    int start_align = 4;  // elements, 1, 2 or 4: every input begins at a multiple
 };
 int64_t glr_fwd_workspace_bytes(const GlrShape& s);
 int64_t glr_bwd_workspace_bytes(const GlrShape& s, bool marks);

@@ -62,13 +62,14 @@ hy_status all_aligned(const Range* r, int n) {
     return HY_OK;
 }
 
-// Inputs may be views that begin at any element; from odd ones a lane takes one channel at a time.
+// Inputs may be views that begin at any element: how many a lane can load together.
 hy_status take_starts(GlrShape& s, const Range* r, int n, int gate) {
     const uintptr_t e = (uintptr_t)size_of(s.dtype);
     for (int i = 0; i < n; ++i) {
         const uintptr_t at = reinterpret_cast<uintptr_t>(r[i].p);
         if (at % e != 0) return HY_ERR_ALIGN;
-        if (at % (2 * e) != 0 && (i != gate || s.group == 1)) s.odd_start = true;
+        if (i != gate || s.group == 1)
+            while (at % (s.start_align * e) != 0) s.start_align /= 2;
     }
     return HY_OK;
 }
