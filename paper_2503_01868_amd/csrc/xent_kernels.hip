@@ -52,24 +52,51 @@ __global__ __launch_bounds__(256) void pack_kernel(const char* src, uint16_t* ds
     for (int x = 0; x < (T::kBytes == 4 ? 3 : 1); ++x) dst[x * rows * ld + i] = part[x];
 }
 
-// Rows of D values -> planes of D rows of `ld` bf16 numbers; zeros behind the last row, and for the rows whose target is none.
+// Rows of D values -> planes of D rows of `ld` (a multiple of 64) bf16 numbers; zeros behind the last row, and for the rows whose
+// target is none.  Pieces of 64 x 64 through LDS, 8 values a lane.
 template <typename T>
 __global__ __launch_bounds__(256) void turn_kernel(const char* src, uint16_t* dst, int64_t rows, int64_t D, int64_t ld,
                                                    const int64_t* target, int64_t V) {
-    constexpr int N = T::kBytes == 4 ? 3 : 1;
-    __shared__ uint16_t s[N][64][65];
+    constexpr int N = T::kBytes == 4 ? 3 : 1, kPitch = 72;
+    __shared__ __attribute__((aligned(16))) uint16_t s[N][64][kPitch];
     const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;
-    const int x = threadIdx.x % 64;
-    for (int y = threadIdx.x / 64; y < 64; y += 4) {
-        uint16_t part[3] = {};
-        const int64_t r = r0 + y;
-        if (r < rows && c0 + x < D && (!target || (target[r] >= 0 && target[r] < V))) bits_of<T>(src + (r * D + c0 + x) * T::kBytes, part);
-        for (int i = 0; i < N; ++i) s[i][y][x] = part[i];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int y = threadIdx.x / 8 + 32 * h, x = threadIdx.x % 8 * 8;
+        const int64_t r = r0 + y, c = c0 + x;
+        uint16_t part[8][3] = {};
+        if (r < rows && c < D && (!target || (target[r] >= 0 && target[r] < V))) {
+            const char* p = src + (r * D + c) * T::kBytes;
+            if (D % 8 == 0) {
+                uint4 w[T::kBytes / 2];
+#pragma unroll
+                for (int i = 0; i < T::kBytes / 2; ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) bits_of<T>(reinterpret_cast<const char*>(w) + i * T::kBytes, part[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (c + i < D) bits_of<T>(p + i * T::kBytes, part[i]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            *reinterpret_cast<uint4*>(&s[i][y][x]) = make_uint4(part[0][i] | (uint32_t)part[1][i] << 16, part[2][i] | (uint32_t)part[3][i] << 16,
+                                                                part[4][i] | (uint32_t)part[5][i] << 16, part[6][i] | (uint32_t)part[7][i] << 16);
     }
     __syncthreads();
-    for (int y = threadIdx.x / 64; y < 64; y += 4)
-        if (c0 + y < D && r0 + x < ld)
-            for (int i = 0; i < N; ++i) dst[(i * D + c0 + y) * ld + r0 + x] = s[i][x][y];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int y = threadIdx.x / 8 + 32 * h, x = threadIdx.x % 8 * 8;
+        if (c0 + y >= D) continue;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = s[i][x + 2 * j][y] | (uint32_t)s[i][x + 2 * j + 1][y] << 16;
+            *reinterpret_cast<uint4*>(dst + (i * D + c0 + y) * ld + r0 + x) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
 }
 
 struct XentArgs {
@@ -89,13 +116,24 @@ struct XentArgs {
     float* sum;               // the sum so far (not of the first piece)
     int64_t out_ld;
     bool first, last;
+    float* split;             // [splits][rows][out_ld]: where a product's k is divided among workgroups
+    int32_t splits;
 };
+
+// The target's column within a tile of `width` columns that begins at `first`; -1: it is none of them.
+__device__ __forceinline__ int column_of(int64_t target, int64_t first, int width) {
+    const int64_t c = target - first;
+    return c >= 0 && c < width ? (int)c : -1;
+}
+
+// exp as a power of two: off by 6e-8 (1 + |x|) of itself, so what is small beside the sum it goes into may be off by more.
+__device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
 // Tiles in runs of a few rows of tiles, a run of neighbours for each XCD: what its workgroups share stays in its L2.
 template <int BM, int BN>
-__device__ __forceinline__ void tile_of(const GemmArgs& g, int64_t* m0, int64_t* n0, uint32_t* tn) {
+__device__ __forceinline__ void tile_of(const GemmArgs& g, uint32_t index, int64_t* m0, int64_t* n0, uint32_t* tn) {
     constexpr uint32_t kRun = 8;
-    const uint32_t i = xcd_contiguous(blockIdx.x, (uint32_t)g.mt * (uint32_t)g.nt);
+    const uint32_t i = xcd_contiguous(index, (uint32_t)g.mt * (uint32_t)g.nt);
     const uint32_t per = kRun * (uint32_t)g.nt, first = i / per * kRun;
     const uint32_t h = (uint32_t)g.mt - first < kRun ? (uint32_t)g.mt - first : kRun;
     *tn = i % per / h;
@@ -103,32 +141,37 @@ __device__ __forceinline__ void tile_of(const GemmArgs& g, int64_t* m0, int64_t*
     *n0 = (int64_t)*tn * BN;
 }
 
-template <int BM, int BN, int MW, int NW>
+template <int BM, int BN, int MW, int NW, int ST>
 __global__ __launch_bounds__(MW * NW * kWave) void loss_kernel(XentArgs a) {
-    using G = Gemm<BM, BN, MW, NW>;
-    __shared__ __attribute__((aligned(16))) char lds[2 * G::kBytes];
+    using G = Gemm<BM, BN, MW, NW, ST>;
+    __shared__ __attribute__((aligned(16))) char lds[G::kLds];
     G t;
     int64_t m0, n0;
     uint32_t tn;
-    tile_of<BM, BN>(a.g, &m0, &n0, &tn);
-    t.run(lds, a.g, m0, n0);
+    tile_of<BM, BN>(a.g, blockIdx.x, &m0, &n0, &tn);
+    t.run(lds, a.g, m0, n0, 0, a.g.K / kGemmK * a.g.segments);
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int wm = w % MW, wn = w / MW, li = lane % 16, lq = lane / 16;
     float2(*share)[NW] = reinterpret_cast<float2(*)[NW]>(lds);
+    const int cols = a.g.b.rows - n0 < BN ? (int)(a.g.b.rows - n0) : BN, col0 = wn * G::WN + 4 * lq;
     __syncthreads();  // the tiles have been read
 #pragma unroll
     for (int i = 0; i < G::MI; ++i) {
         const int row = wm * G::WM + i * 16 + li;
         const int64_t m = m0 + row;
-        const int64_t want = m < a.g.a.rows ? a.target[m] - a.v0 : -1;  // of this piece's columns
+        const int want = m < a.g.a.rows ? column_of(a.target[m], a.v0 + n0, BN) : -1;
         float top = -INFINITY;
+        if (cols < BN)
+#pragma unroll
+            for (int j = 0; j < G::NI; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (col0 + j * 16 + r >= cols) t.acc[i][j][r] = -INFINITY;
 #pragma unroll
         for (int j = 0; j < G::NI; ++j)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int64_t n = n0 + wn * G::WN + j * 16 + 4 * lq + r;
-                if (n >= a.g.b.rows) t.acc[i][j][r] = -INFINITY;
-                else if (n == want) a.zt[m] = t.acc[i][j][r];
+                if (col0 + j * 16 + r == want) a.zt[m] = t.acc[i][j][r];
                 top = fmaxf(top, t.acc[i][j][r]);
             }
         top = fmaxf(top, __shfl_xor(top, 16, kWave));
@@ -138,7 +181,7 @@ __global__ __launch_bounds__(MW * NW * kWave) void loss_kernel(XentArgs a) {
 #pragma unroll
         for (int j = 0; j < G::NI; ++j)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sum += expf(t.acc[i][j][r] - ref);
+            for (int r = 0; r < 4; ++r) sum += fast_exp(t.acc[i][j][r] - ref);
         sum += __shfl_xor(sum, 16, kWave);
         sum += __shfl_xor(sum, 32, kWave);
         if (lq == 0) share[row][wn] = make_float2(top, sum);
@@ -149,7 +192,7 @@ __global__ __launch_bounds__(MW * NW * kWave) void loss_kernel(XentArgs a) {
         float top = -INFINITY, sum = 0.0f;
         for (int x = 0; x < NW; ++x) top = fmaxf(top, share[row][x].x);
         const float ref = top == -INFINITY ? 0.0f : top;
-        for (int x = 0; x < NW; ++x) sum += share[row][x].y * expf(share[row][x].x - ref);
+        for (int x = 0; x < NW; ++x) sum += share[row][x].y * fast_exp(share[row][x].x - ref);
         a.part[(m0 + row) * a.tiles + a.tile0 + tn] = make_float2(top, sum);
     }
 }
@@ -176,41 +219,44 @@ __global__ __launch_bounds__(256) void join_kernel(const float2* part, const flo
     }
 }
 
-template <typename T, int BM, int BN, int MW, int NW>
+template <typename T, int BM, int BN, int MW, int NW, int ST>
 __global__ __launch_bounds__(MW * NW * kWave) void grad_kernel(XentArgs a) {
-    using G = Gemm<BM, BN, MW, NW>;
+    using G = Gemm<BM, BN, MW, NW, ST>;
     constexpr int N = T::kBytes == 4 ? 3 : 1;
-    __shared__ __attribute__((aligned(16))) char lds[2 * G::kBytes];
+    __shared__ __attribute__((aligned(16))) char lds[G::kLds];
     G t;
     int64_t m0, n0;
     uint32_t tn;
-    tile_of<BM, BN>(a.g, &m0, &n0, &tn);
-    t.run(lds, a.g, m0, n0);
+    tile_of<BM, BN>(a.g, blockIdx.x, &m0, &n0, &tn);
+    t.run(lds, a.g, m0, n0, 0, a.g.K / kGemmK * a.g.segments);
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int wm = w % MW, wn = w / MW, li = lane % 16, lq = lane / 16;
-    const int64_t rows = a.g.a.rows, cols = a.g.b.rows;
+    const int64_t rows = a.g.a.rows;
+    const int cols = a.g.b.rows - n0 < BN ? (int)(a.g.b.rows - n0) : BN, col0 = wn * G::WN + 4 * lq;
 #pragma unroll
     for (int i = 0; i < G::MI; ++i) {
         const int64_t m = m0 + wm * G::WM + i * 16 + li;
-        int64_t want = -1;
+        int want = -1;
         float lse = 0.0f, d = 0.0f;
         bool counts = false;
         if (m < rows) {
-            want = a.target[m];
-            counts = want >= 0 && want < a.V;
-            want -= a.v0;
+            const int64_t v = a.target[m];
+            counts = v >= 0 && v < a.V;
+            want = column_of(v, a.v0 + n0, BN);
             lse = a.lse[m];
             d = a.dloss[m];
         }
 #pragma unroll
         for (int j = 0; j < G::NI; ++j) {
-            const int64_t n = n0 + wn * G::WN + j * 16 + 4 * lq;
+            const int col = col0 + j * 16;
+            const int64_t n = n0 + col;
             uint16_t part[4][3];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                float p = expf(t.acc[i][j][r] - lse);
-                if (n + r == want) p -= 1.0f;
-                p = counts && n + r < cols ? d * p : 0.0f;  // zeros, whatever is in the row
+                const float z = t.acc[i][j][r] - lse;
+                float p = N == 3 ? expf(z) : fast_exp(z);
+                if (col + r == want) p -= 1.0f;
+                p = counts && col + r < cols ? d * p : 0.0f;  // zeros, whatever is in the row
                 if constexpr (N == 3) parts_of(p, part[r]);
                 else part[r][0] = (uint16_t)pack_bf16x2(p, 0.0f);
             }
@@ -222,24 +268,53 @@ __global__ __launch_bounds__(MW * NW * kWave) void grad_kernel(XentArgs a) {
                 if (m < a.pt_ld)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
-                        if (n + r < cols) a.pt[x * a.pt_plane + (n + r) * a.pt_ld + m] = part[r][x];
+                        if (col + r < cols) a.pt[x * a.pt_plane + (n + r) * a.pt_ld + m] = part[r][x];
             }
         }
     }
 }
 
+// Up to four neighbouring elements of a product on their way out: a share of it; or with the sum so far, to the sum or to the
+// result.  none: the row takes no part.
+template <typename T>
+__device__ __forceinline__ void finish(const XentArgs& a, float (&f)[4], int64_t at, int have, bool none, float* split) {
+    const bool four = have == 4 && a.out_ld % 4 == 0;
+    float* to = split ? split : a.last ? nullptr : a.sum;
+    if (!split)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            if (none) f[r] = 0.0f;
+            if (!a.first && r < have) f[r] += a.sum[at + r];
+        }
+    if (four) {
+        if (to) Pack<F32, 4>::store(to + at, Pack<F32, 4>::pack(f));
+        else Pack<T, 4>::store(a.out + at * T::kBytes, Pack<T, 4>::pack(f));
+        return;
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+        if (r < have) {
+            const float one[1] = {f[r]};
+            if (to) to[at + r] = f[r];
+            else Pack<T, 1>::store(a.out + (at + r) * T::kBytes, Pack<T, 1>::pack(one));
+        }
+}
+
 // out = A B^T, or its sum over pieces.
-template <typename T, int BM, int BN, int MW, int NW>
+template <typename T, int BM, int BN, int MW, int NW, int ST>
 __global__ __launch_bounds__(MW * NW * kWave) void product_kernel(XentArgs a) {
-    using G = Gemm<BM, BN, MW, NW>;
-    __shared__ __attribute__((aligned(16))) char lds[2 * G::kBytes];
+    using G = Gemm<BM, BN, MW, NW, ST>;
+    __shared__ __attribute__((aligned(16))) char lds[G::kLds];
     G t;
     int64_t m0, n0;
     uint32_t tn;
-    tile_of<BM, BN>(a.g, &m0, &n0, &tn);
-    t.run(lds, a.g, m0, n0);
+    const uint32_t tiles = (uint32_t)a.g.mt * (uint32_t)a.g.nt, share = blockIdx.x / tiles;
+    tile_of<BM, BN>(a.g, blockIdx.x - share * tiles, &m0, &n0, &tn);
+    const int steps = a.g.K / kGemmK * a.g.segments;
+    t.run(lds, a.g, m0, n0, (int)((int64_t)steps * share / a.splits), (int)((int64_t)steps * (share + 1) / a.splits));
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int wm = w % MW, wn = w / MW, li = lane % 16, lq = lane / 16;
+    float* split = a.splits > 1 ? a.split + share * a.g.a.rows * a.out_ld : nullptr;
 #pragma unroll
     for (int i = 0; i < G::MI; ++i) {
         const int64_t m = m0 + wm * G::WM + i * 16 + li;
@@ -249,26 +324,30 @@ __global__ __launch_bounds__(MW * NW * kWave) void product_kernel(XentArgs a) {
         for (int j = 0; j < G::NI; ++j) {
             const int64_t n = n0 + wn * G::WN + j * 16 + 4 * lq, at = m * a.out_ld + n;
             const int have = a.g.b.rows - n < 4 ? (int)(a.g.b.rows - n) : 4;
-            float f[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                f[r] = none ? 0.0f : t.acc[i][j][r];
-                if (!a.first && r < have) f[r] += a.sum[at + r];
-            }
-            if (have == 4 && a.out_ld % 4 == 0) {
-                if (!a.last) Pack<F32, 4>::store(a.sum + at, Pack<F32, 4>::pack(f));
-                else Pack<T, 4>::store(a.out + at * T::kBytes, Pack<T, 4>::pack(f));
-            } else {
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (r < have) {
-                        const float one[1] = {f[r]};
-                        if (!a.last) a.sum[at + r] = f[r];
-                        else Pack<T, 1>::store(a.out + (at + r) * T::kBytes, Pack<T, 1>::pack(one));
-                    }
-            }
+            float f[4] = {t.acc[i][j][0], t.acc[i][j][1], t.acc[i][j][2], t.acc[i][j][3]};
+            finish<T>(a, f, at, have, none, split);
         }
     }
+}
+
+// The sum of a product's shares, in their order; four elements a lane.
+template <typename T>
+__global__ __launch_bounds__(256) void gather_kernel(XentArgs a) {
+    const int64_t quads = (a.out_ld + 3) / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= a.g.a.rows * quads) return;
+    const int64_t m = i / quads, n = i % quads * 4, at = m * a.out_ld + n;
+    const int have = a.out_ld - n < 4 ? (int)(a.out_ld - n) : 4;
+    float f[4] = {};
+    for (int s = 0; s < a.splits; ++s) {
+        const float* p = a.split + s * a.g.a.rows * a.out_ld + at;
+        if (have == 4 && a.out_ld % 4 == 0) {
+            const float4 x = *reinterpret_cast<const float4*>(p);
+            f[0] += x.x, f[1] += x.y, f[2] += x.z, f[3] += x.w;
+        } else {
+            for (int r = 0; r < have; ++r) f[r] += p[r];
+        }
+    }
+    finish<T>(a, f, at, have, a.target && (a.target[m] < 0 || a.target[m] >= a.V), nullptr);
 }
 
 __global__ __launch_bounds__(256) void zero_kernel(char* p, int64_t bytes) {
@@ -329,21 +408,6 @@ struct FwdSpace {
     }
 };
 
-struct BwdSpace {
-    uint16_t *x, *w, *xt, *wt, *p, *pt;
-    float* sum;
-    BwdSpace(const XentShape& s, const Layout& l, Carver& c) {
-        const int64_t piece = std::min(l.piece, s.V), ld = up(piece, kGemmK);
-        x = l.packed ? c.take<uint16_t>(l.planes * s.N * l.ld) : nullptr;
-        w = l.packed ? c.take<uint16_t>(l.planes * piece * l.ld) : nullptr;
-        xt = c.take<uint16_t>(l.planes * s.D * l.nt);
-        wt = c.take<uint16_t>(l.planes * s.D * ld);
-        p = c.take<uint16_t>(l.planes * s.N * ld);
-        pt = c.take<uint16_t>(l.planes * piece * l.nt);
-        sum = l.pieces > 1 ? c.take<float>(s.N * s.D) : nullptr;
-    }
-};
-
 GemmArgs product_of(const GemmOperand& a, const GemmOperand& b, int64_t K, int planes) {
     GemmArgs g{};
     g.a = a, g.b = b, g.K = (int32_t)K;
@@ -354,39 +418,98 @@ GemmArgs product_of(const GemmOperand& a, const GemmOperand& b, int64_t K, int p
     return g;
 }
 
-// Tiles of 256 x 256 where they fill most of the chip, else of 128 x 128.
-bool large_tiles(const GemmArgs& g) { return cut(g.a.rows, 256) * cut(g.b.rows, 256) >= 192; }
+// Tiles of 256 x 256 (1.10 PFLOP/s at 8192 x 4096 x 4096) where they fill most of the chip; else of 128 x 128: four steps in
+// LDS (0.85 PFLOP/s with one workgroup per compute unit, 8192 x 512 x 4096), or two, where more workgroups than compute units
+// can share them.
+enum class Tile { k256, k128Deep, k128 };
+Tile tile_for(const GemmArgs& g) {
+    if (cut(g.a.rows, 256) * cut(g.b.rows, 256) >= 192) return Tile::k256;
+    return cut(g.a.rows, 128) * cut(g.b.rows, 128) <= 256 ? Tile::k128Deep : Tile::k128;
+}
+int64_t edge_of(Tile t) { return t == Tile::k256 ? 256 : 128; }
 
 template <typename F>
 hy_status by_tile(XentArgs& a, F f) {
-    const bool large = large_tiles(a.g);
-    const int64_t mt = cut(a.g.a.rows, large ? 256 : 128), nt = cut(a.g.b.rows, large ? 256 : 128);
-    if (mt > INT32_MAX / nt) return HY_ERR_UNSUPPORTED;
+    const Tile tile = tile_for(a.g);
+    const int64_t mt = cut(a.g.a.rows, edge_of(tile)), nt = cut(a.g.b.rows, edge_of(tile));
+    if (mt > INT32_MAX / 16 / nt) return HY_ERR_UNSUPPORTED;
     a.g.mt = (int32_t)mt, a.g.nt = (int32_t)nt;
-    return f(large, dim3((uint32_t)(mt * nt)));
+    return f(tile, dim3((uint32_t)(mt * nt)));
 }
 
 hy_status losses(XentArgs& a, hipStream_t st) {
-    return by_tile(a, [&](bool large, dim3 grid) {
-        return large ? launch_kernel(loss_kernel<256, 256, 2, 4>, grid, dim3(512), st, a)
-                     : launch_kernel(loss_kernel<128, 128, 2, 2>, grid, dim3(256), st, a);
+    return by_tile(a, [&](Tile tile, dim3 grid) {
+        if (tile == Tile::k256) return launch_kernel(loss_kernel<256, 256, 2, 4, 2>, grid, dim3(512), st, a);
+        if (tile == Tile::k128) return launch_kernel(loss_kernel<128, 128, 2, 4, 2>, grid, dim3(512), st, a);
+        return launch_kernel(loss_kernel<128, 128, 2, 4, 4>, grid, dim3(512), st, a);
     });
 }
 
 template <typename T>
 hy_status gradients(XentArgs& a, hipStream_t st) {
-    return by_tile(a, [&](bool large, dim3 grid) {
-        return large ? launch_kernel(grad_kernel<T, 256, 256, 2, 4>, grid, dim3(512), st, a)
-                     : launch_kernel(grad_kernel<T, 128, 128, 2, 2>, grid, dim3(256), st, a);
+    return by_tile(a, [&](Tile tile, dim3 grid) {
+        if (tile == Tile::k256) return launch_kernel(grad_kernel<T, 256, 256, 2, 4, 2>, grid, dim3(512), st, a);
+        if (tile == Tile::k128) return launch_kernel(grad_kernel<T, 128, 128, 2, 4, 2>, grid, dim3(512), st, a);
+        return launch_kernel(grad_kernel<T, 128, 128, 2, 4, 4>, grid, dim3(512), st, a);
     });
 }
 
+// Into how many shares a product's k is divided: where its tiles leave half of the compute units or more without work, as many as
+// they hold, of at least 8 steps each.
+int32_t splits_for(const GemmArgs& g) {
+    if (tile_for(g) != Tile::k128Deep) return 1;
+    const int64_t tiles = cut(g.a.rows, 128) * cut(g.b.rows, 128), steps = (int64_t)(g.K / kGemmK) * g.segments;
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>({256 / tiles, steps / 8, 16}));
+}
+int64_t split_floats(const GemmArgs& g, int64_t ld) {
+    const int32_t n = splits_for(g);
+    return n > 1 ? n * g.a.rows * ld : 0;
+}
+
+// The two products of a piece of `cols` columns.
+GemmArgs dw_product(const XentShape& s, const Layout& l, int64_t cols, const uint16_t* pt = nullptr, const uint16_t* xt = nullptr) {
+    return product_of(GemmOperand{pt, l.nt, cols * l.nt, cols}, GemmOperand{xt, l.nt, s.D * l.nt, s.D}, l.nt, l.planes);
+}
+GemmArgs dx_product(const XentShape& s, const Layout& l, int64_t cols, const uint16_t* p = nullptr, const uint16_t* wt = nullptr) {
+    const int64_t ld = up(cols, kGemmK);
+    return product_of(GemmOperand{p, ld, s.N * ld, s.N}, GemmOperand{wt, ld, s.D * ld, s.D}, ld, l.planes);
+}
+
+struct BwdSpace {
+    uint16_t *x, *w, *xt, *wt, *p, *pt;
+    float *sum, *split;
+    BwdSpace(const XentShape& s, const Layout& l, Carver& c) {
+        const int64_t piece = std::min(l.piece, s.V), ld = up(piece, kGemmK);
+        x = l.packed ? c.take<uint16_t>(l.planes * s.N * l.ld) : nullptr;
+        w = l.packed ? c.take<uint16_t>(l.planes * piece * l.ld) : nullptr;
+        xt = c.take<uint16_t>(l.planes * s.D * l.nt);
+        wt = c.take<uint16_t>(l.planes * s.D * ld);
+        p = c.take<uint16_t>(l.planes * s.N * ld);
+        pt = c.take<uint16_t>(l.planes * piece * l.nt);
+        sum = l.pieces > 1 ? c.take<float>(s.N * s.D) : nullptr;
+        int64_t most = 0;
+        for (int64_t v = 0; v < s.V; v += l.piece) {
+            const int64_t cols = std::min(l.piece, s.V - v);
+            most = std::max({most, split_floats(dw_product(s, l, cols), s.D), split_floats(dx_product(s, l, cols), s.D)});
+        }
+        split = c.take<float>(most);
+    }
+};
+
 template <typename T>
-hy_status product(XentArgs& a, hipStream_t st) {
-    return by_tile(a, [&](bool large, dim3 grid) {
-        return large ? launch_kernel(product_kernel<T, 256, 256, 2, 4>, grid, dim3(512), st, a)
-                     : launch_kernel(product_kernel<T, 128, 128, 2, 2>, grid, dim3(256), st, a);
+hy_status product(XentArgs& a, float* split, hipStream_t st) {
+    a.split = split;
+    a.splits = splits_for(a.g);
+    hy_status rc = by_tile(a, [&](Tile tile, dim3 grid) {
+        grid.x *= (uint32_t)a.splits;
+        if (tile == Tile::k256) return launch_kernel(product_kernel<T, 256, 256, 2, 4, 2>, grid, dim3(512), st, a);
+        if (tile == Tile::k128) return launch_kernel(product_kernel<T, 128, 128, 2, 4, 2>, grid, dim3(512), st, a);
+        return launch_kernel(product_kernel<T, 128, 128, 2, 4, 4>, grid, dim3(512), st, a);
     });
+    if (rc != HY_OK || a.splits == 1) return rc;
+    const int64_t lanes = a.g.a.rows * ((a.out_ld + 3) / 4);
+    if (cut(lanes, 256) > INT32_MAX) return HY_ERR_UNSUPPORTED;
+    return launch_kernel(gather_kernel<T>, dim3((uint32_t)cut(lanes, 256)), dim3(256), st, a);
 }
 
 template <typename T>
@@ -434,7 +557,7 @@ hy_status forward(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t s
             for (int64_t u = 0; u < s.V; u += l.piece) {
                 GemmArgs g = a.g;
                 g.b.rows = std::min(l.piece, s.V - u);
-                a.tiles += cut(g.b.rows, large_tiles(g) ? 256 : 128);
+                a.tiles += cut(g.b.rows, edge_of(tile_for(g)));
             }
         }
         rc = losses(a, st);
@@ -464,14 +587,14 @@ hy_status backward(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t 
         a.pt = b.pt, a.pt_ld = l.nt, a.pt_plane = cols * l.nt;
         if (rc == HY_OK) rc = gradients<T>(a, st);
         XentArgs dw{};
-        dw.g = product_of(GemmOperand{b.pt, l.nt, a.pt_plane, cols}, GemmOperand{b.xt, l.nt, s.D * l.nt, s.D}, l.nt, l.planes);
+        dw.g = dw_product(s, l, cols, b.pt, b.xt);
         dw.out = (char*)p.dw + v * s.D * T::kBytes, dw.out_ld = s.D, dw.first = dw.last = true;
-        if (rc == HY_OK) rc = product<T>(dw, st);
+        if (rc == HY_OK) rc = product<T>(dw, b.split, st);
         XentArgs dx{};
-        dx.g = product_of(GemmOperand{b.p, ld, a.p_plane, s.N}, GemmOperand{b.wt, ld, s.D * ld, s.D}, ld, l.planes);
+        dx.g = dx_product(s, l, cols, b.p, b.wt);
         dx.out = (char*)p.dx, dx.out_ld = s.D, dx.sum = b.sum, dx.first = v == 0, dx.last = v + l.piece >= s.V;
         dx.target = p.target, dx.V = s.V;
-        if (rc == HY_OK) rc = product<T>(dx, st);
+        if (rc == HY_OK) rc = product<T>(dx, b.split, st);
     }
     return rc;
 }
