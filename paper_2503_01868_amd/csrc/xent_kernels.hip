@@ -35,6 +35,16 @@ __device__ __forceinline__ void parts_of(float x, uint16_t (&part)[3]) {
     part[2] = (uint16_t)(__float_as_uint(rest - __uint_as_float(m & 0xffff0000u)) >> 16);
 }
 
+// Part x of what a number is held as in the products, of two numbers in a word.
+template <typename T>
+__device__ __forceinline__ uint32_t part_pair(float lo, float hi, int x) {
+    if constexpr (T::kBytes == 2) return pack_bf16x2(lo, hi);
+    uint16_t a[3], b[3];
+    parts_of(lo, a);
+    parts_of(hi, b);
+    return a[x] | (uint32_t)b[x] << 16;
+}
+
 template <typename T>
 __device__ __forceinline__ void bits_of(const char* p, uint16_t (&part)[3]) {
     if constexpr (T::kBytes == 4) parts_of(*reinterpret_cast<const float*>(p), part);
@@ -120,6 +130,12 @@ struct XentArgs {
     int32_t splits;
 };
 
+// A row of a tile of P: its target's column, whether it takes part, lse and dloss.
+struct RowNeeds {
+    int32_t want, counts;
+    float lse, weight;
+};
+
 // The target's column within a tile of `width` columns that begins at `first`; -1: it is none of them.
 __device__ __forceinline__ int column_of(int64_t target, int64_t first, int width) {
     const int64_t c = target - first;
@@ -144,11 +160,14 @@ __device__ __forceinline__ void tile_of(const GemmArgs& g, uint32_t index, int64
 template <int BM, int BN, int MW, int NW, int ST>
 __global__ __launch_bounds__(MW * NW * kWave) void loss_kernel(XentArgs a) {
     using G = Gemm<BM, BN, MW, NW, ST>;
-    __shared__ __attribute__((aligned(16))) char lds[G::kLds];
+    __shared__ __attribute__((aligned(16))) char lds[G::kLds + BM * 4];
+    int* const wants = reinterpret_cast<int*>(lds + G::kLds);  // what the rows need, loaded in front of the product
     G t;
     int64_t m0, n0;
     uint32_t tn;
     tile_of<BM, BN>(a.g, blockIdx.x, &m0, &n0, &tn);
+    for (int row = threadIdx.x; row < BM; row += G::kThreads)
+        wants[row] = m0 + row < a.g.a.rows ? column_of(a.target[m0 + row], a.v0 + n0, BN) : -1;
     t.run(lds, a.g, m0, n0, 0, a.g.K / kGemmK * a.g.segments);
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int wm = w % MW, wn = w / MW, li = lane % 16, lq = lane / 16;
@@ -159,7 +178,7 @@ __global__ __launch_bounds__(MW * NW * kWave) void loss_kernel(XentArgs a) {
     for (int i = 0; i < G::MI; ++i) {
         const int row = wm * G::WM + i * 16 + li;
         const int64_t m = m0 + row;
-        const int want = m < a.g.a.rows ? column_of(a.target[m], a.v0 + n0, BN) : -1;
+        const int want = wants[row];
         float top = -INFINITY;
         if (cols < BN)
 #pragma unroll
@@ -223,11 +242,18 @@ template <typename T, int BM, int BN, int MW, int NW, int ST>
 __global__ __launch_bounds__(MW * NW * kWave) void grad_kernel(XentArgs a) {
     using G = Gemm<BM, BN, MW, NW, ST>;
     constexpr int N = T::kBytes == 4 ? 3 : 1;
-    __shared__ __attribute__((aligned(16))) char lds[G::kLds];
+    __shared__ __attribute__((aligned(16))) char lds[G::kLds + BM * 16];
+    // What the rows need, loaded in front of the product (a part of the same array: beside another one the compiler takes any
+    // read from LDS for one of the loads into it, and waits).
+    RowNeeds* const needs = reinterpret_cast<RowNeeds*>(lds + G::kLds);
     G t;
     int64_t m0, n0;
     uint32_t tn;
     tile_of<BM, BN>(a.g, blockIdx.x, &m0, &n0, &tn);
+    for (int row = threadIdx.x; row < BM; row += G::kThreads) {
+        const int64_t m = m0 + row < a.g.a.rows ? m0 + row : 0, v = a.target[m];
+        needs[row] = RowNeeds{column_of(v, a.v0 + n0, BN), m0 + row < a.g.a.rows && v >= 0 && v < a.V, a.lse[m], a.dloss[m]};
+    }
     t.run(lds, a.g, m0, n0, 0, a.g.K / kGemmK * a.g.segments);
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int wm = w % MW, wn = w / MW, li = lane % 16, lq = lane / 16;
@@ -235,41 +261,63 @@ __global__ __launch_bounds__(MW * NW * kWave) void grad_kernel(XentArgs a) {
     const int cols = a.g.b.rows - n0 < BN ? (int)(a.g.b.rows - n0) : BN, col0 = wn * G::WN + 4 * lq;
 #pragma unroll
     for (int i = 0; i < G::MI; ++i) {
-        const int64_t m = m0 + wm * G::WM + i * 16 + li;
-        int want = -1;
-        float lse = 0.0f, d = 0.0f;
-        bool counts = false;
-        if (m < rows) {
-            const int64_t v = a.target[m];
-            counts = v >= 0 && v < a.V;
-            want = column_of(v, a.v0 + n0, BN);
-            lse = a.lse[m];
-            d = a.dloss[m];
-        }
+        const RowNeeds need = needs[wm * G::WM + i * 16 + li];
 #pragma unroll
-        for (int j = 0; j < G::NI; ++j) {
-            const int col = col0 + j * 16;
-            const int64_t n = n0 + col;
-            uint16_t part[4][3];
+        for (int j = 0; j < G::NI; ++j)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const float z = t.acc[i][j][r] - lse;
-                float p = N == 3 ? expf(z) : fast_exp(z);
-                if (col + r == want) p -= 1.0f;
-                p = counts && col + r < cols ? d * p : 0.0f;  // zeros, whatever is in the row
-                if constexpr (N == 3) parts_of(p, part[r]);
-                else part[r][0] = (uint16_t)pack_bf16x2(p, 0.0f);
+                const int col = col0 + j * 16 + r;
+                const float z = t.acc[i][j][r] - need.lse;
+                float p = T::kBytes == 4 ? expf(z) : fast_exp(z);
+                if (col == need.want) p -= 1.0f;
+                t.acc[i][j][r] = need.counts && col < cols ? need.weight * p : 0.0f;  // zeros, whatever is in the row
             }
+    }
+    // Both orders go out through the wave's own part of LDS, so that a row leaves in 16-byte pieces side by side.  As they are in
+    // the registers, four columns or one row at a time, they took a fifth of the kernel's time.
+    constexpr int kT = G::WM / 2, kTMask = kT / 8 - 1;         // P^T: words of a row; pieces of 8 words trade places by row
+    constexpr int kPMask = G::WN / 8 < 8 ? G::WN / 8 - 1 : 7;  // P: pieces of 4 words trade places by row
+    uint32_t* own = reinterpret_cast<uint32_t*>(lds) + w * (G::WM * G::WN / 2);
+    __syncthreads();  // the tiles have been read
 #pragma unroll
-            for (int x = 0; x < N; ++x) {
-                if (m < rows && n < a.p_ld)  // p_ld: a multiple of 64
-                    *reinterpret_cast<uint2*>(a.p + x * a.p_plane + m * a.p_ld + n) =
-                        make_uint2(part[0][x] | (uint32_t)part[1][x] << 16, part[2][x] | (uint32_t)part[3][x] << 16);
-                if (m < a.pt_ld)
+    for (int x = 0; x < N; ++x) {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (col + r < cols) a.pt[x * a.pt_plane + (n + r) * a.pt_ld + m] = part[r][x];
+        for (int i = 0; i < G::MI; ++i)
+#pragma unroll
+            for (int j = 0; j < G::NI; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    // columns 2 h and 2 h + 1 of this row and of its neighbour: an even lane takes the first of both rows, an odd
+                    // one the second
+                    const uint32_t mine = part_pair<T>(t.acc[i][j][2 * h], t.acc[i][j][2 * h + 1], x);
+                    const uint32_t other = __builtin_amdgcn_update_dpp(0, mine, 0xb1, 0xf, 0xf, true);
+                    const uint32_t both = li % 2 ? other >> 16 | (mine & 0xffff0000u) : (mine & 0xffffu) | other << 16;
+                    const int row = j * 16 + 4 * lq + 2 * h + li % 2, word = i * 8 + li / 2;
+                    own[row * kT + (word ^ ((((row >> 1 & 6) | (row & 1)) & kTMask) * 8))] = both;
+                }
+        constexpr int kTLanes = kT / 4;  // lanes of a row
+#pragma unroll
+        for (int y = 0; y < G::WN; y += kWave / kTLanes) {
+            const int row = y + lane / kTLanes, word = lane % kTLanes * 4;
+            const uint4 v = *reinterpret_cast<const uint4*>(own + row * kT + (word ^ ((((row >> 1 & 6) | (row & 1)) & kTMask) * 8)));
+            const int64_t n = n0 + wn * G::WN + row, m = m0 + wm * G::WM + 2 * word;
+            if (n < a.g.b.rows && m < a.pt_ld) *reinterpret_cast<uint4*>(a.pt + x * a.pt_plane + n * a.pt_ld + m) = v;
+        }
+#pragma unroll
+        for (int i = 0; i < G::MI; ++i)
+#pragma unroll
+            for (int j = 0; j < G::NI; ++j) {
+                const int row = i * 16 + li, piece = j * 2 + lq / 2;
+                *reinterpret_cast<uint2*>(own + row * (G::WN / 2) + (piece ^ (row & kPMask)) * 4 + lq % 2 * 2) =
+                    make_uint2(part_pair<T>(t.acc[i][j][0], t.acc[i][j][1], x), part_pair<T>(t.acc[i][j][2], t.acc[i][j][3], x));
             }
+        constexpr int kPLanes = G::WN / 8;
+#pragma unroll
+        for (int y = 0; y < G::WM; y += kWave / kPLanes) {
+            const int row = y + lane / kPLanes, piece = lane % kPLanes;
+            const uint4 v = *reinterpret_cast<const uint4*>(own + row * (G::WN / 2) + (piece ^ (row & kPMask)) * 4);
+            const int64_t m = m0 + wm * G::WM + row, n = n0 + wn * G::WN + 8 * piece;
+            if (m < rows && n < a.p_ld) *reinterpret_cast<uint4*>(a.p + x * a.p_plane + m * a.p_ld + n) = v;
         }
     }
 }
@@ -304,13 +352,16 @@ __device__ __forceinline__ void finish(const XentArgs& a, float (&f)[4], int64_t
 template <typename T, int BM, int BN, int MW, int NW, int ST>
 __global__ __launch_bounds__(MW * NW * kWave) void product_kernel(XentArgs a) {
     using G = Gemm<BM, BN, MW, NW, ST>;
-    __shared__ __attribute__((aligned(16))) char lds[G::kLds];
+    __shared__ __attribute__((aligned(16))) char lds[G::kLds + BM * 4];
+    int* const nones = reinterpret_cast<int*>(lds + G::kLds);
     G t;
     int64_t m0, n0;
     uint32_t tn;
     const uint32_t tiles = (uint32_t)a.g.mt * (uint32_t)a.g.nt, share = blockIdx.x / tiles;
     tile_of<BM, BN>(a.g, blockIdx.x - share * tiles, &m0, &n0, &tn);
     const int steps = a.g.K / kGemmK * a.g.segments;
+    for (int row = threadIdx.x; row < BM; row += G::kThreads)
+        nones[row] = a.target && m0 + row < a.g.a.rows && (a.target[m0 + row] < 0 || a.target[m0 + row] >= a.V);
     t.run(lds, a.g, m0, n0, (int)((int64_t)steps * share / a.splits), (int)((int64_t)steps * (share + 1) / a.splits));
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int wm = w % MW, wn = w / MW, li = lane % 16, lq = lane / 16;
@@ -319,7 +370,7 @@ __global__ __launch_bounds__(MW * NW * kWave) void product_kernel(XentArgs a) {
     for (int i = 0; i < G::MI; ++i) {
         const int64_t m = m0 + wm * G::WM + i * 16 + li;
         if (m >= a.g.a.rows) continue;
-        const bool none = a.target && (a.target[m] < 0 || a.target[m] >= a.V);
+        const bool none = nones[m - m0];
 #pragma unroll
         for (int j = 0; j < G::NI; ++j) {
             const int64_t n = n0 + wn * G::WN + j * 16 + 4 * lq, at = m * a.out_ld + n;
