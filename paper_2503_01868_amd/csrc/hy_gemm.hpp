@@ -15,13 +15,16 @@ struct GemmOperand {
     int64_t rows;
 };
 
-// One product: the sum over `segments` pairs of planes of products over K (a multiple of kGemmK).
+// One product: the sum over `segments` pairs of planes of products over K (a multiple of kGemmK).  tail > 0: the rows hold only
+// K - kGemmK + tail numbers, a multiple of 8, and what is behind them counts as zeros.
 struct GemmArgs {
     GemmOperand a, b;
-    int32_t K, segments;
+    int32_t K, segments, tail;
     uint32_t aplanes, bplanes;  // the planes of segment i in bits 4 i .. 4 i + 3
     int32_t mt, nt;             // tiles
 };
+
+__device__ uint4 gemm_zeros;  // (where the loads behind a tail go)
 
 typedef __attribute__((address_space(3))) void* lds_ptr_t;
 typedef const __attribute__((address_space(1))) void* global_ptr_t;
@@ -71,6 +74,19 @@ struct Gemm {
             char* to = lds + stage * kBytes + w * 1024;
             const char* pa = abase + ((g.aplanes >> 4 * seg & 15) * g.a.plane + k * kGemmK) * 2;
             const char* pb = bbase + ((g.bplanes >> 4 * seg & 15) * g.b.plane + k * kGemmK) * 2;
+            if (g.tail > 0 && k == steps - 1) {
+                const bool beyond = ((lane % 8) ^ (lane / 8)) * 8 >= g.tail;
+                const char* none = reinterpret_cast<const char*>(&gemm_zeros);
+#pragma unroll
+                for (int i = 0; i < AL; ++i)
+                    __builtin_amdgcn_global_load_lds((global_ptr_t)(beyond ? none : pa + ao[i]), (lds_ptr_t)(to + i * kWaves * 1024), 16, 0, 0);
+#pragma unroll
+                for (int i = 0; i < BL; ++i)
+                    __builtin_amdgcn_global_load_lds((global_ptr_t)(beyond ? none : pb + bo[i]),
+                                                     (lds_ptr_t)(to + BM * kRowBytes + i * kWaves * 1024), 16, 0, 0);
+                k = 0, ++seg;
+                return;
+            }
 #pragma unroll
             for (int i = 0; i < AL; ++i)
                 __builtin_amdgcn_global_load_lds((global_ptr_t)(pa + ao[i]), (lds_ptr_t)(to + i * kWaves * 1024), 16, 0, 0);

@@ -216,6 +216,114 @@ __global__ __launch_bounds__(MW * NW * kWave) void loss_kernel(XentArgs a) {
     }
 }
 
+// Few rows of fp32 x: the losses' part of kFewWords words and up to 16 NT rows per workgroup, bounded by the bytes of W, which go from
+// memory to registers, become parts there and are multiplied.  The eight waves divide k; x comes from the caches.
+constexpr int kFewWords = 64, kFewWaves = 8, kFewTiles = kFewWords / 16;
+
+// Values k .. k + 7 of a row of D (a multiple of 4); zeros from D on.
+__device__ __forceinline__ void few_load(float4 (&v)[2], const float* row, int64_t k, int64_t D) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        v[i] = k + 4 * i < D ? *reinterpret_cast<const float4*>(row + k + 4 * i) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+}
+__device__ __forceinline__ void few_parts(bf16x8_t (&f)[3], const float4 (&w)[2]) {
+    const float v[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w};
+    uint16_t part[8][3];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) parts_of(v[i], part[i]);
+#pragma unroll
+    for (int x = 0; x < 3; ++x) {
+        Words<4> o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o.w[i] = part[2 * i][x] | (uint32_t)part[2 * i + 1][x] << 16;
+        f[x] = __builtin_bit_cast(bf16x8_t, o);
+    }
+}
+
+template <int NT>
+__global__ __launch_bounds__(kFewWaves * kWave) void few_kernel(const float* x, const float* w, const int64_t* target, float2* part, float* zt,
+                                                                int64_t N, int64_t V, int64_t D, int64_t tiles) {
+    constexpr int U = 2;  // steps of 32 k on their way together
+    __shared__ f32x4_t sums[kFewWaves][kFewTiles * NT][kWave];
+    __shared__ float2 tops[kFewTiles][16 * NT];
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, li = lane % 16, lq = lane / 16;
+    const int64_t v0 = (int64_t)blockIdx.x * kFewWords;
+    const float *wr[kFewTiles], *xr[NT];
+#pragma unroll
+    for (int i = 0; i < kFewTiles; ++i) wr[i] = w + std::min(v0 + i * 16 + li, V - 1) * D;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) xr[j] = x + std::min((int64_t)(j * 16 + li), N - 1) * D;
+    f32x4_t acc[kFewTiles][NT] = {};
+    const int64_t steps = (D + 31) / 32, each = (steps + kFewWaves - 1) / kFewWaves;
+    const int64_t end = std::min(steps, each * (wv + 1));
+    for (int64_t s = each * wv; s < end; s += U) {
+        float4 rw[U][kFewTiles][2], rx[U][NT][2];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t k = s + u < end ? (s + u) * 32 + lq * 8 : D;  // (from D on: zeros)
+#pragma unroll
+            for (int i = 0; i < kFewTiles; ++i) few_load(rw[u][i], wr[i], k, D);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) few_load(rx[u][j], xr[j], k, D);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            bf16x8_t fx[NT][3], fw[3];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) few_parts(fx[j], rx[u][j]);
+#pragma unroll
+            for (int i = 0; i < kFewTiles; ++i) {
+                few_parts(fw, rw[u][i]);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    constexpr int a[6] = {2, 0, 1, 1, 0, 0}, b[6] = {0, 2, 1, 0, 1, 0};  // the smallest products first
+#pragma unroll
+                    for (int y = 0; y < 6; ++y) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[b[y]], fx[j][a[y]], acc[i][j], 0, 0, 0);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kFewTiles; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) sums[wv][i * NT + j][lane] = acc[i][j];
+    __syncthreads();
+    // a wave joins the waves' shares of its pieces of 16 words by 16 rows: lane (li, lq) has row li, words 4 lq .. 4 lq + 3
+    for (int piece = wv; piece < kFewTiles * NT; piece += kFewWaves) {
+        const int i = piece / NT, j = piece % NT;
+        f32x4_t z = sums[0][piece][lane];
+        for (int y = 1; y < kFewWaves; ++y) z += sums[y][piece][lane];
+        const int64_t m = j * 16 + li;
+        const int want = m < N ? column_of(target[m], v0, kFewWords) : -1;
+        float top = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int word = i * 16 + 4 * lq + r;
+            if (v0 + word >= V) z[r] = -INFINITY;
+            else if (word == want) zt[m] = z[r];
+            top = fmaxf(top, z[r]);
+        }
+        top = fmaxf(top, __shfl_xor(top, 16, kWave));
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        const float ref = top == -INFINITY ? 0.0f : top;
+        float sum = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum += fast_exp(z[r] - ref);
+        sum += __shfl_xor(sum, 16, kWave);
+        sum += __shfl_xor(sum, 32, kWave);
+        if (lq == 0) tops[i][m] = make_float2(top, sum);
+    }
+    __syncthreads();
+    const int m = threadIdx.x;
+    if (m < 16 * NT && m < N) {
+        float top = -INFINITY, sum = 0.0f;
+        for (int i = 0; i < kFewTiles; ++i) top = fmaxf(top, tops[i][m].x);
+        const float ref = top == -INFINITY ? 0.0f : top;
+        for (int i = 0; i < kFewTiles; ++i) sum += tops[i][m].y * fast_exp(tops[i][m].x - ref);
+        part[m * tiles + blockIdx.x] = make_float2(top, sum);
+    }
+}
+
 // A wave joins the tiles of a row.
 __global__ __launch_bounds__(256) void join_kernel(const float2* part, const float* zt, const int64_t* target, float* loss,
                                                    float* lse, int64_t rows, int64_t tiles, int64_t V) {
@@ -412,8 +520,9 @@ int64_t cut(int64_t n, int64_t by) { return (n + by - 1) / by; }
 // How a problem is laid out.
 struct Layout {
     int planes;
-    bool packed;              // x and W are copied for the products (fp32, or rows that are no multiple of 128 bytes)
-    int64_t ld;               // of x and W in the products
+    bool packed;              // x and W are copied for the products (fp32, or rows that are no multiple of 16 bytes)
+    int64_t K, ld;            // of x and W in the products: D rounded up, and the distance of rows
+    int32_t tail;
     int64_t nt;               // N rounded up: the k of dW
     int64_t piece, pieces;    // columns of the vocabulary at a time
 };
@@ -423,8 +532,10 @@ constexpr int64_t kPieceBytes = INT64_C(512) << 20;  // of P and its transpose
 Layout layout_of(const XentShape& s) {
     Layout l;
     l.planes = s.dtype == HY_F32 ? 3 : 1;
-    l.packed = s.dtype == HY_F32 || s.D % kGemmK != 0;
-    l.ld = up(s.D, kGemmK);
+    l.packed = s.dtype == HY_F32 || s.D % 8 != 0;
+    l.K = up(s.D, kGemmK);
+    l.ld = l.packed ? l.K : s.D;
+    l.tail = l.packed ? 0 : (int32_t)(s.D % kGemmK);
     l.nt = up(s.N, kGemmK);
     const int64_t most = std::max<int64_t>(1024, kPieceBytes / (4 * l.planes * l.nt) / 256 * 256);
     l.pieces = cut(s.V, most);
@@ -444,14 +555,24 @@ struct Carver {
     }
 };
 
+// Up to 32 rows of fp32 values that begin where 16 bytes do: without the copies in parts.
+bool few_rows(const XentShape& s) { return s.dtype == HY_F32 && s.N <= 32 && s.D % 4 == 0 && cut(s.V, kFewWords) <= INT32_MAX; }
+
 struct FwdSpace {
     uint16_t *x, *w;
     float2* part;
     float* zt;
     int64_t tiles;
     FwdSpace(const XentShape& s, const Layout& l, Carver& c) {
+        if (few_rows(s)) {
+            x = w = nullptr;
+            tiles = cut(s.V, kFewWords);
+            part = c.take<float2>(s.N * tiles);
+            zt = c.take<float>(s.N);
+            return;
+        }
         tiles = 0;
-        for (int64_t i = 0; i < l.pieces; ++i) tiles += cut(std::min(l.piece, s.V - i * l.piece), 128);
+        for (int64_t i = 0; i < l.pieces; ++i) tiles += cut(std::min(l.piece, s.V - i * l.piece), s.N <= 64 ? 64 : 128);
         x = l.packed ? c.take<uint16_t>(l.planes * s.N * l.ld) : nullptr;
         w = l.packed ? c.take<uint16_t>(l.planes * std::min(l.piece, s.V) * l.ld) : nullptr;
         part = c.take<float2>(s.N * tiles);
@@ -472,34 +593,55 @@ GemmArgs product_of(const GemmOperand& a, const GemmOperand& b, int64_t K, int p
 // Tiles of 256 x 256 (1.10 PFLOP/s at 8192 x 4096 x 4096) where they fill most of the chip; else of 128 x 128: four steps in
 // LDS (0.85 PFLOP/s with one workgroup per compute unit, 8192 x 512 x 4096), or two, where more workgroups than compute units
 // can share them.
-enum class Tile { k256, k128Deep, k128 };
+enum class Tile { k256, k128Deep, k128, kFew32, kFew64 };
 Tile tile_for(const GemmArgs& g) {
     if (cut(g.a.rows, 256) * cut(g.b.rows, 256) >= 192) return Tile::k256;
     return cut(g.a.rows, 128) * cut(g.b.rows, 128) <= 256 ? Tile::k128Deep : Tile::k128;
 }
-int64_t edge_of(Tile t) { return t == Tile::k256 ? 256 : 128; }
+struct Edges {
+    int64_t rows, cols;
+};
+Edges edges_of(Tile t) {
+    switch (t) {
+        case Tile::k256: return {256, 256};
+        case Tile::kFew32: return {32, 64};
+        case Tile::kFew64: return {64, 64};
+        default: return {128, 128};
+    }
+}
+// Losses of few rows are bounded by the bytes of W: narrow tiles with many steps on their way (8 x 65536 x 4096: 134 us in tiles of
+// 256 x 256, 106 in tiles of 32 x 64).
+Tile loss_tile(const GemmArgs& g) { return g.a.rows <= 32 ? Tile::kFew32 : g.a.rows <= 64 ? Tile::kFew64 : tile_for(g); }
 
 template <typename F>
-hy_status by_tile(XentArgs& a, F f) {
-    const Tile tile = tile_for(a.g);
-    const int64_t mt = cut(a.g.a.rows, edge_of(tile)), nt = cut(a.g.b.rows, edge_of(tile));
+hy_status by_tile(XentArgs& a, Tile tile, F f) {
+    const Edges e = edges_of(tile);
+    const int64_t mt = cut(a.g.a.rows, e.rows), nt = cut(a.g.b.rows, e.cols);
     if (mt > INT32_MAX / 16 / nt) return HY_ERR_UNSUPPORTED;
     a.g.mt = (int32_t)mt, a.g.nt = (int32_t)nt;
-    return f(tile, dim3((uint32_t)(mt * nt)));
+    return f(dim3((uint32_t)(mt * nt)));
 }
 
 hy_status losses(XentArgs& a, hipStream_t st) {
-    return by_tile(a, [&](Tile tile, dim3 grid) {
-        if (tile == Tile::k256) return launch_kernel(loss_kernel<256, 256, 2, 4, 2>, grid, dim3(512), st, a);
-        if (tile == Tile::k128) return launch_kernel(loss_kernel<128, 128, 2, 4, 2>, grid, dim3(512), st, a);
-        return launch_kernel(loss_kernel<128, 128, 2, 4, 4>, grid, dim3(512), st, a);
+    const Tile tile = loss_tile(a.g);
+    return by_tile(a, tile, [&](dim3 grid) {
+        switch (tile) {
+            case Tile::k256: return launch_kernel(loss_kernel<256, 256, 2, 4, 2>, grid, dim3(512), st, a);
+            case Tile::k128: return launch_kernel(loss_kernel<128, 128, 2, 4, 2>, grid, dim3(512), st, a);
+            case Tile::k128Deep: return launch_kernel(loss_kernel<128, 128, 2, 4, 4>, grid, dim3(512), st, a);
+            case Tile::kFew32: return launch_kernel(loss_kernel<32, 64, 1, 4, 6>, grid, dim3(256), st, a);
+            default: return launch_kernel(loss_kernel<64, 64, 1, 4, 4>, grid, dim3(256), st, a);
+        }
     });
 }
 
 template <typename T>
 hy_status gradients(XentArgs& a, hipStream_t st) {
-    return by_tile(a, [&](Tile tile, dim3 grid) {
-        if (tile == Tile::k256) return launch_kernel(grad_kernel<T, 256, 256, 2, 4, 2>, grid, dim3(512), st, a);
+    Tile tile = tile_for(a.g);
+    if (T::kBytes == 4 && tile == Tile::k256) tile = Tile::k128;  // (three parts of 256 x 256 values do not fit the registers)
+    return by_tile(a, tile, [&](dim3 grid) {
+        if constexpr (T::kBytes == 2)
+            if (tile == Tile::k256) return launch_kernel(grad_kernel<T, 256, 256, 2, 4, 2>, grid, dim3(512), st, a);
         if (tile == Tile::k128) return launch_kernel(grad_kernel<T, 128, 128, 2, 4, 2>, grid, dim3(512), st, a);
         return launch_kernel(grad_kernel<T, 128, 128, 2, 4, 4>, grid, dim3(512), st, a);
     });
@@ -551,7 +693,8 @@ template <typename T>
 hy_status product(XentArgs& a, float* split, hipStream_t st) {
     a.split = split;
     a.splits = splits_for(a.g);
-    hy_status rc = by_tile(a, [&](Tile tile, dim3 grid) {
+    const Tile tile = tile_for(a.g);
+    hy_status rc = by_tile(a, tile, [&](dim3 grid) {
         grid.x *= (uint32_t)a.splits;
         if (tile == Tile::k256) return launch_kernel(product_kernel<T, 256, 256, 2, 4, 2>, grid, dim3(512), st, a);
         if (tile == Tile::k128) return launch_kernel(product_kernel<T, 128, 128, 2, 4, 2>, grid, dim3(512), st, a);
@@ -597,18 +740,26 @@ hy_status forward(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t s
     a.target = p.target, a.V = s.V;
     a.part = f.part, a.zt = f.zt, a.tiles = f.tiles;
     int64_t tile = 0;
-    for (int64_t v = 0; v < s.V; v += l.piece) {
+    if constexpr (T::kBytes == 4)
+        if (few_rows(s)) {
+            auto* const kernel = s.N <= 16 ? few_kernel<1> : few_kernel<2>;
+            hy_status rc = launch_kernel(kernel, dim3((uint32_t)f.tiles), dim3(kFewWaves * kWave), st, (const float*)p.x, (const float*)p.w,
+                                         p.target, f.part, f.zt, s.N, s.V, s.D, f.tiles);
+            if (rc != HY_OK) return rc;
+        }
+    for (int64_t v = 0; v < s.V && !few_rows(s); v += l.piece) {
         GemmOperand x, w;
         hy_status rc = operands<T>(p, s, l, f.x, f.w, v, &x, &w, st);
         if (rc != HY_OK) return rc;
-        a.g = product_of(x, w, l.ld, l.planes);
+        a.g = product_of(x, w, l.K, l.planes);
+        a.g.tail = l.tail;
         a.v0 = v, a.tile0 = tile;
         if (v == 0) {  // pieces have the same tiles, the last one fewer
             a.tiles = 0;
             for (int64_t u = 0; u < s.V; u += l.piece) {
                 GemmArgs g = a.g;
                 g.b.rows = std::min(l.piece, s.V - u);
-                a.tiles += cut(g.b.rows, edge_of(tile_for(g)));
+                a.tiles += cut(g.b.rows, edges_of(loss_tile(g)).cols);
             }
         }
         rc = losses(a, st);
@@ -631,7 +782,8 @@ hy_status backward(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t 
         rc = operands<T>(p, s, l, b.x, b.w, v, &x, &w, st);
         if (rc == HY_OK) rc = turn<T>((const char*)p.w + v * s.D * T::kBytes, b.wt, cols, s.D, ld, nullptr, 0, st);
         XentArgs a{};
-        a.g = product_of(x, w, l.ld, l.planes);
+        a.g = product_of(x, w, l.K, l.planes);
+        a.g.tail = l.tail;
         a.target = p.target, a.V = s.V, a.v0 = v;
         a.lse = p.lse_in, a.dloss = p.dloss;
         a.p = b.p, a.p_ld = ld, a.p_plane = s.N * ld;

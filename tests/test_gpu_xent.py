@@ -59,7 +59,7 @@ def check(x, w, target, dloss, dtype):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("N,V,D", [(1, 1, 1), (1, 2, 8), (3, 5, 7), (64, 256, 64), (65, 257, 65), (128, 1000, 128), (130, 300, 72),
-                                   (1, 5000, 256), (8, 777, 512), (17, 1000, 192), (33, 130, 64), (257, 129, 320), (300, 1030, 1000), (7, 70, 2048),
+                                   (1, 5000, 256), (8, 777, 512), (17, 1000, 192), (33, 130, 64), (257, 129, 320), (300, 1030, 1000), (7, 70, 2048), (16, 1000, 40), (20, 333, 100), (64, 4097, 136), (48, 100, 4), (200, 300, 8), (129, 257, 1096),
                                    (4096, 3100, 64)])
 def test_losses_and_gradients(N, V, D, dtype):
     say("xent N=%d V=%d D=%d %s" % (N, V, D, dtype))
