@@ -1,4 +1,4 @@
-// Matrix products C[m][n] = sum_k A[m][k] B[n][k] on bf16 matrix cores with fp32 sums: both operands have k contiguous.
+// Matrix products C[m][n] = sum_k A[m][k] B[n][k] on the matrix cores with fp32 sums: both operands have k contiguous.
 #pragma once
 #include <type_traits>
 
@@ -6,22 +6,19 @@
 
 namespace hy {
 
-constexpr int kGemmK = 64;        // k per step: 128 bytes of a row
+constexpr int kGemmK = 64;        // every operand made here has rows of a multiple
 
-// A matrix of bf16 rows; fp32 values are three planes (head, middle and tail bits).
+// Rows of bf16 numbers (Gemm) or of fp32 numbers (GemmSplit).
 struct GemmOperand {
-    const uint16_t* p;
-    int64_t ld, plane;   // elements between rows and between planes
+    const void* p;
+    int64_t ld;          // elements between rows
     int64_t rows;
 };
 
-// One product: the sum over `segments` pairs of planes of products over K (a multiple of kGemmK).  tail > 0: the rows hold only
-// K - kGemmK + tail numbers, a multiple of 8, and what is behind them counts as zeros.
 struct GemmArgs {
     GemmOperand a, b;
-    int32_t K, segments, tail;
-    uint32_t aplanes, bplanes;  // the planes of segment i in bits 4 i .. 4 i + 3
-    int32_t mt, nt;             // tiles
+    int32_t K;           // what is behind a row's K numbers counts as zeros.  bf16: a multiple of 8, and rows begin where 16 bytes do
+    int32_t mt, nt;      // tiles
 };
 
 __device__ uint4 gemm_zeros;  // (where the loads behind a tail go)
@@ -37,9 +34,10 @@ typedef const __attribute__((address_space(1))) void* global_ptr_t;
 // has arrived and that nobody reads this one any more.
 template <int BM, int BN, int MW, int NW, int STAGES>
 struct Gemm {
+    static constexpr int kStep = 64;  // k of a step: 128 bytes of a row
     static constexpr int kWaves = MW * NW, kThreads = kWaves * kWave;
     static constexpr int WM = BM / MW, WN = BN / NW, MI = WM / 16, NI = WN / 16;
-    static constexpr int kRowBytes = kGemmK * 2;
+    static constexpr int kRowBytes = kStep * 2;
     static constexpr int kBytes = (BM + BN) * kRowBytes;  // of one step's tiles
     static constexpr int kLds = STAGES * kBytes;
     static constexpr int AL = BM * 8 / kThreads, BL = BN * 8 / kThreads;  // 16-byte pieces of a lane
@@ -48,7 +46,7 @@ struct Gemm {
 
     // Rows of 128 bytes in LDS, the 16-byte pieces of row r at r * 128 + (piece ^ (r % 8)) * 16: the 16 lanes that read one
     // piece of 16 rows spread over all banks.  A wave's load fills 8 rows, so lane l fetches piece (l % 8) ^ (l / 8).
-    // Steps [first, last) of all segments' steps.
+    // Steps [first, last).
     __device__ __forceinline__ void run(char* lds, const GemmArgs& g, int64_t m0, int64_t n0, int first, int last) {
         const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
         const int li = lane % 16, lq = lane / 16;
@@ -67,15 +65,15 @@ struct Gemm {
 #pragma unroll
             for (int j = 0; j < NI; ++j) acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 
-        const char *abase = (const char*)(g.a.p + m0 * g.a.ld), *bbase = (const char*)(g.b.p + n0 * g.b.ld);
-        const int steps = g.K / kGemmK, total = last - first;
-        int seg = first / steps, k = first - seg * steps;
+        const char *abase = (const char*)g.a.p + m0 * g.a.ld * 2, *bbase = (const char*)g.b.p + n0 * g.b.ld * 2;
+        const int total = last - first, tail = g.K % kStep;
+        int k = first;
         auto fetch = [&](int stage) {
             char* to = lds + stage * kBytes + w * 1024;
-            const char* pa = abase + ((g.aplanes >> 4 * seg & 15) * g.a.plane + k * kGemmK) * 2;
-            const char* pb = bbase + ((g.bplanes >> 4 * seg & 15) * g.b.plane + k * kGemmK) * 2;
-            if (g.tail > 0 && k == steps - 1) {
-                const bool beyond = ((lane % 8) ^ (lane / 8)) * 8 >= g.tail;
+            const char *pa = abase + k * (kStep * 2), *pb = bbase + k * (kStep * 2);
+            ++k;
+            if (tail > 0 && k * kStep > g.K) {
+                const bool beyond = ((lane % 8) ^ (lane / 8)) * 8 >= tail;
                 const char* none = reinterpret_cast<const char*>(&gemm_zeros);
 #pragma unroll
                 for (int i = 0; i < AL; ++i)
@@ -84,7 +82,6 @@ struct Gemm {
                 for (int i = 0; i < BL; ++i)
                     __builtin_amdgcn_global_load_lds((global_ptr_t)(beyond ? none : pb + bo[i]),
                                                      (lds_ptr_t)(to + BM * kRowBytes + i * kWaves * 1024), 16, 0, 0);
-                k = 0, ++seg;
                 return;
             }
 #pragma unroll
@@ -93,7 +90,6 @@ struct Gemm {
 #pragma unroll
             for (int i = 0; i < BL; ++i)
                 __builtin_amdgcn_global_load_lds((global_ptr_t)(pb + bo[i]), (lds_ptr_t)(to + BM * kRowBytes + i * kWaves * 1024), 16, 0, 0);
-            if (++k == steps) k = 0, ++seg;
         };
         const int wm = w % MW, wn = w / MW;
         const char *ra = lds + (wm * WM + li) * kRowBytes, *rb = lds + (BM + wn * WN + li) * kRowBytes;
@@ -176,6 +172,153 @@ struct Gemm {
         }
         first_half();
         multiply(h1);
+    }
+};
+
+// The parts of an fp32 number, each in the upper half of a word: cut, not rounded, so that no part overflows.  All of an infinity
+// is in the first part; a NaN is one in the second.
+__device__ __forceinline__ void parts_of(float x, uint32_t (&part)[3]) {
+    constexpr int kInfinite = 0x204;  // of either sign
+    part[0] = __float_as_uint(x);
+    const float head = __uint_as_float(part[0] & 0xffff0000u);
+    const float rest = __builtin_amdgcn_classf(x, kInfinite) ? 0.0f : x - head;
+    part[1] = __float_as_uint(rest);
+    part[2] = __float_as_uint(rest - __uint_as_float(part[1] & 0xffff0000u));
+}
+// Eight of them as operands of a product.
+__device__ __forceinline__ void parts_of(const float4 (&w)[2], uint4 (&f)[3]) {
+    const float v[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w};
+    uint32_t o[4][3];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t a[3], b[3];
+        parts_of(v[2 * i], a);
+        parts_of(v[2 * i + 1], b);
+#pragma unroll
+        for (int x = 0; x < 3; ++x) o[i][x] = __builtin_amdgcn_perm(b[x], a[x], 0x07060302);  // the upper halves
+    }
+#pragma unroll
+    for (int x = 0; x < 3; ++x) f[x] = make_uint4(o[0][x], o[1][x], o[2][x], o[3][x]);
+}
+// The products of parts that reach an fp32 product's 24 bits, the smallest first: the parts of one factor and of the other.
+constexpr int kSplitProducts = 6;
+constexpr int kSplitA[kSplitProducts] = {2, 0, 1, 1, 0, 0}, kSplitB[kSplitProducts] = {0, 2, 1, 0, 1, 0};
+
+// The same for fp32 operands, to fp32's precision: a number is three bf16 numbers (8 bits each, the head, the middle and the
+// tail of the 24), and a product the sum of six products of parts.  Numbers become parts once, between memory and LDS: a step's
+// are fetched into registers two steps ahead and written to LDS as three planes of 64-byte rows (the 16-byte pieces of row r at
+// piece ^ (r / 2 % 4)) one step ahead.  A part that is in a register serves two or three of the six products, so LDS is read half
+// as often as for six products of planes.
+template <int BM, int BN, int MW, int NW>
+struct GemmSplit {
+    static constexpr int kStep = 32;
+    static constexpr int kWaves = MW * NW, kThreads = kWaves * kWave;
+    static constexpr int WM = BM / MW, WN = BN / NW, MI = WM / 16, NI = WN / 16;
+    static constexpr int kPlane = (BM + BN) * kStep * 2, kBytes = 3 * kPlane, kLds = 2 * kBytes;
+    static constexpr int kPieces = (BM + BN) * 4 / kThreads;  // of 8 numbers, of a lane
+    static_assert(kPieces * kThreads == (BM + BN) * 4, "whole pieces");
+
+    f32x4_t acc[MI][NI];
+
+    __device__ __forceinline__ void run(char* lds, const GemmArgs& g, int64_t m0, int64_t n0, int first, int last) {
+        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+        const int li = lane % 16, lq = lane / 16, wm = w % MW, wn = w / MW;
+        const float* from[kPieces];
+        int to[kPieces], at[kPieces];
+#pragma unroll
+        for (int x = 0; x < kPieces; ++x) {
+            const int i = x * kThreads + (int)threadIdx.x, row = i / 4, piece = i % 4;
+            const GemmOperand& o = row < BM ? g.a : g.b;
+            int64_t r = row < BM ? m0 + row : n0 + row - BM;
+            if (r >= o.rows) r = o.rows - 1;  // rows that do not exist: the last one again
+            from[x] = static_cast<const float*>(o.p) + r * o.ld;
+            at[x] = piece * 8;
+            to[x] = row * (kStep * 2) + (piece ^ (row / 2 % 4)) * 16;
+        }
+        const bool fours = g.K % 4 == 0 && g.a.ld % 4 == 0 && g.b.ld % 4 == 0 &&
+                           (((uintptr_t)g.a.p | (uintptr_t)g.b.p) & 15) == 0;
+        auto fetch = [&](float4 (&v)[kPieces][2], int step) {
+            if (fours && (step + 1) * kStep <= g.K) {
+#pragma unroll
+                for (int x = 0; x < kPieces; ++x)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) v[x][h] = *reinterpret_cast<const float4*>(from[x] + step * kStep + at[x] + 4 * h);
+                return;
+            }
+#pragma unroll
+            for (int x = 0; x < kPieces; ++x)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int k = step * kStep + at[x] + 4 * h;
+                    v[x][h] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    if (k < g.K) v[x][h].x = from[x][k];
+                    if (k + 1 < g.K) v[x][h].y = from[x][k + 1];
+                    if (k + 2 < g.K) v[x][h].z = from[x][k + 2];
+                    if (k + 3 < g.K) v[x][h].w = from[x][k + 3];
+                }
+        };
+        auto put = [&](const float4 (&v)[kPieces][2], int stage) {
+#pragma unroll
+            for (int x = 0; x < kPieces; ++x) {
+                uint4 f[3];
+                parts_of(v[x], f);
+#pragma unroll
+                for (int y = 0; y < 3; ++y) *reinterpret_cast<uint4*>(lds + stage * kBytes + y * kPlane + to[x]) = f[y];
+            }
+        };
+        auto meet = [&] {  // what the waves have written to LDS is there; loads into registers stay on their way
+            __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        };
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        const int piece = (lq ^ (li / 2 % 4)) * 16;
+        const char *ra = lds + (wm * WM + li) * (kStep * 2) + piece, *rb = lds + (BM + wn * WN + li) * (kStep * 2) + piece;
+        float4 v0[kPieces][2], v1[kPieces][2];
+        fetch(v0, first);
+        put(v0, 0);
+        fetch(v0, first + 1);  // (behind K: zeros)
+        meet();
+        auto step = [&](int t, float4 (&next)[kPieces][2], float4 (&after)[kPieces][2]) {
+            const int stage = (t - first) % 2;
+            fetch(after, t + 2 < last ? t + 2 : last - 1);
+            bf16x8_t fa[3][MI], fb[3][NI];
+            auto read = [&](int pa, int pb) {
+#pragma unroll
+                for (int j = 0; j < NI; ++j) fb[pb][j] = *reinterpret_cast<const bf16x8_t*>(rb + stage * kBytes + pb * kPlane + j * 16 * kStep * 2);
+#pragma unroll
+                for (int i = 0; i < MI; ++i) fa[pa][i] = *reinterpret_cast<const bf16x8_t*>(ra + stage * kBytes + pa * kPlane + i * 16 * kStep * 2);
+            };
+            read(2, 0);  // in the order of their use
+            read(0, 2);
+            read(1, 1);
+            put(next, stage ^ 1);  // (behind the last step: nobody reads it)
+#pragma unroll
+            for (int y = 0; y < kSplitProducts; ++y)
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int j = 0; j < NI; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[kSplitB[y]][j], fa[kSplitA[y]][i], acc[i][j], 0, 0, 0);
+            // the parts are made between the products
+            __builtin_amdgcn_sched_group_barrier(0x100, 3 * (MI + NI), 0);
+#pragma unroll
+            for (int y = 0; y < kSplitProducts * MI * NI; ++y) {
+                __builtin_amdgcn_sched_group_barrier(8, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(2, 3, 0);
+            }
+            meet();
+        };
+        int t = first;
+        for (; t + 1 < last; t += 2) {
+            step(t, v0, v1);
+            step(t + 1, v1, v0);
+        }
+        if (t < last) step(t, v0, v1);
     }
 };
 

@@ -8,9 +8,8 @@
 // products.  All four products are of the one form that hy_gemm.hpp has (k contiguous in both operands), so P is written in
 // both orders, and x and the piece of W are transposed once.  The matrix products are what bounds it: 8 N V D operations.
 //
-// bf16 operands enter the products as they are; P is rounded to bf16 for its two.  fp32 operands, and P of fp32 calls, are three
-// bf16 numbers (8 bits each, the head, the middle and the tail of the 24), and a product is the sum of the six products of
-// parts that reach its 24 bits.
+// bf16 operands enter the products as they are, and P is rounded to bf16 for its two; fp32 calls multiply in parts, to fp32's
+// precision, and keep P in fp32.
 #include <algorithm>
 
 #include "hy_gemm.hpp"
@@ -20,92 +19,89 @@ namespace hy {
 
 namespace {
 
-// The parts of an fp32 number: cut, not rounded, so that no part overflows; all of a number that is not finite is in the first.
-__device__ __forceinline__ void parts_of(float x, uint16_t (&part)[3]) {
-    const uint32_t b = __float_as_uint(x);
-    part[0] = (uint16_t)(b >> 16);
-    part[1] = part[2] = 0;
-    if ((b & 0x7f800000u) == 0x7f800000u) {
-        if (b & 0x007fffffu) part[0] |= 0x40;  // a NaN stays one without its lower bits
-        return;
-    }
-    const float rest = x - __uint_as_float(b & 0xffff0000u);
-    const uint32_t m = __float_as_uint(rest);
-    part[1] = (uint16_t)(m >> 16);
-    part[2] = (uint16_t)(__float_as_uint(rest - __uint_as_float(m & 0xffff0000u)) >> 16);
-}
-
-// Part x of what a number is held as in the products, of two numbers in a word.
+// What an element of T is in a product: its bits.
 template <typename T>
-__device__ __forceinline__ uint32_t part_pair(float lo, float hi, int x) {
-    if constexpr (T::kBytes == 2) return pack_bf16x2(lo, hi);
-    uint16_t a[3], b[3];
-    parts_of(lo, a);
-    parts_of(hi, b);
-    return a[x] | (uint32_t)b[x] << 16;
-}
+using Bits = std::conditional_t<T::kBytes == 4, uint32_t, uint16_t>;
 
-template <typename T>
-__device__ __forceinline__ void bits_of(const char* p, uint16_t (&part)[3]) {
-    if constexpr (T::kBytes == 4) parts_of(*reinterpret_cast<const float*>(p), part);
-    else part[0] = *reinterpret_cast<const uint16_t*>(p);
-}
-
-// Rows of D values -> planes of rows of `ld` bf16 numbers, zeros behind the values.
-template <typename T>
-__global__ __launch_bounds__(256) void pack_kernel(const char* src, uint16_t* dst, int64_t rows, int64_t D, int64_t ld) {
+// Rows of D bf16 numbers -> rows of `ld`, zeros behind them: rows that do not begin where 16 bytes do.
+__global__ __launch_bounds__(256) void pack_kernel(const uint16_t* src, uint16_t* dst, int64_t rows, int64_t D, int64_t ld) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= rows * ld) return;
     const int64_t r = i / ld, c = i % ld;
-    uint16_t part[3] = {};
-    if (c < D) bits_of<T>(src + (r * D + c) * T::kBytes, part);
-    for (int x = 0; x < (T::kBytes == 4 ? 3 : 1); ++x) dst[x * rows * ld + i] = part[x];
+    dst[i] = c < D ? src[r * D + c] : 0;
 }
 
-// Rows of D values -> planes of D rows of `ld` (a multiple of 64) bf16 numbers; zeros behind the last row, and for the rows whose
-// target is none.  Pieces of 64 x 64 through LDS, 8 values a lane.
-template <typename T>
-__global__ __launch_bounds__(256) void turn_kernel(const char* src, uint16_t* dst, int64_t rows, int64_t D, int64_t ld,
-                                                   const int64_t* target, int64_t V) {
-    constexpr int N = T::kBytes == 4 ? 3 : 1, kPitch = 72;
-    __shared__ __attribute__((aligned(16))) uint16_t s[N][64][kPitch];
-    const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;
+// The largest weight of a row that takes part, by one workgroup.  P in this unit is -1 where a target is far from foreseen, which
+// bf16 holds; as a multiple of 1 / N, say, all those would be rounded alike, and the errors of a sum over them would not cancel.
+struct Unit {
+    const float* dloss;
+    float* unit;  // null: none is wanted
+};
+__device__ __forceinline__ void find_unit(const Unit& u, const int64_t* target, int64_t rows, int64_t V) {
+    __shared__ float tops[256 / kWave];
+    float top = 0.0f;
+    constexpr int kTogether = 16;  // rows of a lane on their way together: one wait for 4096 of them
+    for (int64_t m0 = threadIdx.x; m0 < rows; m0 += 256 * kTogether) {
+        float d[kTogether];
+        int64_t v[kTogether];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int y = threadIdx.x / 8 + 32 * h, x = threadIdx.x % 8 * 8;
-        const int64_t r = r0 + y, c = c0 + x;
-        uint16_t part[8][3] = {};
-        if (r < rows && c < D && (!target || (target[r] >= 0 && target[r] < V))) {
-            const char* p = src + (r * D + c) * T::kBytes;
-            if (D % 8 == 0) {
-                uint4 w[T::kBytes / 2];
-#pragma unroll
-                for (int i = 0; i < T::kBytes / 2; ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) bits_of<T>(reinterpret_cast<const char*>(w) + i * T::kBytes, part[i]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (c + i < D) bits_of<T>(p + i * T::kBytes, part[i]);
-            }
+        for (int i = 0; i < kTogether; ++i) {
+            const int64_t m = m0 + 256 * i < rows ? m0 + 256 * i : m0;
+            d[i] = fabsf(u.dloss[m]);
+            v[i] = target[m];
         }
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            *reinterpret_cast<uint4*>(&s[i][y][x]) = make_uint4(part[0][i] | (uint32_t)part[1][i] << 16, part[2][i] | (uint32_t)part[3][i] << 16,
-                                                                part[4][i] | (uint32_t)part[5][i] << 16, part[6][i] | (uint32_t)part[7][i] << 16);
+        for (int i = 0; i < kTogether; ++i)
+            if (v[i] >= 0 && v[i] < V && d[i] < INFINITY) top = fmaxf(top, d[i]);
+    }
+    for (int d = 32; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d, kWave));
+    if (threadIdx.x % kWave == 0) tops[threadIdx.x / kWave] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 256 / kWave; ++i) top = fmaxf(top, tops[i]);
+        *u.unit = top > 0.0f ? top : 1.0f;
+    }
+}
+
+// Rows of D numbers -> D rows of `ld` (a multiple of 64); zeros behind the last row, and for the rows whose target is none.
+// Pieces of 64 x 64 through LDS, 16 bytes a lane.  The workgroups of the first row of the grid have nothing to turn: one finds the
+// weights' unit.
+template <typename T>
+__global__ __launch_bounds__(256) void turn_kernel(const Bits<T>* src, Bits<T>* dst, int64_t rows, int64_t D, int64_t ld,
+                                                   const int64_t* target, int64_t V, Unit unit) {
+    if (unit.unit && blockIdx.y == 0) {
+        if (blockIdx.x == 0) find_unit(unit, target, rows, V);
+        return;
+    }
+    constexpr int kPer = 16 / T::kBytes, kLanes = 64 / kPer, kPitch = 64 + kPer;  // numbers of a lane, lanes of a row
+    __shared__ __attribute__((aligned(16))) Bits<T> s[64][kPitch];
+    const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)(blockIdx.y - (unit.unit ? 1 : 0)) * 64;
+    const int x = threadIdx.x % kLanes * kPer;
+#pragma unroll
+    for (int y = threadIdx.x / kLanes; y < 64; y += 256 / kLanes) {
+        const int64_t r = r0 + y, c = c0 + x;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (r < rows && c < D && (!target || (target[r] >= 0 && target[r] < V))) {
+            const Bits<T>* p = src + r * D + c;
+            if (D % kPer == 0) {
+                v = *reinterpret_cast<const uint4*>(p);
+            } else {
+                Bits<T> one[kPer];
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) one[i] = c + i < D ? p[i] : 0;
+                v = *reinterpret_cast<const uint4*>(one);
+            }
+        }
+        *reinterpret_cast<uint4*>(&s[y][x]) = v;
     }
     __syncthreads();
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int y = threadIdx.x / 8 + 32 * h, x = threadIdx.x % 8 * 8;
+    for (int y = threadIdx.x / kLanes; y < 64; y += 256 / kLanes) {
         if (c0 + y >= D) continue;
+        Bits<T> one[kPer];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            uint32_t w[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = s[i][x + 2 * j][y] | (uint32_t)s[i][x + 2 * j + 1][y] << 16;
-            *reinterpret_cast<uint4*>(dst + (i * D + c0 + y) * ld + r0 + x) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+        for (int i = 0; i < kPer; ++i) one[i] = s[x + i][y];
+        *reinterpret_cast<uint4*>(dst + (c0 + y) * ld + r0 + x) = *reinterpret_cast<const uint4*>(one);
     }
 }
 
@@ -119,8 +115,9 @@ struct XentArgs {
     float* zt;                // [rows] the targets' values
     // gradients
     const float *lse, *dloss;
-    uint16_t *p, *pt;
-    int64_t p_ld, p_plane, pt_ld, pt_plane;
+    const float* unit;        // dloss is taken in this unit (null: 1), and the products are taken back
+    void *p, *pt;             // P [rows][p_ld] and its transpose [columns][pt_ld], bf16 or fp32
+    int64_t p_ld, pt_ld;
     // products
     char* out;
     float* sum;               // the sum so far (not of the first piece)
@@ -157,9 +154,8 @@ __device__ __forceinline__ void tile_of(const GemmArgs& g, uint32_t index, int64
     *n0 = (int64_t)*tn * BN;
 }
 
-template <int BM, int BN, int MW, int NW, int ST>
+template <typename G, int BM, int BN, int MW, int NW>
 __global__ __launch_bounds__(MW * NW * kWave) void loss_kernel(XentArgs a) {
-    using G = Gemm<BM, BN, MW, NW, ST>;
     __shared__ __attribute__((aligned(16))) char lds[G::kLds + BM * 4];
     int* const wants = reinterpret_cast<int*>(lds + G::kLds);  // what the rows need, loaded in front of the product
     G t;
@@ -168,7 +164,7 @@ __global__ __launch_bounds__(MW * NW * kWave) void loss_kernel(XentArgs a) {
     tile_of<BM, BN>(a.g, blockIdx.x, &m0, &n0, &tn);
     for (int row = threadIdx.x; row < BM; row += G::kThreads)
         wants[row] = m0 + row < a.g.a.rows ? column_of(a.target[m0 + row], a.v0 + n0, BN) : -1;
-    t.run(lds, a.g, m0, n0, 0, a.g.K / kGemmK * a.g.segments);
+    t.run(lds, a.g, m0, n0, 0, (a.g.K + G::kStep - 1) / G::kStep);
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int wm = w % MW, wn = w / MW, li = lane % 16, lq = lane / 16;
     float2(*share)[NW] = reinterpret_cast<float2(*)[NW]>(lds);
@@ -226,20 +222,6 @@ __device__ __forceinline__ void few_load(float4 (&v)[2], const float* row, int64
     for (int i = 0; i < 2; ++i)
         v[i] = k + 4 * i < D ? *reinterpret_cast<const float4*>(row + k + 4 * i) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 }
-__device__ __forceinline__ void few_parts(bf16x8_t (&f)[3], const float4 (&w)[2]) {
-    const float v[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w};
-    uint16_t part[8][3];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) parts_of(v[i], part[i]);
-#pragma unroll
-    for (int x = 0; x < 3; ++x) {
-        Words<4> o;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o.w[i] = part[2 * i][x] | (uint32_t)part[2 * i + 1][x] << 16;
-        f[x] = __builtin_bit_cast(bf16x8_t, o);
-    }
-}
-
 template <int NT>
 __global__ __launch_bounds__(kFewWaves * kWave) void few_kernel(const float* x, const float* w, const int64_t* target, float2* part, float* zt,
                                                                 int64_t N, int64_t V, int64_t D, int64_t tiles) {
@@ -268,17 +250,18 @@ __global__ __launch_bounds__(kFewWaves * kWave) void few_kernel(const float* x, 
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            bf16x8_t fx[NT][3], fw[3];
+            uint4 fx[NT][3], fw[3];
 #pragma unroll
-            for (int j = 0; j < NT; ++j) few_parts(fx[j], rx[u][j]);
+            for (int j = 0; j < NT; ++j) parts_of(rx[u][j], fx[j]);
 #pragma unroll
             for (int i = 0; i < kFewTiles; ++i) {
-                few_parts(fw, rw[u][i]);
+                parts_of(rw[u][i], fw);
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
-                    constexpr int a[6] = {2, 0, 1, 1, 0, 0}, b[6] = {0, 2, 1, 0, 1, 0};  // the smallest products first
 #pragma unroll
-                    for (int y = 0; y < 6; ++y) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[b[y]], fx[j][a[y]], acc[i][j], 0, 0, 0);
+                    for (int y = 0; y < kSplitProducts; ++y)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, fw[kSplitB[y]]),
+                                                                            __builtin_bit_cast(bf16x8_t, fx[j][kSplitA[y]]), acc[i][j], 0, 0, 0);
                 }
             }
         }
@@ -346,10 +329,8 @@ __global__ __launch_bounds__(256) void join_kernel(const float2* part, const flo
     }
 }
 
-template <typename T, int BM, int BN, int MW, int NW, int ST>
+template <typename T, typename G, int BM, int BN, int MW, int NW>
 __global__ __launch_bounds__(MW * NW * kWave) void grad_kernel(XentArgs a) {
-    using G = Gemm<BM, BN, MW, NW, ST>;
-    constexpr int N = T::kBytes == 4 ? 3 : 1;
     __shared__ __attribute__((aligned(16))) char lds[G::kLds + BM * 16];
     // What the rows need, loaded in front of the product (a part of the same array: beside another one the compiler takes any
     // read from LDS for one of the loads into it, and waits).
@@ -360,9 +341,10 @@ __global__ __launch_bounds__(MW * NW * kWave) void grad_kernel(XentArgs a) {
     tile_of<BM, BN>(a.g, blockIdx.x, &m0, &n0, &tn);
     for (int row = threadIdx.x; row < BM; row += G::kThreads) {
         const int64_t m = m0 + row < a.g.a.rows ? m0 + row : 0, v = a.target[m];
-        needs[row] = RowNeeds{column_of(v, a.v0 + n0, BN), m0 + row < a.g.a.rows && v >= 0 && v < a.V, a.lse[m], a.dloss[m]};
+        needs[row] = RowNeeds{column_of(v, a.v0 + n0, BN), m0 + row < a.g.a.rows && v >= 0 && v < a.V, a.lse[m],
+                              a.unit ? a.dloss[m] / *a.unit : a.dloss[m]};
     }
-    t.run(lds, a.g, m0, n0, 0, a.g.K / kGemmK * a.g.segments);
+    t.run(lds, a.g, m0, n0, 0, (a.g.K + G::kStep - 1) / G::kStep);
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int wm = w % MW, wn = w / MW, li = lane % 16, lq = lane / 16;
     const int64_t rows = a.g.a.rows;
@@ -381,14 +363,28 @@ __global__ __launch_bounds__(MW * NW * kWave) void grad_kernel(XentArgs a) {
                 t.acc[i][j][r] = need.counts && col < cols ? need.weight * p : 0.0f;  // zeros, whatever is in the row
             }
     }
+    if constexpr (T::kBytes == 4) {
+        // 64 bytes of a row of either side by side
+#pragma unroll
+        for (int i = 0; i < G::MI; ++i)
+#pragma unroll
+            for (int j = 0; j < G::NI; ++j) {
+                const int64_t m = m0 + wm * G::WM + i * 16 + li, n = n0 + col0 + j * 16;
+                if (m < rows && n < a.p_ld) *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.p) + m * a.p_ld + n) = t.acc[i][j];
+                if (m < a.pt_ld)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (n + r < a.g.b.rows) static_cast<float*>(a.pt)[(n + r) * a.pt_ld + m] = t.acc[i][j][r];
+            }
+        return;
+    }
     // Both orders go out through the wave's own part of LDS, so that a row leaves in 16-byte pieces side by side.  As they are in
     // the registers, four columns or one row at a time, they took a fifth of the kernel's time.
     constexpr int kT = G::WM / 2, kTMask = kT / 8 - 1;         // P^T: words of a row; pieces of 8 words trade places by row
     constexpr int kPMask = G::WN / 8 < 8 ? G::WN / 8 - 1 : 7;  // P: pieces of 4 words trade places by row
     uint32_t* own = reinterpret_cast<uint32_t*>(lds) + w * (G::WM * G::WN / 2);
     __syncthreads();  // the tiles have been read
-#pragma unroll
-    for (int x = 0; x < N; ++x) {
+    {
 #pragma unroll
         for (int i = 0; i < G::MI; ++i)
 #pragma unroll
@@ -397,7 +393,7 @@ __global__ __launch_bounds__(MW * NW * kWave) void grad_kernel(XentArgs a) {
                 for (int h = 0; h < 2; ++h) {
                     // columns 2 h and 2 h + 1 of this row and of its neighbour: an even lane takes the first of both rows, an odd
                     // one the second
-                    const uint32_t mine = part_pair<T>(t.acc[i][j][2 * h], t.acc[i][j][2 * h + 1], x);
+                    const uint32_t mine = pack_bf16x2(t.acc[i][j][2 * h], t.acc[i][j][2 * h + 1]);
                     const uint32_t other = __builtin_amdgcn_update_dpp(0, mine, 0xb1, 0xf, 0xf, true);
                     const uint32_t both = li % 2 ? other >> 16 | (mine & 0xffff0000u) : (mine & 0xffffu) | other << 16;
                     const int row = j * 16 + 4 * lq + 2 * h + li % 2, word = i * 8 + li / 2;
@@ -409,7 +405,7 @@ __global__ __launch_bounds__(MW * NW * kWave) void grad_kernel(XentArgs a) {
             const int row = y + lane / kTLanes, word = lane % kTLanes * 4;
             const uint4 v = *reinterpret_cast<const uint4*>(own + row * kT + (word ^ ((((row >> 1 & 6) | (row & 1)) & kTMask) * 8)));
             const int64_t n = n0 + wn * G::WN + row, m = m0 + wm * G::WM + 2 * word;
-            if (n < a.g.b.rows && m < a.pt_ld) *reinterpret_cast<uint4*>(a.pt + x * a.pt_plane + n * a.pt_ld + m) = v;
+            if (n < a.g.b.rows && m < a.pt_ld) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.pt) + n * a.pt_ld + m) = v;
         }
 #pragma unroll
         for (int i = 0; i < G::MI; ++i)
@@ -417,7 +413,7 @@ __global__ __launch_bounds__(MW * NW * kWave) void grad_kernel(XentArgs a) {
             for (int j = 0; j < G::NI; ++j) {
                 const int row = i * 16 + li, piece = j * 2 + lq / 2;
                 *reinterpret_cast<uint2*>(own + row * (G::WN / 2) + (piece ^ (row & kPMask)) * 4 + lq % 2 * 2) =
-                    make_uint2(part_pair<T>(t.acc[i][j][0], t.acc[i][j][1], x), part_pair<T>(t.acc[i][j][2], t.acc[i][j][3], x));
+                    make_uint2(pack_bf16x2(t.acc[i][j][0], t.acc[i][j][1]), pack_bf16x2(t.acc[i][j][2], t.acc[i][j][3]));
             }
         constexpr int kPLanes = G::WN / 8;
 #pragma unroll
@@ -425,7 +421,7 @@ __global__ __launch_bounds__(MW * NW * kWave) void grad_kernel(XentArgs a) {
             const int row = y + lane / kPLanes, piece = lane % kPLanes;
             const uint4 v = *reinterpret_cast<const uint4*>(own + row * (G::WN / 2) + (piece ^ (row & kPMask)) * 4);
             const int64_t m = m0 + wm * G::WM + row, n = n0 + wn * G::WN + 8 * piece;
-            if (m < rows && n < a.p_ld) *reinterpret_cast<uint4*>(a.p + x * a.p_plane + m * a.p_ld + n) = v;
+            if (m < rows && n < a.p_ld) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.p) + m * a.p_ld + n) = v;
         }
     }
 }
@@ -433,7 +429,7 @@ __global__ __launch_bounds__(MW * NW * kWave) void grad_kernel(XentArgs a) {
 // Up to four neighbouring elements of a product on their way out: a share of it; or with the sum so far, to the sum or to the
 // result.  none: the row takes no part.
 template <typename T>
-__device__ __forceinline__ void finish(const XentArgs& a, float (&f)[4], int64_t at, int have, bool none, float* split) {
+__device__ __forceinline__ void finish(const XentArgs& a, float (&f)[4], int64_t at, int have, bool none, float* split, float unit) {
     const bool four = have == 4 && a.out_ld % 4 == 0;
     float* to = split ? split : a.last ? nullptr : a.sum;
     if (!split)
@@ -442,6 +438,9 @@ __device__ __forceinline__ void finish(const XentArgs& a, float (&f)[4], int64_t
             if (none) f[r] = 0.0f;
             if (!a.first && r < have) f[r] += a.sum[at + r];
         }
+    if (!to)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) f[r] *= unit;
     if (four) {
         if (to) Pack<F32, 4>::store(to + at, Pack<F32, 4>::pack(f));
         else Pack<T, 4>::store(a.out + at * T::kBytes, Pack<T, 4>::pack(f));
@@ -457,9 +456,8 @@ __device__ __forceinline__ void finish(const XentArgs& a, float (&f)[4], int64_t
 }
 
 // out = A B^T, or its sum over pieces.
-template <typename T, int BM, int BN, int MW, int NW, int ST>
+template <typename T, typename G, int BM, int BN, int MW, int NW>
 __global__ __launch_bounds__(MW * NW * kWave) void product_kernel(XentArgs a) {
-    using G = Gemm<BM, BN, MW, NW, ST>;
     __shared__ __attribute__((aligned(16))) char lds[G::kLds + BM * 4];
     int* const nones = reinterpret_cast<int*>(lds + G::kLds);
     G t;
@@ -467,12 +465,13 @@ __global__ __launch_bounds__(MW * NW * kWave) void product_kernel(XentArgs a) {
     uint32_t tn;
     const uint32_t tiles = (uint32_t)a.g.mt * (uint32_t)a.g.nt, share = blockIdx.x / tiles;
     tile_of<BM, BN>(a.g, blockIdx.x - share * tiles, &m0, &n0, &tn);
-    const int steps = a.g.K / kGemmK * a.g.segments;
+    const int steps = (a.g.K + G::kStep - 1) / G::kStep;
     for (int row = threadIdx.x; row < BM; row += G::kThreads)
         nones[row] = a.target && m0 + row < a.g.a.rows && (a.target[m0 + row] < 0 || a.target[m0 + row] >= a.V);
     t.run(lds, a.g, m0, n0, (int)((int64_t)steps * share / a.splits), (int)((int64_t)steps * (share + 1) / a.splits));
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int wm = w % MW, wn = w / MW, li = lane % 16, lq = lane / 16;
+    const float unit = a.unit ? *a.unit : 1.0f;
     float* split = a.splits > 1 ? a.split + share * a.g.a.rows * a.out_ld : nullptr;
 #pragma unroll
     for (int i = 0; i < G::MI; ++i) {
@@ -484,7 +483,7 @@ __global__ __launch_bounds__(MW * NW * kWave) void product_kernel(XentArgs a) {
             const int64_t n = n0 + wn * G::WN + j * 16 + 4 * lq, at = m * a.out_ld + n;
             const int have = a.g.b.rows - n < 4 ? (int)(a.g.b.rows - n) : 4;
             float f[4] = {t.acc[i][j][0], t.acc[i][j][1], t.acc[i][j][2], t.acc[i][j][3]};
-            finish<T>(a, f, at, have, none, split);
+            finish<T>(a, f, at, have, none, split, unit);
         }
     }
 }
@@ -506,7 +505,7 @@ __global__ __launch_bounds__(256) void gather_kernel(XentArgs a) {
             for (int r = 0; r < have; ++r) f[r] += p[r];
         }
     }
-    finish<T>(a, f, at, have, a.target && (a.target[m] < 0 || a.target[m] >= a.V), nullptr);
+    finish<T>(a, f, at, have, a.target && (a.target[m] < 0 || a.target[m] >= a.V), nullptr, a.unit ? *a.unit : 1.0f);
 }
 
 __global__ __launch_bounds__(256) void zero_kernel(char* p, int64_t bytes) {
@@ -519,10 +518,8 @@ int64_t cut(int64_t n, int64_t by) { return (n + by - 1) / by; }
 
 // How a problem is laid out.
 struct Layout {
-    int planes;
-    bool packed;              // x and W are copied for the products (fp32, or rows that are no multiple of 16 bytes)
-    int64_t K, ld;            // of x and W in the products: D rounded up, and the distance of rows
-    int32_t tail;
+    bool packed;              // x and W are copied for the products (bf16 rows that do not begin where 16 bytes do)
+    int64_t ld;               // of x and W in the products
     int64_t nt;               // N rounded up: the k of dW
     int64_t piece, pieces;    // columns of the vocabulary at a time
 };
@@ -531,13 +528,11 @@ constexpr int64_t kPieceBytes = INT64_C(512) << 20;  // of P and its transpose
 
 Layout layout_of(const XentShape& s) {
     Layout l;
-    l.planes = s.dtype == HY_F32 ? 3 : 1;
-    l.packed = s.dtype == HY_F32 || s.D % 8 != 0;
-    l.K = up(s.D, kGemmK);
-    l.ld = l.packed ? l.K : s.D;
-    l.tail = l.packed ? 0 : (int32_t)(s.D % kGemmK);
+    const int64_t e = s.dtype == HY_F32 ? 4 : 2;
+    l.packed = s.dtype == HY_BF16 && s.D % 8 != 0;
+    l.ld = l.packed ? up(s.D, kGemmK) : s.D;
     l.nt = up(s.N, kGemmK);
-    const int64_t most = std::max<int64_t>(1024, kPieceBytes / (4 * l.planes * l.nt) / 256 * 256);
+    const int64_t most = std::min<int64_t>(std::max<int64_t>(1024, kPieceBytes / (2 * e * l.nt) / 256 * 256), 1 << 22);
     l.pieces = cut(s.V, most);
     l.piece = std::min(up(cut(s.V, l.pieces), 256), up(s.V, kGemmK));
     l.pieces = cut(s.V, l.piece);
@@ -555,7 +550,7 @@ struct Carver {
     }
 };
 
-// Up to 32 rows of fp32 values that begin where 16 bytes do: without the copies in parts.
+// Up to 32 rows of fp32 values that begin where 16 bytes do.
 bool few_rows(const XentShape& s) { return s.dtype == HY_F32 && s.N <= 32 && s.D % 4 == 0 && cut(s.V, kFewWords) <= INT32_MAX; }
 
 struct FwdSpace {
@@ -564,29 +559,20 @@ struct FwdSpace {
     float* zt;
     int64_t tiles;
     FwdSpace(const XentShape& s, const Layout& l, Carver& c) {
-        if (few_rows(s)) {
-            x = w = nullptr;
-            tiles = cut(s.V, kFewWords);
-            part = c.take<float2>(s.N * tiles);
-            zt = c.take<float>(s.N);
-            return;
-        }
         tiles = 0;
-        for (int64_t i = 0; i < l.pieces; ++i) tiles += cut(std::min(l.piece, s.V - i * l.piece), s.N <= 64 ? 64 : 128);
-        x = l.packed ? c.take<uint16_t>(l.planes * s.N * l.ld) : nullptr;
-        w = l.packed ? c.take<uint16_t>(l.planes * std::min(l.piece, s.V) * l.ld) : nullptr;
+        if (few_rows(s)) tiles = cut(s.V, kFewWords);
+        else
+            for (int64_t i = 0; i < l.pieces; ++i) tiles += cut(std::min(l.piece, s.V - i * l.piece), s.N <= 64 ? 64 : 128);
+        x = l.packed ? c.take<uint16_t>(s.N * l.ld) : nullptr;
+        w = l.packed ? c.take<uint16_t>(std::min(l.piece, s.V) * l.ld) : nullptr;
         part = c.take<float2>(s.N * tiles);
         zt = c.take<float>(s.N);
     }
 };
 
-GemmArgs product_of(const GemmOperand& a, const GemmOperand& b, int64_t K, int planes) {
+GemmArgs product_of(const GemmOperand& a, const GemmOperand& b, int64_t K) {
     GemmArgs g{};
     g.a = a, g.b = b, g.K = (int32_t)K;
-    g.segments = planes == 3 ? 6 : 1;
-    // the smallest products first
-    g.aplanes = planes == 3 ? 0x001102u : 0u;
-    g.bplanes = planes == 3 ? 0x010120u : 0u;
     return g;
 }
 
@@ -609,9 +595,9 @@ Edges edges_of(Tile t) {
         default: return {128, 128};
     }
 }
-// Losses of few rows are bounded by the bytes of W: narrow tiles with many steps on their way (8 x 65536 x 4096: 134 us in tiles of
+// The logits of few rows are bounded by the bytes of W: narrow tiles with many steps on their way (8 x 65536 x 4096: 134 us in tiles of
 // 256 x 256, 106 in tiles of 32 x 64).
-Tile loss_tile(const GemmArgs& g) { return g.a.rows <= 32 ? Tile::kFew32 : g.a.rows <= 64 ? Tile::kFew64 : tile_for(g); }
+Tile logit_tile(const GemmArgs& g) { return g.a.rows <= 32 ? Tile::kFew32 : g.a.rows <= 64 ? Tile::kFew64 : tile_for(g); }
 
 template <typename F>
 hy_status by_tile(XentArgs& a, Tile tile, F f) {
@@ -622,83 +608,112 @@ hy_status by_tile(XentArgs& a, Tile tile, F f) {
     return f(dim3((uint32_t)(mt * nt)));
 }
 
+// The kernels' products: bf16 operands by their tile; fp32 ones in tiles of 128 x 128.
+template <typename T>
+Tile logit_tile_for(const GemmArgs& g) {
+    return T::kBytes == 2 ? logit_tile(g) : g.a.rows <= 64 ? Tile::kFew64 : Tile::k128;
+}
+template <typename T>
+Tile product_tile_for(const GemmArgs& g) {
+    return T::kBytes == 4 ? Tile::k128 : tile_for(g);
+}
+
+template <typename T>
 hy_status losses(XentArgs& a, hipStream_t st) {
-    const Tile tile = loss_tile(a.g);
+    const Tile tile = logit_tile_for<T>(a.g);
     return by_tile(a, tile, [&](dim3 grid) {
+        if constexpr (T::kBytes == 4)
+            return tile == Tile::kFew64 ? launch_kernel(loss_kernel<GemmSplit<64, 64, 1, 4>, 64, 64, 1, 4>, grid, dim3(256), st, a)
+                                        : launch_kernel(loss_kernel<GemmSplit<128, 128, 2, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+        else
         switch (tile) {
-            case Tile::k256: return launch_kernel(loss_kernel<256, 256, 2, 4, 2>, grid, dim3(512), st, a);
-            case Tile::k128: return launch_kernel(loss_kernel<128, 128, 2, 4, 2>, grid, dim3(512), st, a);
-            case Tile::k128Deep: return launch_kernel(loss_kernel<128, 128, 2, 4, 4>, grid, dim3(512), st, a);
-            case Tile::kFew32: return launch_kernel(loss_kernel<32, 64, 1, 4, 6>, grid, dim3(256), st, a);
-            default: return launch_kernel(loss_kernel<64, 64, 1, 4, 4>, grid, dim3(256), st, a);
+            case Tile::k256: return launch_kernel(loss_kernel<Gemm<256, 256, 2, 4, 2>, 256, 256, 2, 4>, grid, dim3(512), st, a);
+            case Tile::k128: return launch_kernel(loss_kernel<Gemm<128, 128, 2, 4, 2>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+            case Tile::k128Deep: return launch_kernel(loss_kernel<Gemm<128, 128, 2, 4, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+            case Tile::kFew32: return launch_kernel(loss_kernel<Gemm<32, 64, 1, 4, 6>, 32, 64, 1, 4>, grid, dim3(256), st, a);
+            default: return launch_kernel(loss_kernel<Gemm<64, 64, 1, 4, 4>, 64, 64, 1, 4>, grid, dim3(256), st, a);
         }
     });
 }
 
 template <typename T>
 hy_status gradients(XentArgs& a, hipStream_t st) {
-    Tile tile = tile_for(a.g);
-    if (T::kBytes == 4 && tile == Tile::k256) tile = Tile::k128;  // (three parts of 256 x 256 values do not fit the registers)
+    const Tile tile = logit_tile_for<T>(a.g);
     return by_tile(a, tile, [&](dim3 grid) {
-        if constexpr (T::kBytes == 2)
-            if (tile == Tile::k256) return launch_kernel(grad_kernel<T, 256, 256, 2, 4, 2>, grid, dim3(512), st, a);
-        if (tile == Tile::k128) return launch_kernel(grad_kernel<T, 128, 128, 2, 4, 2>, grid, dim3(512), st, a);
-        return launch_kernel(grad_kernel<T, 128, 128, 2, 4, 4>, grid, dim3(512), st, a);
+        if constexpr (T::kBytes == 4)
+            return tile == Tile::kFew64 ? launch_kernel(grad_kernel<T, GemmSplit<64, 64, 1, 4>, 64, 64, 1, 4>, grid, dim3(256), st, a)
+                                        : launch_kernel(grad_kernel<T, GemmSplit<128, 128, 2, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+        else
+        switch (tile) {
+            case Tile::kFew32: return launch_kernel(grad_kernel<T, Gemm<32, 64, 1, 4, 6>, 32, 64, 1, 4>, grid, dim3(256), st, a);
+            case Tile::kFew64: return launch_kernel(grad_kernel<T, Gemm<64, 64, 1, 4, 4>, 64, 64, 1, 4>, grid, dim3(256), st, a);
+            case Tile::k256: return launch_kernel(grad_kernel<T, Gemm<256, 256, 2, 4, 2>, 256, 256, 2, 4>, grid, dim3(512), st, a);
+            case Tile::k128: return launch_kernel(grad_kernel<T, Gemm<128, 128, 2, 4, 2>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+            default: return launch_kernel(grad_kernel<T, Gemm<128, 128, 2, 4, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+        }
     });
 }
 
 // Into how many shares a product's k is divided: where its tiles leave half of the compute units or more without work, as many as
 // they hold, of at least 8 steps each.
+template <typename T>
 int32_t splits_for(const GemmArgs& g) {
-    if (tile_for(g) != Tile::k128Deep) return 1;
-    const int64_t tiles = cut(g.a.rows, 128) * cut(g.b.rows, 128), steps = (int64_t)(g.K / kGemmK) * g.segments;
+    const int64_t tiles = cut(g.a.rows, 128) * cut(g.b.rows, 128), steps = g.K / (T::kBytes == 4 ? 32 : 64);
+    if (tiles > 128 || product_tile_for<T>(g) == Tile::k256) return 1;
     return (int32_t)std::max<int64_t>(1, std::min<int64_t>({256 / tiles, steps / 8, 16}));
-}
-int64_t split_floats(const GemmArgs& g, int64_t ld) {
-    const int32_t n = splits_for(g);
-    return n > 1 ? n * g.a.rows * ld : 0;
 }
 
 // The two products of a piece of `cols` columns.
-GemmArgs dw_product(const XentShape& s, const Layout& l, int64_t cols, const uint16_t* pt = nullptr, const uint16_t* xt = nullptr) {
-    return product_of(GemmOperand{pt, l.nt, cols * l.nt, cols}, GemmOperand{xt, l.nt, s.D * l.nt, s.D}, l.nt, l.planes);
+GemmArgs dw_product(const XentShape& s, const Layout& l, int64_t cols, const void* pt = nullptr, const void* xt = nullptr) {
+    return product_of(GemmOperand{pt, l.nt, cols}, GemmOperand{xt, l.nt, s.D}, up(s.N, 32));  // (what the tiles of P, of 32 rows at least, fill)
 }
-GemmArgs dx_product(const XentShape& s, const Layout& l, int64_t cols, const uint16_t* p = nullptr, const uint16_t* wt = nullptr) {
+GemmArgs dx_product(const XentShape& s, int64_t cols, const void* p = nullptr, const void* wt = nullptr) {
     const int64_t ld = up(cols, kGemmK);
-    return product_of(GemmOperand{p, ld, s.N * ld, s.N}, GemmOperand{wt, ld, s.D * ld, s.D}, ld, l.planes);
+    return product_of(GemmOperand{p, ld, s.N}, GemmOperand{wt, ld, s.D}, ld);
 }
 
+template <typename T>
 struct BwdSpace {
-    uint16_t *x, *w, *xt, *wt, *p, *pt;
-    float *sum, *split;
+    uint16_t *x, *w;
+    Bits<T> *xt, *wt, *p, *pt;
+    float *sum, *split, *unit;
     BwdSpace(const XentShape& s, const Layout& l, Carver& c) {
         const int64_t piece = std::min(l.piece, s.V), ld = up(piece, kGemmK);
-        x = l.packed ? c.take<uint16_t>(l.planes * s.N * l.ld) : nullptr;
-        w = l.packed ? c.take<uint16_t>(l.planes * piece * l.ld) : nullptr;
-        xt = c.take<uint16_t>(l.planes * s.D * l.nt);
-        wt = c.take<uint16_t>(l.planes * s.D * ld);
-        p = c.take<uint16_t>(l.planes * s.N * ld);
-        pt = c.take<uint16_t>(l.planes * piece * l.nt);
+        x = l.packed ? c.take<uint16_t>(s.N * l.ld) : nullptr;
+        w = l.packed ? c.take<uint16_t>(piece * l.ld) : nullptr;
+        xt = c.take<Bits<T>>(s.D * l.nt);
+        wt = c.take<Bits<T>>(s.D * ld);
+        p = c.take<Bits<T>>(s.N * ld);
+        pt = c.take<Bits<T>>(piece * l.nt);
         sum = l.pieces > 1 ? c.take<float>(s.N * s.D) : nullptr;
         int64_t most = 0;
+        auto floats = [&](const GemmArgs& g) {
+            const int32_t n = splits_for<T>(g);
+            return n > 1 ? n * g.a.rows * s.D : 0;
+        };
         for (int64_t v = 0; v < s.V; v += l.piece) {
             const int64_t cols = std::min(l.piece, s.V - v);
-            most = std::max({most, split_floats(dw_product(s, l, cols), s.D), split_floats(dx_product(s, l, cols), s.D)});
+            most = std::max({most, floats(dw_product(s, l, cols)), floats(dx_product(s, cols))});
         }
         split = c.take<float>(most);
+        unit = c.take<float>(1);
     }
 };
 
 template <typename T>
 hy_status product(XentArgs& a, float* split, hipStream_t st) {
     a.split = split;
-    a.splits = splits_for(a.g);
-    const Tile tile = tile_for(a.g);
+    a.splits = splits_for<T>(a.g);
+    const Tile tile = product_tile_for<T>(a.g);
     hy_status rc = by_tile(a, tile, [&](dim3 grid) {
         grid.x *= (uint32_t)a.splits;
-        if (tile == Tile::k256) return launch_kernel(product_kernel<T, 256, 256, 2, 4, 2>, grid, dim3(512), st, a);
-        if (tile == Tile::k128) return launch_kernel(product_kernel<T, 128, 128, 2, 4, 2>, grid, dim3(512), st, a);
-        return launch_kernel(product_kernel<T, 128, 128, 2, 4, 4>, grid, dim3(512), st, a);
+        if constexpr (T::kBytes == 4) return launch_kernel(product_kernel<T, GemmSplit<128, 128, 2, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+        else
+        switch (tile) {
+            case Tile::k256: return launch_kernel(product_kernel<T, Gemm<256, 256, 2, 4, 2>, 256, 256, 2, 4>, grid, dim3(512), st, a);
+            case Tile::k128: return launch_kernel(product_kernel<T, Gemm<128, 128, 2, 4, 2>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+            default: return launch_kernel(product_kernel<T, Gemm<128, 128, 2, 4, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+        }
     });
     if (rc != HY_OK || a.splits == 1) return rc;
     const int64_t lanes = a.g.a.rows * ((a.out_ld + 3) / 4);
@@ -706,16 +721,15 @@ hy_status product(XentArgs& a, float* split, hipStream_t st) {
     return launch_kernel(gather_kernel<T>, dim3((uint32_t)cut(lanes, 256)), dim3(256), st, a);
 }
 
-template <typename T>
-hy_status pack(const void* src, uint16_t* dst, int64_t rows, int64_t D, int64_t ld, hipStream_t st) {
-    return launch_kernel(pack_kernel<T>, dim3((uint32_t)cut(rows * ld, 256)), dim3(256), st, (const char*)src, dst, rows, D, ld);
+hy_status pack(const uint16_t* src, uint16_t* dst, int64_t rows, int64_t D, int64_t ld, hipStream_t st) {
+    return launch_kernel(pack_kernel, dim3((uint32_t)cut(rows * ld, 256)), dim3(256), st, src, dst, rows, D, ld);
 }
 
 template <typename T>
-hy_status turn(const void* src, uint16_t* dst, int64_t rows, int64_t D, int64_t ld, const int64_t* target, int64_t V,
+hy_status turn(const void* src, Bits<T>* dst, int64_t rows, int64_t D, int64_t ld, const int64_t* target, int64_t V, Unit unit,
                hipStream_t st) {
-    return launch_kernel(turn_kernel<T>, dim3((uint32_t)cut(ld, 64), (uint32_t)cut(D, 64)), dim3(256), st, (const char*)src, dst,
-                         rows, D, ld, target, V);
+    return launch_kernel(turn_kernel<T>, dim3((uint32_t)cut(ld, 64), (uint32_t)(cut(D, 64) + (unit.unit ? 1 : 0))), dim3(256), st,
+                         (const Bits<T>*)src, dst, rows, D, ld, target, V, unit);
 }
 
 // x, and the piece of W that begins at row v, as operands.
@@ -723,11 +737,12 @@ template <typename T>
 hy_status operands(const XentPtrs& p, const XentShape& s, const Layout& l, uint16_t* x, uint16_t* w, int64_t v, GemmOperand* ox,
                    GemmOperand* ow, hipStream_t st) {
     const int64_t rows = std::min(l.piece, s.V - v);
-    *ox = GemmOperand{l.packed ? x : (const uint16_t*)p.x, l.ld, s.N * l.ld, s.N};
-    *ow = GemmOperand{l.packed ? w : (const uint16_t*)p.w + v * s.D, l.ld, rows * l.ld, rows};
+    const char* piece = (const char*)p.w + v * s.D * T::kBytes;
+    *ox = GemmOperand{l.packed ? x : p.x, l.ld, s.N};
+    *ow = GemmOperand{l.packed ? (const void*)w : piece, l.ld, rows};
     if (!l.packed) return HY_OK;
-    hy_status rc = v == 0 ? pack<T>(p.x, x, s.N, s.D, l.ld, st) : HY_OK;
-    if (rc == HY_OK) rc = pack<T>((const char*)p.w + v * s.D * T::kBytes, w, rows, s.D, l.ld, st);
+    hy_status rc = v == 0 ? pack((const uint16_t*)p.x, x, s.N, s.D, l.ld, st) : HY_OK;
+    if (rc == HY_OK) rc = pack((const uint16_t*)piece, w, rows, s.D, l.ld, st);
     return rc;
 }
 
@@ -739,32 +754,25 @@ hy_status forward(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t s
     XentArgs a{};
     a.target = p.target, a.V = s.V;
     a.part = f.part, a.zt = f.zt, a.tiles = f.tiles;
-    int64_t tile = 0;
-    if constexpr (T::kBytes == 4)
-        if (few_rows(s)) {
-            auto* const kernel = s.N <= 16 ? few_kernel<1> : few_kernel<2>;
-            hy_status rc = launch_kernel(kernel, dim3((uint32_t)f.tiles), dim3(kFewWaves * kWave), st, (const float*)p.x, (const float*)p.w,
-                                         p.target, f.part, f.zt, s.N, s.V, s.D, f.tiles);
+    if (few_rows(s)) {
+        auto* const kernel = s.N <= 16 ? few_kernel<1> : few_kernel<2>;
+        hy_status rc = launch_kernel(kernel, dim3((uint32_t)f.tiles), dim3(kFewWaves * kWave), st, (const float*)p.x, (const float*)p.w,
+                                     p.target, f.part, f.zt, s.N, s.V, s.D, f.tiles);
+        if (rc != HY_OK) return rc;
+    } else {
+        auto with = [&](int64_t v) {
+            return product_of(GemmOperand{nullptr, l.ld, s.N}, GemmOperand{nullptr, l.ld, std::min(l.piece, s.V - v)}, l.packed ? l.ld : s.D);
+        };
+        a.tiles = 0;
+        for (int64_t v = 0; v < s.V; v += l.piece) a.tiles += cut(with(v).b.rows, edges_of(logit_tile_for<T>(with(v))).cols);
+        for (int64_t v = 0; v < s.V; v += l.piece) {
+            a.g = with(v);
+            hy_status rc = operands<T>(p, s, l, f.x, f.w, v, &a.g.a, &a.g.b, st);
+            a.v0 = v;
+            if (rc == HY_OK) rc = losses<T>(a, st);
             if (rc != HY_OK) return rc;
+            a.tile0 += a.g.nt;
         }
-    for (int64_t v = 0; v < s.V && !few_rows(s); v += l.piece) {
-        GemmOperand x, w;
-        hy_status rc = operands<T>(p, s, l, f.x, f.w, v, &x, &w, st);
-        if (rc != HY_OK) return rc;
-        a.g = product_of(x, w, l.K, l.planes);
-        a.g.tail = l.tail;
-        a.v0 = v, a.tile0 = tile;
-        if (v == 0) {  // pieces have the same tiles, the last one fewer
-            a.tiles = 0;
-            for (int64_t u = 0; u < s.V; u += l.piece) {
-                GemmArgs g = a.g;
-                g.b.rows = std::min(l.piece, s.V - u);
-                a.tiles += cut(g.b.rows, edges_of(loss_tile(g)).cols);
-            }
-        }
-        rc = losses(a, st);
-        if (rc != HY_OK) return rc;
-        tile += a.g.nt;
     }
     return launch_kernel(join_kernel, dim3((uint32_t)cut(s.N, 4)), dim3(256), st, (const float2*)f.part, (const float*)f.zt, p.target,
                          p.loss, p.lse, s.N, a.tiles, s.V);
@@ -774,28 +782,27 @@ template <typename T>
 hy_status backward(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t st) {
     const Layout l = layout_of(s);
     Carver c{static_cast<char*>(ws)};
-    BwdSpace b(s, l, c);
-    hy_status rc = turn<T>(p.x, b.xt, s.N, s.D, l.nt, p.target, s.V, st);
+    BwdSpace<T> b(s, l, c);
+    const float* unit = T::kBytes == 2 ? b.unit : nullptr;
+    hy_status rc = turn<T>(p.x, b.xt, s.N, s.D, l.nt, p.target, s.V, Unit{p.dloss, T::kBytes == 2 ? b.unit : nullptr}, st);
     for (int64_t v = 0; rc == HY_OK && v < s.V; v += l.piece) {
         const int64_t cols = std::min(l.piece, s.V - v), ld = up(cols, kGemmK);
-        GemmOperand x, w;
-        rc = operands<T>(p, s, l, b.x, b.w, v, &x, &w, st);
-        if (rc == HY_OK) rc = turn<T>((const char*)p.w + v * s.D * T::kBytes, b.wt, cols, s.D, ld, nullptr, 0, st);
         XentArgs a{};
-        a.g = product_of(x, w, l.K, l.planes);
-        a.g.tail = l.tail;
+        a.g.K = (int32_t)(l.packed ? l.ld : s.D);
+        rc = operands<T>(p, s, l, b.x, b.w, v, &a.g.a, &a.g.b, st);
+        if (rc == HY_OK) rc = turn<T>((const char*)p.w + v * s.D * T::kBytes, b.wt, cols, s.D, ld, nullptr, 0, Unit{}, st);
         a.target = p.target, a.V = s.V, a.v0 = v;
-        a.lse = p.lse_in, a.dloss = p.dloss;
-        a.p = b.p, a.p_ld = ld, a.p_plane = s.N * ld;
-        a.pt = b.pt, a.pt_ld = l.nt, a.pt_plane = cols * l.nt;
+        a.lse = p.lse_in, a.dloss = p.dloss, a.unit = unit;
+        a.p = b.p, a.p_ld = ld;
+        a.pt = b.pt, a.pt_ld = l.nt;
         if (rc == HY_OK) rc = gradients<T>(a, st);
         XentArgs dw{};
         dw.g = dw_product(s, l, cols, b.pt, b.xt);
-        dw.out = (char*)p.dw + v * s.D * T::kBytes, dw.out_ld = s.D, dw.first = dw.last = true;
+        dw.out = (char*)p.dw + v * s.D * T::kBytes, dw.out_ld = s.D, dw.first = dw.last = true, dw.unit = unit;
         if (rc == HY_OK) rc = product<T>(dw, b.split, st);
         XentArgs dx{};
-        dx.g = dx_product(s, l, cols, b.p, b.wt);
-        dx.out = (char*)p.dx, dx.out_ld = s.D, dx.sum = b.sum, dx.first = v == 0, dx.last = v + l.piece >= s.V;
+        dx.g = dx_product(s, cols, b.p, b.wt);
+        dx.out = (char*)p.dx, dx.out_ld = s.D, dx.sum = b.sum, dx.first = v == 0, dx.last = v + l.piece >= s.V, dx.unit = unit;
         dx.target = p.target, dx.V = s.V;
         if (rc == HY_OK) rc = product<T>(dx, b.split, st);
     }
@@ -806,7 +813,7 @@ hy_status backward(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t 
 bool served(const XentShape& s) {
     const Layout l = layout_of(s);
     return l.ld <= (1 << 22) && l.nt <= (1 << 22) && l.piece <= (1 << 22) && cut(s.N, 128) * cut(l.piece, 128) <= INT32_MAX &&
-           cut(s.N * l.ld, 256) <= INT32_MAX && cut(l.piece * l.ld, 256) <= INT32_MAX && l.ld <= 64 * 65535;
+           cut(s.N * l.ld, 256) <= INT32_MAX && cut(l.piece * l.ld, 256) <= INT32_MAX && l.ld <= 64 * 65534;
 }
 
 }  // namespace
@@ -821,7 +828,8 @@ int64_t xent_fwd_workspace_bytes(const XentShape& s) {
 int64_t xent_bwd_workspace_bytes(const XentShape& s) {
     const Layout l = layout_of(s);
     Carver c{nullptr};
-    BwdSpace b(s, l, c);
+    if (s.dtype == HY_F32) BwdSpace<F32>(s, l, c);
+    else BwdSpace<BF16>(s, l, c);
     return c.at - (char*)nullptr;
 }
 
