@@ -330,7 +330,11 @@ class AdamwPlan:
         if rc != HY_OK:
             raise HyenaError(rc, "hyena_adamw_table")
         self._n, self._chunks = n, chunks.value
-        self._table = table.to(params[0].device) if n else table
+        if n:
+            with _on(params[0]):
+                table = table.to(params[0].device)
+                self._home = _stream(params[0], None)  # the stream from whose pool the table is
+        self._table = table
         self._fn = lb.hyena_adamw_step
 
     def __call__(self, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.95, eps: float = 1e-8, grad_scale=None,
@@ -344,8 +348,11 @@ class AdamwPlan:
                                        or grad_scale.numel() != 1 or grad_scale.get_device() != first.get_device()):
             raise ValueError("grad_scale must be one float32 number on the parameters' GPU")
         with _on(first):
+            on = _stream(first, stream)
+            if on != self._home:  # the table must outlive a step on another stream, also where the plan does not
+                self._table.record_stream(torch.cuda.ExternalStream(on, device=first.device))
             rc = self._fn(self._table.data_ptr(), self._n, self._chunks, *self._kinds, lr, beta1, beta2, eps, step,
-                          _ptr(grad_scale), _stream(first, stream))
+                          _ptr(grad_scale), on)
         if rc != HY_OK:
             raise HyenaError(rc, "hyena_adamw_step")
 

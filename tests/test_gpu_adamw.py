@@ -178,3 +178,23 @@ def test_refusals():
     with pytest.raises(ValueError):
         hy.adamw_state([p], bits=4)
     hy.plan_adamw([], [], [], [])(lr=1e-3, step=1)
+
+
+def test_a_step_on_another_stream_outlives_its_plan():
+    """The table's memory must not go to other work of the stream that it came from while a step elsewhere still reads it."""
+    rng = np.random.default_rng(11)
+    made = [torch.from_numpy(rng.normal(size=n).astype(np.float32)).cuda() for n in (70000, 5, 4097)]
+    grads = [torch.full_like(p, 1e-2) for p in made]
+    ref, other = [p.clone() for p in made], [p.clone() for p in made]
+    hy.plan_adamw(ref, grads, **hy.adamw_state(ref))(lr=1e-3, step=1)
+    state = hy.adamw_state(other)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    plan = hy.plan_adamw(other, grads, **state)
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(2000000)  # the step starts a little later than what follows here
+    plan(lr=1e-3, step=1, stream=side)
+    del plan
+    junk = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in (256, 512, 1024, 2048)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(ref, other)) and len(junk) == 4
