@@ -215,8 +215,7 @@ struct GemmSplit {
     static constexpr int kWaves = MW * NW, kThreads = kWaves * kWave;
     static constexpr int WM = BM / MW, WN = BN / NW, MI = WM / 16, NI = WN / 16;
     static constexpr int kPlane = (BM + BN) * kStep * 2, kBytes = 3 * kPlane, kLds = 2 * kBytes;
-    static constexpr int kPieces = (BM + BN) * 4 / kThreads;  // of 8 numbers, of a lane
-    static_assert(kPieces * kThreads == (BM + BN) * 4, "whole pieces");
+    static constexpr int kPieces = ((BM + BN) * 4 + kThreads - 1) / kThreads;  // of 8 numbers, of a lane
 
     f32x4_t acc[MI][NI];
 
@@ -227,7 +226,9 @@ struct GemmSplit {
         int to[kPieces], at[kPieces];
 #pragma unroll
         for (int x = 0; x < kPieces; ++x) {
-            const int i = x * kThreads + (int)threadIdx.x, row = i / 4, piece = i % 4;
+            int i = x * kThreads + (int)threadIdx.x;
+            if ((x + 1) * kThreads > (BM + BN) * 4 && i >= (BM + BN) * 4) i -= x * kThreads;  // none is left: the first ones, as their lanes do
+            const int row = i / 4, piece = i % 4;
             const GemmOperand& o = row < BM ? g.a : g.b;
             int64_t r = row < BM ? m0 + row : n0 + row - BM;
             if (r >= o.rows) r = o.rows - 1;  // rows that do not exist: the last one again

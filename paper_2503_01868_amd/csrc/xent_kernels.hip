@@ -579,7 +579,7 @@ GemmArgs product_of(const GemmOperand& a, const GemmOperand& b, int64_t K) {
 // Tiles of 256 x 256 (1.10 PFLOP/s at 8192 x 4096 x 4096) where they fill most of the chip; else of 128 x 128: four steps in
 // LDS (0.85 PFLOP/s with one workgroup per compute unit, 8192 x 512 x 4096), or two, where more workgroups than compute units
 // can share them.
-enum class Tile { k256, k128Deep, k128, kFew32, kFew64 };
+enum class Tile { k256, k128Deep, k128, kFew32, kFew64, kWide };
 Tile tile_for(const GemmArgs& g) {
     if (cut(g.a.rows, 256) * cut(g.b.rows, 256) >= 192) return Tile::k256;
     return cut(g.a.rows, 128) * cut(g.b.rows, 128) <= 256 ? Tile::k128Deep : Tile::k128;
@@ -592,6 +592,7 @@ Edges edges_of(Tile t) {
         case Tile::k256: return {256, 256};
         case Tile::kFew32: return {32, 64};
         case Tile::kFew64: return {64, 64};
+        case Tile::kWide: return {128, 192};
         default: return {128, 128};
     }
 }
@@ -608,14 +609,20 @@ hy_status by_tile(XentArgs& a, Tile tile, F f) {
     return f(dim3((uint32_t)(mt * nt)));
 }
 
-// The kernels' products: bf16 operands by their tile; fp32 ones in tiles of 128 x 128.
+// fp32 operands: one workgroup per compute unit has room in LDS, so tiles of 128 x 128, or of 128 x 192 where fewer rounds of them are
+// less work for the busiest compute unit and k is not divided instead (1003 x 5003 x 1000: 320 tiles, or 216: MEASURED).
+Tile split_tile(const GemmArgs& g) {
+    const int64_t square = cut(g.a.rows, 128) * cut(g.b.rows, 128), wide = cut(g.a.rows, 128) * cut(g.b.rows, 192);
+    return square > 128 && 3 * cut(wide, 256) < 2 * cut(square, 256) ? Tile::kWide : Tile::k128;
+}
+
 template <typename T>
 Tile logit_tile_for(const GemmArgs& g) {
-    return T::kBytes == 2 ? logit_tile(g) : g.a.rows <= 64 ? Tile::kFew64 : Tile::k128;
+    return T::kBytes == 2 ? logit_tile(g) : g.a.rows <= 64 ? Tile::kFew64 : split_tile(g);
 }
 template <typename T>
 Tile product_tile_for(const GemmArgs& g) {
-    return T::kBytes == 4 ? Tile::k128 : tile_for(g);
+    return T::kBytes == 4 ? split_tile(g) : tile_for(g);
 }
 
 template <typename T>
@@ -623,8 +630,11 @@ hy_status losses(XentArgs& a, hipStream_t st) {
     const Tile tile = logit_tile_for<T>(a.g);
     return by_tile(a, tile, [&](dim3 grid) {
         if constexpr (T::kBytes == 4)
-            return tile == Tile::kFew64 ? launch_kernel(loss_kernel<GemmSplit<64, 64, 1, 4>, 64, 64, 1, 4>, grid, dim3(256), st, a)
-                                        : launch_kernel(loss_kernel<GemmSplit<128, 128, 2, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+            switch (tile) {
+                case Tile::kFew64: return launch_kernel(loss_kernel<GemmSplit<64, 64, 1, 4>, 64, 64, 1, 4>, grid, dim3(256), st, a);
+                case Tile::kWide: return launch_kernel(loss_kernel<GemmSplit<128, 192, 2, 4>, 128, 192, 2, 4>, grid, dim3(512), st, a);
+                default: return launch_kernel(loss_kernel<GemmSplit<128, 128, 2, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+            }
         else
         switch (tile) {
             case Tile::k256: return launch_kernel(loss_kernel<Gemm<256, 256, 2, 4, 2>, 256, 256, 2, 4>, grid, dim3(512), st, a);
@@ -641,8 +651,11 @@ hy_status gradients(XentArgs& a, hipStream_t st) {
     const Tile tile = logit_tile_for<T>(a.g);
     return by_tile(a, tile, [&](dim3 grid) {
         if constexpr (T::kBytes == 4)
-            return tile == Tile::kFew64 ? launch_kernel(grad_kernel<T, GemmSplit<64, 64, 1, 4>, 64, 64, 1, 4>, grid, dim3(256), st, a)
-                                        : launch_kernel(grad_kernel<T, GemmSplit<128, 128, 2, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+            switch (tile) {
+                case Tile::kFew64: return launch_kernel(grad_kernel<T, GemmSplit<64, 64, 1, 4>, 64, 64, 1, 4>, grid, dim3(256), st, a);
+                case Tile::kWide: return launch_kernel(grad_kernel<T, GemmSplit<128, 192, 2, 4>, 128, 192, 2, 4>, grid, dim3(512), st, a);
+                default: return launch_kernel(grad_kernel<T, GemmSplit<128, 128, 2, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+            }
         else
         switch (tile) {
             case Tile::kFew32: return launch_kernel(grad_kernel<T, Gemm<32, 64, 1, 4, 6>, 32, 64, 1, 4>, grid, dim3(256), st, a);
@@ -707,7 +720,9 @@ hy_status product(XentArgs& a, float* split, hipStream_t st) {
     const Tile tile = product_tile_for<T>(a.g);
     hy_status rc = by_tile(a, tile, [&](dim3 grid) {
         grid.x *= (uint32_t)a.splits;
-        if constexpr (T::kBytes == 4) return launch_kernel(product_kernel<T, GemmSplit<128, 128, 2, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+        if constexpr (T::kBytes == 4)
+            return tile == Tile::kWide ? launch_kernel(product_kernel<T, GemmSplit<128, 192, 2, 4>, 128, 192, 2, 4>, grid, dim3(512), st, a)
+                                       : launch_kernel(product_kernel<T, GemmSplit<128, 128, 2, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
         else
         switch (tile) {
             case Tile::k256: return launch_kernel(product_kernel<T, Gemm<256, 256, 2, 4, 2>, 256, 256, 2, 4>, grid, dim3(512), st, a);
