@@ -610,7 +610,7 @@ hy_status by_tile(XentArgs& a, Tile tile, F f) {
 }
 
 // fp32 operands: one workgroup per compute unit has room in LDS, so tiles of 128 x 128, or of 128 x 192 where fewer rounds of them are
-// less work for the busiest compute unit and k is not divided instead (1003 x 5003 x 1000: 320 tiles, or 216: MEASURED).
+// less work for the busiest compute unit and k is not divided instead (1003 x 5003 x 1000: 320 tiles, or 216: 369 us a training step, or 294).
 Tile split_tile(const GemmArgs& g) {
     const int64_t square = cut(g.a.rows, 128) * cut(g.b.rows, 128), wide = cut(g.a.rows, 128) * cut(g.b.rows, 192);
     return square > 128 && 3 * cut(wide, 256) < 2 * cut(square, 256) ? Tile::kWide : Tile::k128;
@@ -622,7 +622,8 @@ Tile logit_tile_for(const GemmArgs& g) {
 }
 template <typename T>
 Tile product_tile_for(const GemmArgs& g) {
-    return T::kBytes == 4 ? split_tile(g) : tile_for(g);
+    if (T::kBytes == 2) return tile_for(g);
+    return g.a.rows <= 64 || g.K <= 64 ? Tile::kFew64 : split_tile(g);
 }
 
 template <typename T>
@@ -671,9 +672,12 @@ hy_status gradients(XentArgs& a, hipStream_t st) {
 // they hold, of at least 8 steps each.
 template <typename T>
 int32_t splits_for(const GemmArgs& g) {
-    const int64_t tiles = cut(g.a.rows, 128) * cut(g.b.rows, 128), steps = g.K / (T::kBytes == 4 ? 32 : 64);
-    if (tiles > 128 || product_tile_for<T>(g) == Tile::k256) return 1;
-    return (int32_t)std::max<int64_t>(1, std::min<int64_t>({256 / tiles, steps / 8, 16}));
+    const Tile tile = product_tile_for<T>(g);
+    const Edges e = edges_of(tile);
+    const int64_t tiles = cut(g.a.rows, e.rows) * cut(g.b.rows, e.cols), steps = g.K / (T::kBytes == 4 ? 32 : 64);
+    const int64_t room = tile == Tile::kFew64 ? 3 * 256 : 256;
+    if (2 * tiles > room || tile == Tile::k256) return 1;
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>({room / tiles, steps / 8, 16}));
 }
 
 // The two products of a piece of `cols` columns.
@@ -721,8 +725,11 @@ hy_status product(XentArgs& a, float* split, hipStream_t st) {
     hy_status rc = by_tile(a, tile, [&](dim3 grid) {
         grid.x *= (uint32_t)a.splits;
         if constexpr (T::kBytes == 4)
-            return tile == Tile::kWide ? launch_kernel(product_kernel<T, GemmSplit<128, 192, 2, 4>, 128, 192, 2, 4>, grid, dim3(512), st, a)
-                                       : launch_kernel(product_kernel<T, GemmSplit<128, 128, 2, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+            switch (tile) {
+                case Tile::kFew64: return launch_kernel(product_kernel<T, GemmSplit<64, 64, 1, 4>, 64, 64, 1, 4>, grid, dim3(256), st, a);
+                case Tile::kWide: return launch_kernel(product_kernel<T, GemmSplit<128, 192, 2, 4>, 128, 192, 2, 4>, grid, dim3(512), st, a);
+                default: return launch_kernel(product_kernel<T, GemmSplit<128, 128, 2, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+            }
         else
         switch (tile) {
             case Tile::k256: return launch_kernel(product_kernel<T, Gemm<256, 256, 2, 4, 2>, 256, 256, 2, 4>, grid, dim3(512), st, a);
