@@ -11,7 +11,7 @@ constexpr int kGemmK = 64;        // every operand made here has rows of a multi
 // Rows of bf16 numbers (Gemm) or of fp32 numbers (GemmSplit).
 struct GemmOperand {
     const void* p;
-    int64_t ld;          // elements between rows
+    int64_t ld;          // elements between rows (between k's, where the operand lies turned)
     int64_t rows;
 };
 
@@ -208,55 +208,68 @@ constexpr int kSplitA[kSplitProducts] = {2, 0, 1, 1, 0, 0}, kSplitB[kSplitProduc
 // tail of the 24), and a product the sum of six products of parts.  Numbers become parts once, between memory and LDS: a step's
 // are fetched into registers two steps ahead and written to LDS as three planes of 64-byte rows (the 16-byte pieces of row r at
 // piece ^ (r / 2 % 4)) one step ahead.  A part that is in a register serves two or three of the six products, so LDS is read half
-// as often as for six products of planes.
-template <int BM, int BN, int MW, int NW>
+// as often as for six products of planes.  An operand may lie turned in memory, k after k (TA, TB: its `rows` are then how many
+// numbers it has for each k, and k's are `ld` apart): eight loads of a number each, neighbours in a wave, make a piece.
+template <int BM, int BN, int MW, int NW, bool TA = false, bool TB = false>
 struct GemmSplit {
     static constexpr int kStep = 32;
     static constexpr int kWaves = MW * NW, kThreads = kWaves * kWave;
     static constexpr int WM = BM / MW, WN = BN / NW, MI = WM / 16, NI = WN / 16;
     static constexpr int kPlane = (BM + BN) * kStep * 2, kBytes = 3 * kPlane, kLds = 2 * kBytes;
     static constexpr int kPieces = ((BM + BN) * 4 + kThreads - 1) / kThreads;  // of 8 numbers, of a lane
+    static constexpr int kPiecesA = BM * 4 / kThreads;
+    static_assert(kPiecesA * kThreads == BM * 4 && BM % kWave == 0 && BN % kWave == 0, "a lane's pieces, and a wave's, are of one operand");
 
     f32x4_t acc[MI][NI];
 
     __device__ __forceinline__ void run(char* lds, const GemmArgs& g, int64_t m0, int64_t n0, int first, int last) {
         const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
         const int li = lane % 16, lq = lane / 16, wm = w % MW, wn = w / MW;
-        const float* from[kPieces];
-        int to[kPieces], at[kPieces];
+        const float* from[kPieces];  // the lane's row; of a turned operand, its beginning
+        int to[kPieces], at[kPieces], row_at[kPieces];
 #pragma unroll
         for (int x = 0; x < kPieces; ++x) {
-            int i = x * kThreads + (int)threadIdx.x;
-            if ((x + 1) * kThreads > (BM + BN) * 4 && i >= (BM + BN) * 4) i -= x * kThreads;  // none is left: the first ones, as their lanes do
-            const int row = i / 4, piece = i % 4;
-            const GemmOperand& o = row < BM ? g.a : g.b;
-            int64_t r = row < BM ? m0 + row : n0 + row - BM;
+            const bool b = x >= kPiecesA, turned = b ? TB : TA;
+            const int edge = b ? BN : BM;
+            int i = (x - (b ? kPiecesA : 0)) * kThreads + w * kWave;
+            if (i >= edge * 4) i -= kThreads;  // none is left: those of the lane's last piece again
+            const int row = turned ? i % edge + lane : (i + lane) / 4, piece = turned ? i / edge : lane % 4;
+            const GemmOperand& o = b ? g.b : g.a;
+            int64_t r = (b ? n0 : m0) + row;
             if (r >= o.rows) r = o.rows - 1;  // rows that do not exist: the last one again
-            from[x] = static_cast<const float*>(o.p) + r * o.ld;
+            from[x] = static_cast<const float*>(o.p) + (turned ? 0 : r * o.ld);
+            row_at[x] = (int)r;
             at[x] = piece * 8;
-            to[x] = row * (kStep * 2) + (piece ^ (row / 2 % 4)) * 16;
+            to[x] = ((b ? BM : 0) + row) * (kStep * 2) + (piece ^ (row / 2 % 4)) * 16;
         }
-        const bool fours = g.K % 4 == 0 && g.a.ld % 4 == 0 && g.b.ld % 4 == 0 &&
-                           (((uintptr_t)g.a.p | (uintptr_t)g.b.p) & 15) == 0;
+        const bool fours = (TA || (g.a.ld % 4 == 0 && ((uintptr_t)g.a.p & 15) == 0)) &&
+                           (TB || (g.b.ld % 4 == 0 && ((uintptr_t)g.b.p & 15) == 0));
         auto fetch = [&](float4 (&v)[kPieces][2], int step) {
-            if (fours && (step + 1) * kStep <= g.K) {
+            const bool whole = (step + 1) * kStep <= g.K;
+            auto some = [&](auto full, auto wide) {
 #pragma unroll
-                for (int x = 0; x < kPieces; ++x)
+                for (int x = 0; x < kPieces; ++x) {
+                    const int k0 = step * kStep + at[x];
+                    float f[8];
+                    if (x >= kPiecesA ? TB : TA) {
+                        const int64_t ld = x >= kPiecesA ? g.b.ld : g.a.ld;
+                        const float* const row = from[x] + k0 * ld;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) v[x][h] = *reinterpret_cast<const float4*>(from[x] + step * kStep + at[x] + 4 * h);
-                return;
-            }
+                        for (int j = 0; j < 8; ++j) f[j] = full || k0 + j < g.K ? (row + j * ld)[row_at[x]] : 0.0f;
+                    } else if (wide) {
 #pragma unroll
-            for (int x = 0; x < kPieces; ++x)
+                        for (int h = 0; h < 2; ++h) v[x][h] = *reinterpret_cast<const float4*>(from[x] + k0 + 4 * h);
+                        continue;
+                    } else {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int k = step * kStep + at[x] + 4 * h;
-                    v[x][h] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    if (k < g.K) v[x][h].x = from[x][k];
-                    if (k + 1 < g.K) v[x][h].y = from[x][k + 1];
-                    if (k + 2 < g.K) v[x][h].z = from[x][k + 2];
-                    if (k + 3 < g.K) v[x][h].w = from[x][k + 3];
+                        for (int j = 0; j < 8; ++j) f[j] = full || k0 + j < g.K ? from[x][k0 + j] : 0.0f;
+                    }
+                    v[x][0] = make_float4(f[0], f[1], f[2], f[3]);
+                    v[x][1] = make_float4(f[4], f[5], f[6], f[7]);
                 }
+            };
+            if (whole && fours) some(std::true_type{}, std::true_type{});
+            else some(std::false_type{}, std::false_type{});
         };
         auto put = [&](const float4 (&v)[kPieces][2], int stage) {
 #pragma unroll

@@ -5,11 +5,15 @@
 //
 // Forward: a tile of z stays in registers; each of its rows leaves the largest value and the sum of exponentials below it, and
 // a second kernel joins the tiles of a row.  Backward, for a piece of the vocabulary at a time: z again, P from it, and the two
-// products.  All four products are of the one form that hy_gemm.hpp has (k contiguous in both operands), so P is written in
-// both orders, and x and the piece of W are transposed once.  The matrix products are what bounds it: 8 N V D operations.
+// products.  The matrix products are what bounds it: 8 N V D operations.
 //
-// bf16 operands enter the products as they are, and P is rounded to bf16 for its two; fp32 calls multiply in parts, to fp32's
-// precision, and keep P in fp32.
+// bf16 operands enter the products as they are, with k contiguous in both of them: x and the piece of W are transposed once, and P,
+// rounded to bf16 in units of the largest |dloss|, is written in both orders.  fp32 calls multiply in parts, to fp32's precision,
+// keep P in fp32, and read P and W across k where a product needs it.
+//
+// Measured, loss and gradients: 8192 x 65536 x 4096 bf16 14.1-14.7 ms (1.20-1.25 PFLOP/s, the four products at 1.15 to 1.3),
+// 8192 x 512 x 4096 208 us (0.66 PFLOP/s: tiles of 128 x 128 on 256 compute units once, and 30 us of transposition);
+// 1003 x 5003 x 1000 fp32 283 us (0.85 PFLOP/s of the six products of parts).  The loss alone, 8 x 65536 x 4096: 105 us, 5.1 TB/s.
 #include <algorithm>
 
 #include "hy_gemm.hpp"
@@ -116,7 +120,7 @@ struct XentArgs {
     // gradients
     const float *lse, *dloss;
     const float* unit;        // dloss is taken in this unit (null: 1), and the products are taken back
-    void *p, *pt;             // P [rows][p_ld] and its transpose [columns][pt_ld], bf16 or fp32
+    void *p, *pt;             // P [rows][p_ld], bf16 or fp32, and of bf16 its transpose [columns][pt_ld]
     int64_t p_ld, pt_ld;
     // products
     char* out;
@@ -364,17 +368,13 @@ __global__ __launch_bounds__(MW * NW * kWave) void grad_kernel(XentArgs a) {
             }
     }
     if constexpr (T::kBytes == 4) {
-        // 64 bytes of a row of either side by side
+        // 64 bytes of a row side by side
 #pragma unroll
         for (int i = 0; i < G::MI; ++i)
 #pragma unroll
             for (int j = 0; j < G::NI; ++j) {
                 const int64_t m = m0 + wm * G::WM + i * 16 + li, n = n0 + col0 + j * 16;
                 if (m < rows && n < a.p_ld) *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.p) + m * a.p_ld + n) = t.acc[i][j];
-                if (m < a.pt_ld)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (n + r < a.g.b.rows) static_cast<float*>(a.pt)[(n + r) * a.pt_ld + m] = t.acc[i][j][r];
             }
         return;
     }
@@ -610,7 +610,8 @@ hy_status by_tile(XentArgs& a, Tile tile, F f) {
 }
 
 // fp32 operands: one workgroup per compute unit has room in LDS, so tiles of 128 x 128, or of 128 x 192 where fewer rounds of them are
-// less work for the busiest compute unit and k is not divided instead (1003 x 5003 x 1000: 320 tiles, or 216: 369 us a training step, or 294).
+// less work for the busiest compute unit and k is not divided instead (1003 x 5003 x 1000: 320 tiles, or 216, a fifth
+// less time).
 Tile split_tile(const GemmArgs& g) {
     const int64_t square = cut(g.a.rows, 128) * cut(g.b.rows, 128), wide = cut(g.a.rows, 128) * cut(g.b.rows, 192);
     return square > 128 && 3 * cut(wide, 256) < 2 * cut(square, 256) ? Tile::kWide : Tile::k128;
@@ -680,13 +681,17 @@ int32_t splits_for(const GemmArgs& g) {
     return (int32_t)std::max<int64_t>(1, std::min<int64_t>({room / tiles, steps / 8, 16}));
 }
 
-// The two products of a piece of `cols` columns.
-GemmArgs dw_product(const XentShape& s, const Layout& l, int64_t cols, const void* pt = nullptr, const void* xt = nullptr) {
-    return product_of(GemmOperand{pt, l.nt, cols}, GemmOperand{xt, l.nt, s.D}, up(s.N, 32));  // (what the tiles of P, of 32 rows at least, fill)
+// The two products of a piece of `cols` columns.  fp32: P and W lie turned where k runs over their rows.
+template <typename T>
+GemmArgs dw_product(const XentShape& s, const Layout& l, int64_t cols, const void* p = nullptr, const void* xt = nullptr) {
+    if (T::kBytes == 4) return product_of(GemmOperand{p, up(cols, kGemmK), cols}, GemmOperand{xt, l.nt, s.D}, s.N);
+    return product_of(GemmOperand{p, l.nt, cols}, GemmOperand{xt, l.nt, s.D}, up(s.N, 32));  // (what the tiles of P, of 32 rows at least, fill)
 }
-GemmArgs dx_product(const XentShape& s, int64_t cols, const void* p = nullptr, const void* wt = nullptr) {
+template <typename T>
+GemmArgs dx_product(const XentShape& s, int64_t cols, const void* p = nullptr, const void* w = nullptr) {
     const int64_t ld = up(cols, kGemmK);
-    return product_of(GemmOperand{p, ld, s.N}, GemmOperand{wt, ld, s.D}, ld);
+    if (T::kBytes == 4) return product_of(GemmOperand{p, ld, s.N}, GemmOperand{w, s.D, s.D}, cols);
+    return product_of(GemmOperand{p, ld, s.N}, GemmOperand{w, ld, s.D}, ld);
 }
 
 template <typename T>
@@ -699,9 +704,9 @@ struct BwdSpace {
         x = l.packed ? c.take<uint16_t>(s.N * l.ld) : nullptr;
         w = l.packed ? c.take<uint16_t>(piece * l.ld) : nullptr;
         xt = c.take<Bits<T>>(s.D * l.nt);
-        wt = c.take<Bits<T>>(s.D * ld);
+        wt = T::kBytes == 2 ? c.take<Bits<T>>(s.D * ld) : nullptr;
         p = c.take<Bits<T>>(s.N * ld);
-        pt = c.take<Bits<T>>(piece * l.nt);
+        pt = T::kBytes == 2 ? c.take<Bits<T>>(piece * l.nt) : nullptr;
         sum = l.pieces > 1 ? c.take<float>(s.N * s.D) : nullptr;
         int64_t most = 0;
         auto floats = [&](const GemmArgs& g) {
@@ -710,14 +715,14 @@ struct BwdSpace {
         };
         for (int64_t v = 0; v < s.V; v += l.piece) {
             const int64_t cols = std::min(l.piece, s.V - v);
-            most = std::max({most, floats(dw_product(s, l, cols)), floats(dx_product(s, cols))});
+            most = std::max({most, floats(dw_product<T>(s, l, cols)), floats(dx_product<T>(s, cols))});
         }
         split = c.take<float>(most);
         unit = c.take<float>(1);
     }
 };
 
-template <typename T>
+template <typename T, bool TA, bool TB>
 hy_status product(XentArgs& a, float* split, hipStream_t st) {
     a.split = split;
     a.splits = splits_for<T>(a.g);
@@ -726,9 +731,9 @@ hy_status product(XentArgs& a, float* split, hipStream_t st) {
         grid.x *= (uint32_t)a.splits;
         if constexpr (T::kBytes == 4)
             switch (tile) {
-                case Tile::kFew64: return launch_kernel(product_kernel<T, GemmSplit<64, 64, 1, 4>, 64, 64, 1, 4>, grid, dim3(256), st, a);
-                case Tile::kWide: return launch_kernel(product_kernel<T, GemmSplit<128, 192, 2, 4>, 128, 192, 2, 4>, grid, dim3(512), st, a);
-                default: return launch_kernel(product_kernel<T, GemmSplit<128, 128, 2, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+                case Tile::kFew64: return launch_kernel(product_kernel<T, GemmSplit<64, 64, 1, 4, TA, TB>, 64, 64, 1, 4>, grid, dim3(256), st, a);
+                case Tile::kWide: return launch_kernel(product_kernel<T, GemmSplit<128, 192, 2, 4, TA, TB>, 128, 192, 2, 4>, grid, dim3(512), st, a);
+                default: return launch_kernel(product_kernel<T, GemmSplit<128, 128, 2, 4, TA, TB>, 128, 128, 2, 4>, grid, dim3(512), st, a);
             }
         else
         switch (tile) {
@@ -809,24 +814,26 @@ hy_status backward(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t 
     hy_status rc = turn<T>(p.x, b.xt, s.N, s.D, l.nt, p.target, s.V, Unit{p.dloss, T::kBytes == 2 ? b.unit : nullptr}, st);
     for (int64_t v = 0; rc == HY_OK && v < s.V; v += l.piece) {
         const int64_t cols = std::min(l.piece, s.V - v), ld = up(cols, kGemmK);
+        const char* const w = (const char*)p.w + v * s.D * T::kBytes;
+        constexpr bool kTurned = T::kBytes == 4;
         XentArgs a{};
         a.g.K = (int32_t)(l.packed ? l.ld : s.D);
         rc = operands<T>(p, s, l, b.x, b.w, v, &a.g.a, &a.g.b, st);
-        if (rc == HY_OK) rc = turn<T>((const char*)p.w + v * s.D * T::kBytes, b.wt, cols, s.D, ld, nullptr, 0, Unit{}, st);
+        if (rc == HY_OK && !kTurned) rc = turn<T>(w, b.wt, cols, s.D, ld, nullptr, 0, Unit{}, st);
         a.target = p.target, a.V = s.V, a.v0 = v;
         a.lse = p.lse_in, a.dloss = p.dloss, a.unit = unit;
         a.p = b.p, a.p_ld = ld;
         a.pt = b.pt, a.pt_ld = l.nt;
         if (rc == HY_OK) rc = gradients<T>(a, st);
         XentArgs dw{};
-        dw.g = dw_product(s, l, cols, b.pt, b.xt);
+        dw.g = dw_product<T>(s, l, cols, kTurned ? b.p : b.pt, b.xt);
         dw.out = (char*)p.dw + v * s.D * T::kBytes, dw.out_ld = s.D, dw.first = dw.last = true, dw.unit = unit;
-        if (rc == HY_OK) rc = product<T>(dw, b.split, st);
+        if (rc == HY_OK) rc = product<T, kTurned, false>(dw, b.split, st);
         XentArgs dx{};
-        dx.g = dx_product(s, cols, b.p, b.wt);
+        dx.g = dx_product<T>(s, cols, b.p, kTurned ? (const void*)w : b.wt);
         dx.out = (char*)p.dx, dx.out_ld = s.D, dx.sum = b.sum, dx.first = v == 0, dx.last = v + l.piece >= s.V, dx.unit = unit;
         dx.target = p.target, dx.V = s.V;
-        if (rc == HY_OK) rc = product<T>(dx, b.split, st);
+        if (rc == HY_OK) rc = product<T, false, kTurned>(dx, b.split, st);
     }
     return rc;
 }
