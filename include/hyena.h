@@ -399,6 +399,7 @@ int64_t hyena_bwd_shard_workspace_bytes(int64_t B, int64_t L, int64_t D, int32_t
  * a row; negative: HY_ERR_SHAPE).  Outputs are dense.  q, k, v, g may begin at any element, every other
  * pointer is 16-byte aligned; where a size is zero the pointers to what is empty may be NULL.
  * workspace: hyena_glr_fwd_workspace_bytes(...) bytes, disjoint from every argument, contents undefined afterwards.
+ * D and the distances between steps are at most 2^26 elements (HY_ERR_UNSUPPORTED); L and whole tensors may pass 2^32.
  */
 #define HYENA_GLR_MARK_ROWS 64
 hy_status hyena_glr_fwd(const void *q, const void *k, const void *v, const void *g, const float *state_in, void *y,
@@ -436,7 +437,8 @@ hy_status hyena_glr_step(const void *q, const void *k, const void *v, const void
  * x: [N,D], w: [V,D], dense, of `dtype`; target: int64 [N]; loss, lse: fp32 [N].  A row whose target is outside 0 .. V - 1 takes no
  * part: its loss is 0 (its lse is written all the same).  The products run on the bf16 matrix cores with fp32 sums: bf16
  * operands as they are, fp32 operands as three bf16 parts each, to fp32's precision.
- * V, D >= 1 (HY_ERR_SHAPE); N = 0 is an empty problem.  workspace: hyena_xent_fwd_workspace_bytes(...) bytes.
+ * V, D >= 1 (HY_ERR_SHAPE); N = 0 is an empty problem; N, D up to 4194112 and N D up to 2^39 (HY_ERR_UNSUPPORTED).
+ * workspace: hyena_xent_fwd_workspace_bytes(...) bytes.
  */
 hy_status hyena_xent_fwd(const void *x, const void *w, const int64_t *target, float *loss, float *lse, void *workspace,
                          int64_t workspace_bytes, int64_t N, int64_t V, int64_t D, int32_t dtype, void *hip_stream);
@@ -446,7 +448,8 @@ int64_t hyena_xent_fwd_workspace_bytes(int64_t N, int64_t V, int64_t D, int32_t 
  * Backward of hyena_xent_fwd.  With dloss[n] = dLoss/dloss[n] (fp32 [N]; 1/N for a mean) and lse as the forward call wrote it,
  *     P[n,v] = dloss[n] * (exp(z[n,v] - lse[n]) - [v = target[n]]),   dx = P W,   dw = P^T x
  * dx: [N,D], dw: [V,D], of `dtype`, overwritten; zeros in dx for rows that take no part, and nothing in dw from them, whatever
- * they hold.  P is rounded to bf16 for its two products in bf16 calls; sums are fp32, in a fixed order, one rounding per stored
+ * they hold.  P is rounded to bf16 for its two products in bf16 calls, in units of the largest |dloss| (a constant weight such as
+ * 1 / N costs no rounding), and kept in fp32 in fp32 calls; sums are fp32, in a fixed order, one rounding per stored
  * element.  The vocabulary is taken in pieces: workspace (hyena_xent_bwd_workspace_bytes(...) bytes) holds P of one piece.
  */
 hy_status hyena_xent_bwd(const float *dloss, const void *x, const void *w, const int64_t *target, const float *lse, void *dx,

@@ -58,6 +58,15 @@ def _glr_input(name: str, t: torch.Tensor, shape, ref: torch.Tensor) -> None:
         raise ValueError("%s must have contiguous channels" % name)
 
 
+def _glr_inputs(named, ref: torch.Tensor) -> None:
+    """_glr_input of every (name, tensor, shape); the flags alone where they are as they mostly are."""
+    dtype, gpu = ref.dtype, ref.get_device()
+    for name, t, shape in named:
+        if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == gpu and t.shape == shape
+                and t.is_contiguous()):
+            _glr_input(name, t, shape, ref)
+
+
 def _glr_shapes(first: torch.Tensor, group: int, dims: int):
     """Shapes of an activation and of the log decays."""
     if not isinstance(first, torch.Tensor) or not first.is_cuda:
@@ -116,8 +125,7 @@ def _output(t, shape, ref: torch.Tensor, name: str):
 def _glr_fwd(q, k, v, g, group, state_in, want_state, want_marks, out, workspace, stream):
     shape, gates = _glr_shapes(q, group, 3)
     code = _dtype_code(q)
-    for name, t, s in (("q", q, shape), ("k", k, shape), ("v", v, shape), ("g", g, gates)):
-        _glr_input(name, t, s, q)
+    _glr_inputs((("q", q, shape), ("k", k, shape), ("v", v, shape), ("g", g, gates)), q)
     B, L, D = shape
     before = _glr_state("state_in", state_in, B, D, q)
     lb = lib()
@@ -153,8 +161,7 @@ def hyena_glr_bwd(dy, q, k, v, g, group: int = 1, marks=None, state_in=None, dst
     group = int(group)
     shape, gates = _glr_shapes(dy, group, 3)
     code = _dtype_code(dy)
-    for name, t, s in (("dy", dy, shape), ("q", q, shape), ("k", k, shape), ("v", v, shape), ("g", g, gates)):
-        _glr_input(name, t, s, dy)
+    _glr_inputs((("dy", dy, shape), ("q", q, shape), ("k", k, shape), ("v", v, shape), ("g", g, gates)), dy)
     B, L, D = shape
     if marks is not None and (marks.dtype != torch.float32 or marks.shape != (B, -(-L // GLR_MARK_ROWS), D)
                               or not marks.is_contiguous() or marks.get_device() != dy.get_device()):
@@ -181,8 +188,8 @@ def hyena_glr_step(q, k, v, g, state, group: int = 1, out=None, stream=None) -> 
     group = int(group)
     shape, gates = _glr_shapes(q, group, 2)
     code = _dtype_code(q)
-    for name, t, s in (("q", q, shape), ("k", k, shape), ("v", v, shape), ("g", g, gates)):
-        _glr_input(name, t, s, q)
+    _glr_inputs((("q", q, shape), ("k", k, shape), ("v", v, shape), ("g", g, gates)), q)
+    for name, t in (("q", q), ("k", k), ("v", v), ("g", g)):
         if not t.is_contiguous():
             raise ValueError("%s must be contiguous" % name)
     B, D = shape
@@ -190,7 +197,7 @@ def hyena_glr_step(q, k, v, g, state, group: int = 1, out=None, stream=None) -> 
         raise ValueError("state must be a contiguous float32 [B, D] tensor on the same GPU")
     st = _glr_state("state", state, B, D, q)
     with _on(q), _under(q, stream):
-        y = _output(out, shape, q, "out")
+        y = torch.empty_like(q) if out is None else _output(out, shape, q, "out")
         rc = lib().hyena_glr_step(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), st, y.data_ptr(), B, D, group, code,
                                   _stream(q, stream))
     if rc != HY_OK:
@@ -217,7 +224,11 @@ def _xent_column(name, t, N, x):
     if (not isinstance(t, torch.Tensor) or t.dtype != torch.float32 or t.shape != (N,) or not t.is_contiguous()
             or t.get_device() != x.get_device()):
         raise ValueError("%s must be a contiguous float32 [N] tensor on x's GPU" % name)
-    return t.data_ptr()
+
+
+def _at_16_bytes(t):
+    """A column as the library takes it: one that begins between (tokens[1:], say) is copied."""
+    return t if t.data_ptr() % 16 == 0 else t.clone()
 
 
 def hyena_xent_fwd(x, w, target, workspace=None, stream=None):
@@ -227,6 +238,7 @@ def hyena_xent_fwd(x, w, target, workspace=None, stream=None):
     lb = lib()
     with _on(x), _under(x, stream):
         loss, lse = (torch.empty(N, dtype=torch.float32, device=x.device) for _ in range(2))
+        target = _at_16_bytes(target)
         ws, nbytes, keep = _workspace(int(lb.hyena_xent_fwd_workspace_bytes(N, V, D, code)), workspace, x)
         rc = lb.hyena_xent_fwd(x.data_ptr(), w.data_ptr(), target.data_ptr(), loss.data_ptr(), lse.data_ptr(), ws, nbytes, N, V, D,
                                code, _stream(x, stream))
@@ -239,13 +251,15 @@ def hyena_xent_bwd(dloss, x, w, target, lse, workspace=None, stream=None):
     """(dx, dw) of ``hyena_xent_fwd``, given the gradient of every row's loss (1 / N for a mean) and the ``lse`` it returned; see
     ``hyena_xent_bwd`` in hyena.h."""
     N, V, D, code = _xent_inputs(x, w, target)
-    dl, ls = _xent_column("dloss", dloss, N, x), _xent_column("lse", lse, N, x)
+    _xent_column("dloss", dloss, N, x)
+    _xent_column("lse", lse, N, x)
     lb = lib()
     with _on(x), _under(x, stream):
         dx, dw = torch.empty_like(x), torch.empty_like(w)
+        dloss, target, lse = _at_16_bytes(dloss), _at_16_bytes(target), _at_16_bytes(lse)
         ws, nbytes, keep = _workspace(int(lb.hyena_xent_bwd_workspace_bytes(N, V, D, code)), workspace, x)
-        rc = lb.hyena_xent_bwd(dl, x.data_ptr(), w.data_ptr(), target.data_ptr(), ls, dx.data_ptr(), dw.data_ptr(), ws, nbytes, N, V,
-                               D, code, _stream(x, stream))
+        rc = lb.hyena_xent_bwd(dloss.data_ptr(), x.data_ptr(), w.data_ptr(), target.data_ptr(), lse.data_ptr(), dx.data_ptr(),
+                               dw.data_ptr(), ws, nbytes, N, V, D, code, _stream(x, stream))
     if rc != HY_OK:
         raise HyenaError(rc, "hyena_xent_bwd")
     return dx, dw

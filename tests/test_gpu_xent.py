@@ -172,3 +172,22 @@ def test_refusals():
         hy.hyena_xent_bwd(dloss.double(), x, w, target, lse)
     with pytest.raises(ValueError):
         hy.hyena_xent_bwd(dloss, x, w, target, lse[:3])
+
+
+@pytest.mark.parametrize("N,V,D", [(260, 11008, 36), (400, 390, 8300), (33, 40, 70), (64, 1000, 130), (1000, 50, 200), (7, 9000, 132)])
+def test_float_rows_by_every_tile(N, V, D):
+    """Tiles that are wider than high in either kind of product, tiles of few rows or short k, k divided among workgroups."""
+    say("xent f32 %d x %d x %d" % (N, V, D))
+    check(*make(N + V + D, N, V, D, "f32"), "f32")
+
+
+def test_columns_that_begin_between_16_bytes():
+    """The targets of a text are the text one further."""
+    x, w, target, dloss = make(5, 101, 300, 64, "bf16")
+    text, weights = (torch.cat([t[:1], t]) for t in (target, dloss))
+    loss, lse = hy.hyena_xent_fwd(x, w, target)
+    shifted = hy.hyena_xent_fwd(x, w, text[1:])
+    assert torch.equal(loss, shifted[0]) and torch.equal(lse, shifted[1])
+    column = torch.cat([lse[:1], lse])[1:]
+    for a, b in zip(hy.hyena_xent_bwd(dloss, x, w, target, lse), hy.hyena_xent_bwd(weights[1:], x, w, text[1:], column)):
+        assert torch.equal(a, b)
