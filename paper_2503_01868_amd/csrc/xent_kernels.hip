@@ -333,6 +333,31 @@ __global__ __launch_bounds__(256) void join_kernel(const float2* part, const flo
     }
 }
 
+// A wave's part of a result, rounded to bf16, to rows of `ld` (a multiple of 8) from (m0, n0) on, as far as there are `rows` and `cols`
+// (a multiple of 8): through its own part of LDS, so that a row leaves in 16-byte pieces side by side.
+template <typename G>
+__device__ __forceinline__ void rows_out(const f32x4_t (&acc)[G::MI][G::NI], uint32_t* own, uint16_t* to, int64_t ld, int64_t m0, int64_t n0,
+                                         int64_t rows, int64_t cols) {
+    const int lane = threadIdx.x % kWave, li = lane % 16, lq = lane / 16;
+    constexpr int kMask = G::WN / 8 < 8 ? G::WN / 8 - 1 : 7;  // pieces of 4 words trade places by row
+#pragma unroll
+    for (int i = 0; i < G::MI; ++i)
+#pragma unroll
+        for (int j = 0; j < G::NI; ++j) {
+            const int row = i * 16 + li, piece = j * 2 + lq / 2;
+            *reinterpret_cast<uint2*>(own + row * (G::WN / 2) + (piece ^ (row & kMask)) * 4 + lq % 2 * 2) =
+                make_uint2(pack_bf16x2(acc[i][j][0], acc[i][j][1]), pack_bf16x2(acc[i][j][2], acc[i][j][3]));
+        }
+    constexpr int kLanes = G::WN / 8;
+#pragma unroll
+    for (int y = 0; y < G::WM; y += kWave / kLanes) {
+        const int row = y + lane / kLanes, piece = lane % kLanes;
+        const uint4 v = *reinterpret_cast<const uint4*>(own + row * (G::WN / 2) + (piece ^ (row & kMask)) * 4);
+        const int64_t m = m0 + row, n = n0 + 8 * piece;
+        if (m < rows && n < cols) *reinterpret_cast<uint4*>(to + m * ld + n) = v;
+    }
+}
+
 template <typename T, typename G, int BM, int BN, int MW, int NW>
 __global__ __launch_bounds__(MW * NW * kWave) void grad_kernel(XentArgs a) {
     __shared__ __attribute__((aligned(16))) char lds[G::kLds + BM * 16];
@@ -380,8 +405,7 @@ __global__ __launch_bounds__(MW * NW * kWave) void grad_kernel(XentArgs a) {
     }
     // Both orders go out through the wave's own part of LDS, so that a row leaves in 16-byte pieces side by side.  As they are in
     // the registers, four columns or one row at a time, they took a fifth of the kernel's time.
-    constexpr int kT = G::WM / 2, kTMask = kT / 8 - 1;         // P^T: words of a row; pieces of 8 words trade places by row
-    constexpr int kPMask = G::WN / 8 < 8 ? G::WN / 8 - 1 : 7;  // P: pieces of 4 words trade places by row
+    constexpr int kT = G::WM / 2, kTMask = kT / 8 - 1;  // P^T: words of a row; pieces of 8 words trade places by row
     uint32_t* own = reinterpret_cast<uint32_t*>(lds) + w * (G::WM * G::WN / 2);
     __syncthreads();  // the tiles have been read
     {
@@ -407,22 +431,7 @@ __global__ __launch_bounds__(MW * NW * kWave) void grad_kernel(XentArgs a) {
             const int64_t n = n0 + wn * G::WN + row, m = m0 + wm * G::WM + 2 * word;
             if (n < a.g.b.rows && m < a.pt_ld) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.pt) + n * a.pt_ld + m) = v;
         }
-#pragma unroll
-        for (int i = 0; i < G::MI; ++i)
-#pragma unroll
-            for (int j = 0; j < G::NI; ++j) {
-                const int row = i * 16 + li, piece = j * 2 + lq / 2;
-                *reinterpret_cast<uint2*>(own + row * (G::WN / 2) + (piece ^ (row & kPMask)) * 4 + lq % 2 * 2) =
-                    make_uint2(pack_bf16x2(t.acc[i][j][0], t.acc[i][j][1]), pack_bf16x2(t.acc[i][j][2], t.acc[i][j][3]));
-            }
-        constexpr int kPLanes = G::WN / 8;
-#pragma unroll
-        for (int y = 0; y < G::WM; y += kWave / kPLanes) {
-            const int row = y + lane / kPLanes, piece = lane % kPLanes;
-            const uint4 v = *reinterpret_cast<const uint4*>(own + row * (G::WN / 2) + (piece ^ (row & kPMask)) * 4);
-            const int64_t m = m0 + wm * G::WM + row, n = n0 + wn * G::WN + 8 * piece;
-            if (m < rows && n < a.p_ld) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.p) + m * a.p_ld + n) = v;
-        }
+        rows_out<G>(t.acc, own, static_cast<uint16_t*>(a.p), a.p_ld, m0 + wm * G::WM, n0 + wn * G::WN, rows, a.p_ld);
     }
 }
 
@@ -473,6 +482,21 @@ __global__ __launch_bounds__(MW * NW * kWave) void product_kernel(XentArgs a) {
     const int wm = w % MW, wn = w / MW, li = lane % 16, lq = lane / 16;
     const float unit = a.unit ? *a.unit : 1.0f;
     float* split = a.splits > 1 ? a.split + share * a.g.a.rows * a.out_ld : nullptr;
+    if constexpr (T::kBytes == 2)
+        if (!split && a.first && a.last && a.out_ld % 8 == 0) {
+            __syncthreads();  // the tiles have been read
+#pragma unroll
+            for (int i = 0; i < G::MI; ++i) {
+                const bool none = nones[wm * G::WM + i * 16 + li];
+#pragma unroll
+                for (int j = 0; j < G::NI; ++j)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) t.acc[i][j][r] = none ? 0.0f : t.acc[i][j][r] * unit;
+            }
+            rows_out<G>(t.acc, reinterpret_cast<uint32_t*>(lds) + w * (G::WM * G::WN / 2), reinterpret_cast<uint16_t*>(a.out), a.out_ld,
+                        m0 + wm * G::WM, n0 + wn * G::WN, a.g.a.rows, a.g.b.rows);
+            return;
+        }
 #pragma unroll
     for (int i = 0; i < G::MI; ++i) {
         const int64_t m = m0 + wm * G::WM + i * 16 + li;
@@ -576,12 +600,14 @@ GemmArgs product_of(const GemmOperand& a, const GemmOperand& b, int64_t K) {
     return g;
 }
 
-// Tiles of 256 x 256 (1.10 PFLOP/s at 8192 x 4096 x 4096) where they fill most of the chip; else of 128 x 128: four steps in
+// Tiles of 256 x 256 (1.10 PFLOP/s at 8192 x 4096 x 4096) where they fill most of the chip and are more than a few steps long (60 rows
+// against 60000 symbols of width 4096, dW's k of 64: 727 us a training step so, 710 in tiles of 128 x 128; the same at a k of 512,
+// 3-7% more time at 1024); else of 128 x 128: four steps in
 // LDS (0.85 PFLOP/s with one workgroup per compute unit, 8192 x 512 x 4096), or two, where more workgroups than compute units
 // can share them.
 enum class Tile { k256, k128Deep, k128, kFew32, kFew64, kWide };
 Tile tile_for(const GemmArgs& g) {
-    if (cut(g.a.rows, 256) * cut(g.b.rows, 256) >= 192) return Tile::k256;
+    if (cut(g.a.rows, 256) * cut(g.b.rows, 256) >= 192 && g.K > 256) return Tile::k256;
     return cut(g.a.rows, 128) * cut(g.b.rows, 128) <= 256 ? Tile::k128Deep : Tile::k128;
 }
 struct Edges {
