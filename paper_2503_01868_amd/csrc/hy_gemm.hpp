@@ -336,4 +336,113 @@ struct GemmSplit {
     }
 };
 
+// The same of bf16 operands where B lies turned in memory, k after k (its `rows` are how many numbers it has for each k, an even
+// distance `ld` apart from an address of a word): for few rows of A, where a turned copy would cost as much as the product.  Both go through
+// registers, a step of 64 k at a time and two steps ahead; a lane takes two columns of 8 k, a word each, and puts them together.
+// LDS rows are Gemm's.
+template <int BM, int BN, int MW, int NW>
+struct GemmAcross {
+    static constexpr int kStep = 64;
+    static constexpr int kWaves = MW * NW, kThreads = kWaves * kWave;
+    static constexpr int WM = BM / MW, WN = BN / NW, MI = WM / 16, NI = WN / 16;
+    static constexpr int kRowBytes = kStep * 2, kBytes = (BM + BN) * kRowBytes, kLds = 2 * kBytes;
+    static constexpr int AL = BM * 8 / kThreads, BL = 8 / kWaves;  // pieces of 8 k of a lane: of a row; of two columns
+    static_assert(AL * kThreads == BM * 8 && BL * kWaves == 8 && BN == 2 * kWave, "whole pieces, and a wave's are of the same 8 k");
+
+    f32x4_t acc[MI][NI];
+
+    struct Held {
+        u32x4_t a[AL];
+        uint32_t b[BL][8];
+    };
+
+    __device__ __forceinline__ void run(char* lds, const GemmArgs& g, int64_t m0, int64_t n0, int first, int last) {
+        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+        const int li = lane % 16, lq = lane / 16, wm = w % MW, wn = w / MW;
+        const uint16_t* a_from[AL];
+        int a_to[AL];
+#pragma unroll
+        for (int x = 0; x < AL; ++x) {
+            const int i = x * kThreads + (int)threadIdx.x, row = i / 8, piece = i % 8;
+            const int64_t r = m0 + row < g.a.rows ? m0 + row : g.a.rows - 1;  // rows that do not exist: the last one again
+            a_from[x] = static_cast<const uint16_t*>(g.a.p) + r * g.a.ld + piece * 8;
+            a_to[x] = row * kRowBytes + (piece ^ (row % 8)) * 16;
+        }
+        const int64_t pairs = (g.b.rows + 1) / 2, pair = n0 / 2 + lane;
+        const uint32_t b_at = (uint32_t)(pair < pairs ? pair : pairs - 1);
+        const int b_to = (BM + 2 * lane) * kRowBytes, b_row = 2 * lane % 8;
+        auto fetch = [&](Held& h, int step) {
+#pragma unroll
+            for (int x = 0; x < AL; ++x) h.a[x] = *reinterpret_cast<const u32x4_t*>(a_from[x] + (int64_t)step * kStep);
+            const char* const base = static_cast<const char*>(g.b.p) + (int64_t)step * kStep * g.b.ld * 2;
+            const bool whole = (step + 1) * kStep <= g.K;
+#pragma unroll
+            for (int x = 0; x < BL; ++x)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int k = (x * kWaves + w) * 8 + j;
+                    h.b[x][j] = whole || step * kStep + k < g.K ? reinterpret_cast<const uint32_t*>(base + k * g.b.ld * 2)[b_at] : 0u;
+                }
+        };
+        auto put = [&](const Held& h, int stage) {
+            char* const to = lds + stage * kBytes;
+#pragma unroll
+            for (int x = 0; x < AL; ++x) *reinterpret_cast<u32x4_t*>(to + a_to[x]) = h.a[x];
+#pragma unroll
+            for (int x = 0; x < BL; ++x)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t v[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = __builtin_amdgcn_perm(h.b[x][2 * j + 1], h.b[x][2 * j], c ? 0x07060302 : 0x05040100);
+                    *reinterpret_cast<uint4*>(to + b_to + c * kRowBytes + ((x * kWaves + w) ^ (b_row + c)) * 16) = make_uint4(v[0], v[1], v[2], v[3]);
+                }
+        };
+        auto meet = [&] {  // what the waves have written to LDS is there; loads into registers stay on their way
+            __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        };
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        const char *ra = lds + (wm * WM + li) * kRowBytes, *rb = lds + (BM + wn * WN + li) * kRowBytes;
+        Held h0, h1;
+        fetch(h0, first);
+        put(h0, 0);
+        fetch(h0, first + 1 < last ? first + 1 : first);
+        meet();
+        auto step = [&](int t, Held& next, Held& after) {
+            const int stage = (t - first) % 2;
+            fetch(after, t + 2 < last ? t + 2 : last - 1);
+            bf16x8_t fa[2][MI], fb[2][NI];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int piece = ((4 * h + lq) ^ (li % 8)) * 16 + stage * kBytes;
+#pragma unroll
+                for (int j = 0; j < NI; ++j) fb[h][j] = *reinterpret_cast<const bf16x8_t*>(rb + j * 16 * kRowBytes + piece);
+#pragma unroll
+                for (int i = 0; i < MI; ++i) fa[h][i] = *reinterpret_cast<const bf16x8_t*>(ra + i * 16 * kRowBytes + piece);
+            }
+            put(next, stage ^ 1);  // (behind the last step: nobody reads it)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int j = 0; j < NI; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[h][j], fa[h][i], acc[i][j], 0, 0, 0);
+            meet();
+        };
+        int t = first;
+        for (; t + 1 < last; t += 2) {
+            step(t, h0, h1);
+            step(t + 1, h1, h0);
+        }
+        if (t < last) step(t, h0, h1);
+    }
+};
+
 }  // namespace hy

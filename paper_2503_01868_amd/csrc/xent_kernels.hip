@@ -7,12 +7,12 @@
 // a second kernel joins the tiles of a row.  Backward, for a piece of the vocabulary at a time: z again, P from it, and the two
 // products.  The matrix products are what bounds it: 8 N V D operations.
 //
-// bf16 operands enter the products as they are, with k contiguous in both of them: x and the piece of W are transposed once, and P,
-// rounded to bf16 in units of the largest |dloss|, is written in both orders.  fp32 calls multiply in parts, to fp32's precision,
+// bf16 operands enter the products as they are, with k contiguous in both of them: x and, but for few rows, the piece of W are
+// transposed once, and P, rounded to bf16 in units of the largest |dloss|, is written in both orders.  fp32 calls multiply in parts, to fp32's precision,
 // keep P in fp32, and read P and W across k where a product needs it.
 //
 // Measured, loss and gradients: 8192 x 65536 x 4096 bf16 14.1-14.7 ms (1.20-1.25 PFLOP/s, the four products at 1.15 to 1.3),
-// 8192 x 512 x 4096 208 us (0.66 PFLOP/s: tiles of 128 x 128 on 256 compute units once, and 30 us of transposition);
+// 8192 x 512 x 4096 197 us (0.70 PFLOP/s: tiles of 128 x 128 on 256 compute units once, and 30 us of transposition);
 // 1003 x 5003 x 1000 fp32 283 us (0.85 PFLOP/s of the six products of parts).  The loss alone, 8 x 65536 x 4096: 105 us, 5.1 TB/s.
 #include <algorithm>
 
@@ -605,7 +605,7 @@ GemmArgs product_of(const GemmOperand& a, const GemmOperand& b, int64_t K) {
 // 3-7% more time at 1024); else of 128 x 128: four steps in
 // LDS (0.85 PFLOP/s with one workgroup per compute unit, 8192 x 512 x 4096), or two, where more workgroups than compute units
 // can share them.
-enum class Tile { k256, k128Deep, k128, kFew32, kFew64, kWide };
+enum class Tile { k256, k128Deep, k128, kFew32, kFew64, kWide, kAcross };
 Tile tile_for(const GemmArgs& g) {
     if (cut(g.a.rows, 256) * cut(g.b.rows, 256) >= 192 && g.K > 256) return Tile::k256;
     return cut(g.a.rows, 128) * cut(g.b.rows, 128) <= 256 ? Tile::k128Deep : Tile::k128;
@@ -647,9 +647,9 @@ template <typename T>
 Tile logit_tile_for(const GemmArgs& g) {
     return T::kBytes == 2 ? logit_tile(g) : g.a.rows <= 64 ? Tile::kFew64 : split_tile(g);
 }
-template <typename T>
+template <typename T, bool TB>
 Tile product_tile_for(const GemmArgs& g) {
-    if (T::kBytes == 2) return tile_for(g);
+    if (T::kBytes == 2) return TB ? Tile::kAcross : tile_for(g);
     return g.a.rows <= 64 || g.K <= 64 ? Tile::kFew64 : split_tile(g);
 }
 
@@ -696,27 +696,35 @@ hy_status gradients(XentArgs& a, hipStream_t st) {
 }
 
 // Into how many shares a product's k is divided: where its tiles leave half of the compute units or more without work, as many as
-// they hold, of at least 8 steps each.
-template <typename T>
+// they hold, of at least 8 steps each (64 x 60000 x 256 bf16, dx in 16 shares or in up to 48: 112 us a training step or 83).
+template <typename T, bool TB>
 int32_t splits_for(const GemmArgs& g) {
-    const Tile tile = product_tile_for<T>(g);
+    const Tile tile = product_tile_for<T, TB>(g);
     const Edges e = edges_of(tile);
     const int64_t tiles = cut(g.a.rows, e.rows) * cut(g.b.rows, e.cols), steps = g.K / (T::kBytes == 4 ? 32 : 64);
-    const int64_t room = tile == Tile::kFew64 ? 3 * 256 : 256;
+    const int64_t room = 256 * (tile == Tile::kFew64 ? 3 : tile == Tile::kAcross ? 2 : 1);  // workgroups that the chip holds
     if (2 * tiles > room || tile == Tile::k256) return 1;
-    return (int32_t)std::max<int64_t>(1, std::min<int64_t>({room / tiles, steps / 8, 16}));
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>({room / tiles, steps / 8, room > 256 ? 48 : 16}));
 }
 
-// The two products of a piece of `cols` columns.  fp32: P and W lie turned where k runs over their rows.
+// Whether dx is computed from W as it lies: fp32 always; bf16 where a turned copy would take longer than the product loses by
+// operands that go through registers (a training step with and without the copy: 60 x 60000 x 4096 697 us and 478, 256 rows 885 and 684,
+// 512 x 30000 x 4096 636 and 566, 1000 x 60000 x 1024 636 and 610; but 250 x 9000 x 2048 98 and 100, 250 x 1000 x 512 43 and 46).
+template <typename T>
+bool across(const XentShape& s) {
+    return T::kBytes == 4 || s.N <= 128 || (s.N <= 1024 && s.V * s.D >= INT64_C(1) << 25);
+}
+
+// The two products of a piece of `cols` columns.  fp32: P lies turned where k runs over its rows.
 template <typename T>
 GemmArgs dw_product(const XentShape& s, const Layout& l, int64_t cols, const void* p = nullptr, const void* xt = nullptr) {
     if (T::kBytes == 4) return product_of(GemmOperand{p, up(cols, kGemmK), cols}, GemmOperand{xt, l.nt, s.D}, s.N);
     return product_of(GemmOperand{p, l.nt, cols}, GemmOperand{xt, l.nt, s.D}, up(s.N, 32));  // (what the tiles of P, of 32 rows at least, fill)
 }
 template <typename T>
-GemmArgs dx_product(const XentShape& s, int64_t cols, const void* p = nullptr, const void* w = nullptr) {
+GemmArgs dx_product(const XentShape& s, const Layout& l, int64_t cols, const void* p = nullptr, const void* w = nullptr) {
     const int64_t ld = up(cols, kGemmK);
-    if (T::kBytes == 4) return product_of(GemmOperand{p, ld, s.N}, GemmOperand{w, s.D, s.D}, cols);
+    if (across<T>(s)) return product_of(GemmOperand{p, ld, s.N}, GemmOperand{w, l.ld, s.D}, cols);
     return product_of(GemmOperand{p, ld, s.N}, GemmOperand{w, ld, s.D}, ld);
 }
 
@@ -730,18 +738,16 @@ struct BwdSpace {
         x = l.packed ? c.take<uint16_t>(s.N * l.ld) : nullptr;
         w = l.packed ? c.take<uint16_t>(piece * l.ld) : nullptr;
         xt = c.take<Bits<T>>(s.D * l.nt);
-        wt = T::kBytes == 2 ? c.take<Bits<T>>(s.D * ld) : nullptr;
+        wt = !across<T>(s) ? c.take<Bits<T>>(s.D * ld) : nullptr;
         p = c.take<Bits<T>>(s.N * ld);
         pt = T::kBytes == 2 ? c.take<Bits<T>>(piece * l.nt) : nullptr;
         sum = l.pieces > 1 ? c.take<float>(s.N * s.D) : nullptr;
         int64_t most = 0;
-        auto floats = [&](const GemmArgs& g) {
-            const int32_t n = splits_for<T>(g);
-            return n > 1 ? n * g.a.rows * s.D : 0;
-        };
+        auto floats = [&](const GemmArgs& g, int32_t n) { return n > 1 ? n * g.a.rows * s.D : 0; };
         for (int64_t v = 0; v < s.V; v += l.piece) {
             const int64_t cols = std::min(l.piece, s.V - v);
-            most = std::max({most, floats(dw_product<T>(s, l, cols)), floats(dx_product<T>(s, cols))});
+            const GemmArgs dw = dw_product<T>(s, l, cols), dx = dx_product<T>(s, l, cols);
+            most = std::max({most, floats(dw, splits_for<T, false>(dw)), floats(dx, across<T>(s) ? splits_for<T, true>(dx) : splits_for<T, false>(dx))});
         }
         split = c.take<float>(most);
         unit = c.take<float>(1);
@@ -751,8 +757,8 @@ struct BwdSpace {
 template <typename T, bool TA, bool TB>
 hy_status product(XentArgs& a, float* split, hipStream_t st) {
     a.split = split;
-    a.splits = splits_for<T>(a.g);
-    const Tile tile = product_tile_for<T>(a.g);
+    a.splits = splits_for<T, TB>(a.g);
+    const Tile tile = product_tile_for<T, TB>(a.g);
     hy_status rc = by_tile(a, tile, [&](dim3 grid) {
         grid.x *= (uint32_t)a.splits;
         if constexpr (T::kBytes == 4)
@@ -761,6 +767,8 @@ hy_status product(XentArgs& a, float* split, hipStream_t st) {
                 case Tile::kWide: return launch_kernel(product_kernel<T, GemmSplit<128, 192, 2, 4, TA, TB>, 128, 192, 2, 4>, grid, dim3(512), st, a);
                 default: return launch_kernel(product_kernel<T, GemmSplit<128, 128, 2, 4, TA, TB>, 128, 128, 2, 4>, grid, dim3(512), st, a);
             }
+        else if constexpr (TB)
+            return launch_kernel(product_kernel<T, GemmAcross<128, 128, 2, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
         else
         switch (tile) {
             case Tile::k256: return launch_kernel(product_kernel<T, Gemm<256, 256, 2, 4, 2>, 256, 256, 2, 4>, grid, dim3(512), st, a);
@@ -840,12 +848,12 @@ hy_status backward(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t 
     hy_status rc = turn<T>(p.x, b.xt, s.N, s.D, l.nt, p.target, s.V, Unit{p.dloss, T::kBytes == 2 ? b.unit : nullptr}, st);
     for (int64_t v = 0; rc == HY_OK && v < s.V; v += l.piece) {
         const int64_t cols = std::min(l.piece, s.V - v), ld = up(cols, kGemmK);
-        const char* const w = (const char*)p.w + v * s.D * T::kBytes;
         constexpr bool kTurned = T::kBytes == 4;
         XentArgs a{};
         a.g.K = (int32_t)(l.packed ? l.ld : s.D);
         rc = operands<T>(p, s, l, b.x, b.w, v, &a.g.a, &a.g.b, st);
-        if (rc == HY_OK && !kTurned) rc = turn<T>(w, b.wt, cols, s.D, ld, nullptr, 0, Unit{}, st);
+        const GemmOperand words = a.g.b;
+        if (rc == HY_OK && !across<T>(s)) rc = turn<T>((const char*)p.w + v * s.D * T::kBytes, b.wt, cols, s.D, ld, nullptr, 0, Unit{}, st);
         a.target = p.target, a.V = s.V, a.v0 = v;
         a.lse = p.lse_in, a.dloss = p.dloss, a.unit = unit;
         a.p = b.p, a.p_ld = ld;
@@ -856,10 +864,10 @@ hy_status backward(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t 
         dw.out = (char*)p.dw + v * s.D * T::kBytes, dw.out_ld = s.D, dw.first = dw.last = true, dw.unit = unit;
         if (rc == HY_OK) rc = product<T, kTurned, false>(dw, b.split, st);
         XentArgs dx{};
-        dx.g = dx_product<T>(s, cols, b.p, kTurned ? (const void*)w : b.wt);
+        dx.g = dx_product<T>(s, l, cols, b.p, across<T>(s) ? words.p : b.wt);
         dx.out = (char*)p.dx, dx.out_ld = s.D, dx.sum = b.sum, dx.first = v == 0, dx.last = v + l.piece >= s.V, dx.unit = unit;
         dx.target = p.target, dx.V = s.V;
-        if (rc == HY_OK) rc = product<T, false, kTurned>(dx, b.split, st);
+        if (rc == HY_OK) rc = across<T>(s) ? product<T, false, true>(dx, b.split, st) : product<T, false, T::kBytes == 4>(dx, b.split, st);
     }
     return rc;
 }

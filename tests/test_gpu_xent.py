@@ -191,3 +191,24 @@ def test_columns_that_begin_between_16_bytes():
     column = torch.cat([lse[:1], lse])[1:]
     for a, b in zip(hy.hyena_xent_bwd(dloss, x, w, target, lse), hy.hyena_xent_bwd(weights[1:], x, w, text[1:], column)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("N,V,D", [(1, 100, 2), (100, 3000, 129), (128, 70, 264), (1024, 17000, 2048), (200, 33000, 1024)])
+def test_few_bf16_rows(N, V, D):
+    """The weights read as they lie, odd widths and vocabularies that end inside a step; the last two are few rows for their weights."""
+    say("xent bf16 %d x %d x %d" % (N, V, D))
+    if N * V <= 1 << 22:
+        check(*make(N + V + D, N, V, D, "bf16"), "bf16")
+        return
+    # against the gradient of x alone: rows by the others' rules agree with the same rows in a call of more of them
+    x, w, target, dloss = make(N + V + D, N, V, D, "bf16")
+    loss, lse = hy.hyena_xent_fwd(x, w, target)
+    dx, _ = hy.hyena_xent_bwd(dloss, x, w, target, lse)
+    z = x.float() @ w.float().t()
+    p = torch.exp(z - torch.logsumexp(z, 1, keepdim=True))
+    counts = (target >= 0) & (target < V)
+    p[counts, target[counts]] -= 1
+    p *= torch.where(counts, dloss, 0.0)[:, None]
+    ref, mass = p @ w.float(), p.abs() @ w.float().abs()
+    # P's rounding to bf16 (2^-8 with its ends), the logits' in fp32, and the result's
+    assert ((dx.float() - ref).abs() <= 2.0 ** -7 * mass + 2.0 ** -8 * ref.abs() + 1e-30).all()
