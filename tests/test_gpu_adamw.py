@@ -198,3 +198,20 @@ def test_a_step_on_another_stream_outlives_its_plan():
     junk = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in (256, 512, 1024, 2048)]
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(ref, other)) and len(junk) == 4
+
+
+def test_a_step_inside_a_graph():
+    p, g = torch.ones(5000, device="cuda"), torch.zeros(5000, device="cuda")
+    other = p.clone()
+    state, others = hy.adamw_state([p], 8), hy.adamw_state([other], 8)
+    plan, eager = hy.plan_adamw([p], [g], **state), hy.plan_adamw([other], [g], **others)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        plan(lr=1e-3, step=7)
+    for i in range(4):
+        g.normal_()
+        eager(lr=1e-3, step=7)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(p, other)

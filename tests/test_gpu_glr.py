@@ -245,3 +245,26 @@ def test_refusals():
         hy.hyena_glr_fwd(q, k, v, g, 4, out=q)
     with pytest.raises(ValueError):
         hy.hyena_glr_step(q[:, 0], k[:, 0], v[:, 0], g[:, 0], state, 4)
+
+
+def test_a_token_inside_a_graph():
+    """A decoder's step captured once: every replay takes the state one token further, as eager calls do."""
+    q, k, v, g, _, _, _ = make(21, 4, 1, 256, 16, "bf16")
+    q, k, v, g = (t[:, 0].contiguous() for t in (q, k, v, g))
+    state = torch.zeros(4, 256, device="cuda")
+    other = state.clone()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        hy.hyena_glr_step(q, k, v, g, state, 16)
+    side.synchronize()
+    state.zero_()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = hy.hyena_glr_step(q, k, v, g, state, 16)
+    for i in range(4):
+        k.copy_(torch.randn_like(k))
+        eager = hy.hyena_glr_step(q, k, v, g, other, 16)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, eager) and torch.equal(state, other)
