@@ -8,8 +8,8 @@
 // products.  The matrix products are what bounds it: 8 N V D operations.
 //
 // bf16 operands enter the products as they are, with k contiguous in both of them: x and, but for few rows, the piece of W are
-// transposed once, and P, rounded to bf16 in units of the largest |dloss|, is written in both orders.  fp32 calls multiply in parts, to fp32's precision,
-// keep P in fp32, and read P and W across k where a product needs it.
+// transposed once, and P, rounded to bf16 in units of the largest |dloss|, is written in both orders.  fp32 calls multiply in parts,
+// to fp32's precision, keep P in fp32, and read P and W across k where a product needs it.
 //
 // Measured, loss and gradients: 8192 x 65536 x 4096 bf16 14.1-14.7 ms (1.20-1.25 PFLOP/s, the four products at 1.15 to 1.3),
 // 8192 x 512 x 4096 197 us (0.70 PFLOP/s: tiles of 128 x 128 on 256 compute units once, and 30 us of transposition);
@@ -664,13 +664,13 @@ hy_status losses(XentArgs& a, hipStream_t st) {
                 default: return launch_kernel(loss_kernel<GemmSplit<128, 128, 2, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
             }
         else
-        switch (tile) {
-            case Tile::k256: return launch_kernel(loss_kernel<Gemm<256, 256, 2, 4, 2>, 256, 256, 2, 4>, grid, dim3(512), st, a);
-            case Tile::k128: return launch_kernel(loss_kernel<Gemm<128, 128, 2, 4, 2>, 128, 128, 2, 4>, grid, dim3(512), st, a);
-            case Tile::k128Deep: return launch_kernel(loss_kernel<Gemm<128, 128, 2, 4, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
-            case Tile::kFew32: return launch_kernel(loss_kernel<Gemm<32, 64, 1, 4, 6>, 32, 64, 1, 4>, grid, dim3(256), st, a);
-            default: return launch_kernel(loss_kernel<Gemm<64, 64, 1, 4, 4>, 64, 64, 1, 4>, grid, dim3(256), st, a);
-        }
+            switch (tile) {
+                case Tile::k256: return launch_kernel(loss_kernel<Gemm<256, 256, 2, 4, 2>, 256, 256, 2, 4>, grid, dim3(512), st, a);
+                case Tile::k128: return launch_kernel(loss_kernel<Gemm<128, 128, 2, 4, 2>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+                case Tile::k128Deep: return launch_kernel(loss_kernel<Gemm<128, 128, 2, 4, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+                case Tile::kFew32: return launch_kernel(loss_kernel<Gemm<32, 64, 1, 4, 6>, 32, 64, 1, 4>, grid, dim3(256), st, a);
+                default: return launch_kernel(loss_kernel<Gemm<64, 64, 1, 4, 4>, 64, 64, 1, 4>, grid, dim3(256), st, a);
+            }
     });
 }
 
@@ -685,13 +685,13 @@ hy_status gradients(XentArgs& a, hipStream_t st) {
                 default: return launch_kernel(grad_kernel<T, GemmSplit<128, 128, 2, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
             }
         else
-        switch (tile) {
-            case Tile::kFew32: return launch_kernel(grad_kernel<T, Gemm<32, 64, 1, 4, 6>, 32, 64, 1, 4>, grid, dim3(256), st, a);
-            case Tile::kFew64: return launch_kernel(grad_kernel<T, Gemm<64, 64, 1, 4, 4>, 64, 64, 1, 4>, grid, dim3(256), st, a);
-            case Tile::k256: return launch_kernel(grad_kernel<T, Gemm<256, 256, 2, 4, 2>, 256, 256, 2, 4>, grid, dim3(512), st, a);
-            case Tile::k128: return launch_kernel(grad_kernel<T, Gemm<128, 128, 2, 4, 2>, 128, 128, 2, 4>, grid, dim3(512), st, a);
-            default: return launch_kernel(grad_kernel<T, Gemm<128, 128, 2, 4, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
-        }
+            switch (tile) {
+                case Tile::kFew32: return launch_kernel(grad_kernel<T, Gemm<32, 64, 1, 4, 6>, 32, 64, 1, 4>, grid, dim3(256), st, a);
+                case Tile::kFew64: return launch_kernel(grad_kernel<T, Gemm<64, 64, 1, 4, 4>, 64, 64, 1, 4>, grid, dim3(256), st, a);
+                case Tile::k256: return launch_kernel(grad_kernel<T, Gemm<256, 256, 2, 4, 2>, 256, 256, 2, 4>, grid, dim3(512), st, a);
+                case Tile::k128: return launch_kernel(grad_kernel<T, Gemm<128, 128, 2, 4, 2>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+                default: return launch_kernel(grad_kernel<T, Gemm<128, 128, 2, 4, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+            }
     });
 }
 
@@ -747,7 +747,8 @@ struct BwdSpace {
         for (int64_t v = 0; v < s.V; v += l.piece) {
             const int64_t cols = std::min(l.piece, s.V - v);
             const GemmArgs dw = dw_product<T>(s, l, cols), dx = dx_product<T>(s, l, cols);
-            most = std::max({most, floats(dw, splits_for<T, false>(dw)), floats(dx, across<T>(s) ? splits_for<T, true>(dx) : splits_for<T, false>(dx))});
+            const int32_t dx_splits = across<T>(s) ? splits_for<T, true>(dx) : splits_for<T, false>(dx);
+            most = std::max({most, floats(dw, splits_for<T, false>(dw)), floats(dx, dx_splits)});
         }
         split = c.take<float>(most);
         unit = c.take<float>(1);
@@ -770,11 +771,11 @@ hy_status product(XentArgs& a, float* split, hipStream_t st) {
         else if constexpr (TB)
             return launch_kernel(product_kernel<T, GemmAcross<128, 128, 2, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
         else
-        switch (tile) {
-            case Tile::k256: return launch_kernel(product_kernel<T, Gemm<256, 256, 2, 4, 2>, 256, 256, 2, 4>, grid, dim3(512), st, a);
-            case Tile::k128: return launch_kernel(product_kernel<T, Gemm<128, 128, 2, 4, 2>, 128, 128, 2, 4>, grid, dim3(512), st, a);
-            default: return launch_kernel(product_kernel<T, Gemm<128, 128, 2, 4, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
-        }
+            switch (tile) {
+                case Tile::k256: return launch_kernel(product_kernel<T, Gemm<256, 256, 2, 4, 2>, 256, 256, 2, 4>, grid, dim3(512), st, a);
+                case Tile::k128: return launch_kernel(product_kernel<T, Gemm<128, 128, 2, 4, 2>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+                default: return launch_kernel(product_kernel<T, Gemm<128, 128, 2, 4, 4>, 128, 128, 2, 4>, grid, dim3(512), st, a);
+            }
     });
     if (rc != HY_OK || a.splits == 1) return rc;
     const int64_t lanes = a.g.a.rows * ((a.out_ld + 3) / 4);
