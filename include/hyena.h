@@ -387,8 +387,10 @@ int64_t hyena_bwd_shard_workspace_bytes(int64_t B, int64_t L, int64_t D, int32_t
  *     s[b,t,c] = a[b,t,c] * s[b,t-1,c] + k[b,t,c] * v[b,t,c],   a[b,t,c] = exp(g[b,t,c / group]),
  *     y[b,t,c] = q[b,t,c] * s[b,t,c],
  * with s[b,-1,c] = state_in[b,c] (NULL: zero).  g is the logarithm of the decay: decays close to 1 keep their precision in
- * bfloat16 that way, and g = -infinity forgets everything before its step (the first step of a document in a packed
- * sequence; every gradient through it is zero).  g > 0 grows and overflows as the definition does.
+ * bfloat16 that way.  A decay of zero (g = -infinity, or so low that exp(g) is zero: below about -87, as the lowest number of
+ * the type) forgets everything before its step, infinities and NaN included (the first step of a document in a packed
+ * sequence; every gradient through it is zero); a state of zero stays zero under any decay.  g > 0 grows, and overflows where
+ * the states themselves do.
  * q, k, v, y: [B,L,D], g: [B,L,D/group], of `dtype`; state_in, state_out: fp32 [B,D], the state after the last step
  * (NULL: not wanted; an empty sequence hands state_in on).  The state, the decays and every sum are fp32, y is rounded
  * once.
@@ -532,7 +534,7 @@ hy_status hyena_stream_gate(const void *q, const void *k, const void *v, void *y
  *   "li_wait"  how Hyena-LI's tiles come by the states of the tiles before them, where it can do them in one pass:
  *              0 = wait for them (for a bounded time), 1 = compute them again, 2 = two passes everywhere
  *   "glr_wait" how the tiles of the gated linear recurrence come by the states of the tiles before them: 0 = wait for them
- *              (for a bounded time), 1 = compute them again (the same bits)
+ *              (for a bounded time), 1 = compute them again, 2 = look once, then compute them again (all three the same bits)
  * Unknown names return HY_ERR_UNSUPPORTED.  Results depend on these only through rounding, within the
  * documented precision of each entry point.
  */

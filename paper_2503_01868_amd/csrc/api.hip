@@ -846,7 +846,7 @@ hy_status hyena_set_option(const char* name, int32_t value) {
         if (value > 2) return HY_ERR_SHAPE;
         t.li_wait = value;
     } else if (strcmp(name, "glr_wait") == 0) {
-        if (value > 1) return HY_ERR_SHAPE;
+        if (value > 2) return HY_ERR_SHAPE;
         t.glr_wait = value;
     } else {
         return HY_ERR_UNSUPPORTED;

@@ -4,12 +4,18 @@
 // A the product of its a and H its result from zero.  The gradient runs the other way with the same A: with m[t] = dLoss/ds[t]
 // and c[t] = a[t] m[t] (what a step hands to the one before it), m[t] = q[t] dy[t] + c[t+1], so a stretch takes c -> A c + C.
 //
+// A is held as G = log A, the sum of the stretch's g: where g > 0, A may pass fp32's range over a stretch while the states stay
+// within it, because they are small or zero.  A s is taken as R (R s), R = exp(G / 2): what it gives is in range whenever the
+// product is.  A product with a decay or a state of zero is zero, whatever the other factor is (times0): a decay of zero forgets
+// infinities and NaN too, and an infinite decay makes nothing of nothing.  G is -infinity exactly if a stretch has a decay of
+// zero; other decays, however small their product, hand on what is not finite.
+//
 // One pass: a workgroup loads a tile of kGlrRows steps by 64 to 256 channels into registers, each of kWaves waves kRowsPerWave
-// rows, sums it up, publishes (A, H), takes the state at its edge from the tiles before it (behind it, backward) and writes the
+// rows, sums it up, publishes (G, H), takes the state at its edge from the tiles before it (behind it, backward) and writes the
 // tile's results from the registers.  Every tensor is read and written once: that traffic is what bounds it.
 //
 // The edge.  Tiles are grouped in blocks of kBlockTiles.  The state at the first tile of a block is that of the block before,
-// taken through that block's joint (A, H); the state at a tile is its block's, taken through the joint sums of the tiles between.
+// taken through that block's joint (G, H); the state at a tile is its block's, taken through the joint sums of the tiles between.
 // The last tile of a block publishes its joint sums and, once it has its own state, the next block's.  So a state is always the
 // result of the same operations, wherever they are done: results do not depend on timing.  A tile reads the sums before it in
 // its block, and the states and joint sums of the kBlocksBack blocks before, nearest first: a state travels 32 tiles per exchange
@@ -47,7 +53,7 @@ struct GlrArgs {
     float* edge_out;           // [B, D]: what comes out at the other end, or null
     const float* marks;        // [B, tiles, D] states before the tiles (backward)
     float* marks_out;          // forward, or null
-    // records, in the order of the walk: (A, H) (backward: (A, C)) of the tiles [tiles, B, D] and of the blocks [blocks, B, D],
+    // records, in the order of the walk: (G, H) (backward: (G, C)) of the tiles [tiles, B, D] and of the blocks [blocks, B, D],
     // and the states at the blocks' first tiles [blocks, B, D]
     uint64_t *sums, *joint;
     uint32_t* states;
@@ -56,16 +62,56 @@ struct GlrArgs {
     int32_t polls;
 };
 
+// x * y, and 0 where either of them is 0.
+extern "C" __device__ float glr_fmul_legacy(float, float) __asm("llvm.amdgcn.fmul.legacy");
+__device__ __forceinline__ float times0(float x, float y) { return glr_fmul_legacy(x, y); }
+
+// The decay of two stretches, as logarithms.
+__device__ __forceinline__ float both(float G, float H) { return G == -INFINITY || H == -INFINITY ? -INFINITY : G + H; }
+
+// R of a stretch.  No product of decays that is not zero becomes zero (or forgets NaN): below 2^-245 it may as well be 2^-245.
+__device__ __forceinline__ float root_of(float G) {
+    const float r = __builtin_amdgcn_exp2f((G < -170.0f ? -170.0f : G) * 0.72134752f);
+    return G == -INFINITY ? 0.0f : r;
+}
+
+// A s + H
+__device__ __forceinline__ float through(float R, float s, float H) { return times0(R, times0(R, s)) + H; }
+
+// The sum of the g of a lane's rows, and whether one of their decays is zero.
+template <int N>
+struct Logs {
+    float sum[N];
+    bool dead[N];
+    __device__ __forceinline__ Logs() {
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum[i] = 0.0f, dead[i] = false;
+    }
+    __device__ __forceinline__ float get(int i) const { return dead[i] ? -INFINITY : sum[i]; }
+};
+
 // VEC channels per lane; SHARED: both channels of a lane (or its only one) take the gate of their group.
 template <typename T, int VEC, bool SHARED>
 struct Io {
     using P = Pack<T, VEC>;
     using G = Pack<T, SHARED ? 1 : VEC>;
+    static constexpr int kGates = SHARED ? 1 : VEC;
     static __device__ __forceinline__ void gates(const typename G::Raw& r, float (&a)[VEC]) {
-        float f[SHARED ? 1 : VEC];
+        float f[kGates];
         G::unpack(r, f);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) a[i] = i == 0 || !SHARED ? decay(f[SHARED ? 0 : i]) : a[0];
+    }
+    // there: the row exists
+    static __device__ __forceinline__ void gates(const typename G::Raw& r, float (&a)[VEC], Logs<kGates>& logs, bool there = true) {
+        float f[kGates];
+        G::unpack(r, f);
+        gates(r, a);
+#pragma unroll
+        for (int i = 0; i < kGates; ++i) {
+            logs.sum[i] += there ? f[i] : 0.0f;
+            logs.dead[i] = logs.dead[i] || (there && a[i] == 0.0f);
+        }
     }
     // exp(g).  fp32 calls take the full function; for bf16 calls the power of two of the rounded product is enough (6e-8 times
     // 1 + |g| of a) and a tenth of the instructions: with the full function the vector ALUs were what bounded the kernels.
@@ -162,23 +208,37 @@ __device__ __forceinline__ void load_rows(typename PK::Raw (&r)[kRowsPerWave], c
 
 template <int VEC>
 struct Shared {
-    float A[kWaves][kWave * VEC], H[kWaves][kWave * VEC];  // of the waves
+    float G[kWaves][kWave * VEC], R[kWaves][kWave * VEC], H[kWaves][kWave * VEC];  // of the waves
     float S[kWave * VEC];                                  // the state at the tile's edge
     int32_t lost;                                          // no state came
 };
 
-// What waves [0, w) (REV: (w, last]) of the workgroup make of the state at its edge; all of them with w = kWaves (REV: -1).
+// The state at its edge -> the one that wave w begins with: through waves [0, w) (REV: (w, last]) of the workgroup.
 template <int VEC, bool REV>
-__device__ __forceinline__ void join(const Shared<VEC>& s, int w, int lane, float (&A)[VEC], float (&H)[VEC]) {
+__device__ __forceinline__ void join(const Shared<VEC>& s, int w, int lane, float (&S)[VEC]) {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) A[i] = 1.0f, H[i] = 0.0f;
-    for (int x = REV ? kWaves - 1 : 0; REV ? x > w : x < w; x += REV ? -1 : 1)
+    for (int y = 0; y < kWaves - 1; ++y) {
+        const int x = REV ? kWaves - 1 - y : y;
+        if (REV ? x <= w : x >= w) break;
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const float xa = s.A[x][lane * VEC + i];
-            H[i] = fmaf(xa, H[i], s.H[x][lane * VEC + i]);
-            A[i] *= xa;
+        for (int i = 0; i < VEC; ++i) S[i] = through(s.R[x][lane * VEC + i], S[i], s.H[x][lane * VEC + i]);
+    }
+}
+
+// G and H of the tile, for N channels from `slot` on; `together`: the waves whose sums are on their way from LDS at a time.
+template <int VEC, bool REV, int together, int N>
+__device__ __forceinline__ void join_all(const Shared<VEC>& s, int slot, float (&G)[N], float (&H)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) G[i] = 0.0f, H[i] = 0.0f;
+#pragma unroll together
+    for (int x = 0; x < kWaves; ++x) {
+        const int w = REV ? kWaves - 1 - x : x;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            H[i] = through(s.R[w][slot + i], H[i], s.H[w][slot + i]);
+            G[i] = both(G[i], s.G[w][slot + i]);
         }
+    }
 }
 
 // f(r) for the wave's n rows, in their order or backwards; all of them without a test per row.
@@ -201,55 +261,62 @@ __device__ __forceinline__ uint32_t word_of(float x) {
     return b == kUnset ? 0x7fc00000u : b;
 }
 
-// x and y of the steps (k and v forward, q and dy backward) -> A and H (C) of the wave's rows, into LDS.
+// x and y of the steps (k and v forward, q and dy backward) -> H (C) of the wave's rows, into LDS.
 template <typename T, int VEC, bool REV, typename Gates>
 __device__ __forceinline__ void sum_rows(Shared<VEC>& s, const typename Pack<T, VEC>::Raw (&x)[kRowsPerWave],
                                          const typename Pack<T, VEC>::Raw (&y)[kRowsPerWave],
                                          const Place& p, int n, Gates gates) {
     using P = Pack<T, VEC>;
-    float A[VEC], H[VEC];
+    float H[VEC];
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) A[i] = 1.0f, H[i] = 0.0f;
+    for (int i = 0; i < VEC; ++i) H[i] = 0.0f;
     for_rows<REV>(n, [&](int r) {
         float fx[VEC], fy[VEC], ga[VEC];
         P::unpack(x[r], fx);
         P::unpack(y[r], fy);
         gates(r, ga);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            H[i] = REV ? ga[i] * fmaf(fx[i], fy[i], H[i]) : fmaf(ga[i], H[i], fx[i] * fy[i]);
-            A[i] *= ga[i];
-        }
+        for (int i = 0; i < VEC; ++i)
+            H[i] = REV ? times0(ga[i], fmaf(fx[i], fy[i], H[i])) : fmaf(fx[i], fy[i], times0(ga[i], H[i]));
     });
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) s.A[p.w][p.lane * VEC + i] = A[i], s.H[p.w][p.lane * VEC + i] = H[i];
+    for (int i = 0; i < VEC; ++i) s.H[p.w][p.lane * VEC + i] = H[i];
+}
+// And their G and R.
+template <int VEC, int N>
+__device__ __forceinline__ void put_logs(Shared<VEC>& s, const Place& p, const Logs<N>& logs) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        const float G = logs.get(i % N);
+        s.G[p.w][p.lane * VEC + i] = G, s.R[p.w][p.lane * VEC + i] = root_of(G);
+    }
 }
 
-// The wave's sums of any tile, row by row from memory: sum_rows' operations in few registers.
+// The wave's sums of any tile, row by row from memory: the same operations in few registers.
 template <typename T, int VEC, bool SHARED, bool REV>
 __device__ __forceinline__ void sum_tile(Shared<VEC>& s, const GlrArgs& a, const Place& p, int tile) {
     using P = Pack<T, VEC>;
     using IO = Io<T, VEC, SHARED>;
     const Rows at = rows_of(a, tile, p.w);
     const Src &sx = REV ? a.q : a.k, &sy = REV ? a.dy : a.v;
-    float A[VEC], H[VEC];
+    Logs<IO::kGates> logs;
+    float H[VEC];
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) A[i] = 1.0f, H[i] = 0.0f;
+    for (int i = 0; i < VEC; ++i) H[i] = 0.0f;
 #pragma unroll 1
     for (int j = 0; j < at.n; ++j) {
         const int64_t t = at.first + (REV ? at.n - 1 - j : j);
         float fx[VEC], fy[VEC], ga[VEC];
         P::unpack(P::load(sx.p + p.b * sx.bstride + t * sx.rstride + p.c * T::kBytes), fx);
         P::unpack(P::load(sy.p + p.b * sy.bstride + t * sy.rstride + p.c * T::kBytes), fy);
-        IO::gates(IO::G::load(a.g.p + p.b * a.g.bstride + t * a.g.rstride + p.c / (uint32_t)a.group * T::kBytes), ga);
+        IO::gates(IO::G::load(a.g.p + p.b * a.g.bstride + t * a.g.rstride + p.c / (uint32_t)a.group * T::kBytes), ga, logs);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            H[i] = REV ? ga[i] * fmaf(fx[i], fy[i], H[i]) : fmaf(ga[i], H[i], fx[i] * fy[i]);
-            A[i] *= ga[i];
-        }
+        for (int i = 0; i < VEC; ++i)
+            H[i] = REV ? times0(ga[i], fmaf(fx[i], fy[i], H[i])) : fmaf(fx[i], fy[i], times0(ga[i], H[i]));
     }
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) s.A[p.w][p.lane * VEC + i] = A[i], s.H[p.w][p.lane * VEC + i] = H[i];
+    for (int i = 0; i < VEC; ++i) s.H[p.w][p.lane * VEC + i] = H[i];
+    put_logs(s, p, logs);
 }
 
 // A record's words, as they are, and whether they are there.
@@ -257,13 +324,13 @@ __device__ __forceinline__ uint64_t peek(const uint64_t* p) { return __hip_atomi
 __device__ __forceinline__ uint32_t peek(const uint32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ bool is_set(uint64_t x) { return (uint32_t)x != kUnset && (uint32_t)(x >> 32) != kUnset; }
 __device__ __forceinline__ bool is_set(uint32_t x) { return x != kUnset; }
-__device__ __forceinline__ void publish(uint64_t* p, float A, float H) {
-    __hip_atomic_store(p, word_of(A) | (uint64_t)word_of(H) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+__device__ __forceinline__ void publish(uint64_t* p, float G, float H) {
+    __hip_atomic_store(p, word_of(G) | (uint64_t)word_of(H) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 __device__ __forceinline__ void publish(uint32_t* p, float s) {
     __hip_atomic_store(p, word_of(s), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-__device__ __forceinline__ float A_of(uint64_t x) { return __uint_as_float((uint32_t)x); }
+__device__ __forceinline__ float G_of(uint64_t x) { return __uint_as_float((uint32_t)x); }
 __device__ __forceinline__ float H_of(uint64_t x) { return __uint_as_float((uint32_t)(x >> 32)); }
 
 // Whether the tile's walk goes on behind its block.
@@ -279,14 +346,11 @@ __device__ __forceinline__ void find_edge(Shared<VEC>& s, const GlrArgs& a, cons
     const int64_t per = a.B * a.D, here = p.b * a.D;  // (the same in all lanes; a lane's own part is c)
     const int block = p.order / kBlockTiles, inside = p.order % kBlockTiles;
     const bool ends = ends_block(a, p), last = p.order + 1 == a.tiles;
-    float tA = 1.0f, tH = 0.0f;
-    for (int x = 0; x < kWaves; ++x) {
-        const int w = REV ? kWaves - 1 - x : x;
-        tH = fmaf(s.A[w][slot], tH, s.H[w][slot]);
-        tA *= s.A[w][slot];
-    }
-    if (!last && inside < BT && there) publish(a.sums + (p.order * per + here) + c, tA, tH);
-    float cA = 1.0f, cH = 0.0f, S = a.edge_in ? a.edge_in[here + c] : 0.0f;
+    float tile_G[1], tile_H[1];
+    join_all<VEC, REV, 8>(s, slot, tile_G, tile_H);
+    const float tG = tile_G[0], tH = tile_H[0];
+    if (!last && inside < BT && there) publish(a.sums + (p.order * per + here) + c, tG, tH);
+    float cG = 0.0f, cH = 0.0f, S = a.edge_in ? a.edge_in[here + c] : 0.0f;
     bool summed = inside == 0, found = block == 0;
     uint64_t jnt[BB];       // of block - i
     uint32_t have = 1;      // bits
@@ -309,18 +373,18 @@ __device__ __forceinline__ void find_edge(Shared<VEC>& s, const GlrArgs& a, cons
             }
         if (!summed) {
             bool set = true;
-            float A = 1.0f, H = 0.0f;
 #pragma unroll
             for (int i = 0; i < BT; ++i)
-                if (i < inside) {
-                    set = set && is_set(sum[i]);
-                    H = fmaf(A_of(sum[i]), H, H_of(sum[i]));
-                    A *= A_of(sum[i]);
-                }
+                if (i < inside) set = set && is_set(sum[i]);
             summed = __all(set || !there);
             if (summed) {
-                cA = A, cH = H;
-                if (ends && there) publish(a.joint + (block * per + here) + c, cA * tA, fmaf(tA, cH, tH));
+#pragma unroll
+                for (int i = 0; i < BT; ++i)
+                    if (i < inside) {
+                        cH = through(root_of(G_of(sum[i])), cH, H_of(sum[i]));
+                        cG = both(cG, G_of(sum[i]));
+                    }
+                if (ends && there) publish(a.joint + (block * per + here) + c, both(cG, tG), through(root_of(tG), cH, tH));
             }
         }
         if (!found) {
@@ -338,7 +402,7 @@ __device__ __forceinline__ void find_edge(Shared<VEC>& s, const GlrArgs& a, cons
 #pragma unroll
                 for (int i = BB - 1; i >= 0; --i) {
                     if (i == from && i < block) S = __uint_as_float(st[i]);
-                    if (i > 0 && i <= from) S = fmaf(A_of(jnt[i]), S, H_of(jnt[i]));
+                    if (i > 0 && i <= from) S = through(root_of(G_of(jnt[i])), S, H_of(jnt[i]));
                 }
             }
         }
@@ -347,10 +411,11 @@ __device__ __forceinline__ void find_edge(Shared<VEC>& s, const GlrArgs& a, cons
         if (p.lane == 0) s.lost = 1;
         return;
     }
-    if (ends && there) publish(a.states + ((block + 1) * per + here) + c, fmaf(cA * tA, S, fmaf(tA, cH, tH)));
-    S = fmaf(cA, S, cH);
+    const float tR = root_of(tG);
+    if (ends && there) publish(a.states + ((block + 1) * per + here) + c, through(root_of(both(cG, tG)), S, through(tR, cH, tH)));
+    S = through(root_of(cG), S, cH);
     s.S[slot] = S;
-    if (last && a.edge_out && there) a.edge_out[here + c] = fmaf(tA, S, tH);
+    if (last && a.edge_out && there) a.edge_out[here + c] = through(tR, S, tH);
 }
 
 // No state came in time: the workgroup walks the sequence up to its tile.  S: the state; the waves' sums are back in LDS.
@@ -358,32 +423,40 @@ template <typename T, int VEC, bool SHARED, bool REV>
 __device__ __forceinline__ void walk(Shared<VEC>& s, const GlrArgs& a, const Place& p, float (&S)[VEC]) {
     const int64_t per = a.B * a.D, here = p.b * a.D + p.c;
     const int block = p.order / kBlockTiles;
-    float A[VEC], H[VEC], cA[VEC], cH[VEC], B0[VEC];  // B0: the block's state
+    float tG[VEC], tH[VEC], cG[VEC], cH[VEC], B0[VEC];  // B0: the block's state
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) B0[i] = a.edge_in ? a.edge_in[here + i] : 0.0f, cA[i] = 1.0f, cH[i] = 0.0f;
+    for (int i = 0; i < VEC; ++i) B0[i] = a.edge_in ? a.edge_in[here + i] : 0.0f, cG[i] = 0.0f, cH[i] = 0.0f;
     for (int x = 0; x <= p.order; ++x) {
         if (x > 0 && x % kBlockTiles == 0)
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) B0[i] = fmaf(cA[i], B0[i], cH[i]), cA[i] = 1.0f, cH[i] = 0.0f;
-        if (x == p.order)
+            for (int i = 0; i < VEC; ++i) B0[i] = through(root_of(cG[i]), B0[i], cH[i]), cG[i] = 0.0f, cH[i] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) S[i] = fmaf(cA[i], B0[i], cH[i]);
+        for (int i = 0; i < VEC; ++i) S[i] = through(root_of(cG[i]), B0[i], cH[i]);
         __syncthreads();
         sum_tile<T, VEC, SHARED, REV>(s, a, p, REV ? a.tiles - 1 - x : x);
         __syncthreads();
-        join<VEC, REV>(s, REV ? -1 : kWaves, p.lane, A, H);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) cH[i] = fmaf(A[i], cH[i], H[i]), cA[i] *= A[i];
-    }
-    if (p.w == 0 && p.there)
+        join_all<VEC, REV, 1>(s, p.lane * VEC, tG, tH);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            if (ends_block(a, p)) {
-                publish(a.joint + block * per + here + i, cA[i], cH[i]);
-                publish(a.states + (block + 1) * per + here + i, fmaf(cA[i], B0[i], cH[i]));
-            }
-            if (a.edge_out && p.order + 1 == a.tiles) a.edge_out[here + i] = fmaf(A[i], S[i], H[i]);
+            cH[i] = through(root_of(tG[i]), cH[i], tH[i]);
+            cG[i] = both(cG[i], tG[i]);
         }
+    }
+    if (p.w != 0 || !p.there) return;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        tH[i] = through(root_of(tG[i]), S[i], tH[i]);
+        B0[i] = through(root_of(cG[i]), B0[i], cH[i]);
+    }
+    if (ends_block(a, p))
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            publish(a.joint + block * per + here + i, cG[i], cH[i]);
+            publish(a.states + (block + 1) * per + here + i, B0[i]);
+        }
+    if (a.edge_out && p.order + 1 == a.tiles)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) a.edge_out[here + i] = tH[i];
 }
 
 // With the waves' sums on their way to LDS: the state at the tile's edge.
@@ -436,8 +509,10 @@ __global__ __launch_bounds__(kWaves * kWave, 4) void glr_fwd_kernel(GlrArgs a) {
     load_rows<P>(v, a.v, a, p, at, lane_bytes);
     load_rows<typename IO::G>(g, a.g, a, p, at, p.c / (uint32_t)a.group * T::kBytes);
     if constexpr (Y) load_rows<P>(q, a.q, a, p, at, lane_bytes);
-    sum_rows<T, VEC, false>(s, k, v, p, at.n, [&](int r, float(&ga)[VEC]) { IO::gates(g[r], ga); });
-    float S[VEC], eA[VEC], eH[VEC];
+    Logs<IO::kGates> logs;
+    sum_rows<T, VEC, false>(s, k, v, p, at.n, [&](int r, float(&ga)[VEC]) { IO::gates(g[r], ga, logs); });
+    put_logs(s, p, logs);
+    float S[VEC];
     edge_of<T, VEC, SHARED, false>(s, a, p, S);
     keep_raw(k);
     keep_raw(v);
@@ -446,9 +521,7 @@ __global__ __launch_bounds__(kWaves * kWave, 4) void glr_fwd_kernel(GlrArgs a) {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) a.marks_out[(p.b * a.tiles + p.tile) * a.D + p.c + i] = S[i];
     if (!Y || !p.there) return;
-    join<VEC, false>(s, p.w, p.lane, eA, eH);
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) S[i] = fmaf(eA[i], S[i], eH[i]);
+    join<VEC, false>(s, p.w, p.lane, S);
     const auto yp = buffer_of(a.y + (p.b * a.L + at.first) * a.D * T::kBytes);
     const uint32_t step = (uint32_t)a.D * T::kBytes;
     for_rows<false>(at.n, [&](int r) {
@@ -459,7 +532,7 @@ __global__ __launch_bounds__(kWaves * kWave, 4) void glr_fwd_kernel(GlrArgs a) {
         IO::gates(g[r], ga);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            S[i] = fmaf(ga[i], S[i], fk[i] * fv[i]);
+            S[i] = fmaf(fk[i], fv[i], times0(ga[i], S[i]));
             fq[i] *= S[i];
         }
         buffer_store<P>(yp, lane_bytes, r * step, P::pack(fq));
@@ -497,14 +570,16 @@ __global__ __launch_bounds__(kWaves * kWave, 4) void glr_bwd_kernel(GlrArgs a) {
     load_rows<typename IO::G>(g, a.g, a, p, at, p.c / (uint32_t)a.group * T::kBytes);
     load_rows<P>(k, a.k, a, p, at, lane_bytes);
     load_rows<P>(v, a.v, a, p, at, lane_bytes);
-    float S[VEC], R[VEC], eA[VEC], eH[VEC], decay[kRowsPerWave][SHARED ? 1 : VEC];
+    float S[VEC], R[VEC], decay[kRowsPerWave][IO::kGates];
+    Logs<IO::kGates> logs;
 #pragma unroll
-    for (int r = 0; r < kRowsPerWave; ++r) {
+    for (int r = kRowsPerWave - 1; r >= 0; --r) {  // (a branch for whole tiles keeps later loads behind it)
         float ga[VEC];
-        IO::gates(g[r], ga);
+        IO::gates(g[r], ga, logs, r < at.n);
 #pragma unroll
-        for (int i = 0; i < (SHARED ? 1 : VEC); ++i) decay[r][i] = ga[i];
+        for (int i = 0; i < IO::kGates; ++i) decay[r][i] = ga[i];
     }
+    put_logs(s, p, logs);
     auto gates = [&](int r, float(&ga)[VEC]) {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) ga[i] = decay[r][SHARED ? 0 : i];
@@ -513,15 +588,13 @@ __global__ __launch_bounds__(kWaves * kWave, 4) void glr_bwd_kernel(GlrArgs a) {
     edge_of<T, VEC, SHARED, true>(s, a, p, R);
     keep_raw(q);
     keep_raw(dy);
-    join<VEC, true>(s, p.w, p.lane, eA, eH);
+    join<VEC, true>(s, p.w, p.lane, R);
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) R[i] = fmaf(eA[i], R[i], eH[i]);
+    for (int i = 0; i < VEC; ++i) S[i] = a.marks[(p.b * a.tiles + p.tile) * a.D + p.c + i];
     __syncthreads();
     sum_rows<T, VEC, false>(s, k, v, p, at.n, gates);
     __syncthreads();
-    join<VEC, false>(s, p.w, p.lane, eA, eH);
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) S[i] = fmaf(eA[i], a.marks[(p.b * a.tiles + p.tile) * a.D + p.c + i], eH[i]);
+    join<VEC, false>(s, p.w, p.lane, S);
     keep_raw(k);
     keep_raw(v);
 
@@ -538,7 +611,7 @@ __global__ __launch_bounds__(kWaves * kWave, 4) void glr_bwd_kernel(GlrArgs a) {
         gates(r, ga);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            kept[r][i] = ga[i] * S[i];
+            kept[r][i] = times0(ga[i], S[i]);
             S[i] = fmaf(fk[i], fv[i], kept[r][i]);
             fy[i] *= S[i];
         }
@@ -554,8 +627,8 @@ __global__ __launch_bounds__(kWaves * kWave, 4) void glr_bwd_kernel(GlrArgs a) {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
             const float m = fmaf(fq[i], fy[i], R[i]);
-            R[i] = ga[i] * m;
-            dg[i] = p.there ? m * kept[r][i] : 0.0f;
+            R[i] = times0(ga[i], m);
+            dg[i] = p.there ? times0(m, kept[r][i]) : 0.0f;
             const float mv = m * fv[i];
             fv[i] = m * fk[i];
             fk[i] = mv;
@@ -613,7 +686,7 @@ __global__ __launch_bounds__(256) void glr_step_kernel(const char* q, const char
     Pack<F32, VEC>::unpack(rs, s);
 #pragma unroll
     for (int j = 0; j < VEC; ++j) {
-        s[j] = fmaf(ga[j], s[j], fk[j] * fv[j]);
+        s[j] = fmaf(fk[j], fv[j], times0(ga[j], s[j]));
         fq[j] *= s[j];
     }
     Pack<F32, VEC>::store(state + i, Pack<F32, VEC>::pack(s));
@@ -711,7 +784,7 @@ hy_status take_records(GlrArgs& a, const GlrShape& s, void* ws, hipStream_t st) 
     a.sums = static_cast<uint64_t*>(ws);
     a.joint = a.sums + tiles_of(s) * s.B * s.D;
     a.states = reinterpret_cast<uint32_t*>(a.joint + blocks_of(s) * s.B * s.D);
-    a.polls = tuning().glr_wait == 1 ? 0 : kPolls;
+    a.polls = tuning().glr_wait == 0 ? kPolls : tuning().glr_wait == 1 ? 0 : 1;
     if (bytes == 0) return HY_OK;
     const int64_t per = 256 * kMarks * 16;
     if ((bytes + per - 1) / per > INT32_MAX) return HY_ERR_UNSUPPORTED;

@@ -129,7 +129,7 @@ struct Tuning {
     int mr_rows = 0;
     int mr_waves = 0;
     int se_walk = 0;  // 0: by size, 1: always the walking SE kernel where it applies, 2: never
-    int glr_wait = 0; // the gated linear recurrence: 0: wait for earlier tiles' states, 1: compute them again
+    int glr_wait = 0; // the gated linear recurrence: 0: wait for earlier tiles' states, 1: compute them again, 2: look once
     int li_wait = 0;  // Hyena-LI in one pass: 0: wait for earlier tiles' states, 1: recompute them, 2: never in one pass
 };
 // The options as the calling thread's current entry point sees them.  Every extern "C" function that sizes or

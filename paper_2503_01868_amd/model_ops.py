@@ -142,8 +142,9 @@ def _glr_fwd(q, k, v, g, group, state_in, want_state, want_marks, out, workspace
 
 
 def hyena_glr_fwd(q, k, v, g, group: int = 1, out=None, workspace=None, stream=None) -> torch.Tensor:
-    """y = q * s with s[t] = exp(g[t]) s[t-1] + k[t] v[t] from a zero state; ``g`` is [B, L, D // group].  Inputs may be views
-    whose channels are contiguous; see ``hyena_glr_fwd`` in hyena.h."""
+    """y = q * s with s[t] = exp(g[t]) s[t-1] + k[t] v[t] from a zero state; ``g`` is [B, L, D // group].  A decay of
+    zero forgets everything before its step, NaN included.  Inputs may be views whose channels are contiguous; see
+    ``hyena_glr_fwd`` in hyena.h."""
     return _glr_fwd(q, k, v, g, int(group), None, False, False, out, workspace, stream)[0]
 
 
