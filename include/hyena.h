@@ -401,7 +401,8 @@ int64_t hyena_bwd_shard_workspace_bytes(int64_t B, int64_t L, int64_t D, int32_t
  * a row; negative: HY_ERR_SHAPE).  Outputs are dense.  q, k, v, g may begin at any element, every other
  * pointer is 16-byte aligned; where a size is zero the pointers to what is empty may be NULL.
  * workspace: hyena_glr_fwd_workspace_bytes(...) bytes, disjoint from every argument, contents undefined afterwards.
- * D and the distances between steps are at most 2^26 elements (HY_ERR_UNSUPPORTED); L and whole tensors may pass 2^32.
+ * D and the distances between steps are at most 2^26 elements, and B ceil(L / 64) ceil(D / 64) below 2^23 tiles is served (more
+ * where a tile is wider than 64 channels), else HY_ERR_UNSUPPORTED.  Whole tensors may pass 2^32 elements.
  */
 #define HYENA_GLR_MARK_ROWS 64
 hy_status hyena_glr_fwd(const void *q, const void *k, const void *v, const void *g, const float *state_in, void *y,
@@ -428,7 +429,7 @@ int64_t hyena_glr_bwd_workspace_bytes(int64_t B, int64_t L, int64_t D, int32_t g
 
 /*
  * One step of hyena_glr_fwd for B sequences, in place on their states: state = exp(g) * state + k (.) v, y = q (.) state.
- * q, k, v, y: dense [B,D], g: dense [B,D/group], of `dtype`; state: fp32 [B,D].
+ * q, k, v, y: dense [B,D], g: dense [B,D/group], of `dtype`; state: fp32 [B,D].  B D up to 2^32 - 256 (HY_ERR_UNSUPPORTED).
  */
 hy_status hyena_glr_step(const void *q, const void *k, const void *v, const void *g, float *state, void *y, int64_t B,
                          int64_t D, int32_t group, int32_t dtype, void *hip_stream);
@@ -439,7 +440,7 @@ hy_status hyena_glr_step(const void *q, const void *k, const void *v, const void
  * x: [N,D], w: [V,D], dense, of `dtype`; target: int64 [N]; loss, lse: fp32 [N].  A row whose target is outside 0 .. V - 1 takes no
  * part: its loss is 0 (its lse is written all the same).  The products run on the bf16 matrix cores with fp32 sums: bf16
  * operands as they are, fp32 operands as three bf16 parts each, to fp32's precision.
- * V, D >= 1 (HY_ERR_SHAPE); N = 0 is an empty problem; N, D up to 4194112 and N D up to 2^39 (HY_ERR_UNSUPPORTED).
+ * V, D >= 1 (HY_ERR_SHAPE); N = 0 is an empty problem; N and D up to 4194112 (HY_ERR_UNSUPPORTED).
  * workspace: hyena_xent_fwd_workspace_bytes(...) bytes.
  */
 hy_status hyena_xent_fwd(const void *x, const void *w, const int64_t *target, float *loss, float *lse, void *workspace,
@@ -453,6 +454,7 @@ int64_t hyena_xent_fwd_workspace_bytes(int64_t N, int64_t V, int64_t D, int32_t 
  * they hold.  P is rounded to bf16 for its two products in bf16 calls, in units of the largest |dloss| (a constant weight such as
  * 1 / N costs no rounding), and kept in fp32 in fp32 calls; sums are fp32, in a fixed order, one rounding per stored
  * element.  The vocabulary is taken in pieces: workspace (hyena_xent_bwd_workspace_bytes(...) bytes) holds P of one piece.
+ * N D and V D up to 2^35 are served (HY_ERR_UNSUPPORTED).
  */
 hy_status hyena_xent_bwd(const float *dloss, const void *x, const void *w, const int64_t *target, const float *lse, void *dx,
                          void *dw, void *workspace, int64_t workspace_bytes, int64_t N, int64_t V, int64_t D,
@@ -474,8 +476,9 @@ int64_t hyena_xent_bwd_workspace_bytes(int64_t N, int64_t V, int64_t D, int32_t 
  * hyena_adamw_table writes, into host memory, the table that the step reads: table_bytes >= hyena_adamw_table_bytes(...) of
  * the same arguments (-1: not a valid problem).  The caller copies it to the device, once for as long as the tensors stay where
  * they are, and hands the copy to hyena_adamw_step with the same n_tensors, param, grad, bits and with_master, and with the
- * number of chunks that it returned.  The arguments are checked when the table is made: pointers NULL (HY_ERR_NULL; an empty
- * tensor's may be), a written array that overlaps another array or pointers off their element's alignment (HY_ERR_ALIGN).
+ * number of chunks that it returned (of up to 4096 elements each, fewer than 2^24 in all: else HY_ERR_SHAPE).  The arguments are
+ * checked when the table is made: pointers NULL (HY_ERR_NULL; an empty tensor's may be), a written array that overlaps another
+ * array or pointers off their element's alignment (HY_ERR_ALIGN).
  * hyena_adamw_step(step >= 1, 0 <= beta < 1, eps >= 0; else HY_ERR_SHAPE) reads grad_scale, one fp32 number in device
  * memory, if it is not NULL.
  */

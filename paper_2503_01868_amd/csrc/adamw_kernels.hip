@@ -20,7 +20,7 @@ namespace {
 
 constexpr int kPer = 4;                               // elements of a lane
 constexpr int kBlock = kAdamwBlock;                   // of a wave at a time
-constexpr int kWaves = 4;
+constexpr int kWaves = kAdamwThreads / kWave;
 constexpr int kBlocks = kAdamwChunk / kBlock / kWaves;  // of a wave
 static_assert(kPer * kWave == kBlock, "a wave takes a block");
 

@@ -481,16 +481,15 @@ __device__ __forceinline__ void edge_of(Shared<VEC>& s, const GlrArgs& a, const 
 
 constexpr int kMarks = 4;  // 16-byte pieces per lane
 __global__ __launch_bounds__(256) void glr_unset_kernel(uint4* rec, int64_t n) {
-    const int64_t i0 = (int64_t)blockIdx.x * 256 * kMarks + threadIdx.x;
+    for (int64_t i0 = (int64_t)blockIdx.x * 256 * kMarks + threadIdx.x; i0 < n; i0 += (int64_t)gridDim.x * 256 * kMarks)
 #pragma unroll
-    for (int x = 0; x < kMarks; ++x)
-        if (i0 + 256 * x < n) store_words<4>(rec + i0 + 256 * x, Words<4>{{kUnset, kUnset, kUnset, kUnset}});
+        for (int x = 0; x < kMarks; ++x)
+            if (i0 + 256 * x < n) store_words<4>(rec + i0 + 256 * x, Words<4>{{kUnset, kUnset, kUnset, kUnset}});
 }
 
 // The state of sequences without steps goes on as it is.
 __global__ __launch_bounds__(256) void glr_hand_on_kernel(const float* in, float* out, int64_t n) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i < n) out[i] = in ? in[i] : 0.0f;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) out[i] = in ? in[i] : 0.0f;
 }
 
 // Y: q comes in and y goes out; else the states alone.  Bound by the bytes, and by the wait for the edge in launches of a few rounds:
@@ -660,11 +659,11 @@ __global__ __launch_bounds__(kWaves * kWave, 4) void glr_bwd_kernel(GlrArgs a) {
 // dg[row][n] = sum over the group's parts, in their order.
 template <typename T>
 __global__ __launch_bounds__(256) void glr_dg_kernel(const float* parts, char* dg, int64_t n, int32_t per) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= n) return;
-    float s[1] = {0.0f};
-    for (int32_t j = 0; j < per; ++j) s[0] += parts[i * per + j];
-    Pack<T, 1>::store(dg + i * T::kBytes, Pack<T, 1>::pack(s));
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        float s[1] = {0.0f};
+        for (int32_t j = 0; j < per; ++j) s[0] += parts[i * per + j];
+        Pack<T, 1>::store(dg + i * T::kBytes, Pack<T, 1>::pack(s));
+    }
 }
 
 // One step of every sequence: the state is updated where it is.  64 x 4096: 2.6 us, a launch's time.
@@ -764,14 +763,14 @@ GlrArgs args_of(const GlrPtrs& p, const GlrShape& s, int vec, int64_t* grid) {
     // 32 bits address the rows of a wave
     bool near = s.D <= (INT64_C(1) << 26);
     for (int i = 0; i < 5; ++i) near = near && s.rstride[i] <= (INT64_C(1) << 26);
-    *grid = near && tiles <= INT32_MAX && ncb <= INT32_MAX && s.B <= INT32_MAX / tiles / ncb ? s.B * tiles * ncb : -1;
+    *grid = near && s.B <= most_workgroups(kWaves * kWave) / tiles / ncb ? s.B * tiles * ncb : -1;
     a.tiles = (int32_t)tiles, a.ncb = (int32_t)ncb;
     a.part = part_of(s.group, (int32_t)width);
     return a;
 }
 
 hy_status hand_on(const float* in, float* out, const GlrShape& s, hipStream_t st) {
-    return launch_kernel(glr_hand_on_kernel, dim3((uint32_t)((s.B * s.D + 255) / 256)), dim3(256), st, in, out, s.B * s.D);
+    return launch_kernel(glr_hand_on_kernel, dim3(workgroups_for(s.B * s.D, 256, 256)), dim3(256), st, in, out, s.B * s.D);
 }
 
 // Records of the tiles: none where a sequence is one tile.
@@ -786,9 +785,8 @@ hy_status take_records(GlrArgs& a, const GlrShape& s, void* ws, hipStream_t st) 
     a.states = reinterpret_cast<uint32_t*>(a.joint + blocks_of(s) * s.B * s.D);
     a.polls = tuning().glr_wait == 0 ? kPolls : tuning().glr_wait == 1 ? 0 : 1;
     if (bytes == 0) return HY_OK;
-    const int64_t per = 256 * kMarks * 16;
-    if ((bytes + per - 1) / per > INT32_MAX) return HY_ERR_UNSUPPORTED;
-    return launch_kernel(glr_unset_kernel, dim3((uint32_t)((bytes + per - 1) / per)), dim3(256), st, static_cast<uint4*>(ws), bytes / 16);
+    return launch_kernel(glr_unset_kernel, dim3(workgroups_for(bytes / 16, 256 * kMarks, 256)), dim3(256), st, static_cast<uint4*>(ws),
+                         bytes / 16);
 }
 
 }  // namespace
@@ -838,8 +836,7 @@ hy_status launch_glr_bwd(const GlrPtrs& p, const GlrShape& s, void* ws, hipStrea
         rc = by_kind(s, vec, [&](auto kernels) { return kernels.backward(a, (uint32_t)grid, st); });
     if (rc == HY_OK && a.part != s.group) {
         const int64_t out = s.B * s.L * (s.D / s.group);
-        if ((out + 255) / 256 > INT32_MAX) return HY_ERR_UNSUPPORTED;
-        const dim3 g((uint32_t)((out + 255) / 256)), b(256);
+        const dim3 g(workgroups_for(out, 256, 256)), b(256);
         const float* parts = a.dg_parts;
         const int32_t per = s.group / a.part;
         rc = s.dtype == HY_F32 ? launch_kernel(glr_dg_kernel<F32>, g, b, st, parts, (char*)p.dg, out, per)
@@ -850,7 +847,7 @@ hy_status launch_glr_bwd(const GlrPtrs& p, const GlrShape& s, void* ws, hipStrea
 
 hy_status launch_glr_step(const GlrPtrs& p, const GlrShape& s, hipStream_t st) {
     const int64_t n = s.B * s.D;
-    if ((n + 255) / 256 > INT32_MAX) return HY_ERR_UNSUPPORTED;
+    if ((n + 255) / 256 > most_workgroups(256)) return HY_ERR_UNSUPPORTED;
     return by_kind(s, vec_of(s, 4), [&](auto kernels) { return kernels.step(p, n, s.group, st); });
 }
 

@@ -296,6 +296,7 @@ hy_status launch_glr_step(const GlrPtrs& p, const GlrShape& s, hipStream_t st);
 // AdamW over many tensors: a table in device memory, an entry per tensor and the owner of each chunk of kAdamwChunk elements.
 constexpr int kAdamwBlock = HYENA_ADAMW_BLOCK;  // elements that share a scale where the states have 8 bits
 constexpr int kAdamwChunk = 4096;
+constexpr int kAdamwThreads = 256;
 struct AdamwEntry {
     void* param;
     const void* grad;
@@ -332,6 +333,14 @@ int64_t xent_fwd_workspace_bytes(const XentShape& s);
 int64_t xent_bwd_workspace_bytes(const XentShape& s);
 hy_status launch_xent_fwd(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t st);
 hy_status launch_xent_bwd(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t st);
+
+// How many workgroups HIP takes: it counts fewer than 2^32 threads.
+constexpr int64_t most_workgroups(int64_t threads) { return INT64_C(0xffffffff) / threads; }
+// Workgroups for n items, `per` of them each; a kernel that runs over its items in steps of its grid may have fewer.
+inline uint32_t workgroups_for(int64_t n, int64_t per, int64_t threads) {
+    const int64_t w = (n + per - 1) / per, most = most_workgroups(threads);
+    return (uint32_t)(w < most ? w : most);
+}
 
 // Launches `kernel` and returns the status of THIS launch as hipLaunchKernel reports it.  The thread's sticky
 // "last error" is neither read nor cleared: an error left behind by an earlier, unrelated HIP call of the caller

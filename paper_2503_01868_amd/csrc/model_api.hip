@@ -85,6 +85,8 @@ hy_status check_xent(int64_t N, int64_t V, int64_t D, int32_t dtype) {
 
 // ---- AdamW
 
+constexpr int64_t kMostChunks = most_workgroups(kAdamwThreads);  // one workgroup each
+
 int64_t chunks_of(int64_t count) { return (count + kAdamwChunk - 1) / kAdamwChunk; }
 
 // The chunks of all tensors; -1: not a valid problem.
@@ -94,7 +96,7 @@ int64_t adamw_chunks(const hy_adamw_tensor* t, int64_t n) {
     for (int64_t i = 0; i < n; ++i) {
         if (t[i].count < 0 || t[i].count > kMostElements) return -1;
         all += chunks_of(t[i].count);
-        if (all > INT32_MAX) return -1;  // one workgroup each
+        if (all > kMostChunks) return -1;
     }
     return n > INT32_MAX ? -1 : all;
 }
@@ -242,7 +244,7 @@ hy_status hyena_adamw_step(const void* table, int64_t n_tensors, int64_t chunks,
                            const float* grad_scale, void* hip_stream) {
     hy_status rc = check_adamw_kinds(param, grad, bits, with_master);
     if (rc != HY_OK) return rc;
-    if (n_tensors < 0 || chunks < 0 || chunks > INT32_MAX || (n_tensors == 0 && chunks > 0)) return HY_ERR_SHAPE;
+    if (n_tensors < 0 || chunks < 0 || chunks > kMostChunks || (n_tensors == 0 && chunks > 0)) return HY_ERR_SHAPE;
     if (step < 1 || !(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1) || !(eps >= 0)) return HY_ERR_SHAPE;
     if (chunks == 0) return HY_OK;
     if (!table) return HY_ERR_NULL;

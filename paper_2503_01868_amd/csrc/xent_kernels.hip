@@ -29,10 +29,10 @@ using Bits = std::conditional_t<T::kBytes == 4, uint32_t, uint16_t>;
 
 // Rows of D bf16 numbers -> rows of `ld`, zeros behind them: rows that do not begin where 16 bytes do.
 __global__ __launch_bounds__(256) void pack_kernel(const uint16_t* src, uint16_t* dst, int64_t rows, int64_t D, int64_t ld) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= rows * ld) return;
-    const int64_t r = i / ld, c = i % ld;
-    dst[i] = c < D ? src[r * D + c] : 0;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * ld; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / ld, c = i % ld;
+        dst[i] = c < D ? src[r * D + c] : 0;
+    }
 }
 
 // The largest weight of a row that takes part, by one workgroup.  P in this unit is -1 where a target is far from foreseen, which
@@ -533,8 +533,8 @@ __global__ __launch_bounds__(256) void gather_kernel(XentArgs a) {
 }
 
 __global__ __launch_bounds__(256) void zero_kernel(char* p, int64_t bytes) {
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 2;
-    if (i < bytes) *reinterpret_cast<uint16_t*>(p + i) = 0;
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 2; i < bytes; i += (int64_t)gridDim.x * 512)
+        *reinterpret_cast<uint16_t*>(p + i) = 0;
 }
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
@@ -575,7 +575,7 @@ struct Carver {
 };
 
 // Up to 32 rows of fp32 values that begin where 16 bytes do.
-bool few_rows(const XentShape& s) { return s.dtype == HY_F32 && s.N <= 32 && s.D % 4 == 0 && cut(s.V, kFewWords) <= INT32_MAX; }
+bool few_rows(const XentShape& s) { return s.dtype == HY_F32 && s.N <= 32 && s.D % 4 == 0 && cut(s.V, kFewWords) <= most_workgroups(kFewWaves * kWave); }
 
 struct FwdSpace {
     uint16_t *x, *w;
@@ -626,11 +626,17 @@ Edges edges_of(Tile t) {
 // 256 x 256, 106 in tiles of 32 x 64).
 Tile logit_tile(const GemmArgs& g) { return g.a.rows <= 32 ? Tile::kFew32 : g.a.rows <= 64 ? Tile::kFew64 : tile_for(g); }
 
+// Whether HIP takes a workgroup for every tile (more than one only where tiles are few).
+bool launchable(const GemmArgs& g, Tile tile) {
+    const Edges e = edges_of(tile);
+    return cut(g.a.rows, e.rows) <= most_workgroups(tile == Tile::kFew32 || tile == Tile::kFew64 ? 256 : 512) / cut(g.b.rows, e.cols);
+}
+
 template <typename F>
 hy_status by_tile(XentArgs& a, Tile tile, F f) {
     const Edges e = edges_of(tile);
     const int64_t mt = cut(a.g.a.rows, e.rows), nt = cut(a.g.b.rows, e.cols);
-    if (mt > INT32_MAX / 16 / nt) return HY_ERR_UNSUPPORTED;
+    if (!launchable(a.g, tile)) return HY_ERR_UNSUPPORTED;
     a.g.mt = (int32_t)mt, a.g.nt = (int32_t)nt;
     return f(dim3((uint32_t)(mt * nt)));
 }
@@ -778,13 +784,12 @@ hy_status product(XentArgs& a, float* split, hipStream_t st) {
             }
     });
     if (rc != HY_OK || a.splits == 1) return rc;
-    const int64_t lanes = a.g.a.rows * ((a.out_ld + 3) / 4);
-    if (cut(lanes, 256) > INT32_MAX) return HY_ERR_UNSUPPORTED;
+    const int64_t lanes = a.g.a.rows * ((a.out_ld + 3) / 4);  // (of few tiles: far from the launch's limit)
     return launch_kernel(gather_kernel<T>, dim3((uint32_t)cut(lanes, 256)), dim3(256), st, a);
 }
 
 hy_status pack(const uint16_t* src, uint16_t* dst, int64_t rows, int64_t D, int64_t ld, hipStream_t st) {
-    return launch_kernel(pack_kernel, dim3((uint32_t)cut(rows * ld, 256)), dim3(256), st, src, dst, rows, D, ld);
+    return launch_kernel(pack_kernel, dim3(workgroups_for(rows * ld, 256, 256)), dim3(256), st, src, dst, rows, D, ld);
 }
 
 template <typename T>
@@ -873,11 +878,24 @@ hy_status backward(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t 
     return rc;
 }
 
-// Row distances that a lane's 32-bit offsets within a tile reach, and grids of 2^31 workgroups.
-bool served(const XentShape& s) {
+// Row distances that a lane's 32-bit offsets within a tile reach, and a workgroup for every tile of every product of a piece (the
+// last one may be narrower, and take other tiles).
+template <typename T>
+bool served_as(const XentShape& s, const Layout& l, bool backward) {
+    if (l.ld > 64 * 65534 || l.nt > (1 << 22) || l.piece > (1 << 22)) return false;
+    for (const int64_t cols : {std::min(l.piece, s.V), s.V - (l.pieces - 1) * l.piece}) {
+        const GemmArgs z = product_of(GemmOperand{nullptr, l.ld, s.N}, GemmOperand{nullptr, l.ld, cols}, l.packed ? l.ld : s.D);
+        if (!launchable(z, logit_tile_for<T>(z))) return false;
+        if (!backward) continue;
+        const GemmArgs dw = dw_product<T>(s, l, cols), dx = dx_product<T>(s, l, cols);
+        if (!launchable(dw, product_tile_for<T, false>(dw))) return false;
+        if (!launchable(dx, across<T>(s) ? product_tile_for<T, true>(dx) : product_tile_for<T, false>(dx))) return false;
+    }
+    return true;
+}
+bool served(const XentShape& s, bool backward) {
     const Layout l = layout_of(s);
-    return l.ld <= (1 << 22) && l.nt <= (1 << 22) && l.piece <= (1 << 22) && cut(s.N, 128) * cut(l.piece, 128) <= INT32_MAX &&
-           cut(s.N * l.ld, 256) <= INT32_MAX && cut(l.piece * l.ld, 256) <= INT32_MAX && l.ld <= 64 * 65534;
+    return s.dtype == HY_F32 ? served_as<F32>(s, l, backward) : served_as<BF16>(s, l, backward);
 }
 
 }  // namespace
@@ -898,17 +916,16 @@ int64_t xent_bwd_workspace_bytes(const XentShape& s) {
 }
 
 hy_status launch_xent_fwd(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t st) {
-    if (!served(s)) return HY_ERR_UNSUPPORTED;
+    if (!served(s, false)) return HY_ERR_UNSUPPORTED;
     return s.dtype == HY_F32 ? forward<F32>(p, s, ws, st) : forward<BF16>(p, s, ws, st);
 }
 
 hy_status launch_xent_bwd(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t st) {
     if (s.N == 0) {  // no rows: nothing but zeros for the weights
         const int64_t bytes = s.V * s.D * (s.dtype == HY_F32 ? 4 : 2);
-        if (cut(bytes, 512) > INT32_MAX) return HY_ERR_UNSUPPORTED;
-        return launch_kernel(zero_kernel, dim3((uint32_t)cut(bytes, 512)), dim3(256), st, (char*)p.dw, bytes);
+        return launch_kernel(zero_kernel, dim3(workgroups_for(bytes, 512, 256)), dim3(256), st, (char*)p.dw, bytes);
     }
-    if (!served(s)) return HY_ERR_UNSUPPORTED;
+    if (!served(s, true)) return HY_ERR_UNSUPPORTED;
     return s.dtype == HY_F32 ? backward<F32>(p, s, ws, st) : backward<BF16>(p, s, ws, st);
 }
 
