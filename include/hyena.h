@@ -441,7 +441,7 @@ hy_status hyena_glr_step(const void *q, const void *k, const void *v, const void
  * part: its loss is 0 (its lse is written all the same).  The products run on the bf16 matrix cores with fp32 sums: bf16
  * operands as they are, fp32 operands as three bf16 parts each, to fp32's precision.
  * V, D >= 1 (HY_ERR_SHAPE); N = 0 is an empty problem; N and D up to 4194112 (HY_ERR_UNSUPPORTED).
- * workspace: hyena_xent_fwd_workspace_bytes(...) bytes.
+ * workspace: hyena_xent_fwd_workspace_bytes(...) bytes (-1, here and below: not a valid problem, or sizes not served).
  */
 hy_status hyena_xent_fwd(const void *x, const void *w, const int64_t *target, float *loss, float *lse, void *workspace,
                          int64_t workspace_bytes, int64_t N, int64_t V, int64_t D, int32_t dtype, void *hip_stream);

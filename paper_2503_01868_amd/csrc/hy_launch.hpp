@@ -329,6 +329,8 @@ struct XentShape {
     int64_t N, V, D;
     hy_dtype dtype;
 };
+// Whether the sizes (N, V, D >= 1) can be launched; the calls below take no others.
+bool xent_served(const XentShape& s, bool backward);
 int64_t xent_fwd_workspace_bytes(const XentShape& s);
 int64_t xent_bwd_workspace_bytes(const XentShape& s);
 hy_status launch_xent_fwd(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t st);

@@ -161,12 +161,16 @@ extern "C" {
 
 int64_t hyena_xent_fwd_workspace_bytes(int64_t N, int64_t V, int64_t D, int32_t dtype) {
     if (check_xent(N, V, D, dtype) != HY_OK) return -1;
-    return N == 0 ? 0 : xent_fwd_workspace_bytes(XentShape{N, V, D, static_cast<hy_dtype>(dtype)});
+    if (N == 0) return 0;
+    const XentShape s{N, V, D, static_cast<hy_dtype>(dtype)};
+    return xent_served(s, false) ? xent_fwd_workspace_bytes(s) : -1;
 }
 
 int64_t hyena_xent_bwd_workspace_bytes(int64_t N, int64_t V, int64_t D, int32_t dtype) {
     if (check_xent(N, V, D, dtype) != HY_OK) return -1;
-    return N == 0 ? 0 : xent_bwd_workspace_bytes(XentShape{N, V, D, static_cast<hy_dtype>(dtype)});
+    if (N == 0) return 0;
+    const XentShape s{N, V, D, static_cast<hy_dtype>(dtype)};
+    return xent_served(s, true) ? xent_bwd_workspace_bytes(s) : -1;
 }
 
 hy_status hyena_xent_fwd(const void* x, const void* w, const int64_t* target, float* loss, float* lse, void* workspace,
@@ -181,6 +185,7 @@ hy_status hyena_xent_fwd(const void* x, const void* w, const int64_t* target, fl
     const Range all[5] = {{x, N * D * e}, {w, V * D * e}, {target, N * 8}, {loss, N * 4}, {lse, N * 4}};
     rc = all_aligned(all, 5);
     if (rc == HY_OK) rc = check_disjoint(all, 3, all + 3, 2);
+    if (rc == HY_OK && !xent_served(s, false)) return HY_ERR_UNSUPPORTED;
     if (rc == HY_OK) rc = check_workspace(workspace, workspace_bytes, xent_fwd_workspace_bytes(s), all, 5);
     if (rc != HY_OK) return rc;
     XentPtrs p;
@@ -200,6 +205,7 @@ hy_status hyena_xent_bwd(const float* dloss, const void* x, const void* w, const
     const Range all[7] = {{x, N * D * e}, {w, V * D * e}, {target, N * 8}, {dloss, N * 4}, {lse, N * 4}, {dx, N * D * e}, {dw, V * D * e}};
     rc = all_aligned(all, 7);
     if (rc == HY_OK) rc = check_disjoint(all, 5, all + 5, 2);
+    if (rc == HY_OK && N > 0 && !xent_served(s, true)) return HY_ERR_UNSUPPORTED;
     if (rc == HY_OK) rc = check_workspace(workspace, workspace_bytes, N > 0 ? xent_bwd_workspace_bytes(s) : 0, all, 7);
     if (rc != HY_OK) return rc;
     XentPtrs p;

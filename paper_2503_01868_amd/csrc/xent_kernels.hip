@@ -546,6 +546,7 @@ struct Layout {
     int64_t ld;               // of x and W in the products
     int64_t nt;               // N rounded up: the k of dW
     int64_t piece, pieces;    // columns of the vocabulary at a time
+    int64_t sizes[2];         // of all pieces but the last, and of the last
 };
 
 constexpr int64_t kPieceBytes = INT64_C(512) << 20;  // of P and its transpose
@@ -560,6 +561,8 @@ Layout layout_of(const XentShape& s) {
     l.pieces = cut(s.V, most);
     l.piece = std::min(up(cut(s.V, l.pieces), 256), up(s.V, kGemmK));
     l.pieces = cut(s.V, l.piece);
+    l.sizes[1] = s.V - (l.pieces - 1) * l.piece;
+    l.sizes[0] = l.pieces > 1 ? l.piece : l.sizes[1];
     return l;
 }
 
@@ -583,10 +586,8 @@ struct FwdSpace {
     float* zt;
     int64_t tiles;
     FwdSpace(const XentShape& s, const Layout& l, Carver& c) {
-        tiles = 0;
-        if (few_rows(s)) tiles = cut(s.V, kFewWords);
-        else
-            for (int64_t i = 0; i < l.pieces; ++i) tiles += cut(std::min(l.piece, s.V - i * l.piece), s.N <= 64 ? 64 : 128);
+        const int64_t edge = s.N <= 64 ? 64 : 128;  // the narrowest tiles
+        tiles = few_rows(s) ? cut(s.V, kFewWords) : (l.pieces - 1) * cut(l.sizes[0], edge) + cut(l.sizes[1], edge);
         x = l.packed ? c.take<uint16_t>(s.N * l.ld) : nullptr;
         w = l.packed ? c.take<uint16_t>(std::min(l.piece, s.V) * l.ld) : nullptr;
         part = c.take<float2>(s.N * tiles);
@@ -598,6 +599,11 @@ GemmArgs product_of(const GemmOperand& a, const GemmOperand& b, int64_t K) {
     GemmArgs g{};
     g.a = a, g.b = b, g.K = (int32_t)K;
     return g;
+}
+
+// The logits of a piece of `cols` columns.
+GemmArgs logits_of(const XentShape& s, const Layout& l, int64_t cols) {
+    return product_of(GemmOperand{nullptr, l.ld, s.N}, GemmOperand{nullptr, l.ld, cols}, l.packed ? l.ld : s.D);
 }
 
 // Tiles of 256 x 256 (1.10 PFLOP/s at 8192 x 4096 x 4096) where they fill most of the chip and are more than a few steps long (60 rows
@@ -750,8 +756,7 @@ struct BwdSpace {
         sum = l.pieces > 1 ? c.take<float>(s.N * s.D) : nullptr;
         int64_t most = 0;
         auto floats = [&](const GemmArgs& g, int32_t n) { return n > 1 ? n * g.a.rows * s.D : 0; };
-        for (int64_t v = 0; v < s.V; v += l.piece) {
-            const int64_t cols = std::min(l.piece, s.V - v);
+        for (const int64_t cols : l.sizes) {
             const GemmArgs dw = dw_product<T>(s, l, cols), dx = dx_product<T>(s, l, cols);
             const int32_t dx_splits = across<T>(s) ? splits_for<T, true>(dx) : splits_for<T, false>(dx);
             most = std::max({most, floats(dw, splits_for<T, false>(dw)), floats(dx, dx_splits)});
@@ -827,13 +832,13 @@ hy_status forward(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t s
                                      p.target, f.part, f.zt, s.N, s.V, s.D, f.tiles);
         if (rc != HY_OK) return rc;
     } else {
-        auto with = [&](int64_t v) {
-            return product_of(GemmOperand{nullptr, l.ld, s.N}, GemmOperand{nullptr, l.ld, std::min(l.piece, s.V - v)}, l.packed ? l.ld : s.D);
+        auto tiles = [&](int64_t cols) {
+            const GemmArgs z = logits_of(s, l, cols);
+            return cut(cols, edges_of(logit_tile_for<T>(z)).cols);
         };
-        a.tiles = 0;
-        for (int64_t v = 0; v < s.V; v += l.piece) a.tiles += cut(with(v).b.rows, edges_of(logit_tile_for<T>(with(v))).cols);
+        a.tiles = (l.pieces - 1) * tiles(l.sizes[0]) + tiles(l.sizes[1]);
         for (int64_t v = 0; v < s.V; v += l.piece) {
-            a.g = with(v);
+            a.g = logits_of(s, l, std::min(l.piece, s.V - v));
             hy_status rc = operands<T>(p, s, l, f.x, f.w, v, &a.g.a, &a.g.b, st);
             a.v0 = v;
             if (rc == HY_OK) rc = losses<T>(a, st);
@@ -882,9 +887,8 @@ hy_status backward(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t 
 // last one may be narrower, and take other tiles).
 template <typename T>
 bool served_as(const XentShape& s, const Layout& l, bool backward) {
-    if (l.ld > 64 * 65534 || l.nt > (1 << 22) || l.piece > (1 << 22)) return false;
-    for (const int64_t cols : {std::min(l.piece, s.V), s.V - (l.pieces - 1) * l.piece}) {
-        const GemmArgs z = product_of(GemmOperand{nullptr, l.ld, s.N}, GemmOperand{nullptr, l.ld, cols}, l.packed ? l.ld : s.D);
+    for (const int64_t cols : l.sizes) {
+        const GemmArgs z = logits_of(s, l, cols);
         if (!launchable(z, logit_tile_for<T>(z))) return false;
         if (!backward) continue;
         const GemmArgs dw = dw_product<T>(s, l, cols), dx = dx_product<T>(s, l, cols);
@@ -893,12 +897,15 @@ bool served_as(const XentShape& s, const Layout& l, bool backward) {
     }
     return true;
 }
-bool served(const XentShape& s, bool backward) {
+
+}  // namespace
+
+bool xent_served(const XentShape& s, bool backward) {
+    constexpr int64_t kMost = 64 * 65533;  // (a row of workgroups more in turn_kernel's grid)
+    if (s.N > kMost || s.D > kMost) return false;
     const Layout l = layout_of(s);
     return s.dtype == HY_F32 ? served_as<F32>(s, l, backward) : served_as<BF16>(s, l, backward);
 }
-
-}  // namespace
 
 int64_t xent_fwd_workspace_bytes(const XentShape& s) {
     const Layout l = layout_of(s);
@@ -916,7 +923,6 @@ int64_t xent_bwd_workspace_bytes(const XentShape& s) {
 }
 
 hy_status launch_xent_fwd(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t st) {
-    if (!served(s, false)) return HY_ERR_UNSUPPORTED;
     return s.dtype == HY_F32 ? forward<F32>(p, s, ws, st) : forward<BF16>(p, s, ws, st);
 }
 
@@ -925,7 +931,6 @@ hy_status launch_xent_bwd(const XentPtrs& p, const XentShape& s, void* ws, hipSt
         const int64_t bytes = s.V * s.D * (s.dtype == HY_F32 ? 4 : 2);
         return launch_kernel(zero_kernel, dim3(workgroups_for(bytes, 512, 256)), dim3(256), st, (char*)p.dw, bytes);
     }
-    if (!served(s, true)) return HY_ERR_UNSUPPORTED;
     return s.dtype == HY_F32 ? backward<F32>(p, s, ws, st) : backward<BF16>(p, s, ws, st);
 }
 

@@ -1,6 +1,7 @@
 """Host-only checks of the sizes that the entry points around the mixers refuse: what HIP cannot launch (2^32 threads and more)
 is refused as unsupported before anything is enqueued."""
 import ctypes
+import time
 
 import pytest
 
@@ -60,3 +61,41 @@ def test_adamw_of_too_many_chunks():
     rows[0].count = 4096 * ((1 << 24) - 1)
     assert binding.lib().hyena_adamw_table_bytes(rows, 1) > 0
     assert binding.lib().hyena_adamw_step(P[0], 1, 1 << 24, 0, 0, 32, 0, 1e-3, 0.9, 0.95, 1e-8, 1, None, None) == 2
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_a_vocabulary_of_any_size_is_sized_at_once(dtype):
+    """Two sizes of pieces occur, however many pieces there are: 2^49 words take no longer than 2^20."""
+    lb = binding.lib()
+    sizes = (lb.hyena_xent_fwd_workspace_bytes, lb.hyena_xent_bwd_workspace_bytes)
+    for N, D in ((64, 8), (1000, 8), (8, 7), (1, 1)):
+        begin = time.perf_counter()
+        for size in sizes:
+            assert size(N, 1 << 48, D, dtype) > 0
+            size(N, (1 << 49) + 12345, D, dtype)
+        assert time.perf_counter() - begin < 0.05
+    for size in sizes:  # what cannot be launched has no size
+        assert size(1 << 23, 10, 64, dtype) == -1 == size(10, 10, 1 << 23, dtype) and size(1 << 60, 1, 1, dtype) == -1
+        assert size(1, 1, 1 << 60, dtype) == -1
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("N,V,D", [(64, 5000, 64), (65, 70000, 1000), (300, 33001, 999), (4000, 1 << 20, 512), (1 << 20, 1500, 64), (1 << 20, 2100, 72),
+                                   (131072, 1024, 64), (131072, 1025, 64), (8192, 65536, 4096), (2, (1 << 23) + 5, 8)])
+def test_the_workspace_of_a_call_is_what_its_kernels_were_given_before(N, V, D, dtype):
+    """Against sums piece by piece, written out here from what a call keeps: at least the pairs of a row's tiles, the targets' values and
+    the copies of rows that do not begin where 16 bytes do."""
+    lb = binding.lib()
+    e, packed = 4 if dtype == 0 else 2, dtype == 1 and D % 8 != 0
+    up = lambda n, to: -(-n // to) * to  # noqa: E731
+    most = min(max(1024, (512 << 20) // (2 * e * up(N, 64)) // 256 * 256), 1 << 22)
+    piece = min(up(-(-V // -(-V // most)), 256), up(V, 64))
+    cols = [min(piece, V - v) for v in range(0, V, piece)]
+    if dtype == 0 and N <= 32 and D % 4 == 0:
+        tiles = -(-V // 64)
+    else:
+        tiles = sum(-(-c // (64 if N <= 64 else 128)) for c in cols)
+    need = up(N * tiles * 8, 256) + up(N * 4, 256)
+    if packed:
+        need += up(N * up(D, 64) * 2, 256) + up(min(piece, V) * up(D, 64) * 2, 256)
+    assert lb.hyena_xent_fwd_workspace_bytes(N, V, D, dtype) == need
