@@ -327,9 +327,10 @@ __global__ __launch_bounds__(256) void join_kernel(const float2* part, const flo
     }
     for (int d = 32; d > 0; d /= 2) sum += __shfl_xor(sum, d, kWave);
     if (lane == 0) {
-        const float all = ref + logf(sum);
-        lse[m] = all;
-        loss[m] = target[m] >= 0 && target[m] < V ? all - zt[m] : 0.0f;
+        const float rest = logf(sum);
+        lse[m] = ref + rest;
+        // (lse less the target's value would lose what is small beside the largest value)
+        loss[m] = target[m] >= 0 && target[m] < V ? (ref - zt[m]) + rest : 0.0f;
     }
 }
 

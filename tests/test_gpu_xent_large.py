@@ -31,3 +31,17 @@ def test_rows_that_are_copied_and_have_more_than_2_to_the_32_numbers():
         end = 2.0 ** -20 * (1 + np.abs(rs).max())
         assert np.abs(lse[at:at + 100].double().cpu().numpy() - rs).max() <= dz + end
         assert np.abs(loss[at:at + 100].double().cpu().numpy() - rl).max() <= 2 * dz + end
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N,V,at", [(3, 5, 2), (200, 300, 290), (40, 300, 3)])
+def test_losses_that_are_small_beside_their_logits(N, V, at, dtype):
+    """A target at 40, four words at 25, the others at -40: the loss is log(1 + 4 e^-15), 1.2e-6, where numbers of 40 are 3.8e-6
+    apart.  Four additions to 1, the logarithm and the joins of tiles: 8 roundings of 2^-24 at the most.  (All products are exact.)"""
+    x = torch.ones(N, 64, device="cuda", dtype=dtype)
+    w = torch.full((V, 64), -0.625, device="cuda", dtype=dtype)
+    w[at] = 0.625
+    w[[(at + i) % V for i in range(1, 5)]] = 0.390625
+    loss, lse = hy.hyena_xent_fwd(x, w, torch.full((N,), at, device="cuda"))
+    assert (lse == 40).all()
+    assert (loss.double() - np.log1p(4 * np.exp(-15.0))).abs().max() <= 8 * 2.0 ** -24
