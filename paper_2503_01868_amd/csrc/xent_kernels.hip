@@ -166,13 +166,14 @@ __global__ __launch_bounds__(MW * NW * kWave) void loss_kernel(XentArgs a) {
     int64_t m0, n0;
     uint32_t tn;
     tile_of<BM, BN>(a.g, blockIdx.x, &m0, &n0, &tn);
+    const int cols = a.g.b.rows - n0 < BN ? (int)(a.g.b.rows - n0) : BN;  // of the piece: behind it are the next one's targets
     for (int row = threadIdx.x; row < BM; row += G::kThreads)
-        wants[row] = m0 + row < a.g.a.rows ? column_of(a.target[m0 + row], a.v0 + n0, BN) : -1;
+        wants[row] = m0 + row < a.g.a.rows ? column_of(a.target[m0 + row], a.v0 + n0, cols) : -1;
     t.run(lds, a.g, m0, n0, 0, (a.g.K + G::kStep - 1) / G::kStep);
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const int wm = w % MW, wn = w / MW, li = lane % 16, lq = lane / 16;
     float2(*share)[NW] = reinterpret_cast<float2(*)[NW]>(lds);
-    const int cols = a.g.b.rows - n0 < BN ? (int)(a.g.b.rows - n0) : BN, col0 = wn * G::WN + 4 * lq;
+    const int col0 = wn * G::WN + 4 * lq;
     __syncthreads();  // the tiles have been read
 #pragma unroll
     for (int i = 0; i < G::MI; ++i) {

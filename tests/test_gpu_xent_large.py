@@ -45,3 +45,60 @@ def test_losses_that_are_small_beside_their_logits(N, V, at, dtype):
     loss, lse = hy.hyena_xent_fwd(x, w, torch.full((N,), at, device="cuda"))
     assert (lse == 40).all()
     assert (loss.double() - np.log1p(4 * np.exp(-15.0))).abs().max() <= 8 * 2.0 ** -24
+
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def make(seed, N, V, D, dtype, ignored=0.2):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    x = torch.randn(N, D, generator=gen, device="cuda").to(DTYPES[dtype])
+    w = (torch.randn(V, D, generator=gen, device="cuda") * 2 / np.sqrt(D)).to(DTYPES[dtype])
+    target = torch.randint(0, V, (N,), generator=gen, device="cuda")
+    out = torch.rand(N, generator=gen, device="cuda") < ignored
+    target = torch.where(out, torch.tensor([-100, -1, V, 1 << 40], device="cuda")[target % 4], target)
+    dloss = (0.5 + torch.rand(N, generator=gen, device="cuda")) / N
+    return x, w, target, dloss
+
+
+def check(x, w, target, dloss, dtype):
+    """Losses and gradients against their definition in 64 bits.  A logit is a fp32 sum of D products: 4 sqrt(D) roundings of 2^-24
+    of the sum of magnitudes; exp, log and the sum over V: 2^-20.  An element of P is off by its parts times the logits' error,
+    and by its own rounding where it becomes bf16; its products by 4 sqrt(k) roundings and the result's own."""
+    D, V = x.shape[1], w.shape[0]
+    X, W, d = x.double(), w.double(), dloss.double()
+    z = X @ W.t().contiguous()
+    rs = torch.logsumexp(z, 1)
+    counts = (target >= 0) & (target < V)
+    rows = torch.nonzero(counts)[:, 0]
+    rl = torch.zeros_like(rs)
+    rl[rows] = rs[rows] - z[rows, target[rows]]
+    dz = float(4 * np.sqrt(D) * 2.0 ** -24 * (X.abs() @ W.abs().t().contiguous()).max())
+    end = float(2.0 ** -20 * (1 + rs.abs().max()))
+    loss, lse = hy.hyena_xent_fwd(x, w, target)
+    assert (lse.double() - rs).abs().max() <= dz + end
+    assert (loss.double() - rl).abs().max() <= 2 * dz + end and (loss[~counts] == 0).all()
+    dx, dw = hy.hyena_xent_bwd(dloss, x, w, target, lse)
+    p = torch.exp(z - rs[:, None]) * torch.where(counts, d, 0.0)[:, None]
+    del z
+    one = torch.zeros_like(p)
+    one[rows, target[rows]] = d[rows]
+    off = 2 * dz + 2.0 ** -20 + 4 * np.sqrt(max(x.shape[0], V)) * 2.0 ** -24 + (2.0 ** -8 if dtype == "bf16" else 0.0)
+    own = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -22
+    for name, got, ref, mass in (("dx", dx, (p - one) @ W, (p + one) @ W.abs()),
+                                 ("dw", dw, (p - one).t().contiguous() @ X, (p + one).t().contiguous() @ X.abs())):
+        assert torch.isfinite(got).all(), name
+        worst = float(((got.double() - ref).abs() - (off * mass + own * ref.abs() + 1e-30)).max())
+        assert worst <= 0, (name, worst)
+    assert (dx[~counts] == 0).all()
+
+
+@pytest.mark.parametrize("D", [40, 37])
+def test_float_pieces_that_end_inside_a_tile(D):
+    """Tiles of 192 columns over pieces of 2048: the first piece's last tile ends among the next one's targets."""
+    N, V = 20481, 3900
+    say("xent f32 in pieces %d x %d x %d" % (N, V, D))
+    x, w, target, dloss = make(3, N, V, D, "f32")
+    target[::3] = 2040 + torch.arange(len(target[::3]), device="cuda") % 160
+    check(x, w, target, dloss, "f32")
