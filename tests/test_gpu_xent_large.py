@@ -102,3 +102,29 @@ def test_float_pieces_that_end_inside_a_tile(D):
     x, w, target, dloss = make(3, N, V, D, "f32")
     target[::3] = 2040 + torch.arange(len(target[::3]), device="cuda") % 160
     check(x, w, target, dloss, "f32")
+
+
+@pytest.mark.parametrize("N,V,D", [(3553, 3601, 3592), (1024, 17000, 2048), (200, 33000, 1024), (4099, 8191, 4104)])
+def test_tiles_of_256(N, V, D):
+    """Logits, P in both orders and both products in tiles of 256 x 256, ragged in every direction (and calls of few rows for their
+    weights, which take some of them)."""
+    say("xent bf16 %d x %d x %d" % (N, V, D))
+    check(*make(N + V + D, N, V, D, "bf16"), "bf16")
+
+
+@pytest.mark.parametrize("N,V,D,dtype", [(65600, 2500, 65, "bf16"), (40, 2200000, 16, "bf16"), (40, 2200000, 9, "bf16"), (33, 1100000, 12, "f32"),
+                                         (20, 1100000, 12, "f32"), (9000, 16000, 72, "bf16"), (16000, 9100, 520, "bf16")])
+def test_vocabularies_in_pieces(N, V, D, dtype):
+    """Rows that are copied, few rows against millions of words, and pieces of large tiles."""
+    say("xent %s in pieces %d x %d x %d" % (dtype, N, V, D))
+    check(*make(N + V + D, N, V, D, dtype), dtype)
+
+
+def test_losses_alone_of_every_tile_agree_with_each_other():
+    """The losses of some rows, in a call of them alone and among others: the same numbers but for the order of the sums over V."""
+    x, w, target, _ = make(9, 2000, 6000, 512, "bf16", ignored=0.0)
+    loss, lse = hy.hyena_xent_fwd(x, w, target)
+    bound = 2.0 ** -20 * (1 + float(lse.abs().max())) + 8 * np.sqrt(512) * 2.0 ** -24 * float((x[:1].float().abs() @ w.float().abs().t()).max())
+    for rows in (1, 30, 60, 100, 300):
+        some = hy.hyena_xent_fwd(x[:rows], w, target[:rows])
+        assert (some[0] - loss[:rows]).abs().max() <= bound and (some[1] - lse[:rows]).abs().max() <= bound
