@@ -13,7 +13,7 @@ using namespace hy;
 
 namespace {
 
-constexpr int64_t kMostElements = INT64_C(1) << 60;  // of one tensor, gaps between its rows included
+constexpr int64_t kMostElements = INT64_C(1) << 56;  // of one tensor, gaps between its rows included: no sum of bytes passes 63 bits
 
 bool known(int32_t dtype) { return dtype == HY_F32 || dtype == HY_BF16; }
 
@@ -25,7 +25,9 @@ bool fits(int64_t a, int64_t b, int64_t c) {
 }
 
 hy_status check_glr(int64_t B, int64_t L, int64_t D, int32_t group, int32_t dtype) {
-    if (B < 0 || L < 0 || D < 0 || group < 1 || D % group != 0 || !fits(B, L + 1, D)) return HY_ERR_SHAPE;
+    if (B < 0 || L < 0 || D < 0 || group < 1 || D % group != 0 || L > kMostElements) return HY_ERR_SHAPE;
+    // (also of what is empty: strides are computed all the same)
+    if (!fits(std::max<int64_t>(B, 1), L + 1, std::max<int64_t>(D, 1))) return HY_ERR_SHAPE;
     return known(dtype) ? HY_OK : HY_ERR_DTYPE;
 }
 
@@ -79,7 +81,7 @@ int64_t marks_bytes(const GlrShape& s) { return s.B * ((s.L + kGlrRows - 1) / kG
 // ---- cross entropy
 
 hy_status check_xent(int64_t N, int64_t V, int64_t D, int32_t dtype) {
-    if (N < 0 || V < 1 || D < 1 || !fits(N, D, 1) || !fits(V, D, 1) || !fits(N, V, 1)) return HY_ERR_SHAPE;
+    if (N < 0 || V < 1 || D < 1 || !fits(std::max<int64_t>(N, 1), D, 1) || !fits(V, D, 1) || !fits(N, V, 1)) return HY_ERR_SHAPE;
     return known(dtype) ? HY_OK : HY_ERR_DTYPE;
 }
 
@@ -91,14 +93,14 @@ int64_t chunks_of(int64_t count) { return (count + kAdamwChunk - 1) / kAdamwChun
 
 // The chunks of all tensors; -1: not a valid problem.
 int64_t adamw_chunks(const hy_adamw_tensor* t, int64_t n) {
-    if (n < 0 || (n > 0 && !t)) return -1;
+    if (n < 0 || n > INT32_MAX || (n > 0 && !t)) return -1;
     int64_t all = 0;
     for (int64_t i = 0; i < n; ++i) {
         if (t[i].count < 0 || t[i].count > kMostElements) return -1;
         all += chunks_of(t[i].count);
         if (all > kMostChunks) return -1;
     }
-    return n > INT32_MAX ? -1 : all;
+    return all;
 }
 
 struct Span {
@@ -250,7 +252,7 @@ hy_status hyena_adamw_step(const void* table, int64_t n_tensors, int64_t chunks,
                            const float* grad_scale, void* hip_stream) {
     hy_status rc = check_adamw_kinds(param, grad, bits, with_master);
     if (rc != HY_OK) return rc;
-    if (n_tensors < 0 || chunks < 0 || chunks > kMostChunks || (n_tensors == 0 && chunks > 0)) return HY_ERR_SHAPE;
+    if (n_tensors < 0 || n_tensors > INT32_MAX || chunks < 0 || chunks > kMostChunks || (n_tensors == 0 && chunks > 0)) return HY_ERR_SHAPE;
     if (step < 1 || !(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1) || !(eps >= 0)) return HY_ERR_SHAPE;
     if (chunks == 0) return HY_OK;
     if (!table) return HY_ERR_NULL;

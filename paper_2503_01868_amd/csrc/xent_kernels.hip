@@ -570,11 +570,12 @@ Layout layout_of(const XentShape& s) {
 
 // Pieces of the workspace, in order.
 struct Carver {
-    char* at;
+    uintptr_t at;  // (a number: sizes are found without a workspace)
+    explicit Carver(void* ws) : at(reinterpret_cast<uintptr_t>(ws)) {}
     template <typename T>
     T* take(int64_t n) {
-        char* p = at;
-        at += up(n * (int64_t)sizeof(T), 256);
+        const uintptr_t p = at;
+        at += (uintptr_t)up(n * (int64_t)sizeof(T), 256);
         return reinterpret_cast<T*>(p);
     }
 };
@@ -823,7 +824,7 @@ hy_status operands(const XentPtrs& p, const XentShape& s, const Layout& l, uint1
 template <typename T>
 hy_status forward(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t st) {
     const Layout l = layout_of(s);
-    Carver c{static_cast<char*>(ws)};
+    Carver c(ws);
     FwdSpace f(s, l, c);
     XentArgs a{};
     a.target = p.target, a.V = s.V;
@@ -855,7 +856,7 @@ hy_status forward(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t s
 template <typename T>
 hy_status backward(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t st) {
     const Layout l = layout_of(s);
-    Carver c{static_cast<char*>(ws)};
+    Carver c(ws);
     BwdSpace<T> b(s, l, c);
     const float* unit = T::kBytes == 2 ? b.unit : nullptr;
     hy_status rc = turn<T>(p.x, b.xt, s.N, s.D, l.nt, p.target, s.V, Unit{p.dloss, T::kBytes == 2 ? b.unit : nullptr}, st);
@@ -911,17 +912,17 @@ bool xent_served(const XentShape& s, bool backward) {
 
 int64_t xent_fwd_workspace_bytes(const XentShape& s) {
     const Layout l = layout_of(s);
-    Carver c{nullptr};
+    Carver c(nullptr);
     FwdSpace f(s, l, c);
-    return c.at - (char*)nullptr;
+    return (int64_t)c.at;
 }
 
 int64_t xent_bwd_workspace_bytes(const XentShape& s) {
     const Layout l = layout_of(s);
-    Carver c{nullptr};
+    Carver c(nullptr);
     if (s.dtype == HY_F32) BwdSpace<F32>(s, l, c);
     else BwdSpace<BF16>(s, l, c);
-    return c.at - (char*)nullptr;
+    return (int64_t)c.at;
 }
 
 hy_status launch_xent_fwd(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t st) {
