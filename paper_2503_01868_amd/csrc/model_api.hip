@@ -81,7 +81,8 @@ int64_t marks_bytes(const GlrShape& s) { return s.B * ((s.L + kGlrRows - 1) / kG
 // ---- cross entropy
 
 hy_status check_xent(int64_t N, int64_t V, int64_t D, int32_t dtype) {
-    if (N < 0 || V < 1 || D < 1 || !fits(std::max<int64_t>(N, 1), D, 1) || !fits(V, D, 1) || !fits(N, V, 1)) return HY_ERR_SHAPE;
+    if (N < 0 || V < 1 || D < 1 || !fits(std::max<int64_t>(N, 1), D, 1) || !fits(V, D, 1)) return HY_ERR_SHAPE;
+    if (N > (INT64_C(1) << 60) / V) return HY_ERR_SHAPE;  // (logits: a pair is kept of 64 of them)
     return known(dtype) ? HY_OK : HY_ERR_DTYPE;
 }
 
