@@ -439,7 +439,9 @@ hy_status hyena_glr_step(const void *q, const void *k, const void *v, const void
  *     lse[n] = log sum_v exp(z[n,v]),   loss[n] = lse[n] - z[n,target[n]],   z[n,v] = sum_d x[n,d] w[v,d]
  * x: [N,D], w: [V,D], dense, of `dtype`; target: int64 [N]; loss, lse: fp32 [N].  A row whose target is outside 0 .. V - 1 takes no
  * part: its loss is 0 (its lse is written all the same).  The products run on the bf16 matrix cores with fp32 sums: bf16
- * operands as they are, fp32 operands as three bf16 parts each, to fp32's precision.
+ * operands as they are, fp32 operands as three bf16 parts each, to fp32's precision (of numbers below 2^-110 lower parts may be
+ * lost; an infinity makes infinities or NaN of its logits).  The exponentials are the hardware's power of two of a rounded
+ * product, which may cost lse some 1e-7 beside its own rounding; a loss that is small beside its logits keeps its bits.
  * V, D >= 1 (HY_ERR_SHAPE); N = 0 is an empty problem; N and D up to 4194112 (HY_ERR_UNSUPPORTED).
  * workspace: hyena_xent_fwd_workspace_bytes(...) bytes (-1, here and below: not a valid problem, or sizes not served).
  */
@@ -452,7 +454,8 @@ int64_t hyena_xent_fwd_workspace_bytes(int64_t N, int64_t V, int64_t D, int32_t 
  *     P[n,v] = dloss[n] * (exp(z[n,v] - lse[n]) - [v = target[n]]),   dx = P W,   dw = P^T x
  * dx: [N,D], dw: [V,D], of `dtype`, overwritten; zeros in dx for rows that take no part, and nothing in dw from them, whatever
  * they hold.  P is rounded to bf16 for its two products in bf16 calls, in units of the largest |dloss| (a constant weight such as
- * 1 / N costs no rounding), and kept in fp32 in fp32 calls; sums are fp32, in a fixed order, one rounding per stored
+ * 1 / N costs no rounding; a probability is off by 2^-9 of itself, which a caller who needs more of spares with fp32 copies of x and
+ * w), and kept in fp32 in fp32 calls; sums are fp32, in a fixed order, one rounding per stored
  * element.  The vocabulary is taken in pieces: workspace (hyena_xent_bwd_workspace_bytes(...) bytes) holds P of one piece.
  * N D and V D up to 2^35 are served (HY_ERR_UNSUPPORTED).
  */

@@ -69,7 +69,8 @@ __device__ __forceinline__ float times0(float x, float y) { return glr_fmul_lega
 // The decay of two stretches, as logarithms.
 __device__ __forceinline__ float both(float G, float H) { return G == -INFINITY || H == -INFINITY ? -INFINITY : G + H; }
 
-// R of a stretch.  No product of decays that is not zero becomes zero (or forgets NaN): below 2^-245 it may as well be 2^-245.
+// R of a stretch: the power of two of a rounded product, in fp32 calls too (off by 6e-8 (2 + |G|) of itself; where G is far below zero,
+// that is little of a state).  No product of decays that is not zero becomes zero (or forgets NaN): below 2^-245 it may as well be 2^-245.
 __device__ __forceinline__ float root_of(float G) {
     const float r = __builtin_amdgcn_exp2f((G < -170.0f ? -170.0f : G) * 0.72134752f);
     return G == -INFINITY ? 0.0f : r;
@@ -113,8 +114,9 @@ struct Io {
             logs.dead[i] = logs.dead[i] || (there && a[i] == 0.0f);
         }
     }
-    // exp(g).  fp32 calls take the full function; for bf16 calls the power of two of the rounded product is enough (6e-8 times
-    // 1 + |g| of a) and a tenth of the instructions: with the full function the vector ALUs were what bounded the kernels.
+    // exp(g) of a step (stretches: root_of).  fp32 calls take the full function; for bf16 calls the power of two of the rounded
+    // product is enough (6e-8 times 1 + |g| of a) and a tenth of the instructions: with the full function the vector ALUs were what
+    // bounded the kernels.
     static __device__ __forceinline__ float decay(float g) {
         if constexpr (T::kBytes == 4) return expf(g);
         return __builtin_amdgcn_exp2f(g * 1.44269504f);
@@ -493,7 +495,8 @@ __global__ __launch_bounds__(256) void glr_hand_on_kernel(const float* in, float
 }
 
 // Y: q comes in and y goes out; else the states alone.  Bound by the bytes, and by the wait for the edge in launches of a few rounds:
-// 8192 x 4096 bf16 74 us (4.5 TB/s; 63 if nothing waited), 131072 x 1024 262 us (4.6), 3 x 5003 x 1000 fp32 60 us (5.0).
+// 8192 x 4096 bf16 76 us (4.4 TB/s of its tensors), 131072 x 1024 with a gate for 16 channels 265 us (4.1; the looks for the edge read
+// 100 MB beside the inputs' 822), 3 x 5003 x 1000 fp32 61 us (4.1; rows of 4000 bytes end inside lines, a quarter is read twice).
 template <typename T, int VEC, bool SHARED, bool Y>
 __global__ __launch_bounds__(kWaves * kWave, 4) void glr_fwd_kernel(GlrArgs a) {
     using P = Pack<T, VEC>;
@@ -552,8 +555,8 @@ __device__ __forceinline__ float sum_of_neighbours(float x, int lanes) {
 }
 
 // dq, dk, dv, dg of every tile from the state before it and the gradient behind it.  Two channels a lane: with four the rows that are
-// held spill.  8192 x 4096 bf16 120 us (5.1 TB/s of 617 MB), 131072 x 1024 with a gate for 16 channels 508 us (4.1; vector instructions
-// fill 48% of it).
+// held spill.  8192 x 4096 bf16 124 us (5.0 TB/s of 617 MB), 131072 x 1024 with a gate for 16 channels 520 us (3.7 TB/s of its tensors; the
+// looks for the edge read 145 MB beside the inputs' 1099, and vector instructions fill half of it).
 template <typename T, int VEC, bool SHARED>
 __global__ __launch_bounds__(kWaves * kWave, 4) void glr_bwd_kernel(GlrArgs a) {
     using P = Pack<T, VEC>;

@@ -177,7 +177,8 @@ struct Gemm {
 };
 
 // The parts of an fp32 number, each in the upper half of a word: cut, not rounded, so that no part overflows.  All of an infinity
-// is in the first part; a NaN is one in the second.
+// is in the first part; a NaN is one in the second.  (An infinity meets the lower parts of the other factor too, and makes NaN where
+// one of them is zero, that is, where 16 bits hold the factor.)
 __device__ __forceinline__ void parts_of(float x, uint32_t (&part)[3]) {
     constexpr int kInfinite = 0x204;  // of either sign
     part[0] = __float_as_uint(x);

@@ -82,8 +82,8 @@ def test_a_vocabulary_of_any_size_is_sized_at_once(dtype):
 @pytest.mark.parametrize("dtype", [0, 1])
 @pytest.mark.parametrize("N,V,D", [(64, 5000, 64), (65, 70000, 1000), (300, 33001, 999), (4000, 1 << 20, 512), (1 << 20, 1500, 64), (1 << 20, 2100, 72),
                                    (131072, 1024, 64), (131072, 1025, 64), (8192, 65536, 4096), (2, (1 << 23) + 5, 8)])
-def test_the_workspace_of_a_call_is_what_its_kernels_were_given_before(N, V, D, dtype):
-    """Against sums piece by piece, written out here from what a call keeps: at least the pairs of a row's tiles, the targets' values and
+def test_the_workspace_holds_pairs_targets_and_copies(N, V, D, dtype):
+    """Against sums piece by piece, written out here from what a call keeps: the pairs of a row's tiles, the targets' values and
     the copies of rows that do not begin where 16 bytes do."""
     lb = binding.lib()
     e, packed = 4 if dtype == 0 else 2, dtype == 1 and D % 8 != 0
