@@ -503,6 +503,114 @@ hy_status hyena_adamw_step(const void *table, int64_t n_tensors, int64_t chunks,
                            const float *grad_scale, void *hip_stream);
 
 /*
+ * Linear attention with a decay for each head: a memory of dk x dv numbers per head whose decay is data,
+ *     S[b,t,h] = a[b,t,h] S[b,t-1,h] + k[b,t,h']^T v[b,t,h],   a = exp(g[b,t,h]),   h' = h / group,
+ *     y[b,t,h] = scale * q[b,t,h'] S[b,t,h]
+ * with S[b,-1,h] = state_in[b,h] (NULL: zero).  `group` heads of v and g share a head of q and k.  g is the logarithm of the
+ * decay; below about -87, where exp(g) is zero, it forgets everything before its step, infinities and NaN included (the first
+ * step of a document in a packed sequence; every gradient through it is zero).  g > 0 grows, and a product of decays and states
+ * overflows where it passes fp32's range.
+ * q, k: [B,L,H/group,dk], v, y: [B,L,H,dv], g: [B,L,H], of `dtype`; state_in, state_out: fp32 [B,H,dk,dv], the state after the
+ * last step (NULL: not wanted; an empty sequence hands state_in on).
+ * Steps are taken in chunks: inside one, products of q, k, v on the matrix cores, between them the states.  States, decays and
+ * every sum are fp32 and y is rounded once; in bf16 calls the products of q and k inside a chunk, with their decays, and the
+ * states are rounded to bf16 where they are multiplied (not where they are kept), in fp32 calls nothing is.
+ * marks (NULL: not wanted): hyena_la_marks_bytes(...) bytes of states for hyena_la_bwd, in the order and type of its own (a
+ * copy of them is as good).
+ * strides: NULL where q, k, v, g are dense, else host memory with distances in elements, {batch, step, head} of q, k and v and
+ * {batch, step} of g: {q_batch, q_step, q_head, k_batch, ..., v_head, g_batch, g_step} (channels, and heads of g, are
+ * contiguous; 0 repeats; negative: HY_ERR_SHAPE).  Outputs are dense.  q, k, v, g may begin at any element, every other pointer
+ * is 16-byte aligned; where a size is zero the pointers to what is empty may be NULL.
+ * workspace: hyena_la_fwd_workspace_bytes(...) bytes, disjoint from every argument, contents undefined afterwards.
+ * dk, dv >= 1 (HY_ERR_SHAPE); dk up to 128 and B H ceil(dv / 64) ceil(L / 64) below 2^23 are served (else HY_ERR_UNSUPPORTED; the
+ * sizes' queries return -1).
+ */
+hy_status hyena_la_fwd(const void *q, const void *k, const void *v, const void *g, const float *state_in, void *y,
+                       float *state_out, void *marks, const int64_t *strides, void *workspace, int64_t workspace_bytes,
+                       int64_t B, int64_t L, int64_t H, int32_t group, int64_t dk, int64_t dv, double scale, int32_t dtype,
+                       void *hip_stream);
+int64_t hyena_la_fwd_workspace_bytes(int64_t B, int64_t L, int64_t H, int32_t group, int64_t dk, int64_t dv, int32_t dtype);
+int64_t hyena_la_marks_bytes(int64_t B, int64_t L, int64_t H, int32_t group, int64_t dk, int64_t dv, int32_t dtype);
+
+/*
+ * Backward of hyena_la_fwd.  With dy = dLoss/dy, dstate_out = dLoss/d state_out (NULL: zero) and
+ *     M[b,t,h] = scale q[b,t,h']^T dy[b,t,h] + a[b,t+1,h] M[b,t+1,h]      (+ dstate_out[b,h] at the last step):
+ *     dq = scale dy S^T,  dk = v M^T  (each summed over the heads that share a row),  dv = k M,
+ *     dg[b,t,h] = a[b,t,h] <S[b,t-1,h], M[b,t,h]>,   dstate_in[b,h] = a[b,0,h] M[b,0,h]   (NULL: not wanted)
+ * dq, dk: dense [B,L,H/group,dk], dv: dense [B,L,H,dv], dg: dense [B,L,H], of `dtype`; fp32 inside, with bf16 calls' products
+ * rounded as in the forward call; sums in a fixed order, one rounding per stored element.  marks: what the forward call wrote
+ * for the same inputs, or NULL: the states are computed again, from state_in (which is not looked at otherwise).  strides: as
+ * there, with dy in front: {dy_batch, dy_step, dy_head, q_batch, ...}.
+ * workspace: hyena_la_bwd_workspace_bytes(..., marks given or not) bytes.
+ */
+hy_status hyena_la_bwd(const void *dy, const void *q, const void *k, const void *v, const void *g, const void *marks,
+                       const float *state_in, const float *dstate_out, void *dq, void *dk, void *dv, void *dg, float *dstate_in,
+                       const int64_t *strides, void *workspace, int64_t workspace_bytes, int64_t B, int64_t L, int64_t H,
+                       int32_t group, int64_t d_k, int64_t d_v, double scale, int32_t dtype, void *hip_stream);
+int64_t hyena_la_bwd_workspace_bytes(int64_t B, int64_t L, int64_t H, int32_t group, int64_t dk, int64_t dv, int32_t dtype,
+                                     int32_t with_marks);
+
+/*
+ * One step of hyena_la_fwd for B sequences, in place on their states.  q, k: dense [B,H/group,dk], v, y: dense [B,H,dv],
+ * g: dense [B,H], of `dtype`, beginning at any element (y: 16-byte aligned); state: fp32 [B,H,dk,dv].  Nothing is rounded but y.
+ * dk up to 65536, and B H ceil(dv / 32) below 2^23 is served (HY_ERR_UNSUPPORTED).
+ */
+hy_status hyena_la_step(const void *q, const void *k, const void *v, const void *g, float *state, void *y, int64_t B, int64_t H,
+                        int32_t group, int64_t dk, int64_t dv, double scale, int32_t dtype, void *hip_stream);
+
+/*
+ * Root-mean-square norm of rows, after the residual's addition:
+ *     h[n] = x[n] + residual[n] (rounded to `dtype`: the sum that goes on; residual NULL: h = x),
+ *     rstd[n] = 1 / sqrt(sum_d h[n,d]^2 / D + eps),   y[n,d] = h[n,d] * rstd[n] * w[d]   (w NULL: 1)
+ * x, residual, h, y: [N,D], w: [D], of `dtype`; rstd: fp32 [N] (NULL: not wanted).  h: where the sum goes (NULL: not wanted; it
+ * may be x or the residual themselves, of the same rows, in place; only with a residual).  x_stride, r_stride: distances between
+ * rows of x and of the residual in elements (channels are contiguous; 0 repeats a row); h and y are dense, so a sum in place
+ * needs dense rows.
+ * y_scale NULL: y is of `dtype`, rounded once from fp32.  y_scale fp32 [N]: y holds OCP e4m3 numbers, one byte each,
+ *     u = h[n,d] * w[d],   top = max_d |u|,   y = e4m3(u * (448 / top)),   y_scale[n] = top * (1 / 448) * rstd[n],
+ * value = y * y_scale: of u, so that the numbers do not depend on how rstd is rounded.  A row whose top is below 2^-100 is held
+ * as zeros with a scale of zero.  An element of u that is not finite takes no part in top and is held as NaN (and an infinity of
+ * h makes every finite element of its row zero, as rstd is zero).
+ * Sums are fp32, in a fixed order.  Pointers may begin at any element of theirs.  D >= 1 (HY_ERR_SHAPE), up to 2^31 - 1
+ * (HY_ERR_UNSUPPORTED).
+ */
+hy_status hyena_rmsnorm_fwd(const void *x, const void *residual, const void *w, void *y, float *y_scale, void *h, float *rstd,
+                            int64_t N, int64_t D, int64_t x_stride, int64_t r_stride, double eps, int32_t dtype,
+                            void *hip_stream);
+
+/*
+ * Backward of hyena_rmsnorm_fwd (of the 8-bit form too: its rounding passes gradients on).  With dy = dLoss/dy and dh = dLoss/dh
+ * along the residual (NULL: zero), rstd as the forward call wrote it:
+ *     dx[n,d] = dh[n,d] + rstd[n] * (w[d] dy[n,d] - h[n,d] rstd[n]^2 / D sum_e w[e] dy[n,e] h[n,e]),
+ *     dw[d] = sum_n dy[n,d] h[n,d] rstd[n]
+ * dx is the gradient of x and of the residual alike.  dy, h, dh, dx: dense [N,D] (dx may be dh or dy themselves, in place), w, dw:
+ * [D] (both NULL: no weights; dw NULL: not wanted), of `dtype`; fp32 inside, sums in a fixed order, one rounding per stored element.
+ * workspace: hyena_rmsnorm_bwd_workspace_bytes(N, D, dtype) bytes, 16-byte aligned (only looked at where dw is wanted).
+ */
+hy_status hyena_rmsnorm_bwd(const void *dy, const void *h, const float *rstd, const void *w, const void *dh, void *dx, void *dw,
+                            void *workspace, int64_t workspace_bytes, int64_t N, int64_t D, int32_t dtype, void *hip_stream);
+int64_t hyena_rmsnorm_bwd_workspace_bytes(int64_t N, int64_t D, int32_t dtype);
+
+/*
+ * The next token of every row of logits.  With z = logits[n], T = temperature[n] and w[v] = exp((z[v] - max z) / T) in 64 bits:
+ *   1. of all words the top_k[n] largest logits are kept (equal ones: the lowest indexes; top_k < 1 or >= V: all);
+ *   2. of those, in that order, the fewest whose weights add up to at least top_p[n] times the weights of all of step 1 (one at
+ *      least; top_p >= 1: all);
+ *   3. of those, the words with w[v] >= min_p[n] (the likeliest has 1, and always stays);
+ * token[n] = the lowest index v up to which the kept weights' sum is more than u[n] times the sum of all of them (the last kept
+ * word with a weight, should u be 1 or more), prob[n] = w[token] / that sum.  T <= 0: the largest logit, of equal
+ * ones the lowest index, with probability 1.  NaN among the logits count as -infinity.  +infinities share
+ * everything among themselves.  A row of which every logit is -infinity has token -1 and probability 0.
+ * logits: [N,V] of `dtype`, rows `stride` elements apart (words are contiguous; 0 repeats a row), beginning at any element; u: fp32
+ * [N], in [0, 1); temperature, top_p, min_p: fp32 [N], top_k: int32 [N], each NULL for the one value behind it, for every row.  NaN
+ * in them counts as 1 (temperature, top_p) or 0 (min_p, u).  token: int64 [N]; prob: fp32 [N] (NULL: not wanted).
+ * V >= 1 (HY_ERR_SHAPE), up to 2^22, N up to 2^22 (HY_ERR_UNSUPPORTED).
+ */
+hy_status hyena_sample(const void *logits, const float *u, const float *temperature, double temperature_all, const int32_t *top_k,
+                       int32_t top_k_all, const float *top_p, double top_p_all, const float *min_p, double min_p_all,
+                       int64_t *token, float *prob, int64_t N, int64_t V, int64_t stride, int32_t dtype, void *hip_stream);
+
+/*
  * Plain device-to-device streaming copy of `bytes` bytes (a multiple of 16) with the same launch
  * shape as the streaming kernels.  Used to measure the practical HBM ceiling and to calibrate
  * hardware byte counters; not part of the operator.

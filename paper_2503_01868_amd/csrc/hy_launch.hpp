@@ -336,6 +336,64 @@ int64_t xent_bwd_workspace_bytes(const XentShape& s);
 hy_status launch_xent_fwd(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t st);
 hy_status launch_xent_bwd(const XentPtrs& p, const XentShape& s, void* ws, hipStream_t st);
 
+// Linear attention with a decay for each head.  Strides in elements, {batch, step, head} of each input in the order of the kLa
+// constants; outputs are dense.
+constexpr int kLaQ = 0, kLaK = 1, kLaV = 2, kLaG = 3, kLaDy = 4;
+struct LaPtrs {
+    const void *q = nullptr, *k = nullptr, *v = nullptr, *g = nullptr, *dy = nullptr, *marks_in = nullptr;
+    const float *state_in = nullptr, *dstate_out = nullptr;
+    void *y = nullptr, *marks = nullptr, *dq = nullptr, *dk = nullptr, *dv = nullptr, *dg = nullptr;
+    float *state_out = nullptr, *dstate_in = nullptr;
+};
+struct LaShape {
+    int64_t B, L, H;
+    int32_t group;
+    int64_t dk, dv;
+    double scale;
+    hy_dtype dtype;
+    int64_t stride[5][3];
+};
+// Whether the sizes can be launched; the calls below take no others, and none with B, H, dk or dv of zero.
+bool la_served(const LaShape& s);
+int64_t la_marks_bytes(const LaShape& s);
+int64_t la_fwd_workspace_bytes(const LaShape& s);
+int64_t la_bwd_workspace_bytes(const LaShape& s, bool marks);
+hy_status launch_la_fwd(const LaPtrs& p, const LaShape& s, void* ws, hipStream_t st);
+hy_status launch_la_bwd(const LaPtrs& p, const LaShape& s, void* ws, hipStream_t st);
+// One step of B sequences, the states (p.state_out) updated in place; everything dense, L and strides not looked at, any dk.
+hy_status launch_la_step(const LaPtrs& p, const LaShape& s, hipStream_t st);
+
+// Root-mean-square norm of rows.
+struct NormPtrs {
+    const void *x = nullptr, *residual = nullptr, *w = nullptr;
+    void *y = nullptr, *h = nullptr;  // h: backward, an input
+    float *y_scale = nullptr, *rstd = nullptr;
+    const void *dy = nullptr, *dh = nullptr;
+    void *dx = nullptr, *dw = nullptr;
+};
+struct NormShape {
+    int64_t N, D, x_stride, r_stride;
+    double eps;
+    int32_t dtype;
+};
+int64_t norm_bwd_workspace_bytes(int64_t N, int64_t D);
+hy_status launch_norm_fwd(const NormPtrs& p, const NormShape& s, hipStream_t st);
+hy_status launch_norm_bwd(const NormPtrs& p, const NormShape& s, void* ws, hipStream_t st);
+
+// Tokens of rows of logits.
+struct SamplePtrs {
+    const void* logits;
+    const float *u, *temperature, *top_p, *min_p;
+    const int32_t* top_k;
+    int64_t* token;
+    float* prob;
+};
+struct SampleAll {  // what holds for every row where there is no array
+    double temperature, top_p, min_p;
+    int32_t top_k;
+};
+hy_status launch_sample(const SamplePtrs& p, const SampleAll& all, int64_t N, int64_t V, int64_t stride, int32_t dtype, hipStream_t st);
+
 // How many workgroups HIP takes: it counts fewer than 2^32 threads.
 constexpr int64_t most_workgroups(int64_t threads) { return INT64_C(0xffffffff) / threads; }
 // Workgroups for n items, `per` of them each; a kernel that runs over its items in steps of its grid may have fewer.

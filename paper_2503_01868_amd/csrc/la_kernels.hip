@@ -1,0 +1,1234 @@
+// Linear attention with a decay for each head,
+//     S[t] = exp(g[t]) S[t-1] + k[t]^T v[t],   y[t] = scale q[t] S[t],
+// and its gradients.  A chunk of C steps is taken at once: with b the running sum of g inside the chunk and S the state in front,
+//     y_i = scale exp(b_i) q_i S + sum_{j <= i} A_ij v_j,   A_ij = scale exp(b_i - b_j) (q_i . k_j),
+//     S'  = exp(b_C) S + sum_j exp(b_C - b_j) k_j^T v_j,
+// matrix products all of them.  Every factor is the exponential of a difference of sums (held as two floats, made in double), never a
+// quotient of exponentials, so nothing overflows that the states do not.  A decay of zero ends a document: factors across it are
+// zeros by selection, not by multiplication, whatever is on its other side.
+//
+// A workgroup walks chunks in their order with the state in registers (the backward pass in the other order with the state's
+// gradient).  Where heads are too few to fill the card, a sequence is cut into segments: a walk that makes states only, a
+// scan over the segments' ends, and the walk itself.  The state's products take the factor of k or q as three bf16 parts, so that states
+// are sums of fp32 products in bf16 calls too; what is rounded to bf16 is A and the copies of S that are multiplied.
+//
+// A product mixes rows, and a zero times an infinity is none: a chunk that holds anything not finite, or decays above one that
+// would make something so of finite numbers, is taken again a row at a time.
+#include <type_traits>
+
+#include "hy_common.hpp"
+#include "hy_launch.hpp"
+
+namespace hy {
+
+namespace {
+
+typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4_t* lds_quad_t;
+
+constexpr float kForgets = -87.3f;  // exp of less is below the smallest normal number
+constexpr double kLog2E = 1.4426950408889634074;
+constexpr float kMostGrowth = 64.0f;  // bits by which decays above one may grow a state within a chunk that is taken at once
+
+// Factors as exp2(d) = r r, r = exp2(d / 2): growth beyond the range of one factor is left to the products it is in.
+__device__ __forceinline__ float half_factor(float d) {
+    const float x = 0.5f * d;
+    return __builtin_amdgcn_exp2f(x > 127.0f ? 127.0f : x);  // (of NaN: NaN)
+}
+
+// Eight numbers of a row of an operand: k = 8 lq + e of a block of 32 (lane: li = lane % 16, lq = lane / 16), or in the order of
+// accumulators ("turned"), k = 16 (e / 4) + 4 lq + e % 4.  A product's result has in lane (li, lq), register r, row 4 lq + r of its
+// first operand and row li of the second.
+template <typename T>
+struct Frag;
+template <>
+struct Frag<BF16> {
+    bf16x8_t x;
+};
+template <>
+struct Frag<F32> {
+    float x[8];
+};
+
+__device__ __forceinline__ void multiply(f32x4_t& acc, const Frag<BF16>& a, const Frag<BF16>& b) {
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.x, b.x, acc, 0, 0, 0);
+}
+__device__ __forceinline__ void multiply(f32x4_t& acc, const Frag<F32>& a, const Frag<F32>& b) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x[e], b.x[e], acc, 0, 0, 0);
+}
+
+template <typename T>
+using Elem = std::conditional_t<std::is_same_v<T, F32>, float, uint16_t>;
+
+// Steps of a chunk: what LDS holds of them.
+template <typename T>
+constexpr int kChunk = T::kBytes == 2 ? 64 : 32;
+
+// Rows of D numbers in LDS and their distance: 16 bytes more than they take, so that 16 rows at a column spread over the banks.
+template <typename T, int D>
+constexpr int kPitch = D + 16 / T::kBytes;
+
+__device__ __forceinline__ Frag<BF16> frag_of(const float (&f)[8], BF16) {
+    Words<4> w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w.w[i] = pack_bf16x2(f[2 * i], f[2 * i + 1]);
+    return Frag<BF16>{__builtin_bit_cast(bf16x8_t, w)};
+}
+__device__ __forceinline__ Frag<F32> frag_of(const float (&f)[8], F32) {
+    Frag<F32> r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.x[i] = f[i];
+    return r;
+}
+__device__ __forceinline__ void floats_of(const Frag<BF16>& a, float (&f)[8]) {
+    const Words<4> w = __builtin_bit_cast(Words<4>, a.x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[2 * i] = bf16_lo(w.w[i]), f[2 * i + 1] = bf16_hi(w.w[i]);
+}
+__device__ __forceinline__ void floats_of(const Frag<F32>& a, float (&f)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = a.x[i];
+}
+
+// Row `row`, k from `k0`.
+template <int PITCH>
+__device__ __forceinline__ Frag<BF16> row_frag(const uint16_t* t, int row, int k0, int lq) {
+    return Frag<BF16>{*reinterpret_cast<const bf16x8_t*>(t + row * PITCH + k0 + 8 * lq)};
+}
+template <int PITCH>
+__device__ __forceinline__ Frag<F32> row_frag(const float* t, int row, int k0, int lq) {
+    Frag<F32> r;
+    const float4 *p = reinterpret_cast<const float4*>(t + row * PITCH + k0 + 8 * lq), a = p[0], b = p[1];
+    r.x[0] = a.x, r.x[1] = a.y, r.x[2] = a.z, r.x[3] = a.w, r.x[4] = b.x, r.x[5] = b.y, r.x[6] = b.z, r.x[7] = b.w;
+    return r;
+}
+template <int PITCH>
+__device__ __forceinline__ Frag<BF16> turned_row_frag(const uint16_t* t, int row, int k0, int lq) {
+    const uint2 a = *reinterpret_cast<const uint2*>(t + row * PITCH + k0 + 4 * lq), b = *reinterpret_cast<const uint2*>(t + row * PITCH + k0 + 16 + 4 * lq);
+    return Frag<BF16>{__builtin_bit_cast(bf16x8_t, make_uint4(a.x, a.y, b.x, b.y))};
+}
+template <int PITCH>
+__device__ __forceinline__ Frag<F32> turned_row_frag(const float* t, int row, int k0, int lq) {
+    Frag<F32> r;
+    const float4 a = *reinterpret_cast<const float4*>(t + row * PITCH + k0 + 4 * lq), b = *reinterpret_cast<const float4*>(t + row * PITCH + k0 + 16 + 4 * lq);
+    r.x[0] = a.x, r.x[1] = a.y, r.x[2] = a.z, r.x[3] = a.w, r.x[4] = b.x, r.x[5] = b.y, r.x[6] = b.z, r.x[7] = b.w;
+    return r;
+}
+// Columns of a tile as rows of an operand: lane li has column `c0` + li (STEP 4), or c0 + 8 (li / 4) + li % 4 (STEP 8), k = rows from
+// k0 in the plain order.  bf16: LDS turns 4 x 16 numbers at a time; lane l of 16 says where row l / 4 has its columns 4 (l % 4) and
+// gets column l.
+template <int PITCH, int STEP>
+__device__ __forceinline__ Frag<BF16> column_frag(const uint16_t* t, int k0, int c0, int li, int lq) {
+    const uint16_t* p = t + (k0 + 8 * lq + li / 4) * PITCH + c0 + STEP * (li % 4);
+    const s16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_quad_t)p), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_quad_t)(p + 4 * PITCH));
+    const uint2 ua = __builtin_bit_cast(uint2, a), ub = __builtin_bit_cast(uint2, b);
+    return Frag<BF16>{__builtin_bit_cast(bf16x8_t, make_uint4(ua.x, ua.y, ub.x, ub.y))};
+}
+template <int PITCH, int STEP>
+__device__ __forceinline__ Frag<F32> column_frag(const float* t, int k0, int c0, int li, int lq) {
+    const float* p = t + (k0 + 8 * lq) * PITCH + c0 + STEP * (li / 4) + li % 4;
+    Frag<F32> r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r.x[e] = p[e * PITCH];
+    return r;
+}
+
+// Four results next to each other in LDS.
+__device__ __forceinline__ void put4(uint16_t* p, const f32x4_t& v) { *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])); }
+__device__ __forceinline__ void put4(float* p, const f32x4_t& v) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
+
+// acc += first (x) (f as fp32 numbers): of bf16 products f is three parts, which make its 24 bits.
+__device__ __forceinline__ void multiply_wide(f32x4_t& acc, const Frag<BF16>& a, const Frag<BF16> (&f)[3]) {
+    multiply(acc, a, f[2]);
+    multiply(acc, a, f[1]);
+    multiply(acc, a, f[0]);
+}
+__device__ __forceinline__ void multiply_wide(f32x4_t& acc, const Frag<F32>& a, const Frag<F32> (&f)[1]) { multiply(acc, a, f[0]); }
+template <typename T>
+constexpr int kParts = T::kBytes == 2 ? 3 : 1;
+__device__ __forceinline__ void wide_frag(float (&f)[8], Frag<BF16> (&o)[3]) {
+#pragma unroll
+    for (int x = 0; x < 3; ++x) {
+        o[x] = frag_of(f, BF16{});
+        float part[8];
+        floats_of(o[x], part);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = fabsf(part[e]) < INFINITY ? f[e] - part[e] : 0.0f;
+    }
+}
+__device__ __forceinline__ void wide_frag(float (&f)[8], Frag<F32> (&o)[1]) { o[0] = frag_of(f, F32{}); }
+
+// Where a tensor's rows are: [B, L, heads, d], channels contiguous.
+struct Rows {
+    const char* p;
+    int64_t batch, step, head;  // bytes
+    int32_t d, wide;            // wide: 8 numbers from a multiple of 8 on can be moved by 16 bytes
+};
+
+// What a chunk's steps do to a state, in LDS: sums of log2 decays up to and with a step (two floats), the last step up to and with it
+// that forgets (-1: none), and whether the chunk can be taken at once.
+template <int C>
+struct Decays {
+    float hi[C], lo[C];
+    int32_t forgot[C];
+    float from_start[C], to_end[C];  // half factors; zero: none
+    float whole;                     // of the whole chunk
+    double sum;                      // of the whole chunk
+};
+
+// A wave makes them; lane t has step t.  g: its log decay (0 behind the last step).
+template <int C>
+__device__ __forceinline__ void make_decays(Decays<C>& s, float g, int lane, bool& odd) {
+    const bool forgets = g < kForgets, inside = lane < C;
+    odd = !(fabsf(g) < INFINITY) && !forgets;
+    if (__builtin_amdgcn_ballot_w64(g > 0.0f && inside) != 0) {
+        float up = g > 0.0f && inside ? g * (float)kLog2E : 0.0f;
+#pragma unroll
+        for (int d = kWave / 2; d > 0; d /= 2) up += __shfl_xor(up, d, kWave);
+        odd |= up > kMostGrowth;
+    }
+    double b = forgets || !inside ? 0.0 : (double)g * kLog2E;
+#pragma unroll
+    for (int d = 1; d < C; d *= 2) {
+        const double x = __shfl_up(b, d, kWave);
+        if (lane >= d) b += x;
+    }
+    const unsigned long long all = __builtin_amdgcn_ballot_w64(forgets && inside), upto = all & (~0ull >> (63 - lane));
+    const int forgot = upto ? 63 - __builtin_clzll(upto) : -1, last = all ? 63 - __builtin_clzll(all) : -1;
+    const double end = __shfl(b, C - 1, kWave);
+    const float hi = (float)b, lo = hi - hi == 0.0f ? (float)(b - (double)hi) : 0.0f;
+    if (inside) {
+        s.hi[lane] = hi, s.lo[lane] = lo, s.forgot[lane] = forgot;
+        s.from_start[lane] = forgot < 0 ? half_factor((float)b) : 0.0f;
+        s.to_end[lane] = lane >= last ? half_factor((float)(end - b)) : 0.0f;
+    }
+    if (lane == 0) {
+        s.whole = last < 0 ? half_factor((float)end) : 0.0f;
+        s.sum = last < 0 ? end : -INFINITY;
+    }
+}
+__device__ __forceinline__ float scaled(float x, float half) { return half == 0.0f ? 0.0f : x * half * half; }
+
+// Rows [0, n) of a chunk to a tile of C rows, zeros behind them and behind the d-th number; whether all of it is finite.
+template <typename T, int C, int D, int NT>
+__device__ __forceinline__ bool load_tile(Elem<T>* tile, const Rows& x, const char* from, int n, int c0) {
+    constexpr int kPieces = C * D / 8, kEach = (kPieces + NT - 1) / NT, kPerRow = D / 8, W = T::kBytes == 2 ? 4 : 8;
+    uint32_t worst = 0;
+    Words<W> r[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int at = i * NT + (int)threadIdx.x, row = at / kPerRow, c = c0 + at % kPerRow * 8;
+        const char* p = from + row * x.step + (int64_t)c * T::kBytes;
+        r[i] = zero_words<W>();
+        if (row >= n || c >= x.d) continue;  // (n <= C: none behind the tile either)
+        if (x.wide) {
+            const Words<4> a = load_words<4>(p);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r[i].w[j] = a.w[j];
+            if constexpr (W == 8) {
+                const Words<4> b = load_words<4>(p + 16);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) r[i].w[4 + j] = b.w[j];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (c + j >= x.d) continue;
+                if constexpr (W == 8) r[i].w[j] = *reinterpret_cast<const uint32_t*>(p + 4 * j);
+                else r[i].w[j / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + 2 * j) << 16 * (j % 2);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int at = i * NT + (int)threadIdx.x, row = at / kPerRow, c = at % kPerRow * 8;
+        if (kPieces % NT != 0 && at >= kPieces) continue;
+#pragma unroll
+        for (int j = 0; j < W; ++j) {  // the largest exponent
+            worst = max(worst, r[i].w[j] & 0x7fffffffu);
+            if constexpr (W == 4) worst = max(worst, (r[i].w[j] & 0x7fffu) << 16);
+        }
+#pragma unroll
+        for (int j = 0; j < W; j += 4) {
+            const Words<4> o{{r[i].w[j], r[i].w[j + 1], r[i].w[j + 2], r[i].w[j + 3]}};
+            store_words<4>(tile + row * kPitch<T, D> + c + j * (4 / T::kBytes), o);
+        }
+    }
+    return worst < 0x7f800000u;
+}
+
+template <typename T>
+__device__ __forceinline__ float number(const char* p) {
+    float f[1];
+    Pack<T, 1>::unpack(Pack<T, 1>::load(p), f);
+    return f[0];
+}
+
+struct LaArgs {
+    Rows q, k, v, g, dy;  // (g: head is not looked at)
+    const float *state_in, *dstate_out;
+    char *y, *marks, *dv;
+    const char* marks_in;
+    float *state_out, *dstate_in;
+    void *dq, *dk;         // of T, or the heads' shares in fp32
+    void* dg;              // of T, or the tiles' shares in fp32
+    float* ends;           // states (and their gradients) at the segments' ends: [segment][head and tile][DK DV], and their log2 decays
+    double* sums;
+    int64_t L, chunks, each;  // chunks of a segment
+    int32_t H, group, dk_, dv_, tiles, segments, shares;
+    float scale;
+};
+
+// A head, a tile of its columns and a segment: the workgroup's.
+struct Place {
+    int64_t b, item;  // item: (b H + h) tiles + tile
+    int32_t h, hk, tile, segment;
+};
+__device__ __forceinline__ Place place_of(const LaArgs& a, uint32_t i) {
+    Place p;
+    const uint32_t n = (uint32_t)a.segments;
+    p.segment = (int32_t)(i % n);
+    p.item = i / n;
+    p.tile = (int32_t)(p.item % a.tiles);
+    const int64_t bh = p.item / a.tiles;
+    p.h = (int32_t)(bh % a.H);
+    p.b = bh / a.H;
+    p.hk = p.h / a.group;
+    return p;
+}
+
+// The state of a wave: DK rows by 16 CT columns, in 16 x 16 pieces, as results of (rows of k) x (columns of v): lane (li, lq)
+// has column li of piece ct, rows 16 dt + 4 lq + r.  CT = 2: the columns of two pieces are taken in turn, 4 and 4, so that a lane has 8 next
+// to each other in what is made of them.
+template <int DT, int CT>
+struct State {
+    f32x4_t s[DT][CT];
+    static __device__ __forceinline__ int column(int li, int ct) { return CT == 2 ? 8 * (li / 4) + 4 * ct + li % 4 : 16 * ct + li; }
+
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int j = 0; j < CT; ++j) s[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    // from / to [dk][dv] numbers of a head; c0: the wave's first column
+    __device__ __forceinline__ void load(const float* p, int dk, int dv, int c0, int li, int lq) {
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int j = 0; j < CT; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int d = 16 * i + 4 * lq + r, c = c0 + column(li, j);
+                    s[i][j][r] = d < dk && c < dv ? p[(int64_t)d * dv + c] : 0.0f;
+                }
+    }
+    __device__ __forceinline__ void store(float* p, int dk, int dv, int c0, int li, int lq) const {
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int j = 0; j < CT; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int d = 16 * i + 4 * lq + r, c = c0 + column(li, j);
+                    if (d < dk && c < dv) p[(int64_t)d * dv + c] = s[i][j][r];
+                }
+    }
+    // the library's own order: pieces, then lanes
+    __device__ __forceinline__ void load_own(const float* p, int lane) {
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int j = 0; j < CT; ++j) s[i][j] = *reinterpret_cast<const f32x4_t*>(p + ((i * CT + j) * kWave + lane) * 4);
+    }
+    __device__ __forceinline__ void store_own(float* p, int lane) const {
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int j = 0; j < CT; ++j) *reinterpret_cast<f32x4_t*>(p + ((i * CT + j) * kWave + lane) * 4) = s[i][j];
+    }
+    __device__ __forceinline__ void decay(float half) {
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int j = 0; j < CT; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[i][j][r] = scaled(s[i][j][r], half);
+    }
+};
+
+// States as marks: of T, the same order.
+template <typename T>
+__device__ __forceinline__ void store_mark(char* p, const f32x4_t& v) {
+    const float f[4] = {v[0], v[1], v[2], v[3]};
+    Pack<T, 4>::store(p, Pack<T, 4>::pack(f));
+}
+template <typename T>
+__device__ __forceinline__ f32x4_t load_mark(const char* p) {
+    float f[4];
+    Pack<T, 4>::unpack(Pack<T, 4>::load(p), f);
+    return f32x4_t{f[0], f[1], f[2], f[3]};
+}
+
+// s += first^T (x) weighted second over the chunk's rows: rows of `a` become the state's rows, columns of `b` its columns, of which
+// the wave has `mine` in `fb`; `half` are the rows' half factors.
+template <typename T, int DK, int C, int DT, int CT, int KB>
+__device__ __forceinline__ void add_rows(State<DT, CT>& s, const Elem<T>* a, const Frag<T> (&fb)[CT][KB], const float* half, float scale, int li, int lq) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+        Frag<T> parts[CT][kParts<T>];
+#pragma unroll
+        for (int j = 0; j < CT; ++j) {
+            float f[8];
+            floats_of(fb[j][kb], f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = scaled(f[e] * scale, half[32 * kb + 8 * lq + e]);
+            wide_frag(f, parts[j]);
+        }
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+            const Frag<T> fa = column_frag<kPitch<T, DK>, 4>(a, 32 * kb, 16 * i, li, lq);
+#pragma unroll
+            for (int j = 0; j < CT; ++j) multiply_wide(s.s[i][j], fa, parts[j]);
+        }
+    }
+}
+
+// ---- the walk forward: states at the segments' ends (OUT false), or outputs, marks and the last state
+
+template <typename T, int DK, int DV, bool OUT>
+struct WalkLds {
+    static constexpr int C = kChunk<T>;
+    Elem<T> k[C * kPitch<T, DK>], v[C * kPitch<T, DV>];
+    Elem<T> q[OUT ? C * kPitch<T, DK> : 1], a[OUT ? C * kPitch<T, C> : 1];
+    Decays<C> d;
+};
+
+template <typename T, int DK, int DV, bool OUT, bool MARKS>
+__global__ __launch_bounds__(256) void la_walk_kernel(LaArgs a) {
+    constexpr int C = kChunk<T>, NT = 256, NW = 4, IT = C / 16, KB = C / 32, DT = DK / 16, CT = DV / NW / 16, WC = 16 * CT;
+    constexpr int PK = kPitch<T, DK>, PV = kPitch<T, DV>, PA = kPitch<T, C>;
+    __shared__ __attribute__((aligned(16))) WalkLds<T, DK, DV, OUT> s;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, li = lane % 16, lq = lane / 16;
+    const Place at = place_of(a, blockIdx.x);
+    if (!OUT && at.segment == a.segments - 1) return;
+    const char *kp = a.k.p + at.b * a.k.batch + at.hk * a.k.head, *vp = a.v.p + at.b * a.v.batch + at.h * a.v.head;
+    const char *qp = a.q.p + at.b * a.q.batch + at.hk * a.q.head, *gp = a.g.p + at.b * a.g.batch + (int64_t)at.h * T::kBytes;
+    const int c0 = at.tile * DV, cw = w * WC;  // the tile's columns, the wave's in it
+
+    const int64_t bh = at.b * a.H + at.h, head_state = bh * a.dk_ * a.dv_;
+    const int64_t items = (int64_t)gridDim.x / a.segments;
+    State<DT, CT> S;
+    if (at.segment > 0 && OUT) S.load_own(a.ends + ((at.segment - 1) * items + at.item) * (DK * DV) + w * (DK * WC), lane);
+    else if (at.segment == 0 && a.state_in) S.load(a.state_in + head_state, a.dk_, a.dv_, c0 + cw, li, lq);
+    else S.clear();
+    if constexpr (OUT) {  // blocks above the diagonal are read, as zeros
+        for (int i = threadIdx.x; i < C * PA; i += NT) s.a[i] = 0;
+    }
+    const int64_t first = at.segment * a.each, last = first + a.each < a.chunks ? first + a.each : a.chunks;
+    double sum = 0.0;
+
+    // steps [t, t + n) at once; `look`: only if all of them are finite
+    auto take = [&](int64_t t, int n, bool look) -> bool {
+        __syncthreads();  // nobody reads the chunk before any more
+        bool fine = load_tile<T, C, DK, NT>(s.k, a.k, kp + t * a.k.step, n, 0);
+        fine &= load_tile<T, C, DV, NT>(s.v, a.v, vp + t * a.v.step, n, c0);
+        if constexpr (OUT) load_tile<T, C, DK, NT>(s.q, a.q, qp + t * a.q.step, n, 0);
+        if (w == 0) {
+            bool odd;
+            make_decays<C>(s.d, lane < n ? number<T>(gp + (t + lane) * a.g.step) : 0.0f, lane, odd);
+            fine &= !odd;
+        }
+        if (look) {
+            if (__syncthreads_or(!fine)) return false;
+        } else {
+            __syncthreads();
+        }
+        Frag<T> fv[CT][KB];
+#pragma unroll
+        for (int j = 0; j < CT; ++j)
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                if constexpr (CT == 2) fv[j][kb] = column_frag<PV, 8>(s.v, 32 * kb, cw + 4 * j, li, lq);
+                else fv[j][kb] = column_frag<PV, 4>(s.v, 32 * kb, cw + 16 * j, li, lq);
+            }
+        if constexpr (OUT) {
+            // A below the diagonal, a block of 16 x 16 a wave at a time
+            constexpr int kBlocks = IT * (IT + 1) / 2;
+#pragma unroll
+            for (int x = 0; x < (kBlocks + NW - 1) / NW; ++x) {
+                const int block = x * NW + w;
+                if (block >= kBlocks) break;
+                int it = 0;
+                while ((it + 1) * (it + 2) / 2 <= block) ++it;
+                const int jt = block - it * (it + 1) / 2;
+                f32x4_t p = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int kb = 0; kb < DK / 32; ++kb)
+                    multiply(p, row_frag<PK>(s.k, 16 * jt + li, 32 * kb, lq), row_frag<PK>(s.q, 16 * it + li, 32 * kb, lq));
+                const int i = 16 * it + li, j0 = 16 * jt + 4 * lq, forgot = s.d.forgot[i];
+                const float hi = s.d.hi[i], lo = s.d.lo[i];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float half = half_factor((hi - s.d.hi[j0 + r]) + (lo - s.d.lo[j0 + r]));
+                    p[r] = j0 + r <= i && j0 + r >= forgot ? p[r] * a.scale * half * half : 0.0f;
+                }
+                put4(s.a + i * PA + j0, p);
+            }
+            __syncthreads();
+            Frag<T> fs[DK / 32][CT];  // the state as an operand
+#pragma unroll
+            for (int x = 0; x < DK / 32; ++x)
+#pragma unroll
+                for (int j = 0; j < CT; ++j) {
+                    float f[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) f[e] = S.s[2 * x + e / 4][j][e % 4];
+                    fs[x][j] = frag_of(f, T{});
+                }
+#pragma unroll
+            for (int it = 0; it < IT; ++it) {
+                const int i = 16 * it + li;
+                f32x4_t o[CT];
+#pragma unroll
+                for (int j = 0; j < CT; ++j) o[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int x = 0; x < DK / 32; ++x) {
+                    const Frag<T> fq = turned_row_frag<PK>(s.q, i, 32 * x, lq);
+#pragma unroll
+                    for (int j = 0; j < CT; ++j) multiply(o[j], fs[x][j], fq);
+                }
+                const float half = s.d.from_start[i];
+#pragma unroll
+                for (int j = 0; j < CT; ++j)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[j][r] = scaled(o[j][r] * a.scale, half);
+#pragma unroll
+                for (int kb = 0; kb <= it / 2; ++kb) {
+                    const Frag<T> fa = row_frag<PA>(s.a, i, 32 * kb, lq);
+#pragma unroll
+                    for (int j = 0; j < CT; ++j) multiply(o[j], fv[j][kb], fa);
+                }
+                if (i < n) {
+                    char* const to = a.y + ((at.b * a.L + t + i) * a.H + at.h) * a.dv_ * T::kBytes;
+                    const int c = c0 + cw + (CT == 2 ? 8 : 4) * lq;
+                    float f[4 * CT];
+#pragma unroll
+                    for (int e = 0; e < 4 * CT; ++e) f[e] = o[e / 4][e % 4];
+                    if (a.dv_ % 8 == 0) {
+                        if (c < a.dv_)
+#pragma unroll
+                            for (int e = 0; e < 4 * CT; e += 16 / T::kBytes < 4 * CT ? 16 / T::kBytes : 4 * CT) {
+                                constexpr int kN = 16 / T::kBytes < 4 * CT ? 16 / T::kBytes : 4 * CT;
+                                float part[kN];
+#pragma unroll
+                                for (int x = 0; x < kN; ++x) part[x] = f[e + x];
+                                Pack<T, kN>::store(to + (c + e) * T::kBytes, Pack<T, kN>::pack(part));
+                            }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4 * CT; ++e)
+                            if (c + e < a.dv_) {
+                                const float one[1] = {f[e]};
+                                Pack<T, 1>::store(to + (c + e) * T::kBytes, Pack<T, 1>::pack(one));
+                            }
+                    }
+                }
+            }
+        }
+        S.decay(s.d.whole);
+        add_rows<T, DK, C>(S, s.k, fv, s.d.to_end, 1.0f, li, lq);
+        sum = sum == -INFINITY || s.d.sum == -INFINITY ? -INFINITY : sum + s.d.sum;  // (nothing undoes a reset, NaN neither)
+        return true;
+    };
+
+    for (int64_t x = first; x < last; ++x) {
+        if constexpr (MARKS) {
+            char* const m = a.marks + ((at.item * a.chunks + x) * (DK * DV) + w * (DK * WC)) * T::kBytes;
+#pragma unroll
+            for (int i = 0; i < DT; ++i)
+#pragma unroll
+                for (int j = 0; j < CT; ++j) store_mark<T>(m + ((i * CT + j) * kWave + lane) * 4 * T::kBytes, S.s[i][j]);
+        }
+        const int64_t t = x * C;
+        const int n = a.L - t < C ? (int)(a.L - t) : C;
+        if (!take(t, n, true))
+            for (int i = 0; i < n; ++i) take(t + i, 1, false);
+    }
+    if constexpr (OUT) {
+        if (at.segment == a.segments - 1 && a.state_out) S.store(a.state_out + head_state, a.dk_, a.dv_, c0 + cw, li, lq);
+    } else if (a.ends) {
+        S.store_own(a.ends + (at.segment * items + at.item) * (DK * DV) + w * (DK * WC), lane);
+        if (threadIdx.x == 0) a.sums[at.segment * items + at.item] = sum;
+    }
+}
+
+// The same in the other order for the gradients of states: rows of q, columns of dy.
+template <typename T, int DK, int DV>
+struct BackLds {
+    static constexpr int C = kChunk<T>;
+    Elem<T> q[C * kPitch<T, DK>], dy[C * kPitch<T, DV>];
+    Decays<C> d;
+};
+template <typename T, int DK, int DV>
+__global__ __launch_bounds__(256) void la_back_kernel(LaArgs a) {
+    constexpr int C = kChunk<T>, NT = 256, NW = 4, KB = C / 32, DT = DK / 16, CT = DV / NW / 16, WC = 16 * CT;
+    constexpr int PV = kPitch<T, DV>;
+    __shared__ __attribute__((aligned(16))) BackLds<T, DK, DV> s;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, li = lane % 16, lq = lane / 16;
+    const Place at = place_of(a, blockIdx.x);
+    if (at.segment == 0) return;
+    const char *qp = a.q.p + at.b * a.q.batch + at.hk * a.q.head, *dyp = a.dy.p + at.b * a.dy.batch + at.h * a.dy.head;
+    const char* gp = a.g.p + at.b * a.g.batch + (int64_t)at.h * T::kBytes;
+    const int c0 = at.tile * DV, cw = w * WC;
+    const int64_t items = (int64_t)gridDim.x / a.segments;
+    State<DT, CT> M;
+    if (at.segment == a.segments - 1 && a.dstate_out) M.load(a.dstate_out + (at.b * a.H + at.h) * a.dk_ * a.dv_, a.dk_, a.dv_, c0 + cw, li, lq);
+    else M.clear();
+    const int64_t first = at.segment * a.each, last = first + a.each < a.chunks ? first + a.each : a.chunks;
+    double sum = 0.0;
+    auto take = [&](int64_t t, int n, bool look) -> bool {
+        __syncthreads();
+        bool fine = load_tile<T, C, DK, NT>(s.q, a.q, qp + t * a.q.step, n, 0);
+        fine &= load_tile<T, C, DV, NT>(s.dy, a.dy, dyp + t * a.dy.step, n, c0);
+        if (w == 0) {
+            bool odd;
+            make_decays<C>(s.d, lane < n ? number<T>(gp + (t + lane) * a.g.step) : 0.0f, lane, odd);
+            fine &= !odd;
+        }
+        if (look) {
+            if (__syncthreads_or(!fine)) return false;
+        } else {
+            __syncthreads();
+        }
+        Frag<T> fb[CT][KB];
+#pragma unroll
+        for (int j = 0; j < CT; ++j)
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                if constexpr (CT == 2) fb[j][kb] = column_frag<PV, 8>(s.dy, 32 * kb, cw + 4 * j, li, lq);
+                else fb[j][kb] = column_frag<PV, 4>(s.dy, 32 * kb, cw + 16 * j, li, lq);
+            }
+        M.decay(s.d.whole);
+        add_rows<T, DK, C>(M, s.q, fb, s.d.from_start, a.scale, li, lq);
+        sum = sum == -INFINITY || s.d.sum == -INFINITY ? -INFINITY : sum + s.d.sum;  // (nothing undoes a reset, NaN neither)
+        return true;
+    };
+    for (int64_t x = last - 1; x >= first; --x) {
+        const int64_t t = x * C;
+        const int n = a.L - t < C ? (int)(a.L - t) : C;
+        if (!take(t, n, true))
+            for (int i = n - 1; i >= 0; --i) take(t + i, 1, false);
+    }
+    M.store_own(a.ends + (at.segment * items + at.item) * (DK * DV) + w * (DK * WC), lane);
+    if (threadIdx.x == 0) a.sums[at.segment * items + at.item] = sum;
+}
+
+// Ends of segments made by themselves -> ends of everything up to them (BACK: from them on): e[s] += decay of s * e[s - 1].
+template <bool BACK>
+__global__ __launch_bounds__(256) void la_ends_kernel(float* ends, const double* sums, int64_t items, int32_t size, int32_t segments) {
+    const int64_t n = items * (size / 4);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t item = i / (size / 4);
+        float4 e = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int x = 0; x < segments - 1; ++x) {  // (nothing comes behind the last)
+            const int at = BACK ? segments - 1 - x : x;
+            float4* const p = reinterpret_cast<float4*>(ends) + at * n + i;
+            const double d = sums[at * items + item];
+            const float half = d == -INFINITY ? 0.0f : half_factor((float)d);
+            const float4 own = *p;
+            e.x = scaled(e.x, half) + own.x, e.y = scaled(e.y, half) + own.y, e.z = scaled(e.z, half) + own.z, e.w = scaled(e.w, half) + own.w;
+            *p = e;
+        }
+    }
+}
+
+// ---- the backward walk
+
+template <typename T, int DK, int DV>
+struct BwdLds {
+    static constexpr int C = kChunk<T>, IT = C / 16, NW = DV / 16;
+    Elem<T> q[C * kPitch<T, DK>], k[C * kPitch<T, DK>], v[C * kPitch<T, DV>], dy[C * kPitch<T, DV>];
+    Elem<T> a[C * kPitch<T, C>], e[C * kPitch<T, C>];  // A and its gradient's part for q and k
+    Elem<T> s[DV * kPitch<T, DK>];                     // the state in front of the chunk, then the gradient of that behind it, turned
+    float row[IT][C], col[IT][C];                      // shares of the log decays' gradients: of pairs of steps, by row and by column
+    float far_q[DK / 16][C], far_k[DK / 16][C];        // of q with the state, and of k with its gradient
+    float both[NW];                                    // <S, M>
+    Decays<C> d;
+};
+
+template <typename T, int DK, int DV, bool SHARES>
+__global__ __launch_bounds__(DV * 4) void la_bwd_kernel(LaArgs a) {
+    constexpr int C = kChunk<T>, NW = DV / 16, NT = NW * kWave, IT = C / 16, KB = C / 32, DT = DK / 16;
+    constexpr int PK = kPitch<T, DK>, PV = kPitch<T, DV>, PA = kPitch<T, C>;
+    __shared__ __attribute__((aligned(16))) BwdLds<T, DK, DV> s;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, li = lane % 16, lq = lane / 16;
+    const Place at = place_of(a, blockIdx.x);
+    const char *kp = a.k.p + at.b * a.k.batch + at.hk * a.k.head, *vp = a.v.p + at.b * a.v.batch + at.h * a.v.head;
+    const char *qp = a.q.p + at.b * a.q.batch + at.hk * a.q.head, *dyp = a.dy.p + at.b * a.dy.batch + at.h * a.dy.head;
+    const char* gp = a.g.p + at.b * a.g.batch + (int64_t)at.h * T::kBytes;
+    const int c0 = at.tile * DV, cw = w * 16;
+    const int64_t items = (int64_t)gridDim.x / a.segments, head_state = (at.b * a.H + at.h) * a.dk_ * a.dv_;
+    State<DT, 1> M;  // the gradient of the state behind the chunk
+    if (at.segment < a.segments - 1) {
+        // (made by the walk of 4 waves: their columns)
+        constexpr int CT4 = DV / 64, WC4 = 16 * CT4;
+        const float* p = a.ends + ((at.segment + 1) * items + at.item) * (DK * DV);
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+            const int c = cw + li, w4 = c / WC4, in = c % WC4;
+            const int j = CT4 == 2 ? in / 4 % 2 : 0, l = CT4 == 2 ? in / 8 * 4 + in % 4 : in;
+            M.s[i][0] = *reinterpret_cast<const f32x4_t*>(p + w4 * (DK * WC4) + ((i * CT4 + j) * kWave + lq * 16 + l) * 4);
+        }
+    } else if (a.dstate_out) {
+        M.load(a.dstate_out + head_state, a.dk_, a.dv_, c0 + cw, li, lq);
+    } else {
+        M.clear();
+    }
+    for (int i = threadIdx.x; i < C * PA; i += NT) s.a[i] = 0, s.e[i] = 0;
+    const int64_t first = at.segment * a.each, last = first + a.each < a.chunks ? first + a.each : a.chunks;
+    const int64_t heads_qk = a.H / a.group, rows_all = (int64_t)gridDim.x / a.segments / a.tiles / a.H * a.L;  // B L
+    const int64_t share = (int64_t)(at.h % a.group) * a.tiles + at.tile;
+
+    // a row of dq or dk: four numbers from d on
+    auto give = [&](void* base, int64_t t, int d, const f32x4_t& v) {
+        if (d >= a.dk_) return;
+        const int64_t e = ((at.b * a.L + t) * heads_qk + at.hk) * a.dk_ + d;
+        if constexpr (SHARES) {
+            float* p = static_cast<float*>(base) + share * (rows_all * heads_qk * a.dk_) + e;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (d + r < a.dk_) p[r] = v[r];
+        } else {
+            const float f[4] = {v[0], v[1], v[2], v[3]};
+            char* p = static_cast<char*>(base) + e * T::kBytes;
+            if (a.dk_ % 4 == 0) {
+                Pack<T, 4>::store(p, Pack<T, 4>::pack(f));
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (d + r < a.dk_) {
+                        const float one[1] = {f[r]};
+                        Pack<T, 1>::store(p + r * T::kBytes, Pack<T, 1>::pack(one));
+                    }
+            }
+        }
+    };
+    // the wave's share of the state in front of chunk x
+    auto mark = [&](State<DT, 1>& S, int64_t x) {
+        constexpr int CT4 = DV / 64, WC4 = 16 * CT4;
+        const char* p = a.marks_in + (at.item * a.chunks + x) * (DK * DV) * T::kBytes;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+            const int c = cw + li, w4 = c / WC4, in = c % WC4;
+            const int j = CT4 == 2 ? in / 4 % 2 : 0, l = CT4 == 2 ? in / 8 * 4 + in % 4 : in;
+            S.s[i][0] = load_mark<T>(p + (w4 * (DK * WC4) + ((i * CT4 + j) * kWave + lq * 16 + l) * 4) * T::kBytes);
+        }
+    };
+    // steps [t, t + n) of chunk x, from step `t0` of it on
+    auto take = [&](int64_t x, int64_t t, int n, bool look) -> bool {
+        __syncthreads();
+        bool fine = load_tile<T, C, DK, NT>(s.q, a.q, qp + t * a.q.step, n, 0);
+        fine &= load_tile<T, C, DK, NT>(s.k, a.k, kp + t * a.k.step, n, 0);
+        fine &= load_tile<T, C, DV, NT>(s.v, a.v, vp + t * a.v.step, n, c0);
+        fine &= load_tile<T, C, DV, NT>(s.dy, a.dy, dyp + t * a.dy.step, n, c0);
+        if (w == 0) {
+            bool odd;
+            make_decays<C>(s.d, lane < n ? number<T>(gp + (t + lane) * a.g.step) : 0.0f, lane, odd);
+            fine &= !odd;
+        }
+        State<DT, 1> S;
+        mark(S, x);
+        if (look) {
+            if (__syncthreads_or(!fine)) return false;
+        } else {
+            __syncthreads();
+            // the state in front of step t, from that in front of its chunk: number by number
+            const int c = c0 + cw + li;
+            for (int64_t u = x * C; u < t; ++u) {
+                const float g = number<T>(gp + u * a.g.step);
+                const float half = g < kForgets ? 0.0f : half_factor((float)((double)g * kLog2E));
+                const float vc = c < a.dv_ ? number<T>(vp + u * a.v.step + (int64_t)c * T::kBytes) : 0.0f;
+                for (int i = 0; i < DT; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int d = 16 * i + 4 * lq + r;
+                        const float kd = d < a.dk_ ? number<T>(kp + u * a.k.step + (int64_t)d * T::kBytes) : 0.0f;
+                        S.s[i][0][r] = scaled(S.s[i][0][r], half) + kd * vc;
+                    }
+            }
+        }
+        // <S, M>, and S to LDS
+        {
+            float both = 0.0f;
+#pragma unroll
+            for (int i = 0; i < DT; ++i) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) both += s.d.whole == 0.0f ? 0.0f : scaled(S.s[i][0][r], s.d.whole) * M.s[i][0][r];
+                put4(s.s + (cw + li) * PK + 16 * i + 4 * lq, S.s[i][0]);
+            }
+#pragma unroll
+            for (int d = kWave / 2; d > 0; d /= 2) both += __shfl_xor(both, d, kWave);
+            if (lane == 0) s.both[w] = both;
+        }
+        // A, its gradient's part E_ij = scale exp(b_i - b_j) (dy_i . v_j), and W = (dy_i . v_j) A_ij below the diagonal
+        constexpr int kBlocks = IT * (IT + 1) / 2;
+#pragma unroll
+        for (int y = 0; y < (kBlocks + NW - 1) / NW; ++y) {
+            const int block = y * NW + w;
+            if (block >= kBlocks) break;
+            int it = 0;
+            while ((it + 1) * (it + 2) / 2 <= block) ++it;
+            const int jt = block - it * (it + 1) / 2;
+            f32x4_t p = {0.0f, 0.0f, 0.0f, 0.0f}, e = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int kb = 0; kb < DK / 32; ++kb)
+                multiply(p, row_frag<PK>(s.k, 16 * jt + li, 32 * kb, lq), row_frag<PK>(s.q, 16 * it + li, 32 * kb, lq));
+#pragma unroll
+            for (int kb = 0; kb < DV / 32; ++kb)
+                multiply(e, row_frag<PV>(s.v, 16 * jt + li, 32 * kb, lq), row_frag<PV>(s.dy, 16 * it + li, 32 * kb, lq));
+            const int i = 16 * it + li, j0 = 16 * jt + 4 * lq, forgot = s.d.forgot[i];
+            const float hi = s.d.hi[i], lo = s.d.lo[i];
+            float row = 0.0f, col[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const bool in = j0 + r <= i && j0 + r >= forgot;
+                const float half = half_factor((hi - s.d.hi[j0 + r]) + (lo - s.d.lo[j0 + r]));
+                p[r] = in ? p[r] * a.scale * half * half : 0.0f;
+                col[r] = in && j0 + r < i ? p[r] * e[r] : 0.0f;
+                e[r] = in ? e[r] * a.scale * half * half : 0.0f;
+                row += col[r];
+            }
+            put4(s.a + i * PA + j0, p);
+            put4(s.e + i * PA + j0, e);
+            row += __shfl_xor(row, 16, kWave);
+            row += __shfl_xor(row, 32, kWave);
+            if (lq == 0) s.row[jt][i] = row;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+#pragma unroll
+                for (int d = 1; d < 16; d *= 2) col[r] += __shfl_xor(col[r], d, kWave);
+                if (li == 0) s.col[it][j0 + r] = col[r];
+            }
+        }
+        // dv of the wave's columns from M in registers
+        f32x4_t dv[IT];
+        Frag<T> fdy[KB];
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) fdy[kb] = column_frag<PV, 4>(s.dy, 32 * kb, cw, li, lq);
+        {
+            Frag<T> fm[DK / 32];
+#pragma unroll
+            for (int y = 0; y < DK / 32; ++y) {
+                float f[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = M.s[2 * y + e / 4][0][e % 4];
+                fm[y] = frag_of(f, T{});
+            }
+#pragma unroll
+            for (int jt = 0; jt < IT; ++jt) {
+                dv[jt] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int y = 0; y < DK / 32; ++y) multiply(dv[jt], fm[y], turned_row_frag<PK>(s.k, 16 * jt + li, 32 * y, lq));
+                const float half = s.d.to_end[16 * jt + li];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) dv[jt][r] = scaled(dv[jt][r], half);
+            }
+        }
+        __syncthreads();  // A, E and S are there
+#pragma unroll
+        for (int jt = 0; jt < IT; ++jt) {
+#pragma unroll
+            for (int kb = jt / 2; kb < KB; ++kb) multiply(dv[jt], fdy[kb], column_frag<PA, 4>(s.a, 32 * kb, 16 * jt, li, lq));
+            const int j = 16 * jt + li, c = c0 + cw + 4 * lq;
+            if (j < n && c < a.dv_) {
+                const float f[4] = {dv[jt][0], dv[jt][1], dv[jt][2], dv[jt][3]};
+                char* p = a.dv + (((at.b * a.L + t + j) * a.H + at.h) * a.dv_ + c) * T::kBytes;
+                if (a.dv_ % 4 == 0) {
+                    Pack<T, 4>::store(p, Pack<T, 4>::pack(f));
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (c + r < a.dv_) {
+                            const float one[1] = {f[r]};
+                            Pack<T, 1>::store(p + r * T::kBytes, Pack<T, 1>::pack(one));
+                        }
+                }
+            }
+        }
+        // dq and dk, blocks of 16 rows by 16 numbers: dt = w % DT + ..., rows in turn
+        constexpr int kBand = NW < DT ? NW : DT;  // waves side by side
+        auto blocks = [&](auto&& f) {
+#pragma unroll
+            for (int y = 0; y < DT / kBand; ++y)
+#pragma unroll
+                for (int z = 0; z < (IT * kBand + NW - 1) / NW; ++z) {
+                    const int it = z * (NW / kBand) + w / kBand;
+                    if (it < IT) f(it, y * kBand + w % kBand);
+                }
+        };
+        blocks([&](int it, int dt) {
+            const int i = 16 * it + li;
+            f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int kb = 0; kb < DV / 32; ++kb)
+                multiply(o, column_frag<PK, 4>(s.s, 32 * kb, 16 * dt, li, lq), row_frag<PV>(s.dy, i, 32 * kb, lq));
+            const float half = s.d.from_start[i];
+            float far = 0.0f;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                o[r] = scaled(o[r] * a.scale, half);
+                float q[1];
+                Pack<T, 1>::unpack(Pack<T, 1>::load(s.q + i * PK + 16 * dt + 4 * lq + r), q);
+                far += half == 0.0f ? 0.0f : q[0] * o[r];
+            }
+            far += __shfl_xor(far, 16, kWave);
+            far += __shfl_xor(far, 32, kWave);
+            if (lq == 0) s.far_q[dt][i] = far;
+            for (int kb = 0; kb <= it / 2; ++kb) multiply(o, column_frag<PK, 4>(s.k, 32 * kb, 16 * dt, li, lq), row_frag<PA>(s.e, i, 32 * kb, lq));
+            if (i < n) give(a.dq, t + i, 16 * dt + 4 * lq, o);
+        });
+        __syncthreads();  // S has been read
+#pragma unroll
+        for (int i = 0; i < DT; ++i) put4(s.s + (cw + li) * PK + 16 * i + 4 * lq, M.s[i][0]);
+        __syncthreads();
+        blocks([&](int jt, int dt) {
+            const int j = 16 * jt + li;
+            f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int kb = 0; kb < DV / 32; ++kb)
+                multiply(o, column_frag<PK, 4>(s.s, 32 * kb, 16 * dt, li, lq), row_frag<PV>(s.v, j, 32 * kb, lq));
+            const float half = s.d.to_end[j];
+            float far = 0.0f;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                o[r] = scaled(o[r], half);
+                float k[1];
+                Pack<T, 1>::unpack(Pack<T, 1>::load(s.k + j * PK + 16 * dt + 4 * lq + r), k);
+                far += half == 0.0f ? 0.0f : k[0] * o[r];
+            }
+            far += __shfl_xor(far, 16, kWave);
+            far += __shfl_xor(far, 32, kWave);
+            if (lq == 0) s.far_k[dt][j] = far;
+            for (int kb = jt / 2; kb < KB; ++kb) multiply(o, column_frag<PK, 4>(s.q, 32 * kb, 16 * dt, li, lq), column_frag<PA, 4>(s.e, 32 * kb, 16 * jt, li, lq));
+            if (j < n) give(a.dk, t + j, 16 * dt + 4 * lq, o);
+        });
+        {
+            M.decay(s.d.whole);
+            Frag<T> fb[1][KB];
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) fb[0][kb] = fdy[kb];
+            add_rows<T, DK, C>(M, s.q, fb, s.d.from_start, a.scale, li, lq);
+        }
+        __syncthreads();  // the shares of dg are there
+        if (w == 0) {
+            // pairs of steps on both sides of decay t: inside the chunk, those whose later step is from t on less those whose earlier
+            // step is too; those with an earlier step in front of the chunk; those with a later step behind it; those with both
+            double near = 0.0, col = 0.0;
+            if (lane < C) {
+                for (int x2 = 0; x2 <= lane / 16; ++x2) near += (double)s.row[x2][lane];
+                for (int x2 = lane / 16; x2 < IT; ++x2) near -= (double)s.col[x2][lane];
+                for (int x2 = 0; x2 < DT; ++x2) near += (double)s.far_q[x2][lane], col += (double)s.far_k[x2][lane];
+            }
+            double both = 0.0;
+            for (int x2 = 0; x2 < NW; ++x2) both += (double)s.both[x2];
+            double upto = col;
+#pragma unroll
+            for (int d = 1; d < kWave; d *= 2) {
+                const double f = __shfl_up(upto, d, kWave), g = __shfl_down(near, d, kWave);
+                if (lane >= d) upto += f;
+                if (lane + d < kWave) near += g;
+            }
+            if (lane < n) {
+                const float g = number<T>(gp + (t + lane) * a.g.step);
+                const float one[1] = {g < kForgets ? 0.0f : (float)(near + (upto - col) + both)};
+                const int64_t e = (at.b * a.L + t + lane) * a.H + at.h;
+                if (a.tiles > 1) static_cast<float*>(a.dg)[at.tile * (rows_all * a.H) + e] = one[0];
+                else Pack<T, 1>::store(static_cast<char*>(a.dg) + e * T::kBytes, Pack<T, 1>::pack(one));
+            }
+        }
+        return true;
+    };
+    for (int64_t x = last - 1; x >= first; --x) {
+        const int64_t t = x * C;
+        const int n = a.L - t < C ? (int)(a.L - t) : C;
+        if (!take(x, t, n, true))
+            for (int i = n - 1; i >= 0; --i) take(x, t + i, 1, false);
+    }
+    if (at.segment == 0 && a.dstate_in) M.store(a.dstate_in + head_state, a.dk_, a.dv_, c0 + cw, li, lq);
+}
+
+// out[r][d] = sum over the shares: heads that share a row of q and k, and tiles of their columns; [share][rows].
+template <typename T>
+__global__ __launch_bounds__(256) void la_shares_kernel(const float* shares, void* out, int64_t n, int32_t count) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        float sum = 0.0f;
+        for (int x = 0; x < count; ++x) sum += shares[x * n + i];
+        const float one[1] = {sum};
+        Pack<T, 1>::store(static_cast<char*>(out) + i * T::kBytes, Pack<T, 1>::pack(one));
+    }
+}
+
+__global__ __launch_bounds__(256) void la_copy_kernel(const float* from, float* to, int64_t n) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) to[i] = from ? from[i] : 0.0f;
+}
+
+// ---- one token: the state, read and written, is what it costs.  A workgroup has 4 CL columns of a head's state (VEC = 1: CL), a
+// lane VEC of them in every (256 / CL)-th row.
+struct StepArgs {
+    const char *q, *k, *v, *g;
+    char* y;
+    float* state;
+    int32_t H, group, dk, dv, slices;
+    float scale;
+};
+template <typename T, int CL, int VEC>
+__global__ __launch_bounds__(256) void la_step_kernel(StepArgs a) {
+    constexpr int kRows = 256 / CL;
+    __shared__ float sum[kRows][CL * VEC];
+    const int cl = threadIdx.x % CL, row = threadIdx.x / CL;
+    const int64_t bh = blockIdx.x / (uint32_t)a.slices, b = bh / a.H;
+    const int h = (int)(bh % a.H), c = ((int)(blockIdx.x % (uint32_t)a.slices) * CL + cl) * VEC;
+    const int64_t qk = (b * (a.H / a.group) + h / a.group) * a.dk;
+    const float g = number<T>(a.g + bh * T::kBytes);
+    const float half = g < kForgets ? 0.0f : half_factor((float)((double)g * kLog2E));
+    float v[VEC] = {}, y[VEC] = {};
+    if (c < a.dv) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) v[j] = number<T>(a.v + (bh * a.dv + c + j) * T::kBytes);
+        float* const p = a.state + bh * a.dk * a.dv + c;
+#pragma unroll 8
+        for (int d = row; d < a.dk; d += kRows) {
+            float s[VEC];
+            Pack<F32, VEC>::unpack(Pack<F32, VEC>::load(p + (int64_t)d * a.dv), s);
+            const float k = number<T>(a.k + (qk + d) * T::kBytes), q = number<T>(a.q + (qk + d) * T::kBytes);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                s[j] = scaled(s[j], half) + k * v[j];
+                y[j] = fmaf(q, s[j], y[j]);
+            }
+            Pack<F32, VEC>::store(p + (int64_t)d * a.dv, Pack<F32, VEC>::pack(s));
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) sum[row][cl * VEC + j] = y[j];
+    __syncthreads();
+    const int i = threadIdx.x, at = (int)(blockIdx.x % (uint32_t)a.slices) * (CL * VEC) + i;
+    if (i < CL * VEC && at < a.dv) {
+        float f = 0.0f;
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) f += sum[r][i];
+        const float one[1] = {f * a.scale};
+        Pack<T, 1>::store(a.y + (bh * a.dv + at) * T::kBytes, Pack<T, 1>::pack(one));
+    }
+}
+
+// ---- sizes
+
+int chunk_of(const LaShape& s) { return s.dtype == HY_F32 ? kChunk<F32> : kChunk<BF16>; }
+int64_t chunks_of(const LaShape& s) { return (s.L + chunk_of(s) - 1) / chunk_of(s); }
+int tile_rows(const LaShape& s) { return s.dk > 64 ? 128 : 64; }     // DK
+int tile_columns(const LaShape& s) { return s.dv > 64 ? 128 : 64; }  // DV
+int64_t tiles_of(const LaShape& s) { return (s.dv + tile_columns(s) - 1) / tile_columns(s); }
+int64_t items_of(const LaShape& s) { return s.B * s.H * tiles_of(s); }
+int64_t state_size(const LaShape& s) { return (int64_t)tile_rows(s) * tile_columns(s); }
+
+// Segments of a sequence, so that `want` workgroups are there, of 4 chunks at the least.
+struct Cut {
+    int64_t segments, each;
+};
+Cut cut(const LaShape& s, int64_t want) {
+    const int64_t chunks = chunks_of(s), items = items_of(s);
+    int64_t n = (want + items - 1) / items;
+    if (n > (chunks + 3) / 4) n = (chunks + 3) / 4;
+    if (n < 1) n = 1;
+    const int64_t each = (chunks + n - 1) / n;
+    return Cut{(chunks + each - 1) / each, each};
+}
+constexpr int64_t kForwardGroups = 512, kBackwardGroups = 256;
+
+int64_t ends_bytes(const LaShape& s, const Cut& c) {
+    return c.segments > 1 ? c.segments * items_of(s) * (state_size(s) * 4 + 8) : 0;
+}
+int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
+
+Rows rows_of(const void* p, const LaShape& s, int which, int64_t d) {
+    const int64_t e = s.dtype == HY_F32 ? 4 : 2;
+    const int64_t* st = s.stride[which];
+    const bool wide = d % 8 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0 && st[0] * e % 16 == 0 && st[1] * e % 16 == 0 && st[2] * e % 16 == 0;
+    return Rows{static_cast<const char*>(p), st[0] * e, st[1] * e, st[2] * e, (int32_t)d, wide};
+}
+
+LaArgs args_of(const LaPtrs& p, const LaShape& s) {
+    LaArgs a{};
+    a.q = rows_of(p.q, s, kLaQ, s.dk), a.k = rows_of(p.k, s, kLaK, s.dk), a.v = rows_of(p.v, s, kLaV, s.dv);
+    a.g = rows_of(p.g, s, kLaG, 1), a.dy = rows_of(p.dy, s, kLaDy, s.dv);
+    a.state_in = p.state_in, a.dstate_out = p.dstate_out;
+    a.y = static_cast<char*>(p.y), a.state_out = p.state_out, a.dstate_in = p.dstate_in;
+    a.L = s.L, a.chunks = chunks_of(s);
+    a.H = (int32_t)s.H, a.group = s.group, a.dk_ = (int32_t)s.dk, a.dv_ = (int32_t)s.dv, a.tiles = (int32_t)tiles_of(s);
+    a.scale = (float)s.scale;
+    return a;
+}
+
+// f<T, DK, DV>
+template <typename F>
+hy_status by_tile(const LaShape& s, F&& f) {
+    using std::integral_constant;
+    auto columns = [&](auto t, auto dk) {
+        return tile_columns(s) == 128 ? f(t, dk, integral_constant<int, 128>{}) : f(t, dk, integral_constant<int, 64>{});
+    };
+    auto rows = [&](auto t) { return tile_rows(s) == 128 ? columns(t, integral_constant<int, 128>{}) : columns(t, integral_constant<int, 64>{}); };
+    return s.dtype == HY_F32 ? rows(F32{}) : rows(BF16{});
+}
+
+hy_status scan_ends(const LaArgs& a, const LaShape& s, bool back, hipStream_t st) {
+    const int64_t items = items_of(s);
+    const dim3 grid(workgroups_for(items * (state_size(s) / 4), 256, 256));
+    return back ? launch_kernel(la_ends_kernel<true>, grid, dim3(256), st, a.ends, static_cast<const double*>(a.sums), items, (int32_t)state_size(s), a.segments)
+                : launch_kernel(la_ends_kernel<false>, grid, dim3(256), st, a.ends, static_cast<const double*>(a.sums), items, (int32_t)state_size(s), a.segments);
+}
+
+// The forward walk: outputs, or with `out` false the marks alone.
+hy_status walk(LaArgs a, const LaShape& s, const Cut& c, void* ws, bool out, hipStream_t st) {
+    const int64_t items = items_of(s);
+    a.segments = (int32_t)c.segments, a.each = c.each;
+    a.ends = static_cast<float*>(ws), a.sums = reinterpret_cast<double*>(static_cast<float*>(ws) + c.segments * items * state_size(s));
+    const dim3 grid((uint32_t)(items * c.segments));
+    if (c.segments > 1) {
+        hy_status rc = by_tile(s, [&](auto t, auto dk, auto dv) {
+            return launch_kernel(la_walk_kernel<decltype(t), decltype(dk)::value, decltype(dv)::value, false, false>, grid, dim3(256), st, a);
+        });
+        if (rc == HY_OK) rc = scan_ends(a, s, false, st);
+        if (rc != HY_OK) return rc;
+    }
+    return by_tile(s, [&](auto t, auto dk, auto dv) {
+        using T = decltype(t);
+        constexpr int DK = decltype(dk)::value, DV = decltype(dv)::value;
+        (void)out;
+        return a.marks ? launch_kernel(la_walk_kernel<T, DK, DV, true, true>, grid, dim3(256), st, a)
+                       : launch_kernel(la_walk_kernel<T, DK, DV, true, false>, grid, dim3(256), st, a);
+    });
+}
+
+// Workspace of the backward call: segments' ends, shares of dq and dk, shares of dg, and marks, if the caller has none.
+struct BwdParts {
+    Cut cut, walk_cut;
+    int64_t ends, shares, dg, marks, y, all;  // bytes
+    int32_t count;
+};
+BwdParts bwd_parts(const LaShape& s, bool with_marks) {
+    BwdParts b{};
+    b.cut = cut(s, kBackwardGroups), b.walk_cut = cut(s, kForwardGroups);
+    b.count = (int32_t)(s.group * tiles_of(s));
+    b.ends = up16(ends_bytes(s, b.cut));
+    if (!with_marks && ends_bytes(s, b.walk_cut) > b.ends) b.ends = up16(ends_bytes(s, b.walk_cut));
+    b.shares = b.count > 1 ? up16(b.count * s.B * s.L * (s.H / s.group) * s.dk * 4) : 0;
+    b.dg = tiles_of(s) > 1 ? up16(tiles_of(s) * s.B * s.L * s.H * 4) : 0;
+    b.marks = with_marks ? 0 : up16(la_marks_bytes(s));
+    b.y = with_marks ? 0 : up16(s.B * s.L * s.H * s.dv * (s.dtype == HY_F32 ? 4 : 2));
+    b.all = b.ends + 2 * b.shares + b.dg + b.marks + b.y;
+    return b;
+}
+
+}  // namespace
+
+bool la_served(const LaShape& s) {
+    const int64_t most = INT64_C(1) << 23;
+    if (s.dk > 128 || s.H > INT32_MAX || s.dv > INT32_MAX) return false;
+    if (s.B == 0 || s.H == 0 || s.dv == 0 || s.L == 0) return true;
+    const int64_t tiles = (s.dv + 63) / 64, chunks = (s.L + 63) / 64;
+    return s.B < most && s.H < most && tiles < most && chunks < most && s.B * s.H < most && s.B * s.H * tiles < most && s.B * s.H * tiles * chunks < most;
+}
+
+int64_t la_marks_bytes(const LaShape& s) { return items_of(s) * chunks_of(s) * state_size(s) * (s.dtype == HY_F32 ? 4 : 2); }
+
+int64_t la_fwd_workspace_bytes(const LaShape& s) { return ends_bytes(s, cut(s, kForwardGroups)); }
+
+int64_t la_bwd_workspace_bytes(const LaShape& s, bool marks) { return bwd_parts(s, marks).all; }
+
+hy_status launch_la_fwd(const LaPtrs& p, const LaShape& s, void* ws, hipStream_t st) {
+    if (s.L == 0) {
+        const int64_t n = s.B * s.H * s.dk * s.dv;
+        return launch_kernel(la_copy_kernel, dim3(workgroups_for(n, 256, 256)), dim3(256), st, p.state_in, p.state_out, n);
+    }
+    LaArgs a = args_of(p, s);
+    a.marks = static_cast<char*>(p.marks);
+    return walk(a, s, cut(s, kForwardGroups), ws, true, st);
+}
+
+hy_status launch_la_bwd(const LaPtrs& p, const LaShape& s, void* ws, hipStream_t st) {
+    if (s.L == 0) {
+        const int64_t n = s.B * s.H * s.dk * s.dv;
+        return launch_kernel(la_copy_kernel, dim3(workgroups_for(n, 256, 256)), dim3(256), st, p.dstate_out, p.dstate_in, n);
+    }
+    const BwdParts b = bwd_parts(s, p.marks_in != nullptr);
+    char* const base = static_cast<char*>(ws);
+    char *const shares_q = base + b.ends, *const shares_k = shares_q + b.shares, *const shares_g = shares_k + b.shares;
+    char *const marks = shares_g + b.dg, *const y = marks + b.marks;
+    LaArgs a = args_of(p, s);
+    a.marks_in = static_cast<const char*>(p.marks_in);
+    if (!a.marks_in) {
+        LaArgs f = a;
+        f.marks = marks, f.y = y, f.state_out = nullptr;
+        const hy_status rc = walk(f, s, b.walk_cut, base, false, st);
+        if (rc != HY_OK) return rc;
+        a.marks_in = marks;
+    }
+    const int64_t items = items_of(s);
+    a.segments = (int32_t)b.cut.segments, a.each = b.cut.each;
+    a.ends = reinterpret_cast<float*>(base), a.sums = reinterpret_cast<double*>(a.ends + b.cut.segments * items * state_size(s));
+    a.dv = static_cast<char*>(p.dv);
+    a.dq = b.count > 1 ? shares_q : p.dq, a.dk = b.count > 1 ? shares_k : p.dk, a.dg = b.dg > 0 ? shares_g : p.dg;
+    const dim3 grid((uint32_t)(items * b.cut.segments));
+    hy_status rc = HY_OK;
+    if (b.cut.segments > 1) {
+        rc = by_tile(s, [&](auto t, auto dk, auto dv) {
+            return launch_kernel(la_back_kernel<decltype(t), decltype(dk)::value, decltype(dv)::value>, grid, dim3(256), st, a);
+        });
+        if (rc == HY_OK) rc = scan_ends(a, s, true, st);
+        if (rc != HY_OK) return rc;
+    }
+    rc = by_tile(s, [&](auto t, auto dk, auto dv) {
+        using T = decltype(t);
+        constexpr int DK = decltype(dk)::value, DV = decltype(dv)::value;
+        return b.count > 1 ? launch_kernel(la_bwd_kernel<T, DK, DV, true>, grid, dim3(DV * 4), st, a)
+                           : launch_kernel(la_bwd_kernel<T, DK, DV, false>, grid, dim3(DV * 4), st, a);
+    });
+    auto reduce = [&](const void* from, void* to, int64_t n, int32_t count) {
+        const dim3 g(workgroups_for(n, 256, 256));
+        const float* f = static_cast<const float*>(from);
+        return s.dtype == HY_F32 ? launch_kernel(la_shares_kernel<F32>, g, dim3(256), st, f, to, n, count)
+                                 : launch_kernel(la_shares_kernel<BF16>, g, dim3(256), st, f, to, n, count);
+    };
+    const int64_t nqk = s.B * s.L * (s.H / s.group) * s.dk;
+    if (rc == HY_OK && b.count > 1) rc = reduce(shares_q, p.dq, nqk, b.count);
+    if (rc == HY_OK && b.count > 1) rc = reduce(shares_k, p.dk, nqk, b.count);
+    if (rc == HY_OK && b.dg > 0) rc = reduce(shares_g, p.dg, s.B * s.L * s.H, (int32_t)tiles_of(s));
+    return rc;
+}
+
+hy_status launch_la_step(const LaPtrs& p, const LaShape& s, hipStream_t st) {
+    StepArgs a{};
+    a.q = static_cast<const char*>(p.q), a.k = static_cast<const char*>(p.k), a.v = static_cast<const char*>(p.v);
+    a.g = static_cast<const char*>(p.g), a.y = static_cast<char*>(p.y), a.state = p.state_out;
+    a.H = (int32_t)s.H, a.group = s.group, a.dk = (int32_t)s.dk, a.dv = (int32_t)s.dv, a.scale = (float)s.scale;
+    const bool fours = s.dv % 4 == 0;
+    const int64_t heads = s.B * s.H;
+    // 128 columns of a head a workgroup, 32 where that leaves compute units idle
+    auto run = [&](auto t, auto cl, auto vec) {
+        constexpr int CL = decltype(cl)::value, VEC = decltype(vec)::value;
+        a.slices = (int32_t)((s.dv + CL * VEC - 1) / (CL * VEC));
+        return launch_kernel(la_step_kernel<decltype(t), CL, VEC>, dim3((uint32_t)(heads * a.slices)), dim3(256), st, a);
+    };
+    auto by = [&](auto t) {
+        using std::integral_constant;
+        if (!fours) return run(t, integral_constant<int, 32>{}, integral_constant<int, 1>{});
+        return heads < 512 ? run(t, integral_constant<int, 8>{}, integral_constant<int, 4>{}) : run(t, integral_constant<int, 32>{}, integral_constant<int, 4>{});
+    };
+    return s.dtype == HY_F32 ? by(F32{}) : by(BF16{});
+}
+
+}  // namespace hy

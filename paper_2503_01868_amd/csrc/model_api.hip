@@ -5,24 +5,13 @@
 #include <algorithm>
 #include <vector>
 
-#include "hy_checks.hpp"
 #include "hy_common.hpp"
 #include "hy_launch.hpp"
+#include "hy_model_checks.hpp"
 
 using namespace hy;
 
 namespace {
-
-constexpr int64_t kMostElements = INT64_C(1) << 56;  // of one tensor, gaps between its rows included: no sum of bytes passes 63 bits
-
-bool known(int32_t dtype) { return dtype == HY_F32 || dtype == HY_BF16; }
-
-int64_t size_of(int32_t dtype) { return dtype == HY_F32 ? 4 : 2; }
-
-// a * b * c <= kMostElements, for values that are not negative
-bool fits(int64_t a, int64_t b, int64_t c) {
-    return a == 0 || b == 0 || c == 0 || (a <= kMostElements / b && a * b <= kMostElements / c);
-}
 
 hy_status check_glr(int64_t B, int64_t L, int64_t D, int32_t group, int32_t dtype) {
     if (B < 0 || L < 0 || D < 0 || group < 1 || D % group != 0 || L > kMostElements) return HY_ERR_SHAPE;
@@ -56,12 +45,6 @@ Range glr_range(const GlrShape& s, const void* p, int i) {
     if (empty(s.B, s.L, s.D)) return Range{p, 0};
     const int64_t row = i == kGlrG ? s.D / s.group : s.D;
     return Range{p, ((s.B - 1) * s.bstride[i] + (s.L - 1) * s.rstride[i] + row) * size_of(s.dtype)};
-}
-
-hy_status all_aligned(const Range* r, int n) {
-    for (int i = 0; i < n; ++i)
-        if (!aligned16(r[i].p)) return HY_ERR_ALIGN;
-    return HY_OK;
 }
 
 // Inputs may be views that begin at any element: how many a lane can load together.
