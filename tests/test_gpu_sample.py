@@ -146,6 +146,48 @@ def test_large_vocabularies(dtype, V):
             assert abs(float(prob[n]) - float(w[words[at]] / upto[-1])) <= 1e-6 * float(prob[n])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [4096, 4097, 9001, 70001])
+def test_what_long_rows_leave_to_choose_from(V, dtype):
+    """top_k at the ends of what is gathered from a row, words in a few runs, among infinities and NaN, rows of equal logits, rows
+    that begin anywhere."""
+    N = 4
+    z, u, rng = make(V + 1, N, V, dtype)
+    say("sample long V=%d %s" % (V, dtype))
+    for k in (1, 2, 1000, 2047, 2048, 2049, 4095):
+        check(z, u, 1.1, top_k=k)
+        check(z, u, 0.9, k, 0.9, 0.01)
+    for m in (1e-300, 1e-4, 0.3, 1.0, 2.0):
+        check(z, u, 1.3, min_p=m)
+    crowded = z.clone()
+    crowded[0, :3000] += 20  # what counts lies in the first pieces
+    crowded[1, V // 2:V // 2 + 50] += 20
+    crowded[2] = 1.0
+    crowded[3] = -float("inf")
+    crowded[3, [5, V - 1]] = 0.0
+    check(crowded, u, 1.0, 40, 0.95, 0.01)
+    check(crowded, u, 1.0, min_p=0.5)
+    check(crowded, u, 1.0, 2000, 0.5)
+    odd = z.clone()
+    odd[0, ::3] = float("nan")
+    odd[1, [7, V // 2, V - 2]] = float("inf")
+    odd[2, ::2] = -float("inf")
+    odd[3] = -odd[3].abs()
+    for t in (1.0, 1e-30, float("inf")):
+        check(odd, u, t, 50, 0.9)
+        check(odd, u, t, min_p=0.1)
+    check(odd, u, 0.0)
+    few = torch.from_numpy(rng.integers(-20, 3, size=(N, V)).astype(np.float32)).to(DTYPES[dtype]).cuda()
+    few[:, 1000:] -= 40
+    check(few, u, 1.0, 60, 0.7)
+    for first in (1, 2, 3, 5):
+        padded = torch.full((N, V + 9), float("nan"), dtype=z.dtype, device="cuda")
+        padded[:, first:V + first] = z
+        check(padded[:, first:V + first], u, 0.8, 30, 0.9)
+        check(padded[:, first:V + first], u, 0.8)
+        check(padded[:, first:V + first], u, 0.0)
+
+
 def test_tokens_come_as_often_as_they_are_likely():
     z, _, _ = make(8, 1, 300, "f32")
     N = 20000
