@@ -12,12 +12,16 @@
 // scan over the segments' ends, and the walk itself.  The state's products take the factor of k or q as three bf16 parts, so that states
 // are sums of fp32 products in bf16 calls too; what is rounded to bf16 is A and the copies of S that are multiplied.
 //
-// A product mixes rows, and a zero times an infinity is none: a chunk that holds anything not finite, or decays above one that
-// would make something so of finite numbers, is taken again a row at a time.
+// A product mixes rows, and a zero times an infinity is none: a chunk that holds anything not finite, or so large that a product on the
+// way could become so, or decays far above one, is taken a row at a time, by the formulas as they stand.
+#include <string.h>
+
+#include <cmath>
 #include <type_traits>
 
 #include "hy_common.hpp"
 #include "hy_launch.hpp"
+#include "hy_scan.hpp"
 
 namespace hy {
 
@@ -29,13 +33,19 @@ typedef __attribute__((address_space(3))) s16x4_t* lds_quad_t;
 
 constexpr float kForgets = -87.3f;  // exp of less is below the smallest normal number
 constexpr double kLog2E = 1.4426950408889634074;
-constexpr float kMostGrowth = 64.0f;  // bits by which decays above one may grow a state within a chunk that is taken at once
+// Of a chunk that is taken at once: bits by which decays above one may grow a state, and what numbers (times a scale above one) stay
+// below, so that products of two numbers, a factor and a sum over 128 are finite: 24 + 2 * 46 + 7 < 127.
+constexpr float kMostGrowth = 24.0f, kMostNumber = 0x1p46f;
 
-// Factors as exp2(d) = r r, r = exp2(d / 2): growth beyond the range of one factor is left to the products it is in.
+// The factor of one step as exp2(d) = r r, r = exp2(d / 2): growth beyond the range of one factor is left to the products it is in.
 __device__ __forceinline__ float half_factor(float d) {
     const float x = 0.5f * d;
     return __builtin_amdgcn_exp2f(x > 127.0f ? 127.0f : x);  // (of NaN: NaN)
 }
+__device__ __forceinline__ float step_factor(float g) { return g < kForgets ? 0.0f : half_factor((float)((double)g * kLog2E)); }
+__device__ __forceinline__ float scaled(float x, float half) { return half == 0.0f ? 0.0f : x * half * half; }
+// By the factor of several steps, which is a number, or zero: then nothing is left, whatever x is.
+__device__ __forceinline__ float weighted(float x, float factor) { return factor == 0.0f ? 0.0f : x * factor; }
 
 // Eight numbers of a row of an operand: k = 8 lq + e of a block of 32 (lane: li = lane % 16, lq = lane / 16), or in the order of
 // accumulators ("turned"), k = 16 (e / 4) + 4 lq + e % 4.  A product's result has in lane (li, lq), register r, row 4 lq + r of its
@@ -152,10 +162,11 @@ __device__ __forceinline__ void wide_frag(float (&f)[8], Frag<BF16> (&o)[3]) {
 #pragma unroll
     for (int x = 0; x < 3; ++x) {
         o[x] = frag_of(f, BF16{});
+        if (x == 2) break;
         float part[8];
         floats_of(o[x], part);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = fabsf(part[e]) < INFINITY ? f[e] - part[e] : 0.0f;
+        for (int e = 0; e < 8; ++e) f[e] -= part[e];  // (numbers, all of them: chunks with others are not taken at once)
     }
 }
 __device__ __forceinline__ void wide_frag(float (&f)[8], Frag<F32> (&o)[1]) { o[0] = frag_of(f, F32{}); }
@@ -164,107 +175,133 @@ __device__ __forceinline__ void wide_frag(float (&f)[8], Frag<F32> (&o)[1]) { o[
 struct Rows {
     const char* p;
     int64_t batch, step, head;  // bytes
-    int32_t d, wide;            // wide: 8 numbers from a multiple of 8 on can be moved by 16 bytes
+    int32_t d, wide;            // wide: 8 numbers from a multiple of 8 on can be moved by 16 bytes, and rows of a chunk are near
 };
 
 // What a chunk's steps do to a state, in LDS: sums of log2 decays up to and with a step (two floats), the last step up to and with it
-// that forgets (-1: none), and whether the chunk can be taken at once.
+// that forgets (-1: none), factors from the chunk's start to behind a step, from behind it to the end, and of the whole.
 template <int C>
 struct Decays {
     float hi[C], lo[C];
     int32_t forgot[C];
-    float from_start[C], to_end[C];  // half factors; zero: none
-    float whole;                     // of the whole chunk
-    double sum;                      // of the whole chunk
+    float from_start[C], to_end[C];
+    float whole;
+    double sum;
 };
 
-// A wave makes them; lane t has step t.  g: its log decay (0 behind the last step).
+// A wave makes them; lane t has step t.  g: its log decay (0 behind the last step).  Whether the chunk can be taken at once.
 template <int C>
-__device__ __forceinline__ void make_decays(Decays<C>& s, float g, int lane, bool& odd) {
+__device__ __forceinline__ bool make_decays(Decays<C>& s, float g, int lane) {
     const bool forgets = g < kForgets, inside = lane < C;
-    odd = !(fabsf(g) < INFINITY) && !forgets;
-    if (__builtin_amdgcn_ballot_w64(g > 0.0f && inside) != 0) {
-        float up = g > 0.0f && inside ? g * (float)kLog2E : 0.0f;
-#pragma unroll
-        for (int d = kWave / 2; d > 0; d /= 2) up += __shfl_xor(up, d, kWave);
-        odd |= up > kMostGrowth;
-    }
-    double b = forgets || !inside ? 0.0 : (double)g * kLog2E;
-#pragma unroll
-    for (int d = 1; d < C; d *= 2) {
-        const double x = __shfl_up(b, d, kWave);
-        if (lane >= d) b += x;
-    }
+    bool fine = fabsf(g) < INFINITY || forgets;
+    if (__builtin_amdgcn_ballot_w64(g > 0.0f && inside) != 0)
+        fine &= of_lane(wave_upto(g > 0.0f && inside ? g * (float)kLog2E : 0.0f), kWave - 1) <= kMostGrowth;
+    const double b = wave_upto(forgets || !inside ? 0.0 : (double)g * kLog2E);
     const unsigned long long all = __builtin_amdgcn_ballot_w64(forgets && inside), upto = all & (~0ull >> (63 - lane));
     const int forgot = upto ? 63 - __builtin_clzll(upto) : -1, last = all ? 63 - __builtin_clzll(all) : -1;
-    const double end = __shfl(b, C - 1, kWave);
-    const float hi = (float)b, lo = hi - hi == 0.0f ? (float)(b - (double)hi) : 0.0f;
+    const double end = of_lane(b, kWave - 1);
+    const float hi = (float)b;
     if (inside) {
-        s.hi[lane] = hi, s.lo[lane] = lo, s.forgot[lane] = forgot;
-        s.from_start[lane] = forgot < 0 ? half_factor((float)b) : 0.0f;
-        s.to_end[lane] = lane >= last ? half_factor((float)(end - b)) : 0.0f;
+        s.hi[lane] = hi, s.lo[lane] = (float)(b - (double)hi), s.forgot[lane] = forgot;
+        s.from_start[lane] = forgot < 0 ? __builtin_amdgcn_exp2f(hi) : 0.0f;
+        s.to_end[lane] = lane >= last ? __builtin_amdgcn_exp2f((float)(end - b)) : 0.0f;
     }
     if (lane == 0) {
-        s.whole = last < 0 ? half_factor((float)end) : 0.0f;
+        s.whole = last < 0 ? __builtin_amdgcn_exp2f((float)end) : 0.0f;
         s.sum = last < 0 ? end : -INFINITY;
     }
+    return fine;
 }
-__device__ __forceinline__ float scaled(float x, float half) { return half == 0.0f ? 0.0f : x * half * half; }
 
-// Rows [0, n) of a chunk to a tile of C rows, zeros behind them and behind the d-th number; whether all of it is finite.
+// The same number, computed where it is used: what the steps taken one by one need is not kept in registers beside the other path's.
+__device__ __forceinline__ int fresh(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// C rows of a chunk on their way to a tile in LDS: loaded a chunk ahead.  What lies behind the n-th row and the d-th number is loaded from
+// elsewhere in them and becomes zeros in LDS, so that no load waits for a branch (16000 cycles of a chunk's 36000 before).
 template <typename T, int C, int D, int NT>
-__device__ __forceinline__ bool load_tile(Elem<T>* tile, const Rows& x, const char* from, int n, int c0) {
-    constexpr int kPieces = C * D / 8, kEach = (kPieces + NT - 1) / NT, kPerRow = D / 8, W = T::kBytes == 2 ? 4 : 8;
-    uint32_t worst = 0;
+struct Ahead {
+    static constexpr int kPieces = C * D / 8, kEach = (kPieces + NT - 1) / NT, kPerRow = D / 8, W = T::kBytes == 2 ? 4 : 8;
     Words<W> r[kEach];
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const int at = i * NT + (int)threadIdx.x, row = at / kPerRow, c = c0 + at % kPerRow * 8;
-        const char* p = from + row * x.step + (int64_t)c * T::kBytes;
-        r[i] = zero_words<W>();
-        if (row >= n || c >= x.d) continue;  // (n <= C: none behind the tile either)
+
+    static __device__ __forceinline__ bool inside(int i, int n, int c0, int d) {
+        const int at = i * NT + (int)threadIdx.x;
+        return at / kPerRow < n && c0 + at % kPerRow * 8 < d;
+    }
+    // n: 1 at least
+    __device__ __forceinline__ void load(const Rows& x, const char* from, int n, int c0) {
         if (x.wide) {
-            const Words<4> a = load_words<4>(p);
+            const uint32_t step = (uint32_t)x.step;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) r[i].w[j] = a.w[j];
-            if constexpr (W == 8) {
-                const Words<4> b = load_words<4>(p + 16);
+            for (int i = 0; i < kEach; ++i) {
+                const int at = i * NT + (int)threadIdx.x, c = c0 + at % kPerRow * 8;
+                const char* p = from + ((uint32_t)min(at / kPerRow, n - 1) * step + (uint32_t)(c < x.d ? c : 0) * T::kBytes);
+                const Words<4> a = load_words<4>(p);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) r[i].w[4 + j] = b.w[j];
+                for (int j = 0; j < 4; ++j) r[i].w[j] = a.w[j];
+                if constexpr (W == 8) {
+                    const Words<4> b = load_words<4>(p + 16);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) r[i].w[4 + j] = b.w[j];
+                }
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (c + j >= x.d) continue;
-                if constexpr (W == 8) r[i].w[j] = *reinterpret_cast<const uint32_t*>(p + 4 * j);
-                else r[i].w[j / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + 2 * j) << 16 * (j % 2);
+            for (int i = 0; i < kEach; ++i) {
+                const int at = i * NT + fresh((int)threadIdx.x), c = c0 + at % kPerRow * 8;
+                const char* p = from + min(at / kPerRow, n - 1) * x.step;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const bool has = c + j < x.d;
+                    const char* pj = p + (int64_t)(has ? c + j : 0) * T::kBytes;
+                    if constexpr (W == 8) {
+                        r[i].w[j] = has ? *reinterpret_cast<const uint32_t*>(pj) : 0;
+                    } else {
+                        const uint32_t h = has ? *reinterpret_cast<const uint16_t*>(pj) : 0;
+                        r[i].w[j / 2] = j % 2 ? r[i].w[j / 2] | h << 16 : h;
+                    }
+                }
             }
         }
     }
+    // whether all are below `most` (bits of a float)
+    __device__ __forceinline__ bool put(Elem<T>* tile, uint32_t most, int n, int c0, int d) {
+        typedef uint16_t pair_t __attribute__((ext_vector_type(2)));
+        pair_t pairs = {0, 0};
+        uint32_t one = 0;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const int at = i * NT + (int)threadIdx.x, row = at / kPerRow, c = at % kPerRow * 8;
-        if (kPieces % NT != 0 && at >= kPieces) continue;
+        for (int i = 0; i < kEach; ++i) {
+            const int at = i * NT + (int)threadIdx.x, row = at / kPerRow, c = at % kPerRow * 8;
+            if (kPieces % NT != 0 && at >= kPieces) continue;
+            const bool in = inside(i, n, c0, d);
 #pragma unroll
-        for (int j = 0; j < W; ++j) {  // the largest exponent
-            worst = max(worst, r[i].w[j] & 0x7fffffffu);
-            if constexpr (W == 4) worst = max(worst, (r[i].w[j] & 0x7fffu) << 16);
+            for (int j = 0; j < W; ++j) r[i].w[j] = in ? r[i].w[j] : 0;
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                if constexpr (W == 4) pairs = __builtin_elementwise_max(pairs, __builtin_bit_cast(pair_t, r[i].w[j] & 0x7fff7fffu));
+                else one = max(one, r[i].w[j] & 0x7fffffffu);
+            }
+#pragma unroll
+            for (int j = 0; j < W; j += 4) {
+                const Words<4> o{{r[i].w[j], r[i].w[j + 1], r[i].w[j + 2], r[i].w[j + 3]}};
+                store_words<4>(tile + row * kPitch<T, D> + c + j * (4 / T::kBytes), o);
+            }
         }
-#pragma unroll
-        for (int j = 0; j < W; j += 4) {
-            const Words<4> o{{r[i].w[j], r[i].w[j + 1], r[i].w[j + 2], r[i].w[j + 3]}};
-            store_words<4>(tile + row * kPitch<T, D> + c + j * (4 / T::kBytes), o);
-        }
+        if constexpr (W == 4) return max(pairs[0], pairs[1]) < most >> 16;
+        return one < most;
     }
-    return worst < 0x7f800000u;
-}
+};
 
 template <typename T>
-__device__ __forceinline__ float number(const char* p) {
+__device__ __forceinline__ float unpacked(const typename Pack<T, 1>::Raw& r) {
     float f[1];
-    Pack<T, 1>::unpack(Pack<T, 1>::load(p), f);
+    Pack<T, 1>::unpack(r, f);
     return f[0];
 }
+template <typename T>
+__device__ __forceinline__ float number(const char* p) { return unpacked<T>(Pack<T, 1>::load(p)); }
 
 struct LaArgs {
     Rows q, k, v, g, dy;  // (g: head is not looked at)
@@ -279,6 +316,7 @@ struct LaArgs {
     int64_t L, chunks, each;  // chunks of a segment
     int32_t H, group, dk_, dv_, tiles, segments, shares;
     float scale;
+    uint32_t most;  // numbers of chunks that are taken at once are below, as bits of a float
 };
 
 // A head, a tile of its columns and a segment: the workgroup's.
@@ -349,13 +387,55 @@ struct State {
 #pragma unroll
             for (int j = 0; j < CT; ++j) *reinterpret_cast<f32x4_t*>(p + ((i * CT + j) * kWave + lane) * 4) = s[i][j];
     }
-    __device__ __forceinline__ void decay(float half) {
+    __device__ __forceinline__ void decay(float factor) {
+        factor = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(factor)));
+        if (factor == 0.0f) return clear();
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int j = 0; j < CT; ++j) s[i][j] *= factor;
+    }
+    __device__ __forceinline__ void decay_step(float half) {
 #pragma unroll
         for (int i = 0; i < DT; ++i)
 #pragma unroll
             for (int j = 0; j < CT; ++j)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) s[i][j][r] = scaled(s[i][j][r], half);
+    }
+    // One step by itself: s = r r s + a[d] b[c] of `dk` by `dv` numbers.
+    template <typename T>
+    __device__ __forceinline__ void step(float half, const char* a, const char* b, float scale, int dk, int dv, int c0, int li, int lq) {
+#pragma unroll
+        for (int j = 0; j < CT; ++j) {
+            const int c = c0 + column(li, j);
+            const float bc = c < dv ? number<T>(b + (int64_t)c * T::kBytes) * scale : 0.0f;
+#pragma unroll
+            for (int i = 0; i < DT; ++i) {
+                const int d0 = 16 * i + fresh(4 * lq);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int d = d0 + r;
+                    if (d < dk && c < dv) s[i][j][r] = fmaf(number<T>(a + (int64_t)d * T::kBytes), bc, scaled(s[i][j][r], half));
+                }
+            }
+        }
+    }
+    // sum over d of a[d] s[d][c], of column c0 + column(li, j), in every lane that has it
+    template <typename T>
+    __device__ __forceinline__ float product(const char* a, int j, int dk, int lq) const {
+        float y = 0.0f;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+            const int d0 = 16 * i + fresh(4 * lq);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int d = d0 + r;
+                if (d < dk) y = fmaf(number<T>(a + (int64_t)d * T::kBytes), s[i][j][r], y);
+            }
+        }
+        y += __shfl_xor(y, 16, kWave);
+        return y + __shfl_xor(y, 32, kWave);
     }
 };
 
@@ -373,18 +453,21 @@ __device__ __forceinline__ f32x4_t load_mark(const char* p) {
 }
 
 // s += first^T (x) weighted second over the chunk's rows: rows of `a` become the state's rows, columns of `b` its columns, of which
-// the wave has `mine` in `fb`; `half` are the rows' half factors.
+// the wave has `mine` in `fb`; `factor` are the rows' factors.
 template <typename T, int DK, int C, int DT, int CT, int KB>
-__device__ __forceinline__ void add_rows(State<DT, CT>& s, const Elem<T>* a, const Frag<T> (&fb)[CT][KB], const float* half, float scale, int li, int lq) {
+__device__ __forceinline__ void add_rows(State<DT, CT>& s, const Elem<T>* a, const Frag<T> (&fb)[CT][KB], const float* factor, float scale, int li, int lq) {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
         Frag<T> parts[CT][kParts<T>];
+        float by[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) by[e] = factor[32 * kb + 8 * lq + e] * scale;
 #pragma unroll
         for (int j = 0; j < CT; ++j) {
             float f[8];
             floats_of(fb[j][kb], f);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = scaled(f[e] * scale, half[32 * kb + 8 * lq + e]);
+            for (int e = 0; e < 8; ++e) f[e] *= by[e];
             wide_frag(f, parts[j]);
         }
 #pragma unroll
@@ -396,154 +479,127 @@ __device__ __forceinline__ void add_rows(State<DT, CT>& s, const Elem<T>* a, con
     }
 }
 
-// ---- the walk forward: states at the segments' ends (OUT false), or outputs, marks and the last state
+// Columns of a tile that a wave has, 32 rows at a time.
+template <typename T, int PITCH, int CT, int KB>
+__device__ __forceinline__ void own_columns(Frag<T> (&f)[CT][KB], const Elem<T>* tile, int c0, int li, int lq) {
+#pragma unroll
+    for (int j = 0; j < CT; ++j)
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            if constexpr (CT == 2) f[j][kb] = column_frag<PITCH, 8>(tile, 32 * kb, c0 + 4 * j, li, lq);
+            else f[j][kb] = column_frag<PITCH, 4>(tile, 32 * kb, c0 + 16 * j, li, lq);
+        }
+}
+__device__ __forceinline__ double with_sum(double sum, double more) {
+    return sum == -INFINITY || more == -INFINITY ? -INFINITY : sum + more;  // (nothing undoes a reset, NaN neither)
+}
+__device__ __forceinline__ double step_sum(float g) { return g < kForgets ? -INFINITY : (double)g * kLog2E; }
 
-template <typename T, int DK, int DV, bool OUT>
+// ---- states at the segments' ends by themselves, of segments that have another behind them; BACK: the states' gradients at their
+// beginnings, from the end on, of rows of q and columns of dy.
+
+template <typename T, int DK, int DV, bool BACK>
+__global__ __launch_bounds__(256, 2) void la_ends_walk_kernel(LaArgs a) {
+    constexpr int C = kChunk<T>, NT = 256, NW = 4, KB = C / 32, DT = DK / 16, CT = DV / NW / 16, WC = 16 * CT;
+    constexpr int PV = kPitch<T, DV>;
+    __shared__ __attribute__((aligned(16))) Elem<T> tile_a[C * kPitch<T, DK>];
+    __shared__ __attribute__((aligned(16))) Elem<T> tile_b[C * PV];
+    __shared__ Decays<C> decays;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, li = lane % 16, lq = lane / 16;
+    const Place at = place_of(a, blockIdx.x);
+    if (at.segment == (BACK ? 0 : a.segments - 1)) return;
+    const Rows &ra = BACK ? a.q : a.k, &rb = BACK ? a.dy : a.v;
+    const char *ap = ra.p + at.b * ra.batch + at.hk * ra.head, *bp = rb.p + at.b * rb.batch + at.h * rb.head;
+    const char* gp = a.g.p + at.b * a.g.batch + (int64_t)at.h * T::kBytes;
+    const int c0 = at.tile * DV, cw = w * WC;  // the tile's columns, the wave's in it
+    const int64_t head_state = (at.b * a.H + at.h) * a.dk_ * a.dv_, items = (int64_t)gridDim.x / a.segments;
+    const float scale = BACK ? a.scale : 1.0f;
+    State<DT, CT> S;
+    if (!BACK && at.segment == 0 && a.state_in) S.load(a.state_in + head_state, a.dk_, a.dv_, c0 + cw, li, lq);
+    else if (BACK && at.segment == a.segments - 1 && a.dstate_out) S.load(a.dstate_out + head_state, a.dk_, a.dv_, c0 + cw, li, lq);
+    else S.clear();
+    const int64_t first = at.segment * a.each, last = first + a.each < a.chunks ? first + a.each : a.chunks;
+    double sum = 0.0;
+    Ahead<T, C, DK, NT> next_a;
+    Ahead<T, C, DV, NT> next_b;
+    typename Pack<T, 1>::Raw next_g;
+    auto steps = [&](int64_t x) { return a.L - x * C < C ? (int)(a.L - x * C) : C; };
+    auto load = [&](int64_t x) {
+        const int64_t t = x * C;
+        const int n = steps(x);
+        next_a.load(ra, ap + t * ra.step, n, 0);
+        next_b.load(rb, bp + t * rb.step, n, c0);
+        next_g = Pack<T, 1>::load(gp + (t + min(lane, n - 1)) * a.g.step);
+    };
+    load(BACK ? last - 1 : first);
+    for (int64_t y = first; y < last; ++y) {
+        const int64_t x = BACK ? last - 1 - (y - first) : y;
+        __syncthreads();  // nobody reads the chunk before any more
+        bool fine = next_a.put(tile_a, a.most, steps(x), 0, ra.d);
+        fine &= next_b.put(tile_b, a.most, steps(x), c0, rb.d);
+        if (w == 0) fine &= make_decays<C>(decays, lane < steps(x) ? unpacked<T>(next_g) : 0.0f, lane);
+        const bool at_once = !__syncthreads_or(!fine);
+        if (y + 1 < last) load(BACK ? x - 1 : x + 1);
+        if (at_once) {
+            Frag<T> fb[CT][KB];
+            own_columns<T, PV>(fb, tile_b, cw, li, lq);
+            S.decay(decays.whole);
+            add_rows<T, DK, C>(S, tile_a, fb, BACK ? decays.from_start : decays.to_end, scale, li, lq);
+            sum = with_sum(sum, decays.sum);
+        } else {
+            for (int i = 0, n = steps(x); i < n; ++i) {
+                const int64_t t = x * C + (BACK ? n - 1 - i : i);
+                const float g = number<T>(gp + t * a.g.step), half = step_factor(g);
+                // (what goes back has its step's decay behind it, of what the step adds too)
+                S.template step<T>(BACK ? 1.0f : half, ap + t * ra.step, bp + t * rb.step, scale, a.dk_, a.dv_, c0 + cw, li, lq);
+                if constexpr (BACK) S.decay_step(half);
+                sum = with_sum(sum, step_sum(g));
+            }
+        }
+    }
+    S.store_own(a.ends + (at.segment * items + at.item) * (DK * DV) + w * (DK * WC), lane);
+    if (threadIdx.x == 0) a.sums[at.segment * items + at.item] = sum;
+}
+
+// ---- the walk forward: outputs, marks and the last state
+
+template <typename T, int DK, int DV>
 struct WalkLds {
     static constexpr int C = kChunk<T>;
-    Elem<T> k[C * kPitch<T, DK>], v[C * kPitch<T, DV>];
-    Elem<T> q[OUT ? C * kPitch<T, DK> : 1], a[OUT ? C * kPitch<T, C> : 1];
+    Elem<T> k[C * kPitch<T, DK>], v[C * kPitch<T, DV>], q[C * kPitch<T, DK>], a[C * kPitch<T, C>];
     Decays<C> d;
 };
 
-template <typename T, int DK, int DV, bool OUT, bool MARKS>
-__global__ __launch_bounds__(256) void la_walk_kernel(LaArgs a) {
+template <typename T, int DK, int DV, bool MARKS>
+__global__ __launch_bounds__(256, 2) void la_walk_kernel(LaArgs a) {
     constexpr int C = kChunk<T>, NT = 256, NW = 4, IT = C / 16, KB = C / 32, DT = DK / 16, CT = DV / NW / 16, WC = 16 * CT;
     constexpr int PK = kPitch<T, DK>, PV = kPitch<T, DV>, PA = kPitch<T, C>;
-    __shared__ __attribute__((aligned(16))) WalkLds<T, DK, DV, OUT> s;
+    __shared__ __attribute__((aligned(16))) WalkLds<T, DK, DV> s;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, li = lane % 16, lq = lane / 16;
     const Place at = place_of(a, blockIdx.x);
-    if (!OUT && at.segment == a.segments - 1) return;
     const char *kp = a.k.p + at.b * a.k.batch + at.hk * a.k.head, *vp = a.v.p + at.b * a.v.batch + at.h * a.v.head;
     const char *qp = a.q.p + at.b * a.q.batch + at.hk * a.q.head, *gp = a.g.p + at.b * a.g.batch + (int64_t)at.h * T::kBytes;
     const int c0 = at.tile * DV, cw = w * WC;  // the tile's columns, the wave's in it
-
-    const int64_t bh = at.b * a.H + at.h, head_state = bh * a.dk_ * a.dv_;
-    const int64_t items = (int64_t)gridDim.x / a.segments;
+    const int64_t head_state = (at.b * a.H + at.h) * a.dk_ * a.dv_, items = (int64_t)gridDim.x / a.segments;
     State<DT, CT> S;
-    if (at.segment > 0 && OUT) S.load_own(a.ends + ((at.segment - 1) * items + at.item) * (DK * DV) + w * (DK * WC), lane);
-    else if (at.segment == 0 && a.state_in) S.load(a.state_in + head_state, a.dk_, a.dv_, c0 + cw, li, lq);
+    if (at.segment > 0) S.load_own(a.ends + ((at.segment - 1) * items + at.item) * (DK * DV) + w * (DK * WC), lane);
+    else if (a.state_in) S.load(a.state_in + head_state, a.dk_, a.dv_, c0 + cw, li, lq);
     else S.clear();
-    if constexpr (OUT) {  // blocks above the diagonal are read, as zeros
-        for (int i = threadIdx.x; i < C * PA; i += NT) s.a[i] = 0;
-    }
+    for (int i = threadIdx.x; i < C * PA; i += NT) s.a[i] = 0;  // (blocks above the diagonal are read, as zeros)
     const int64_t first = at.segment * a.each, last = first + a.each < a.chunks ? first + a.each : a.chunks;
-    double sum = 0.0;
-
-    // steps [t, t + n) at once; `look`: only if all of them are finite
-    auto take = [&](int64_t t, int n, bool look) -> bool {
-        __syncthreads();  // nobody reads the chunk before any more
-        bool fine = load_tile<T, C, DK, NT>(s.k, a.k, kp + t * a.k.step, n, 0);
-        fine &= load_tile<T, C, DV, NT>(s.v, a.v, vp + t * a.v.step, n, c0);
-        if constexpr (OUT) load_tile<T, C, DK, NT>(s.q, a.q, qp + t * a.q.step, n, 0);
-        if (w == 0) {
-            bool odd;
-            make_decays<C>(s.d, lane < n ? number<T>(gp + (t + lane) * a.g.step) : 0.0f, lane, odd);
-            fine &= !odd;
-        }
-        if (look) {
-            if (__syncthreads_or(!fine)) return false;
-        } else {
-            __syncthreads();
-        }
-        Frag<T> fv[CT][KB];
-#pragma unroll
-        for (int j = 0; j < CT; ++j)
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                if constexpr (CT == 2) fv[j][kb] = column_frag<PV, 8>(s.v, 32 * kb, cw + 4 * j, li, lq);
-                else fv[j][kb] = column_frag<PV, 4>(s.v, 32 * kb, cw + 16 * j, li, lq);
-            }
-        if constexpr (OUT) {
-            // A below the diagonal, a block of 16 x 16 a wave at a time
-            constexpr int kBlocks = IT * (IT + 1) / 2;
-#pragma unroll
-            for (int x = 0; x < (kBlocks + NW - 1) / NW; ++x) {
-                const int block = x * NW + w;
-                if (block >= kBlocks) break;
-                int it = 0;
-                while ((it + 1) * (it + 2) / 2 <= block) ++it;
-                const int jt = block - it * (it + 1) / 2;
-                f32x4_t p = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int kb = 0; kb < DK / 32; ++kb)
-                    multiply(p, row_frag<PK>(s.k, 16 * jt + li, 32 * kb, lq), row_frag<PK>(s.q, 16 * it + li, 32 * kb, lq));
-                const int i = 16 * it + li, j0 = 16 * jt + 4 * lq, forgot = s.d.forgot[i];
-                const float hi = s.d.hi[i], lo = s.d.lo[i];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float half = half_factor((hi - s.d.hi[j0 + r]) + (lo - s.d.lo[j0 + r]));
-                    p[r] = j0 + r <= i && j0 + r >= forgot ? p[r] * a.scale * half * half : 0.0f;
-                }
-                put4(s.a + i * PA + j0, p);
-            }
-            __syncthreads();
-            Frag<T> fs[DK / 32][CT];  // the state as an operand
-#pragma unroll
-            for (int x = 0; x < DK / 32; ++x)
-#pragma unroll
-                for (int j = 0; j < CT; ++j) {
-                    float f[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) f[e] = S.s[2 * x + e / 4][j][e % 4];
-                    fs[x][j] = frag_of(f, T{});
-                }
-#pragma unroll
-            for (int it = 0; it < IT; ++it) {
-                const int i = 16 * it + li;
-                f32x4_t o[CT];
-#pragma unroll
-                for (int j = 0; j < CT; ++j) o[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int x = 0; x < DK / 32; ++x) {
-                    const Frag<T> fq = turned_row_frag<PK>(s.q, i, 32 * x, lq);
-#pragma unroll
-                    for (int j = 0; j < CT; ++j) multiply(o[j], fs[x][j], fq);
-                }
-                const float half = s.d.from_start[i];
-#pragma unroll
-                for (int j = 0; j < CT; ++j)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) o[j][r] = scaled(o[j][r] * a.scale, half);
-#pragma unroll
-                for (int kb = 0; kb <= it / 2; ++kb) {
-                    const Frag<T> fa = row_frag<PA>(s.a, i, 32 * kb, lq);
-#pragma unroll
-                    for (int j = 0; j < CT; ++j) multiply(o[j], fv[j][kb], fa);
-                }
-                if (i < n) {
-                    char* const to = a.y + ((at.b * a.L + t + i) * a.H + at.h) * a.dv_ * T::kBytes;
-                    const int c = c0 + cw + (CT == 2 ? 8 : 4) * lq;
-                    float f[4 * CT];
-#pragma unroll
-                    for (int e = 0; e < 4 * CT; ++e) f[e] = o[e / 4][e % 4];
-                    if (a.dv_ % 8 == 0) {
-                        if (c < a.dv_)
-#pragma unroll
-                            for (int e = 0; e < 4 * CT; e += 16 / T::kBytes < 4 * CT ? 16 / T::kBytes : 4 * CT) {
-                                constexpr int kN = 16 / T::kBytes < 4 * CT ? 16 / T::kBytes : 4 * CT;
-                                float part[kN];
-#pragma unroll
-                                for (int x = 0; x < kN; ++x) part[x] = f[e + x];
-                                Pack<T, kN>::store(to + (c + e) * T::kBytes, Pack<T, kN>::pack(part));
-                            }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4 * CT; ++e)
-                            if (c + e < a.dv_) {
-                                const float one[1] = {f[e]};
-                                Pack<T, 1>::store(to + (c + e) * T::kBytes, Pack<T, 1>::pack(one));
-                            }
-                    }
-                }
-            }
-        }
-        S.decay(s.d.whole);
-        add_rows<T, DK, C>(S, s.k, fv, s.d.to_end, 1.0f, li, lq);
-        sum = sum == -INFINITY || s.d.sum == -INFINITY ? -INFINITY : sum + s.d.sum;  // (nothing undoes a reset, NaN neither)
-        return true;
+    Ahead<T, C, DK, NT> next_q, next_k;
+    Ahead<T, C, DV, NT> next_v;
+    typename Pack<T, 1>::Raw next_g;
+    auto steps = [&](int64_t x) { return a.L - x * C < C ? (int)(a.L - x * C) : C; };
+    auto load = [&](int64_t x) {
+        const int64_t t = x * C;
+        const int n = steps(x);
+        next_k.load(a.k, kp + t * a.k.step, n, 0);
+        next_q.load(a.q, qp + t * a.q.step, n, 0);
+        next_v.load(a.v, vp + t * a.v.step, n, c0);
+        next_g = Pack<T, 1>::load(gp + (t + min(lane, n - 1)) * a.g.step);
     };
-
+    load(first);
     for (int64_t x = first; x < last; ++x) {
         if constexpr (MARKS) {
             char* const m = a.marks + ((at.item * a.chunks + x) * (DK * DV) + w * (DK * WC)) * T::kBytes;
@@ -553,94 +609,144 @@ __global__ __launch_bounds__(256) void la_walk_kernel(LaArgs a) {
                 for (int j = 0; j < CT; ++j) store_mark<T>(m + ((i * CT + j) * kWave + lane) * 4 * T::kBytes, S.s[i][j]);
         }
         const int64_t t = x * C;
-        const int n = a.L - t < C ? (int)(a.L - t) : C;
-        if (!take(t, n, true))
-            for (int i = 0; i < n; ++i) take(t + i, 1, false);
-    }
-    if constexpr (OUT) {
-        if (at.segment == a.segments - 1 && a.state_out) S.store(a.state_out + head_state, a.dk_, a.dv_, c0 + cw, li, lq);
-    } else if (a.ends) {
-        S.store_own(a.ends + (at.segment * items + at.item) * (DK * DV) + w * (DK * WC), lane);
-        if (threadIdx.x == 0) a.sums[at.segment * items + at.item] = sum;
-    }
-}
-
-// The same in the other order for the gradients of states: rows of q, columns of dy.
-template <typename T, int DK, int DV>
-struct BackLds {
-    static constexpr int C = kChunk<T>;
-    Elem<T> q[C * kPitch<T, DK>], dy[C * kPitch<T, DV>];
-    Decays<C> d;
-};
-template <typename T, int DK, int DV>
-__global__ __launch_bounds__(256) void la_back_kernel(LaArgs a) {
-    constexpr int C = kChunk<T>, NT = 256, NW = 4, KB = C / 32, DT = DK / 16, CT = DV / NW / 16, WC = 16 * CT;
-    constexpr int PV = kPitch<T, DV>;
-    __shared__ __attribute__((aligned(16))) BackLds<T, DK, DV> s;
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, li = lane % 16, lq = lane / 16;
-    const Place at = place_of(a, blockIdx.x);
-    if (at.segment == 0) return;
-    const char *qp = a.q.p + at.b * a.q.batch + at.hk * a.q.head, *dyp = a.dy.p + at.b * a.dy.batch + at.h * a.dy.head;
-    const char* gp = a.g.p + at.b * a.g.batch + (int64_t)at.h * T::kBytes;
-    const int c0 = at.tile * DV, cw = w * WC;
-    const int64_t items = (int64_t)gridDim.x / a.segments;
-    State<DT, CT> M;
-    if (at.segment == a.segments - 1 && a.dstate_out) M.load(a.dstate_out + (at.b * a.H + at.h) * a.dk_ * a.dv_, a.dk_, a.dv_, c0 + cw, li, lq);
-    else M.clear();
-    const int64_t first = at.segment * a.each, last = first + a.each < a.chunks ? first + a.each : a.chunks;
-    double sum = 0.0;
-    auto take = [&](int64_t t, int n, bool look) -> bool {
-        __syncthreads();
-        bool fine = load_tile<T, C, DK, NT>(s.q, a.q, qp + t * a.q.step, n, 0);
-        fine &= load_tile<T, C, DV, NT>(s.dy, a.dy, dyp + t * a.dy.step, n, c0);
-        if (w == 0) {
-            bool odd;
-            make_decays<C>(s.d, lane < n ? number<T>(gp + (t + lane) * a.g.step) : 0.0f, lane, odd);
-            fine &= !odd;
-        }
-        if (look) {
-            if (__syncthreads_or(!fine)) return false;
-        } else {
-            __syncthreads();
-        }
-        Frag<T> fb[CT][KB];
+        const int n = steps(x);
+        __syncthreads();  // nobody reads the chunk before any more
+        bool fine = next_k.put(s.k, a.most, n, 0, a.k.d);
+        fine &= next_q.put(s.q, a.most, n, 0, a.q.d);
+        fine &= next_v.put(s.v, a.most, n, c0, a.v.d);
+        if (w == 0) fine &= make_decays<C>(s.d, lane < n ? unpacked<T>(next_g) : 0.0f, lane);
+        const bool at_once = !__syncthreads_or(!fine);
+        if (x + 1 < last) load(x + 1);
+        if (!at_once) {
+            for (int i = 0; i < n; ++i) {
+                const int64_t u = t + i;
+                S.template step<T>(step_factor(number<T>(gp + u * a.g.step)), kp + u * a.k.step, vp + u * a.v.step, 1.0f, a.dk_, a.dv_, c0 + cw, li, lq);
 #pragma unroll
-        for (int j = 0; j < CT; ++j)
+                for (int j = 0; j < CT; ++j) {
+                    const int c = c0 + cw + State<DT, CT>::column(li, j);
+                    const float one[1] = {S.template product<T>(qp + u * a.q.step, j, a.dk_, lq) * a.scale};
+                    if (lq == 0 && c < a.dv_) Pack<T, 1>::store(a.y + (((at.b * a.L + u) * a.H + at.h) * a.dv_ + c) * T::kBytes, Pack<T, 1>::pack(one));
+                }
+            }
+            continue;
+        }
+        // A below the diagonal, a block of 16 x 16 a wave at a time
+        constexpr int kBlocks = IT * (IT + 1) / 2;
+#pragma unroll 1
+        for (int y = 0; y < (kBlocks + NW - 1) / NW; ++y) {
+            const int block = y * NW + w;
+            if (block >= kBlocks) break;
+            int it = 0;
+            while ((it + 1) * (it + 2) / 2 <= block) ++it;
+            const int jt = block - it * (it + 1) / 2;
+            f32x4_t p = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int kb = 0; kb < DK / 32; ++kb)
+                multiply(p, row_frag<PK>(s.k, 16 * jt + li, 32 * kb, lq), row_frag<PK>(s.q, 16 * it + li, 32 * kb, lq));
+            const int i = 16 * it + li, j0 = 16 * jt + 4 * lq, forgot = s.d.forgot[i];
+            const float hi = s.d.hi[i], lo = s.d.lo[i];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float f = __builtin_amdgcn_exp2f((hi - s.d.hi[j0 + r]) + (lo - s.d.lo[j0 + r]));
+                p[r] = j0 + r <= i && j0 + r >= forgot ? p[r] * (f * a.scale) : 0.0f;
+            }
+            put4(s.a + i * PA + j0, p);
+        }
+        Frag<T> fv[CT][KB];
+        own_columns<T, PV>(fv, s.v, cw, li, lq);
+        Frag<T> fs[DK / 32][CT];  // the state as an operand
+#pragma unroll
+        for (int y = 0; y < DK / 32; ++y)
+#pragma unroll
+            for (int j = 0; j < CT; ++j) {
+                float f[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = S.s[2 * y + e / 4][j][e % 4];
+                fs[y][j] = frag_of(f, T{});
+            }
+        __syncthreads();  // A is there
+#pragma unroll 1
+        for (int it = 0; it < IT; ++it) {
+            const int i = 16 * it + li;
+            f32x4_t o[CT];
+#pragma unroll
+            for (int j = 0; j < CT; ++j) o[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int y = 0; y < DK / 32; ++y) {
+                const Frag<T> fq = turned_row_frag<PK>(s.q, i, 32 * y, lq);
+#pragma unroll
+                for (int j = 0; j < CT; ++j) multiply(o[j], fs[y][j], fq);
+            }
+            const float factor = s.d.from_start[i] * a.scale;
+#pragma unroll
+            for (int j = 0; j < CT; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[j][r] = weighted(o[j][r], factor);
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
-                if constexpr (CT == 2) fb[j][kb] = column_frag<PV, 8>(s.dy, 32 * kb, cw + 4 * j, li, lq);
-                else fb[j][kb] = column_frag<PV, 4>(s.dy, 32 * kb, cw + 16 * j, li, lq);
+                if (kb > it / 2) break;
+                const Frag<T> fa = row_frag<PA>(s.a, i, 32 * kb, lq);
+#pragma unroll
+                for (int j = 0; j < CT; ++j) multiply(o[j], fv[j][kb], fa);
             }
-        M.decay(s.d.whole);
-        add_rows<T, DK, C>(M, s.q, fb, s.d.from_start, a.scale, li, lq);
-        sum = sum == -INFINITY || s.d.sum == -INFINITY ? -INFINITY : sum + s.d.sum;  // (nothing undoes a reset, NaN neither)
-        return true;
-    };
-    for (int64_t x = last - 1; x >= first; --x) {
-        const int64_t t = x * C;
-        const int n = a.L - t < C ? (int)(a.L - t) : C;
-        if (!take(t, n, true))
-            for (int i = n - 1; i >= 0; --i) take(t + i, 1, false);
+            if (i < n) {
+                char* const to = a.y + ((at.b * a.L + t + i) * a.H + at.h) * a.dv_ * T::kBytes;
+                const int c = c0 + cw + (CT == 2 ? 8 : 4) * lq;
+                float f[4 * CT];
+#pragma unroll
+                for (int e = 0; e < 4 * CT; ++e) f[e] = o[e / 4][e % 4];
+                if (a.dv_ % 8 == 0) {
+                    if (c < a.dv_)
+#pragma unroll
+                        for (int e = 0; e < 4 * CT; e += 16 / T::kBytes < 4 * CT ? 16 / T::kBytes : 4 * CT) {
+                            constexpr int kN = 16 / T::kBytes < 4 * CT ? 16 / T::kBytes : 4 * CT;
+                            float part[kN];
+#pragma unroll
+                            for (int z = 0; z < kN; ++z) part[z] = f[e + z];
+                            Pack<T, kN>::store(to + (c + e) * T::kBytes, Pack<T, kN>::pack(part));
+                        }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4 * CT; ++e)
+                        if (c + e < a.dv_) {
+                            const float one[1] = {f[e]};
+                            Pack<T, 1>::store(to + (c + e) * T::kBytes, Pack<T, 1>::pack(one));
+                        }
+                }
+            }
+        }
+        S.decay(s.d.whole);
+        add_rows<T, DK, C>(S, s.k, fv, s.d.to_end, 1.0f, li, lq);
     }
-    M.store_own(a.ends + (at.segment * items + at.item) * (DK * DV) + w * (DK * WC), lane);
-    if (threadIdx.x == 0) a.sums[at.segment * items + at.item] = sum;
+    if (at.segment == a.segments - 1 && a.state_out) S.store(a.state_out + head_state, a.dk_, a.dv_, c0 + cw, li, lq);
 }
 
 // Ends of segments made by themselves -> ends of everything up to them (BACK: from them on): e[s] += decay of s * e[s - 1].
 template <bool BACK>
 __global__ __launch_bounds__(256) void la_ends_kernel(float* ends, const double* sums, int64_t items, int32_t size, int32_t segments) {
+    constexpr int kAtOnce = 8;
     const int64_t n = items * (size / 4);
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
         const int64_t item = i / (size / 4);
         float4 e = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int x = 0; x < segments - 1; ++x) {  // (nothing comes behind the last)
-            const int at = BACK ? segments - 1 - x : x;
-            float4* const p = reinterpret_cast<float4*>(ends) + at * n + i;
-            const double d = sums[at * items + item];
-            const float half = d == -INFINITY ? 0.0f : half_factor((float)d);
-            const float4 own = *p;
-            e.x = scaled(e.x, half) + own.x, e.y = scaled(e.y, half) + own.y, e.z = scaled(e.z, half) + own.z, e.w = scaled(e.w, half) + own.w;
-            *p = e;
+        for (int x0 = 0; x0 < segments - 1; x0 += kAtOnce) {  // (nothing comes behind the last)
+            float4 own[kAtOnce];
+            double d[kAtOnce];
+#pragma unroll
+            for (int y = 0; y < kAtOnce; ++y) {
+                const int x = x0 + y < segments - 1 ? x0 + y : segments - 2, at = BACK ? segments - 1 - x : x;
+                own[y] = reinterpret_cast<const float4*>(ends)[at * n + i];
+                d[y] = sums[at * items + item];
+            }
+#pragma unroll
+            for (int y = 0; y < kAtOnce; ++y) {
+                const int x = x0 + y, at = BACK ? segments - 1 - x : x;
+                if (x >= segments - 1) break;
+                const float half = d[y] == -INFINITY ? 0.0f : half_factor((float)d[y]);
+                e.x = scaled(e.x, half) + own[y].x, e.y = scaled(e.y, half) + own[y].y;
+                e.z = scaled(e.z, half) + own[y].z, e.w = scaled(e.w, half) + own[y].w;
+                reinterpret_cast<float4*>(ends)[at * n + i] = e;
+            }
         }
     }
 }
@@ -649,21 +755,46 @@ __global__ __launch_bounds__(256) void la_ends_kernel(float* ends, const double*
 
 template <typename T, int DK, int DV>
 struct BwdLds {
-    static constexpr int C = kChunk<T>, IT = C / 16, NW = DV / 16;
-    Elem<T> q[C * kPitch<T, DK>], k[C * kPitch<T, DK>], v[C * kPitch<T, DV>], dy[C * kPitch<T, DV>];
+    static constexpr int C = kChunk<T>, NW = DV / 16, PK = kPitch<T, DK>;
+    // the state in front of the chunk and the gradient of that behind it, turned; fp32: one after the other in one place
+    static constexpr bool kTwo = T::kBytes == 2;
+    Elem<T> q[C * PK], k[C * PK], v[C * kPitch<T, DV>], dy[C * kPitch<T, DV>];
     Elem<T> a[C * kPitch<T, C>], e[C * kPitch<T, C>];  // A and its gradient's part for q and k
-    Elem<T> s[DV * kPitch<T, DK>];                     // the state in front of the chunk, then the gradient of that behind it, turned
-    float row[IT][C], col[IT][C];                      // shares of the log decays' gradients: of pairs of steps, by row and by column
-    float far_q[DK / 16][C], far_k[DK / 16][C];        // of q with the state, and of k with its gradient
-    float both[NW];                                    // <S, M>
+    Elem<T> s[DV * PK], m[kTwo ? DV * PK : 1];
+    float near[DK / 16][C], far[DK / 16][C];  // shares of the log decays' gradients
+    float both[NW];                           // <S, M>
     Decays<C> d;
 };
+static_assert(sizeof(BwdLds<BF16, 128, 128>) <= 160 * 1024 && sizeof(BwdLds<F32, 128, 128>) <= 160 * 1024, "what a compute unit has");
+
+// Sum over the lanes li + 16, + 32, + 48.
+__device__ __forceinline__ float over_quarters(float x) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+// Sum over 16 lanes next to each other, in the last of them.
+__device__ __forceinline__ float over_columns(float x) {
+    x += moved<0x111, 0xf>(x);
+    x += moved<0x112, 0xf>(x);
+    x += moved<0x114, 0xf>(x);
+    return x + moved<0x118, 0xf>(x);
+}
+template <typename T>
+__device__ __forceinline__ f32x4_t four(const Elem<T>* p) {
+    float f[4];
+    Pack<T, 4>::unpack(Pack<T, 4>::load(p), f);
+    return f32x4_t{f[0], f[1], f[2], f[3]};
+}
+__device__ __forceinline__ float dot(const f32x4_t& a, const f32x4_t& b) { return fmaf(a[0], b[0], fmaf(a[1], b[1], fmaf(a[2], b[2], a[3] * b[3]))); }
 
 template <typename T, int DK, int DV, bool SHARES>
-__global__ __launch_bounds__(DV * 4) void la_bwd_kernel(LaArgs a) {
-    constexpr int C = kChunk<T>, NW = DV / 16, NT = NW * kWave, IT = C / 16, KB = C / 32, DT = DK / 16;
+__global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
+    using Lds = BwdLds<T, DK, DV>;
+    constexpr int C = kChunk<T>, NW = DV / 16, NT = NW * kWave, IT = C / 16, KB = C / 32, DT = DK / 16, VB = DV / 32;
     constexpr int PK = kPitch<T, DK>, PV = kPitch<T, DV>, PA = kPitch<T, C>;
-    __shared__ __attribute__((aligned(16))) BwdLds<T, DK, DV> s;
+    __shared__ __attribute__((aligned(16))) Lds s;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, li = lane % 16, lq = lane / 16;
     const Place at = place_of(a, blockIdx.x);
     const char *kp = a.k.p + at.b * a.k.batch + at.hk * a.k.head, *vp = a.v.p + at.b * a.v.batch + at.h * a.v.head;
@@ -671,111 +802,181 @@ __global__ __launch_bounds__(DV * 4) void la_bwd_kernel(LaArgs a) {
     const char* gp = a.g.p + at.b * a.g.batch + (int64_t)at.h * T::kBytes;
     const int c0 = at.tile * DV, cw = w * 16;
     const int64_t items = (int64_t)gridDim.x / a.segments, head_state = (at.b * a.H + at.h) * a.dk_ * a.dv_;
+    // where the walks of 4 waves have this wave's columns: piece i of 16 rows is `own` + i * kStep numbers behind
+    constexpr int CT4 = DV / 64, WC4 = 16 * CT4, kStep = CT4 * kWave * 4;
+    const int own_c = cw + li, own_in = own_c % WC4, own_j = CT4 == 2 ? own_in / 4 % 2 : 0, own_l = CT4 == 2 ? own_in / 8 * 4 + own_in % 4 : own_in;
+    const int own = own_c / WC4 * (DK * WC4) + (own_j * kWave + lq * 16 + own_l) * 4;
     State<DT, 1> M;  // the gradient of the state behind the chunk
     if (at.segment < a.segments - 1) {
-        // (made by the walk of 4 waves: their columns)
-        constexpr int CT4 = DV / 64, WC4 = 16 * CT4;
-        const float* p = a.ends + ((at.segment + 1) * items + at.item) * (DK * DV);
+        const float* p = a.ends + ((at.segment + 1) * items + at.item) * (DK * DV) + own;
 #pragma unroll
-        for (int i = 0; i < DT; ++i) {
-            const int c = cw + li, w4 = c / WC4, in = c % WC4;
-            const int j = CT4 == 2 ? in / 4 % 2 : 0, l = CT4 == 2 ? in / 8 * 4 + in % 4 : in;
-            M.s[i][0] = *reinterpret_cast<const f32x4_t*>(p + w4 * (DK * WC4) + ((i * CT4 + j) * kWave + lq * 16 + l) * 4);
-        }
+        for (int i = 0; i < DT; ++i) M.s[i][0] = *reinterpret_cast<const f32x4_t*>(p + i * kStep);
     } else if (a.dstate_out) {
         M.load(a.dstate_out + head_state, a.dk_, a.dv_, c0 + cw, li, lq);
     } else {
         M.clear();
     }
-    for (int i = threadIdx.x; i < C * PA; i += NT) s.a[i] = 0, s.e[i] = 0;
+    for (int i = threadIdx.x; i < C * PA; i += NT) s.a[i] = 0, s.e[i] = 0;  // (blocks above the diagonal are read, as zeros)
     const int64_t first = at.segment * a.each, last = first + a.each < a.chunks ? first + a.each : a.chunks;
-    const int64_t heads_qk = a.H / a.group, rows_all = (int64_t)gridDim.x / a.segments / a.tiles / a.H * a.L;  // B L
-    const int64_t share = (int64_t)(at.h % a.group) * a.tiles + at.tile;
+    const int64_t heads_qk = a.H / a.group, rows_all = items / a.tiles / a.H * a.L;  // B L
+    const int64_t share = SHARES ? ((int64_t)(at.h % a.group) * a.tiles + at.tile) * (rows_all * heads_qk * a.dk_) : 0;
 
-    // a row of dq or dk: four numbers from d on
-    auto give = [&](void* base, int64_t t, int d, const f32x4_t& v) {
+    // `count` numbers of a row of dq or dk from d on
+    auto give = [&](void* base, int64_t t, int d, const float* v, auto count) {
+        constexpr int N = decltype(count)::value;
         if (d >= a.dk_) return;
-        const int64_t e = ((at.b * a.L + t) * heads_qk + at.hk) * a.dk_ + d;
-        if constexpr (SHARES) {
-            float* p = static_cast<float*>(base) + share * (rows_all * heads_qk * a.dk_) + e;
+        const int64_t e = share + ((at.b * a.L + t) * heads_qk + at.hk) * a.dk_ + d;
+        using O = std::conditional_t<SHARES, F32, T>;
+        char* p = static_cast<char*>(base) + e * O::kBytes;
+        if (N > 1 && a.dk_ % 4 == 0) {
+            float f[N];
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (d + r < a.dk_) p[r] = v[r];
+            for (int r = 0; r < N; ++r) f[r] = v[r];
+            Pack<O, N>::store(p, Pack<O, N>::pack(f));
         } else {
-            const float f[4] = {v[0], v[1], v[2], v[3]};
-            char* p = static_cast<char*>(base) + e * T::kBytes;
-            if (a.dk_ % 4 == 0) {
-                Pack<T, 4>::store(p, Pack<T, 4>::pack(f));
-            } else {
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (d + r < a.dk_) {
-                        const float one[1] = {f[r]};
-                        Pack<T, 1>::store(p + r * T::kBytes, Pack<T, 1>::pack(one));
-                    }
-            }
+            for (int r = 0; r < N; ++r)
+                if (d + r < a.dk_) {
+                    const float one[1] = {v[r]};
+                    Pack<O, 1>::store(p + r * O::kBytes, Pack<O, 1>::pack(one));
+                }
         }
     };
-    // the wave's share of the state in front of chunk x
-    auto mark = [&](State<DT, 1>& S, int64_t x) {
-        constexpr int CT4 = DV / 64, WC4 = 16 * CT4;
-        const char* p = a.marks_in + (at.item * a.chunks + x) * (DK * DV) * T::kBytes;
-#pragma unroll
-        for (int i = 0; i < DT; ++i) {
-            const int c = cw + li, w4 = c / WC4, in = c % WC4;
-            const int j = CT4 == 2 ? in / 4 % 2 : 0, l = CT4 == 2 ? in / 8 * 4 + in % 4 : in;
-            S.s[i][0] = load_mark<T>(p + (w4 * (DK * WC4) + ((i * CT4 + j) * kWave + lq * 16 + l) * 4) * T::kBytes);
-        }
+    auto give_four = [&](void* base, int64_t t, int d, const f32x4_t& v) {
+        const float f[4] = {v[0], v[1], v[2], v[3]};
+        give(base, t, d, f, std::integral_constant<int, 4>{});
     };
-    // steps [t, t + n) of chunk x, from step `t0` of it on
-    auto take = [&](int64_t x, int64_t t, int n, bool look) -> bool {
-        __syncthreads();
-        bool fine = load_tile<T, C, DK, NT>(s.q, a.q, qp + t * a.q.step, n, 0);
-        fine &= load_tile<T, C, DK, NT>(s.k, a.k, kp + t * a.k.step, n, 0);
-        fine &= load_tile<T, C, DV, NT>(s.v, a.v, vp + t * a.v.step, n, c0);
-        fine &= load_tile<T, C, DV, NT>(s.dy, a.dy, dyp + t * a.dy.step, n, c0);
-        if (w == 0) {
-            bool odd;
-            make_decays<C>(s.d, lane < n ? number<T>(gp + (t + lane) * a.g.step) : 0.0f, lane, odd);
-            fine &= !odd;
-        }
-        State<DT, 1> S;
-        mark(S, x);
-        if (look) {
-            if (__syncthreads_or(!fine)) return false;
-        } else {
-            __syncthreads();
-            // the state in front of step t, from that in front of its chunk: number by number
-            const int c = c0 + cw + li;
-            for (int64_t u = x * C; u < t; ++u) {
-                const float g = number<T>(gp + u * a.g.step);
-                const float half = g < kForgets ? 0.0f : half_factor((float)((double)g * kLog2E));
-                const float vc = c < a.dv_ ? number<T>(vp + u * a.v.step + (int64_t)c * T::kBytes) : 0.0f;
-                for (int i = 0; i < DT; ++i)
+    auto give_decay = [&](int64_t t, float x) {
+        const float one[1] = {x};
+        const int64_t e = (at.b * a.L + t) * a.H + at.h;
+        if (a.tiles > 1) static_cast<float*>(a.dg)[at.tile * (rows_all * a.H) + e] = x;
+        else Pack<T, 1>::store(static_cast<char*>(a.dg) + e * T::kBytes, Pack<T, 1>::pack(one));
+    };
+    auto dv_row = [&](int64_t t) { return a.dv + ((at.b * a.L + t) * a.H + at.h) * a.dv_ * T::kBytes; };
+    auto steps = [&](int64_t x) { return a.L - x * C < C ? (int)(a.L - x * C) : C; };
+
+    Ahead<T, C, DK, NT> next_q, next_k;
+    Ahead<T, C, DV, NT> next_v, next_dy;
+    typename Pack<T, 4>::Raw next_s[DT];
+    typename Pack<T, 1>::Raw next_g;
+    float g_now = 0.0f;
+    auto load = [&](int64_t x) {
+        const int64_t t = x * C;
+        const int n = steps(x);
+        next_q.load(a.q, qp + t * a.q.step, n, 0);
+        next_k.load(a.k, kp + t * a.k.step, n, 0);
+        next_v.load(a.v, vp + t * a.v.step, n, c0);
+        next_dy.load(a.dy, dyp + t * a.dy.step, n, c0);
+        const char* p = a.marks_in + ((at.item * a.chunks + x) * (DK * DV) + own) * T::kBytes;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int d = 16 * i + 4 * lq + r;
-                        const float kd = d < a.dk_ ? number<T>(kp + u * a.k.step + (int64_t)d * T::kBytes) : 0.0f;
-                        S.s[i][0][r] = scaled(S.s[i][0][r], half) + kd * vc;
-                    }
-            }
+        for (int i = 0; i < DT; ++i) next_s[i] = Pack<T, 4>::load(p + i * kStep * T::kBytes);
+        next_g = Pack<T, 1>::load(gp + (t + min(lane, n - 1)) * a.g.step);
+    };
+    // The last wave's: gradients of the log decays of a chunk that was taken at once.  Pairs of steps on both sides of decay t: those
+    // with an earlier step in front of the chunk and a later one behind it; those with a later one behind it; of those inside the
+    // chunk or with an earlier step in front of it, all whose later step is from t on less those whose earlier step is, too.
+    int64_t done = -1;
+    auto give_decays = [&]() {
+        if (done < 0 || w != NW - 1) return;
+        double near = 0.0, far = 0.0, both = 0.0;
+        if (lane < C) {
+#pragma unroll
+            for (int y = 0; y < DT; ++y) near += (double)s.near[y][lane], far += (double)s.far[y][lane];
         }
-        // <S, M>, and S to LDS
+#pragma unroll
+        for (int y = 0; y < NW; ++y) both += (double)s.both[y];
+        const double upto = wave_upto(far);
+        // (from behind: what is not finite stays in front of itself)
+        const int turn = kWave - 1 - lane;
+        const double from = __shfl(wave_upto((double)__shfl(near, turn, kWave)), turn, kWave);
+        const int64_t t = done * C + lane;
+        if (lane < steps(done)) give_decay(t, g_now < kForgets ? 0.0f : (float)(from + (upto - far) + both));
+    };
+    load(last - 1);
+    for (int64_t x = last - 1; x >= first; --x) {
+        const int64_t t = x * C;
+        const int n = steps(x);
+        __syncthreads();  // nobody reads the chunk behind any more
+        give_decays();
+        bool fine = next_q.put(s.q, a.most, n, 0, a.q.d);
+        fine &= next_k.put(s.k, a.most, n, 0, a.k.d);
+        fine &= next_v.put(s.v, a.most, n, c0, a.v.d);
+        fine &= next_dy.put(s.dy, a.most, n, c0, a.dy.d);
+        f32x4_t sm[DT];
         {
-            float both = 0.0f;
+            Elem<T>* p = s.s + (cw + li) * PK + 4 * lq;
 #pragma unroll
             for (int i = 0; i < DT; ++i) {
+                store_words<Pack<T, 4>::kWords>(p + 16 * i, next_s[i]);
+                float f[4];
+                Pack<T, 4>::unpack(next_s[i], f);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) both += s.d.whole == 0.0f ? 0.0f : scaled(S.s[i][0][r], s.d.whole) * M.s[i][0][r];
-                put4(s.s + (cw + li) * PK + 16 * i + 4 * lq, S.s[i][0]);
+                for (int r = 0; r < 4; ++r) sm[i][r] = f[r];
+                if constexpr (Lds::kTwo) put4(s.m + (cw + li) * PK + 16 * i + 4 * lq, M.s[i][0]);
             }
-#pragma unroll
-            for (int d = kWave / 2; d > 0; d /= 2) both += __shfl_xor(both, d, kWave);
-            if (lane == 0) s.both[w] = both;
         }
-        // A, its gradient's part E_ij = scale exp(b_i - b_j) (dy_i . v_j), and W = (dy_i . v_j) A_ij below the diagonal
-        constexpr int kBlocks = IT * (IT + 1) / 2;
+        g_now = lane < n ? unpacked<T>(next_g) : 0.0f;
+        if (w == 0) fine &= make_decays<C>(s.d, g_now, lane);
+        const bool at_once = !__syncthreads_or(!fine);
+        if (x > first) load(x - 1);
+        done = -1;
+        if (!at_once) {
+            float *const sum_q = reinterpret_cast<float*>(s.q), *const sum_k = reinterpret_cast<float*>(s.k);
+            const char* mark = a.marks_in + ((at.item * a.chunks + x) * (DK * DV) + own) * T::kBytes;
+            const int c = c0 + cw + li;
+            for (int i = n - 1; i >= 0; --i) {
+                const int64_t u = t + i;
+                State<DT, 1> S;
 #pragma unroll
+                for (int y = 0; y < DT; ++y) S.s[y][0] = load_mark<T>(mark + y * kStep * T::kBytes);
+                for (int64_t z = t; z < u; ++z)
+                    S.template step<T>(step_factor(number<T>(gp + z * a.g.step)), kp + z * a.k.step, vp + z * a.v.step, 1.0f, a.dk_, a.dv_, c0 + cw, li, lq);
+                const float half = step_factor(number<T>(gp + u * a.g.step));
+                M.template step<T>(1.0f, qp + u * a.q.step, dyp + u * a.dy.step, a.scale, a.dk_, a.dv_, c0 + cw, li, lq);
+                float both = 0.0f;
+                if (half != 0.0f)
+#pragma unroll
+                    for (int y = 0; y < DT; ++y)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) both = fmaf(scaled(S.s[y][0][r], half), M.s[y][0][r], both);
+                S.template step<T>(half, kp + u * a.k.step, vp + u * a.v.step, 1.0f, a.dk_, a.dv_, c0 + cw, li, lq);
+                const float dv[1] = {M.template product<T>(kp + u * a.k.step, 0, a.dk_, lq)};
+                const float dyc = c < a.dv_ ? number<T>(dyp + u * a.dy.step + (int64_t)c * T::kBytes) * a.scale : 0.0f;
+                const float vc = c < a.dv_ ? number<T>(vp + u * a.v.step + (int64_t)c * T::kBytes) : 0.0f;
+                if (lq == 0 && c < a.dv_) Pack<T, 1>::store(dv_row(u) + c * T::kBytes, Pack<T, 1>::pack(dv));
+                __syncthreads();  // the step behind has been given
+                both = of_lane(wave_upto(both), kWave - 1);
+                if (lane == 0) s.both[w] = both;
+#pragma unroll
+                for (int y = 0; y < DT; ++y) {
+                    const int d0 = 16 * y + fresh(4 * lq);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {  // (columns behind the last add nothing)
+                        const float fq = over_columns(c < a.dv_ ? S.s[y][0][r] * dyc : 0.0f), fk = over_columns(c < a.dv_ ? M.s[y][0][r] * vc : 0.0f);
+                        if (li == 15) sum_q[w * DK + d0 + r] = fq, sum_k[w * DK + d0 + r] = fk;
+                    }
+                }
+                __syncthreads();
+                const int d = threadIdx.x;
+                if (d < DK) {
+                    float fq[1] = {0.0f}, fk[1] = {0.0f};
+                    for (int y = 0; y < NW; ++y) fq[0] += sum_q[y * DK + d], fk[0] += sum_k[y * DK + d];
+                    give(a.dq, u, d, fq, std::integral_constant<int, 1>{});
+                    give(a.dk, u, d, fk, std::integral_constant<int, 1>{});
+                }
+                if (threadIdx.x == 0) {
+                    float f = 0.0f;
+                    for (int y = 0; y < NW; ++y) f += s.both[y];
+                    give_decay(u, f);
+                }
+                M.decay_step(half);
+            }
+            continue;
+        }
+        done = x;
+        // A, and its gradient's part E_ij = scale exp(b_i - b_j) (dy_i . v_j)
+        constexpr int kBlocks = IT * (IT + 1) / 2;
+#pragma unroll 1
         for (int y = 0; y < (kBlocks + NW - 1) / NW; ++y) {
             const int block = y * NW + w;
             if (block >= kBlocks) break;
@@ -787,37 +988,36 @@ __global__ __launch_bounds__(DV * 4) void la_bwd_kernel(LaArgs a) {
             for (int kb = 0; kb < DK / 32; ++kb)
                 multiply(p, row_frag<PK>(s.k, 16 * jt + li, 32 * kb, lq), row_frag<PK>(s.q, 16 * it + li, 32 * kb, lq));
 #pragma unroll
-            for (int kb = 0; kb < DV / 32; ++kb)
+            for (int kb = 0; kb < VB; ++kb)
                 multiply(e, row_frag<PV>(s.v, 16 * jt + li, 32 * kb, lq), row_frag<PV>(s.dy, 16 * it + li, 32 * kb, lq));
             const int i = 16 * it + li, j0 = 16 * jt + 4 * lq, forgot = s.d.forgot[i];
             const float hi = s.d.hi[i], lo = s.d.lo[i];
-            float row = 0.0f, col[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const bool in = j0 + r <= i && j0 + r >= forgot;
-                const float half = half_factor((hi - s.d.hi[j0 + r]) + (lo - s.d.lo[j0 + r]));
-                p[r] = in ? p[r] * a.scale * half * half : 0.0f;
-                col[r] = in && j0 + r < i ? p[r] * e[r] : 0.0f;
-                e[r] = in ? e[r] * a.scale * half * half : 0.0f;
-                row += col[r];
+                const float f = __builtin_amdgcn_exp2f((hi - s.d.hi[j0 + r]) + (lo - s.d.lo[j0 + r])) * a.scale;
+                p[r] = in ? p[r] * f : 0.0f;
+                e[r] = in ? e[r] * f : 0.0f;
             }
             put4(s.a + i * PA + j0, p);
             put4(s.e + i * PA + j0, e);
-            row += __shfl_xor(row, 16, kWave);
-            row += __shfl_xor(row, 32, kWave);
-            if (lq == 0) s.row[jt][i] = row;
+        }
+        // <S, M>
+        {
+            const float whole = s.d.whole;
+            float both = 0.0f;
+            if (whole != 0.0f)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
+                for (int i = 0; i < DT; ++i)
 #pragma unroll
-                for (int d = 1; d < 16; d *= 2) col[r] += __shfl_xor(col[r], d, kWave);
-                if (li == 0) s.col[it][j0 + r] = col[r];
-            }
+                    for (int r = 0; r < 4; ++r) both = fmaf(sm[i][r] * whole, M.s[i][0][r], both);
+            both = of_lane(wave_upto(both), kWave - 1);
+            if (lane == 0) s.both[w] = both;
         }
         // dv of the wave's columns from M in registers
         f32x4_t dv[IT];
-        Frag<T> fdy[KB];
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) fdy[kb] = column_frag<PV, 4>(s.dy, 32 * kb, cw, li, lq);
+        Frag<T> fdy[1][KB];
+        own_columns<T, PV>(fdy, s.dy, cw, li, lq);
         {
             Frag<T> fm[DK / 32];
 #pragma unroll
@@ -832,20 +1032,20 @@ __global__ __launch_bounds__(DV * 4) void la_bwd_kernel(LaArgs a) {
                 dv[jt] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int y = 0; y < DK / 32; ++y) multiply(dv[jt], fm[y], turned_row_frag<PK>(s.k, 16 * jt + li, 32 * y, lq));
-                const float half = s.d.to_end[16 * jt + li];
+                const float factor = s.d.to_end[16 * jt + li];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) dv[jt][r] = scaled(dv[jt][r], half);
+                for (int r = 0; r < 4; ++r) dv[jt][r] = weighted(dv[jt][r], factor);
             }
         }
-        __syncthreads();  // A, E and S are there
+        __syncthreads();  // A and E are there
 #pragma unroll
         for (int jt = 0; jt < IT; ++jt) {
 #pragma unroll
-            for (int kb = jt / 2; kb < KB; ++kb) multiply(dv[jt], fdy[kb], column_frag<PA, 4>(s.a, 32 * kb, 16 * jt, li, lq));
+            for (int kb = jt / 2; kb < KB; ++kb) multiply(dv[jt], fdy[0][kb], column_frag<PA, 4>(s.a, 32 * kb, 16 * jt, li, lq));
             const int j = 16 * jt + li, c = c0 + cw + 4 * lq;
             if (j < n && c < a.dv_) {
                 const float f[4] = {dv[jt][0], dv[jt][1], dv[jt][2], dv[jt][3]};
-                char* p = a.dv + (((at.b * a.L + t + j) * a.H + at.h) * a.dv_ + c) * T::kBytes;
+                char* p = dv_row(t + j) + c * T::kBytes;
                 if (a.dv_ % 4 == 0) {
                     Pack<T, 4>::store(p, Pack<T, 4>::pack(f));
                 } else {
@@ -858,116 +1058,89 @@ __global__ __launch_bounds__(DV * 4) void la_bwd_kernel(LaArgs a) {
                 }
             }
         }
-        // dq and dk, blocks of 16 rows by 16 numbers: dt = w % DT + ..., rows in turn
-        constexpr int kBand = NW < DT ? NW : DT;  // waves side by side
-        auto blocks = [&](auto&& f) {
+        // dq and dk: a wave has blocks of 16 rows, every NW / kBand-th, by 16 numbers of every kBand-th
+        constexpr int kBand = NW < DT ? NW : DT, kRows = (IT * kBand + NW - 1) / NW;
+        float near[DT / kBand][kRows];
 #pragma unroll
-            for (int y = 0; y < DT / kBand; ++y)
+        for (int y = 0; y < DT / kBand; ++y) {
+            const int dt = y * kBand + w % kBand;
+            Frag<T> fs[VB], fk[KB];
 #pragma unroll
-                for (int z = 0; z < (IT * kBand + NW - 1) / NW; ++z) {
-                    const int it = z * (NW / kBand) + w / kBand;
-                    if (it < IT) f(it, y * kBand + w % kBand);
-                }
-        };
-        blocks([&](int it, int dt) {
-            const int i = 16 * it + li;
-            f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int kb = 0; kb < VB; ++kb) fs[kb] = column_frag<PK, 4>(s.s, 32 * kb, 16 * dt, li, lq);
 #pragma unroll
-            for (int kb = 0; kb < DV / 32; ++kb)
-                multiply(o, column_frag<PK, 4>(s.s, 32 * kb, 16 * dt, li, lq), row_frag<PV>(s.dy, i, 32 * kb, lq));
-            const float half = s.d.from_start[i];
-            float far = 0.0f;
+            for (int kb = 0; kb < KB; ++kb) fk[kb] = column_frag<PK, 4>(s.k, 32 * kb, 16 * dt, li, lq);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                o[r] = scaled(o[r] * a.scale, half);
-                float q[1];
-                Pack<T, 1>::unpack(Pack<T, 1>::load(s.q + i * PK + 16 * dt + 4 * lq + r), q);
-                far += half == 0.0f ? 0.0f : q[0] * o[r];
-            }
-            far += __shfl_xor(far, 16, kWave);
-            far += __shfl_xor(far, 32, kWave);
-            if (lq == 0) s.far_q[dt][i] = far;
-            for (int kb = 0; kb <= it / 2; ++kb) multiply(o, column_frag<PK, 4>(s.k, 32 * kb, 16 * dt, li, lq), row_frag<PA>(s.e, i, 32 * kb, lq));
-            if (i < n) give(a.dq, t + i, 16 * dt + 4 * lq, o);
-        });
-        __syncthreads();  // S has been read
+            for (int z = 0; z < kRows; ++z) {
+                const int it = z * (NW / kBand) + w / kBand, i = 16 * it + li;
+                if (it >= IT) continue;
+                f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < DT; ++i) put4(s.s + (cw + li) * PK + 16 * i + 4 * lq, M.s[i][0]);
-        __syncthreads();
-        blocks([&](int jt, int dt) {
-            const int j = 16 * jt + li;
-            f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
+                for (int kb = 0; kb < VB; ++kb) multiply(o, fs[kb], row_frag<PV>(s.dy, i, 32 * kb, lq));
+                const float factor = s.d.from_start[i] * a.scale;
 #pragma unroll
-            for (int kb = 0; kb < DV / 32; ++kb)
-                multiply(o, column_frag<PK, 4>(s.s, 32 * kb, 16 * dt, li, lq), row_frag<PV>(s.v, j, 32 * kb, lq));
-            const float half = s.d.to_end[j];
-            float far = 0.0f;
+                for (int r = 0; r < 4; ++r) o[r] = weighted(o[r], factor);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                o[r] = scaled(o[r], half);
-                float k[1];
-                Pack<T, 1>::unpack(Pack<T, 1>::load(s.k + j * PK + 16 * dt + 4 * lq + r), k);
-                far += half == 0.0f ? 0.0f : k[0] * o[r];
-            }
-            far += __shfl_xor(far, 16, kWave);
-            far += __shfl_xor(far, 32, kWave);
-            if (lq == 0) s.far_k[dt][j] = far;
-            for (int kb = jt / 2; kb < KB; ++kb) multiply(o, column_frag<PK, 4>(s.q, 32 * kb, 16 * dt, li, lq), column_frag<PA, 4>(s.e, 32 * kb, 16 * jt, li, lq));
-            if (j < n) give(a.dk, t + j, 16 * dt + 4 * lq, o);
-        });
-        {
-            M.decay(s.d.whole);
-            Frag<T> fb[1][KB];
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb) fb[0][kb] = fdy[kb];
-            add_rows<T, DK, C>(M, s.q, fb, s.d.from_start, a.scale, li, lq);
-        }
-        __syncthreads();  // the shares of dg are there
-        if (w == 0) {
-            // pairs of steps on both sides of decay t: inside the chunk, those whose later step is from t on less those whose earlier
-            // step is too; those with an earlier step in front of the chunk; those with a later step behind it; those with both
-            double near = 0.0, col = 0.0;
-            if (lane < C) {
-                for (int x2 = 0; x2 <= lane / 16; ++x2) near += (double)s.row[x2][lane];
-                for (int x2 = lane / 16; x2 < IT; ++x2) near -= (double)s.col[x2][lane];
-                for (int x2 = 0; x2 < DT; ++x2) near += (double)s.far_q[x2][lane], col += (double)s.far_k[x2][lane];
-            }
-            double both = 0.0;
-            for (int x2 = 0; x2 < NW; ++x2) both += (double)s.both[x2];
-            double upto = col;
-#pragma unroll
-            for (int d = 1; d < kWave; d *= 2) {
-                const double f = __shfl_up(upto, d, kWave), g = __shfl_down(near, d, kWave);
-                if (lane >= d) upto += f;
-                if (lane + d < kWave) near += g;
-            }
-            if (lane < n) {
-                const float g = number<T>(gp + (t + lane) * a.g.step);
-                const float one[1] = {g < kForgets ? 0.0f : (float)(near + (upto - col) + both)};
-                const int64_t e = (at.b * a.L + t + lane) * a.H + at.h;
-                if (a.tiles > 1) static_cast<float*>(a.dg)[at.tile * (rows_all * a.H) + e] = one[0];
-                else Pack<T, 1>::store(static_cast<char*>(a.dg) + e * T::kBytes, Pack<T, 1>::pack(one));
+                for (int kb = 0; kb < KB; ++kb)
+                    if (kb <= it / 2) multiply(o, fk[kb], row_frag<PA>(s.e, i, 32 * kb, lq));
+                near[y][z] = dot(four<T>(s.q + i * PK + 16 * dt + 4 * lq), o);
+                if (i < n) give_four(a.dq, t + i, 16 * dt + 4 * lq, o);
             }
         }
-        return true;
-    };
-    for (int64_t x = last - 1; x >= first; --x) {
-        const int64_t t = x * C;
-        const int n = a.L - t < C ? (int)(a.L - t) : C;
-        if (!take(x, t, n, true))
-            for (int i = n - 1; i >= 0; --i) take(x, t + i, 1, false);
+        if constexpr (!Lds::kTwo) {
+            __syncthreads();  // S has been read
+#pragma unroll
+            for (int i = 0; i < DT; ++i) put4(s.s + (cw + li) * PK + 16 * i + 4 * lq, M.s[i][0]);
+            __syncthreads();
+        }
+        const Elem<T>* const sm_t = Lds::kTwo ? s.m : s.s;
+#pragma unroll
+        for (int y = 0; y < DT / kBand; ++y) {
+            const int dt = y * kBand + w % kBand;
+            Frag<T> fm[VB], fq[KB];
+#pragma unroll
+            for (int kb = 0; kb < VB; ++kb) fm[kb] = column_frag<PK, 4>(sm_t, 32 * kb, 16 * dt, li, lq);
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) fq[kb] = column_frag<PK, 4>(s.q, 32 * kb, 16 * dt, li, lq);
+#pragma unroll
+            for (int z = 0; z < kRows; ++z) {
+                const int jt = z * (NW / kBand) + w / kBand, j = 16 * jt + li;
+                if (jt >= IT) continue;
+                f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f}, o2 = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int kb = 0; kb < VB; ++kb) multiply(o, fm[kb], row_frag<PV>(s.v, j, 32 * kb, lq));
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+                    if (kb >= jt / 2) multiply(o2, fq[kb], column_frag<PA, 4>(s.e, 32 * kb, 16 * jt, li, lq));
+                const float factor = s.d.to_end[j];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[r] = weighted(o[r], factor);
+                const f32x4_t k4 = four<T>(s.k + j * PK + 16 * dt + 4 * lq);
+                const float far = over_quarters(dot(k4, o)), less = over_quarters(near[y][z] - dot(k4, o2));
+                if (lq == 0) s.far[dt][j] = far, s.near[dt][j] = less;
+                o += o2;
+                if (j < n) give_four(a.dk, t + j, 16 * dt + 4 * lq, o);
+            }
+        }
+        M.decay(s.d.whole);
+        add_rows<T, DK, C>(M, s.q, fdy, s.d.from_start, a.scale, li, lq);
     }
+    __syncthreads();
+    give_decays();
     if (at.segment == 0 && a.dstate_in) M.store(a.dstate_in + head_state, a.dk_, a.dv_, c0 + cw, li, lq);
 }
 
 // out[r][d] = sum over the shares: heads that share a row of q and k, and tiles of their columns; [share][rows].
-template <typename T>
+template <typename T, int VEC>
 __global__ __launch_bounds__(256) void la_shares_kernel(const float* shares, void* out, int64_t n, int32_t count) {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        float sum = 0.0f;
-        for (int x = 0; x < count; ++x) sum += shares[x * n + i];
-        const float one[1] = {sum};
-        Pack<T, 1>::store(static_cast<char*>(out) + i * T::kBytes, Pack<T, 1>::pack(one));
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * VEC; i < n; i += (int64_t)gridDim.x * 256 * VEC) {
+        float sum[VEC] = {};
+        for (int x = 0; x < count; ++x) {
+            float f[VEC];
+            Pack<F32, VEC>::unpack(Pack<F32, VEC>::load_nt(shares + x * n + i), f);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) sum[j] += f[j];
+        }
+        Pack<T, VEC>::store(static_cast<char*>(out) + i * T::kBytes, Pack<T, VEC>::pack(sum));
     }
 }
 
@@ -992,8 +1165,7 @@ __global__ __launch_bounds__(256) void la_step_kernel(StepArgs a) {
     const int64_t bh = blockIdx.x / (uint32_t)a.slices, b = bh / a.H;
     const int h = (int)(bh % a.H), c = ((int)(blockIdx.x % (uint32_t)a.slices) * CL + cl) * VEC;
     const int64_t qk = (b * (a.H / a.group) + h / a.group) * a.dk;
-    const float g = number<T>(a.g + bh * T::kBytes);
-    const float half = g < kForgets ? 0.0f : half_factor((float)((double)g * kLog2E));
+    const float half = step_factor(number<T>(a.g + bh * T::kBytes));
     float v[VEC] = {}, y[VEC] = {};
     if (c < a.dv) {
 #pragma unroll
@@ -1057,7 +1229,8 @@ int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 Rows rows_of(const void* p, const LaShape& s, int which, int64_t d) {
     const int64_t e = s.dtype == HY_F32 ? 4 : 2;
     const int64_t* st = s.stride[which];
-    const bool wide = d % 8 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0 && st[0] * e % 16 == 0 && st[1] * e % 16 == 0 && st[2] * e % 16 == 0;
+    const bool wide = d % 8 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0 && st[0] * e % 16 == 0 && st[1] * e % 16 == 0 && st[2] * e % 16 == 0 &&
+                      st[1] < (INT64_C(1) << 24);  // (a chunk's rows within 2^32 bytes)
     return Rows{static_cast<const char*>(p), st[0] * e, st[1] * e, st[2] * e, (int32_t)d, wide};
 }
 
@@ -1070,6 +1243,9 @@ LaArgs args_of(const LaPtrs& p, const LaShape& s) {
     a.L = s.L, a.chunks = chunks_of(s);
     a.H = (int32_t)s.H, a.group = s.group, a.dk_ = (int32_t)s.dk, a.dv_ = (int32_t)s.dv, a.tiles = (int32_t)tiles_of(s);
     a.scale = (float)s.scale;
+    const float most = fabsf(a.scale) <= 1.0f ? kMostNumber : kMostNumber / fabsf(a.scale);  // (NaN: none is below)
+    static_assert(sizeof(most) == sizeof(a.most), "its bits");
+    if (most > 0.0f) memcpy(&a.most, &most, sizeof most);
     return a;
 }
 
@@ -1099,7 +1275,7 @@ hy_status walk(LaArgs a, const LaShape& s, const Cut& c, void* ws, bool out, hip
     const dim3 grid((uint32_t)(items * c.segments));
     if (c.segments > 1) {
         hy_status rc = by_tile(s, [&](auto t, auto dk, auto dv) {
-            return launch_kernel(la_walk_kernel<decltype(t), decltype(dk)::value, decltype(dv)::value, false, false>, grid, dim3(256), st, a);
+            return launch_kernel(la_ends_walk_kernel<decltype(t), decltype(dk)::value, decltype(dv)::value, false>, grid, dim3(256), st, a);
         });
         if (rc == HY_OK) rc = scan_ends(a, s, false, st);
         if (rc != HY_OK) return rc;
@@ -1108,8 +1284,8 @@ hy_status walk(LaArgs a, const LaShape& s, const Cut& c, void* ws, bool out, hip
         using T = decltype(t);
         constexpr int DK = decltype(dk)::value, DV = decltype(dv)::value;
         (void)out;
-        return a.marks ? launch_kernel(la_walk_kernel<T, DK, DV, true, true>, grid, dim3(256), st, a)
-                       : launch_kernel(la_walk_kernel<T, DK, DV, true, false>, grid, dim3(256), st, a);
+        return a.marks ? launch_kernel(la_walk_kernel<T, DK, DV, true>, grid, dim3(256), st, a)
+                       : launch_kernel(la_walk_kernel<T, DK, DV, false>, grid, dim3(256), st, a);
     });
 }
 
@@ -1186,7 +1362,7 @@ hy_status launch_la_bwd(const LaPtrs& p, const LaShape& s, void* ws, hipStream_t
     hy_status rc = HY_OK;
     if (b.cut.segments > 1) {
         rc = by_tile(s, [&](auto t, auto dk, auto dv) {
-            return launch_kernel(la_back_kernel<decltype(t), decltype(dk)::value, decltype(dv)::value>, grid, dim3(256), st, a);
+            return launch_kernel(la_ends_walk_kernel<decltype(t), decltype(dk)::value, decltype(dv)::value, true>, grid, dim3(256), st, a);
         });
         if (rc == HY_OK) rc = scan_ends(a, s, true, st);
         if (rc != HY_OK) return rc;
@@ -1198,10 +1374,15 @@ hy_status launch_la_bwd(const LaPtrs& p, const LaShape& s, void* ws, hipStream_t
                            : launch_kernel(la_bwd_kernel<T, DK, DV, false>, grid, dim3(DV * 4), st, a);
     });
     auto reduce = [&](const void* from, void* to, int64_t n, int32_t count) {
-        const dim3 g(workgroups_for(n, 256, 256));
         const float* f = static_cast<const float*>(from);
-        return s.dtype == HY_F32 ? launch_kernel(la_shares_kernel<F32>, g, dim3(256), st, f, to, n, count)
-                                 : launch_kernel(la_shares_kernel<BF16>, g, dim3(256), st, f, to, n, count);
+        auto sums = [&](auto t, auto vec) {
+            constexpr int VEC = decltype(vec)::value;
+            return launch_kernel(la_shares_kernel<decltype(t), VEC>, dim3(workgroups_for(n, 256 * VEC, 256)), dim3(256), st, f, to, n, count);
+        };
+        using std::integral_constant;
+        const bool fours = n % 4 == 0 && (reinterpret_cast<uintptr_t>(to) | reinterpret_cast<uintptr_t>(from)) % 16 == 0;
+        if (s.dtype == HY_F32) return fours ? sums(F32{}, integral_constant<int, 4>{}) : sums(F32{}, integral_constant<int, 1>{});
+        return fours ? sums(BF16{}, integral_constant<int, 4>{}) : sums(BF16{}, integral_constant<int, 1>{});
     };
     const int64_t nqk = s.B * s.L * (s.H / s.group) * s.dk;
     if (rc == HY_OK && b.count > 1) rc = reduce(shares_q, p.dq, nqk, b.count);
