@@ -324,16 +324,16 @@ struct Place {
     int64_t b, item;  // item: (b H + h) tiles + tile
     int32_t h, hk, tile, segment;
 };
+__device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ Place place_of(const LaArgs& a, uint32_t i) {
-    Place p;
-    const uint32_t n = (uint32_t)a.segments;
-    p.segment = (int32_t)(i % n);
-    p.item = i / n;
-    p.tile = (int32_t)(p.item % a.tiles);
-    const int64_t bh = p.item / a.tiles;
-    p.h = (int32_t)(bh % a.H);
-    p.b = bh / a.H;
-    p.hk = p.h / a.group;
+    Place p;  // (all below 2^31, and kept in scalar registers: pointers made of them are, too)
+    const uint32_t n = (uint32_t)a.segments, item = (uint32_t)uniform((int32_t)(i / n)), bh = (uint32_t)uniform((int32_t)(item / (uint32_t)a.tiles));
+    p.segment = uniform((int32_t)(i % n));
+    p.item = item;
+    p.tile = uniform((int32_t)(item % (uint32_t)a.tiles));
+    p.h = uniform((int32_t)(bh % (uint32_t)a.H));
+    p.b = uniform((int32_t)(bh / (uint32_t)a.H));
+    p.hk = uniform(p.h / a.group);
     return p;
 }
 
@@ -512,7 +512,7 @@ __global__ __launch_bounds__(256, 2) void la_ends_walk_kernel(LaArgs a) {
     const char *ap = ra.p + at.b * ra.batch + at.hk * ra.head, *bp = rb.p + at.b * rb.batch + at.h * rb.head;
     const char* gp = a.g.p + at.b * a.g.batch + (int64_t)at.h * T::kBytes;
     const int c0 = at.tile * DV, cw = w * WC;  // the tile's columns, the wave's in it
-    const int64_t head_state = (at.b * a.H + at.h) * a.dk_ * a.dv_, items = (int64_t)gridDim.x / a.segments;
+    const int64_t head_state = (at.b * a.H + at.h) * a.dk_ * a.dv_, items = uniform((int32_t)(gridDim.x / (uint32_t)a.segments));
     const float scale = BACK ? a.scale : 1.0f;
     State<DT, CT> S;
     if (!BACK && at.segment == 0 && a.state_in) S.load(a.state_in + head_state, a.dk_, a.dv_, c0 + cw, li, lq);
@@ -580,7 +580,7 @@ __global__ __launch_bounds__(256, 2) void la_walk_kernel(LaArgs a) {
     const char *kp = a.k.p + at.b * a.k.batch + at.hk * a.k.head, *vp = a.v.p + at.b * a.v.batch + at.h * a.v.head;
     const char *qp = a.q.p + at.b * a.q.batch + at.hk * a.q.head, *gp = a.g.p + at.b * a.g.batch + (int64_t)at.h * T::kBytes;
     const int c0 = at.tile * DV, cw = w * WC;  // the tile's columns, the wave's in it
-    const int64_t head_state = (at.b * a.H + at.h) * a.dk_ * a.dv_, items = (int64_t)gridDim.x / a.segments;
+    const int64_t head_state = (at.b * a.H + at.h) * a.dk_ * a.dv_, items = uniform((int32_t)(gridDim.x / (uint32_t)a.segments));
     State<DT, CT> S;
     if (at.segment > 0) S.load_own(a.ends + ((at.segment - 1) * items + at.item) * (DK * DV) + w * (DK * WC), lane);
     else if (a.state_in) S.load(a.state_in + head_state, a.dk_, a.dv_, c0 + cw, li, lq);
@@ -634,6 +634,7 @@ __global__ __launch_bounds__(256, 2) void la_walk_kernel(LaArgs a) {
         constexpr int kBlocks = IT * (IT + 1) / 2;
 #pragma unroll 1
         for (int y = 0; y < (kBlocks + NW - 1) / NW; ++y) {
+            const int part = fresh(lane), li = part % 16, lq = part / 16;  // (addresses of one phase at a time)
             const int block = y * NW + w;
             if (block >= kBlocks) break;
             int it = 0;
@@ -653,7 +654,10 @@ __global__ __launch_bounds__(256, 2) void la_walk_kernel(LaArgs a) {
             put4(s.a + i * PA + j0, p);
         }
         Frag<T> fv[CT][KB];
-        own_columns<T, PV>(fv, s.v, cw, li, lq);
+        {
+            const int part = fresh(lane), li = part % 16, lq = part / 16;
+            own_columns<T, PV>(fv, s.v, cw, li, lq);
+        }
         Frag<T> fs[DK / 32][CT];  // the state as an operand
 #pragma unroll
         for (int y = 0; y < DK / 32; ++y)
@@ -667,6 +671,7 @@ __global__ __launch_bounds__(256, 2) void la_walk_kernel(LaArgs a) {
         __syncthreads();  // A is there
 #pragma unroll 1
         for (int it = 0; it < IT; ++it) {
+            const int part = fresh(lane), li = part % 16, lq = part / 16;
             const int i = 16 * it + li;
             f32x4_t o[CT];
 #pragma unroll
@@ -716,7 +721,10 @@ __global__ __launch_bounds__(256, 2) void la_walk_kernel(LaArgs a) {
             }
         }
         S.decay(s.d.whole);
-        add_rows<T, DK, C>(S, s.k, fv, s.d.to_end, 1.0f, li, lq);
+        {
+            const int part = fresh(lane), li = part % 16, lq = part / 16;
+            add_rows<T, DK, C>(S, s.k, fv, s.d.to_end, 1.0f, li, lq);
+        }
     }
     if (at.segment == a.segments - 1 && a.state_out) S.store(a.state_out + head_state, a.dk_, a.dv_, c0 + cw, li, lq);
 }
@@ -801,7 +809,7 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
     const char *qp = a.q.p + at.b * a.q.batch + at.hk * a.q.head, *dyp = a.dy.p + at.b * a.dy.batch + at.h * a.dy.head;
     const char* gp = a.g.p + at.b * a.g.batch + (int64_t)at.h * T::kBytes;
     const int c0 = at.tile * DV, cw = w * 16;
-    const int64_t items = (int64_t)gridDim.x / a.segments, head_state = (at.b * a.H + at.h) * a.dk_ * a.dv_;
+    const int64_t items = uniform((int32_t)(gridDim.x / (uint32_t)a.segments)), head_state = (at.b * a.H + at.h) * a.dk_ * a.dv_;
     // where the walks of 4 waves have this wave's columns: piece i of 16 rows is `own` + i * kStep numbers behind
     constexpr int CT4 = DV / 64, WC4 = 16 * CT4, kStep = CT4 * kWave * 4;
     const int own_c = cw + li, own_in = own_c % WC4, own_j = CT4 == 2 ? own_in / 4 % 2 : 0, own_l = CT4 == 2 ? own_in / 8 * 4 + own_in % 4 : own_in;
@@ -902,22 +910,31 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
         fine &= next_k.put(s.k, a.most, n, 0, a.k.d);
         fine &= next_v.put(s.v, a.most, n, c0, a.v.d);
         fine &= next_dy.put(s.dy, a.most, n, c0, a.dy.d);
-        f32x4_t sm[DT];
         {
             Elem<T>* p = s.s + (cw + li) * PK + 4 * lq;
 #pragma unroll
             for (int i = 0; i < DT; ++i) {
                 store_words<Pack<T, 4>::kWords>(p + 16 * i, next_s[i]);
-                float f[4];
-                Pack<T, 4>::unpack(next_s[i], f);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) sm[i][r] = f[r];
                 if constexpr (Lds::kTwo) put4(s.m + (cw + li) * PK + 16 * i + 4 * lq, M.s[i][0]);
             }
         }
         g_now = lane < n ? unpacked<T>(next_g) : 0.0f;
         if (w == 0) fine &= make_decays<C>(s.d, g_now, lane);
         const bool at_once = !__syncthreads_or(!fine);
+        {  // <S, M>
+            const float whole = s.d.whole;
+            float both = 0.0f;
+            if (whole != 0.0f)
+#pragma unroll
+                for (int i = 0; i < DT; ++i) {
+                    float f[4];
+                    Pack<T, 4>::unpack(next_s[i], f);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) both = fmaf(f[r] * whole, M.s[i][0][r], both);
+                }
+            both = wave_upto(both);
+            if (lane == kWave - 1) s.both[w] = both;
+        }
         if (x > first) load(x - 1);
         done = -1;
         if (!at_once) {
@@ -978,6 +995,7 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
         constexpr int kBlocks = IT * (IT + 1) / 2;
 #pragma unroll 1
         for (int y = 0; y < (kBlocks + NW - 1) / NW; ++y) {
+            const int part = fresh(lane), li = part % 16, lq = part / 16;  // (addresses of one phase at a time)
             const int block = y * NW + w;
             if (block >= kBlocks) break;
             int it = 0;
@@ -1002,23 +1020,10 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
             put4(s.a + i * PA + j0, p);
             put4(s.e + i * PA + j0, e);
         }
-        // <S, M>
-        {
-            const float whole = s.d.whole;
-            float both = 0.0f;
-            if (whole != 0.0f)
-#pragma unroll
-                for (int i = 0; i < DT; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) both = fmaf(sm[i][r] * whole, M.s[i][0][r], both);
-            both = of_lane(wave_upto(both), kWave - 1);
-            if (lane == 0) s.both[w] = both;
-        }
         // dv of the wave's columns from M in registers
         f32x4_t dv[IT];
-        Frag<T> fdy[1][KB];
-        own_columns<T, PV>(fdy, s.dy, cw, li, lq);
         {
+            const int part = fresh(lane), li = part % 16, lq = part / 16;
             Frag<T> fm[DK / 32];
 #pragma unroll
             for (int y = 0; y < DK / 32; ++y) {
@@ -1038,8 +1043,14 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
             }
         }
         __syncthreads();  // A and E are there
+        Frag<T> fdy[1][KB];
+        {
+            const int part = fresh(lane), li = part % 16, lq = part / 16;
+            own_columns<T, PV>(fdy, s.dy, cw, li, lq);
+        }
 #pragma unroll
         for (int jt = 0; jt < IT; ++jt) {
+            const int part = fresh(lane), li = part % 16, lq = part / 16;
 #pragma unroll
             for (int kb = jt / 2; kb < KB; ++kb) multiply(dv[jt], fdy[0][kb], column_frag<PA, 4>(s.a, 32 * kb, 16 * jt, li, lq));
             const int j = 16 * jt + li, c = c0 + cw + 4 * lq;
@@ -1063,6 +1074,7 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
         float near[DT / kBand][kRows];
 #pragma unroll
         for (int y = 0; y < DT / kBand; ++y) {
+            const int part = fresh(lane), li = part % 16, lq = part / 16;
             const int dt = y * kBand + w % kBand;
             Frag<T> fs[VB], fk[KB];
 #pragma unroll
@@ -1084,6 +1096,7 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
                     if (kb <= it / 2) multiply(o, fk[kb], row_frag<PA>(s.e, i, 32 * kb, lq));
                 near[y][z] = dot(four<T>(s.q + i * PK + 16 * dt + 4 * lq), o);
                 if (i < n) give_four(a.dq, t + i, 16 * dt + 4 * lq, o);
+                __builtin_amdgcn_sched_barrier(0);  // (blocks side by side need more registers than there are)
             }
         }
         if constexpr (!Lds::kTwo) {
@@ -1095,6 +1108,7 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
         const Elem<T>* const sm_t = Lds::kTwo ? s.m : s.s;
 #pragma unroll
         for (int y = 0; y < DT / kBand; ++y) {
+            const int part = fresh(lane), li = part % 16, lq = part / 16;
             const int dt = y * kBand + w % kBand;
             Frag<T> fm[VB], fq[KB];
 #pragma unroll
@@ -1119,10 +1133,14 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
                 if (lq == 0) s.far[dt][j] = far, s.near[dt][j] = less;
                 o += o2;
                 if (j < n) give_four(a.dk, t + j, 16 * dt + 4 * lq, o);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         M.decay(s.d.whole);
-        add_rows<T, DK, C>(M, s.q, fdy, s.d.from_start, a.scale, li, lq);
+        {
+            const int part = fresh(lane), li = part % 16, lq = part / 16;
+            add_rows<T, DK, C>(M, s.q, fdy, s.d.from_start, a.scale, li, lq);
+        }
     }
     __syncthreads();
     give_decays();
