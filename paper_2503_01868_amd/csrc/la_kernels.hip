@@ -226,17 +226,14 @@ struct Ahead {
     static constexpr int kPieces = C * D / 8, kEach = (kPieces + NT - 1) / NT, kPerRow = D / 8, W = T::kBytes == 2 ? 4 : 8;
     Words<W> r[kEach];
 
-    static __device__ __forceinline__ bool inside(int i, int n, int c0, int d) {
-        const int at = i * NT + (int)threadIdx.x;
-        return at / kPerRow < n && c0 + at % kPerRow * 8 < d;
-    }
     // n: 1 at least
     __device__ __forceinline__ void load(const Rows& x, const char* from, int n, int c0) {
         if (x.wide) {
             const uint32_t step = (uint32_t)x.step;
+            const int me = fresh((int)threadIdx.x);
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
-                const int at = i * NT + (int)threadIdx.x, c = c0 + at % kPerRow * 8;
+                const int at = i * NT + me, c = c0 + at % kPerRow * 8;
                 const char* p = from + ((uint32_t)min(at / kPerRow, n - 1) * step + (uint32_t)(c < x.d ? c : 0) * T::kBytes);
                 const Words<4> a = load_words<4>(p);
 #pragma unroll
@@ -271,11 +268,12 @@ struct Ahead {
         typedef uint16_t pair_t __attribute__((ext_vector_type(2)));
         pair_t pairs = {0, 0};
         uint32_t one = 0;
+        const int me = fresh((int)threadIdx.x);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int at = i * NT + (int)threadIdx.x, row = at / kPerRow, c = at % kPerRow * 8;
+            const int at = i * NT + me, row = at / kPerRow, c = at % kPerRow * 8;
             if (kPieces % NT != 0 && at >= kPieces) continue;
-            const bool in = inside(i, n, c0, d);
+            const bool in = row < n && c0 + c < d;
 #pragma unroll
             for (int j = 0; j < W; ++j) r[i].w[j] = in ? r[i].w[j] : 0;
 #pragma unroll
@@ -499,8 +497,8 @@ __device__ __forceinline__ double step_sum(float g) { return g < kForgets ? -INF
 // beginnings, from the end on, of rows of q and columns of dy.
 
 template <typename T, int DK, int DV, bool BACK>
-__global__ __launch_bounds__(256, 2) void la_ends_walk_kernel(LaArgs a) {
-    constexpr int C = kChunk<T>, NT = 256, NW = 4, KB = C / 32, DT = DK / 16, CT = DV / NW / 16, WC = 16 * CT;
+__global__ __launch_bounds__(DV * 4, T::kBytes == 2 && DV == 128 ? 4 : 2) void la_ends_walk_kernel(LaArgs a) {
+    constexpr int C = kChunk<T>, NT = DV * 4, KB = C / 32, DT = DK / 16, CT = 1, WC = 16 * CT;
     constexpr int PV = kPitch<T, DV>;
     __shared__ __attribute__((aligned(16))) Elem<T> tile_a[C * kPitch<T, DK>];
     __shared__ __attribute__((aligned(16))) Elem<T> tile_b[C * PV];
@@ -541,6 +539,7 @@ __global__ __launch_bounds__(256, 2) void la_ends_walk_kernel(LaArgs a) {
         const bool at_once = !__syncthreads_or(!fine);
         if (y + 1 < last) load(BACK ? x - 1 : x + 1);
         if (at_once) {
+            const int part = fresh(lane), li = part % 16, lq = part / 16;
             Frag<T> fb[CT][KB];
             own_columns<T, PV>(fb, tile_b, cw, li, lq);
             S.decay(decays.whole);
@@ -548,6 +547,7 @@ __global__ __launch_bounds__(256, 2) void la_ends_walk_kernel(LaArgs a) {
             sum = with_sum(sum, decays.sum);
         } else {
             for (int i = 0, n = steps(x); i < n; ++i) {
+                const int part = fresh(lane), li = part % 16, lq = part / 16;
                 const int64_t t = x * C + (BACK ? n - 1 - i : i);
                 const float g = number<T>(gp + t * a.g.step), half = step_factor(g);
                 // (what goes back has its step's decay behind it, of what the step adds too)
@@ -571,8 +571,8 @@ struct WalkLds {
 };
 
 template <typename T, int DK, int DV, bool MARKS>
-__global__ __launch_bounds__(256, 2) void la_walk_kernel(LaArgs a) {
-    constexpr int C = kChunk<T>, NT = 256, NW = 4, IT = C / 16, KB = C / 32, DT = DK / 16, CT = DV / NW / 16, WC = 16 * CT;
+__global__ __launch_bounds__(DV * 4, T::kBytes == 2 && DV == 128 ? 4 : 2) void la_walk_kernel(LaArgs a) {
+    constexpr int C = kChunk<T>, NW = DV / 16, NT = NW * kWave, IT = C / 16, KB = C / 32, DT = DK / 16, CT = 1, WC = 16 * CT;
     constexpr int PK = kPitch<T, DK>, PV = kPitch<T, DV>, PA = kPitch<T, C>;
     __shared__ __attribute__((aligned(16))) WalkLds<T, DK, DV> s;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, li = lane % 16, lq = lane / 16;
@@ -603,10 +603,11 @@ __global__ __launch_bounds__(256, 2) void la_walk_kernel(LaArgs a) {
     for (int64_t x = first; x < last; ++x) {
         if constexpr (MARKS) {
             char* const m = a.marks + ((at.item * a.chunks + x) * (DK * DV) + w * (DK * WC)) * T::kBytes;
+            const int part = fresh(lane);
 #pragma unroll
             for (int i = 0; i < DT; ++i)
 #pragma unroll
-                for (int j = 0; j < CT; ++j) store_mark<T>(m + ((i * CT + j) * kWave + lane) * 4 * T::kBytes, S.s[i][j]);
+                for (int j = 0; j < CT; ++j) store_mark<T>(m + ((i * CT + j) * kWave + part) * 4 * T::kBytes, S.s[i][j]);
         }
         const int64_t t = x * C;
         const int n = steps(x);
@@ -619,6 +620,7 @@ __global__ __launch_bounds__(256, 2) void la_walk_kernel(LaArgs a) {
         if (x + 1 < last) load(x + 1);
         if (!at_once) {
             for (int i = 0; i < n; ++i) {
+                const int part = fresh(lane), li = part % 16, lq = part / 16;
                 const int64_t u = t + i;
                 S.template step<T>(step_factor(number<T>(gp + u * a.g.step)), kp + u * a.k.step, vp + u * a.v.step, 1.0f, a.dk_, a.dv_, c0 + cw, li, lq);
 #pragma unroll
@@ -810,10 +812,8 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
     const char* gp = a.g.p + at.b * a.g.batch + (int64_t)at.h * T::kBytes;
     const int c0 = at.tile * DV, cw = w * 16;
     const int64_t items = uniform((int32_t)(gridDim.x / (uint32_t)a.segments)), head_state = (at.b * a.H + at.h) * a.dk_ * a.dv_;
-    // where the walks of 4 waves have this wave's columns: piece i of 16 rows is `own` + i * kStep numbers behind
-    constexpr int CT4 = DV / 64, WC4 = 16 * CT4, kStep = CT4 * kWave * 4;
-    const int own_c = cw + li, own_in = own_c % WC4, own_j = CT4 == 2 ? own_in / 4 % 2 : 0, own_l = CT4 == 2 ? own_in / 8 * 4 + own_in % 4 : own_in;
-    const int own = own_c / WC4 * (DK * WC4) + (own_j * kWave + lq * 16 + own_l) * 4;
+    const int own = w * (DK * 16) + lane * 4;  // this lane's numbers in states of the library's own order, piece by piece
+    constexpr int kStep = kWave * 4;
     State<DT, 1> M;  // the gradient of the state behind the chunk
     if (at.segment < a.segments - 1) {
         const float* p = a.ends + ((at.segment + 1) * items + at.item) * (DK * DV) + own;
@@ -940,8 +940,8 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
         if (!at_once) {
             float *const sum_q = reinterpret_cast<float*>(s.q), *const sum_k = reinterpret_cast<float*>(s.k);
             const char* mark = a.marks_in + ((at.item * a.chunks + x) * (DK * DV) + own) * T::kBytes;
-            const int c = c0 + cw + li;
             for (int i = n - 1; i >= 0; --i) {
+                const int part = fresh(lane), li = part % 16, lq = part / 16, c = c0 + cw + li;
                 const int64_t u = t + i;
                 State<DT, 1> S;
 #pragma unroll
@@ -1293,7 +1293,7 @@ hy_status walk(LaArgs a, const LaShape& s, const Cut& c, void* ws, bool out, hip
     const dim3 grid((uint32_t)(items * c.segments));
     if (c.segments > 1) {
         hy_status rc = by_tile(s, [&](auto t, auto dk, auto dv) {
-            return launch_kernel(la_ends_walk_kernel<decltype(t), decltype(dk)::value, decltype(dv)::value, false>, grid, dim3(256), st, a);
+            return launch_kernel(la_ends_walk_kernel<decltype(t), decltype(dk)::value, decltype(dv)::value, false>, grid, dim3(decltype(dv)::value * 4), st, a);
         });
         if (rc == HY_OK) rc = scan_ends(a, s, false, st);
         if (rc != HY_OK) return rc;
@@ -1302,8 +1302,8 @@ hy_status walk(LaArgs a, const LaShape& s, const Cut& c, void* ws, bool out, hip
         using T = decltype(t);
         constexpr int DK = decltype(dk)::value, DV = decltype(dv)::value;
         (void)out;
-        return a.marks ? launch_kernel(la_walk_kernel<T, DK, DV, true>, grid, dim3(256), st, a)
-                       : launch_kernel(la_walk_kernel<T, DK, DV, false>, grid, dim3(256), st, a);
+        return a.marks ? launch_kernel(la_walk_kernel<T, DK, DV, true>, grid, dim3(DV * 4), st, a)
+                       : launch_kernel(la_walk_kernel<T, DK, DV, false>, grid, dim3(DV * 4), st, a);
     });
 }
 
@@ -1380,7 +1380,7 @@ hy_status launch_la_bwd(const LaPtrs& p, const LaShape& s, void* ws, hipStream_t
     hy_status rc = HY_OK;
     if (b.cut.segments > 1) {
         rc = by_tile(s, [&](auto t, auto dk, auto dv) {
-            return launch_kernel(la_ends_walk_kernel<decltype(t), decltype(dk)::value, decltype(dv)::value, true>, grid, dim3(256), st, a);
+            return launch_kernel(la_ends_walk_kernel<decltype(t), decltype(dk)::value, decltype(dv)::value, true>, grid, dim3(decltype(dv)::value * 4), st, a);
         });
         if (rc == HY_OK) rc = scan_ends(a, s, true, st);
         if (rc != HY_OK) return rc;
