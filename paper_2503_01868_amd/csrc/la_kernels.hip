@@ -223,32 +223,38 @@ __device__ __forceinline__ int fresh(int x) {
 // elsewhere in them and becomes zeros in LDS, so that no load waits for a branch (16000 cycles of a chunk's 36000 before).
 template <typename T, int C, int D, int NT>
 struct Ahead {
-    static constexpr int kPieces = C * D / 8, kEach = (kPieces + NT - 1) / NT, kPerRow = D / 8, W = T::kBytes == 2 ? 4 : 8;
+    static constexpr int kPerRow = D / 8, kRows = NT / kPerRow, kEach = C > kRows ? C / kRows : 1, W = T::kBytes == 2 ? 4 : 8;
+    static constexpr bool kIdle = kRows > C;  // lanes behind the last row load another's and put nothing
+    static_assert(NT % kPerRow == 0 && (kIdle || C % kRows == 0), "a lane has the same columns of every kRows-th row");
     Words<W> r[kEach];
 
+    __device__ __forceinline__ void load_one(int i, const char* p) {
+        const Words<4> a = load_words<4>(p);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r[i].w[j] = a.w[j];
+        if constexpr (W == 8) {
+            const Words<4> b = load_words<4>(p + 16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r[i].w[4 + j] = b.w[j];
+        }
+    }
     // n: 1 at least
     __device__ __forceinline__ void load(const Rows& x, const char* from, int n, int c0) {
+        const uint32_t me = (uint32_t)fresh((int)threadIdx.x), row0 = me / kPerRow;
+        const int c = c0 + (int)(me % kPerRow) * 8;
         if (x.wide) {
-            const uint32_t step = (uint32_t)x.step;
-            const int me = fresh((int)threadIdx.x);
+            const uint32_t step = (uint32_t)x.step, at = row0 * step + (uint32_t)(c < x.d ? c : 0) * T::kBytes;
+            if (n == C && !kIdle) {
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                const int at = i * NT + me, c = c0 + at % kPerRow * 8;
-                const char* p = from + ((uint32_t)min(at / kPerRow, n - 1) * step + (uint32_t)(c < x.d ? c : 0) * T::kBytes);
-                const Words<4> a = load_words<4>(p);
+                for (int i = 0; i < kEach; ++i) load_one(i, from + (int64_t)(i * kRows) * x.step + at);
+            } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) r[i].w[j] = a.w[j];
-                if constexpr (W == 8) {
-                    const Words<4> b = load_words<4>(p + 16);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) r[i].w[4 + j] = b.w[j];
-                }
+                for (int i = 0; i < kEach; ++i) load_one(i, from + (min(row0 + i * kRows, (uint32_t)n - 1) * step + (uint32_t)(c < x.d ? c : 0) * T::kBytes));
             }
         } else {
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
-                const int at = i * NT + fresh((int)threadIdx.x), c = c0 + at % kPerRow * 8;
-                const char* p = from + min(at / kPerRow, n - 1) * x.step;
+                const char* p = from + (int64_t)min(row0 + i * kRows, (uint32_t)n - 1) * x.step;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const bool has = c + j < x.d;
@@ -268,14 +274,19 @@ struct Ahead {
         typedef uint16_t pair_t __attribute__((ext_vector_type(2)));
         pair_t pairs = {0, 0};
         uint32_t one = 0;
-        const int me = fresh((int)threadIdx.x);
+        const uint32_t me = (uint32_t)fresh((int)threadIdx.x), row0 = me / kPerRow, c = me % kPerRow * 8;
+        if (n < C || c0 + D > d) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const bool in = row0 + i * kRows < (uint32_t)n && c0 + (int)c < d;
+#pragma unroll
+                for (int j = 0; j < W; ++j) r[i].w[j] = in ? r[i].w[j] : 0;
+            }
+        }
+        Elem<T>* const to = tile + row0 * kPitch<T, D> + c;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int at = i * NT + me, row = at / kPerRow, c = at % kPerRow * 8;
-            if (kPieces % NT != 0 && at >= kPieces) continue;
-            const bool in = row < n && c0 + c < d;
-#pragma unroll
-            for (int j = 0; j < W; ++j) r[i].w[j] = in ? r[i].w[j] : 0;
+            if (kIdle && row0 >= C) continue;
 #pragma unroll
             for (int j = 0; j < W; ++j) {
                 if constexpr (W == 4) pairs = __builtin_elementwise_max(pairs, __builtin_bit_cast(pair_t, r[i].w[j] & 0x7fff7fffu));
@@ -284,7 +295,7 @@ struct Ahead {
 #pragma unroll
             for (int j = 0; j < W; j += 4) {
                 const Words<4> o{{r[i].w[j], r[i].w[j + 1], r[i].w[j + 2], r[i].w[j + 3]}};
-                store_words<4>(tile + row * kPitch<T, D> + c + j * (4 / T::kBytes), o);
+                store_words<4>(to + i * kRows * kPitch<T, D> + j * (4 / T::kBytes), o);
             }
         }
         if constexpr (W == 4) return max(pairs[0], pairs[1]) < most >> 16;
