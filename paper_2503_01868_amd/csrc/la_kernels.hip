@@ -238,47 +238,45 @@ struct Ahead {
             for (int j = 0; j < 4; ++j) r[i].w[4 + j] = b.w[j];
         }
     }
-    // n: 1 at least
+    // n: 1 at least.  (One path: where two of them load the same registers, a load waits for those before it.)
     __device__ __forceinline__ void load(const Rows& x, const char* from, int n, int c0) {
-        const uint32_t me = (uint32_t)fresh((int)threadIdx.x), row0 = me / kPerRow;
+        if (!x.wide) return;
+        const uint32_t me = (uint32_t)fresh((int)threadIdx.x), row0 = me / kPerRow, step = (uint32_t)x.step;
         const int c = c0 + (int)(me % kPerRow) * 8;
-        if (x.wide) {
-            const uint32_t step = (uint32_t)x.step, at = row0 * step + (uint32_t)(c < x.d ? c : 0) * T::kBytes;
-            if (n == C && !kIdle) {
+        const uint32_t at = (uint32_t)(c < x.d ? c : 0) * T::kBytes;
 #pragma unroll
-                for (int i = 0; i < kEach; ++i) load_one(i, from + (int64_t)(i * kRows) * x.step + at);
-            } else {
-#pragma unroll
-                for (int i = 0; i < kEach; ++i) load_one(i, from + (min(row0 + i * kRows, (uint32_t)n - 1) * step + (uint32_t)(c < x.d ? c : 0) * T::kBytes));
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                const char* p = from + (int64_t)min(row0 + i * kRows, (uint32_t)n - 1) * x.step;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const bool has = c + j < x.d;
-                    const char* pj = p + (int64_t)(has ? c + j : 0) * T::kBytes;
-                    if constexpr (W == 8) {
-                        r[i].w[j] = has ? *reinterpret_cast<const uint32_t*>(pj) : 0;
-                    } else {
-                        const uint32_t h = has ? *reinterpret_cast<const uint16_t*>(pj) : 0;
-                        r[i].w[j / 2] = j % 2 ? r[i].w[j / 2] | h << 16 : h;
-                    }
-                }
-            }
-        }
+        for (int i = 0; i < kEach; ++i) load_one(i, from + (min(row0 + i * kRows, (uint32_t)n - 1) * step + at));
     }
-    // whether all are below `most` (bits of a float)
-    __device__ __forceinline__ bool put(Elem<T>* tile, uint32_t most, int n, int c0, int d) {
+    // Whether all are below `most` (bits of a float).  Rows that cannot be moved by 16 bytes are loaded here, number by number.
+    __device__ __forceinline__ bool put(Elem<T>* tile, uint32_t most, const Rows& x, const char* from, int n, int c0) {
         typedef uint16_t pair_t __attribute__((ext_vector_type(2)));
         pair_t pairs = {0, 0};
         uint32_t one = 0;
         const uint32_t me = (uint32_t)fresh((int)threadIdx.x), row0 = me / kPerRow, c = me % kPerRow * 8;
-        if (n < C || c0 + D > d) {
+        if (!x.wide) {
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
-                const bool in = row0 + i * kRows < (uint32_t)n && c0 + (int)c < d;
+                const char* p = from + (int64_t)min(row0 + i * kRows, (uint32_t)n - 1) * x.step;
+                uint32_t f[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int at = c0 + (int)c + j;
+                    const char* pj = p + (int64_t)(at < x.d ? at : 0) * T::kBytes;
+                    if constexpr (W == 8) f[j] = *reinterpret_cast<const uint32_t*>(pj);
+                    else f[j] = *reinterpret_cast<const uint16_t*>(pj);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if (c0 + (int)c + j >= x.d) f[j] = 0;
+                    if constexpr (W == 8) r[i].w[j] = f[j];
+                    else r[i].w[j / 2] = j % 2 ? r[i].w[j / 2] | f[j] << 16 : f[j];
+                }
+            }
+        }
+        if (n < C || c0 + D > x.d) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const bool in = row0 + i * kRows < (uint32_t)n && c0 + (int)c < x.d;
 #pragma unroll
                 for (int j = 0; j < W; ++j) r[i].w[j] = in ? r[i].w[j] : 0;
             }
@@ -531,21 +529,21 @@ __global__ __launch_bounds__(DV * 4, T::kBytes == 2 && DV == 128 ? 4 : 2) void l
     double sum = 0.0;
     Ahead<T, C, DK, NT> next_a;
     Ahead<T, C, DV, NT> next_b;
-    typename Pack<T, 1>::Raw next_g;
+    typename Pack<T, 1>::Raw next_g{};  // (64 lines of memory: the waves' that need it)
     auto steps = [&](int64_t x) { return a.L - x * C < C ? (int)(a.L - x * C) : C; };
     auto load = [&](int64_t x) {
         const int64_t t = x * C;
         const int n = steps(x);
         next_a.load(ra, ap + t * ra.step, n, 0);
         next_b.load(rb, bp + t * rb.step, n, c0);
-        next_g = Pack<T, 1>::load(gp + (t + min(lane, n - 1)) * a.g.step);
+        if (w == 0) next_g = Pack<T, 1>::load(gp + (t + min(lane, n - 1)) * a.g.step);
     };
     load(BACK ? last - 1 : first);
     for (int64_t y = first; y < last; ++y) {
         const int64_t x = BACK ? last - 1 - (y - first) : y;
         __syncthreads();  // nobody reads the chunk before any more
-        bool fine = next_a.put(tile_a, a.most, steps(x), 0, ra.d);
-        fine &= next_b.put(tile_b, a.most, steps(x), c0, rb.d);
+        bool fine = next_a.put(tile_a, a.most, ra, ap + x * C * ra.step, steps(x), 0);
+        fine &= next_b.put(tile_b, a.most, rb, bp + x * C * rb.step, steps(x), c0);
         if (w == 0) fine &= make_decays<C>(decays, lane < steps(x) ? unpacked<T>(next_g) : 0.0f, lane);
         const bool at_once = !__syncthreads_or(!fine);
         if (y + 1 < last) load(BACK ? x - 1 : x + 1);
@@ -600,7 +598,7 @@ __global__ __launch_bounds__(DV * 4, T::kBytes == 2 && DV == 128 ? 4 : 2) void l
     const int64_t first = at.segment * a.each, last = first + a.each < a.chunks ? first + a.each : a.chunks;
     Ahead<T, C, DK, NT> next_q, next_k;
     Ahead<T, C, DV, NT> next_v;
-    typename Pack<T, 1>::Raw next_g;
+    typename Pack<T, 1>::Raw next_g{};  // (64 lines of memory: the waves' that need it)
     auto steps = [&](int64_t x) { return a.L - x * C < C ? (int)(a.L - x * C) : C; };
     auto load = [&](int64_t x) {
         const int64_t t = x * C;
@@ -608,7 +606,7 @@ __global__ __launch_bounds__(DV * 4, T::kBytes == 2 && DV == 128 ? 4 : 2) void l
         next_k.load(a.k, kp + t * a.k.step, n, 0);
         next_q.load(a.q, qp + t * a.q.step, n, 0);
         next_v.load(a.v, vp + t * a.v.step, n, c0);
-        next_g = Pack<T, 1>::load(gp + (t + min(lane, n - 1)) * a.g.step);
+        if (w == 0) next_g = Pack<T, 1>::load(gp + (t + min(lane, n - 1)) * a.g.step);
     };
     load(first);
     for (int64_t x = first; x < last; ++x) {
@@ -623,9 +621,9 @@ __global__ __launch_bounds__(DV * 4, T::kBytes == 2 && DV == 128 ? 4 : 2) void l
         const int64_t t = x * C;
         const int n = steps(x);
         __syncthreads();  // nobody reads the chunk before any more
-        bool fine = next_k.put(s.k, a.most, n, 0, a.k.d);
-        fine &= next_q.put(s.q, a.most, n, 0, a.q.d);
-        fine &= next_v.put(s.v, a.most, n, c0, a.v.d);
+        bool fine = next_k.put(s.k, a.most, a.k, kp + t * a.k.step, n, 0);
+        fine &= next_q.put(s.q, a.most, a.q, qp + t * a.q.step, n, 0);
+        fine &= next_v.put(s.v, a.most, a.v, vp + t * a.v.step, n, c0);
         if (w == 0) fine &= make_decays<C>(s.d, lane < n ? unpacked<T>(next_g) : 0.0f, lane);
         const bool at_once = !__syncthreads_or(!fine);
         if (x + 1 < last) load(x + 1);
@@ -877,7 +875,7 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
     Ahead<T, C, DK, NT> next_q, next_k;
     Ahead<T, C, DV, NT> next_v, next_dy;
     typename Pack<T, 4>::Raw next_s[DT];
-    typename Pack<T, 1>::Raw next_g;
+    typename Pack<T, 1>::Raw next_g{};  // (64 lines of memory: the waves' that need it)
     float g_now = 0.0f;
     auto load = [&](int64_t x) {
         const int64_t t = x * C;
@@ -889,7 +887,7 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
         const char* p = a.marks_in + ((at.item * a.chunks + x) * (DK * DV) + own) * T::kBytes;
 #pragma unroll
         for (int i = 0; i < DT; ++i) next_s[i] = Pack<T, 4>::load(p + i * kStep * T::kBytes);
-        next_g = Pack<T, 1>::load(gp + (t + min(lane, n - 1)) * a.g.step);
+        if (w == 0 || w == NW - 1) next_g = Pack<T, 1>::load(gp + (t + min(lane, n - 1)) * a.g.step);
     };
     // The last wave's: gradients of the log decays of a chunk that was taken at once.  Pairs of steps on both sides of decay t: those
     // with an earlier step in front of the chunk and a later one behind it; those with a later one behind it; of those inside the
@@ -917,10 +915,10 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
         const int n = steps(x);
         __syncthreads();  // nobody reads the chunk behind any more
         give_decays();
-        bool fine = next_q.put(s.q, a.most, n, 0, a.q.d);
-        fine &= next_k.put(s.k, a.most, n, 0, a.k.d);
-        fine &= next_v.put(s.v, a.most, n, c0, a.v.d);
-        fine &= next_dy.put(s.dy, a.most, n, c0, a.dy.d);
+        bool fine = next_q.put(s.q, a.most, a.q, qp + t * a.q.step, n, 0);
+        fine &= next_k.put(s.k, a.most, a.k, kp + t * a.k.step, n, 0);
+        fine &= next_v.put(s.v, a.most, a.v, vp + t * a.v.step, n, c0);
+        fine &= next_dy.put(s.dy, a.most, a.dy, dyp + t * a.dy.step, n, c0);
         {
             Elem<T>* p = s.s + (cw + li) * PK + 4 * lq;
 #pragma unroll
