@@ -195,62 +195,93 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_bwd_kernel(NormArg
 #pragma unroll
             for (int j = 0; j < VEC; ++j) mine[i * VEC + j] = 0.0f;
     int turn = 0;
-    for (int64_t n = group; n < a.N; n += (int64_t)gridDim.x * kRows, turn ^= 1) {
-        const char *hrow = static_cast<const char*>(a.p.h) + n * a.D * T::kBytes, *dyrow = static_cast<const char*>(a.p.dy) + n * a.D * T::kBytes;
-        const float rstd = a.p.rstd[n];
-        float h[N][VEC], dy[N][VEC];
-        float sum = 0.0f, none = 0.0f;
-        auto take = [&](int64_t i, float (&fh)[VEC], float (&fd)[VEC], float (&share)[VEC]) {
-            piece_nt<T, VEC>(hrow, i, a.D, fh);
-            piece_nt<T, VEC>(dyrow, i, a.D, fd);
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) share[j] = fmaf(fd[j] * fh[j], rstd, share[j]);
-            if (w) {
-                float fw[VEC];
-                piece<T, VEC>(w, i, a.D, fw);
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) fd[j] *= fw[j];
-            }
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) sum = fmaf(fd[j], fh[j], sum);
-        };
-        if constexpr (LONG) {
+    if constexpr (LONG) {
+        for (int64_t n = group; n < a.N; n += (int64_t)gridDim.x * kRows, turn ^= 1) {
+            const char *hrow = static_cast<const char*>(a.p.h) + n * a.D * T::kBytes, *dyrow = static_cast<const char*>(a.p.dy) + n * a.D * T::kBytes;
+            const float rstd = a.p.rstd[n];
+            float h[VEC], dy[VEC], fw[VEC];
+            float sum = 0.0f, none = 0.0f;
             for (int64_t i = lane; i < pieces; i += TPR) {
-                float share[VEC] = {};
-                take(i, h[0], dy[0], share);
+                piece_nt<T, VEC>(hrow, i, a.D, h);
+                piece_nt<T, VEC>(dyrow, i, a.D, dy);
                 if (partial)
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) mine[i * VEC + j] += share[j];
-            }
-        } else {
+                    for (int j = 0; j < VEC; ++j) mine[i * VEC + j] = fmaf(dy[j] * h[j], rstd, mine[i * VEC + j]);
+                if (w) piece<T, VEC>(w, i, a.D, fw);
 #pragma unroll
-            for (int x = 0; x < N; ++x) take(x * TPR + lane, h[x], dy[x], dw[x]);
+                for (int j = 0; j < VEC; ++j) sum = fmaf(w ? dy[j] * fw[j] : dy[j], h[j], sum);
+            }
+            over_row<TPR, false>(sum, none, lds, turn);
+            const float c = sum * a.inverse * (rstd * rstd);
+            for (int64_t i = lane; i < pieces; i += TPR) {
+                float o[VEC], more[VEC] = {};
+                piece<T, VEC>(hrow, i, a.D, h);
+                piece<T, VEC>(dyrow, i, a.D, dy);
+                if (w) piece<T, VEC>(w, i, a.D, fw);
+                if (dh) piece_nt<T, VEC>(dh + n * a.D * T::kBytes, i, a.D, more);
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) o[j] = fmaf(rstd, (w ? dy[j] * fw[j] : dy[j]) - h[j] * c, more[j]);
+                Pack<T, VEC>::store(static_cast<char*>(a.p.dx) + (n * a.D + i * VEC) * T::kBytes, Pack<T, VEC>::pack(o));
+            }
+        }
+        return;
+    }
+    // A row's numbers are on their way while the row before is summed: 8192 rows of 4096 bf16 numbers 90 us without it.
+    using Raw = typename Pack<T, VEC>::Raw;
+    Raw next_h[N], next_dy[N], next_dh[N], raw_w[N];
+    float next_rstd = 0.0f;
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    auto load = [&](int64_t n) {
+        const int64_t row = n * a.D;
+#pragma unroll
+        for (int x = 0; x < N; ++x) {
+            const int64_t i = x * TPR + lane;
+            if (i >= pieces) continue;
+            next_h[x] = Pack<T, VEC>::load_nt(static_cast<const char*>(a.p.h) + (row + i * VEC) * T::kBytes);
+            next_dy[x] = Pack<T, VEC>::load_nt(static_cast<const char*>(a.p.dy) + (row + i * VEC) * T::kBytes);
+            if (dh) next_dh[x] = Pack<T, VEC>::load_nt(dh + (row + i * VEC) * T::kBytes);
+        }
+        next_rstd = a.p.rstd[n];
+    };
+    if (w)
+#pragma unroll
+        for (int x = 0; x < N; ++x)
+            if (x * TPR + lane < pieces) raw_w[x] = Pack<T, VEC>::load(w + (int64_t)(x * TPR + lane) * VEC * T::kBytes);
+    if (group < a.N) load(group);
+    for (int64_t n = group; n < a.N; n += step, turn ^= 1) {
+        const float rstd = next_rstd;
+        Raw rh[N], rdy[N], rdh[N];
+        float sum = 0.0f, none = 0.0f;
+#pragma unroll
+        for (int x = 0; x < N; ++x) rh[x] = next_h[x], rdy[x] = next_dy[x], rdh[x] = next_dh[x];
+        if (n + step < a.N) load(n + step);
+#pragma unroll
+        for (int x = 0; x < N; ++x) {
+            if (x * TPR + lane >= pieces) continue;
+            float h[VEC], dy[VEC], fw[VEC];
+            Pack<T, VEC>::unpack(rh[x], h);
+            Pack<T, VEC>::unpack(rdy[x], dy);
+            if (w) Pack<T, VEC>::unpack(raw_w[x], fw);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                dw[x][j] = fmaf(dy[j] * h[j], rstd, dw[x][j]);
+                sum = fmaf(w ? dy[j] * fw[j] : dy[j], h[j], sum);
+            }
         }
         over_row<TPR, false>(sum, none, lds, turn);
         const float c = sum * a.inverse * (rstd * rstd);
-        auto give = [&](int64_t i, const float (&fh)[VEC], const float (&fd)[VEC]) {
-            if (i >= pieces) return;
-            float o[VEC], more[VEC] = {};
-            if (dh) piece_nt<T, VEC>(dh + n * a.D * T::kBytes, i, a.D, more);
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) o[j] = fmaf(rstd, fd[j] - fh[j] * c, more[j]);
+        for (int x = 0; x < N; ++x) {
+            const int64_t i = x * TPR + lane;
+            if (i >= pieces) continue;
+            float h[VEC], dy[VEC], fw[VEC], more[VEC] = {}, o[VEC];
+            Pack<T, VEC>::unpack(rh[x], h);
+            Pack<T, VEC>::unpack(rdy[x], dy);
+            if (w) Pack<T, VEC>::unpack(raw_w[x], fw);
+            if (dh) Pack<T, VEC>::unpack(rdh[x], more);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) o[j] = fmaf(rstd, (w ? dy[j] * fw[j] : dy[j]) - h[j] * c, more[j]);
             Pack<T, VEC>::store(static_cast<char*>(a.p.dx) + (n * a.D + i * VEC) * T::kBytes, Pack<T, VEC>::pack(o));
-        };
-        if constexpr (LONG) {
-            for (int64_t i = lane; i < pieces; i += TPR) {
-                piece<T, VEC>(hrow, i, a.D, h[0]);
-                piece<T, VEC>(dyrow, i, a.D, dy[0]);
-                if (w) {
-                    float fw[VEC];
-                    piece<T, VEC>(w, i, a.D, fw);
-#pragma unroll
-                    for (int j = 0; j < VEC; ++j) dy[0][j] *= fw[j];
-                }
-                give(i, h[0], dy[0]);
-            }
-        } else {
-#pragma unroll
-            for (int x = 0; x < N; ++x) give(x * TPR + lane, h[x], dy[x]);
         }
     }
     if constexpr (!LONG) {
