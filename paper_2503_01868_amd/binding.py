@@ -106,7 +106,7 @@ class _Unmarshalled:
     def _none(*args):
         return None
 
-    gated = bwd = chain_fwd = chain_bwd = li = _none
+    gated = bwd = chain_fwd = chain_bwd = li = norm_fwd = norm_bwd = la_step = sample = _none
 
 
 _fast = _Unmarshalled
@@ -124,7 +124,8 @@ def _load_fast() -> None:
         module.init(tuple(ctypes.cast(getattr(_lib, name), ctypes.c_void_p).value for name in (
             "hyena_se_fwd", "hyena_mr_fwd", "hyena_se_bwd", "hyena_mr_bwd", "hyena_bwd_workspace_bytes", "hyena_chain_fwd",
             "hyena_chain_workspace_bytes", "hyena_chain_bwd", "hyena_chain_bwd_workspace_bytes", "hyena_li_fwd",
-            "hyena_li_workspace_bytes")), _current_raw_stream)
+            "hyena_li_workspace_bytes", "hyena_rmsnorm_fwd", "hyena_rmsnorm_bwd", "hyena_rmsnorm_bwd_workspace_bytes",
+            "hyena_la_step", "hyena_sample")), _current_raw_stream)
     except (ImportError, OSError, AttributeError) as e:
         warnings.warn("native marshalling not loaded, calls are marshalled through ctypes: %s" % e, RuntimeWarning)
         return

@@ -10,6 +10,7 @@ import ctypes
 
 import torch
 
+from . import binding
 from .binding import HY_OK, HyenaError, _dtype_code, _on, _stream, lib
 from .model_ops import _ptr, _under, _workspace
 
@@ -167,6 +168,10 @@ def hyena_la_bwd(dy, q, k, v, g, scale: float = 1.0, marks=None, state_in=None, 
 def hyena_la_step(q, k, v, g, state, scale: float = 1.0, out=None, stream=None) -> torch.Tensor:
     """One token of B sequences: updates the float32 [B, H, dk, dv] ``state`` in place and returns y [B, H, dv], from ``q`` and
     ``k`` [B, H // group, dk], ``v`` [B, H, dv] and ``g`` [B, H]; see ``hyena_la_step`` in hyena.h."""
+    if out is None and stream is None:
+        y = binding._fast.la_step(q, k, v, g, state, scale)
+        if y is not None:
+            return y
     (B,), H, group, dk, dv, code = _la_sizes(q, k, v, g, 3)
     for name, t in (("q", q), ("k", k), ("v", v), ("g", g)):
         if not t.is_contiguous():
@@ -250,6 +255,10 @@ def hyena_rmsnorm_fwd(x, w=None, residual=None, eps: float = 1e-6, total=None, w
     last dimension; ``w`` [D] or None.  ``total``: where the sum goes, the residual itself to add in place.  rstd, float32, is None
     unless ``want_rstd``; ``hyena_rmsnorm_bwd`` takes it and the sum.  x and the residual may be views whose rows are the same
     distance apart; see ``hyena_rmsnorm_fwd`` in hyena.h."""
+    if total is None and out is None and stream is None:
+        made = binding._fast.norm_fwd(x, w, residual, eps, want_rstd)
+        if made is not None:
+            return made
     y, _, total, rstd = _norm_fwd(x, w, residual, eps, total, want_rstd, out, False, stream, "hyena_rmsnorm_fwd")
     return y, total, rstd
 
@@ -264,6 +273,10 @@ def hyena_rmsnorm_bwd(dy, total, rstd, w=None, dtotal=None, want_dw: bool = True
     """(dx, dw) of ``hyena_rmsnorm_fwd`` (of its 8-bit form too), given what it returned: dx is the gradient of x and of the
     residual alike, with ``dtotal``, what comes back along the residual, added.  ``dx``: where it goes, ``dtotal`` or ``dy``
     themselves to write in place.  dw is None without weights; see ``hyena_rmsnorm_bwd`` in hyena.h."""
+    if dx is None and workspace is None and stream is None:
+        made = binding._fast.norm_bwd(dy, total, rstd, w, dtotal, want_dw)
+        if made is not None:
+            return made
     N, D, _ = _rows("dy", dy)
     if D < 1:
         raise ValueError("dy must have at least one channel")
@@ -303,6 +316,10 @@ def hyena_sample(logits, u, temperature=1.0, top_k=None, top_p=None, min_p=None,
     weight, of them those with at least ``min_p`` times the likeliest's; the token, int64, is where the running sum of what is kept
     passes u, and prob, float32, the probability it was drawn with (None unless ``want_prob``).  A temperature of 0 takes the largest logit.  Each setting
     is a number, a tensor with one for every row (float32; top_k int32), or None; see ``hyena_sample`` in hyena.h."""
+    if want_prob and stream is None:
+        made = binding._fast.sample(logits, u, temperature, top_k, top_p, min_p)
+        if made is not None:
+            return made
     if not isinstance(logits, torch.Tensor) or not logits.is_cuda or logits.dim() != 2 or logits.shape[1] < 1:
         raise ValueError("logits must be a [N, V] tensor on the GPU")
     N, V = logits.shape

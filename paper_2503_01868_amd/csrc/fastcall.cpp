@@ -32,8 +32,13 @@ struct Entries {
     decltype(&hyena_chain_bwd_workspace_bytes) chain_bwd_workspace;
     decltype(&hyena_li_fwd) li_fwd;
     decltype(&hyena_li_workspace_bytes) li_workspace;
+    decltype(&hyena_rmsnorm_fwd) norm_fwd;
+    decltype(&hyena_rmsnorm_bwd) norm_bwd;
+    decltype(&hyena_rmsnorm_bwd_workspace_bytes) norm_bwd_workspace;
+    decltype(&hyena_la_step) la_step;
+    decltype(&hyena_sample) sample;
 } e;
-constexpr int kEntries = 11;
+constexpr int kEntries = 16;
 static_assert(sizeof(Entries) == kEntries * sizeof(void*), "a table of addresses");
 PyObject* raw_stream = nullptr;
 
@@ -54,6 +59,23 @@ const at::Tensor* plain(PyObject* o) {
     return &t;
 }
 
+// The type's code and the current stream of a tensor on the current GPU.
+bool here(const at::Tensor& x, int& code, void*& stream) {
+    const auto type = x.scalar_type();
+    if (type != at::kFloat && type != at::kBFloat16) return false;
+    if (c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice() != x.device()) return false;
+    code = type == at::kFloat ? HY_F32 : HY_BF16;
+    PyObject* index = PyLong_FromLong(x.device().index());
+    if (!index) throw python_error();
+    PyObject* s = PyObject_CallOneArg(raw_stream, index);
+    Py_DECREF(index);
+    if (!s) throw python_error();
+    stream = PyLong_AsVoidPtr(s);
+    Py_DECREF(s);
+    if (PyErr_Occurred()) throw python_error();
+    return true;
+}
+
 struct Problem {
     int64_t B, L, D, group;
     int code;
@@ -70,27 +92,15 @@ bool activations(PyObject* const* a, int n, PyObject* group, Problem& p) {
     }
     const at::Tensor& x = *p.x[0];
     if (x.dim() != 3 || x.numel() == 0) return false;
-    const auto type = x.scalar_type();
-    if (type != at::kFloat && type != at::kBFloat16) return false;
     for (int i = 1; i < n; ++i)
-        if (p.x[i]->sizes() != x.sizes() || p.x[i]->scalar_type() != type || p.x[i]->device() != x.device()) return false;
-    if (c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice() != x.device()) return false;
+        if (p.x[i]->sizes() != x.sizes() || p.x[i]->scalar_type() != x.scalar_type() || p.x[i]->device() != x.device()) return false;
     p.B = x.size(0);
     p.L = x.size(1);
     p.D = x.size(2);
-    p.code = type == at::kFloat ? HY_F32 : HY_BF16;
     int overflow = 0;
     p.group = PyLong_AsLongLongAndOverflow(group, &overflow);
     if (overflow || p.group < 1 || p.group > 0x7fffffff) return false;
-    PyObject* index = PyLong_FromLong(x.device().index());
-    if (!index) throw python_error();
-    PyObject* s = PyObject_CallOneArg(raw_stream, index);
-    Py_DECREF(index);
-    if (!s) throw python_error();
-    p.stream = PyLong_AsVoidPtr(s);
-    Py_DECREF(s);
-    if (PyErr_Occurred()) throw python_error();
-    return true;
+    return here(x, p.code, p.stream);
 }
 
 // taps per filter of a [D / group, taps] table beside the activations, or 0
@@ -116,6 +126,7 @@ bool launched(F&& call) {
     return rc == HY_OK;
 }
 
+// (an undefined tensor is None)
 PyObject* tuple_of(std::initializer_list<at::Tensor> ts) {
     PyObject* r = PyTuple_New((Py_ssize_t)ts.size());
     if (!r) throw python_error();
@@ -268,6 +279,141 @@ PyObject* li(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// None, or a plain tensor of these sizes and type on x's GPU; false for anything else
+bool optional(PyObject* o, const at::Tensor& x, at::IntArrayRef sizes, at::ScalarType type, const at::Tensor*& t) {
+    t = nullptr;
+    if (o == Py_None) return true;
+    t = plain(o);
+    return t && t->sizes() == sizes && t->scalar_type() == type && t->device() == x.device();
+}
+void* address(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
+
+// [..., D] activations of at least one row
+const at::Tensor* rows(PyObject* o, int64_t& N, int64_t& D) {
+    const at::Tensor* x = plain(o);
+    if (!raw_stream || !plain_context() || !x || x->dim() < 1 || x->numel() == 0) return nullptr;
+    D = x->size(-1);
+    N = x->numel() / D;
+    return x;
+}
+
+// (x, w, residual, eps, want_rstd) -> (y, total, rstd)
+PyObject* norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int64_t N, D;
+    int code;
+    void* stream;
+    const at::Tensor *x = n == 5 ? rows(a[0], N, D) : nullptr, *w, *r;
+    if (!x || !PyFloat_CheckExact(a[3]) || !PyBool_Check(a[4]) || !optional(a[1], *x, x->sizes().slice(x->dim() - 1), x->scalar_type(), w) ||
+        !optional(a[2], *x, x->sizes(), x->scalar_type(), r) || !here(*x, code, stream))
+        Py_RETURN_NONE;
+    const double eps = PyFloat_AS_DOUBLE(a[3]);
+    const at::Tensor y = at::empty_like(*x), total = r ? at::empty_like(*x) : at::Tensor(),
+                     rstd = a[4] == Py_True ? at::empty(x->sizes().slice(0, x->dim() - 1), x->options().dtype(at::kFloat)) : at::Tensor();
+    void *xp = x->data_ptr(), *rp = address(r), *wp = address(w), *yp = y.data_ptr(), *tp = address(total), *sp = address(rstd);
+    if (!launched([&] { return e.norm_fwd(xp, rp, wp, yp, nullptr, tp, static_cast<float*>(sp), N, D, D, r ? D : 0, eps, code, stream); }))
+        Py_RETURN_NONE;
+    return tuple_of({y, r ? total : *x, rstd});
+    END_HANDLE_TH_ERRORS
+}
+
+// (dy, total, rstd, w, dtotal, want_dw) -> (dx, dw)
+PyObject* norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int64_t N, D;
+    int code;
+    void* stream;
+    const at::Tensor *dy = n == 6 ? rows(a[0], N, D) : nullptr, *h, *s, *w, *dh;
+    if (!dy || !PyBool_Check(a[5]) || !optional(a[1], *dy, dy->sizes(), dy->scalar_type(), h) || !h ||
+        !optional(a[2], *dy, dy->sizes().slice(0, dy->dim() - 1), at::kFloat, s) || !s ||
+        !optional(a[3], *dy, dy->sizes().slice(dy->dim() - 1), dy->scalar_type(), w) ||
+        !optional(a[4], *dy, dy->sizes(), dy->scalar_type(), dh) || !here(*dy, code, stream))
+        Py_RETURN_NONE;
+    const bool want = w && a[5] == Py_True;
+    const int64_t need = want ? e.norm_bwd_workspace(N, D, code) : 0;
+    if (need < 0) Py_RETURN_NONE;
+    const at::Tensor dx = at::empty_like(*dy), dw = want ? at::empty_like(*w) : at::Tensor(),
+                     ws = need > 0 ? at::empty({need}, dy->options().dtype(at::kByte)) : at::Tensor();
+    void *yp = dy->data_ptr(), *hp = h->data_ptr(), *sp = s->data_ptr(), *wp = address(w), *dhp = address(dh), *xp = dx.data_ptr(),
+         *dwp = address(dw), *wsp = address(ws);
+    if (!launched([&] { return e.norm_bwd(yp, hp, static_cast<float*>(sp), wp, dhp, xp, dwp, wsp, need, N, D, code, stream); })) Py_RETURN_NONE;
+    return tuple_of({dx, dw});
+    END_HANDLE_TH_ERRORS
+}
+
+// (q, k, v, g, state, scale) -> y
+PyObject* la_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 6 || !raw_stream || !plain_context() || !PyFloat_CheckExact(a[5])) Py_RETURN_NONE;
+    const at::Tensor* t[5];
+    for (int i = 0; i < 5; ++i)
+        if (!(t[i] = plain(a[i]))) Py_RETURN_NONE;
+    const at::Tensor &q = *t[0], &k = *t[1], &v = *t[2], &g = *t[3], &state = *t[4];
+    if (v.dim() != 3 || q.dim() != 3 || v.numel() == 0 || q.numel() == 0) Py_RETURN_NONE;
+    const int64_t B = v.size(0), H = v.size(1), dv = v.size(2), dk = q.size(2), group = H / q.size(1);
+    if (q.size(0) != B || H % q.size(1) != 0 || k.sizes() != q.sizes() || g.dim() != 2 || g.size(0) != B || g.size(1) != H ||
+        state.dim() != 4 || state.size(0) != B || state.size(1) != H || state.size(2) != dk || state.size(3) != dv ||
+        state.scalar_type() != at::kFloat || group > 0x7fffffff)
+        Py_RETURN_NONE;
+    for (int i = 0; i < 5; ++i)
+        if (t[i]->device() != v.device() || (i < 4 && t[i]->scalar_type() != v.scalar_type())) Py_RETURN_NONE;
+    int code;
+    void* stream;
+    if (!here(v, code, stream)) Py_RETURN_NONE;
+    const double scale = PyFloat_AS_DOUBLE(a[5]);
+    const at::Tensor y = at::empty_like(v);
+    void *qp = q.data_ptr(), *kp = k.data_ptr(), *vp = v.data_ptr(), *gp = g.data_ptr(), *sp = state.data_ptr(), *yp = y.data_ptr();
+    if (!launched([&] { return e.la_step(qp, kp, vp, gp, static_cast<float*>(sp), yp, B, H, (int32_t)group, dk, dv, scale, code, stream); }))
+        Py_RETURN_NONE;
+    return THPVariable_Wrap(y);
+    END_HANDLE_TH_ERRORS
+}
+
+// A setting of every row, or the one number of all; false for anything else
+bool setting(PyObject* o, const at::Tensor& x, at::IntArrayRef each, at::ScalarType type, double otherwise, const at::Tensor*& t, double& one) {
+    one = otherwise;
+    t = nullptr;
+    if (o == Py_None) return true;
+    if (PyFloat_CheckExact(o)) {
+        one = PyFloat_AS_DOUBLE(o);
+        return type == at::kFloat;
+    }
+    if (PyLong_CheckExact(o)) {
+        int overflow = 0;
+        const long long v = PyLong_AsLongLongAndOverflow(o, &overflow);
+        one = (double)v;
+        return !overflow && v > -(1 << 30) && v < 1 << 30;
+    }
+    return optional(o, x, each, type, t);
+}
+
+// (logits, u, temperature, top_k, top_p, min_p) -> (token, prob)
+PyObject* sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const at::Tensor* z = n == 6 && raw_stream && plain_context() ? plain(a[0]) : nullptr;
+    if (!z || z->dim() != 2 || z->numel() == 0) Py_RETURN_NONE;
+    const int64_t N = z->size(0), V = z->size(1), each[1] = {N};
+    const at::Tensor *u, *t, *k, *p, *m;
+    double t1, k1, p1, m1;
+    int code;
+    void* stream;
+    if (!optional(a[1], *z, each, at::kFloat, u) || !u || !setting(a[2], *z, each, at::kFloat, 1.0, t, t1) ||
+        !setting(a[3], *z, each, at::kInt, 0.0, k, k1) || !setting(a[4], *z, each, at::kFloat, 1.0, p, p1) ||
+        !setting(a[5], *z, each, at::kFloat, 0.0, m, m1) || !here(*z, code, stream))
+        Py_RETURN_NONE;
+    const at::Tensor token = at::empty(each, z->options().dtype(at::kLong)), prob = at::empty(each, z->options().dtype(at::kFloat));
+    void *zp = z->data_ptr(), *up = u->data_ptr(), *tp = address(t), *kp = address(k), *pp = address(p), *mp = address(m), *op = token.data_ptr(),
+         *qp = prob.data_ptr();
+    auto f = [](void* x) { return static_cast<float*>(x); };
+    if (!launched([&] {
+            return e.sample(zp, f(up), f(tp), t1, static_cast<int32_t*>(kp), (int32_t)k1, f(pp), p1, f(mp), m1, static_cast<int64_t*>(op), f(qp), N, V,
+                            N > 1 ? V : 0, code, stream);
+        }))
+        Py_RETURN_NONE;
+    return tuple_of({token, prob});
+    END_HANDLE_TH_ERRORS
+}
+
 // (addresses in the order of Entries, callable: device index -> raw stream)
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (n != 2 || !PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) != kEntries || !PyCallable_Check(a[1])) {
@@ -286,7 +432,8 @@ PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 #define FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {FAST(gated), FAST(bwd), FAST(chain_fwd), FAST(chain_bwd), FAST(li), FAST(init), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {FAST(gated), FAST(bwd), FAST(chain_fwd), FAST(chain_bwd), FAST(li),
+                         FAST(norm_fwd), FAST(norm_bwd), FAST(la_step), FAST(sample), FAST(init), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
