@@ -321,7 +321,7 @@ struct LaArgs {
     float* ends;           // states (and their gradients) at the segments' ends: [segment][head and tile][DK DV], and their log2 decays
     double* sums;
     int64_t L, chunks, each;  // chunks of a segment
-    int32_t H, group, dk_, dv_, tiles, segments, shares;
+    int32_t H, group, dk_, dv_, tiles, segments, finer;  // finer: segments of the ends for one of the walk
     float scale;
     uint32_t most;  // numbers of chunks that are taken at once are below, as bits of a float
 };
@@ -825,7 +825,7 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
     constexpr int kStep = kWave * 4;
     State<DT, 1> M;  // the gradient of the state behind the chunk
     if (at.segment < a.segments - 1) {
-        const float* p = a.ends + ((at.segment + 1) * items + at.item) * (DK * DV) + own;
+        const float* p = a.ends + ((int64_t)(at.segment + 1) * a.finer * items + at.item) * (DK * DV) + own;
 #pragma unroll
         for (int i = 0; i < DT; ++i) M.s[i][0] = *reinterpret_cast<const f32x4_t*>(p + i * kStep);
     } else if (a.dstate_out) {
@@ -1318,15 +1318,26 @@ hy_status walk(LaArgs a, const LaShape& s, const Cut& c, void* ws, bool out, hip
 
 // Workspace of the backward call: segments' ends, shares of dq and dk, shares of dg, and marks, if the caller has none.
 struct BwdParts {
-    Cut cut, walk_cut;
+    Cut cut, walk_cut, ends_cut;
+    int32_t finer;  // segments that the gradients' ends are walked in, for each of the backward walk's
     int64_t ends, shares, dg, marks, y, all;  // bytes
     int32_t count;
 };
 BwdParts bwd_parts(const LaShape& s, bool with_marks) {
     BwdParts b{};
     b.cut = cut(s, kBackwardGroups), b.walk_cut = cut(s, kForwardGroups);
+    // The walk of the ends has room for two workgroups on a compute unit where the backward walk has one: halves of its segments
+    // (8192 x 32 heads of 128: 53 us in 8 segments of 16 chunks).
+    b.finer = b.cut.segments > 1 && b.cut.each >= 8 ? 2 : 1;
+    if (b.finer == 2) {
+        const int64_t chunks = chunks_of(s), each = (b.cut.each + 1) / 2 * 2;
+        b.cut = Cut{(chunks + each - 1) / each, each};
+        b.ends_cut = Cut{(chunks + each / 2 - 1) / (each / 2), each / 2};
+    } else {
+        b.ends_cut = b.cut;
+    }
     b.count = (int32_t)(s.group * tiles_of(s));
-    b.ends = up16(ends_bytes(s, b.cut));
+    b.ends = up16(ends_bytes(s, b.ends_cut));
     if (!with_marks && ends_bytes(s, b.walk_cut) > b.ends) b.ends = up16(ends_bytes(s, b.walk_cut));
     b.shares = b.count > 1 ? up16(b.count * s.B * s.L * (s.H / s.group) * s.dk * 4) : 0;
     b.dg = tiles_of(s) > 1 ? up16(tiles_of(s) * s.B * s.L * s.H * 4) : 0;
@@ -1381,17 +1392,20 @@ hy_status launch_la_bwd(const LaPtrs& p, const LaShape& s, void* ws, hipStream_t
         a.marks_in = marks;
     }
     const int64_t items = items_of(s);
-    a.segments = (int32_t)b.cut.segments, a.each = b.cut.each;
-    a.ends = reinterpret_cast<float*>(base), a.sums = reinterpret_cast<double*>(a.ends + b.cut.segments * items * state_size(s));
+    a.segments = (int32_t)b.cut.segments, a.each = b.cut.each, a.finer = b.finer;
+    a.ends = reinterpret_cast<float*>(base), a.sums = reinterpret_cast<double*>(a.ends + b.ends_cut.segments * items * state_size(s));
     a.dv = static_cast<char*>(p.dv);
     a.dq = b.count > 1 ? shares_q : p.dq, a.dk = b.count > 1 ? shares_k : p.dk, a.dg = b.dg > 0 ? shares_g : p.dg;
     const dim3 grid((uint32_t)(items * b.cut.segments));
     hy_status rc = HY_OK;
     if (b.cut.segments > 1) {
+        LaArgs f = a;
+        f.segments = (int32_t)b.ends_cut.segments, f.each = b.ends_cut.each;
+        const dim3 ends_grid((uint32_t)(items * b.ends_cut.segments));
         rc = by_tile(s, [&](auto t, auto dk, auto dv) {
-            return launch_kernel(la_ends_walk_kernel<decltype(t), decltype(dk)::value, decltype(dv)::value, true>, grid, dim3(decltype(dv)::value * 4), st, a);
+            return launch_kernel(la_ends_walk_kernel<decltype(t), decltype(dk)::value, decltype(dv)::value, true>, ends_grid, dim3(decltype(dv)::value * 4), st, f);
         });
-        if (rc == HY_OK) rc = scan_ends(a, s, true, st);
+        if (rc == HY_OK) rc = scan_ends(f, s, true, st);
         if (rc != HY_OK) return rc;
     }
     rc = by_tile(s, [&](auto t, auto dk, auto dv) {
