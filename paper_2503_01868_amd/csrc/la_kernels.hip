@@ -396,11 +396,11 @@ struct State {
     }
     __device__ __forceinline__ void decay(float factor) {
         factor = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(factor)));
-        if (factor == 0.0f) return clear();
 #pragma unroll
         for (int i = 0; i < DT; ++i)
 #pragma unroll
             for (int j = 0; j < CT; ++j) s[i][j] *= factor;
+        if (factor == 0.0f) clear();  // (of infinities, too)
     }
     __device__ __forceinline__ void decay_step(float half) {
 #pragma unroll
@@ -679,6 +679,8 @@ __global__ __launch_bounds__(DV * 4, T::kBytes == 2 && DV == 128 ? 4 : 2) void l
                 for (int e = 0; e < 8; ++e) f[e] = S.s[2 * y + e / 4][j][e % 4];
                 fs[y][j] = frag_of(f, T{});
             }
+        char* const y_rows = a.y + ((at.b * a.L + t) * a.H + at.h) * a.dv_ * T::kBytes;
+        const uint32_t v_row = (uint32_t)a.H * (uint32_t)a.dv_ * T::kBytes;
         __syncthreads();  // A is there
 #pragma unroll 1
         for (int it = 0; it < IT; ++it) {
@@ -706,7 +708,7 @@ __global__ __launch_bounds__(DV * 4, T::kBytes == 2 && DV == 128 ? 4 : 2) void l
                 for (int j = 0; j < CT; ++j) multiply(o[j], fv[j][kb], fa);
             }
             if (i < n) {
-                char* const to = a.y + ((at.b * a.L + t + i) * a.H + at.h) * a.dv_ * T::kBytes;
+                char* const to = y_rows + (uint64_t)(uint32_t)i * v_row;
                 const int c = c0 + cw + (CT == 2 ? 8 : 4) * lq;
                 float f[4 * CT];
 #pragma unroll
@@ -838,13 +840,14 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
     const int64_t heads_qk = a.H / a.group, rows_all = items / a.tiles / a.H * a.L;  // B L
     const int64_t share = SHARES ? ((int64_t)(at.h % a.group) * a.tiles + at.tile) * (rows_all * heads_qk * a.dk_) : 0;
 
-    // `count` numbers of a row of dq or dk from d on
-    auto give = [&](void* base, int64_t t, int d, const float* v, auto count) {
+    // `count` numbers of a row of dq or dk from d on: row i of those from step t on
+    using O = std::conditional_t<SHARES, F32, T>;
+    const uint32_t k_row = (uint32_t)heads_qk * (uint32_t)a.dk_ * O::kBytes, v_row = (uint32_t)a.H * (uint32_t)a.dv_ * T::kBytes;
+    auto give = [&](void* base, int64_t t, int i, int d, const float* v, auto count) {
         constexpr int N = decltype(count)::value;
         if (d >= a.dk_) return;
-        const int64_t e = share + ((at.b * a.L + t) * heads_qk + at.hk) * a.dk_ + d;
-        using O = std::conditional_t<SHARES, F32, T>;
-        char* p = static_cast<char*>(base) + e * O::kBytes;
+        char* p = static_cast<char*>(base) + (share + ((at.b * a.L + t) * heads_qk + at.hk) * a.dk_) * O::kBytes;
+        p += (uint64_t)(uint32_t)i * k_row + (uint32_t)d * O::kBytes;
         if (N > 1 && a.dk_ % 4 == 0) {
             float f[N];
 #pragma unroll
@@ -859,9 +862,9 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
                 }
         }
     };
-    auto give_four = [&](void* base, int64_t t, int d, const f32x4_t& v) {
+    auto give_four = [&](void* base, int64_t t, int i, int d, const f32x4_t& v) {
         const float f[4] = {v[0], v[1], v[2], v[3]};
-        give(base, t, d, f, std::integral_constant<int, 4>{});
+        give(base, t, i, d, f, std::integral_constant<int, 4>{});
     };
     auto give_decay = [&](int64_t t, float x) {
         const float one[1] = {x};
@@ -987,8 +990,8 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
                 if (d < DK) {
                     float fq[1] = {0.0f}, fk[1] = {0.0f};
                     for (int y = 0; y < NW; ++y) fq[0] += sum_q[y * DK + d], fk[0] += sum_k[y * DK + d];
-                    give(a.dq, u, d, fq, std::integral_constant<int, 1>{});
-                    give(a.dk, u, d, fk, std::integral_constant<int, 1>{});
+                    give(a.dq, u, 0, d, fq, std::integral_constant<int, 1>{});
+                    give(a.dk, u, 0, d, fk, std::integral_constant<int, 1>{});
                 }
                 if (threadIdx.x == 0) {
                     float f = 0.0f;
@@ -1065,7 +1068,7 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
             const int j = 16 * jt + li, c = c0 + cw + 4 * lq;
             if (j < n && c < a.dv_) {
                 const float f[4] = {dv[jt][0], dv[jt][1], dv[jt][2], dv[jt][3]};
-                char* p = dv_row(t + j) + c * T::kBytes;
+                char* p = dv_row(t) + (uint64_t)(uint32_t)j * v_row + (uint32_t)c * T::kBytes;
                 if (a.dv_ % 4 == 0) {
                     Pack<T, 4>::store(p, Pack<T, 4>::pack(f));
                 } else {
@@ -1104,7 +1107,7 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
                 for (int kb = 0; kb < KB; ++kb)
                     if (kb <= it / 2) multiply(o, fk[kb], row_frag<PA>(s.e, i, 32 * kb, lq));
                 near[y][z] = dot(four<T>(s.q + i * PK + 16 * dt + 4 * lq), o);
-                if (i < n) give_four(a.dq, t + i, 16 * dt + 4 * lq, o);
+                if (i < n) give_four(a.dq, t, i, 16 * dt + 4 * lq, o);
                 __builtin_amdgcn_sched_barrier(0);  // (blocks side by side need more registers than there are)
             }
         }
@@ -1141,7 +1144,7 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
                 const float far = over_quarters(dot(k4, o)), less = over_quarters(near[y][z] - dot(k4, o2));
                 if (lq == 0) s.far[dt][j] = far, s.near[dt][j] = less;
                 o += o2;
-                if (j < n) give_four(a.dk, t + j, 16 * dt + 4 * lq, o);
+                if (j < n) give_four(a.dk, t, j, 16 * dt + 4 * lq, o);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
