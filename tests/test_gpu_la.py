@@ -163,6 +163,69 @@ def test_what_is_not_finite_stays_in_its_document_and_behind_its_step(dtype, bad
             close(dv_[:, at + 1:], ref[2][:, at + 1:], size[2][:, at + 1:], dtype, name + " dv behind")
 
 
+def within_range(q, k, v, g, dy, state, dstate, scale, dtype):
+    """``check`` of whatever fp32 can hold: three factors of 2^50 are 2^150, so where the sum of the terms' magnitudes is 2^127 or more
+    the sum may pass through an infinity on its way, whatever it is in the end."""
+    group = v.shape[2] // q.shape[2]
+    w = [wide(x) for x in (q, k, v, g)]
+    a = [abs(x) for x in w[:3]] + w[3:]
+    ref = block_ref.la(*w, group, scale, wide(state)) + block_ref.la_grads(wide(dy), *w, group, scale, wide(state), wide(dstate))
+    size = (block_ref.la(*a, group, scale, abs(wide(state)))
+            + block_ref.la_grads(abs(wide(dy)), *a, group, scale, abs(wide(state)), abs(wide(dstate))))
+    y, s, marks = hy.hyena_la_fwd_carry(q, k, v, g, scale, state_in=state, want_marks=True)
+    for given in (marks, None):
+        got = (y, s) + hy.hyena_la_bwd(dy, q, k, v, g, scale, marks=given, state_in=state, dstate_out=dstate, want_dstate=True)
+        for name, x, r, z in zip(("y", "state", "dq", "dk", "dv", "dg", "dstate"), got, ref, size):
+            held = z < 2.0 ** 127
+            assert held.mean() > 0.9, name
+            extra = 2e-5 * z[held].max() if name == "dg" else 0.0
+            close(x, np.where(held, r, np.nan), np.where(held, z, 0.0), "f32" if name in ("state", "dstate") else dtype, name, extra=extra)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,L,H,group,dk,dv", [(1, 200, 2, 2, 128, 200), (2, 130, 3, 1, 100, 64), (1, 70, 2, 1, 64, 128), (1, 65, 1, 1, 20, 33)])
+def test_chunks_that_are_taken_a_step_at_a_time(B, L, H, group, dk, dv, dtype):
+    """Numbers of 2^50 in one step: products of them are taken by the formulas, not at once, in every width, with shared heads and
+    several tiles of columns, beside chunks that are; a scale that is not below one."""
+    q, k, v, g, dy, state, dstate = make(12, B, L, H, group, dk, dv, dtype, resets=0.02)
+    t = 40
+    for x in (q, k, v, dy):
+        x[:, t] *= 2.0 ** 50
+    g[:, t + 1] = -float("inf")
+    within_range(q, k, v, g, dy, state, dstate, 0.5, dtype)
+    q, k, v, g, dy, state, dstate = make(13, B, L, H, group, dk, dv, dtype)
+    check(q, k, v, g, dy, state, dstate, 37.0, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_states_that_are_not_finite_end_at_a_reset(dtype):
+    """An infinity in the state in front, and in the gradient of the state behind: what lies across a reset does not know of them."""
+    B, L, H, dk, dv = 1, 200, 2, 40, 72
+    q, k, v, g, dy, state, dstate = make(14, B, L, H, 1, dk, dv, dtype)
+    first, second = 21, 150
+    g[:, [first, second]] = -float("inf")
+    w = [wide(x) for x in (q, k, v, g)]
+    a = [abs(x) for x in w[:3]] + w[3:]
+    ry, rs = block_ref.la(*w, 1, 0.3, wide(state))
+    ay, as_ = block_ref.la(*a, 1, 0.3, abs(wide(state)))
+    ref = block_ref.la_grads(wide(dy), *w, 1, 0.3, wide(state), wide(dstate))
+    size = block_ref.la_grads(abs(wide(dy)), *a, 1, 0.3, abs(wide(state)), abs(wide(dstate)))
+    bad_in, bad_out = state.clone(), dstate.clone()
+    bad_in[:, :, 3, 5] = float("inf")
+    bad_out[:, :, 7, 11] = float("inf")
+    y, s, marks = hy.hyena_la_fwd_carry(q, k, v, g, 0.3, state_in=bad_in, want_marks=True)
+    touched = np.zeros(ry.shape, dtype=bool)
+    touched[:, :first, :, 5] = True
+    close(y, np.where(touched, np.nan, ry), ay, dtype, "y")
+    close(s, rs, as_, "f32", "state")
+    assert not torch.isfinite(y[:, 0, :, 5]).any()
+    dq, dk_, dv_, dg, ds = hy.hyena_la_bwd(dy, q, k, v, g, 0.3, marks=marks, dstate_out=bad_out, want_dstate=True)
+    for what, got, r, z, lo, hi in (("dq", dq, ref[0], size[0], first, L), ("dk", dk_, ref[1], size[1], 0, second), ("dv", dv_, ref[2], size[2], 0, second),
+                                    ("dg", dg, ref[3], size[3], first, second + 1)):
+        close(got[:, lo:hi], r[:, lo:hi], z[:, lo:hi], dtype, what, extra=2e-5 * z.max() if what == "dg" else 0.0)
+    close(ds, ref[4], size[4], "f32", "dstate")
+
+
 @pytest.mark.parametrize("dtype,group,dk,dv", [("bf16", 1, 128, 128), ("bf16", 2, 40, 72), ("f32", 3, 33, 20)])
 def test_stretches_and_single_tokens_continue_each_other(dtype, group, dk, dv):
     B, L, H = 2, 170, 2 * group
