@@ -359,16 +359,21 @@ struct State {
             for (int j = 0; j < CT; ++j) s[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     }
     // from / to [dk][dv] numbers of a head; c0: the wave's first column
+    // (all loads first: one that waits for a branch waits for memory, 32 times in a row)
     __device__ __forceinline__ void load(const float* p, int dk, int dv, int c0, int li, int lq) {
 #pragma unroll
         for (int i = 0; i < DT; ++i)
 #pragma unroll
             for (int j = 0; j < CT; ++j)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int d = 16 * i + 4 * lq + r, c = c0 + column(li, j);
-                    s[i][j][r] = d < dk && c < dv ? p[(int64_t)d * dv + c] : 0.0f;
-                }
+                for (int r = 0; r < 4; ++r) s[i][j][r] = p[(int64_t)min(16 * i + 4 * lq + r, dk - 1) * dv + min(c0 + column(li, j), dv - 1)];
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int j = 0; j < CT; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (16 * i + 4 * lq + r >= dk || c0 + column(li, j) >= dv) s[i][j][r] = 0.0f;
     }
     __device__ __forceinline__ void store(float* p, int dk, int dv, int c0, int li, int lq) const {
 #pragma unroll
@@ -1237,7 +1242,7 @@ int64_t tiles_of(const LaShape& s) { return (s.dv + tile_columns(s) - 1) / tile_
 int64_t items_of(const LaShape& s) { return s.B * s.H * tiles_of(s); }
 int64_t state_size(const LaShape& s) { return (int64_t)tile_rows(s) * tile_columns(s); }
 
-// Segments of a sequence, so that `want` workgroups are there, of 4 chunks at the least.
+// Segments of a sequence, so that `want` workgroups are there, of 4 chunks at the least (2: the same time where heads are few).
 struct Cut {
     int64_t segments, each;
 };
