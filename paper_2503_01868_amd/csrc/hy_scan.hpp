@@ -42,4 +42,10 @@ __device__ __forceinline__ X of_lane(X x, int l) {
     }
 }
 
+// The same number, but what is computed from it is computed where it is used and not kept in registers from before a loop.
+__device__ __forceinline__ int fresh(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 }  // namespace hy

@@ -213,12 +213,6 @@ __device__ __forceinline__ bool make_decays(Decays<C>& s, float g, int lane) {
     return fine;
 }
 
-// The same number, computed where it is used: what the steps taken one by one need is not kept in registers beside the other path's.
-__device__ __forceinline__ int fresh(int x) {
-    asm volatile("" : "+v"(x));
-    return x;
-}
-
 // C rows of a chunk on their way to a tile in LDS: loaded a chunk ahead.  What lies behind the n-th row and the d-th number is loaded from
 // elsewhere in them and becomes zeros in LDS, so that no load waits for a branch (16000 cycles of a chunk's 36000 before).
 template <typename T, int C, int D, int NT>

@@ -120,6 +120,7 @@ __device__ __forceinline__ X block_upto(Lds<NT>& s, X x, X& total, int& turn) {
         if (j == w) before = total;
         total += at[j];
     }
+    total = of_lane(total, 0);
     return before + upto;
 }
 template <int NT>
@@ -132,7 +133,7 @@ __device__ __forceinline__ uint32_t block_max(Lds<NT>& s, uint32_t x, int& turn)
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < NT / kWave; ++j) x = max(x, at[j]);
-    return x;
+    return of_lane(x, 0);
 }
 
 // A row's words, wave by wave and piece by piece.  Pieces begin where 16 bytes do: the first has `pad` places in front of the row.
@@ -263,9 +264,9 @@ __device__ __forceinline__ Border find_border(Lds<NT>& s, X* bins, const uint32_
         }
         __syncthreads();
         find_bin<NT>(s, bins, need, turn);
-        const int bin = s.bin;
-        need -= s.above;
-        const bool all = s.inside == need;
+        const int bin = of_lane(s.bin, 0);
+        need -= of_lane(s.above, 0);
+        const bool all = of_lane(s.inside, 0) == need;
 #pragma unroll
         for (int e = 0; e < E; ++e)
             if (key[e] >= lo && key[e] <= hi && bin_of(key[e]) == bin) {
@@ -273,7 +274,7 @@ __device__ __forceinline__ Border find_border(Lds<NT>& s, X* bins, const uint32_
                 atomicMax(&s.high, key[e]);
             }
         __syncthreads();
-        lo = s.low, hi = s.high;
+        lo = of_lane(s.low, 0), hi = of_lane(s.high, 0);
         if (all || lo == hi || --most == 0) return Border{lo, need, all};
         even = false;
         __syncthreads();  // (the next round's beginning)
@@ -384,13 +385,15 @@ __global__ __launch_bounds__(NT, NT == 512 ? 4 : 1) void sample_kernel(SampleArg
 
         double T_n = a.p.temperature ? (double)a.p.temperature[n] : a.all.temperature;
         double top_p = a.p.top_p ? (double)a.p.top_p[n] : a.all.top_p, min_p = a.p.min_p ? (double)a.p.min_p[n] : a.all.min_p;
-        const int32_t top_k = a.p.top_k ? a.p.top_k[n] : a.all.top_k;
         double u = a.p.u[n];
         if (T_n != T_n) T_n = 1.0;
         if (top_p != top_p) top_p = 1.0;
         if (min_p != min_p) min_p = 0.0;
         if (!(u > 0.0)) u = 0.0;
-        const Settings set{1.0 / T_n, top_p, min_p, u, top_k};
+        // (the same for all lanes: in scalar registers)
+        T_n = of_lane(T_n, 0), top_p = of_lane(top_p, 0), min_p = of_lane(min_p, 0), u = of_lane(u, 0);
+        const int32_t top_k = of_lane(a.p.top_k ? a.p.top_k[n] : a.all.top_k, 0);
+        const Settings set{of_lane(1.0 / T_n, 0), top_p, min_p, u, top_k};
         __syncthreads();  // (the row before)
 
         uint32_t key[kEach], top = 0, from = none, listed = 0;  // the list's words, its least key and the largest, how many
@@ -547,6 +550,7 @@ __global__ __launch_bounds__(NT, NT == 512 ? 4 : 1) void sample_kernel(SampleArg
                 top = block_max<NT>(s, most, turn);
             }
         }
+        from = of_lane(from, 0), top = of_lane(top, 0), listed = of_lane(listed, 0);
         if (listed > 0) {
             choose_listed<NT, kBits>(a, s, n, key, word, from, top, (int32_t)listed, set, turn);
             continue;
