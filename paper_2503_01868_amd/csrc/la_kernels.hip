@@ -126,19 +126,19 @@ __device__ __forceinline__ Frag<F32> turned_row_frag(const float* t, int row, in
     r.x[0] = a.x, r.x[1] = a.y, r.x[2] = a.z, r.x[3] = a.w, r.x[4] = b.x, r.x[5] = b.y, r.x[6] = b.z, r.x[7] = b.w;
     return r;
 }
-// Columns of a tile as rows of an operand: lane li has column `c0` + li (STEP 4), or c0 + 8 (li / 4) + li % 4 (STEP 8), k = rows from
+// Columns of a tile as rows of an operand: lane li has column `c0` + li, k = rows from
 // k0 in the plain order.  bf16: LDS turns 4 x 16 numbers at a time; lane l of 16 says where row l / 4 has its columns 4 (l % 4) and
 // gets column l.
-template <int PITCH, int STEP>
+template <int PITCH>
 __device__ __forceinline__ Frag<BF16> column_frag(const uint16_t* t, int k0, int c0, int li, int lq) {
-    const uint16_t* p = t + (k0 + 8 * lq + li / 4) * PITCH + c0 + STEP * (li % 4);
+    const uint16_t* p = t + (k0 + 8 * lq + li / 4) * PITCH + c0 + 4 * (li % 4);
     const s16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_quad_t)p), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_quad_t)(p + 4 * PITCH));
     const uint2 ua = __builtin_bit_cast(uint2, a), ub = __builtin_bit_cast(uint2, b);
     return Frag<BF16>{__builtin_bit_cast(bf16x8_t, make_uint4(ua.x, ua.y, ub.x, ub.y))};
 }
-template <int PITCH, int STEP>
+template <int PITCH>
 __device__ __forceinline__ Frag<F32> column_frag(const float* t, int k0, int c0, int li, int lq) {
-    const float* p = t + (k0 + 8 * lq) * PITCH + c0 + STEP * (li / 4) + li % 4;
+    const float* p = t + (k0 + 8 * lq) * PITCH + c0 + li;
     Frag<F32> r;
 #pragma unroll
     for (int e = 0; e < 8; ++e) r.x[e] = p[e * PITCH];
@@ -338,98 +338,76 @@ __device__ __forceinline__ Place place_of(const LaArgs& a, uint32_t i) {
     return p;
 }
 
-// The state of a wave: DK rows by 16 CT columns, in 16 x 16 pieces, as results of (rows of k) x (columns of v): lane (li, lq)
-// has column li of piece ct, rows 16 dt + 4 lq + r.  CT = 2: the columns of two pieces are taken in turn, 4 and 4, so that a lane has 8 next
-// to each other in what is made of them.
-template <int DT, int CT>
+// The state of a wave: DK rows by 16 columns, in 16 x 16 pieces, as results of (rows of k) x (columns of v): lane (li, lq) has column li,
+// rows 16 i + 4 lq + r of piece i.
+template <int DT>
 struct State {
-    f32x4_t s[DT][CT];
-    static __device__ __forceinline__ int column(int li, int ct) { return CT == 2 ? 8 * (li / 4) + 4 * ct + li % 4 : 16 * ct + li; }
+    f32x4_t s[DT];
 
     __device__ __forceinline__ void clear() {
 #pragma unroll
-        for (int i = 0; i < DT; ++i)
-#pragma unroll
-            for (int j = 0; j < CT; ++j) s[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int i = 0; i < DT; ++i) s[i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    // from / to [dk][dv] numbers of a head; c0: the wave's first column
-    // (all loads first: one that waits for a branch waits for memory, 32 times in a row)
-    __device__ __forceinline__ void load(const float* p, int dk, int dv, int c0, int li, int lq) {
+    // from / to [dk][dv] numbers of a head; c: the lane's column (all loads first: one that waits for a branch waits for memory, 32 times
+    // in a row)
+    __device__ __forceinline__ void load(const float* p, int dk, int dv, int c, int lq) {
 #pragma unroll
         for (int i = 0; i < DT; ++i)
 #pragma unroll
-            for (int j = 0; j < CT; ++j)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) s[i][j][r] = p[(int64_t)min(16 * i + 4 * lq + r, dk - 1) * dv + min(c0 + column(li, j), dv - 1)];
+            for (int r = 0; r < 4; ++r) s[i][r] = p[(int64_t)min(16 * i + 4 * lq + r, dk - 1) * dv + min(c, dv - 1)];
 #pragma unroll
         for (int i = 0; i < DT; ++i)
 #pragma unroll
-            for (int j = 0; j < CT; ++j)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (16 * i + 4 * lq + r >= dk || c0 + column(li, j) >= dv) s[i][j][r] = 0.0f;
+            for (int r = 0; r < 4; ++r)
+                if (16 * i + 4 * lq + r >= dk || c >= dv) s[i][r] = 0.0f;
     }
-    __device__ __forceinline__ void store(float* p, int dk, int dv, int c0, int li, int lq) const {
+    __device__ __forceinline__ void store(float* p, int dk, int dv, int c, int lq) const {
 #pragma unroll
         for (int i = 0; i < DT; ++i)
 #pragma unroll
-            for (int j = 0; j < CT; ++j)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int d = 16 * i + 4 * lq + r, c = c0 + column(li, j);
-                    if (d < dk && c < dv) p[(int64_t)d * dv + c] = s[i][j][r];
-                }
+            for (int r = 0; r < 4; ++r) {
+                const int d = 16 * i + 4 * lq + r;
+                if (d < dk && c < dv) p[(int64_t)d * dv + c] = s[i][r];
+            }
     }
     // the library's own order: pieces, then lanes
     __device__ __forceinline__ void load_own(const float* p, int lane) {
 #pragma unroll
-        for (int i = 0; i < DT; ++i)
-#pragma unroll
-            for (int j = 0; j < CT; ++j) s[i][j] = *reinterpret_cast<const f32x4_t*>(p + ((i * CT + j) * kWave + lane) * 4);
+        for (int i = 0; i < DT; ++i) s[i] = *reinterpret_cast<const f32x4_t*>(p + (i * kWave + lane) * 4);
     }
     __device__ __forceinline__ void store_own(float* p, int lane) const {
 #pragma unroll
-        for (int i = 0; i < DT; ++i)
-#pragma unroll
-            for (int j = 0; j < CT; ++j) *reinterpret_cast<f32x4_t*>(p + ((i * CT + j) * kWave + lane) * 4) = s[i][j];
+        for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4_t*>(p + (i * kWave + lane) * 4) = s[i];
     }
     __device__ __forceinline__ void decay(float factor) {
         factor = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(factor)));
 #pragma unroll
-        for (int i = 0; i < DT; ++i)
-#pragma unroll
-            for (int j = 0; j < CT; ++j) s[i][j] *= factor;
+        for (int i = 0; i < DT; ++i) s[i] *= factor;
         if (factor == 0.0f) clear();  // (of infinities, too)
     }
     __device__ __forceinline__ void decay_step(float half) {
 #pragma unroll
         for (int i = 0; i < DT; ++i)
 #pragma unroll
-            for (int j = 0; j < CT; ++j)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) s[i][j][r] = scaled(s[i][j][r], half);
+            for (int r = 0; r < 4; ++r) s[i][r] = scaled(s[i][r], half);
     }
     // One step by itself: s = r r s + a[d] b[c] of `dk` by `dv` numbers.
     template <typename T>
-    __device__ __forceinline__ void step(float half, const char* a, const char* b, float scale, int dk, int dv, int c0, int li, int lq) {
+    __device__ __forceinline__ void step(float half, const char* a, const char* b, float scale, int dk, int dv, int c, int lq) {
+        const float bc = c < dv ? number<T>(b + (int64_t)c * T::kBytes) * scale : 0.0f;
 #pragma unroll
-        for (int j = 0; j < CT; ++j) {
-            const int c = c0 + column(li, j);
-            const float bc = c < dv ? number<T>(b + (int64_t)c * T::kBytes) * scale : 0.0f;
+        for (int i = 0; i < DT; ++i) {
+            const int d0 = 16 * i + fresh(4 * lq);
 #pragma unroll
-            for (int i = 0; i < DT; ++i) {
-                const int d0 = 16 * i + fresh(4 * lq);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int d = d0 + r;
-                    if (d < dk && c < dv) s[i][j][r] = fmaf(number<T>(a + (int64_t)d * T::kBytes), bc, scaled(s[i][j][r], half));
-                }
+            for (int r = 0; r < 4; ++r) {
+                const int d = d0 + r;
+                if (d < dk && c < dv) s[i][r] = fmaf(number<T>(a + (int64_t)d * T::kBytes), bc, scaled(s[i][r], half));
             }
         }
     }
-    // sum over d of a[d] s[d][c], of column c0 + column(li, j), in every lane that has it
+    // sum over d of a[d] s[d][c], in every lane that has the column
     template <typename T>
-    __device__ __forceinline__ float product(const char* a, int j, int dk, int lq) const {
+    __device__ __forceinline__ float product(const char* a, int dk, int lq) const {
         float y = 0.0f;
 #pragma unroll
         for (int i = 0; i < DT; ++i) {
@@ -437,7 +415,7 @@ struct State {
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int d = d0 + r;
-                if (d < dk) y = fmaf(number<T>(a + (int64_t)d * T::kBytes), s[i][j][r], y);
+                if (d < dk) y = fmaf(number<T>(a + (int64_t)d * T::kBytes), s[i][r], y);
             }
         }
         y += __shfl_xor(y, 16, kWave);
@@ -460,41 +438,25 @@ __device__ __forceinline__ f32x4_t load_mark(const char* p) {
 
 // s += first^T (x) weighted second over the chunk's rows: rows of `a` become the state's rows, columns of `b` its columns, of which
 // the wave has `mine` in `fb`; `factor` are the rows' factors.
-template <typename T, int DK, int C, int DT, int CT, int KB>
-__device__ __forceinline__ void add_rows(State<DT, CT>& s, const Elem<T>* a, const Frag<T> (&fb)[CT][KB], const float* factor, float scale, int li, int lq) {
+template <typename T, int DK, int DT, int KB>
+__device__ __forceinline__ void add_rows(State<DT>& s, const Elem<T>* a, const Frag<T> (&fb)[KB], const float* factor, float scale, int li, int lq) {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-        Frag<T> parts[CT][kParts<T>];
-        float by[8];
+        Frag<T> parts[kParts<T>];
+        float f[8];
+        floats_of(fb[kb], f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) by[e] = factor[32 * kb + 8 * lq + e] * scale;
+        for (int e = 0; e < 8; ++e) f[e] *= factor[32 * kb + 8 * lq + e] * scale;
+        wide_frag(f, parts);
 #pragma unroll
-        for (int j = 0; j < CT; ++j) {
-            float f[8];
-            floats_of(fb[j][kb], f);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] *= by[e];
-            wide_frag(f, parts[j]);
-        }
-#pragma unroll
-        for (int i = 0; i < DT; ++i) {
-            const Frag<T> fa = column_frag<kPitch<T, DK>, 4>(a, 32 * kb, 16 * i, li, lq);
-#pragma unroll
-            for (int j = 0; j < CT; ++j) multiply_wide(s.s[i][j], fa, parts[j]);
-        }
+        for (int i = 0; i < DT; ++i) multiply_wide(s.s[i], column_frag<kPitch<T, DK>>(a, 32 * kb, 16 * i, li, lq), parts);
     }
 }
-
-// Columns of a tile that a wave has, 32 rows at a time.
-template <typename T, int PITCH, int CT, int KB>
-__device__ __forceinline__ void own_columns(Frag<T> (&f)[CT][KB], const Elem<T>* tile, int c0, int li, int lq) {
+// The columns of a tile that a wave has, 32 rows at a time.
+template <typename T, int PITCH, int KB>
+__device__ __forceinline__ void own_columns(Frag<T> (&f)[KB], const Elem<T>* tile, int c0, int li, int lq) {
 #pragma unroll
-    for (int j = 0; j < CT; ++j)
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-            if constexpr (CT == 2) f[j][kb] = column_frag<PITCH, 8>(tile, 32 * kb, c0 + 4 * j, li, lq);
-            else f[j][kb] = column_frag<PITCH, 4>(tile, 32 * kb, c0 + 16 * j, li, lq);
-        }
+    for (int kb = 0; kb < KB; ++kb) f[kb] = column_frag<PITCH>(tile, 32 * kb, c0, li, lq);
 }
 __device__ __forceinline__ double with_sum(double sum, double more) {
     return sum == -INFINITY || more == -INFINITY ? -INFINITY : sum + more;  // (nothing undoes a reset, NaN neither)
@@ -506,7 +468,7 @@ __device__ __forceinline__ double step_sum(float g) { return g < kForgets ? -INF
 
 template <typename T, int DK, int DV, bool BACK>
 __global__ __launch_bounds__(DV * 4, T::kBytes == 2 && DV == 128 ? 4 : 2) void la_ends_walk_kernel(LaArgs a) {
-    constexpr int C = kChunk<T>, NT = DV * 4, KB = C / 32, DT = DK / 16, CT = 1, WC = 16 * CT;
+    constexpr int C = kChunk<T>, NT = DV * 4, KB = C / 32, DT = DK / 16;
     constexpr int PV = kPitch<T, DV>;
     __shared__ __attribute__((aligned(16))) Elem<T> tile_a[C * kPitch<T, DK>];
     __shared__ __attribute__((aligned(16))) Elem<T> tile_b[C * PV];
@@ -517,12 +479,12 @@ __global__ __launch_bounds__(DV * 4, T::kBytes == 2 && DV == 128 ? 4 : 2) void l
     const Rows &ra = BACK ? a.q : a.k, &rb = BACK ? a.dy : a.v;
     const char *ap = ra.p + at.b * ra.batch + at.hk * ra.head, *bp = rb.p + at.b * rb.batch + at.h * rb.head;
     const char* gp = a.g.p + at.b * a.g.batch + (int64_t)at.h * T::kBytes;
-    const int c0 = at.tile * DV, cw = w * WC;  // the tile's columns, the wave's in it
+    const int c0 = at.tile * DV, cw = w * 16;  // the tile's columns, the wave's in it
     const int64_t head_state = (at.b * a.H + at.h) * a.dk_ * a.dv_, items = uniform((int32_t)(gridDim.x / (uint32_t)a.segments));
     const float scale = BACK ? a.scale : 1.0f;
-    State<DT, CT> S;
-    if (!BACK && at.segment == 0 && a.state_in) S.load(a.state_in + head_state, a.dk_, a.dv_, c0 + cw, li, lq);
-    else if (BACK && at.segment == a.segments - 1 && a.dstate_out) S.load(a.dstate_out + head_state, a.dk_, a.dv_, c0 + cw, li, lq);
+    State<DT> S;
+    if (!BACK && at.segment == 0 && a.state_in) S.load(a.state_in + head_state, a.dk_, a.dv_, c0 + cw + li, lq);
+    else if (BACK && at.segment == a.segments - 1 && a.dstate_out) S.load(a.dstate_out + head_state, a.dk_, a.dv_, c0 + cw + li, lq);
     else S.clear();
     const int64_t first = at.segment * a.each, last = first + a.each < a.chunks ? first + a.each : a.chunks;
     double sum = 0.0;
@@ -548,10 +510,10 @@ __global__ __launch_bounds__(DV * 4, T::kBytes == 2 && DV == 128 ? 4 : 2) void l
         if (y + 1 < last) load(BACK ? x - 1 : x + 1);
         if (at_once) {
             const int part = fresh(lane), li = part % 16, lq = part / 16;
-            Frag<T> fb[CT][KB];
+            Frag<T> fb[KB];
             own_columns<T, PV>(fb, tile_b, cw, li, lq);
             S.decay(decays.whole);
-            add_rows<T, DK, C>(S, tile_a, fb, BACK ? decays.from_start : decays.to_end, scale, li, lq);
+            add_rows<T, DK>(S, tile_a, fb, BACK ? decays.from_start : decays.to_end, scale, li, lq);
             sum = with_sum(sum, decays.sum);
         } else {
             for (int i = 0, n = steps(x); i < n; ++i) {
@@ -559,13 +521,13 @@ __global__ __launch_bounds__(DV * 4, T::kBytes == 2 && DV == 128 ? 4 : 2) void l
                 const int64_t t = x * C + (BACK ? n - 1 - i : i);
                 const float g = number<T>(gp + t * a.g.step), half = step_factor(g);
                 // (what goes back has its step's decay behind it, of what the step adds too)
-                S.template step<T>(BACK ? 1.0f : half, ap + t * ra.step, bp + t * rb.step, scale, a.dk_, a.dv_, c0 + cw, li, lq);
+                S.template step<T>(BACK ? 1.0f : half, ap + t * ra.step, bp + t * rb.step, scale, a.dk_, a.dv_, c0 + cw + li, lq);
                 if constexpr (BACK) S.decay_step(half);
                 sum = with_sum(sum, step_sum(g));
             }
         }
     }
-    S.store_own(a.ends + (at.segment * items + at.item) * (DK * DV) + w * (DK * WC), lane);
+    S.store_own(a.ends + (at.segment * items + at.item) * (DK * DV) + w * (DK * 16), lane);
     if (threadIdx.x == 0) a.sums[at.segment * items + at.item] = sum;
 }
 
@@ -580,18 +542,18 @@ struct WalkLds {
 
 template <typename T, int DK, int DV, bool MARKS>
 __global__ __launch_bounds__(DV * 4, T::kBytes == 2 && DV == 128 ? 4 : 2) void la_walk_kernel(LaArgs a) {
-    constexpr int C = kChunk<T>, NW = DV / 16, NT = NW * kWave, IT = C / 16, KB = C / 32, DT = DK / 16, CT = 1, WC = 16 * CT;
+    constexpr int C = kChunk<T>, NW = DV / 16, NT = NW * kWave, IT = C / 16, KB = C / 32, DT = DK / 16;
     constexpr int PK = kPitch<T, DK>, PV = kPitch<T, DV>, PA = kPitch<T, C>;
     __shared__ __attribute__((aligned(16))) WalkLds<T, DK, DV> s;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, li = lane % 16, lq = lane / 16;
     const Place at = place_of(a, blockIdx.x);
     const char *kp = a.k.p + at.b * a.k.batch + at.hk * a.k.head, *vp = a.v.p + at.b * a.v.batch + at.h * a.v.head;
     const char *qp = a.q.p + at.b * a.q.batch + at.hk * a.q.head, *gp = a.g.p + at.b * a.g.batch + (int64_t)at.h * T::kBytes;
-    const int c0 = at.tile * DV, cw = w * WC;  // the tile's columns, the wave's in it
+    const int c0 = at.tile * DV, cw = w * 16;  // the tile's columns, the wave's in it
     const int64_t head_state = (at.b * a.H + at.h) * a.dk_ * a.dv_, items = uniform((int32_t)(gridDim.x / (uint32_t)a.segments));
-    State<DT, CT> S;
-    if (at.segment > 0) S.load_own(a.ends + ((at.segment - 1) * items + at.item) * (DK * DV) + w * (DK * WC), lane);
-    else if (a.state_in) S.load(a.state_in + head_state, a.dk_, a.dv_, c0 + cw, li, lq);
+    State<DT> S;
+    if (at.segment > 0) S.load_own(a.ends + ((at.segment - 1) * items + at.item) * (DK * DV) + w * (DK * 16), lane);
+    else if (a.state_in) S.load(a.state_in + head_state, a.dk_, a.dv_, c0 + cw + li, lq);
     else S.clear();
     for (int i = threadIdx.x; i < C * PA; i += NT) s.a[i] = 0;  // (blocks above the diagonal are read, as zeros)
     const int64_t first = at.segment * a.each, last = first + a.each < a.chunks ? first + a.each : a.chunks;
@@ -610,12 +572,10 @@ __global__ __launch_bounds__(DV * 4, T::kBytes == 2 && DV == 128 ? 4 : 2) void l
     load(first);
     for (int64_t x = first; x < last; ++x) {
         if constexpr (MARKS) {
-            char* const m = a.marks + ((at.item * a.chunks + x) * (DK * DV) + w * (DK * WC)) * T::kBytes;
+            char* const m = a.marks + ((at.item * a.chunks + x) * (DK * DV) + w * (DK * 16)) * T::kBytes;
             const int part = fresh(lane);
 #pragma unroll
-            for (int i = 0; i < DT; ++i)
-#pragma unroll
-                for (int j = 0; j < CT; ++j) store_mark<T>(m + ((i * CT + j) * kWave + part) * 4 * T::kBytes, S.s[i][j]);
+            for (int i = 0; i < DT; ++i) store_mark<T>(m + (i * kWave + part) * 4 * T::kBytes, S.s[i]);
         }
         const int64_t t = x * C;
         const int n = steps(x);
@@ -630,13 +590,10 @@ __global__ __launch_bounds__(DV * 4, T::kBytes == 2 && DV == 128 ? 4 : 2) void l
             for (int i = 0; i < n; ++i) {
                 const int part = fresh(lane), li = part % 16, lq = part / 16;
                 const int64_t u = t + i;
-                S.template step<T>(step_factor(number<T>(gp + u * a.g.step)), kp + u * a.k.step, vp + u * a.v.step, 1.0f, a.dk_, a.dv_, c0 + cw, li, lq);
-#pragma unroll
-                for (int j = 0; j < CT; ++j) {
-                    const int c = c0 + cw + State<DT, CT>::column(li, j);
-                    const float one[1] = {S.template product<T>(qp + u * a.q.step, j, a.dk_, lq) * a.scale};
-                    if (lq == 0 && c < a.dv_) Pack<T, 1>::store(a.y + (((at.b * a.L + u) * a.H + at.h) * a.dv_ + c) * T::kBytes, Pack<T, 1>::pack(one));
-                }
+                S.template step<T>(step_factor(number<T>(gp + u * a.g.step)), kp + u * a.k.step, vp + u * a.v.step, 1.0f, a.dk_, a.dv_, c0 + cw + li, lq);
+                const int c = c0 + cw + li;
+                const float one[1] = {S.template product<T>(qp + u * a.q.step, a.dk_, lq) * a.scale};
+                if (lq == 0 && c < a.dv_) Pack<T, 1>::store(a.y + (((at.b * a.L + u) * a.H + at.h) * a.dv_ + c) * T::kBytes, Pack<T, 1>::pack(one));
             }
             continue;
         }
@@ -663,21 +620,19 @@ __global__ __launch_bounds__(DV * 4, T::kBytes == 2 && DV == 128 ? 4 : 2) void l
             }
             put4(s.a + i * PA + j0, p);
         }
-        Frag<T> fv[CT][KB];
+        Frag<T> fv[KB];
         {
             const int part = fresh(lane), li = part % 16, lq = part / 16;
             own_columns<T, PV>(fv, s.v, cw, li, lq);
         }
-        Frag<T> fs[DK / 32][CT];  // the state as an operand
+        Frag<T> fs[DK / 32];  // the state as an operand
 #pragma unroll
-        for (int y = 0; y < DK / 32; ++y)
+        for (int y = 0; y < DK / 32; ++y) {
+            float f[8];
 #pragma unroll
-            for (int j = 0; j < CT; ++j) {
-                float f[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] = S.s[2 * y + e / 4][j][e % 4];
-                fs[y][j] = frag_of(f, T{});
-            }
+            for (int e = 0; e < 8; ++e) f[e] = S.s[2 * y + e / 4][e % 4];
+            fs[y] = frag_of(f, T{});
+        }
         char* const y_rows = a.y + ((at.b * a.L + t) * a.H + at.h) * a.dv_ * T::kBytes;
         const uint32_t v_row = (uint32_t)a.H * (uint32_t)a.dv_ * T::kBytes;
         __syncthreads();  // A is there
@@ -685,49 +640,29 @@ __global__ __launch_bounds__(DV * 4, T::kBytes == 2 && DV == 128 ? 4 : 2) void l
         for (int it = 0; it < IT; ++it) {
             const int part = fresh(lane), li = part % 16, lq = part / 16;
             const int i = 16 * it + li;
-            f32x4_t o[CT];
+            f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int j = 0; j < CT; ++j) o[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int y = 0; y < DK / 32; ++y) {
-                const Frag<T> fq = turned_row_frag<PK>(s.q, i, 32 * y, lq);
-#pragma unroll
-                for (int j = 0; j < CT; ++j) multiply(o[j], fs[y][j], fq);
-            }
+            for (int y = 0; y < DK / 32; ++y) multiply(o, fs[y], turned_row_frag<PK>(s.q, i, 32 * y, lq));
             const float factor = s.d.from_start[i] * a.scale;
 #pragma unroll
-            for (int j = 0; j < CT; ++j)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) o[j][r] = weighted(o[j][r], factor);
+            for (int r = 0; r < 4; ++r) o[r] = weighted(o[r], factor);
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
                 if (kb > it / 2) break;
-                const Frag<T> fa = row_frag<PA>(s.a, i, 32 * kb, lq);
-#pragma unroll
-                for (int j = 0; j < CT; ++j) multiply(o[j], fv[j][kb], fa);
+                multiply(o, fv[kb], row_frag<PA>(s.a, i, 32 * kb, lq));
             }
-            if (i < n) {
-                char* const to = y_rows + (uint64_t)(uint32_t)i * v_row;
-                const int c = c0 + cw + (CT == 2 ? 8 : 4) * lq;
-                float f[4 * CT];
-#pragma unroll
-                for (int e = 0; e < 4 * CT; ++e) f[e] = o[e / 4][e % 4];
-                if (a.dv_ % 8 == 0) {
-                    if (c < a.dv_)
-#pragma unroll
-                        for (int e = 0; e < 4 * CT; e += 16 / T::kBytes < 4 * CT ? 16 / T::kBytes : 4 * CT) {
-                            constexpr int kN = 16 / T::kBytes < 4 * CT ? 16 / T::kBytes : 4 * CT;
-                            float part[kN];
-#pragma unroll
-                            for (int z = 0; z < kN; ++z) part[z] = f[e + z];
-                            Pack<T, kN>::store(to + (c + e) * T::kBytes, Pack<T, kN>::pack(part));
-                        }
+            const int c = c0 + cw + 4 * lq;
+            if (i < n && c < a.dv_) {
+                char* const to = y_rows + (uint64_t)(uint32_t)i * v_row + (uint32_t)c * T::kBytes;
+                const float f[4] = {o[0], o[1], o[2], o[3]};
+                if (a.dv_ % 4 == 0) {
+                    Pack<T, 4>::store(to, Pack<T, 4>::pack(f));
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 4 * CT; ++e)
-                        if (c + e < a.dv_) {
-                            const float one[1] = {f[e]};
-                            Pack<T, 1>::store(to + (c + e) * T::kBytes, Pack<T, 1>::pack(one));
+                    for (int r = 0; r < 4; ++r)
+                        if (c + r < a.dv_) {
+                            const float one[1] = {f[r]};
+                            Pack<T, 1>::store(to + r * T::kBytes, Pack<T, 1>::pack(one));
                         }
                 }
             }
@@ -735,10 +670,10 @@ __global__ __launch_bounds__(DV * 4, T::kBytes == 2 && DV == 128 ? 4 : 2) void l
         S.decay(s.d.whole);
         {
             const int part = fresh(lane), li = part % 16, lq = part / 16;
-            add_rows<T, DK, C>(S, s.k, fv, s.d.to_end, 1.0f, li, lq);
+            add_rows<T, DK>(S, s.k, fv, s.d.to_end, 1.0f, li, lq);
         }
     }
-    if (at.segment == a.segments - 1 && a.state_out) S.store(a.state_out + head_state, a.dk_, a.dv_, c0 + cw, li, lq);
+    if (at.segment == a.segments - 1 && a.state_out) S.store(a.state_out + head_state, a.dk_, a.dv_, c0 + cw + li, lq);
 }
 
 // Ends of segments made by themselves -> ends of everything up to them (BACK: from them on): e[s] += decay of s * e[s - 1].
@@ -824,13 +759,13 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
     const int64_t items = uniform((int32_t)(gridDim.x / (uint32_t)a.segments)), head_state = (at.b * a.H + at.h) * a.dk_ * a.dv_;
     const int own = w * (DK * 16) + lane * 4;  // this lane's numbers in states of the library's own order, piece by piece
     constexpr int kStep = kWave * 4;
-    State<DT, 1> M;  // the gradient of the state behind the chunk
+    State<DT> M;  // the gradient of the state behind the chunk
     if (at.segment < a.segments - 1) {
         const float* p = a.ends + ((int64_t)(at.segment + 1) * a.finer * items + at.item) * (DK * DV) + own;
 #pragma unroll
-        for (int i = 0; i < DT; ++i) M.s[i][0] = *reinterpret_cast<const f32x4_t*>(p + i * kStep);
+        for (int i = 0; i < DT; ++i) M.s[i] = *reinterpret_cast<const f32x4_t*>(p + i * kStep);
     } else if (a.dstate_out) {
-        M.load(a.dstate_out + head_state, a.dk_, a.dv_, c0 + cw, li, lq);
+        M.load(a.dstate_out + head_state, a.dk_, a.dv_, c0 + cw + li, lq);
     } else {
         M.clear();
     }
@@ -926,7 +861,7 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
 #pragma unroll
             for (int i = 0; i < DT; ++i) {
                 store_words<Pack<T, 4>::kWords>(p + 16 * i, next_s[i]);
-                if constexpr (Lds::kTwo) put4(s.m + (cw + li) * PK + 16 * i + 4 * lq, M.s[i][0]);
+                if constexpr (Lds::kTwo) put4(s.m + (cw + li) * PK + 16 * i + 4 * lq, M.s[i]);
             }
         }
         g_now = lane < n ? unpacked<T>(next_g) : 0.0f;
@@ -941,7 +876,7 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
                     float f[4];
                     Pack<T, 4>::unpack(next_s[i], f);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) both = fmaf(f[r] * whole, M.s[i][0][r], both);
+                    for (int r = 0; r < 4; ++r) both = fmaf(f[r] * whole, M.s[i][r], both);
                 }
             both = wave_upto(both);
             if (lane == kWave - 1) s.both[w] = both;
@@ -954,21 +889,21 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
             for (int i = n - 1; i >= 0; --i) {
                 const int part = fresh(lane), li = part % 16, lq = part / 16, c = c0 + cw + li;
                 const int64_t u = t + i;
-                State<DT, 1> S;
+                State<DT> S;
 #pragma unroll
-                for (int y = 0; y < DT; ++y) S.s[y][0] = load_mark<T>(mark + y * kStep * T::kBytes);
+                for (int y = 0; y < DT; ++y) S.s[y] = load_mark<T>(mark + y * kStep * T::kBytes);
                 for (int64_t z = t; z < u; ++z)
-                    S.template step<T>(step_factor(number<T>(gp + z * a.g.step)), kp + z * a.k.step, vp + z * a.v.step, 1.0f, a.dk_, a.dv_, c0 + cw, li, lq);
+                    S.template step<T>(step_factor(number<T>(gp + z * a.g.step)), kp + z * a.k.step, vp + z * a.v.step, 1.0f, a.dk_, a.dv_, c0 + cw + li, lq);
                 const float half = step_factor(number<T>(gp + u * a.g.step));
-                M.template step<T>(1.0f, qp + u * a.q.step, dyp + u * a.dy.step, a.scale, a.dk_, a.dv_, c0 + cw, li, lq);
+                M.template step<T>(1.0f, qp + u * a.q.step, dyp + u * a.dy.step, a.scale, a.dk_, a.dv_, c0 + cw + li, lq);
                 float both = 0.0f;
                 if (half != 0.0f)
 #pragma unroll
                     for (int y = 0; y < DT; ++y)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) both = fmaf(scaled(S.s[y][0][r], half), M.s[y][0][r], both);
-                S.template step<T>(half, kp + u * a.k.step, vp + u * a.v.step, 1.0f, a.dk_, a.dv_, c0 + cw, li, lq);
-                const float dv[1] = {M.template product<T>(kp + u * a.k.step, 0, a.dk_, lq)};
+                        for (int r = 0; r < 4; ++r) both = fmaf(scaled(S.s[y][r], half), M.s[y][r], both);
+                S.template step<T>(half, kp + u * a.k.step, vp + u * a.v.step, 1.0f, a.dk_, a.dv_, c0 + cw + li, lq);
+                const float dv[1] = {M.template product<T>(kp + u * a.k.step, a.dk_, lq)};
                 const float dyc = c < a.dv_ ? number<T>(dyp + u * a.dy.step + (int64_t)c * T::kBytes) * a.scale : 0.0f;
                 const float vc = c < a.dv_ ? number<T>(vp + u * a.v.step + (int64_t)c * T::kBytes) : 0.0f;
                 if (lq == 0 && c < a.dv_) Pack<T, 1>::store(dv_row(u) + c * T::kBytes, Pack<T, 1>::pack(dv));
@@ -980,7 +915,7 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
                     const int d0 = 16 * y + fresh(4 * lq);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {  // (columns behind the last add nothing)
-                        const float fq = over_columns(c < a.dv_ ? S.s[y][0][r] * dyc : 0.0f), fk = over_columns(c < a.dv_ ? M.s[y][0][r] * vc : 0.0f);
+                        const float fq = over_columns(c < a.dv_ ? S.s[y][r] * dyc : 0.0f), fk = over_columns(c < a.dv_ ? M.s[y][r] * vc : 0.0f);
                         if (li == 15) sum_q[w * DK + d0 + r] = fq, sum_k[w * DK + d0 + r] = fk;
                     }
                 }
@@ -1040,7 +975,7 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
             for (int y = 0; y < DK / 32; ++y) {
                 float f[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] = M.s[2 * y + e / 4][0][e % 4];
+                for (int e = 0; e < 8; ++e) f[e] = M.s[2 * y + e / 4][e % 4];
                 fm[y] = frag_of(f, T{});
             }
 #pragma unroll
@@ -1054,7 +989,7 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
             }
         }
         __syncthreads();  // A and E are there
-        Frag<T> fdy[1][KB];
+        Frag<T> fdy[KB];
         {
             const int part = fresh(lane), li = part % 16, lq = part / 16;
             own_columns<T, PV>(fdy, s.dy, cw, li, lq);
@@ -1063,7 +998,7 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
         for (int jt = 0; jt < IT; ++jt) {
             const int part = fresh(lane), li = part % 16, lq = part / 16;
 #pragma unroll
-            for (int kb = jt / 2; kb < KB; ++kb) multiply(dv[jt], fdy[0][kb], column_frag<PA, 4>(s.a, 32 * kb, 16 * jt, li, lq));
+            for (int kb = jt / 2; kb < KB; ++kb) multiply(dv[jt], fdy[kb], column_frag<PA>(s.a, 32 * kb, 16 * jt, li, lq));
             const int j = 16 * jt + li, c = c0 + cw + 4 * lq;
             if (j < n && c < a.dv_) {
                 const float f[4] = {dv[jt][0], dv[jt][1], dv[jt][2], dv[jt][3]};
@@ -1089,9 +1024,9 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
             const int dt = y * kBand + w % kBand;
             Frag<T> fs[VB], fk[KB];
 #pragma unroll
-            for (int kb = 0; kb < VB; ++kb) fs[kb] = column_frag<PK, 4>(s.s, 32 * kb, 16 * dt, li, lq);
+            for (int kb = 0; kb < VB; ++kb) fs[kb] = column_frag<PK>(s.s, 32 * kb, 16 * dt, li, lq);
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) fk[kb] = column_frag<PK, 4>(s.k, 32 * kb, 16 * dt, li, lq);
+            for (int kb = 0; kb < KB; ++kb) fk[kb] = column_frag<PK>(s.k, 32 * kb, 16 * dt, li, lq);
 #pragma unroll
             for (int z = 0; z < kRows; ++z) {
                 const int it = z * (NW / kBand) + w / kBand, i = 16 * it + li;
@@ -1113,7 +1048,7 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
         if constexpr (!Lds::kTwo) {
             __syncthreads();  // S has been read
 #pragma unroll
-            for (int i = 0; i < DT; ++i) put4(s.s + (cw + li) * PK + 16 * i + 4 * lq, M.s[i][0]);
+            for (int i = 0; i < DT; ++i) put4(s.s + (cw + li) * PK + 16 * i + 4 * lq, M.s[i]);
             __syncthreads();
         }
         const Elem<T>* const sm_t = Lds::kTwo ? s.m : s.s;
@@ -1123,9 +1058,9 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
             const int dt = y * kBand + w % kBand;
             Frag<T> fm[VB], fq[KB];
 #pragma unroll
-            for (int kb = 0; kb < VB; ++kb) fm[kb] = column_frag<PK, 4>(sm_t, 32 * kb, 16 * dt, li, lq);
+            for (int kb = 0; kb < VB; ++kb) fm[kb] = column_frag<PK>(sm_t, 32 * kb, 16 * dt, li, lq);
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) fq[kb] = column_frag<PK, 4>(s.q, 32 * kb, 16 * dt, li, lq);
+            for (int kb = 0; kb < KB; ++kb) fq[kb] = column_frag<PK>(s.q, 32 * kb, 16 * dt, li, lq);
 #pragma unroll
             for (int z = 0; z < kRows; ++z) {
                 const int jt = z * (NW / kBand) + w / kBand, j = 16 * jt + li;
@@ -1135,7 +1070,7 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
                 for (int kb = 0; kb < VB; ++kb) multiply(o, fm[kb], row_frag<PV>(s.v, j, 32 * kb, lq));
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb)
-                    if (kb >= jt / 2) multiply(o2, fq[kb], column_frag<PA, 4>(s.e, 32 * kb, 16 * jt, li, lq));
+                    if (kb >= jt / 2) multiply(o2, fq[kb], column_frag<PA>(s.e, 32 * kb, 16 * jt, li, lq));
                 const float factor = s.d.to_end[j];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) o[r] = weighted(o[r], factor);
@@ -1150,12 +1085,12 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
         M.decay(s.d.whole);
         {
             const int part = fresh(lane), li = part % 16, lq = part / 16;
-            add_rows<T, DK, C>(M, s.q, fdy, s.d.from_start, a.scale, li, lq);
+            add_rows<T, DK>(M, s.q, fdy, s.d.from_start, a.scale, li, lq);
         }
     }
     __syncthreads();
     give_decays();
-    if (at.segment == 0 && a.dstate_in) M.store(a.dstate_in + head_state, a.dk_, a.dv_, c0 + cw, li, lq);
+    if (at.segment == 0 && a.dstate_in) M.store(a.dstate_in + head_state, a.dk_, a.dv_, c0 + cw + li, lq);
 }
 
 // out[r][d] = sum over the shares: heads that share a row of q and k, and tiles of their columns; [share][rows].
@@ -1296,8 +1231,8 @@ hy_status scan_ends(const LaArgs& a, const LaShape& s, bool back, hipStream_t st
                 : launch_kernel(la_ends_kernel<false>, grid, dim3(256), st, a.ends, static_cast<const double*>(a.sums), items, (int32_t)state_size(s), a.segments);
 }
 
-// The forward walk: outputs, or with `out` false the marks alone.
-hy_status walk(LaArgs a, const LaShape& s, const Cut& c, void* ws, bool out, hipStream_t st) {
+// The forward walk.
+hy_status walk(LaArgs a, const LaShape& s, const Cut& c, void* ws, hipStream_t st) {
     const int64_t items = items_of(s);
     a.segments = (int32_t)c.segments, a.each = c.each;
     a.ends = static_cast<float*>(ws), a.sums = reinterpret_cast<double*>(static_cast<float*>(ws) + c.segments * items * state_size(s));
@@ -1312,7 +1247,6 @@ hy_status walk(LaArgs a, const LaShape& s, const Cut& c, void* ws, bool out, hip
     return by_tile(s, [&](auto t, auto dk, auto dv) {
         using T = decltype(t);
         constexpr int DK = decltype(dk)::value, DV = decltype(dv)::value;
-        (void)out;
         return a.marks ? launch_kernel(la_walk_kernel<T, DK, DV, true>, grid, dim3(DV * 4), st, a)
                        : launch_kernel(la_walk_kernel<T, DK, DV, false>, grid, dim3(DV * 4), st, a);
     });
@@ -1372,7 +1306,7 @@ hy_status launch_la_fwd(const LaPtrs& p, const LaShape& s, void* ws, hipStream_t
     }
     LaArgs a = args_of(p, s);
     a.marks = static_cast<char*>(p.marks);
-    return walk(a, s, cut(s, kForwardGroups), ws, true, st);
+    return walk(a, s, cut(s, kForwardGroups), ws, st);
 }
 
 hy_status launch_la_bwd(const LaPtrs& p, const LaShape& s, void* ws, hipStream_t st) {
@@ -1389,7 +1323,7 @@ hy_status launch_la_bwd(const LaPtrs& p, const LaShape& s, void* ws, hipStream_t
     if (!a.marks_in) {
         LaArgs f = a;
         f.marks = marks, f.y = y, f.state_out = nullptr;
-        const hy_status rc = walk(f, s, b.walk_cut, base, false, st);
+        const hy_status rc = walk(f, s, b.walk_cut, base, st);
         if (rc != HY_OK) return rc;
         a.marks_in = marks;
     }
