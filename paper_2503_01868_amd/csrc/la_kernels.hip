@@ -7,10 +7,16 @@
 // quotient of exponentials, so nothing overflows that the states do not.  A decay of zero ends a document: factors across it are
 // zeros by selection, not by multiplication, whatever is on its other side.
 //
-// A workgroup walks chunks in their order with the state in registers (the backward pass in the other order with the state's
-// gradient).  Where heads are too few to fill the card, a sequence is cut into segments: a walk that makes states only, a
+// A workgroup walks chunks in their order with the state in registers, 16 columns a wave (the backward pass in the other order with the
+// state's gradient).  Where heads are too few to fill the card, a sequence is cut into segments: a walk that makes states only, a
 // scan over the segments' ends, and the walk itself.  The state's products take the factor of k or q as three bf16 parts, so that states
 // are sums of fp32 products in bf16 calls too; what is rounded to bf16 is A and the copies of S that are multiplied.
+//
+// Measured (MI355X, 8192 steps x 32 heads of 128 x 128, bf16): ends 43 us, scan 12, walk 88 (112 with marks), gradients' ends 43, backward
+// walk 220.  The bytes of the walk are 268 MB, 48 us; what bounds it is issue: vector instructions 55% busy, LDS 50%, matrix cores 24%, of
+// waves that do the same phase between barriers.  On the way: loads ahead of a chunk that waited for branches or for spilled
+// addresses cost half of a chunk's time (162 -> 90 us), places in vector registers spilled (backward 406 -> 228).  Tried without gain:
+// 4 waves of 32 columns, rows 32 bytes further apart in LDS (more conflicts), two blocks of 16 rows at once, 2 chunks a segment.
 //
 // A product mixes rows, and a zero times an infinity is none: a chunk that holds anything not finite, or so large that a product on the
 // way could become so, or decays far above one, is taken a row at a time, by the formulas as they stand.
@@ -744,6 +750,11 @@ __device__ __forceinline__ f32x4_t four(const Elem<T>* p) {
 }
 __device__ __forceinline__ float dot(const f32x4_t& a, const f32x4_t& b) { return fmaf(a[0], b[0], fmaf(a[1], b[1], fmaf(a[2], b[2], a[3] * b[3]))); }
 
+// For every chunk, from what lies in LDS and M in registers: A and E below the diagonal; dv = to_end k M + A^T dy;
+// dq = from_start scale dy S^T + E k; dk = to_end v M^T + E^T q; and M itself.  dg needs no products of its own: the pairs of steps on both
+// sides of a decay are what q . dq and k . dk add up to on both sides of it.  160 KB of LDS leave room for one workgroup of 8 waves on a
+// compute unit: vector instructions 41% busy, LDS 38%, matrix cores 14%.  dq and dk of heads that share q and k go to shares in fp32 and are
+// summed afterwards in a fixed order (32768 steps, 16 heads of 64 x 128 by four: 25 us each).
 template <typename T, int DK, int DV, bool SHARES>
 __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
     using Lds = BwdLds<T, DK, DV>;
@@ -1112,7 +1123,8 @@ __global__ __launch_bounds__(256) void la_copy_kernel(const float* from, float* 
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) to[i] = from ? from[i] : 0.0f;
 }
 
-// ---- one token: the state, read and written, is what it costs.  A workgroup has 4 CL columns of a head's state (VEC = 1: CL), a
+// ---- one token: the state, read and written, is what it costs (64 x 32 heads of 128 x 128: 268 MB in 41-52 us, by what the caches still
+// hold of it).  A workgroup has 4 CL columns of a head's state (VEC = 1: CL), a
 // lane VEC of them in every (256 / CL)-th row.
 struct StepArgs {
     const char *q, *k, *v, *g;
