@@ -1123,9 +1123,8 @@ __global__ __launch_bounds__(256) void la_copy_kernel(const float* from, float* 
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) to[i] = from ? from[i] : 0.0f;
 }
 
-// ---- one token: the state, read and written, is what it costs (64 x 32 heads of 128 x 128: 268 MB in 41-52 us, by what the caches still
-// hold of it).  A workgroup has 4 CL columns of a head's state (VEC = 1: CL), a
-// lane VEC of them in every (256 / CL)-th row.
+// ---- one token: the state, read and written, is what it costs (64 x 32 heads of 128 x 128: 268 MB in 50 us).  A workgroup has 4 CL columns
+// of a head's state (VEC = 1: CL), a lane VEC of them in every (256 / CL)-th row.
 struct StepArgs {
     const char *q, *k, *v, *g;
     char* y;
@@ -1133,7 +1132,7 @@ struct StepArgs {
     int32_t H, group, dk, dv, slices;
     float scale;
 };
-template <typename T, int CL, int VEC>
+template <typename T, int CL, int VEC, bool STREAM>
 __global__ __launch_bounds__(256) void la_step_kernel(StepArgs a) {
     constexpr int kRows = 256 / CL;
     __shared__ float sum[kRows][CL * VEC];
@@ -1150,7 +1149,7 @@ __global__ __launch_bounds__(256) void la_step_kernel(StepArgs a) {
 #pragma unroll 8
         for (int d = row; d < a.dk; d += kRows) {
             float s[VEC];
-            Pack<F32, VEC>::unpack(Pack<F32, VEC>::load(p + (int64_t)d * a.dv), s);
+            Pack<F32, VEC>::unpack(STREAM ? Pack<F32, VEC>::load_nt(p + (int64_t)d * a.dv) : Pack<F32, VEC>::load(p + (int64_t)d * a.dv), s);
             const float k = number<T>(a.k + (qk + d) * T::kBytes), q = number<T>(a.q + (qk + d) * T::kBytes);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
@@ -1388,15 +1387,20 @@ hy_status launch_la_step(const LaPtrs& p, const LaShape& s, hipStream_t st) {
     const bool fours = s.dv % 4 == 0;
     const int64_t heads = s.B * s.H;
     // 128 columns of a head a workgroup, 32 where that leaves compute units idle
-    auto run = [&](auto t, auto cl, auto vec) {
+    auto run = [&](auto t, auto cl, auto vec, auto stream) {
         constexpr int CL = decltype(cl)::value, VEC = decltype(vec)::value;
         a.slices = (int32_t)((s.dv + CL * VEC - 1) / (CL * VEC));
-        return launch_kernel(la_step_kernel<decltype(t), CL, VEC>, dim3((uint32_t)(heads * a.slices)), dim3(256), st, a);
+        return launch_kernel(la_step_kernel<decltype(t), CL, VEC, decltype(stream)::value>, dim3((uint32_t)(heads * a.slices)), dim3(256), st, a);
     };
     auto by = [&](auto t) {
         using std::integral_constant;
-        if (!fours) return run(t, integral_constant<int, 32>{}, integral_constant<int, 1>{});
-        return heads < 512 ? run(t, integral_constant<int, 8>{}, integral_constant<int, 4>{}) : run(t, integral_constant<int, 32>{}, integral_constant<int, 4>{});
+        if (!fours) return run(t, integral_constant<int, 32>{}, integral_constant<int, 1>{}, std::false_type{});
+        if (heads < 512) return run(t, integral_constant<int, 8>{}, integral_constant<int, 4>{}, std::false_type{});
+        // States that the other layers' push out of the memory-side cache (256 MiB) between two tokens are read as a stream: 64 x 32 of
+        // 128 x 128 (128 MiB) with another such state between two tokens 50 us instead of 55, with none 51 instead of 41.
+        const bool large = heads * s.dk * s.dv * 4 >= INT64_C(1) << 26;
+        return large ? run(t, integral_constant<int, 32>{}, integral_constant<int, 4>{}, std::true_type{})
+                     : run(t, integral_constant<int, 32>{}, integral_constant<int, 4>{}, std::false_type{});
     };
     return s.dtype == HY_F32 ? by(F32{}) : by(BF16{});
 }
