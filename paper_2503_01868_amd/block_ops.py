@@ -256,7 +256,7 @@ def hyena_rmsnorm_fwd(x, w=None, residual=None, eps: float = 1e-6, total=None, w
     unless ``want_rstd``; ``hyena_rmsnorm_bwd`` takes it and the sum.  x and the residual may be views whose rows are the same
     distance apart; see ``hyena_rmsnorm_fwd`` in hyena.h."""
     if total is None and out is None and stream is None:
-        made = binding._fast.norm_fwd(x, w, residual, eps, want_rstd)
+        made = binding._fast.norm_fwd(x, w, residual, eps, want_rstd, False)
         if made is not None:
             return made
     y, _, total, rstd = _norm_fwd(x, w, residual, eps, total, want_rstd, out, False, stream, "hyena_rmsnorm_fwd")
@@ -266,6 +266,10 @@ def hyena_rmsnorm_fwd(x, w=None, residual=None, eps: float = 1e-6, total=None, w
 def hyena_rmsnorm_fwd_8bit(x, w=None, residual=None, eps: float = 1e-6, total=None, want_rstd: bool = False, stream=None):
     """(y, scale, total, rstd): ``hyena_rmsnorm_fwd`` with y as float8_e4m3fn numbers and a float32 scale for every row (value =
     number * scale, the row's largest at 448)."""
+    if total is None and stream is None:
+        made = binding._fast.norm_fwd(x, w, residual, eps, want_rstd, True)
+        if made is not None:
+            return made
     return _norm_fwd(x, w, residual, eps, total, want_rstd, None, True, stream, "hyena_rmsnorm_fwd")
 
 

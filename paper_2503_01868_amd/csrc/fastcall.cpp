@@ -297,23 +297,26 @@ const at::Tensor* rows(PyObject* o, int64_t& N, int64_t& D) {
     return x;
 }
 
-// (x, w, residual, eps, want_rstd) -> (y, total, rstd)
+// (x, w, residual, eps, want_rstd, eight) -> (y, total, rstd), or with 8 bits (y, scale, total, rstd)
 PyObject* norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     int64_t N, D;
     int code;
     void* stream;
-    const at::Tensor *x = n == 5 ? rows(a[0], N, D) : nullptr, *w, *r;
-    if (!x || !PyFloat_CheckExact(a[3]) || !PyBool_Check(a[4]) || !optional(a[1], *x, x->sizes().slice(x->dim() - 1), x->scalar_type(), w) ||
-        !optional(a[2], *x, x->sizes(), x->scalar_type(), r) || !here(*x, code, stream))
+    const at::Tensor *x = n == 6 ? rows(a[0], N, D) : nullptr, *w, *r;
+    if (!x || !PyFloat_CheckExact(a[3]) || !PyBool_Check(a[4]) || !PyBool_Check(a[5]) ||
+        !optional(a[1], *x, x->sizes().slice(x->dim() - 1), x->scalar_type(), w) || !optional(a[2], *x, x->sizes(), x->scalar_type(), r) ||
+        !here(*x, code, stream))
         Py_RETURN_NONE;
     const double eps = PyFloat_AS_DOUBLE(a[3]);
-    const at::Tensor y = at::empty_like(*x), total = r ? at::empty_like(*x) : at::Tensor(),
-                     rstd = a[4] == Py_True ? at::empty(x->sizes().slice(0, x->dim() - 1), x->options().dtype(at::kFloat)) : at::Tensor();
-    void *xp = x->data_ptr(), *rp = address(r), *wp = address(w), *yp = y.data_ptr(), *tp = address(total), *sp = address(rstd);
-    if (!launched([&] { return e.norm_fwd(xp, rp, wp, yp, nullptr, tp, static_cast<float*>(sp), N, D, D, r ? D : 0, eps, code, stream); }))
-        Py_RETURN_NONE;
-    return tuple_of({y, r ? total : *x, rstd});
+    const bool eight = a[5] == Py_True;
+    auto of_rows = [&](bool wanted) { return wanted ? at::empty(x->sizes().slice(0, x->dim() - 1), x->options().dtype(at::kFloat)) : at::Tensor(); };
+    const at::Tensor y = eight ? at::empty(x->sizes(), x->options().dtype(at::kFloat8_e4m3fn)) : at::empty_like(*x), scale = of_rows(eight),
+                     total = r ? at::empty_like(*x) : at::Tensor(), rstd = of_rows(a[4] == Py_True);
+    void *xp = x->data_ptr(), *rp = address(r), *wp = address(w), *yp = y.data_ptr(), *tp = address(total);
+    float *const cp = static_cast<float*>(address(scale)), *const sp = static_cast<float*>(address(rstd));
+    if (!launched([&] { return e.norm_fwd(xp, rp, wp, yp, cp, tp, sp, N, D, D, r ? D : 0, eps, code, stream); })) Py_RETURN_NONE;
+    return eight ? tuple_of({y, scale, r ? total : *x, rstd}) : tuple_of({y, r ? total : *x, rstd});
     END_HANDLE_TH_ERRORS
 }
 

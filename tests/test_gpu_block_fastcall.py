@@ -29,6 +29,8 @@ def calls(dtype):
         return hy.hyena_la_step(*args[:4], state, *args[4:]), state
 
     return [("norm", lambda: hy.hyena_rmsnorm_fwd(x, w, residual=r, want_rstd=True)), ("norm alone", lambda: hy.hyena_rmsnorm_fwd(x)),
+            ("norm in 8 bits", lambda: hy.hyena_rmsnorm_fwd_8bit(x, w, residual=r, want_rstd=True)),
+            ("norm alone in 8 bits", lambda: hy.hyena_rmsnorm_fwd_8bit(x)),
             ("norm bwd", lambda: hy.hyena_rmsnorm_bwd(dy, total, rstd, w, dtotal=r)), ("norm bwd alone", lambda: hy.hyena_rmsnorm_bwd(dy, total, rstd)),
             ("norm bwd without dw", lambda: hy.hyena_rmsnorm_bwd(dy, total, rstd, w, want_dw=False)), ("step", lambda: step(q, k, v, g, 0.3)),
             ("sample", lambda: hy.hyena_sample(z, u, t, top_k, p, m)), ("sample by numbers", lambda: hy.hyena_sample(z, u, 0.7, 20, 0.9, 0.01)),
@@ -55,6 +57,8 @@ def test_the_same_bits(dtype, monkeypatch):
         assert isinstance(fast, tuple) and len(fast) == len(slow)
         for x, y in zip(fast, slow):
             assert (x is None) == (y is None), name
+            if x is not None and x.dtype == torch.float8_e4m3fn:
+                x, y = x.view(torch.uint8), y.view(torch.uint8)
             assert x is None or (torch.equal(x, y) and x.dtype == y.dtype and not x.requires_grad), name
     x = normal(1, 4, 64, dtype=dtype)
     assert hy.hyena_rmsnorm_fwd(x)[1] is x
@@ -67,7 +71,7 @@ def test_what_is_not_plain_takes_the_other_path():
     for bad in ((x[:, ::2], None, None, 1e-6, False), (x, w.double(), None, 1e-6, False), (x, w[:32], None, 1e-6, False), (x, w, x[:4], 1e-6, False),
                 (x.cpu(), None, None, 1e-6, False), (x.half(), None, None, 1e-6, False), (None, None, None, 1e-6, False), (x, w, None, "1", False),
                 (x[:0], w, None, 1e-6, False)):
-        assert fast.norm_fwd(*bad) is None
+        assert fast.norm_fwd(*bad, False) is None and fast.norm_fwd(*bad, True) is None
     rstd = torch.ones(8, device="cuda:0")
     for bad in ((x, None, rstd, w, None, True), (x, x, None, w, None, True), (x, x, rstd[:4], w, None, True), (x, x, rstd, w[:3], None, True),
                 (x, x, rstd.bfloat16(), w, None, True), (x, x, rstd, w, x[:1], True), (x, x.bfloat16(), rstd, w, None, True)):
