@@ -508,8 +508,9 @@ hy_status hyena_adamw_step(const void *table, int64_t n_tensors, int64_t chunks,
  *     y[b,t,h] = scale * q[b,t,h'] S[b,t,h]
  * with S[b,-1,h] = state_in[b,h] (NULL: zero).  `group` heads of v and g share a head of q and k.  g is the logarithm of the
  * decay; below about -87, where exp(g) is zero, it forgets everything before its step, infinities and NaN included (the first
- * step of a document in a packed sequence; every gradient through it is zero).  g > 0 grows, and a product of decays and states
- * overflows where it passes fp32's range.
+ * step of a document in a packed sequence; every gradient through it is zero).  Nothing else forgets: decays that together leave
+ * nothing of a number multiply it, and an infinity or NaN in a state stays until such a step.  g > 0 grows, and a product of decays and
+ * states overflows where it passes fp32's range.
  * q, k: [B,L,H/group,dk], v, y: [B,L,H,dv], g: [B,L,H], of `dtype`; state_in, state_out: fp32 [B,H,dk,dv], the state after the
  * last step (NULL: not wanted; an empty sequence hands state_in on).
  * Steps are taken in chunks: inside one, products of q, k, v on the matrix cores, between them the states.  States, decays and
@@ -537,6 +538,8 @@ int64_t hyena_la_marks_bytes(int64_t B, int64_t L, int64_t H, int32_t group, int
  *     M[b,t,h] = scale q[b,t,h']^T dy[b,t,h] + a[b,t+1,h] M[b,t+1,h]      (+ dstate_out[b,h] at the last step):
  *     dq = scale dy S^T,  dk = v M^T  (each summed over the heads that share a row),  dv = k M,
  *     dg[b,t,h] = a[b,t,h] <S[b,t-1,h], M[b,t,h]>,   dstate_in[b,h] = a[b,0,h] M[b,0,h]   (NULL: not wanted)
+ * (dg is made of sums over a chunk's pairs of steps, of which those that do not reach over step t cancel: it is as exact as fp32 makes
+ * the largest of them, whatever it is itself)
  * dq, dk: dense [B,L,H/group,dk], dv: dense [B,L,H,dv], dg: dense [B,L,H], of `dtype`; fp32 inside, with bf16 calls' products
  * rounded as in the forward call; sums in a fixed order, one rounding per stored element.  marks: what the forward call wrote
  * for the same inputs, or NULL: the states are computed again, from state_in (which is not looked at otherwise).  strides: as

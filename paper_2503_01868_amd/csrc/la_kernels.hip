@@ -4,8 +4,10 @@
 //     y_i = scale exp(b_i) q_i S + sum_{j <= i} A_ij v_j,   A_ij = scale exp(b_i - b_j) (q_i . k_j),
 //     S'  = exp(b_C) S + sum_j exp(b_C - b_j) k_j^T v_j,
 // matrix products all of them.  Every factor is the exponential of a difference of sums (held as two floats, made in double), never a
-// quotient of exponentials, so nothing overflows that the states do not.  A decay of zero ends a document: factors across it are
-// zeros by selection, not by multiplication, whatever is on its other side.
+// quotient of exponentials, so nothing overflows that the states do not, and is multiplied in as its root, twice, so that of a large number
+// what is left stays.  A decay of zero ends a document: factors across it are zeros by selection, not by multiplication, whatever is
+// on its other side.  Nothing else forgets: a product of decays that leaves nothing of a number is not zero itself (its root is 2^-126 at the
+// least), and an infinity or NaN in a state stays.
 //
 // A workgroup walks chunks in their order with the state in registers, 16 columns a wave (the backward pass in the other order with the
 // state's gradient).  Where heads are too few to fill the card, a sequence is cut into segments: a walk that makes states only, a
@@ -19,7 +21,8 @@
 // 4 waves of 32 columns, rows 32 bytes further apart in LDS (more conflicts), two blocks of 16 rows at once, 2 chunks a segment.
 //
 // A product mixes rows, and a zero times an infinity is none: a chunk that holds anything not finite, or so large that a product on the
-// way could become so, or decays far above one, is taken a row at a time, by the formulas as they stand.
+// way could become so, or decays far above one, or that meets a state with such a number, is taken a row at a time, by the formulas as they
+// stand.  (NaN in a state need not be looked for: products keep it in its row and column.)
 #include <string.h>
 
 #include <cmath>
@@ -40,18 +43,18 @@ typedef __attribute__((address_space(3))) s16x4_t* lds_quad_t;
 constexpr float kForgets = -87.3f;  // exp of less is below the smallest normal number
 constexpr double kLog2E = 1.4426950408889634074;
 // Of a chunk that is taken at once: bits by which decays above one may grow a state, and what numbers (times a scale above one) stay
-// below, so that products of two numbers, a factor and a sum over 128 are finite: 24 + 2 * 46 + 7 < 127.
-constexpr float kMostGrowth = 24.0f, kMostNumber = 0x1p46f;
+// below, so that products of two numbers, a factor and a sum over 128 are finite: 24 + 2 * 46 + 7 < 127; and what the states' numbers
+// stay below, so that those of a state and the other's gradient are, and of one with a number of the chunk: 2 * 56 + 14 < 127.
+constexpr float kMostGrowth = 24.0f, kMostNumber = 0x1p46f, kMostState = 0x1p56f;
 
-// The factor of one step as exp2(d) = r r, r = exp2(d / 2): growth beyond the range of one factor is left to the products it is in.
+// A factor exp2(d) as its root r = exp2(d / 2), multiplied in twice: growth beyond the range of one factor is left to the products it is in,
+// and a root is zero for a reset alone (2^-252 of the largest number is below 2^-124).
 __device__ __forceinline__ float half_factor(float d) {
     const float x = 0.5f * d;
-    return __builtin_amdgcn_exp2f(x > 127.0f ? 127.0f : x);  // (of NaN: NaN)
+    return __builtin_amdgcn_exp2f(x > 127.0f ? 127.0f : x < -126.0f ? -126.0f : x);  // (of NaN: NaN)
 }
 __device__ __forceinline__ float step_factor(float g) { return g < kForgets ? 0.0f : half_factor((float)((double)g * kLog2E)); }
 __device__ __forceinline__ float scaled(float x, float half) { return half == 0.0f ? 0.0f : x * half * half; }
-// By the factor of several steps, which is a number, or zero: then nothing is left, whatever x is.
-__device__ __forceinline__ float weighted(float x, float factor) { return factor == 0.0f ? 0.0f : x * factor; }
 
 // Eight numbers of a row of an operand: k = 8 lq + e of a block of 32 (lane: li = lane % 16, lq = lane / 16), or in the order of
 // accumulators ("turned"), k = 16 (e / 4) + 4 lq + e % 4.  A product's result has in lane (li, lq), register r, row 4 lq + r of its
@@ -184,8 +187,8 @@ struct Rows {
     int32_t d, wide;            // wide: 8 numbers from a multiple of 8 on can be moved by 16 bytes, and rows of a chunk are near
 };
 
-// What a chunk's steps do to a state, in LDS: sums of log2 decays up to and with a step (two floats), the last step up to and with it
-// that forgets (-1: none), factors from the chunk's start to behind a step, from behind it to the end, and of the whole.
+// What a chunk's steps do to a state, in LDS: halves of the sums of log2 decays up to and with a step (two floats), the last step up to and with it
+// that forgets (-1: none), roots of the factors from the chunk's start to behind a step, from behind it to the end, and of the whole.
 template <int C>
 struct Decays {
     float hi[C], lo[C];
@@ -208,12 +211,12 @@ __device__ __forceinline__ bool make_decays(Decays<C>& s, float g, int lane) {
     const double end = of_lane(b, kWave - 1);
     const float hi = (float)b;
     if (inside) {
-        s.hi[lane] = hi, s.lo[lane] = (float)(b - (double)hi), s.forgot[lane] = forgot;
-        s.from_start[lane] = forgot < 0 ? __builtin_amdgcn_exp2f(hi) : 0.0f;
-        s.to_end[lane] = lane >= last ? __builtin_amdgcn_exp2f((float)(end - b)) : 0.0f;
+        s.hi[lane] = 0.5f * hi, s.lo[lane] = 0.5f * (float)(b - (double)hi), s.forgot[lane] = forgot;
+        s.from_start[lane] = forgot < 0 ? half_factor(hi) : 0.0f;
+        s.to_end[lane] = lane >= last ? half_factor((float)(end - b)) : 0.0f;
     }
     if (lane == 0) {
-        s.whole = last < 0 ? __builtin_amdgcn_exp2f((float)end) : 0.0f;
+        s.whole = last < 0 ? half_factor((float)end) : 0.0f;
         s.sum = last < 0 ? end : -INFINITY;
     }
     return fine;
@@ -344,6 +347,9 @@ __device__ __forceinline__ Place place_of(const LaArgs& a, uint32_t i) {
     return p;
 }
 
+// max(most, |a|, |b|), NaN left out.
+__device__ __forceinline__ float larger(float most, float a, float b) { return fmaxf(fmaxf(most, fabsf(a)), fabsf(b)); }
+
 // The state of a wave: DK rows by 16 columns, in 16 x 16 pieces, as results of (rows of k) x (columns of v): lane (li, lq) has column li,
 // rows 16 i + 4 lq + r of piece i.
 template <int DT>
@@ -385,11 +391,25 @@ struct State {
 #pragma unroll
         for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4_t*>(p + (i * kWave + lane) * 4) = s[i];
     }
-    __device__ __forceinline__ void decay(float factor) {
-        factor = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(factor)));
+    __device__ __forceinline__ void decay(float half) {
+        half = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(half)));
+        const float factor = half * half;
+        if (half > 0x1p-63f) {
 #pragma unroll
-        for (int i = 0; i < DT; ++i) s[i] *= factor;
-        if (factor == 0.0f) clear();  // (of infinities, too)
+            for (int i = 0; i < DT; ++i) s[i] *= factor;
+        } else if (half != 0.0f) {
+#pragma unroll
+            for (int i = 0; i < DT; ++i) s[i] = s[i] * half * half;
+        } else {
+            clear();  // (of infinities, too)
+        }
+    }
+    // The largest magnitude that is not NaN.
+    __device__ __forceinline__ float largest() const {
+        float most = 0.0f;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) most = larger(larger(most, s[i][0], s[i][1]), s[i][2], s[i][3]);
+        return most;
     }
     __device__ __forceinline__ void decay_step(float half) {
 #pragma unroll
@@ -443,16 +463,19 @@ __device__ __forceinline__ f32x4_t load_mark(const char* p) {
 }
 
 // s += first^T (x) weighted second over the chunk's rows: rows of `a` become the state's rows, columns of `b` its columns, of which
-// the wave has `mine` in `fb`; `factor` are the rows' factors.
+// the wave has `mine` in `fb`; `half` are the roots of the rows' factors.
 template <typename T, int DK, int DT, int KB>
-__device__ __forceinline__ void add_rows(State<DT>& s, const Elem<T>* a, const Frag<T> (&fb)[KB], const float* factor, float scale, int li, int lq) {
+__device__ __forceinline__ void add_rows(State<DT>& s, const Elem<T>* a, const Frag<T> (&fb)[KB], const float* half, float scale, int li, int lq) {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
         Frag<T> parts[kParts<T>];
         float f[8];
         floats_of(fb[kb], f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] *= factor[32 * kb + 8 * lq + e] * scale;
+        for (int e = 0; e < 8; ++e) {
+            const float h = half[32 * kb + 8 * lq + e];
+            f[e] = f[e] * (h * scale) * h;  // (numbers, all of them: nothing to select)
+        }
         wide_frag(f, parts);
 #pragma unroll
         for (int i = 0; i < DT; ++i) multiply_wide(s.s[i], column_frag<kPitch<T, DK>>(a, 32 * kb, 16 * i, li, lq), parts);
@@ -590,6 +613,7 @@ __global__ __launch_bounds__(DV * 4, T::kBytes == 2 && DV == 128 ? 4 : 2) void l
         fine &= next_q.put(s.q, a.most, a.q, qp + t * a.q.step, n, 0);
         fine &= next_v.put(s.v, a.most, a.v, vp + t * a.v.step, n, c0);
         if (w == 0) fine &= make_decays<C>(s.d, lane < n ? unpacked<T>(next_g) : 0.0f, lane);
+        fine &= S.largest() < kMostState;
         const bool at_once = !__syncthreads_or(!fine);
         if (x + 1 < last) load(x + 1);
         if (!at_once) {
@@ -621,8 +645,8 @@ __global__ __launch_bounds__(DV * 4, T::kBytes == 2 && DV == 128 ? 4 : 2) void l
             const float hi = s.d.hi[i], lo = s.d.lo[i];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const float f = __builtin_amdgcn_exp2f((hi - s.d.hi[j0 + r]) + (lo - s.d.lo[j0 + r]));
-                p[r] = j0 + r <= i && j0 + r >= forgot ? p[r] * (f * a.scale) : 0.0f;
+                const float half = __builtin_amdgcn_exp2f((hi - s.d.hi[j0 + r]) + (lo - s.d.lo[j0 + r]));
+                p[r] = j0 + r <= i && j0 + r >= forgot ? p[r] * (half * a.scale) * half : 0.0f;
             }
             put4(s.a + i * PA + j0, p);
         }
@@ -649,9 +673,9 @@ __global__ __launch_bounds__(DV * 4, T::kBytes == 2 && DV == 128 ? 4 : 2) void l
             f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int y = 0; y < DK / 32; ++y) multiply(o, fs[y], turned_row_frag<PK>(s.q, i, 32 * y, lq));
-            const float factor = s.d.from_start[i] * a.scale;
+            const float half = s.d.from_start[i], first = half * a.scale;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[r] = weighted(o[r], factor);
+            for (int r = 0; r < 4; ++r) o[r] = half == 0.0f ? 0.0f : o[r] * first * half;
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
                 if (kb > it / 2) break;
@@ -877,21 +901,19 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
         }
         g_now = lane < n ? unpacked<T>(next_g) : 0.0f;
         if (w == 0) fine &= make_decays<C>(s.d, g_now, lane);
-        const bool at_once = !__syncthreads_or(!fine);
-        {  // <S, M>
-            const float whole = s.d.whole;
-            float both = 0.0f;
-            if (whole != 0.0f)
+        float both = 0.0f, most = M.largest();  // <S, M>
 #pragma unroll
-                for (int i = 0; i < DT; ++i) {
-                    float f[4];
-                    Pack<T, 4>::unpack(next_s[i], f);
+        for (int i = 0; i < DT; ++i) {
+            float f[4];
+            Pack<T, 4>::unpack(next_s[i], f);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) both = fmaf(f[r] * whole, M.s[i][r], both);
-                }
-            both = wave_upto(both);
-            if (lane == kWave - 1) s.both[w] = both;
+            for (int r = 0; r < 4; ++r) both = fmaf(f[r], M.s[i][r], both);
+            most = larger(larger(most, f[0], f[1]), f[2], f[3]);
         }
+        fine &= most < kMostState;
+        both = wave_upto(both);
+        const bool at_once = !__syncthreads_or(!fine);
+        if (lane == kWave - 1) s.both[w] = scaled(both, s.d.whole);
         if (x > first) load(x - 1);
         done = -1;
         if (!at_once) {
@@ -970,9 +992,9 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const bool in = j0 + r <= i && j0 + r >= forgot;
-                const float f = __builtin_amdgcn_exp2f((hi - s.d.hi[j0 + r]) + (lo - s.d.lo[j0 + r])) * a.scale;
-                p[r] = in ? p[r] * f : 0.0f;
-                e[r] = in ? e[r] * f : 0.0f;
+                const float half = __builtin_amdgcn_exp2f((hi - s.d.hi[j0 + r]) + (lo - s.d.lo[j0 + r])), first = half * a.scale;
+                p[r] = in ? p[r] * first * half : 0.0f;
+                e[r] = in ? e[r] * first * half : 0.0f;
             }
             put4(s.a + i * PA + j0, p);
             put4(s.e + i * PA + j0, e);
@@ -994,9 +1016,9 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
                 dv[jt] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int y = 0; y < DK / 32; ++y) multiply(dv[jt], fm[y], turned_row_frag<PK>(s.k, 16 * jt + li, 32 * y, lq));
-                const float factor = s.d.to_end[16 * jt + li];
+                const float half = s.d.to_end[16 * jt + li];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) dv[jt][r] = weighted(dv[jt][r], factor);
+                for (int r = 0; r < 4; ++r) dv[jt][r] = scaled(dv[jt][r], half);
             }
         }
         __syncthreads();  // A and E are there
@@ -1045,9 +1067,9 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
                 f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int kb = 0; kb < VB; ++kb) multiply(o, fs[kb], row_frag<PV>(s.dy, i, 32 * kb, lq));
-                const float factor = s.d.from_start[i] * a.scale;
+                const float half = s.d.from_start[i], first = half * a.scale;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) o[r] = weighted(o[r], factor);
+                for (int r = 0; r < 4; ++r) o[r] = half == 0.0f ? 0.0f : o[r] * first * half;
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb)
                     if (kb <= it / 2) multiply(o, fk[kb], row_frag<PA>(s.e, i, 32 * kb, lq));
@@ -1082,9 +1104,9 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb)
                     if (kb >= jt / 2) multiply(o2, fq[kb], column_frag<PA>(s.e, 32 * kb, 16 * jt, li, lq));
-                const float factor = s.d.to_end[j];
+                const float half = s.d.to_end[j];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) o[r] = weighted(o[r], factor);
+                for (int r = 0; r < 4; ++r) o[r] = scaled(o[r], half);
                 const f32x4_t k4 = four<T>(s.k + j * PK + 16 * dt + 4 * lq);
                 const float far = over_quarters(dot(k4, o)), less = over_quarters(near[y][z] - dot(k4, o2));
                 if (lq == 0) s.far[dt][j] = far, s.near[dt][j] = less;
