@@ -3,9 +3,10 @@
 // Nothing is sorted.  Logits are compared as whole numbers in their order ("keys", 16 bits of a bf16 number, 32 of an fp32 one).  What
 // top-k and top-p keep is everything above one key and the first few words at it: the key is found by its digits, 11 bits at a time,
 // from counts (top-k) or sums of weights (top-p) of the words with each digit, in LDS.  The sums of top-p are whole multiples of
-// the smallest weight that matters, so that atomic additions give the same bits in any order; the sums that the draw goes by are in
+// 2^-61 of all weights' sum or less, so that atomic additions give the same bits in any order: each weight is rounded to one, and a sum of
+// V words is off by V 2^-62 of it at most (1e-15 for a list of 4096, 3e-14 for 131072 words).  The sums that the draw goes by are in
 // double, in a fixed order: a lane's words, a wave by halves, pieces of 64 lanes in the order of the vocabulary.  The weights are exp in
-// double, for the words in question alone: a border between two words is that of the definition but for some 1e-15.
+// double, for the words in question alone, off by some 3e-16 of themselves for each unit of their exponent.
 //
 // A workgroup takes a row.  Where few words can be chosen at all (a small vocabulary, top_k up to 2048, min_p alone), those are gathered
 // into a list in LDS, in the order of the vocabulary, and everything else happens there: a border that lies below enough of the largest
@@ -88,6 +89,10 @@ __device__ __forceinline__ double exp_of(double x, const double* table) {
     const double t = table[n & (kTable - 1)];
     return ldexp(fma(t, p, t), n >> 6);
 }
+
+// Weights as whole numbers: multiples of 2^-unit.  `sum` is all weights' sum, 1 at least (twice as much would do): below 2^62 altogether.
+__device__ __forceinline__ int unit_of(double sum) { return 61 - ((int)(__builtin_bit_cast(unsigned long long, sum) >> 52) - 1023); }
+__device__ __forceinline__ unsigned long long whole(double weight, int unit) { return (unsigned long long)__builtin_rint(ldexp(weight, unit)); }
 
 template <typename X>
 __device__ __forceinline__ X wave_total(X x) {
@@ -328,18 +333,21 @@ __device__ __forceinline__ void choose_listed(const SampleArgs& a, Lds<NT>& s, i
 #pragma unroll
     for (int e = 0; e < kEach; ++e) w[e] = key[e] ? weight(key[e]) : 0.0;
     if (set.top_p < 1.0) {
-        // (sums of a list's weights of at most 2^unit stay below 2^63)
-        constexpr int unit = 62 - (32 - __builtin_clz((uint32_t)(NT * kEach)));
+        double some = 0.0, sum;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) some += w[e];
+        block_upto<NT, double>(s, some, sum, turn);
+        const int unit = unit_of(sum);
         unsigned long long mine = 0, total;
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) mine += (unsigned long long)ldexp(w[e], unit);
+        for (int e = 0; e < kEach; ++e) mine += whole(w[e], unit);
         block_upto<NT, unsigned long long>(s, mine, total, turn);
         const double most = set.top_p > 0.0 ? __builtin_ceil(set.top_p * (double)total) : 1.0;
         unsigned long long need = most < 1.0 ? 1 : (unsigned long long)most;
         if (need > total) need = total;
-        Border b = find_border<NT, BITS>(s, s.weight, key, [&](int e) { return (unsigned long long)ldexp(w[e], unit); }, least, top, need, INT32_MAX, turn);
+        Border b = find_border<NT, BITS>(s, s.weight, key, [&](int e) { return whole(w[e], unit); }, least, top, need, INT32_MAX, turn);
         if (!b.all) {
-            const unsigned long long one = (unsigned long long)ldexp(weight(b.least), unit);
+            const unsigned long long one = whole(weight(b.least), unit);
             b.need = one > 0 ? (b.need + one - 1) / one : 1;
         }
         drop(b);
@@ -595,9 +603,21 @@ __global__ __launch_bounds__(NT, NT == 512 ? 4 : 1) void sample_kernel(SampleArg
             if (key == none) return 0.0;
             return exp_of(((double)logit_of(key, kBits) - z_top) * scale, s.table);
         };
-        // (sums of V weights of at most 2^unit stay below 2^63)
-        const int unit = 62 - (32 - __builtin_clz((uint32_t)a.V));
-        auto whole_weight = [&](uint32_t key) { return (unsigned long long)ldexp(weight(key), unit); };
+        int unit = 0;
+        if (top_p < 1.0) {  // (the sum of all weights in fp32, to some bits: only its size is asked for)
+            float mine = 0.0f, sum;
+            const float most = (float)z_top, slope = (float)(scale * 1.4426950408889634074);
+            row.spread(1, [&](int32_t, const float(&z)[VEC]) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float x = (z[e] - most) * slope;
+                    mine += z[e] == most ? 1.0f : x > -100.0f ? __builtin_amdgcn_exp2f(x) : 0.0f;  // (NaN: none)
+                }
+            });
+            block_upto<NT, float>(s, mine, sum, turn);
+            unit = unit_of((double)sum);
+        }
+        auto whole_weight = [&](uint32_t key) { return whole(weight(key), unit); };
 
         // kept: keys above `least`, and the first `ties` words of those at it (-1: all)
         uint32_t least = 0;

@@ -1,0 +1,43 @@
+"""The borders of the choice of tokens: the word that a limit stops at is that of the definition in 64 bits, in every way that a row
+is taken (a list of all words, a list gathered from a long row, a long row digit by digit)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import block_ref
+import paper_2503_01868_amd as hy
+
+from gpu_util import say
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def falling(V, dtype):
+    """One likely word and a tail of unlikely ones, the likelier first: the last word that is kept has the highest index."""
+    z = np.concatenate([[0.0], np.linspace(-13.0, -15.0, V - 1)]) if V > 1 else np.zeros(1)
+    return torch.from_numpy(z.astype(np.float32)).to(DTYPES[dtype]).cuda()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,V,top_k", [(1, 1000, None), (1, 4096, None), (1, 9001, 2000), (2, 9001, None), (2, 131072, None), (2, 131072, 100000),
+                                       (300, 2048, None), (300, 20001, None)])
+def test_top_p_stops_at_the_word_that_reaches_it(N, V, top_k, dtype):
+    """top_p next to a sum of weights on both sides, 3e-13 of it away.  The kernel's weights are off by 3 x 2^-53 of themselves for each
+    unit of their exponent, 15 x 3 x 1.2e-16 = 5e-15, and its sums by V 2^-62, 3e-14 at most."""
+    say("sample top_p N=%d V=%d %s" % (N, V, dtype))
+    row = falling(V, dtype)
+    kept = V if top_k is None else top_k
+    w = np.exp(row.double().cpu().numpy()[:kept]).astype(np.longdouble)
+    upto = np.cumsum(w)
+    z, u = row.expand(N, V), torch.ones(N, device="cuda")  # (u of 1: the last word that is kept)
+    for k in sorted({1, 2, 17, kept // 3, kept // 2, (2 * kept) // 3, kept - 2}):
+        p = float(upto[k - 1] / upto[-1])
+        for side, last in ((1 - 3e-13, k - 1), (1 + 3e-13, k)):
+            token, prob = hy.hyena_sample(z, u, 1.0, top_k, p * side)
+            assert token.tolist() == [last] * N, (k, side)
+            want = float(w[last] / upto[last])
+            assert (prob.double() - want).abs().max() <= 2.0 ** -23 * want
