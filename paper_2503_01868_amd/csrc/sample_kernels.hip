@@ -465,7 +465,8 @@ __global__ __launch_bounds__(NT, NT == 512 ? 4 : 1) void sample_kernel(SampleArg
                         low = ~block_max<NT>(s, ~low, turn);
                         from = find_border<NT, kBits>(s, s.count, first, [](int) { return 1u; }, low, top, (unsigned long long)need, 2, turn).least;
                     } else if (near) {
-                        const double z = logit_of(top, kBits), d = fmax(0.0, -T_n * log(min_p)), t = z - d - 1e-6 * (fabs(z) + d);
+                        // (a weight this near to min_p may round to it)
+                        const double z = logit_of(top, kBits), d = fmax(0.0, -T_n * log(min_p)) + T_n * 0x1p-50, t = z - d - 1e-6 * (fabs(z) + d);
                         const float f = (float)t;  // (the margin is more than this rounds)
                         from = f == f ? min(key_of(f, kBits), top) : top;
                     }

@@ -41,3 +41,22 @@ def test_top_p_stops_at_the_word_that_reaches_it(N, V, top_k, dtype):
             assert token.tolist() == [last] * N, (k, side)
             want = float(w[last] / upto[last])
             assert (prob.double() - want).abs().max() <= 2.0 ** -23 * want
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,V", [(3, 700), (3, 9001), (260, 2500)])
+def test_min_p_keeps_words_whose_weight_rounds_to_it(N, V, dtype):
+    """Weights that are 1 in 64 bits though their logits are below the largest: by a temperature that leaves nothing of the distance, or
+    logits next to each other."""
+    say("sample min_p N=%d V=%d %s" % (N, V, dtype))
+    rng = np.random.default_rng(V)
+    far = torch.from_numpy(rng.normal(size=V).astype(np.float32)).to(DTYPES[dtype]).cuda()
+    far[5] = -math.inf
+    near = torch.from_numpy(rng.choice([0.0, -1e-17, -3e-20, -1.0], size=V).astype(np.float32)).to(DTYPES[dtype]).cuda()
+    us = torch.from_numpy(rng.uniform(size=N).astype(np.float32)).cuda()
+    for z, t in ((far, 1e20), (far, math.inf), (near, 1.0)):
+        token, prob = hy.hyena_sample(z.expand(N, V), us, t, min_p=1.0)
+        row = z.double().cpu().numpy()
+        for n in range(min(N, 3)):
+            want, p = block_ref.sample(row, float(us[n]), t, min_p=1.0)
+            assert int(token[n]) == want and abs(float(prob[n]) - p) <= 2.0 ** -23 * p, (t, n)
