@@ -74,8 +74,8 @@ __device__ __forceinline__ float logit_of(uint32_t key, int bits) {
     return __uint_as_float(w & 0x80000000u ? w & 0x7fffffffu : ~(w | ((bits < 32 ? 1u << (32 - bits) : 1u) - 1u)));
 }
 
-// exp(x) for x <= 0: 2^(k / 64) from a table and a power series for what is left, |r| <= ln 2 / 128: the first term left out is below
-// 2^-53 / 10.
+// exp(x) for x <= 0: 2^(k / 64) from a table and a power series for what is left, |r| <= ln 2 / 128: the first term left out, r^6 / 720, is
+// below 2^-53 / 3.
 __device__ __forceinline__ double exp_of(double x, const double* table) {
     if (!(x > -708.0)) return 0.0;
     const double k = __builtin_rint(x * (kTable / 0.693147180559945309417));
@@ -297,6 +297,9 @@ __device__ __forceinline__ Border find_border(Lds<NT>& s, X* bins, const uint32_
 struct Settings {
     double scale, top_p, min_p, u;  // scale: 1 / temperature
     int32_t top_k;
+
+    // What the running sum has to pass.  (Sums are added in several orders, so that one may pass another by its rounding.)
+    __device__ __forceinline__ double want(double sum) const { return u < 1.0 ? u * sum : INFINITY; }
 };
 
 // The choice among the listed words: a lane has `each` of them, in the order of the vocabulary, as keys (0: none).
@@ -360,7 +363,7 @@ __device__ __forceinline__ void choose_listed(const SampleArgs& a, Lds<NT>& s, i
     }
     if (threadIdx.x == 0) s.at = INT32_MAX, s.last = -1;
     double here = block_upto<NT, double>(s, mine, sum, turn) - mine;
-    const double want = set.u * sum;
+    const double want = set.want(sum);
     int32_t hit = INT32_MAX, last = -1;
     double hit_weight = 0.0, last_weight = 0.0;
 #pragma unroll
@@ -766,7 +769,7 @@ __global__ __launch_bounds__(NT, NT == 512 ? 4 : 1) void sample_kernel(SampleArg
             double mine = 0.0;
             for (int j = 0; j < kOwn; ++j) mine += s.block[lane * kOwn + j];
             const double upto = wave_upto(mine);
-            const double sum = of_lane(upto, kWave - 1), want = u * sum;
+            const double sum = of_lane(upto, kWave - 1), want = set.want(sum);
             // the first run up to which there is more than `want`, else the last one that has something
             double before = upto - mine;
             int32_t run = -1, last = -1;

@@ -60,3 +60,18 @@ def test_min_p_keeps_words_whose_weight_rounds_to_it(N, V, dtype):
         for n in range(min(N, 3)):
             want, p = block_ref.sample(row, float(us[n]), t, min_p=1.0)
             assert int(token[n]) == want and abs(float(prob[n]) - p) <= 2.0 ** -23 * p, (t, n)
+
+
+@pytest.mark.parametrize("N,V", [(64, 700), (64, 4000), (64, 9001), (8, 131072), (300, 2000), (300, 20001)])
+@pytest.mark.parametrize("top_k", [None, 300])
+def test_a_u_of_one_takes_the_last_word_that_is_kept(top_k, N, V):
+    """Whatever the sums round to: of rows whose last words are all unlikely."""
+    say("sample u = 1 N=%d V=%d" % (N, V))
+    z = torch.randn(N, V, generator=torch.Generator(device="cuda").manual_seed(V), device="cuda") * 2.5
+    if top_k is None:
+        z[:, -3:] = -60.0
+        last = torch.full((N,), V - 1, device="cuda")
+    else:
+        last = torch.sort(z, dim=1, descending=True, stable=True).indices[:, :top_k].amax(1)
+    for u in (1.0, 2.0, math.inf):
+        assert torch.equal(hy.hyena_sample(z, torch.full((N,), u, device="cuda"), 1.0, top_k)[0], last), u
