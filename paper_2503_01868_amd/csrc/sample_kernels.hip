@@ -77,7 +77,7 @@ __device__ __forceinline__ float logit_of(uint32_t key, int bits) {
 // exp(x) for x <= 0: 2^(k / 64) from a table and a power series for what is left, |r| <= ln 2 / 128: the first term left out, r^6 / 720, is
 // below 2^-53 / 3.
 __device__ __forceinline__ double exp_of(double x, const double* table) {
-    if (!(x > -708.0)) return 0.0;
+    if (!(x > -746.0)) return 0.0;  // (the smallest number is exp(-744.4))
     const double k = __builtin_rint(x * (kTable / 0.693147180559945309417));
     double r = fma(k, -0.693147180559945309417 / kTable, x);
     r = fma(k, -2.3190468138462995584e-17 / kTable, r);  // ln 2 behind its 53 bits

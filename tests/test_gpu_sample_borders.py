@@ -75,3 +75,17 @@ def test_a_u_of_one_takes_the_last_word_that_is_kept(top_k, N, V):
         last = torch.sort(z, dim=1, descending=True, stable=True).indices[:, :top_k].amax(1)
     for u in (1.0, 2.0, math.inf):
         assert torch.equal(hy.hyena_sample(z, torch.full((N,), u, device="cuda"), 1.0, top_k)[0], last), u
+
+
+@pytest.mark.parametrize("N,V", [(3, 700), (3, 9001), (260, 2500)])
+def test_weights_below_the_smallest_normal_number_are_weights(N, V):
+    """exp(-744) is 1e-323 in 64 bits: a u of zero takes the first word that has any weight, and a u of one the last."""
+    say("sample smallest weights N=%d V=%d" % (N, V))
+    z = torch.linspace(-50.0, 0.0, V, device="cuda")
+    for far, there in ((-720.0, True), (-744.0, True), (-750.0, False), (-1e5, False)):
+        z[0], z[-1] = far, far
+        row = z.double().cpu().numpy()
+        token, prob = hy.hyena_sample(z.expand(N, V), torch.zeros(N, device="cuda"))
+        assert block_ref.sample(row, 0.0)[0] == (0 if there else 1) and (token == (0 if there else 1)).all(), far
+        token, prob = hy.hyena_sample(z.expand(N, V), torch.ones(N, device="cuda"))
+        assert (token == (V - 1 if there else V - 2)).all(), far
