@@ -65,7 +65,7 @@ def _la_sizes(q, k, v, g, dims: int):
         raise ValueError("q and k must be %sheads, dk], v %sH, dv] and g %sH] tensors" % (lead, lead, lead))
     H, dv = v.shape[-2:]
     heads, dk = q.shape[-2:]
-    if dk < 1 or dv < 1 or (heads < 1 and H > 0) or (H % heads if heads else H) != 0:
+    if dk < 1 or dv < 1 or (heads == 0) != (H == 0) or (heads and H % heads != 0):
         raise ValueError("the heads of q and k must divide those of v, each at least one number wide")
     at = v.shape[:-2]
     _like("q", q, at + (heads, dk), v, dense=False)
@@ -74,7 +74,7 @@ def _la_sizes(q, k, v, g, dims: int):
     for name, t in (("q", q), ("k", k), ("v", v), ("g", g)):
         if t.shape[-1] > 1 and t.stride(-1) != 1 and t.numel():
             raise ValueError("%s must have contiguous channels" % name)
-    return at, H, max(1, H // heads) if heads else 1, dk, dv, _dtype_code(v)
+    return at, H, H // heads if heads else 1, dk, dv, _dtype_code(v)
 
 
 def _la_state(name: str, t, B, H, dk, dv, ref):
