@@ -538,8 +538,8 @@ int64_t hyena_la_marks_bytes(int64_t B, int64_t L, int64_t H, int32_t group, int
  *     M[b,t,h] = scale q[b,t,h']^T dy[b,t,h] + a[b,t+1,h] M[b,t+1,h]      (+ dstate_out[b,h] at the last step):
  *     dq = scale dy S^T,  dk = v M^T  (each summed over the heads that share a row),  dv = k M,
  *     dg[b,t,h] = a[b,t,h] <S[b,t-1,h], M[b,t,h]>,   dstate_in[b,h] = a[b,0,h] M[b,0,h]   (NULL: not wanted)
- * (dg is made of sums over a chunk's pairs of steps, of which those that do not reach over step t cancel: it is as exact as fp32 makes
- * the largest of them, whatever it is itself)
+ * (dg is made of sums over a chunk's pairs of different steps, of which those that do not reach over step t cancel: it is as exact as
+ * fp32 makes the largest of them, whatever it is itself)
  * dq, dk: dense [B,L,H/group,dk], dv: dense [B,L,H,dv], dg: dense [B,L,H], of `dtype`; fp32 inside, with bf16 calls' products
  * rounded as in the forward call; sums in a fixed order, one rounding per stored element.  marks: what the forward call wrote
  * for the same inputs, or NULL: the states are computed again, from state_in (which is not looked at otherwise).  strides: as

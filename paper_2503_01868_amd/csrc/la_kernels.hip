@@ -744,7 +744,8 @@ struct BwdLds {
     // the state in front of the chunk and the gradient of that behind it, turned; fp32: one after the other in one place
     static constexpr bool kTwo = T::kBytes == 2;
     Elem<T> q[C * PK], k[C * PK], v[C * kPitch<T, DV>], dy[C * kPitch<T, DV>];
-    Elem<T> a[C * kPitch<T, C>], e[C * kPitch<T, C>];  // A and its gradient's part for q and k
+    Elem<T> a[C * kPitch<T, C>], e[C * kPitch<T, C>];  // A and its gradient's part for q and k, this below its diagonal
+    float self[C];                                     // and on it
     Elem<T> s[DV * PK], m[kTwo ? DV * PK : 1];
     float near[DK / 16][C], far[DK / 16][C];  // shares of the log decays' gradients
     float both[NW];                           // <S, M>
@@ -776,7 +777,8 @@ __device__ __forceinline__ float dot(const f32x4_t& a, const f32x4_t& b) { retur
 
 // For every chunk, from what lies in LDS and M in registers: A and E below the diagonal; dv = to_end k M + A^T dy;
 // dq = from_start scale dy S^T + E k; dk = to_end v M^T + E^T q; and M itself.  dg needs no products of its own: the pairs of steps on both
-// sides of a decay are what q . dq and k . dk add up to on both sides of it.  160 KB of LDS leave room for one workgroup of 8 waves on a
+// sides of a decay are what q . dq and k . dk add up to on both sides of it, but for what a step says to itself (E's diagonal, kept apart: it
+// reaches over no decay, and would leave its rounding where the decays leave little).  160 KB of LDS leave room for one workgroup of 8 waves on a
 // compute unit: vector instructions 41% busy, LDS 38%, matrix cores 14%.  dq and dk of heads that share q and k go to shares in fp32 and are
 // summed afterwards in a fixed order (32768 steps, 16 heads of 64 x 128 by four: 25 us each).
 template <typename T, int DK, int DV, bool SHARES>
@@ -874,12 +876,13 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
         }
 #pragma unroll
         for (int y = 0; y < NW; ++y) both += (double)s.both[y];
-        const double upto = wave_upto(far);
+        double before = __shfl_up(wave_upto(far), 1, kWave);  // (not the sum with its own less its own, which may be all there is)
+        if (lane == 0) before = 0.0;
         // (from behind: what is not finite stays in front of itself)
         const int turn = kWave - 1 - lane;
         const double from = __shfl(wave_upto((double)__shfl(near, turn, kWave)), turn, kWave);
         const int64_t t = done * C + lane;
-        if (lane < steps(done)) give_decay(t, g_now < kForgets ? 0.0f : (float)(from + (upto - far) + both));
+        if (lane < steps(done)) give_decay(t, g_now < kForgets ? 0.0f : (float)(from + before + both));
     };
     load(last - 1);
     for (int64_t x = last - 1; x >= first; --x) {
@@ -996,6 +999,10 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
                 p[r] = in ? p[r] * first * half : 0.0f;
                 e[r] = in ? e[r] * first * half : 0.0f;
             }
+            if (it == jt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (j0 + r == i) s.self[i] = e[r], e[r] = 0.0f;
             put4(s.a + i * PA + j0, p);
             put4(s.e + i * PA + j0, e);
         }
@@ -1074,6 +1081,7 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
                 for (int kb = 0; kb < KB; ++kb)
                     if (kb <= it / 2) multiply(o, fk[kb], row_frag<PA>(s.e, i, 32 * kb, lq));
                 near[y][z] = dot(four<T>(s.q + i * PK + 16 * dt + 4 * lq), o);
+                o += s.self[i] * four<T>(s.k + i * PK + 16 * dt + 4 * lq);
                 if (i < n) give_four(a.dq, t, i, 16 * dt + 4 * lq, o);
                 __builtin_amdgcn_sched_barrier(0);  // (blocks side by side need more registers than there are)
             }
@@ -1110,7 +1118,7 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
                 const f32x4_t k4 = four<T>(s.k + j * PK + 16 * dt + 4 * lq);
                 const float far = over_quarters(dot(k4, o)), less = over_quarters(near[y][z] - dot(k4, o2));
                 if (lq == 0) s.far[dt][j] = far, s.near[dt][j] = less;
-                o += o2;
+                o += o2 + s.self[j] * four<T>(s.q + j * PK + 16 * dt + 4 * lq);
                 if (j < n) give_four(a.dk, t, j, 16 * dt + 4 * lq, o);
                 __builtin_amdgcn_sched_barrier(0);
             }
