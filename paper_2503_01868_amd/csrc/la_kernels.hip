@@ -21,8 +21,8 @@
 // 4 waves of 32 columns, rows 32 bytes further apart in LDS (more conflicts), two blocks of 16 rows at once, 2 chunks a segment.
 //
 // A product mixes rows, and a zero times an infinity is none: a chunk that holds anything not finite, or so large that a product on the
-// way could become so, or decays far above one, or that meets a state with such a number, is taken a row at a time, by the formulas as they
-// stand.  (NaN in a state need not be looked for: products keep it in its row and column.)
+// way could become so, or decays far above one, or that meets a state with so large a number, is taken a row at a time, by the formulas as
+// they stand.  (Infinities and NaN in a state need not be looked for: products keep them in their row and column.)
 #include <string.h>
 
 #include <cmath>
@@ -404,12 +404,19 @@ struct State {
             clear();  // (of infinities, too)
         }
     }
-    // The largest magnitude that is not NaN.
-    __device__ __forceinline__ float largest() const {
+    // Whether a number of it is too large for products (not an infinity or NaN).
+    __device__ __forceinline__ bool large() const {
         float most = 0.0f;
 #pragma unroll
         for (int i = 0; i < DT; ++i) most = larger(larger(most, s[i][0], s[i][1]), s[i][2], s[i][3]);
-        return most;
+        if (__builtin_amdgcn_ballot_w64(most >= kMostState) == 0) return false;
+        const uint32_t from = __float_as_uint(kMostState), all = __float_as_uint(INFINITY) - from;
+        uint32_t least = all;  // how far above the limit; numbers below it are far above infinity
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) least = min(least, (__float_as_uint(s[i][r]) & 0x7fffffffu) - from);
+        return least < all;
     }
     __device__ __forceinline__ void decay_step(float half) {
 #pragma unroll
@@ -613,7 +620,7 @@ __global__ __launch_bounds__(DV * 4, T::kBytes == 2 && DV == 128 ? 4 : 2) void l
         fine &= next_q.put(s.q, a.most, a.q, qp + t * a.q.step, n, 0);
         fine &= next_v.put(s.v, a.most, a.v, vp + t * a.v.step, n, c0);
         if (w == 0) fine &= make_decays<C>(s.d, lane < n ? unpacked<T>(next_g) : 0.0f, lane);
-        fine &= S.largest() < kMostState;
+        fine &= !S.large();
         const bool at_once = !__syncthreads_or(!fine);
         if (x + 1 < last) load(x + 1);
         if (!at_once) {
@@ -904,16 +911,18 @@ __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {
         }
         g_now = lane < n ? unpacked<T>(next_g) : 0.0f;
         if (w == 0) fine &= make_decays<C>(s.d, g_now, lane);
-        float both = 0.0f, most = M.largest();  // <S, M>
+        float both = 0.0f;  // <S, M>
+        {
+            State<DT> S;
 #pragma unroll
-        for (int i = 0; i < DT; ++i) {
-            float f[4];
-            Pack<T, 4>::unpack(next_s[i], f);
+            for (int i = 0; i < DT; ++i) {
+                float f[4];
+                Pack<T, 4>::unpack(next_s[i], f);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) both = fmaf(f[r], M.s[i][r], both);
-            most = larger(larger(most, f[0], f[1]), f[2], f[3]);
+                for (int r = 0; r < 4; ++r) S.s[i][r] = f[r], both = fmaf(f[r], M.s[i][r], both);
+            }
+            fine &= !M.large() && !S.large();
         }
-        fine &= most < kMostState;
         both = wave_upto(both);
         const bool at_once = !__syncthreads_or(!fine);
         if (lane == kWave - 1) s.both[w] = scaled(both, s.d.whole);

@@ -169,3 +169,30 @@ def test_large_numbers_leave_what_is_left_of_them(dtype):
     ref, size = block_ref.la_grads(wide(dy), *w, 1, 1.0), block_ref.la_grads(abs(wide(dy)), *a, 1, 1.0)
     for name, x, r, z in zip(("dq", "dk", "dv", "dg"), grads, ref, size):
         close(x, r, z, dtype, name, L, extra=pairs(q, k, size) if name == "dg" else 0.0, least=least)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_numbers_beside_infinities(dtype):
+    """Numbers of 2^100 in columns of a state (rows of its gradient) where others hold an infinity and NaN."""
+    L, decay = 150, -0.9
+    q, k, v, g, dy, state, dstate = make(5, 1, L, 1, 24, 40, dtype, decay)
+    state[0, 0, :, 8] *= 2.0 ** 100
+    dstate[0, 0, 9] *= 2.0 ** 100
+    w = [wide(x) for x in (q, k, v, g)]
+    a = [abs(x) for x in w[:3]] + w[3:]
+    ry, rs = block_ref.la(*w, 1, 0.5, wide(state))
+    ay, as_ = block_ref.la(*a, 1, 0.5, abs(wide(state)))
+    ref = block_ref.la_grads(wide(dy), *w, 1, 0.5, wide(state), wide(dstate))
+    size = block_ref.la_grads(abs(wide(dy)), *a, 1, 0.5, abs(wide(state)), abs(wide(dstate)))
+    state[0, 0, 3, 5], state[0, 0, 4, 6] = float("inf"), float("nan")
+    dstate[0, 0, 7, 11], dstate[0, 0, 8, 12] = -float("inf"), float("nan")
+    ry[..., [5, 6]], rs[0, 0, 3, 5], rs[0, 0, 4, 6] = np.nan, np.nan, np.nan
+    y, s, marks = hy.hyena_la_fwd_carry(q, k, v, g, 0.5, state_in=state, want_marks=True)
+    close(y, ry, ay, dtype, "y", L)
+    close(s, rs, as_, "f32", "state", L)
+    grads = hy.hyena_la_bwd(dy, q, k, v, g, 0.5, marks=marks, dstate_out=dstate, want_dstate=True)
+    for name, x, r, z, at in (("dq", grads[0], ref[0], size[0], [3, 4]), ("dk", grads[1], ref[1], size[1], [7, 8]), ("dv", grads[2], ref[2], size[2], [11, 12])):
+        r = r.copy()
+        r[..., at] = np.nan
+        close(x, r, z, dtype, name, L)
+        assert not np.isfinite(wide(x)[..., at]).any(), name
