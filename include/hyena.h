@@ -574,7 +574,8 @@ hy_status hyena_la_step(const void *q, const void *k, const void *v, const void 
  * value = y * y_scale: of u, so that the numbers do not depend on how rstd is rounded.  A row whose top is below 2^-100 is held
  * as zeros with a scale of zero.  An element of u that is not finite takes no part in top and is held as NaN (and an infinity of
  * h makes every finite element of its row zero, as rstd is zero).
- * Sums are fp32, in a fixed order.  Pointers may begin at any element of theirs.  D >= 1 (HY_ERR_SHAPE), up to 2^31 - 1
+ * Sums are fp32, in a fixed order (a row whose sum of squares passes fp32's range has an rstd of zero, as one that holds an
+ * infinity).  Pointers may begin at any element of theirs.  D >= 1 (HY_ERR_SHAPE), up to 2^31 - 1
  * (HY_ERR_UNSUPPORTED).
  */
 hy_status hyena_rmsnorm_fwd(const void *x, const void *residual, const void *w, void *y, float *y_scale, void *h, float *rstd,

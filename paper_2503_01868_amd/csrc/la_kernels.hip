@@ -14,15 +14,20 @@
 // scan over the segments' ends, and the walk itself.  The state's products take the factor of k or q as three bf16 parts, so that states
 // are sums of fp32 products in bf16 calls too; what is rounded to bf16 is A and the copies of S that are multiplied.
 //
-// Measured (MI355X, 8192 steps x 32 heads of 128 x 128, bf16): ends 43 us, scan 12, walk 88 (112 with marks), gradients' ends 43, backward
-// walk 220.  The bytes of the walk are 268 MB, 48 us; what bounds it is issue: vector instructions 55% busy, LDS 50%, matrix cores 24%, of
-// waves that do the same phase between barriers.  On the way: loads ahead of a chunk that waited for branches or for spilled
-// addresses cost half of a chunk's time (162 -> 90 us), places in vector registers spilled (backward 406 -> 228).  Tried without gain:
-// 4 waves of 32 columns, rows 32 bytes further apart in LDS (more conflicts), two blocks of 16 rows at once, 2 chunks a segment.
+// Measured (MI355X, 8192 steps x 32 heads of 128 x 128, bf16): ends 43 us, scan 12, walk 88 (110-120 with marks), gradients' ends 44, backward
+// walk 235.  The bytes of the walk are 268 MB, 48 us; what bounds it is issue: vector instructions 58% busy, LDS 50%, matrix cores 23%, of
+// waves that do the same phase between barriers; 42% of LDS's cycles are bank conflicts (rows 272 bytes apart begin 4 banks after one
+// another, and a turned read takes 8 banks from each of four rows).  On the way: loads ahead of a chunk that waited for branches or for spilled
+// addresses cost half of a chunk's time (162 -> 90 us), places in vector registers spilled (backward 406 -> 228).  The walk with marks still
+// spills 15 registers (15 of the 216 MB it writes).  Tried without gain: 4 waves of 32 columns, rows 32 bytes further apart in LDS (more
+// conflicts), two blocks of 16 rows at once, 2 chunks a segment.  Roots of factors instead of factors, large states looked for and E's diagonal
+// apart took the backward walk from 222 to 235 us and the others 1-3% up.
 //
 // A product mixes rows, and a zero times an infinity is none: a chunk that holds anything not finite, or so large that a product on the
 // way could become so, or decays far above one, or that meets a state with so large a number, is taken a row at a time, by the formulas as
-// they stand.  (Infinities and NaN in a state need not be looked for: products keep them in their row and column.)
+// they stand.  (Infinities and NaN in a state need not be looked for: products keep them in their row and column.)  The backward pass makes
+// the states of such a chunk again from its mark for every step, a number of updates that grows with the square of the chunk: where all chunks
+// are of this kind, 8192 x 32 heads of 128 take 4.1 ms forward and 107 ms backward.
 #include <string.h>
 
 #include <cmath>
@@ -786,7 +791,7 @@ __device__ __forceinline__ float dot(const f32x4_t& a, const f32x4_t& b) { retur
 // dq = from_start scale dy S^T + E k; dk = to_end v M^T + E^T q; and M itself.  dg needs no products of its own: the pairs of steps on both
 // sides of a decay are what q . dq and k . dk add up to on both sides of it, but for what a step says to itself (E's diagonal, kept apart: it
 // reaches over no decay, and would leave its rounding where the decays leave little).  160 KB of LDS leave room for one workgroup of 8 waves on a
-// compute unit: vector instructions 41% busy, LDS 38%, matrix cores 14%.  dq and dk of heads that share q and k go to shares in fp32 and are
+// compute unit: vector instructions 43% busy, LDS 37% (of which 42% are conflicts), matrix cores 13%.  dq and dk of heads that share q and k go to shares in fp32 and are
 // summed afterwards in a fixed order (32768 steps, 16 heads of 64 x 128 by four: 25 us each).
 template <typename T, int DK, int DV, bool SHARES>
 __global__ __launch_bounds__(DV * 4, 2) void la_bwd_kernel(LaArgs a) {

@@ -4,8 +4,8 @@
 // Every element is read once and written once: the bytes are what it costs.  A row stays in the registers of the lanes that share
 // it (a wave, 4 waves or 16: TPR lanes with N pieces of 16 bytes each) between its sum and its output; rows that do not fit are
 // read again, from the sum just written where there is one.  Sums run over a lane's elements, the lanes of a wave by halves, and the
-// waves in their order, whatever the timing.  8192 rows of 4096 bf16 numbers with the residual (MI355X): forward 49-52 us, 8-bit output 41-45
-// (268 and 235 MB; a large copy moves 5.6 TB/s), gradients 44 and 4 for the sum of dw's shares.
+// waves in their order, whatever the timing.  8192 rows of 4096 bf16 numbers with the residual (MI355X): forward 46-54 us, 8-bit output 45-49
+// (268 and 235 MB; a large copy moves 5.6 TB/s), gradients 41-43 and 4 for the sum of dw's shares.
 #include <type_traits>
 
 #include "hy_common.hpp"

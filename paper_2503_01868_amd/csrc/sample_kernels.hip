@@ -8,14 +8,15 @@
 // double, in a fixed order: a lane's words, a wave by halves, pieces of 64 lanes in the order of the vocabulary.  The weights are exp in
 // double, for the words in question alone, off by some 3e-16 of themselves for each unit of their exponent.
 //
-// A workgroup takes a row.  Where few words can be chosen at all (a small vocabulary, top_k up to 2048, min_p alone), those are gathered
-// into a list in LDS, in the order of the vocabulary, and everything else happens there: a border that lies below enough of the largest
-// logits is taken from every fourth piece of the row, and one pass over the row gathers what is above it.  Otherwise the row is read
-// again for every digit.
+// A workgroup takes a row.  Where few words can be chosen at all (a small vocabulary, min_p alone, a top_k up to half of a list: 2048, or 1024 of
+// more rows than compute units), those are gathered into a list in LDS, in the order of the vocabulary, and everything else happens there: a
+// border that lies below enough of the largest logits is taken from every fourth piece of the row, and one pass over the row gathers what
+// is above it.  Otherwise the row is read again, a piece at a time: for every digit, for words at the border, for the sums of the draw.
 //
-// Measured (MI355X): 512 rows of 131072 fp32 words 75 us, of which reading them once and a quarter is 60 (read again for every digit: 495);
-// 64 rows of 65536 bf16 words 32 us on 64 compute units: 2 for the settings, 2 for the border's pieces, 6 for the gathering, 3 and 5 for the
-// borders of top-k and top-p, and the launch (114); one row of 512 words 9 us, half of it in the two borders (22).
+// Measured (MI355X): 512 rows of 131072 fp32 words 85-88 us, of which reading them once and a quarter is 60; where they are read again, 551 us with
+// top-p alone and 204 with a temperature alone; the largest logit alone 68.  64 rows of 65536 bf16 words 32 us on 64 compute units: 2 for the
+// settings, 2 for the border's pieces, 6 for the gathering, 3 and 5 for the borders of top-k and top-p, and the launch (114 where they were read
+// again); with top-p alone 128.  One row of 512 words 9 us, half of it in the two borders (22).
 #include <type_traits>
 
 #include "hy_common.hpp"
